@@ -331,7 +331,8 @@ ripple_status ripple_get_stats(ripple_ctx* ctx, ripple_stats* out);
  * batches are launched kernel by kernel instead of as a captured graph. */
 ripple_status ripple_set_timing(ripple_ctx* ctx, int32_t on);
 
-/* Text of the last error on ctx (or of the last failed ripple_create if ctx is NULL). */
+/* Text of the last error on ctx (if ctx is NULL, of this thread's last failed call without a context: ripple_create and
+ * the calls of requests). */
 const char* ripple_last_error(ripple_ctx* ctx);
 
 void ripple_destroy(ripple_ctx* ctx);
@@ -355,6 +356,119 @@ ripple_status ripple_probe_reduction_rate(int32_t device, int64_t n_rows, int32_
  * there, from L2 and DRAM otherwise.  Allocates and frees its own scratch on `device` (-1: current). */
 ripple_status ripple_probe_gather_rate(int32_t device, int64_t n_rows, int32_t row_floats,
                                        int64_t n_gathers, float* ms_out);
+
+/* ---- Requests ------------------------------------------------------------------------------------------
+ * Request-based inference (Sec. 2.2): what a serving process runs on the cached rows of the vertices that a
+ * request names.  These calls belong to no context: they read and write the caller's device memory, on the
+ * caller's stream, and return once their kernels are launched.  Nothing is allocated, nothing synchronised, so
+ * they can be captured into a CUDA graph.  Rows that come out of a context (ripple_get_embeddings) are borrowed: the
+ * caller orders these calls and the context's.  All pointers are DEVICE unless marked HOST; matrices are row-major with a
+ * leading dimension in elements (inputs: any >= 0, outputs: >= width).  Text of an error: ripple_last_error(NULL).
+ *
+ * ids: NULL, or for every row of the call the row of the table that it reads.  An id outside the table (a negative
+ * one marks a padding row) leaves that row of every output as it was. */
+typedef enum { RIPPLE_TYPE_F32 = 0, RIPPLE_TYPE_BF16 = 1, RIPPLE_TYPE_F16 = 2 } ripple_type;
+typedef enum { RIPPLE_NORM_NONE = 0, RIPPLE_NORM_LAYER = 1, RIPPLE_NORM_RMS = 2 } ripple_norm_kind;
+typedef enum { RIPPLE_GATE_IDENTITY = 0, RIPPLE_GATE_SIGMOID = 1, RIPPLE_GATE_SILU = 2, RIPPLE_GATE_TANH = 3 } ripple_gate_act;
+
+/* LAYER: (v - mean) / sqrt(mean((v - mean)^2) + eps) * weight + bias;  RMS: v / sqrt(mean(v^2) + eps) * weight + bias.
+ * weight, bias: fp32, one entry per column; NULL: ones, zeros. */
+typedef struct {
+    int32_t kind; /* ripple_norm_kind */
+    float eps;
+    const float* weight;
+    const float* bias;
+} ripple_norm;
+
+/* The norms after a block and before the next one, with the gate, the scale and the sum between them:
+ *   s = residual[ids] + scale * act(gate) * post(y),   n = pre(s).
+ * All of it in fp32, statistics of the unrounded rows; s and n are rounded once. */
+typedef struct {
+    int64_t rows;
+    int32_t width;            /* columns, 1 .. 16384                                                             */
+    int32_t type;             /* ripple_type of y, gate and normed                                               */
+    int32_t stream_type;      /* ripple_type of residual and stream: `type` or F32                               */
+    int32_t gate_act;         /* ripple_gate_act                                                                 */
+    const void* y;            /* the block's output, rows x width; NULL: s = residual[ids]                        */
+    int64_t ld_y;
+    const void* gate;         /* rows x gate_width; NULL: none                                                   */
+    int64_t ld_gate;
+    const void* residual;     /* residual_rows x width; NULL: zeros                                              */
+    int64_t ld_residual;
+    int64_t residual_rows;    /* without ids at least `rows`                                                     */
+    const int32_t* ids;       /* NULL: row i reads residual row i                                                */
+    const float* scale_vector;/* fp32, `width` entries, in place of `scale`; or NULL                             */
+    void* stream;             /* s, rows x width; NULL: not wanted.  s and n may take the place of y, or of        */
+    int64_t ld_stream;        /* residual (without ids), with the same leading dimension and type; other overlaps of */
+    void* normed;             /* outputs and inputs are refused.  n: NULL if pre is NONE                           */
+    int64_t ld_normed;
+    ripple_norm post, pre;
+    float scale;
+    int32_t gate_width;       /* 1 (one gate per row) or `width`                                                 */
+    int32_t device;           /* CUDA device ordinal of the pointers, or -1 for the current device               */
+    int32_t reserved;
+    void* cuda_stream;        /* cudaStream_t                                                                    */
+} ripple_norm_rows_args;
+
+/* rows = 0 is valid.  args: HOST. */
+ripple_status ripple_norm_rows(const ripple_norm_rows_args* args);
+
+/* A projection with the low-rank adapters of many requests beside it:
+ *   y_i = act(x_i W + bias + scale_a (x_i A_a) B_a),  x_i = x[ids_i] (ids NULL: x[i]),  a = slots_i.
+ * W (k x n) is laid out once by ripple_project_layout into a buffer of ripple_project_layout_bytes; the adapters of one
+ * projection, A_a (k x r) and B_a (r x n) with r <= max_rank, live in a bank of `slots` places that ripple_adapter_set fills.
+ * Layout and bank are the caller's device memory, 128-byte aligned.  Sums are fp32; x, W, A and B share one type (fp32 products
+ * are formed on the tensor cores from three bf16 parts per operand, all 24 bits), y has that type or F32. */
+#define RIPPLE_MAX_RANK 64
+#define RIPPLE_MAX_SLOTS 4096
+#define RIPPLE_MAX_PROJECT_K 8192
+#define RIPPLE_MAX_PROJECT_N 65536
+
+/* Bytes of the laid out W of a k x n projection; of a bank.  -1: an argument is out of range. */
+int64_t ripple_project_layout_bytes(int32_t type, int32_t k, int32_t n);
+int64_t ripple_adapter_bytes(int32_t type, int32_t k, int32_t n, int32_t slots, int32_t max_rank);
+
+/* Lays W out (leading dimension ld_w >= n).  Asynchronous on the stream. */
+ripple_status ripple_project_layout(int32_t type, int32_t k, int32_t n, const void* W, int64_t ld_w, void* layout,
+                                    int32_t device, void* cuda_stream);
+
+/* Fills slots first .. first + count - 1: A (count x k x rank) and B (count x rank x n), contiguous; scale: HOST, one per
+ * slot.  rank = 0 (A, B and scale are not read): the slots hold no adapter any more.  A bank is cleared as a whole, first = 0 and
+ * count = slots, before its first use.  Returns once the bank is written; an adapter with an entry or scale that is not finite
+ * is refused (INVALID_ARG; the slots then hold no adapter), because one tenant's product may share instructions
+ * with another's.  No call that reads the bank may be in flight on another stream. */
+ripple_status ripple_adapter_set(void* bank, int32_t type, int32_t k, int32_t n, int32_t slots, int32_t max_rank,
+                                 int32_t first, int32_t count, int32_t rank, const void* A, const void* B,
+                                 const float* scale, int32_t device, void* cuda_stream);
+
+typedef struct {
+    int64_t rows;
+    int32_t type;             /* ripple_type of x, W, A, B                                                       */
+    int32_t out_type;         /* ripple_type of y: `type` or F32                                                 */
+    int32_t k, n;             /* 1 .. RIPPLE_MAX_PROJECT_K, _N                                                    */
+    int32_t act;              /* ripple_act                                                                      */
+    int32_t n_slots, max_rank;/* of the bank                                                                     */
+    int32_t device;           /* CUDA device ordinal of the pointers, or -1 for the current device               */
+    const void* x;            /* x_rows x k                                                                      */
+    int64_t ld_x, x_rows;     /* without ids at least `rows` rows                                                */
+    const int32_t* ids;       /* NULL: row i reads row i of x                                                    */
+    const void* layout;       /* of W                                                                            */
+    const float* bias;        /* fp32, n entries; NULL: zeros                                                    */
+    const void* bank;         /* NULL: no adapters                                                               */
+    const int32_t* slots;     /* `rows` entries; one outside [0, n_slots), or of an empty slot: no adapter.       */
+                              /* Only with a bank                                                                */
+    void* y;                  /* rows x n, sharing no memory with any input                                      */
+    int64_t ld_y;
+    void* workspace;          /* ripple_project_workspace_bytes, 128-byte aligned; of this call alone until it   */
+    int64_t workspace_bytes;  /* has finished on the stream                                                      */
+    void* cuda_stream;        /* cudaStream_t                                                                    */
+} ripple_project_rows_args;
+
+/* Device scratch of a call (rows, type, k, n, bank and max_rank are read).  HOST */
+int64_t ripple_project_workspace_bytes(const ripple_project_rows_args* args);
+
+/* rows = 0 is valid.  args: HOST. */
+ripple_status ripple_project_rows(const ripple_project_rows_args* args);
 
 /* Library version string. */
 const char* ripple_version(void);

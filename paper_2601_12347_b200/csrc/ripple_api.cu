@@ -23,6 +23,15 @@ static void set_err(Ctx* c, const char* fmt, ...) {
     va_end(ap);
 }
 
+namespace rp {
+void note_error(const char* fmt, ...) {   // of a call without a context
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_create_err, sizeof g_create_err, fmt, ap);
+    va_end(ap);
+}
+}  // namespace rp
+
 #define CK(call)                                                                              \
     do {                                                                                      \
         cudaError_t e_ = (call);                                                              \

@@ -34,6 +34,9 @@ EXPORTED = [
     "ripple_get_degrees", "ripple_recompute_full", "ripple_reserve_vertices",
     "ripple_export_graph_static", "ripple_set_timing", "ripple_probe_reduction_rate", "ripple_probe_gather_rate",
     "ripple_get_stats", "ripple_last_error", "ripple_destroy", "ripple_version",
+    # requests (serve.py)
+    "ripple_norm_rows", "ripple_project_layout_bytes", "ripple_adapter_bytes", "ripple_project_layout",
+    "ripple_adapter_set", "ripple_project_workspace_bytes", "ripple_project_rows",
 ]
 # partitioned execution (include/ripple_part.h); the first 18 return a status
 EXPORTED_PART = [
@@ -149,6 +152,18 @@ def load_library(path: Optional[str] = None):
     lib.ripple_reserve_vertices.argtypes = [vp, i64]
     for name in EXPORTED[:16]:
         getattr(lib, name).restype = i32
+    # requests: the argument structures are packed by serve.py
+    lib.ripple_norm_rows.argtypes = [vp]
+    lib.ripple_project_layout_bytes.argtypes = [i32, i32, i32]
+    lib.ripple_adapter_bytes.argtypes = [i32, i32, i32, i32, i32]
+    lib.ripple_project_layout.argtypes = [i32, i32, i32, vp, i64, vp, i32, vp]
+    lib.ripple_adapter_set.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, i32, vp]
+    lib.ripple_project_workspace_bytes.argtypes = [vp]
+    lib.ripple_project_rows.argtypes = [vp]
+    for name in ("ripple_norm_rows", "ripple_project_layout", "ripple_adapter_set", "ripple_project_rows"):
+        getattr(lib, name).restype = i32
+    for name in ("ripple_project_layout_bytes", "ripple_adapter_bytes", "ripple_project_workspace_bytes"):
+        getattr(lib, name).restype = i64
     # partitioned execution
     lib.ripple_part_exports_get.argtypes = [vp, P(_PartExports)]
     lib.ripple_part_set_peer.argtypes = [vp, i32, P(_PartExports)]
@@ -421,6 +436,16 @@ class Ripple:
         ptr, cnt = ctypes.c_void_p(), ctypes.c_int64()
         self._check(self.lib.ripple_get_affected(self.h, layer, ctypes.byref(ptr), ctypes.byref(cnt)))
         return self._view(("A", layer), lambda: _DevArray(ptr.value, (self.n,), "<i4", owner=self._handle))[: cnt.value]
+
+    def answer(self, head, ids, slots=None, layer: Optional[int] = None):
+        """Request-based inference: what `head` (serve.RequestHead) makes of the rows `ids` (CUDA int32) of H^layer (default:
+        the last), each with the adapters of its slot.  Runs on the current stream of the context's device and does not wait for it; the
+        context's next call waits on the device until the rows have been read.  An id out of range leaves its row of the
+        result undefined.  While a graph is captured nothing is ordered: replay it between the context's calls."""
+        got = head(self.embeddings(self.L if layer is None else layer), ids, slots)
+        if not self._torch.cuda.is_current_stream_capturing():
+            self._stream.wait_stream(self._torch.cuda.current_stream(self._device))
+        return got
 
     def degrees(self):
         def make(which):
