@@ -470,6 +470,10 @@ int64_t ripple_project_workspace_bytes(const ripple_project_rows_args* args);
 /* rows = 0 is valid.  args: HOST. */
 ripple_status ripple_project_rows(const ripple_project_rows_args* args);
 
+/* Waits for the device and tells whether a bounded device-side wait of a call of requests gave up since the last query
+ * (TIMEOUT: the results of those calls are not to be used).  The calls themselves return before their kernels have run. */
+ripple_status ripple_request_status(int32_t device);
+
 /* Library version string. */
 const char* ripple_version(void);
 

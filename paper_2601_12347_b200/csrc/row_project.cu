@@ -1,6 +1,7 @@
 // A projection with the low-rank adapters of many requests beside it:
 //   y_i = act(x_i W + bias + scale_a (x_i A_a) B_a),  a = slots_i
 #include "requests.cuh"
+#include "tensor_core.cuh"
 
 #include <algorithm>
 
@@ -34,11 +35,6 @@ __host__ __device__ inline BankView bank_view(const void* bank, int size, int k,
     return {reinterpret_cast<const SlotInfo*>(p), p + bank_a_at(slots), p + bank_b_at(size, k, slots, max_rank), pj_up(max_rank, 16), pj_up(k, PJ_KC)};
 }
 
-// byte offset of 16-byte piece c (0..7) of row r inside a K-major tile with 128-byte rows, swizzled
-__host__ __device__ __forceinline__ uint32_t pj_swz(int r, int c) {
-    return (uint32_t)((r >> 3) * 1024 + (r & 7) * 128 + (((c ^ r) & 7) << 4));
-}
-
 // An fp32 value as three bf16 parts, 8 bits each: the first cut (rounded, values next to the largest would become
 // infinite), the others what is left, rounded; both remainders are exact.  An infinite value has no remainders.
 __device__ __forceinline__ void pj_parts_of(float x, __nv_bfloat16 (&h)[3]) {
@@ -58,7 +54,7 @@ __global__ void k_layout_weights(const T* W, int64_t ld, int k, int n, uint8_t* 
         const int col = (int)(i % PJ_COLS), c = (int)(i / PJ_COLS % 8);
         const int64_t chunk = i / (PJ_COLS * 8);
         const int kc = (int)(chunk % chunks), group = (int)(chunk / chunks), j = group * PJ_COLS + col;
-        uint8_t* to = out + chunk * parts * PJ_CHUNK + pj_swz(col, c);
+        uint8_t* to = out + chunk * parts * PJ_CHUNK + tc_swz(col, c);
         T v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -161,48 +157,470 @@ __global__ void k_shrink_rows(const __grid_constant__ ProjectParams p) {
     }
 }
 
-// the simplest form: a thread per output
-template <typename T>
-__global__ void k_project_simple(const __grid_constant__ ProjectParams p) {
-    pdl_enter();
-    const int j = blockIdx.y * 32 + (threadIdx.x & 31), i = blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (j >= p.n || i >= p.rows) return;
-    const int64_t from = row_of(p, i);
-    if (from < 0) return;
-    const T* const x = static_cast<const T*>(p.x) + from * p.ld_x;
-    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    float sum = 0.f;
-    for (int kk = 0; kk < p.k; ++kk) {
-        const uint8_t* at = p.layout + ((int64_t)(j / PJ_COLS) * p.chunks + kk / PJ_KC) * PARTS * PJ_CHUNK + pj_swz(j % PJ_COLS, kk % PJ_KC / 8) + 2 * (kk % 8);
-        float w;
-        if constexpr (PARTS == 3) {
-            w = 0.f;
-            for (int q = 2; q >= 0; --q) w += to_f32(*reinterpret_cast<const __nv_bfloat16*>(at + q * PJ_CHUNK));
-        } else {
-            w = to_f32(*reinterpret_cast<const T*>(at));
-        }
-        sum += to_f32(x[kk]) * w;
-    }
-    if (p.bias) sum += p.bias[j];
-    const int a = p.bank.info ? slot_of(p, i) : -1;
-    if (a >= 0) {
-        const T* const b = reinterpret_cast<const T*>(p.bank.b) + ((int64_t)a * p.n + j) * p.bank.r_pad;
-        float d = 0.f;
-        for (int r = 0; r < p.bank.info[a].rank; ++r) d += p.t[(int64_t)i * p.bank.r_pad + r] * to_f32(b[r]);
-        sum += d;
-    }
-    if (p.act == RIPPLE_ACT_RELU && sum < 0.f) sum = 0.f;
-    if (p.out_f32) static_cast<float*>(p.y)[(int64_t)i * p.ld_y + j] = sum;
-    else static_cast<T*>(p.y)[(int64_t)i * p.ld_y + j] = from_f32<T>(sum);
+// ---- the product on the tensor cores -------------------------------------------------------------------------------
+// Set where a bounded wait gave up; read and cleared by ripple_request_status.
+__device__ int g_request_timeout;
+
+constexpr int PJ_ROWS = 128;             // rows per tile: the lanes of the accumulator
+constexpr int PJ_LOADERS = 256;          // threads that fetch rows
+constexpr int PJ_EPI_WARPS = 8;          // two per quarter of the lanes
+constexpr int PJ_THREADS = PJ_LOADERS + 32 * PJ_EPI_WARPS + 64;   // and the warps that issue and that fetch weights
+constexpr int PJ_UNIT = 4;               // fp32: chunks (256 entries of K) whose large products share an accumulator
+constexpr uint32_t PJ_SPIN_LIMIT = 1u << 22;
+constexpr int PJ_STAGING = PJ_EPI_WARPS * 32 * 17 * 4;
+
+template <int TYPE, int BN> struct PjShape {
+    static constexpr int PARTS = TYPE == RIPPLE_TYPE_F32 ? 3 : 1;
+    static constexpr int X_PART = PJ_ROWS * 128, X_STAGE = PARTS * X_PART;
+    static constexpr int W_PART = BN * 128, W_STAGE = PARTS * W_PART;
+    static constexpr int STAGE = X_STAGE + W_STAGE;
+    static constexpr int STAGES = 200 * 1024 / STAGE < 8 ? 200 * 1024 / STAGE : 8;
+    static constexpr size_t BYTES = (size_t)STAGES * STAGE + PJ_STAGING + 1024;
+};
+
+// instruction descriptor: fp32 accumulators, both operands K-major, 128 rows, n columns
+__device__ __forceinline__ uint32_t pj_idesc(int type, int n) {
+    const uint32_t t = type == RIPPLE_TYPE_F16 ? 0u : 1u;
+    return (1u << 4) | (t << 7) | (t << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(PJ_ROWS >> 4) << 24);
 }
 
-template <typename T>
+__device__ __forceinline__ void pj_store8(void* to, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+
+template <typename T> __device__ __forceinline__ uint32_t pj_pair(float a, float b) {
+    Piece<T, 2> v;
+    v.v[0] = from_f32<T>(a), v.v[1] = from_f32<T>(b);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+
+// eight entries of a row of B transposed, as fp32
+__device__ __forceinline__ void pj_load8(float (&b)[8], const float* from) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(from) + i);
+        b[4 * i] = v.x, b[4 * i + 1] = v.y, b[4 * i + 2] = v.z, b[4 * i + 3] = v.w;
+    }
+}
+template <typename T> __device__ __forceinline__ void pj_load8(float (&b)[8], const T* from) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4*>(from));
+    const Piece<T, 8>& e = reinterpret_cast<const Piece<T, 8>&>(v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) b[k] = to_f32(e.v[k]);
+}
+
+// A persistent CTA takes tiles of 128 rows x BN output columns: lanes of the accumulator are rows, its columns output columns.
+//   loaders    fetch the rows by id, chunk by chunk of 64 entries, into the swizzled layout that the tensor core reads: 16-bit
+//              rows as asynchronous copies, fp32 rows (and rows that are not 16-byte aligned) through registers,
+//              fp32 entries as three bf16 parts
+//   one thread copies the weights' chunks, one issues the products
+//   epilogue   takes a finished accumulator while the next is being filled, adds t B_a by row, bias, activation, and writes
+// fp32: six products of parts (all but those below 2^-23); the large one of the first parts is handed over every 256 entries
+// and summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
+// Barriers, all waits bounded: full_x[s] (one arrival per loader warp), full_w[s] (bytes), empty[s] (the products that read
+// stage s), acc_full[b], acc_empty[b] (one arrival per epilogue warp).
+template <int TYPE, int BN>
+__global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_constant__ ProjectParams p) {
+    using T = typename Elem<TYPE>::T;
+    using S = PjShape<TYPE, BN>;
+    constexpr int PARTS = S::PARTS, STAGES = S::STAGES, NB = BN / 32;
+    constexpr uint32_t TMEM = 4 * BN < 32 ? 32 : 4 * BN;       // two accumulators and, fp32, two for the small products
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full_x[STAGES], full_w[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int s_fail;
+
+    const int tid = threadIdx.x, warp = __shfl_sync(FULL, tid >> 5, 0), lane = tid & 31;
+    const int col_tiles = (p.n + BN - 1) / BN, row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
+    const int64_t tiles = (int64_t)col_tiles * row_tiles;
+    const int my_tiles = (int)((tiles - blockIdx.x + gridDim.x - 1) / gridDim.x), chunks = p.chunks;
+    uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    auto tile_row = [&](int lt) { return (int)((blockIdx.x + (int64_t)lt * gridDim.x) / col_tiles) * PJ_ROWS; };
+    auto tile_col = [&](int lt) { return (int)((blockIdx.x + (int64_t)lt * gridDim.x) % col_tiles) * BN; };
+    auto tile_n = [&](int lt) { return min(BN, (p.n - tile_col(lt) + 15) & ~15); };
+
+    if (tid == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full_x[s], PJ_LOADERS / 32); mbar_init(&full_w[s], 1); mbar_init(&empty[s], 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], PJ_EPI_WARPS); }
+        mbar_init(&drained, 1);
+        s_fail = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(TMEM) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    pdl_enter();
+
+    if (warp < PJ_LOADERS / 32) {
+        // ---------------- rows ----------------
+        constexpr int RSTEP = PJ_LOADERS / 8, ITS = PJ_ROWS / RSTEP;
+        const int c = tid & 7, rb = tid >> 3;       // thread: piece c (8 entries) of the rows rb + RSTEP it
+        const uint32_t mine = smem_u32(ring) + tc_swz(rb, c);
+        const bool vec = (reinterpret_cast<uintptr_t>(p.x) & 15) == 0 && p.ld_x % (16 / (int)sizeof(T)) == 0;
+        const T *row[ITS], *next[ITS];              // null: nothing to read
+        auto aim = [&](int lt) {
+#pragma unroll
+            for (int it = 0; it < ITS; ++it) {
+                next[it] = nullptr;
+                if (lt >= my_tiles) continue;
+                const int i = tile_row(lt) + rb + RSTEP * it;
+                const int64_t from = i < p.rows ? row_of(p, i) : -1;
+                if (from >= 0) next[it] = static_cast<const T*>(p.x) + from * p.ld_x + c * 8;
+            }
+        };
+        bool ok = true;
+        int s = 0, g = 0;
+        uint32_t ph = 1;                            // (a fresh barrier counts as completed)
+        if (PARTS == 1 && vec) {
+            constexpr int LAG = STAGES - 2;         // chunks in flight
+            aim(0);
+            int told = 0;
+            for (int lt = 0; lt < my_tiles && ok; ++lt) {
+#pragma unroll
+                for (int it = 0; it < ITS; ++it) row[it] = next[it];
+                aim(lt + 1);
+                for (int kc = 0; kc < chunks; ++kc, ++g) {
+                    ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
+                    if (!ok) break;
+                    const int left = p.k - kc * PJ_KC - c * 8;
+                    const uint32_t bytes = left >= 8 ? 16u : left > 0 ? 2u * left : 0u;
+#pragma unroll
+                    for (int it = 0; it < ITS; ++it)
+                        if (row[it]) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                                                  ::"r"(mine + (uint32_t)(s * S::STAGE + it * (RSTEP * 128))), "l"(bytes ? row[it] + kc * PJ_KC : row[it]), "r"(bytes) : "memory");
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                    if (g >= LAG) {
+                        asm volatile("cp.async.wait_group %0;" ::"n"(LAG) : "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&full_x[told]);
+                        if (++told == STAGES) told = 0;
+                    }
+                    if (++s == STAGES) { s = 0; ph ^= 1; }
+                }
+            }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
+            if (lane == 0 && ok)
+                for (int d = 0; d < min(g, LAG); ++d) {
+                    mbar_arrive(&full_x[told]);
+                    if (++told == STAGES) told = 0;
+                }
+        } else {
+            T raw[ITS][8];
+            auto fetch = [&](int kc) {
+                const int left = p.k - kc * PJ_KC - c * 8;
+#pragma unroll
+                for (int it = 0; it < ITS; ++it) {
+                    const T* const from = row[it] + kc * PJ_KC;
+                    if (vec && left >= 8 && row[it]) {
+#pragma unroll
+                        for (int e = 0; e < 8; e += 16 / (int)sizeof(T))
+                            *reinterpret_cast<uint4*>(&raw[it][e]) = __ldg(reinterpret_cast<const uint4*>(from + e));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) raw[it][e] = row[it] && e < left ? from[e] : from_f32<T>(0.f);
+                    }
+                }
+            };
+            aim(0);
+            for (int lt = 0; lt < my_tiles && ok; ++lt) {
+#pragma unroll
+                for (int it = 0; it < ITS; ++it) row[it] = next[it];
+                if (lt == 0) fetch(0);
+                aim(lt + 1);
+                for (int kc = 0; kc < chunks; ++kc) {
+                    ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
+                    if (!ok) break;
+#pragma unroll
+                    for (int it = 0; it < ITS; ++it) {
+                        uint8_t* const to = ring + s * S::STAGE + it * (RSTEP * 128) + tc_swz(rb, c);
+                        if constexpr (PARTS == 3) {
+                            Piece<__nv_bfloat16, 8> part[3];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                __nv_bfloat16 h[3];
+                                pj_parts_of(raw[it][e], h);
+                                part[0].v[e] = h[0], part[1].v[e] = h[1], part[2].v[e] = h[2];
+                            }
+#pragma unroll
+                            for (int q = 0; q < 3; ++q) *reinterpret_cast<Piece<__nv_bfloat16, 8>*>(to + q * S::X_PART) = part[q];
+                        } else {
+                            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(&raw[it][0]);
+                        }
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&full_x[s]);
+                    if (++s == STAGES) { s = 0; ph ^= 1; }
+                    // what the next step stores is requested now: of this tile, or of the one after it
+                    if (kc + 1 < chunks) fetch(kc + 1);
+                    else {
+#pragma unroll
+                        for (int it = 0; it < ITS; ++it) row[it] = next[it];
+                        fetch(0);
+                    }
+                }
+            }
+        }
+        if (!ok) s_fail = 1;
+    } else if (warp < PJ_LOADERS / 32 + PJ_EPI_WARPS) {
+        // ---------------- epilogue ----------------
+        const int q = warp & 3, half = (warp - PJ_LOADERS / 32) >> 2;
+        const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16);
+        float* const staging = reinterpret_cast<float*>(ring + STAGES * S::STAGE) + (warp - PJ_LOADERS / 32) * (32 * 17);
+        const int out_size = p.out_f32 ? 4 : (int)sizeof(T);
+        const bool vec = (reinterpret_cast<uintptr_t>(p.y) & 31) == 0 && p.ld_y * out_size % 32 == 0;
+        const int units = PARTS == 3 ? (chunks + PJ_UNIT - 1) / PJ_UNIT : 1;
+        bool ok = true;
+        int sg = 0;
+        for (int lt = 0; lt < my_tiles && ok; ++lt) {
+            // thread: a row, and the 16-column blocks half, half + 2, ... of the tile
+            const int i = tile_row(lt) + 32 * q + lane, c0 = tile_col(lt), nt = tile_n(lt);
+            const bool live = i < p.rows && row_of(p, i) >= 0;
+            const int a = live && p.bank.info ? slot_of(p, i) : -1;
+            const int rank = a >= 0 ? p.bank.info[a].rank : 0;
+            const bool any = __any_sync(FULL, rank > 0);
+            const uint32_t rows_live = __ballot_sync(FULL, live);
+            // 16 finished sums of this row, from column `at` of y: plus t_i B_a, bias, activation, and out
+            auto finish = [&](float (&y)[16], int at) {
+                if (any) {
+                    const float* const ti = p.t + (int64_t)i * p.bank.r_pad;
+                    const T* const bt = reinterpret_cast<const T*>(p.bank.b) + ((int64_t)(a >= 0 ? a : 0) * p.n + at) * p.bank.r_pad;
+#pragma unroll 1
+                    for (int r = 0; r < rank; r += 8) {
+                        float t[8];
+                        pj_load8(t, ti + r);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            if (at + e >= p.n) continue;
+                            float w[8], d = 0.f;
+                            pj_load8(w, bt + e * p.bank.r_pad + r);
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) d += t[k] * w[k];
+                            y[e] += d;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    if (p.bias && at + e < p.n) y[e] += __ldg(p.bias + at + e);
+                    if (p.act == RIPPLE_ACT_RELU && y[e] < 0.f) y[e] = 0.f;
+                }
+                if (vec && at + 16 <= p.n) {
+                    if (live) {
+                        uint32_t v[8];
+                        if (p.out_f32) {
+                            float* const to = static_cast<float*>(p.y) + (int64_t)i * p.ld_y + at;
+#pragma unroll
+                            for (int e = 0; e < 16; e += 8) {
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) v[k] = __float_as_uint(y[e + k]);
+                                pj_store8(to + e, v);
+                            }
+                        } else if constexpr (PARTS == 1) {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) v[k] = pj_pair<T>(y[2 * k], y[2 * k + 1]);
+                            pj_store8(static_cast<T*>(p.y) + (int64_t)i * p.ld_y + at, v);
+                        }
+                    }
+                } else {
+                    // through shared memory: two rows of 16 columns per store
+                    __syncwarp();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) staging[lane * 17 + e] = y[e];
+                    __syncwarp();
+                    const int e = lane & 15;
+                    if (at + e < p.n) {
+#pragma unroll 4
+                        for (int r = lane >> 4; r < 32; r += 2) {
+                            if (!(rows_live >> r & 1)) continue;
+                            const int64_t to = (int64_t)(i - lane + r) * p.ld_y + at + e;
+                            const float v = staging[r * 17 + e];
+                            if (p.out_f32) static_cast<float*>(p.y)[to] = v;
+                            else static_cast<T*>(p.y)[to] = from_f32<T>(v);
+                        }
+                    }
+                }
+            };
+            constexpr int CARRY = PARTS == 3 ? NB : 1;
+            float sum[CARRY][16];              // fp32: of the units before the last
+            for (int u = 0; u < units && ok; ++u, ++sg) {
+                const int b = sg & 1;
+                const uint32_t large = lanes + (uint32_t)(b * BN), small = lanes + (uint32_t)(2 * BN + (lt & 1) * BN);
+                ok = __all_sync(FULL, mbar_wait_bounded(&acc_full[b], (sg >> 1) & 1, PJ_SPIN_LIMIT));
+                if (!ok) break;
+                tc_fence_after();
+                if (PARTS == 3 && u < units - 1) {
+#pragma unroll
+                    for (int j = 0; j < CARRY; ++j) {
+                        const int at = 16 * (2 * j + half);
+                        if (at >= nt) continue;
+                        uint32_t x[16];
+                        tc_load16(x, large + (uint32_t)at);
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) sum[j][e] = u ? sum[j][e] + __uint_as_float(x[e]) : __uint_as_float(x[e]);
+                    }
+                } else {
+#pragma unroll 1
+                    for (int j = 0; j < NB; ++j) {
+                        const int at = 16 * (2 * j + half);
+                        if (at >= nt) break;
+                        uint32_t x[16];
+                        float y[16];
+                        tc_load16(x, large + (uint32_t)at);
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) y[e] = __uint_as_float(x[e]);
+                        if constexpr (PARTS == 3) {
+                            if (u > 0) {
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) {
+                                    float before = sum[0][e];
+#pragma unroll
+                                    for (int k = 1; k < CARRY; ++k) before = k == j ? sum[k][e] : before;
+                                    y[e] += before;
+                                }
+                            }
+                            tc_load16(x, small + (uint32_t)at);
+                            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                            // (an infinite entry has no parts: its small products may be NaN)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) if (fabsf(y[e]) < INFINITY) y[e] += __uint_as_float(x[e]);
+                        }
+                        finish(y, c0 + at);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&acc_empty[b]);
+            }
+        }
+        if (!ok) s_fail = 1;
+    } else if (warp == PJ_LOADERS / 32 + PJ_EPI_WARPS) {
+        // ---------------- products ----------------
+        const bool lead = tc_elect();
+        const uint64_t d0 = tc_smem_desc(smem_u32(ring));
+        int s = 0, sg = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        for (int lt = 0; lt < my_tiles && ok; ++lt) {
+            const int nt = __shfl_sync(FULL, tile_n(lt), 0);
+            const uint32_t idesc = pj_idesc(TYPE, nt), small = tmem + (uint32_t)(2 * BN + (lt & 1) * BN);
+            uint32_t acc = 0;
+            int left = p.k, b = 0;
+            for (int kc = 0; kc < chunks; ++kc, left -= PJ_KC) {
+                const bool first = PARTS == 3 ? kc % PJ_UNIT == 0 : kc == 0;
+                if (first) {
+                    b = sg & 1;
+                    const int before = sg >> 1;
+                    ++sg;
+                    // the epilogue must have read this accumulator (and with it the small products of the tile before the last)
+                    if (before > 0) ok = __all_sync(FULL, mbar_wait_bounded(&acc_empty[b], (before - 1) & 1, PJ_SPIN_LIMIT));
+                    if (!ok) break;
+                    tc_fence_after();
+                    acc = tmem + (uint32_t)(b * BN);
+                }
+                ok = __all_sync(FULL, mbar_wait_bounded(&full_w[s], ph, PJ_SPIN_LIMIT) && mbar_wait_bounded(&full_x[s], ph, PJ_SPIN_LIMIT));
+                if (!ok) break;
+                fence_async_smem();      // the loaders' stores, for the tensor core (on the reader's side: loads in flight are not waited for)
+                tc_fence_after();
+                const uint64_t x = d0 + (uint64_t)((uint32_t)s * (S::STAGE >> 4)), w = x + (S::X_STAGE >> 4);
+                const bool last = PARTS == 3 ? kc % PJ_UNIT == PJ_UNIT - 1 || kc == chunks - 1 : kc == chunks - 1;
+                if (lead) {
+#pragma unroll
+                    for (int j = 0; j < PJ_KC / 16; ++j) {        // 16 entries = 32 bytes per instruction
+                        if (16 * j < left) {
+                            const uint64_t x1 = x + 2 * j, w1 = w + 2 * j;
+                            tc_mma_bf16(acc, x1, w1, idesc, !first || j != 0);
+                            if constexpr (PARTS == 3) {
+                                constexpr uint64_t XP = S::X_PART >> 4, WP = S::W_PART >> 4;
+                                tc_mma_bf16(small, x1, w1 + WP, idesc, (kc | j) != 0);
+                                tc_mma_bf16(small, x1 + XP, w1, idesc, 1u);
+                                tc_mma_bf16(small, x1 + XP, w1 + WP, idesc, 1u);
+                                tc_mma_bf16(small, x1, w1 + 2 * WP, idesc, 1u);
+                                tc_mma_bf16(small, x1 + 2 * XP, w1, idesc, 1u);
+                            }
+                        }
+                    }
+                    tc_commit(&empty[s]);
+                    if (last) tc_commit(&acc_full[b]);
+                }
+                __syncwarp();
+                if (++s == STAGES) { s = 0; ph ^= 1; }
+            }
+        }
+        // no product of this CTA may be in flight when it frees its tensor memory, however the other roles end
+        if (lead) {
+            if (!ok) s_fail = 1;
+            tc_commit(&drained);
+            mbar_wait_bounded(&drained, 0, PJ_SPIN_LIMIT);
+        }
+    } else if (lane == 0) {
+        // ---------------- weights ----------------
+        int s = 0, g = 0;
+        uint32_t ph = 1;
+        bool ok = true;
+        for (int lt = 0; lt < my_tiles && ok; ++lt) {
+            const int c0 = tile_col(lt), bytes = tile_n(lt) * 128;
+            const uint8_t* from = p.layout + (int64_t)(c0 / PJ_COLS) * chunks * PARTS * PJ_CHUNK + c0 % PJ_COLS * 128;
+            for (int kc = 0; kc < chunks; ++kc, ++g, from += PARTS * PJ_CHUNK) {
+                ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
+                if (!ok) break;
+                mbar_expect(&full_w[s], PARTS * bytes);
+                for (int part = 0; part < PARTS; ++part)
+                    tc_copy_bulk(ring + s * S::STAGE + S::X_STAGE + part * S::W_PART, from + part * PJ_CHUNK, bytes, &full_w[s]);
+                if (++s == STAGES) { s = 0; ph ^= 1; }
+            }
+        }
+        if (!ok) s_fail = 1;
+        // no copy of this CTA may be in flight when it leaves: the latest into each stage (usually long there)
+        for (int k = 0; k < min(g, STAGES); ++k) {
+            const int latest = g - 1 - k;
+            mbar_wait_bounded(&full_w[latest % STAGES], (uint32_t)(latest / STAGES) & 1, PJ_SPIN_LIMIT);
+        }
+    }
+
+    __syncwarp();
+    if (s_fail && lane == 0) g_request_timeout = 1;
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM) : "memory");
+}
+
+static int sm_count() {
+    static int per_device[64];
+    int d = 0, n = 0;
+    if (cudaGetDevice(&d) != cudaSuccess) return 1;
+    if (d < 64 && per_device[d]) return per_device[d];
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, d) != cudaSuccess || n < 1) n = 1;
+    if (d < 64) per_device[d] = n;
+    return n;
+}
+
+template <int TYPE, int BN>
+static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
+    constexpr size_t bytes = PjShape<TYPE, BN>::BYTES;
+    const cudaError_t e = cudaFuncSetAttribute(k_project_rows<TYPE, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != cudaSuccess) return e;
+    const int64_t tiles = (int64_t)((p.n + BN - 1) / BN) * ((p.rows + PJ_ROWS - 1) / PJ_ROWS);
+    return launch(k_project_rows<TYPE, BN>, dim3((unsigned)std::min<int64_t>(tiles, sm_count())), PJ_THREADS, bytes, stream, p);
+}
+
+template <int TYPE>
 static cudaError_t project(const ProjectParams& p, void* stream) {
     if (p.bank.info) {
-        const cudaError_t e = launch(k_shrink_rows<T>, dim3(p.rows), 128, 0, stream, p);
+        const cudaError_t e = launch(k_shrink_rows<typename Elem<TYPE>::T>, dim3(p.rows), 128, 0, stream, p);
         if (e != cudaSuccess) return e;
     }
-    return launch(k_project_simple<T>, dim3((p.rows + 7) / 8, (p.n + 31) / 32), 256, 0, stream, p);
+    // Tiles of 32 columns where those of 128 would leave most SMs without one.
+    const int64_t wide = (int64_t)((p.n + 127) / 128) * ((p.rows + PJ_ROWS - 1) / PJ_ROWS);
+    return wide >= sm_count() / 2 ? project_tiles<TYPE, 128>(p, stream) : project_tiles<TYPE, 32>(p, stream);
 }
 
 }  // namespace rp
@@ -337,8 +755,22 @@ extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) 
     p.n_slots = a->n_slots, p.slots = a->slots, p.t = static_cast<float*>(a->workspace);
     p.y = a->y, p.ld_y = a->ld_y, p.out_f32 = a->out_type == RIPPLE_TYPE_F32;
     cudaError_t e;
-    if (a->type == RIPPLE_TYPE_F32) e = project<float>(p, a->cuda_stream);
-    else if (a->type == RIPPLE_TYPE_BF16) e = project<__nv_bfloat16>(p, a->cuda_stream);
-    else e = project<__half>(p, a->cuda_stream);
+    if (a->type == RIPPLE_TYPE_F32) e = project<RIPPLE_TYPE_F32>(p, a->cuda_stream);
+    else if (a->type == RIPPLE_TYPE_BF16) e = project<RIPPLE_TYPE_BF16>(p, a->cuda_stream);
+    else e = project<RIPPLE_TYPE_F16>(p, a->cuda_stream);
     return e == cudaSuccess ? RIPPLE_OK : launch_failed("project_rows launch", e);
+}
+
+extern "C" ripple_status ripple_request_status(int32_t device) {
+    OnDevice on(device);
+    if (on.err != cudaSuccess) return launch_failed("cudaSetDevice", on.err);
+    int gave_up = 0;
+    const int zero = 0;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&gave_up, g_request_timeout, sizeof(int));
+    if (e == cudaSuccess && gave_up) e = cudaMemcpyToSymbol(g_request_timeout, &zero, sizeof(int));
+    if (e != cudaSuccess) return launch_failed("request_status", e);
+    if (!gave_up) return RIPPLE_OK;
+    note_error("project_rows: a bounded device-side wait gave up; the results of calls since the last query are not to be used");
+    return RIPPLE_ERR_TIMEOUT;
 }

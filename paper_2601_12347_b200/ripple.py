@@ -36,7 +36,7 @@ EXPORTED = [
     "ripple_get_stats", "ripple_last_error", "ripple_destroy", "ripple_version",
     # requests (serve.py)
     "ripple_norm_rows", "ripple_project_layout_bytes", "ripple_adapter_bytes", "ripple_project_layout",
-    "ripple_adapter_set", "ripple_project_workspace_bytes", "ripple_project_rows",
+    "ripple_adapter_set", "ripple_project_workspace_bytes", "ripple_project_rows", "ripple_request_status",
 ]
 # partitioned execution (include/ripple_part.h); the first 18 return a status
 EXPORTED_PART = [
@@ -160,7 +160,9 @@ def load_library(path: Optional[str] = None):
     lib.ripple_adapter_set.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, i32, vp]
     lib.ripple_project_workspace_bytes.argtypes = [vp]
     lib.ripple_project_rows.argtypes = [vp]
-    for name in ("ripple_norm_rows", "ripple_project_layout", "ripple_adapter_set", "ripple_project_rows"):
+    lib.ripple_request_status.argtypes = [i32]
+    for name in ("ripple_norm_rows", "ripple_project_layout", "ripple_adapter_set", "ripple_project_rows",
+                 "ripple_request_status"):
         getattr(lib, name).restype = i32
     for name in ("ripple_project_layout_bytes", "ripple_adapter_bytes", "ripple_project_workspace_bytes"):
         getattr(lib, name).restype = i64

@@ -331,6 +331,12 @@ def project_rows(x, projection: Projection, bank: Optional[AdapterBank] = None, 
     return out
 
 
+def check_requests(device=None) -> None:
+    """Waits for the device; raises RippleError (ERR_TIMEOUT) if a bounded device-side wait gave up since the last check."""
+    index = torch.cuda.current_device() if device is None else torch.device(device).index
+    _check(_ripple.load_library().ripple_request_status(-1 if index is None else index))
+
+
 @dataclass
 class Block:
     """s + scale * post(down(up(pre(s)))): a residual block of a RequestHead.  `up` and `down` with their banks (or None)."""
