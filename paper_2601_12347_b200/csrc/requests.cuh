@@ -87,6 +87,17 @@ inline cudaError_t launch(void (*kernel)(P...), dim3 grid, int block, size_t sme
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
+// multiprocessors of the current device
+inline int sm_count() {
+    static int per_device[64];
+    int d = 0, n = 0;
+    if (cudaGetDevice(&d) != cudaSuccess) return 1;
+    if (d < 64 && per_device[d]) return per_device[d];
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, d) != cudaSuccess || n < 1) n = 1;
+    if (d < 64) per_device[d] = n;
+    return n;
+}
+
 inline ripple_status launch_failed(const char* what, cudaError_t e) {
     note_error("%s failed: %s", what, cudaGetErrorString(e));
     return e == cudaErrorMemoryAllocation ? RIPPLE_ERR_OOM : RIPPLE_ERR_CUDA;

@@ -593,16 +593,6 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM) : "memory");
 }
 
-static int sm_count() {
-    static int per_device[64];
-    int d = 0, n = 0;
-    if (cudaGetDevice(&d) != cudaSuccess) return 1;
-    if (d < 64 && per_device[d]) return per_device[d];
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, d) != cudaSuccess || n < 1) n = 1;
-    if (d < 64) per_device[d] = n;
-    return n;
-}
-
 template <int TYPE, int BN>
 static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
     constexpr size_t bytes = PjShape<TYPE, BN>::BYTES;
