@@ -13,26 +13,29 @@ namespace rp {
 // fp32 weights are three chunks, one per bf16 part.
 constexpr int PJ_COLS = 128, PJ_KC = 64;
 constexpr int PJ_CHUNK = PJ_COLS * 128;
-// Bank: scale and rank of every slot, then A transposed (rank x K, zeros beyond both), then B transposed (n x rank).
+// Bank: scale and rank of every slot; A transposed (rank x K, zeros beyond both; fp32 as three planes of bf16 parts); B transposed
+// (n x rank, zeros beyond the rank) in planes of bf16: one for bf16, two for fp16 (its 11 bits), three for fp32.
 struct SlotInfo { float scale; int32_t rank; };
 
 __host__ __device__ inline int pj_parts(int type) { return type == RIPPLE_TYPE_F32 ? 3 : 1; }
+__host__ __device__ constexpr int pj_b_planes(int type) { return type == RIPPLE_TYPE_F32 ? 3 : type == RIPPLE_TYPE_F16 ? 2 : 1; }
 __host__ __device__ inline int pj_up(int x, int to) { return (x + to - 1) / to * to; }
 __host__ __device__ inline int64_t up128(int64_t x) { return (x + 127) / 128 * 128; }
 
 struct BankView {
     const SlotInfo* info;
-    const uint8_t* a;   // A transposed: slot x r_pad x k_pad
-    const uint8_t* b;   // B transposed: slot x n x r_pad
+    const uint16_t* a;   // slot x plane x r_pad x k_pad
+    const uint16_t* b;   // slot x plane x n x r_pad
     int r_pad, k_pad;
 };
 __host__ __device__ inline int64_t bank_a_at(int slots) { return up128((int64_t)slots * (int64_t)sizeof(SlotInfo) + 128); }
-__host__ __device__ inline int64_t bank_b_at(int size, int k, int slots, int max_rank) {
-    return bank_a_at(slots) + up128((int64_t)slots * pj_up(max_rank, 16) * pj_up(k, PJ_KC) * size);
+__host__ __device__ inline int64_t bank_b_at(int type, int k, int slots, int max_rank) {
+    return bank_a_at(slots) + up128((int64_t)slots * pj_up(max_rank, 16) * pj_up(k, PJ_KC) * pj_parts(type) * 2);
 }
-__host__ __device__ inline BankView bank_view(const void* bank, int size, int k, int slots, int max_rank) {
+__host__ __device__ inline BankView bank_view(const void* bank, int type, int k, int slots, int max_rank) {
     const uint8_t* p = static_cast<const uint8_t*>(bank);
-    return {reinterpret_cast<const SlotInfo*>(p), p + bank_a_at(slots), p + bank_b_at(size, k, slots, max_rank), pj_up(max_rank, 16), pj_up(k, PJ_KC)};
+    return {reinterpret_cast<const SlotInfo*>(p), reinterpret_cast<const uint16_t*>(p + bank_a_at(slots)),
+            reinterpret_cast<const uint16_t*>(p + bank_b_at(type, k, slots, max_rank)), pj_up(max_rank, 16), pj_up(k, PJ_KC)};
 }
 
 // An fp32 value as three bf16 parts, 8 bits each: the first cut (rounded, values next to the largest would become
@@ -80,12 +83,12 @@ __global__ void k_layout_weights(const T* W, int64_t ld, int k, int n, uint8_t* 
 }
 
 // count adapters into the slots from `first`; bad: set where an entry is not finite
-template <typename T>
-__global__ void k_set_adapters(uint8_t* a_out, uint8_t* b_out, const T* A, const T* B, int first, int count, int rank, int k, int n,
-                               int r_pad, int k_pad, int* bad) {
+template <int TYPE>
+__global__ void k_set_adapters(uint16_t* a_out, uint16_t* b_out, const typename Elem<TYPE>::T* A, const typename Elem<TYPE>::T* B, int first,
+                               int count, int rank, int k, int n, int r_pad, int k_pad, int* bad) {
     pdl_enter();
-    T* const at = reinterpret_cast<T*>(a_out);
-    T* const bt = reinterpret_cast<T*>(b_out);
+    using T = typename Elem<TYPE>::T;
+    constexpr int PA = TYPE == RIPPLE_TYPE_F32 ? 3 : 1, PB = pj_b_planes(TYPE);
     const int64_t per_a = (int64_t)r_pad * k_pad, per_b = (int64_t)n * r_pad, total = (per_a + per_b) * count;
     bool fine = true;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
@@ -95,20 +98,40 @@ __global__ void k_set_adapters(uint8_t* a_out, uint8_t* b_out, const T* A, const
         if (e < per_a) {
             const int r = (int)(e / k_pad), kk = (int)(e % k_pad);
             if (r < rank && kk < k) v = A[(s * k + kk) * rank + r];
-            at[(first + s) * per_a + e] = v;
+            uint16_t* const to = a_out + (first + s) * PA * per_a + e;
+            if constexpr (PA == 3) {
+                __nv_bfloat16 h[3];
+                pj_parts_of(v, h);
+                for (int q = 0; q < 3; ++q) to[q * per_a] = __bfloat16_as_ushort(h[q]);
+            } else {
+                to[0] = *reinterpret_cast<const uint16_t*>(&v);
+            }
         } else {
             e -= per_a;
             const int j = (int)(e / r_pad), r = (int)(e % r_pad);
             if (r < rank) v = B[(s * rank + r) * n + j];
-            bt[(first + s) * per_b + e] = v;
+            uint16_t* const to = b_out + (first + s) * PB * per_b + e;
+            float left = to_f32(v);
+            for (int q = 0; q < PB; ++q) {
+                const __nv_bfloat16 h = q == 0 && PB == 3 ? __float2bfloat16_rz(left) : __float2bfloat16_rn(left);
+                to[q * per_b] = __bfloat16_as_ushort(h);
+                left -= __bfloat162float(h);
+            }
         }
         fine = fine && isfinite(to_f32(v));
     }
     if (!fine) *bad = 1;
 }
 
-
 // ---- the product ---------------------------------------------------------------------------------------------------
+// The adapters that the rows of a tile use, in ascending order, and each row's place among them.
+struct alignas(128) TilePlan {
+    int32_t count;
+    uint16_t slot[128];
+    uint8_t row[128];      // 255: none
+};
+constexpr int PJ_NONE = 255;
+
 struct ProjectParams {
     int rows, k, n, act, chunks;
     const void* x;
@@ -119,7 +142,9 @@ struct ProjectParams {
     BankView bank;         // info null: no adapters
     int n_slots;
     const int32_t* slots;
-    float* t;              // rows x bank.r_pad: scale_a x_i A_a
+    TilePlan* plan;        // one per 128 rows
+    void* t;               // t_i = scale_a x_i A_a: fp32, rows x r_pad; 16-bit rows: two bf16 parts, rows x 2 x r_pad
+    int batches;           // tensor-core form of t: batches of adapters that are multiplied side by side
     void* y;
     int64_t ld_y;
     int out_f32;
@@ -136,24 +161,79 @@ __device__ __forceinline__ int slot_of(const ProjectParams& p, int i) {
     return a >= 0 && a < p.n_slots && p.bank.info[a].rank > 0 ? a : -1;
 }
 
-// t_i = scale_a x_i A_a: a warp per row and rank
-template <typename T>
-__global__ void k_shrink_rows(const __grid_constant__ ProjectParams p) {
+__device__ __forceinline__ void plan_tile(const ProjectParams& p, int tile) {
+    constexpr int WORDS = RIPPLE_MAX_SLOTS / 32;
+    __shared__ uint32_t used[WORDS], before[WORDS];
+    const int t = threadIdx.x, i = tile * 128 + t;      // blocks of 128 threads
+    used[t] = 0;
+    __syncthreads();
+    const int a = i < p.rows && row_of(p, i) >= 0 ? slot_of(p, i) : -1;
+    if (a >= 0) atomicOr(&used[a >> 5], 1u << (a & 31));
+    __syncthreads();
+    TilePlan& plan = p.plan[tile];
+    if (t < 32) {
+        int n = 0;
+        for (int w = 0; w < 4; ++w) n += __popc(used[4 * t + w]);
+        int at = warp_inclusive_scan(n) - n;
+        if (t == 31) plan.count = at + n;
+        for (int w = 0; w < 4; ++w) {
+            before[4 * t + w] = at;
+            for (uint32_t left = used[4 * t + w]; left; left &= left - 1) plan.slot[at++] = (uint16_t)(32 * (4 * t + w) + __ffs(left) - 1);
+        }
+    }
+    __syncthreads();
+    plan.row[t] = a < 0 ? PJ_NONE : (uint8_t)(before[a >> 5] + __popc(used[a >> 5] & ((1u << (a & 31)) - 1)));
+}
+static_assert(RIPPLE_MAX_SLOTS == 128 * 32, "a thread of plan_tile clears one word");
+
+__global__ void k_plan_tiles(const __grid_constant__ ProjectParams p) {
     pdl_enter();
-    const int i = blockIdx.x, lane = lane_id();
+    plan_tile(p, blockIdx.x);
+}
+
+template <int TYPE>
+__device__ __forceinline__ void store_t(const ProjectParams& p, int64_t i, int r, float t) {
+    const int rp = p.bank.r_pad;
+    if constexpr (TYPE == RIPPLE_TYPE_F32) {
+        static_cast<float*>(p.t)[i * rp + r] = t;
+    } else {
+        __nv_bfloat16* const to = static_cast<__nv_bfloat16*>(p.t) + i * 2 * rp + r;
+        const __nv_bfloat16 h = __float2bfloat16_rn(t);
+        to[0] = h;
+        to[rp] = __float2bfloat16_rn(__hisinf(h) ? 0.f : t - __bfloat162float(h));
+    }
+}
+
+// Few rows: t_i by a block per row, a warp per rank; the blocks in front plan the tiles.
+template <int TYPE>
+__global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ ProjectParams p) {
+    using T = typename Elem<TYPE>::T;
+    constexpr int PA = TYPE == RIPPLE_TYPE_F32 ? 3 : 1;
+    pdl_enter();
+    const int tiles = (p.rows + 127) / 128;
+    if ((int)blockIdx.x < tiles) return plan_tile(p, blockIdx.x);
+    const int i = blockIdx.x - tiles, lane = lane_id();
     const int64_t from = row_of(p, i);
     const int a = slot_of(p, i);
     if (from < 0 || a < 0) return;
     const T* const x = static_cast<const T*>(p.x) + from * p.ld_x;
     const SlotInfo info = p.bank.info[a];
-    for (int r = threadIdx.x >> 5; r < p.bank.r_pad; r += blockDim.x >> 5) {
+    const int64_t plane = (int64_t)p.bank.r_pad * p.bank.k_pad;
+    for (int r = threadIdx.x >> 5; r < p.bank.r_pad; r += 4) {
         float sum = 0.f;
         if (r < info.rank) {
-            const T* const w = reinterpret_cast<const T*>(p.bank.a) + ((int64_t)a * p.bank.r_pad + r) * p.bank.k_pad;
-            for (int kk = lane; kk < p.k; kk += 32) sum += to_f32(x[kk]) * to_f32(w[kk]);
+            const uint16_t* const w = p.bank.a + (int64_t)a * PA * plane + (int64_t)r * p.bank.k_pad;
+            for (int kk = lane; kk < p.k; kk += 32) {
+                float v;
+                if constexpr (PA == 3)
+                    v = __uint_as_float((uint32_t)w[kk + 2 * plane] << 16) + __uint_as_float((uint32_t)w[kk + plane] << 16) + __uint_as_float((uint32_t)w[kk] << 16);
+                else
+                    v = to_f32(reinterpret_cast<const T*>(w)[kk]);
+                sum += to_f32(x[kk]) * v;
+            }
             sum = warp_sum(sum) * info.scale;
         }
-        if (lane == 0) p.t[(int64_t)i * p.bank.r_pad + r] = sum;
+        if (lane == 0) store_t<TYPE>(p, i, r, sum);
     }
 }
 
@@ -165,6 +245,8 @@ constexpr int PJ_ROWS = 128;             // rows per tile: the lanes of the accu
 constexpr int PJ_LOADERS = 256;          // threads that fetch rows
 constexpr int PJ_EPI_WARPS = 8;          // two per quarter of the lanes
 constexpr int PJ_THREADS = PJ_LOADERS + 32 * PJ_EPI_WARPS + 64;   // and the warps that issue and that fetch weights
+constexpr int PJ_FEW = 1024;             // rows up to which t is computed a block per row
+constexpr int PJ_SHRINK_COLS = 64;       // ranks of adapters side by side, where t is computed on the tensor cores
 constexpr int PJ_UNIT = 4;               // fp32: chunks (256 entries of K) whose large products share an accumulator
 constexpr uint32_t PJ_SPIN_LIMIT = 1u << 22;
 constexpr int PJ_STAGING = PJ_EPI_WARPS * 32 * 17 * 4;
@@ -176,6 +258,7 @@ template <int TYPE, int BN> struct PjShape {
     static constexpr int STAGE = X_STAGE + W_STAGE;
     static constexpr int STAGES = 200 * 1024 / STAGE < 8 ? 200 * 1024 / STAGE : 8;
     static constexpr size_t BYTES = (size_t)STAGES * STAGE + PJ_STAGING + 1024;
+    static constexpr int RANKS = PARTS == 3 ? 64 : 32;      // ranks that a step of t_i B_a takes
 };
 
 // instruction descriptor: fp32 accumulators, both operands K-major, 128 rows, n columns
@@ -195,36 +278,24 @@ template <typename T> __device__ __forceinline__ uint32_t pj_pair(float a, float
     return *reinterpret_cast<uint32_t*>(&v);
 }
 
-// eight entries of a row of B transposed, as fp32
-__device__ __forceinline__ void pj_load8(float (&b)[8], const float* from) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const float4 v = __ldg(reinterpret_cast<const float4*>(from) + i);
-        b[4 * i] = v.x, b[4 * i + 1] = v.y, b[4 * i + 2] = v.z, b[4 * i + 3] = v.w;
-    }
-}
-template <typename T> __device__ __forceinline__ void pj_load8(float (&b)[8], const T* from) {
-    const uint4 v = __ldg(reinterpret_cast<const uint4*>(from));
-    const Piece<T, 8>& e = reinterpret_cast<const Piece<T, 8>&>(v);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) b[k] = to_f32(e.v[k]);
-}
-
-// A persistent CTA takes tiles of 128 rows x BN output columns: lanes of the accumulator are rows, its columns output columns.
+// A persistent CTA takes tiles of 128 rows x BN columns: lanes of the accumulator are rows, its columns output columns.
+// SHRINK: the columns are the ranks of adapters that the tile's rows use, side by side, and each row keeps those of its own: t.
+// Else: columns of y; behind the steps over K come steps over ranks, the adapters of the tile one behind the other, where a
+// row's operand is its t at its adapter's ranks and zero at all others.
 //   loaders    fetch the rows by id, chunk by chunk of 64 entries, into the swizzled layout that the tensor core reads: 16-bit
 //              rows as asynchronous copies, fp32 rows (and rows that are not 16-byte aligned) through registers,
-//              fp32 entries as three bf16 parts
+//              fp32 entries as three bf16 parts; and what comes out of the bank
 //   one thread copies the weights' chunks, one issues the products
-//   epilogue   takes a finished accumulator while the next is being filled, adds t B_a by row, bias, activation, and writes
+//   epilogue   takes a finished accumulator while the next is being filled: bias, activation, and out
 // fp32: six products of parts (all but those below 2^-23); the large one of the first parts is handed over every 256 entries
 // and summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
 // Barriers, all waits bounded: full_x[s] (one arrival per loader warp), full_w[s] (bytes), empty[s] (the products that read
 // stage s), acc_full[b], acc_empty[b] (one arrival per epilogue warp).
-template <int TYPE, int BN>
+template <int TYPE, int BN, bool SHRINK>
 __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_constant__ ProjectParams p) {
     using T = typename Elem<TYPE>::T;
     using S = PjShape<TYPE, BN>;
-    constexpr int PARTS = S::PARTS, STAGES = S::STAGES, NB = BN / 32;
+    constexpr int PARTS = S::PARTS, STAGES = S::STAGES, NB = BN / 32, RANKS = S::RANKS, B_PLANES = pj_b_planes(TYPE);
     constexpr uint32_t TMEM = 4 * BN < 32 ? 32 : 4 * BN;       // two accumulators and, fp32, two for the small products
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full_x[STAGES], full_w[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
@@ -232,13 +303,32 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
     __shared__ volatile int s_fail;
 
     const int tid = threadIdx.x, warp = __shfl_sync(FULL, tid >> 5, 0), lane = tid & 31;
-    const int col_tiles = (p.n + BN - 1) / BN, row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
-    const int64_t tiles = (int64_t)col_tiles * row_tiles;
+    const int across = SHRINK ? p.batches : (p.n + BN - 1) / BN, row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
+    const int64_t tiles = (int64_t)across * row_tiles;
     const int my_tiles = (int)((tiles - blockIdx.x + gridDim.x - 1) / gridDim.x), chunks = p.chunks;
+    const int r_pad = p.bank.r_pad, at_once = SHRINK ? BN / r_pad : 0;
     uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    auto tile_row = [&](int lt) { return (int)((blockIdx.x + (int64_t)lt * gridDim.x) / col_tiles) * PJ_ROWS; };
-    auto tile_col = [&](int lt) { return (int)((blockIdx.x + (int64_t)lt * gridDim.x) % col_tiles) * BN; };
-    auto tile_n = [&](int lt) { return min(BN, (p.n - tile_col(lt) + 15) & ~15); };
+    // A tile: 128 rows, and a tile of columns or a batch of adapters (SHRINK: every `across`-th batch of the row tile's, as many as
+    // its adapters fill).  The next row tile's count of adapters is asked for early.
+    struct Tile { int lt, rows, part, count, count_next; };
+    auto row_tile = [&](int lt) { return (int)((blockIdx.x + (int64_t)lt * gridDim.x) / across); };
+    auto part_of = [&](int lt) { return (int)((blockIdx.x + (int64_t)lt * gridDim.x) % across); };
+    auto adapters = [&](int lt) { return p.plan && lt < my_tiles ? p.plan[row_tile(lt)].count : 0; };
+    auto after = [&](const Tile& t) {
+        Tile n = t;
+        if constexpr (SHRINK) n.part += across;
+        while (!SHRINK || n.part * at_once >= n.count) {
+            if (++n.lt >= my_tiles) break;
+            n.rows = row_tile(n.lt), n.part = part_of(n.lt), n.count = n.count_next;
+            n.count_next = adapters(n.lt + 1);
+            if (!SHRINK) break;
+        }
+        return n;
+    };
+    auto first_tile = [&]() { return after(Tile{-1, 0, 0, 0, adapters(0)}); };
+    // columns that are multiplied
+    auto tile_n = [&](const Tile& t) { return SHRINK ? min(at_once, t.count - t.part * at_once) * r_pad : min(BN, (p.n - t.part * BN + 15) & ~15); };
+    auto rank_steps = [&](int count) { return SHRINK ? 0 : (count * r_pad + RANKS - 1) / RANKS; };
 
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&full_x[s], PJ_LOADERS / 32); mbar_init(&full_w[s], 1); mbar_init(&empty[s], 1); }
@@ -258,115 +348,186 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
     pdl_enter();
 
     if (warp < PJ_LOADERS / 32) {
-        // ---------------- rows ----------------
-        constexpr int RSTEP = PJ_LOADERS / 8, ITS = PJ_ROWS / RSTEP;
+        // ---------------- rows, and what comes out of the bank ----------------
+        constexpr int RSTEP = PJ_LOADERS / 8, ITS = PJ_ROWS / RSTEP, W_ITS = BN / RSTEP;
+        constexpr int LAG = PARTS == 3 ? 1 : STAGES - 2;        // steps whose copies are in flight
         const int c = tid & 7, rb = tid >> 3;       // thread: piece c (8 entries) of the rows rb + RSTEP it
         const uint32_t mine = smem_u32(ring) + tc_swz(rb, c);
         const bool vec = (reinterpret_cast<uintptr_t>(p.x) & 15) == 0 && p.ld_x % (16 / (int)sizeof(T)) == 0;
-        const T *row[ITS], *next[ITS];              // null: nothing to read
-        auto aim = [&](int lt) {
+        const bool regs = PARTS == 3 || !vec;
+        // rank steps: this thread's piece of a step is a plane's ranks from c_rank
+        const int c_plane = PARTS == 3 ? 0 : c >> 2, c_rank = PARTS == 3 ? c * 8 : (c & 3) * 8;
+        // rows (null: nothing to read) and adapters of this tile and the next
+        const T *row[ITS], *next[ITS];
+        uint32_t which = 0, which_next = 0;         // the rows' places among the adapters, a byte each
+        int slot0 = 0, slot0_next = 0, slot1 = 0, slot1_next = 0;
+        auto aim = [&](const Tile& t) {
+#pragma unroll
+            for (int it = 0; it < ITS; ++it) next[it] = nullptr;
+            if (t.lt >= my_tiles) return;
+            const int r0 = t.rows * PJ_ROWS + rb;
 #pragma unroll
             for (int it = 0; it < ITS; ++it) {
-                next[it] = nullptr;
-                if (lt >= my_tiles) continue;
-                const int i = tile_row(lt) + rb + RSTEP * it;
+                const int i = r0 + RSTEP * it;
                 const int64_t from = i < p.rows ? row_of(p, i) : -1;
                 if (from >= 0) next[it] = static_cast<const T*>(p.x) + from * p.ld_x + c * 8;
             }
+            if (!p.plan) return;
+            const TilePlan& plan = p.plan[t.rows];
+            if constexpr (SHRINK) {                 // slots of the rows of A that this thread fetches
+                const int j0 = t.part * at_once + rb / r_pad, j1 = t.part * at_once + (rb + RSTEP) / r_pad;
+                slot0_next = rb < at_once * r_pad && j0 < t.count ? plan.slot[j0] : -1;
+                slot1_next = rb + RSTEP < at_once * r_pad && j1 < t.count ? plan.slot[j1] : -1;
+            } else if (t.count) {
+                which_next = 0;
+#pragma unroll
+                for (int it = 0; it < ITS; ++it) which_next |= (uint32_t)plan.row[rb + RSTEP * it] << (8 * it);
+                const int j = c_rank / r_pad;
+                slot0_next = j < t.count ? plan.slot[j] : -1;
+            }
         };
-        bool ok = true;
-        int s = 0, g = 0;
-        uint32_t ph = 1;                            // (a fresh barrier counts as completed)
-        if (PARTS == 1 && vec) {
-            constexpr int LAG = STAGES - 2;         // chunks in flight
-            aim(0);
-            int told = 0;
-            for (int lt = 0; lt < my_tiles && ok; ++lt) {
+        T raw[ITS][8];
+        auto fetch = [&](const T* const (&rows)[ITS], int kc) {
+            const int left = p.k - kc * PJ_KC - c * 8;
 #pragma unroll
-                for (int it = 0; it < ITS; ++it) row[it] = next[it];
-                aim(lt + 1);
-                for (int kc = 0; kc < chunks; ++kc, ++g) {
-                    ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
-                    if (!ok) break;
-                    const int left = p.k - kc * PJ_KC - c * 8;
-                    const uint32_t bytes = left >= 8 ? 16u : left > 0 ? 2u * left : 0u;
+            for (int it = 0; it < ITS; ++it) {
+                const T* const from = rows[it] + kc * PJ_KC;
+                if (vec && left >= 8 && rows[it]) {
 #pragma unroll
-                    for (int it = 0; it < ITS; ++it)
-                        if (row[it]) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
-                                                  ::"r"(mine + (uint32_t)(s * S::STAGE + it * (RSTEP * 128))), "l"(bytes ? row[it] + kc * PJ_KC : row[it]), "r"(bytes) : "memory");
-                    asm volatile("cp.async.commit_group;" ::: "memory");
-                    if (g >= LAG) {
-                        asm volatile("cp.async.wait_group %0;" ::"n"(LAG) : "memory");
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&full_x[told]);
-                        if (++told == STAGES) told = 0;
-                    }
-                    if (++s == STAGES) { s = 0; ph ^= 1; }
+                    for (int e = 0; e < 8; e += 16 / (int)sizeof(T))
+                        *reinterpret_cast<uint4*>(&raw[it][e]) = __ldg(reinterpret_cast<const uint4*>(from + e));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) raw[it][e] = rows[it] && e < left ? from[e] : from_f32<T>(0.f);
                 }
             }
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            __syncwarp();
-            if (lane == 0 && ok)
-                for (int d = 0; d < min(g, LAG); ++d) {
-                    mbar_arrive(&full_x[told]);
-                    if (++told == STAGES) told = 0;
-                }
-        } else {
-            T raw[ITS][8];
-            auto fetch = [&](int kc) {
-                const int left = p.k - kc * PJ_KC - c * 8;
+        };
+        // a row's t, where the step's ranks are its adapter's
+        auto fetch_t = [&](const Tile& t, int step) {
+            if constexpr (PARTS == 3) {
+                const int q = step * RANKS + c_rank, j = q / r_pad, r = q % r_pad;
+                const int64_t i0 = (int64_t)t.rows * PJ_ROWS + rb;
 #pragma unroll
                 for (int it = 0; it < ITS; ++it) {
-                    const T* const from = row[it] + kc * PJ_KC;
-                    if (vec && left >= 8 && row[it]) {
+                    const bool own = (int)(which >> (8 * it) & 255) == j;
+                    const float4* const from = reinterpret_cast<const float4*>(static_cast<const float*>(p.t) + (i0 + RSTEP * it) * r_pad + r);
 #pragma unroll
-                        for (int e = 0; e < 8; e += 16 / (int)sizeof(T))
-                            *reinterpret_cast<uint4*>(&raw[it][e]) = __ldg(reinterpret_cast<const uint4*>(from + e));
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) raw[it][e] = row[it] && e < left ? from[e] : from_f32<T>(0.f);
-                    }
-                }
-            };
-            aim(0);
-            for (int lt = 0; lt < my_tiles && ok; ++lt) {
-#pragma unroll
-                for (int it = 0; it < ITS; ++it) row[it] = next[it];
-                if (lt == 0) fetch(0);
-                aim(lt + 1);
-                for (int kc = 0; kc < chunks; ++kc) {
-                    ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
-                    if (!ok) break;
-#pragma unroll
-                    for (int it = 0; it < ITS; ++it) {
-                        uint8_t* const to = ring + s * S::STAGE + it * (RSTEP * 128) + tc_swz(rb, c);
-                        if constexpr (PARTS == 3) {
-                            Piece<__nv_bfloat16, 8> part[3];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                __nv_bfloat16 h[3];
-                                pj_parts_of(raw[it][e], h);
-                                part[0].v[e] = h[0], part[1].v[e] = h[1], part[2].v[e] = h[2];
-                            }
-#pragma unroll
-                            for (int q = 0; q < 3; ++q) *reinterpret_cast<Piece<__nv_bfloat16, 8>*>(to + q * S::X_PART) = part[q];
-                        } else {
-                            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(&raw[it][0]);
-                        }
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&full_x[s]);
-                    if (++s == STAGES) { s = 0; ph ^= 1; }
-                    // what the next step stores is requested now: of this tile, or of the one after it
-                    if (kc + 1 < chunks) fetch(kc + 1);
-                    else {
-#pragma unroll
-                        for (int it = 0; it < ITS; ++it) row[it] = next[it];
-                        fetch(0);
-                    }
+                    for (int h = 0; h < 2; ++h) *reinterpret_cast<float4*>(&raw[it][4 * h]) = own ? __ldg(from + h) : make_float4(0.f, 0.f, 0.f, 0.f);
                 }
             }
+        };
+        auto keep = [&](int s) {                    // what was fetched, into a stage
+#pragma unroll
+            for (int it = 0; it < ITS; ++it) {
+                uint8_t* const to = ring + s * S::STAGE + it * (RSTEP * 128) + tc_swz(rb, c);
+                if constexpr (PARTS == 3) {
+                    Piece<__nv_bfloat16, 8> part[3];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        __nv_bfloat16 h[3];
+                        pj_parts_of(raw[it][e], h);
+                        part[0].v[e] = h[0], part[1].v[e] = h[1], part[2].v[e] = h[2];
+                    }
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) *reinterpret_cast<Piece<__nv_bfloat16, 8>*>(to + q * S::X_PART) = part[q];
+                } else {
+                    *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(&raw[it][0]);
+                }
+            }
+        };
+        auto copy = [&](uint32_t to, const void* from, uint32_t bytes) {    // 16 bytes, zeros behind the first `bytes`
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+        };
+        bool ok = true, fetched = false;
+        int s = 0, g = 0, told = 0;
+        uint32_t ph = 1;                            // (a fresh barrier counts as completed)
+        Tile tile = first_tile();
+        aim(tile);
+        while (tile.lt < my_tiles && ok) {
+#pragma unroll
+            for (int it = 0; it < ITS; ++it) row[it] = next[it];
+            which = which_next, slot0 = slot0_next, slot1 = slot1_next;
+            const Tile following = after(tile);
+            const int steps = chunks + rank_steps(tile.count);
+            aim(following);
+            if (regs && !fetched) fetch(row, 0);
+            fetched = true;
+            for (int st = 0; st < steps; ++st, ++g) {
+                ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
+                if (!ok) break;
+                const uint32_t x_to = mine + (uint32_t)(s * S::STAGE), w_to = x_to + S::X_STAGE;
+                if (st < chunks) {
+                    if (regs) {
+                        keep(s);
+                    } else {
+                        const int left = p.k - st * PJ_KC - c * 8;
+                        const uint32_t bytes = left >= 8 ? 16u : left > 0 ? 2u * left : 0u;
+#pragma unroll
+                        for (int it = 0; it < ITS; ++it)
+                            if (row[it]) copy(x_to + it * (RSTEP * 128), bytes ? row[it] + st * PJ_KC : row[it], bytes);
+                    }
+                    if constexpr (SHRINK) {
+                        const int64_t plane = (int64_t)r_pad * p.bank.k_pad;
+#pragma unroll
+                        for (int it = 0; it < W_ITS; ++it) {
+                            const int slot = it ? slot1 : slot0;
+                            if (slot < 0) continue;
+                            const uint16_t* const from = p.bank.a + (int64_t)slot * PARTS * plane + (int64_t)((rb + RSTEP * it) % r_pad) * p.bank.k_pad + st * PJ_KC + c * 8;
+#pragma unroll
+                            for (int q = 0; q < PARTS; ++q) copy(w_to + q * S::W_PART + it * (RSTEP * 128), from + q * plane, 16);
+                        }
+                    }
+                } else if constexpr (!SHRINK) {
+                    const int step = st - chunks, q = step * RANKS + c_rank, j = q / r_pad, r = q % r_pad;
+                    const int slot = step == 0 ? slot0 : j < tile.count ? p.plan[tile.rows].slot[j] : -1;
+                    if constexpr (PARTS == 3) {
+                        keep(s);
+                    } else {
+                        const int64_t i0 = (int64_t)tile.rows * PJ_ROWS + rb;
+#pragma unroll
+                        for (int it = 0; it < ITS; ++it) {
+                            const bool own = (int)(which >> (8 * it) & 255) == j;
+                            const __nv_bfloat16* const t = static_cast<const __nv_bfloat16*>(p.t);
+                            copy(x_to + it * (RSTEP * 128), own ? t + ((i0 + RSTEP * it) * 2 + c_plane) * r_pad + r : t, own ? 16 : 0);
+                        }
+                    }
+                    const int64_t plane = (int64_t)p.n * r_pad;
+#pragma unroll
+                    for (int it = 0; it < W_ITS; ++it) {
+                        const int col = tile.part * BN + rb + RSTEP * it;
+                        const bool real = slot >= 0 && col < p.n;
+                        const uint16_t* const from = p.bank.b + (real ? (int64_t)slot * B_PLANES * plane + (int64_t)col * r_pad + r : 0);
+                        if constexpr (PARTS == 3) {
+#pragma unroll
+                            for (int k = 0; k < B_PLANES; ++k) copy(w_to + k * S::W_PART + it * (RSTEP * 128), from + (real ? k * plane : 0), real ? 16 : 0);
+                        } else if (c_plane < B_PLANES) {
+                            copy(w_to + it * (RSTEP * 128), from + (real ? c_plane * plane : 0), real ? 16 : 0);
+                        }
+                    }
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                if (regs) {                         // what the next step keeps is requested now: of this tile, or of the one after it
+                    if (st + 1 < chunks) fetch(row, st + 1);
+                    else if (st + 1 < steps) fetch_t(tile, st + 1 - chunks);
+                    else fetch(next, 0);
+                }
+                if (g >= LAG) {
+                    asm volatile("cp.async.wait_group %0;" ::"n"(LAG) : "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&full_x[told]);
+                    if (++told == STAGES) told = 0;
+                }
+                if (++s == STAGES) { s = 0; ph ^= 1; }
+            }
+            tile = following;
         }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
+        if (lane == 0 && ok)
+            for (int d = 0; d < min(g, LAG); ++d) {
+                mbar_arrive(&full_x[told]);
+                if (++told == STAGES) told = 0;
+            }
         if (!ok) s_fail = 1;
     } else if (warp < PJ_LOADERS / 32 + PJ_EPI_WARPS) {
         // ---------------- epilogue ----------------
@@ -377,35 +538,52 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
         const bool vec = (reinterpret_cast<uintptr_t>(p.y) & 31) == 0 && p.ld_y * out_size % 32 == 0;
         const int units = PARTS == 3 ? (chunks + PJ_UNIT - 1) / PJ_UNIT : 1;
         bool ok = true;
-        int sg = 0;
-        for (int lt = 0; lt < my_tiles && ok; ++lt) {
+        int sg = 0, worked = 0;                 // accumulators and tiles taken so far
+        for (Tile tile = first_tile(); tile.lt < my_tiles && ok; tile = after(tile)) {
             // thread: a row, and the 16-column blocks half, half + 2, ... of the tile
-            const int i = tile_row(lt) + 32 * q + lane, c0 = tile_col(lt), nt = tile_n(lt);
-            const bool live = i < p.rows && row_of(p, i) >= 0;
-            const int a = live && p.bank.info ? slot_of(p, i) : -1;
-            const int rank = a >= 0 ? p.bank.info[a].rank : 0;
-            const bool any = __any_sync(FULL, rank > 0);
-            const uint32_t rows_live = __ballot_sync(FULL, live);
-            // 16 finished sums of this row, from column `at` of y: plus t_i B_a, bias, activation, and out
-            auto finish = [&](float (&y)[16], int at) {
-                if (any) {
-                    const float* const ti = p.t + (int64_t)i * p.bank.r_pad;
-                    const T* const bt = reinterpret_cast<const T*>(p.bank.b) + ((int64_t)(a >= 0 ? a : 0) * p.n + at) * p.bank.r_pad;
-#pragma unroll 1
-                    for (int r = 0; r < rank; r += 8) {
-                        float t[8];
-                        pj_load8(t, ti + r);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            if (at + e >= p.n) continue;
-                            float w[8], d = 0.f;
-                            pj_load8(w, bt + e * p.bank.r_pad + r);
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) d += t[k] * w[k];
-                            y[e] += d;
-                        }
-                    }
+            const int nt = tile_n(tile);
+            const int i = tile.rows * PJ_ROWS + 32 * q + lane, c0 = SHRINK ? 0 : tile.part * BN;
+            int own = -1, rank = 0;            // SHRINK: the row's adapter within the batch
+            float scale = 0.f;
+            bool live = i < p.rows;
+            if constexpr (SHRINK) {
+                const TilePlan& plan = p.plan[tile.rows];
+                const int at = plan.row[32 * q + lane];
+                if (at != PJ_NONE) {
+                    const SlotInfo info = p.bank.info[plan.slot[at]];
+                    rank = info.rank, scale = info.scale;
+                    own = at - tile.part * at_once;
                 }
+            } else {
+                live = live && row_of(p, i) >= 0;
+            }
+            const uint32_t rows_live = __ballot_sync(FULL, live);
+            // 16 finished sums of this row, from column `at` of the tile
+            auto finish = [&](float (&y)[16], int at) {
+                if constexpr (SHRINK) {
+                    if (own < 0 || own != at / r_pad) return;
+                    const int r = at % r_pad;
+                    uint32_t v[8], w[8];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) y[e] = r + e < rank ? y[e] * scale : 0.f;
+                    if constexpr (PARTS == 3) {
+                        float* const to = static_cast<float*>(p.t) + (int64_t)i * r_pad + r;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = __float_as_uint(y[e]), w[e] = __float_as_uint(y[8 + e]);
+                        pj_store8(to, v), pj_store8(to + 8, w);
+                    } else {
+                        __nv_bfloat16* const to = static_cast<__nv_bfloat16*>(p.t) + (int64_t)i * 2 * r_pad + r;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            v[e] = pj_pair<__nv_bfloat16>(y[2 * e], y[2 * e + 1]);
+                            const float h0 = __uint_as_float(v[e] << 16), h1 = __uint_as_float(v[e] & 0xffff0000u);
+                            w[e] = pj_pair<__nv_bfloat16>(fabsf(h0) < INFINITY ? y[2 * e] - h0 : 0.f, fabsf(h1) < INFINITY ? y[2 * e + 1] - h1 : 0.f);
+                        }
+                        pj_store8(to, v), pj_store8(to + r_pad, w);
+                    }
+                    return;
+                }
+                at += c0;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     if (p.bias && at + e < p.n) y[e] += __ldg(p.bias + at + e);
@@ -451,7 +629,7 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
             float sum[CARRY][16];              // fp32: of the units before the last
             for (int u = 0; u < units && ok; ++u, ++sg) {
                 const int b = sg & 1;
-                const uint32_t large = lanes + (uint32_t)(b * BN), small = lanes + (uint32_t)(2 * BN + (lt & 1) * BN);
+                const uint32_t large = lanes + (uint32_t)(b * BN), small = lanes + (uint32_t)(2 * BN + (worked & 1) * BN);
                 ok = __all_sync(FULL, mbar_wait_bounded(&acc_full[b], (sg >> 1) & 1, PJ_SPIN_LIMIT));
                 if (!ok) break;
                 tc_fence_after();
@@ -493,29 +671,30 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
 #pragma unroll
                             for (int e = 0; e < 16; ++e) if (fabsf(y[e]) < INFINITY) y[e] += __uint_as_float(x[e]);
                         }
-                        finish(y, c0 + at);
+                        finish(y, at);
                     }
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&acc_empty[b]);
             }
+            ++worked;
         }
         if (!ok) s_fail = 1;
     } else if (warp == PJ_LOADERS / 32 + PJ_EPI_WARPS) {
         // ---------------- products ----------------
         const bool lead = tc_elect();
         const uint64_t d0 = tc_smem_desc(smem_u32(ring));
-        int s = 0, sg = 0;
+        int s = 0, sg = 0, worked = 0;
         uint32_t ph = 0;
         bool ok = true;
-        for (int lt = 0; lt < my_tiles && ok; ++lt) {
-            const int nt = __shfl_sync(FULL, tile_n(lt), 0);
-            const uint32_t idesc = pj_idesc(TYPE, nt), small = tmem + (uint32_t)(2 * BN + (lt & 1) * BN);
+        for (Tile tile = first_tile(); tile.lt < my_tiles && ok; tile = after(tile)) {
+            const int count = __shfl_sync(FULL, tile.count, 0), nt = __shfl_sync(FULL, tile_n(tile), 0), steps = chunks + rank_steps(count);
+            const uint32_t idesc = pj_idesc(TYPE, nt), idesc_t = pj_idesc(RIPPLE_TYPE_BF16, nt), small = tmem + (uint32_t)(2 * BN + (worked & 1) * BN);
             uint32_t acc = 0;
-            int left = p.k, b = 0;
-            for (int kc = 0; kc < chunks; ++kc, left -= PJ_KC) {
-                const bool first = PARTS == 3 ? kc % PJ_UNIT == 0 : kc == 0;
+            int left = p.k, left_t = count * r_pad, b = 0;
+            for (int st = 0; st < steps; ++st) {
+                const bool first = PARTS == 3 ? st < chunks && st % PJ_UNIT == 0 : st == 0;
                 if (first) {
                     b = sg & 1;
                     const int before = sg >> 1;
@@ -526,34 +705,52 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
                     tc_fence_after();
                     acc = tmem + (uint32_t)(b * BN);
                 }
-                ok = __all_sync(FULL, mbar_wait_bounded(&full_w[s], ph, PJ_SPIN_LIMIT) && mbar_wait_bounded(&full_x[s], ph, PJ_SPIN_LIMIT));
+                ok = __all_sync(FULL, (SHRINK || mbar_wait_bounded(&full_w[s], ph, PJ_SPIN_LIMIT)) && mbar_wait_bounded(&full_x[s], ph, PJ_SPIN_LIMIT));
                 if (!ok) break;
                 fence_async_smem();      // the loaders' stores, for the tensor core (on the reader's side: loads in flight are not waited for)
                 tc_fence_after();
                 const uint64_t x = d0 + (uint64_t)((uint32_t)s * (S::STAGE >> 4)), w = x + (S::X_STAGE >> 4);
-                const bool last = PARTS == 3 ? kc % PJ_UNIT == PJ_UNIT - 1 || kc == chunks - 1 : kc == chunks - 1;
+                const bool last = st == steps - 1 || (PARTS == 3 && st < chunks - 1 && st % PJ_UNIT == PJ_UNIT - 1);
+                constexpr uint64_t XP = S::X_PART >> 4, WP = S::W_PART >> 4;
                 if (lead) {
+                    if (PARTS == 3 || st < chunks) {
+                        const int here = st < chunks ? left : left_t;
+                        const uint32_t kind = st < chunks ? idesc : idesc_t;
 #pragma unroll
-                    for (int j = 0; j < PJ_KC / 16; ++j) {        // 16 entries = 32 bytes per instruction
-                        if (16 * j < left) {
-                            const uint64_t x1 = x + 2 * j, w1 = w + 2 * j;
-                            tc_mma_bf16(acc, x1, w1, idesc, !first || j != 0);
-                            if constexpr (PARTS == 3) {
-                                constexpr uint64_t XP = S::X_PART >> 4, WP = S::W_PART >> 4;
-                                tc_mma_bf16(small, x1, w1 + WP, idesc, (kc | j) != 0);
-                                tc_mma_bf16(small, x1 + XP, w1, idesc, 1u);
-                                tc_mma_bf16(small, x1 + XP, w1 + WP, idesc, 1u);
-                                tc_mma_bf16(small, x1, w1 + 2 * WP, idesc, 1u);
-                                tc_mma_bf16(small, x1 + 2 * XP, w1, idesc, 1u);
+                        for (int j = 0; j < PJ_KC / 16; ++j) {        // 16 entries = 32 bytes per instruction
+                            if (16 * j < here) {
+                                const uint64_t x1 = x + 2 * j, w1 = w + 2 * j;
+                                tc_mma_bf16(acc, x1, w1, kind, !first || j != 0);
+                                if constexpr (PARTS == 3) {
+                                    tc_mma_bf16(small, x1, w1 + WP, kind, (st | j) != 0);
+                                    tc_mma_bf16(small, x1 + XP, w1, kind, 1u);
+                                    tc_mma_bf16(small, x1 + XP, w1 + WP, kind, 1u);
+                                    tc_mma_bf16(small, x1, w1 + 2 * WP, kind, 1u);
+                                    tc_mma_bf16(small, x1 + 2 * XP, w1, kind, 1u);
+                                }
+                            }
+                        }
+                    } else {
+                        // t in two parts (64 bytes of a row each), B in one or two
+#pragma unroll
+                        for (int j = 0; j < RANKS / 16; ++j) {
+                            if (16 * j < left_t) {
+                                const uint64_t x1 = x + 2 * j, w1 = w + 2 * j;
+                                tc_mma_bf16(acc, x1, w1, idesc_t, 1u);
+                                tc_mma_bf16(acc, x1 + 4, w1, idesc_t, 1u);
+                                if (B_PLANES == 2) tc_mma_bf16(acc, x1, w1 + 4, idesc_t, 1u);
                             }
                         }
                     }
                     tc_commit(&empty[s]);
                     if (last) tc_commit(&acc_full[b]);
                 }
+                if (st < chunks) left -= PJ_KC;
+                else left_t -= RANKS;
                 __syncwarp();
                 if (++s == STAGES) { s = 0; ph ^= 1; }
             }
+            ++worked;
         }
         // no product of this CTA may be in flight when it frees its tensor memory, however the other roles end
         if (lead) {
@@ -561,20 +758,24 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
             tc_commit(&drained);
             mbar_wait_bounded(&drained, 0, PJ_SPIN_LIMIT);
         }
-    } else if (lane == 0) {
+    } else if (lane == 0 && !SHRINK) {
         // ---------------- weights ----------------
         int s = 0, g = 0;
         uint32_t ph = 1;
         bool ok = true;
-        for (int lt = 0; lt < my_tiles && ok; ++lt) {
-            const int c0 = tile_col(lt), bytes = tile_n(lt) * 128;
+        for (Tile tile = first_tile(); tile.lt < my_tiles && ok; tile = after(tile)) {
+            const int steps = chunks + rank_steps(tile.count), c0 = tile.part * BN, bytes = tile_n(tile) * 128;
             const uint8_t* from = p.layout + (int64_t)(c0 / PJ_COLS) * chunks * PARTS * PJ_CHUNK + c0 % PJ_COLS * 128;
-            for (int kc = 0; kc < chunks; ++kc, ++g, from += PARTS * PJ_CHUNK) {
+            for (int st = 0; st < steps; ++st, ++g, from += PARTS * PJ_CHUNK) {
                 ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
                 if (!ok) break;
-                mbar_expect(&full_w[s], PARTS * bytes);
-                for (int part = 0; part < PARTS; ++part)
-                    tc_copy_bulk(ring + s * S::STAGE + S::X_STAGE + part * S::W_PART, from + part * PJ_CHUNK, bytes, &full_w[s]);
+                if (st < chunks) {
+                    mbar_expect(&full_w[s], PARTS * bytes);
+                    for (int part = 0; part < PARTS; ++part)
+                        tc_copy_bulk(ring + s * S::STAGE + S::X_STAGE + part * S::W_PART, from + part * PJ_CHUNK, bytes, &full_w[s]);
+                } else {
+                    mbar_arrive(&full_w[s]);       // (the loaders bring what a step over ranks reads)
+                }
                 if (++s == STAGES) { s = 0; ph ^= 1; }
             }
         }
@@ -593,24 +794,35 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM) : "memory");
 }
 
-template <int TYPE, int BN>
+template <int TYPE, int BN, bool SHRINK>
 static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
     constexpr size_t bytes = PjShape<TYPE, BN>::BYTES;
-    const cudaError_t e = cudaFuncSetAttribute(k_project_rows<TYPE, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    const cudaError_t e = cudaFuncSetAttribute(k_project_rows<TYPE, BN, SHRINK>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e != cudaSuccess) return e;
-    const int64_t tiles = (int64_t)((p.n + BN - 1) / BN) * ((p.rows + PJ_ROWS - 1) / PJ_ROWS);
-    return launch(k_project_rows<TYPE, BN>, dim3((unsigned)std::min<int64_t>(tiles, sm_count())), PJ_THREADS, bytes, stream, p);
+    const int64_t across = SHRINK ? p.batches : (p.n + BN - 1) / BN, tiles = across * ((p.rows + PJ_ROWS - 1) / PJ_ROWS);
+    return launch(k_project_rows<TYPE, BN, SHRINK>, dim3((unsigned)std::min<int64_t>(tiles, sm_count())), PJ_THREADS, bytes, stream, p);
 }
 
 template <int TYPE>
-static cudaError_t project(const ProjectParams& p, void* stream) {
+static cudaError_t project(ProjectParams p, void* stream) {
+    const int row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
     if (p.bank.info) {
-        const cudaError_t e = launch(k_shrink_rows<typename Elem<TYPE>::T>, dim3(p.rows), 128, 0, stream, p);
+        cudaError_t e;
+        if (p.rows <= PJ_FEW) {
+            e = launch(k_shrink_few<TYPE>, dim3(row_tiles + p.rows), 128, 0, stream, p);
+        } else {
+            const int at_once = PJ_SHRINK_COLS / p.bank.r_pad;
+            // batches of adapters side by side while there are SMs for them, one behind the other beyond
+            const int batches = (std::min(p.n_slots, PJ_ROWS) + at_once - 1) / at_once;
+            p.batches = std::max(1, std::min(batches, sm_count() / row_tiles));
+            e = launch(k_plan_tiles, dim3(row_tiles), 128, 0, stream, p);
+            if (e == cudaSuccess) e = project_tiles<TYPE, PJ_SHRINK_COLS, true>(p, stream);
+        }
         if (e != cudaSuccess) return e;
     }
     // Tiles of 32 columns where those of 128 would leave most SMs without one.
-    const int64_t wide = (int64_t)((p.n + 127) / 128) * ((p.rows + PJ_ROWS - 1) / PJ_ROWS);
-    return wide >= sm_count() / 2 ? project_tiles<TYPE, 128>(p, stream) : project_tiles<TYPE, 32>(p, stream);
+    const int64_t wide = (int64_t)((p.n + 127) / 128) * row_tiles;
+    return wide >= sm_count() / 2 ? project_tiles<TYPE, 128, false>(p, stream) : project_tiles<TYPE, 32, false>(p, stream);
 }
 
 }  // namespace rp
@@ -638,8 +850,7 @@ extern "C" int64_t ripple_project_layout_bytes(int32_t type, int32_t k, int32_t 
 
 extern "C" int64_t ripple_adapter_bytes(int32_t type, int32_t k, int32_t n, int32_t slots, int32_t max_rank) {
     if (!shape_ok(type, k, n) || !bank_ok(slots, max_rank)) return -1;
-    const int size = type_size(type);
-    return bank_b_at(size, k, slots, max_rank) + up128((int64_t)slots * n * pj_up(max_rank, 16) * size);
+    return bank_b_at(type, k, slots, max_rank) + up128((int64_t)slots * n * pj_up(max_rank, 16) * pj_b_planes(type) * 2);
 }
 
 extern "C" ripple_status ripple_project_layout(int32_t type, int32_t k, int32_t n, const void* W, int64_t ld_w, void* layout,
@@ -674,7 +885,7 @@ extern "C" ripple_status ripple_adapter_set(void* bank, int32_t type, int32_t k,
     OnDevice on(device);
     if (on.err != cudaSuccess) return launch_failed("cudaSetDevice", on.err);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const BankView v = bank_view(bank, size, k, slots, max_rank);
+    const BankView v = bank_view(bank, type, k, slots, max_rank);
     SlotInfo* info = const_cast<SlotInfo*>(v.info);
     // (the 128 bytes behind the slots' table: the flag)
     int* bad = reinterpret_cast<int*>(static_cast<uint8_t*>(bank) + bank_a_at(slots) - 128);
@@ -683,10 +894,10 @@ extern "C" ripple_status ripple_adapter_set(void* bank, int32_t type, int32_t k,
     cudaError_t e = cudaMemsetAsync(bad, 0, sizeof(int), st);
     if (e == cudaSuccess && rank > 0) {
         const dim3 grid(592);
-        uint8_t *a = const_cast<uint8_t*>(v.a), *b = const_cast<uint8_t*>(v.b);
-        if (type == RIPPLE_TYPE_F32) e = launch(k_set_adapters<float>, grid, 256, 0, cuda_stream, a, b, (const float*)A, (const float*)B, first, count, rank, k, n, v.r_pad, v.k_pad, bad);
-        else if (type == RIPPLE_TYPE_BF16) e = launch(k_set_adapters<__nv_bfloat16>, grid, 256, 0, cuda_stream, a, b, (const __nv_bfloat16*)A, (const __nv_bfloat16*)B, first, count, rank, k, n, v.r_pad, v.k_pad, bad);
-        else e = launch(k_set_adapters<__half>, grid, 256, 0, cuda_stream, a, b, (const __half*)A, (const __half*)B, first, count, rank, k, n, v.r_pad, v.k_pad, bad);
+        uint16_t *a = const_cast<uint16_t*>(v.a), *b = const_cast<uint16_t*>(v.b);
+        if (type == RIPPLE_TYPE_F32) e = launch(k_set_adapters<RIPPLE_TYPE_F32>, grid, 256, 0, cuda_stream, a, b, (const float*)A, (const float*)B, first, count, rank, k, n, v.r_pad, v.k_pad, bad);
+        else if (type == RIPPLE_TYPE_BF16) e = launch(k_set_adapters<RIPPLE_TYPE_BF16>, grid, 256, 0, cuda_stream, a, b, (const __nv_bfloat16*)A, (const __nv_bfloat16*)B, first, count, rank, k, n, v.r_pad, v.k_pad, bad);
+        else e = launch(k_set_adapters<RIPPLE_TYPE_F16>, grid, 256, 0, cuda_stream, a, b, (const __half*)A, (const __half*)B, first, count, rank, k, n, v.r_pad, v.k_pad, bad);
         if (e == cudaSuccess) e = cudaMemcpyAsync(&host_bad, bad, sizeof(int), cudaMemcpyDeviceToHost, st);
         if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     }
@@ -705,7 +916,7 @@ extern "C" int64_t ripple_project_workspace_bytes(const ripple_project_rows_args
     if (!a || a->rows < 0 || !shape_ok(a->type, a->k, a->n)) return -1;
     if (!a->bank) return 0;
     if (!bank_ok(a->n_slots, a->max_rank)) return -1;
-    return up128(a->rows * pj_up(a->max_rank, 16) * 4);
+    return (a->rows + 127) / 128 * (int64_t)sizeof(TilePlan) + up128(a->rows * pj_up(a->max_rank, 16) * 4);
 }
 
 extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) {
@@ -741,8 +952,10 @@ extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) 
     p.rows = (int)a->rows, p.k = a->k, p.n = a->n, p.act = a->act, p.chunks = pj_up(a->k, PJ_KC) / PJ_KC;
     p.x = a->x, p.ld_x = a->ld_x, p.x_rows = a->x_rows, p.ids = a->ids;
     p.layout = static_cast<const uint8_t*>(a->layout), p.bias = a->bias;
-    if (a->bank) p.bank = bank_view(a->bank, size, a->k, a->n_slots, a->max_rank);
-    p.n_slots = a->n_slots, p.slots = a->slots, p.t = static_cast<float*>(a->workspace);
+    if (a->bank) p.bank = bank_view(a->bank, a->type, a->k, a->n_slots, a->max_rank);
+    p.n_slots = a->n_slots, p.slots = a->slots, p.plan = static_cast<TilePlan*>(a->workspace);
+    if (a->bank) p.t = static_cast<uint8_t*>(a->workspace) + (a->rows + 127) / 128 * (int64_t)sizeof(TilePlan);
+    else p.plan = nullptr;
     p.y = a->y, p.ld_y = a->ld_y, p.out_f32 = a->out_type == RIPPLE_TYPE_F32;
     cudaError_t e;
     if (a->type == RIPPLE_TYPE_F32) e = project<RIPPLE_TYPE_F32>(p, a->cuda_stream);
