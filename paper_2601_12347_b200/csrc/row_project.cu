@@ -10,7 +10,7 @@ namespace rp {
 // ---- what a layout and a bank hold ---------------------------------------------------------------------------------
 // Layout of W: its transpose (output columns are rows, K runs along a row), cut into groups of PJ_COLS columns and chunks
 // of PJ_KC entries of K.  A chunk is PJ_COLS rows of 128 bytes in the swizzle that the tensor core reads, zeros beyond K and n;
-// fp32 weights are three chunks, one per bf16 part.
+// fp32 weights are three chunks, one per bf16 part.  Behind the chunks W itself, k x n, for calls of few rows.
 constexpr int PJ_COLS = 128, PJ_KC = 64;
 constexpr int PJ_CHUNK = PJ_COLS * 128;
 // Bank: scale and rank of every slot; A transposed (rank x K, zeros beyond both; fp32 as three planes of bf16 parts); B transposed
@@ -21,6 +21,10 @@ __host__ __device__ inline int pj_parts(int type) { return type == RIPPLE_TYPE_F
 __host__ __device__ constexpr int pj_b_planes(int type) { return type == RIPPLE_TYPE_F32 ? 3 : type == RIPPLE_TYPE_F16 ? 2 : 1; }
 __host__ __device__ inline int pj_up(int x, int to) { return (x + to - 1) / to * to; }
 __host__ __device__ inline int64_t up128(int64_t x) { return (x + 127) / 128 * 128; }
+
+__host__ __device__ inline int64_t layout_plain_at(int type, int k, int n) {
+    return (int64_t)(pj_up(n, PJ_COLS) / PJ_COLS) * (pj_up(k, PJ_KC) / PJ_KC) * pj_parts(type) * PJ_CHUNK;
+}
 
 struct BankView {
     const SlotInfo* info;
@@ -47,10 +51,21 @@ __device__ __forceinline__ void pj_parts_of(float x, __nv_bfloat16 (&h)[3]) {
     h[2] = __float2bfloat16_rn(left - __bfloat162float(h[1]));
 }
 
+// two values; the remainders of an infinite one are NaN (the epilogue drops the small products where the large one is not finite)
+__device__ __forceinline__ void pj_parts_of2(float x0, float x1, uint32_t& a, uint32_t& b, uint32_t& c) {
+    asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(a) : "f"(x1), "f"(x0));
+    x0 -= __uint_as_float(a << 16), x1 -= __uint_as_float(a & 0xffff0000u);
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b) : "f"(x1), "f"(x0));
+    x0 -= __uint_as_float(b << 16), x1 -= __uint_as_float(b & 0xffff0000u);
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(c) : "f"(x1), "f"(x0));
+}
+
 // one thread per 16-byte piece of a 16-bit chunk: eight entries of K of one output column
 template <typename T>
-__global__ void k_layout_weights(const T* W, int64_t ld, int k, int n, uint8_t* out, int chunks, int groups) {
+__global__ void k_layout_weights(const T* W, int64_t ld, int k, int n, uint8_t* out, int chunks, int groups, T* plain) {
     pdl_enter();
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < (int64_t)k * n; i += (int64_t)gridDim.x * blockDim.x)
+        plain[i] = W[i / n * ld + i % n];
     const int parts = sizeof(T) == 4 ? 3 : 1;
     const int64_t pieces = (int64_t)groups * chunks * PJ_COLS * 8;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * blockDim.x) {
@@ -138,6 +153,7 @@ struct ProjectParams {
     int64_t ld_x, x_rows;
     const int32_t* ids;
     const uint8_t* layout;
+    const void* plain;     // W, k x n
     const float* bias;
     BankView bank;         // info null: no adapters
     int n_slots;
@@ -204,36 +220,202 @@ __device__ __forceinline__ void store_t(const ProjectParams& p, int64_t i, int r
     }
 }
 
-// Few rows: t_i by a block per row, a warp per rank; the blocks in front plan the tiles.
-template <int TYPE>
-__global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ ProjectParams p) {
+// eight neighbouring entries as fp32
+__device__ __forceinline__ void load8(float (&v)[8], const float* from) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float4 e = __ldg(reinterpret_cast<const float4*>(from) + i);
+        v[4 * i] = e.x, v[4 * i + 1] = e.y, v[4 * i + 2] = e.z, v[4 * i + 3] = e.w;
+    }
+}
+__device__ __forceinline__ float2 two_of(uint32_t x, __nv_bfloat16) { return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
+__device__ __forceinline__ float2 two_of(uint32_t x, __half) {
+    return make_float2(__half2float(__ushort_as_half((unsigned short)(x & 0xffff))), __half2float(__ushort_as_half((unsigned short)(x >> 16))));
+}
+template <typename T> __device__ __forceinline__ void load8(float (&v)[8], const T* from) {
+    const uint4 e = __ldg(reinterpret_cast<const uint4*>(from));
+    const float2 a = two_of(e.x, T()), b = two_of(e.y, T()), c = two_of(e.z, T()), d = two_of(e.w, T());
+    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
+}
+
+// Few rows: t_i by a block per ROWS rows, a warp per four ranks, eight entries of K per lane; rows of one adapter share its loads.
+// The blocks in front plan the tiles (of the tensor-core form).
+template <int TYPE, int ROWS>
+__global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ ProjectParams p, int planned) {
     using T = typename Elem<TYPE>::T;
-    constexpr int PA = TYPE == RIPPLE_TYPE_F32 ? 3 : 1;
+    constexpr int PA = TYPE == RIPPLE_TYPE_F32 ? 3 : 1, RANKS = 4;
     pdl_enter();
-    const int tiles = (p.rows + 127) / 128;
-    if ((int)blockIdx.x < tiles) return plan_tile(p, blockIdx.x);
-    const int i = blockIdx.x - tiles, lane = lane_id();
-    const int64_t from = row_of(p, i);
-    const int a = slot_of(p, i);
-    if (from < 0 || a < 0) return;
-    const T* const x = static_cast<const T*>(p.x) + from * p.ld_x;
-    const SlotInfo info = p.bank.info[a];
+    if ((int)blockIdx.x < planned) return plan_tile(p, blockIdx.x);
+    const int i0 = (blockIdx.x - planned) * ROWS, lane = lane_id();
+    const T* x[ROWS];
+    int slot[ROWS];
+    bool vec = true;
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) {
+        const int64_t from = i0 + q < p.rows ? row_of(p, i0 + q) : -1;
+        slot[q] = from >= 0 ? slot_of(p, i0 + q) : -1;
+        x[q] = static_cast<const T*>(p.x) + max(from, (int64_t)0) * p.ld_x;
+        vec = vec && (reinterpret_cast<uintptr_t>(x[q]) & 15) == 0;
+    }
     const int64_t plane = (int64_t)p.bank.r_pad * p.bank.k_pad;
-    for (int r = threadIdx.x >> 5; r < p.bank.r_pad; r += 4) {
-        float sum = 0.f;
-        if (r < info.rank) {
-            const uint16_t* const w = p.bank.a + (int64_t)a * PA * plane + (int64_t)r * p.bank.k_pad;
-            for (int kk = lane; kk < p.k; kk += 32) {
-                float v;
-                if constexpr (PA == 3)
-                    v = __uint_as_float((uint32_t)w[kk + 2 * plane] << 16) + __uint_as_float((uint32_t)w[kk + plane] << 16) + __uint_as_float((uint32_t)w[kk] << 16);
-                else
-                    v = to_f32(reinterpret_cast<const T*>(w)[kk]);
-                sum += to_f32(x[kk]) * v;
-            }
-            sum = warp_sum(sum) * info.scale;
+    for (;;) {
+        int a = -1;                          // the first adapter that is left, and its rows
+#pragma unroll
+        for (int q = ROWS - 1; q >= 0; --q) a = slot[q] >= 0 ? slot[q] : a;
+        if (a < 0) break;
+        bool mine[ROWS];
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) {
+            mine[q] = slot[q] == a;
+            if (mine[q]) slot[q] = -1;
         }
-        if (lane == 0) store_t<TYPE>(p, i, r, sum);
+        const SlotInfo info = p.bank.info[a];
+        for (int r0 = (threadIdx.x >> 5) * RANKS; r0 < p.bank.r_pad; r0 += 4 * RANKS) {
+            const uint16_t* const w = p.bank.a + (int64_t)a * PA * plane + (int64_t)r0 * p.bank.k_pad;
+            float sum[ROWS][RANKS] = {};
+            if (r0 < info.rank) {
+                for (int kk = lane * 8; kk < p.k; kk += 256) {
+                    float xv[ROWS][8];
+#pragma unroll
+                    for (int q = 0; q < ROWS; ++q) {
+                        if (vec && kk + 8 <= p.k) {
+                            load8(xv[q], x[q] + kk);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) xv[q][e] = kk + e < p.k ? to_f32(x[q][kk + e]) : 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int r = 0; r < RANKS; ++r) {
+                        float wv[8];
+                        if constexpr (PA == 3) {
+                            float part[8];
+                            load8(wv, reinterpret_cast<const __nv_bfloat16*>(w) + 2 * plane + r * p.bank.k_pad + kk);
+#pragma unroll
+                            for (int h = 1; h >= 0; --h) {
+                                load8(part, reinterpret_cast<const __nv_bfloat16*>(w) + h * plane + r * p.bank.k_pad + kk);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) wv[e] += part[e];
+                            }
+                        } else {
+                            load8(wv, reinterpret_cast<const T*>(w) + r * p.bank.k_pad + kk);
+                        }
+#pragma unroll
+                        for (int q = 0; q < ROWS; ++q)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) sum[q][r] = fmaf(xv[q][e], wv[e], sum[q][r]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < ROWS; ++q) {
+                if (!mine[q]) continue;
+#pragma unroll
+                for (int r = 0; r < RANKS; ++r) sum[q][r] = warp_sum(sum[q][r]);
+                // (entries beyond the rank are zeros whatever the row holds)
+                if (lane < RANKS) {
+                    float t = sum[q][0];
+#pragma unroll
+                    for (int r = 1; r < RANKS; ++r) t = lane == r ? sum[q][r] : t;
+                    store_t<TYPE>(p, i0 + q, r0 + lane, r0 + lane < info.rank ? t * info.scale : 0.f);
+                }
+            }
+        }
+    }
+}
+
+// Few rows: 16 rows x 32 columns of y per block.  A lane is a column, a warp an eighth of every 512 entries of K; what the warps
+// have summed meets in shared memory, where each finishes two rows: t_i B_a, bias, activation.  Sums in fp32 throughout.
+// Latency is all that counts here: one load of W and sixteen products per entry of K and lane, and no pipeline to fill.
+constexpr int PF_ROWS = 16, PF_COLS = 32, PF_K = 512, PF_LD = 20;
+template <int TYPE>
+__global__ void __launch_bounds__(256) k_project_few(const __grid_constant__ ProjectParams p) {
+    using T = typename Elem<TYPE>::T;
+    constexpr int B_PLANES = pj_b_planes(TYPE);
+    if (!p.bank.info) pdl_enter();       // with adapters the kernel before computes t: what it waited for is there, t is waited for below
+    __shared__ __align__(16) float xs[PF_K * PF_LD];
+    __shared__ int64_t from[PF_ROWS];
+    const int warp = threadIdx.x >> 5, lane = lane_id(), i0 = blockIdx.x * PF_ROWS, col = blockIdx.y * PF_COLS + lane;
+    if (threadIdx.x < PF_ROWS) from[threadIdx.x] = i0 + (int)threadIdx.x < p.rows ? row_of(p, i0 + threadIdx.x) : -1;
+    __syncthreads();
+    const T* const w = static_cast<const T*>(p.plain) + min(col, p.n - 1);
+    float sum[PF_ROWS] = {};
+    for (int k0 = 0; k0 < p.k; k0 += PF_K) {
+        const int here = min(PF_K, p.k - k0);
+        // thread: a row and every 16th entry; all of its loads before the first is used
+        {
+            const int r = threadIdx.x >> 4, k1 = threadIdx.x & 15;
+            const int64_t at = from[r];
+            const T* const x = static_cast<const T*>(p.x) + max(at, (int64_t)0) * p.ld_x + k0;
+#pragma unroll
+            for (int half = 0; half < PF_K; half += PF_K / 2) {
+                T v[PF_K / 32];
+#pragma unroll
+                for (int e = 0; e < PF_K / 32; ++e) v[e] = at >= 0 && half + k1 + 16 * e < here ? x[half + k1 + 16 * e] : from_f32<T>(0.f);
+#pragma unroll
+                for (int e = 0; e < PF_K / 32; ++e) if (half + k1 + 16 * e < here) xs[(half + k1 + 16 * e) * PF_LD + r] = to_f32(v[e]);
+            }
+        }
+        __syncthreads();
+        const int per = (here + 7) / 8, end = min((warp + 1) * per, here);
+#pragma unroll 8
+        for (int kk = warp * per; kk < end; ++kk) {
+            const float wv = to_f32(w[(int64_t)(k0 + kk) * p.n]);
+#pragma unroll
+            for (int r = 0; r < PF_ROWS; r += 4) {
+                const float4 x = *reinterpret_cast<const float4*>(xs + kk * PF_LD + r);
+                sum[r] = fmaf(x.x, wv, sum[r]), sum[r + 1] = fmaf(x.y, wv, sum[r + 1]);
+                sum[r + 2] = fmaf(x.z, wv, sum[r + 2]), sum[r + 3] = fmaf(x.w, wv, sum[r + 3]);
+            }
+        }
+        __syncthreads();
+    }
+    float* const part = xs;              // warp x row x column
+#pragma unroll
+    for (int r = 0; r < PF_ROWS; ++r) part[(warp * PF_ROWS + r) * PF_COLS + lane] = sum[r];
+    if (p.bank.info) pdl_enter();
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int r = 2 * warp + h, i = i0 + r;
+        if (i >= p.rows || from[r] < 0) continue;
+        float y = 0.f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) y += part[(q * PF_ROWS + r) * PF_COLS + lane];
+        if (p.bias) y += p.bias[min(col, p.n - 1)];
+        const int a = p.bank.info ? slot_of(p, i) : -1;
+        if (a >= 0) {
+            const int rp = p.bank.r_pad, rank = p.bank.info[a].rank;
+            const int64_t plane = (int64_t)p.n * rp;
+            const __nv_bfloat16* const b = reinterpret_cast<const __nv_bfloat16*>(p.bank.b) + (int64_t)a * B_PLANES * plane + (int64_t)min(col, p.n - 1) * rp;
+            float d = 0.f;
+            for (int k = 0; k < rank; k += 8) {
+                float t[8], bv[8], more[8];
+                if constexpr (TYPE == RIPPLE_TYPE_F32) {
+                    load8(t, static_cast<const float*>(p.t) + (int64_t)i * rp + k);
+                } else {
+                    load8(t, static_cast<const __nv_bfloat16*>(p.t) + (int64_t)i * 2 * rp + k);
+                    load8(more, static_cast<const __nv_bfloat16*>(p.t) + (int64_t)i * 2 * rp + rp + k);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) t[e] += more[e];
+                }
+                load8(bv, b + (B_PLANES - 1) * plane + k);
+#pragma unroll
+                for (int q = B_PLANES - 2; q >= 0; --q) {
+                    load8(more, b + q * plane + k);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) bv[e] += more[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d = fmaf(t[e], bv[e], d);
+            }
+            y += d;
+        }
+        if (p.act == RIPPLE_ACT_RELU && y < 0.f) y = 0.f;
+        if (col < p.n) {
+            if (p.out_f32) static_cast<float*>(p.y)[(int64_t)i * p.ld_y + col] = y;
+            else static_cast<T*>(p.y)[(int64_t)i * p.ld_y + col] = from_f32<T>(y);
+        }
     }
 }
 
@@ -246,6 +428,7 @@ constexpr int PJ_LOADERS = 256;          // threads that fetch rows
 constexpr int PJ_EPI_WARPS = 8;          // two per quarter of the lanes
 constexpr int PJ_THREADS = PJ_LOADERS + 32 * PJ_EPI_WARPS + 64;   // and the warps that issue and that fetch weights
 constexpr int PJ_FEW = 1024;             // rows up to which t is computed a block per row
+constexpr int64_t PJ_FEW_PRODUCTS = 64 << 20;   // rows x K x n up to which y is summed without tensor cores
 constexpr int PJ_SHRINK_COLS = 64;       // ranks of adapters side by side, where t is computed on the tensor cores
 constexpr int PJ_UNIT = 4;               // fp32: chunks (256 entries of K) whose large products share an accumulator
 constexpr uint32_t PJ_SPIN_LIMIT = 1u << 22;
@@ -267,15 +450,25 @@ __device__ __forceinline__ uint32_t pj_idesc(int type, int n) {
     return (1u << 4) | (t << 7) | (t << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(PJ_ROWS >> 4) << 24);
 }
 
+__device__ __forceinline__ uint16_t bits_of(__nv_bfloat16 x) { return __bfloat16_as_ushort(x); }
+__device__ __forceinline__ uint16_t bits_of(__half x) { return __half_as_ushort(x); }
+
 __device__ __forceinline__ void pj_store8(void* to, const uint32_t (&v)[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
 template <typename T> __device__ __forceinline__ uint32_t pj_pair(float a, float b) {
-    Piece<T, 2> v;
-    v.v[0] = from_f32<T>(a), v.v[1] = from_f32<T>(b);
-    return *reinterpret_cast<uint32_t*>(&v);
+    return (uint32_t)bits_of(from_f32<T>(a)) | (uint32_t)bits_of(from_f32<T>(b)) << 16;
+}
+
+// 16 bytes of eight entries
+__device__ __forceinline__ uint4 word_of(const Piece<float, 8>& v, int h) {
+    return make_uint4(__float_as_uint(v.v[4 * h]), __float_as_uint(v.v[4 * h + 1]), __float_as_uint(v.v[4 * h + 2]), __float_as_uint(v.v[4 * h + 3]));
+}
+template <typename T> __device__ __forceinline__ uint4 word_of(const Piece<T, 8>& v, int) {
+    auto two = [&](int e) { return (uint32_t)bits_of(v.v[e]) | (uint32_t)bits_of(v.v[e + 1]) << 16; };
+    return make_uint4(two(0), two(2), two(4), two(6));
 }
 
 // A persistent CTA takes tiles of 128 rows x BN columns: lanes of the accumulator are rows, its columns output columns.
@@ -357,20 +550,20 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
         const bool regs = PARTS == 3 || !vec;
         // rank steps: this thread's piece of a step is a plane's ranks from c_rank
         const int c_plane = PARTS == 3 ? 0 : c >> 2, c_rank = PARTS == 3 ? c * 8 : (c & 3) * 8;
-        // rows (null: nothing to read) and adapters of this tile and the next
-        const T *row[ITS], *next[ITS];
+        // rows of x (negative: nothing to read) and adapters of this tile and the next
+        const T* const x0 = static_cast<const T*>(p.x) + c * 8;
+        int row[ITS], next[ITS];
         uint32_t which = 0, which_next = 0;         // the rows' places among the adapters, a byte each
         int slot0 = 0, slot0_next = 0, slot1 = 0, slot1_next = 0;
         auto aim = [&](const Tile& t) {
 #pragma unroll
-            for (int it = 0; it < ITS; ++it) next[it] = nullptr;
+            for (int it = 0; it < ITS; ++it) next[it] = -1;
             if (t.lt >= my_tiles) return;
             const int r0 = t.rows * PJ_ROWS + rb;
 #pragma unroll
             for (int it = 0; it < ITS; ++it) {
                 const int i = r0 + RSTEP * it;
-                const int64_t from = i < p.rows ? row_of(p, i) : -1;
-                if (from >= 0) next[it] = static_cast<const T*>(p.x) + from * p.ld_x + c * 8;
+                if (i < p.rows) next[it] = (int)row_of(p, i);
             }
             if (!p.plan) return;
             const TilePlan& plan = p.plan[t.rows];
@@ -386,19 +579,22 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
                 slot0_next = j < t.count ? plan.slot[j] : -1;
             }
         };
-        T raw[ITS][8];
-        auto fetch = [&](const T* const (&rows)[ITS], int kc) {
+        constexpr int WORDS = sizeof(T) / 2;        // 16-byte words of eight entries
+        uint4 raw[ITS][WORDS];
+        auto fetch = [&](const int (&rows)[ITS], int kc) {
             const int left = p.k - kc * PJ_KC - c * 8;
 #pragma unroll
             for (int it = 0; it < ITS; ++it) {
-                const T* const from = rows[it] + kc * PJ_KC;
-                if (vec && left >= 8 && rows[it]) {
+                const T* const from = x0 + max(rows[it], 0) * p.ld_x + kc * PJ_KC;
+                if (vec && left >= 8 && rows[it] >= 0) {
 #pragma unroll
-                    for (int e = 0; e < 8; e += 16 / (int)sizeof(T))
-                        *reinterpret_cast<uint4*>(&raw[it][e]) = __ldg(reinterpret_cast<const uint4*>(from + e));
+                    for (int h = 0; h < WORDS; ++h) raw[it][h] = __ldg(reinterpret_cast<const uint4*>(from) + h);
                 } else {
+                    Piece<T, 8> v;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) raw[it][e] = rows[it] && e < left ? from[e] : from_f32<T>(0.f);
+                    for (int e = 0; e < 8; ++e) v.v[e] = rows[it] >= 0 && e < left ? from[e] : from_f32<T>(0.f);
+#pragma unroll
+                    for (int h = 0; h < WORDS; ++h) raw[it][h] = word_of(v, h);
                 }
             }
         };
@@ -410,9 +606,9 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
 #pragma unroll
                 for (int it = 0; it < ITS; ++it) {
                     const bool own = (int)(which >> (8 * it) & 255) == j;
-                    const float4* const from = reinterpret_cast<const float4*>(static_cast<const float*>(p.t) + (i0 + RSTEP * it) * r_pad + r);
+                    const uint4* const from = reinterpret_cast<const uint4*>(static_cast<const float*>(p.t) + (i0 + RSTEP * it) * r_pad + r);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) *reinterpret_cast<float4*>(&raw[it][4 * h]) = own ? __ldg(from + h) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int h = 0; h < WORDS; ++h) raw[it][h] = own ? __ldg(from + h) : make_uint4(0, 0, 0, 0);
                 }
             }
         };
@@ -421,17 +617,17 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
             for (int it = 0; it < ITS; ++it) {
                 uint8_t* const to = ring + s * S::STAGE + it * (RSTEP * 128) + tc_swz(rb, c);
                 if constexpr (PARTS == 3) {
-                    Piece<__nv_bfloat16, 8> part[3];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        __nv_bfloat16 h[3];
-                        pj_parts_of(raw[it][e], h);
-                        part[0].v[e] = h[0], part[1].v[e] = h[1], part[2].v[e] = h[2];
-                    }
-#pragma unroll
-                    for (int q = 0; q < 3; ++q) *reinterpret_cast<Piece<__nv_bfloat16, 8>*>(to + q * S::X_PART) = part[q];
+                    uint4 a, b, d;
+                    auto f = [](uint32_t x) { return __uint_as_float(x); };
+                    pj_parts_of2(f(raw[it][0].x), f(raw[it][0].y), a.x, b.x, d.x);
+                    pj_parts_of2(f(raw[it][0].z), f(raw[it][0].w), a.y, b.y, d.y);
+                    pj_parts_of2(f(raw[it][WORDS - 1].x), f(raw[it][WORDS - 1].y), a.z, b.z, d.z);
+                    pj_parts_of2(f(raw[it][WORDS - 1].z), f(raw[it][WORDS - 1].w), a.w, b.w, d.w);
+                    *reinterpret_cast<uint4*>(to) = a;
+                    *reinterpret_cast<uint4*>(to + S::X_PART) = b;
+                    *reinterpret_cast<uint4*>(to + 2 * S::X_PART) = d;
                 } else {
-                    *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(&raw[it][0]);
+                    *reinterpret_cast<uint4*>(to) = raw[it][0];
                 }
             }
         };
@@ -464,7 +660,7 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
                         const uint32_t bytes = left >= 8 ? 16u : left > 0 ? 2u * left : 0u;
 #pragma unroll
                         for (int it = 0; it < ITS; ++it)
-                            if (row[it]) copy(x_to + it * (RSTEP * 128), bytes ? row[it] + st * PJ_KC : row[it], bytes);
+                            if (row[it] >= 0) copy(x_to + it * (RSTEP * 128), x0 + row[it] * p.ld_x + (bytes ? st * PJ_KC : 0), bytes);
                     }
                     if constexpr (SHRINK) {
                         const int64_t plane = (int64_t)r_pad * p.bank.k_pad;
@@ -806,10 +1002,14 @@ static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
 template <int TYPE>
 static cudaError_t project(ProjectParams p, void* stream) {
     const int row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
+    const bool few = (int64_t)p.rows * p.k * p.n <= PJ_FEW_PRODUCTS && p.rows <= PJ_FEW;
     if (p.bank.info) {
         cudaError_t e;
         if (p.rows <= PJ_FEW) {
-            e = launch(k_shrink_few<TYPE>, dim3(row_tiles + p.rows), 128, 0, stream, p);
+            const int planned = few ? 0 : row_tiles;
+            // (four rows per block once there are several blocks for every SM)
+            if (p.rows <= 4 * sm_count()) e = launch(k_shrink_few<TYPE, 1>, dim3(planned + p.rows), 128, 0, stream, p, planned);
+            else e = launch(k_shrink_few<TYPE, 4>, dim3(planned + (p.rows + 3) / 4), 128, 0, stream, p, planned);
         } else {
             const int at_once = PJ_SHRINK_COLS / p.bank.r_pad;
             // batches of adapters side by side while there are SMs for them, one behind the other beyond
@@ -820,6 +1020,7 @@ static cudaError_t project(ProjectParams p, void* stream) {
         }
         if (e != cudaSuccess) return e;
     }
+    if (few) return launch(k_project_few<TYPE>, dim3((p.rows + PF_ROWS - 1) / PF_ROWS, (p.n + PF_COLS - 1) / PF_COLS), 256, 0, stream, p);
     // Tiles of 32 columns where those of 128 would leave most SMs without one.
     const int64_t wide = (int64_t)((p.n + 127) / 128) * row_tiles;
     return wide >= sm_count() / 2 ? project_tiles<TYPE, 128, false>(p, stream) : project_tiles<TYPE, 32, false>(p, stream);
@@ -845,7 +1046,7 @@ static bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_
 
 extern "C" int64_t ripple_project_layout_bytes(int32_t type, int32_t k, int32_t n) {
     if (!shape_ok(type, k, n)) return -1;
-    return (int64_t)(pj_up(n, PJ_COLS) / PJ_COLS) * (pj_up(k, PJ_KC) / PJ_KC) * pj_parts(type) * PJ_CHUNK;
+    return layout_plain_at(type, k, n) + up128((int64_t)k * n * type_size(type));
 }
 
 extern "C" int64_t ripple_adapter_bytes(int32_t type, int32_t k, int32_t n, int32_t slots, int32_t max_rank) {
@@ -862,10 +1063,11 @@ extern "C" ripple_status ripple_project_layout(int32_t type, int32_t k, int32_t 
     if (on.err != cudaSuccess) return launch_failed("cudaSetDevice", on.err);
     const int chunks = pj_up(k, PJ_KC) / PJ_KC, groups = pj_up(n, PJ_COLS) / PJ_COLS;
     const dim3 grid((unsigned)std::min<int64_t>((int64_t)groups * chunks * PJ_COLS * 8 / 256, 1184));
+    uint8_t* const plain = static_cast<uint8_t*>(layout) + layout_plain_at(type, k, n);
     cudaError_t e;
-    if (type == RIPPLE_TYPE_F32) e = launch(k_layout_weights<float>, grid, 256, 0, cuda_stream, (const float*)W, ld_w, k, n, (uint8_t*)layout, chunks, groups);
-    else if (type == RIPPLE_TYPE_BF16) e = launch(k_layout_weights<__nv_bfloat16>, grid, 256, 0, cuda_stream, (const __nv_bfloat16*)W, ld_w, k, n, (uint8_t*)layout, chunks, groups);
-    else e = launch(k_layout_weights<__half>, grid, 256, 0, cuda_stream, (const __half*)W, ld_w, k, n, (uint8_t*)layout, chunks, groups);
+    if (type == RIPPLE_TYPE_F32) e = launch(k_layout_weights<float>, grid, 256, 0, cuda_stream, (const float*)W, ld_w, k, n, (uint8_t*)layout, chunks, groups, (float*)plain);
+    else if (type == RIPPLE_TYPE_BF16) e = launch(k_layout_weights<__nv_bfloat16>, grid, 256, 0, cuda_stream, (const __nv_bfloat16*)W, ld_w, k, n, (uint8_t*)layout, chunks, groups, (__nv_bfloat16*)plain);
+    else e = launch(k_layout_weights<__half>, grid, 256, 0, cuda_stream, (const __half*)W, ld_w, k, n, (uint8_t*)layout, chunks, groups, (__half*)plain);
     return e == cudaSuccess ? RIPPLE_OK : launch_failed("project_layout launch", e);
 }
 
@@ -952,6 +1154,7 @@ extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) 
     p.rows = (int)a->rows, p.k = a->k, p.n = a->n, p.act = a->act, p.chunks = pj_up(a->k, PJ_KC) / PJ_KC;
     p.x = a->x, p.ld_x = a->ld_x, p.x_rows = a->x_rows, p.ids = a->ids;
     p.layout = static_cast<const uint8_t*>(a->layout), p.bias = a->bias;
+    p.plain = p.layout + layout_plain_at(a->type, a->k, a->n);
     if (a->bank) p.bank = bank_view(a->bank, a->type, a->k, a->n_slots, a->max_rank);
     p.n_slots = a->n_slots, p.slots = a->slots, p.plan = static_cast<TilePlan*>(a->workspace);
     if (a->bank) p.t = static_cast<uint8_t*>(a->workspace) + (a->rows + 127) / 128 * (int64_t)sizeof(TilePlan);

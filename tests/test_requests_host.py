@@ -123,8 +123,8 @@ def test_project_rows_refuses(lib, wrong):
 
 @no_device
 def test_layouts_and_banks_refuse(lib):
-    assert lib.ripple_project_layout_bytes(0, 100, 47) == 2 * 3 * 16384
-    assert lib.ripple_project_layout_bytes(1, 64, 129) == 2 * 16384
+    assert lib.ripple_project_layout_bytes(0, 100, 47) == 2 * 3 * 16384 + 18816      # chunks in three parts, and W to 128 bytes
+    assert lib.ripple_project_layout_bytes(1, 64, 129) == 2 * 16384 + 16512
     for bad in ((3, 8, 8), (0, 0, 8), (0, 8193, 8), (0, 8, 0), (0, 8, 65537)):
         assert lib.ripple_project_layout_bytes(*bad) == -1
         assert lib.ripple_adapter_bytes(*bad, 4, 8) == -1
