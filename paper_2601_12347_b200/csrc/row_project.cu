@@ -543,7 +543,7 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
     if (warp < PJ_LOADERS / 32) {
         // ---------------- rows, and what comes out of the bank ----------------
         constexpr int RSTEP = PJ_LOADERS / 8, ITS = PJ_ROWS / RSTEP, W_ITS = BN / RSTEP;
-        constexpr int LAG = PARTS == 3 ? 1 : STAGES - 2;        // steps whose copies are in flight
+        constexpr int LAG = PARTS == 3 ? 0 : STAGES / 2;        // steps whose copies are in flight when one is told to be there
         const int c = tid & 7, rb = tid >> 3;       // thread: piece c (8 entries) of the rows rb + RSTEP it
         const uint32_t mine = smem_u32(ring) + tc_swz(rb, c);
         const bool vec = (reinterpret_cast<uintptr_t>(p.x) & 15) == 0 && p.ld_x % (16 / (int)sizeof(T)) == 0;
