@@ -424,18 +424,20 @@ __global__ void __launch_bounds__(256) k_project_few(const __grid_constant__ Pro
 __device__ int g_request_timeout;
 
 constexpr int PJ_ROWS = 128;             // rows per tile: the lanes of the accumulator
-constexpr int PJ_LOADERS = 256;          // threads that fetch rows
 constexpr int PJ_EPI_WARPS = 8;          // two per quarter of the lanes
-constexpr int PJ_THREADS = PJ_LOADERS + 32 * PJ_EPI_WARPS + 64;   // and the warps that issue and that fetch weights
 constexpr int PJ_FEW = 1024;             // rows up to which t is computed a block per row
 constexpr int64_t PJ_FEW_PRODUCTS = 64 << 20;   // rows x K x n up to which y is summed without tensor cores
 constexpr int PJ_SHRINK_COLS = 64;       // ranks of adapters side by side, where t is computed on the tensor cores
 constexpr int PJ_UNIT = 4;               // fp32: chunks (256 entries of K) whose large products share an accumulator
 constexpr uint32_t PJ_SPIN_LIMIT = 1u << 22;
-constexpr int PJ_STAGING = PJ_EPI_WARPS * 32 * 17 * 4;
+constexpr int PJ_STAGING = PJ_EPI_WARPS * (32 * 17 + 128) * 4;    // the epilogue's turned blocks, and its bias
 
-template <int TYPE, int BN> struct PjShape {
+// MANY: fp32 rows of more than one unit, whose sums the epilogue carries in registers that twice the loader warps would need
+template <int TYPE, int BN, bool MANY> struct PjShape {
     static constexpr int PARTS = TYPE == RIPPLE_TYPE_F32 ? 3 : 1;
+    static constexpr int LOADERS = PARTS == 3 && !MANY ? 512 : 256;            // threads that fetch rows
+    static constexpr int THREADS = LOADERS + 32 * PJ_EPI_WARPS + 64;          // and the warps that issue and that fetch weights
+    static constexpr uint32_t TMEM = (PARTS == 3 ? 4 : 2) * BN;               // two accumulators and, fp32, two for the small products
     static constexpr int X_PART = PJ_ROWS * 128, X_STAGE = PARTS * X_PART;
     static constexpr int W_PART = BN * 128, W_STAGE = PARTS * W_PART;
     static constexpr int STAGE = X_STAGE + W_STAGE;
@@ -462,6 +464,10 @@ template <typename T> __device__ __forceinline__ uint32_t pj_pair(float a, float
     return (uint32_t)bits_of(from_f32<T>(a)) | (uint32_t)bits_of(from_f32<T>(b)) << 16;
 }
 
+__device__ __forceinline__ void pj_sts(uint32_t to, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
 // 16 bytes of eight entries
 __device__ __forceinline__ uint4 word_of(const Piece<float, 8>& v, int h) {
     return make_uint4(__float_as_uint(v.v[4 * h]), __float_as_uint(v.v[4 * h + 1]), __float_as_uint(v.v[4 * h + 2]), __float_as_uint(v.v[4 * h + 3]));
@@ -484,12 +490,13 @@ template <typename T> __device__ __forceinline__ uint4 word_of(const Piece<T, 8>
 // and summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
 // Barriers, all waits bounded: full_x[s] (one arrival per loader warp), full_w[s] (bytes), empty[s] (the products that read
 // stage s), acc_full[b], acc_empty[b] (one arrival per epilogue warp).
-template <int TYPE, int BN, bool SHRINK>
-__global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_constant__ ProjectParams p) {
+template <int TYPE, int BN, bool SHRINK, bool MANY>
+__global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project_rows(const __grid_constant__ ProjectParams p) {
     using T = typename Elem<TYPE>::T;
-    using S = PjShape<TYPE, BN>;
+    using S = PjShape<TYPE, BN, MANY>;
+    constexpr int PJ_LOADERS = S::LOADERS;
     constexpr int PARTS = S::PARTS, STAGES = S::STAGES, NB = BN / 32, RANKS = S::RANKS, B_PLANES = pj_b_planes(TYPE);
-    constexpr uint32_t TMEM = 4 * BN < 32 ? 32 : 4 * BN;       // two accumulators and, fp32, two for the small products
+    constexpr uint32_t TMEM = S::TMEM;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full_x[STAGES], full_w[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
     __shared__ uint32_t tmem_slot;
@@ -542,60 +549,76 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
 
     if (warp < PJ_LOADERS / 32) {
         // ---------------- rows, and what comes out of the bank ----------------
-        constexpr int RSTEP = PJ_LOADERS / 8, ITS = PJ_ROWS / RSTEP, W_ITS = BN / RSTEP;
+        constexpr int RSTEP = PJ_LOADERS / 8, ITS = PJ_ROWS / RSTEP, W_ITS = (BN + RSTEP - 1) / RSTEP;
         constexpr int LAG = PARTS == 3 ? 0 : STAGES / 2;        // steps whose copies are in flight when one is told to be there
         const int c = tid & 7, rb = tid >> 3;       // thread: piece c (8 entries) of the rows rb + RSTEP it
         const uint32_t mine = smem_u32(ring) + tc_swz(rb, c);
         const bool vec = (reinterpret_cast<uintptr_t>(p.x) & 15) == 0 && p.ld_x % (16 / (int)sizeof(T)) == 0;
         const bool regs = PARTS == 3 || !vec;
+        const int tail = p.k - (chunks - 1) * PJ_KC - c * 8;      // entries of this thread's piece of the last chunk
         // rank steps: this thread's piece of a step is a plane's ranks from c_rank
         const int c_plane = PARTS == 3 ? 0 : c >> 2, c_rank = PARTS == 3 ? c * 8 : (c & 3) * 8;
-        // rows of x (negative: nothing to read) and adapters of this tile and the next
+        // This thread's pieces of the rows of the tile being fetched, at its next chunk (rows that do not exist read row 0 of x, and
+        // their results are dropped); of the rows of A; the rows' places among the adapters, a byte each; and all of it for the next tile.
         const T* const x0 = static_cast<const T*>(p.x) + c * 8;
-        int row[ITS], next[ITS];
-        uint32_t which = 0, which_next = 0;         // the rows' places among the adapters, a byte each
-        int slot0 = 0, slot0_next = 0, slot1 = 0, slot1_next = 0;
+        const T* at[ITS];
+        const uint16_t* a_at[SHRINK ? W_ITS : 1];
+        int next[ITS], slot_next[SHRINK ? W_ITS : 1], slot0 = -1;
+        uint32_t which = 0, which_next = 0;
         auto aim = [&](const Tile& t) {
-#pragma unroll
-            for (int it = 0; it < ITS; ++it) next[it] = -1;
             if (t.lt >= my_tiles) return;
             const int r0 = t.rows * PJ_ROWS + rb;
 #pragma unroll
             for (int it = 0; it < ITS; ++it) {
                 const int i = r0 + RSTEP * it;
-                if (i < p.rows) next[it] = (int)row_of(p, i);
+                next[it] = i < p.rows ? max((int)row_of(p, i), 0) : 0;
             }
             if (!p.plan) return;
             const TilePlan& plan = p.plan[t.rows];
             if constexpr (SHRINK) {                 // slots of the rows of A that this thread fetches
-                const int j0 = t.part * at_once + rb / r_pad, j1 = t.part * at_once + (rb + RSTEP) / r_pad;
-                slot0_next = rb < at_once * r_pad && j0 < t.count ? plan.slot[j0] : -1;
-                slot1_next = rb + RSTEP < at_once * r_pad && j1 < t.count ? plan.slot[j1] : -1;
+#pragma unroll
+                for (int it = 0; it < W_ITS; ++it) {
+                    const int n = rb + RSTEP * it, j = t.part * at_once + n / r_pad;
+                    slot_next[it] = n < at_once * r_pad && j < t.count ? plan.slot[j] : -1;
+                }
             } else if (t.count) {
                 which_next = 0;
 #pragma unroll
                 for (int it = 0; it < ITS; ++it) which_next |= (uint32_t)plan.row[rb + RSTEP * it] << (8 * it);
                 const int j = c_rank / r_pad;
-                slot0_next = j < t.count ? plan.slot[j] : -1;
+                slot_next[0] = j < t.count ? plan.slot[j] : -1;
+            }
+        };
+        auto turn = [&]() {                         // to the next tile
+#pragma unroll
+            for (int it = 0; it < ITS; ++it) at[it] = x0 + next[it] * p.ld_x;
+            which = which_next;
+            if constexpr (SHRINK) {
+                const int64_t plane = (int64_t)r_pad * p.bank.k_pad;
+#pragma unroll
+                for (int it = 0; it < W_ITS; ++it)
+                    a_at[it] = slot_next[it] < 0 ? nullptr : p.bank.a + (int64_t)slot_next[it] * PARTS * plane + (int64_t)((rb + RSTEP * it) % r_pad) * p.bank.k_pad + c * 8;
+            } else {
+                slot0 = slot_next[0];
             }
         };
         constexpr int WORDS = sizeof(T) / 2;        // 16-byte words of eight entries
         uint4 raw[ITS][WORDS];
-        auto fetch = [&](const int (&rows)[ITS], int kc) {
-            const int left = p.k - kc * PJ_KC - c * 8;
+        auto fetch = [&](bool last) {               // the next chunk of the rows, through registers
+            const int left = last ? tail : 8;
 #pragma unroll
             for (int it = 0; it < ITS; ++it) {
-                const T* const from = x0 + max(rows[it], 0) * p.ld_x + kc * PJ_KC;
-                if (vec && left >= 8 && rows[it] >= 0) {
+                if (vec && left >= 8) {
 #pragma unroll
-                    for (int h = 0; h < WORDS; ++h) raw[it][h] = __ldg(reinterpret_cast<const uint4*>(from) + h);
+                    for (int h = 0; h < WORDS; ++h) raw[it][h] = __ldg(reinterpret_cast<const uint4*>(at[it]) + h);
                 } else {
                     Piece<T, 8> v;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v.v[e] = rows[it] >= 0 && e < left ? from[e] : from_f32<T>(0.f);
+                    for (int e = 0; e < 8; ++e) v.v[e] = e < left ? at[it][e] : from_f32<T>(0.f);
 #pragma unroll
                     for (int h = 0; h < WORDS; ++h) raw[it][h] = word_of(v, h);
                 }
+                at[it] += PJ_KC;
             }
         };
         // a row's t, where the step's ranks are its adapter's
@@ -615,7 +638,7 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
         auto keep = [&](int s) {                    // what was fetched, into a stage
 #pragma unroll
             for (int it = 0; it < ITS; ++it) {
-                uint8_t* const to = ring + s * S::STAGE + it * (RSTEP * 128) + tc_swz(rb, c);
+                const uint32_t to = mine + (uint32_t)(s * S::STAGE + it * (RSTEP * 128));
                 if constexpr (PARTS == 3) {
                     uint4 a, b, d;
                     auto f = [](uint32_t x) { return __uint_as_float(x); };
@@ -623,15 +646,16 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
                     pj_parts_of2(f(raw[it][0].z), f(raw[it][0].w), a.y, b.y, d.y);
                     pj_parts_of2(f(raw[it][WORDS - 1].x), f(raw[it][WORDS - 1].y), a.z, b.z, d.z);
                     pj_parts_of2(f(raw[it][WORDS - 1].z), f(raw[it][WORDS - 1].w), a.w, b.w, d.w);
-                    *reinterpret_cast<uint4*>(to) = a;
-                    *reinterpret_cast<uint4*>(to + S::X_PART) = b;
-                    *reinterpret_cast<uint4*>(to + 2 * S::X_PART) = d;
+                    pj_sts(to, a), pj_sts(to + S::X_PART, b), pj_sts(to + 2 * S::X_PART, d);
                 } else {
-                    *reinterpret_cast<uint4*>(to) = raw[it][0];
+                    pj_sts(to, raw[it][0]);
                 }
             }
         };
-        auto copy = [&](uint32_t to, const void* from, uint32_t bytes) {    // 16 bytes, zeros behind the first `bytes`
+        auto copy = [&](uint32_t to, const void* from) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+        };
+        auto copy_some = [&](uint32_t to, const void* from, uint32_t bytes) {    // zeros behind the first `bytes`
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
         };
         bool ok = true, fetched = false;
@@ -640,42 +664,56 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
         Tile tile = first_tile();
         aim(tile);
         while (tile.lt < my_tiles && ok) {
-#pragma unroll
-            for (int it = 0; it < ITS; ++it) row[it] = next[it];
-            which = which_next, slot0 = slot0_next, slot1 = slot1_next;
+            if (!fetched || !regs) turn();
+            if (regs && !fetched) fetch(chunks == 1);
+            fetched = true;
             const Tile following = after(tile);
             const int steps = chunks + rank_steps(tile.count);
             aim(following);
-            if (regs && !fetched) fetch(row, 0);
-            fetched = true;
             for (int st = 0; st < steps; ++st, ++g) {
                 ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
                 if (!ok) break;
                 const uint32_t x_to = mine + (uint32_t)(s * S::STAGE), w_to = x_to + S::X_STAGE;
                 if (st < chunks) {
-                    if (regs) {
-                        keep(s);
-                    } else {
-                        const int left = p.k - st * PJ_KC - c * 8;
-                        const uint32_t bytes = left >= 8 ? 16u : left > 0 ? 2u * left : 0u;
-#pragma unroll
-                        for (int it = 0; it < ITS; ++it)
-                            if (row[it] >= 0) copy(x_to + it * (RSTEP * 128), x0 + row[it] * p.ld_x + (bytes ? st * PJ_KC : 0), bytes);
-                    }
                     if constexpr (SHRINK) {
                         const int64_t plane = (int64_t)r_pad * p.bank.k_pad;
 #pragma unroll
                         for (int it = 0; it < W_ITS; ++it) {
-                            const int slot = it ? slot1 : slot0;
-                            if (slot < 0) continue;
-                            const uint16_t* const from = p.bank.a + (int64_t)slot * PARTS * plane + (int64_t)((rb + RSTEP * it) % r_pad) * p.bank.k_pad + st * PJ_KC + c * 8;
+                            if (!a_at[it]) continue;
 #pragma unroll
-                            for (int q = 0; q < PARTS; ++q) copy(w_to + q * S::W_PART + it * (RSTEP * 128), from + q * plane, 16);
+                            for (int q = 0; q < PARTS; ++q) copy(w_to + q * S::W_PART + it * (RSTEP * 128), a_at[it] + q * plane);
+                            a_at[it] += PJ_KC;
                         }
+                    }
+                    if (regs) {
+                        keep(s);
+                    } else if (st < chunks - 1 || tail >= 8) {
+#pragma unroll
+                        for (int it = 0; it < ITS; ++it) {
+                            copy(x_to + it * (RSTEP * 128), at[it]);
+                            at[it] += PJ_KC;
+                        }
+                    } else {
+#pragma unroll
+                        for (int it = 0; it < ITS; ++it) copy_some(x_to + it * (RSTEP * 128), tail > 0 ? at[it] : at[it] - c * 8, tail > 0 ? 2 * tail : 0);
                     }
                 } else if constexpr (!SHRINK) {
                     const int step = st - chunks, q = step * RANKS + c_rank, j = q / r_pad, r = q % r_pad;
                     const int slot = step == 0 ? slot0 : j < tile.count ? p.plan[tile.rows].slot[j] : -1;
+                    const int64_t plane = (int64_t)p.n * r_pad;
+#pragma unroll
+                    for (int it = 0; it < W_ITS; ++it) {
+                        const int in_tile = rb + RSTEP * it, col = tile.part * BN + in_tile;
+                        if (BN < RSTEP && in_tile >= BN) continue;
+                        const bool real = slot >= 0 && col < p.n;
+                        const uint16_t* const from = p.bank.b + (real ? (int64_t)slot * B_PLANES * plane + (int64_t)col * r_pad + r : 0);
+                        if constexpr (PARTS == 3) {
+#pragma unroll
+                            for (int k = 0; k < B_PLANES; ++k) copy_some(w_to + k * S::W_PART + it * (RSTEP * 128), from + (real ? k * plane : 0), real ? 16 : 0);
+                        } else if (c_plane < B_PLANES) {
+                            copy_some(w_to + it * (RSTEP * 128), from + (real ? c_plane * plane : 0), real ? 16 : 0);
+                        }
+                    }
                     if constexpr (PARTS == 3) {
                         keep(s);
                     } else {
@@ -684,34 +722,21 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
                         for (int it = 0; it < ITS; ++it) {
                             const bool own = (int)(which >> (8 * it) & 255) == j;
                             const __nv_bfloat16* const t = static_cast<const __nv_bfloat16*>(p.t);
-                            copy(x_to + it * (RSTEP * 128), own ? t + ((i0 + RSTEP * it) * 2 + c_plane) * r_pad + r : t, own ? 16 : 0);
-                        }
-                    }
-                    const int64_t plane = (int64_t)p.n * r_pad;
-#pragma unroll
-                    for (int it = 0; it < W_ITS; ++it) {
-                        const int col = tile.part * BN + rb + RSTEP * it;
-                        const bool real = slot >= 0 && col < p.n;
-                        const uint16_t* const from = p.bank.b + (real ? (int64_t)slot * B_PLANES * plane + (int64_t)col * r_pad + r : 0);
-                        if constexpr (PARTS == 3) {
-#pragma unroll
-                            for (int k = 0; k < B_PLANES; ++k) copy(w_to + k * S::W_PART + it * (RSTEP * 128), from + (real ? k * plane : 0), real ? 16 : 0);
-                        } else if (c_plane < B_PLANES) {
-                            copy(w_to + it * (RSTEP * 128), from + (real ? c_plane * plane : 0), real ? 16 : 0);
+                            copy_some(x_to + it * (RSTEP * 128), own ? t + ((i0 + RSTEP * it) * 2 + c_plane) * r_pad + r : t, own ? 16 : 0);
                         }
                     }
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
-                if (regs) {                         // what the next step keeps is requested now: of this tile, or of the one after it
-                    if (st + 1 < chunks) fetch(row, st + 1);
-                    else if (st + 1 < steps) fetch_t(tile, st + 1 - chunks);
-                    else fetch(next, 0);
-                }
                 if (g >= LAG) {
                     asm volatile("cp.async.wait_group %0;" ::"n"(LAG) : "memory");
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&full_x[told]);
                     if (++told == STAGES) told = 0;
+                }
+                if (regs) {                         // what the next step keeps is requested now: of this tile, or of the one after it
+                    if (st + 1 < chunks) fetch(st + 2 == chunks);
+                    else if (st + 1 < steps) fetch_t(tile, st + 1 - chunks);
+                    else if (following.lt < my_tiles) turn(), fetch(chunks == 1);
                 }
                 if (++s == STAGES) { s = 0; ph ^= 1; }
             }
@@ -730,6 +755,7 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
         const int q = warp & 3, half = (warp - PJ_LOADERS / 32) >> 2;
         const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16);
         float* const staging = reinterpret_cast<float*>(ring + STAGES * S::STAGE) + (warp - PJ_LOADERS / 32) * (32 * 17);
+        float* const bias = reinterpret_cast<float*>(ring + STAGES * S::STAGE) + PJ_EPI_WARPS * 32 * 17 + (warp - PJ_LOADERS / 32) * 16 * NB;
         const int out_size = p.out_f32 ? 4 : (int)sizeof(T);
         const bool vec = (reinterpret_cast<uintptr_t>(p.y) & 31) == 0 && p.ld_y * out_size % 32 == 0;
         const int units = PARTS == 3 ? (chunks + PJ_UNIT - 1) / PJ_UNIT : 1;
@@ -754,6 +780,14 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
                 live = live && row_of(p, i) >= 0;
             }
             const uint32_t rows_live = __ballot_sync(FULL, live);
+            if constexpr (!SHRINK) {                // the bias of this warp's columns, while the products are still on their way
+                __syncwarp();
+                for (int e = lane; e < 16 * NB; e += 32) {
+                    const int col = c0 + 16 * (2 * (e >> 4) + half) + (e & 15);
+                    bias[e] = p.bias && col < p.n ? __ldg(p.bias + col) : 0.f;
+                }
+                __syncwarp();
+            }
             // 16 finished sums of this row, from column `at` of the tile
             auto finish = [&](float (&y)[16], int at) {
                 if constexpr (SHRINK) {
@@ -782,7 +816,7 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
                 at += c0;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    if (p.bias && at + e < p.n) y[e] += __ldg(p.bias + at + e);
+                    y[e] += bias[(at - c0) / 32 * 16 + e];
                     if (p.act == RIPPLE_ACT_RELU && y[e] < 0.f) y[e] = 0.f;
                 }
                 if (vec && at + 16 <= p.n) {
@@ -821,7 +855,7 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
                     }
                 }
             };
-            constexpr int CARRY = PARTS == 3 ? NB : 1;
+            constexpr int CARRY = PARTS == 3 && MANY ? NB : 1;
             float sum[CARRY][16];              // fp32: of the units before the last
             for (int u = 0; u < units && ok; ++u, ++sg) {
                 const int b = sg & 1;
@@ -829,7 +863,7 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
                 ok = __all_sync(FULL, mbar_wait_bounded(&acc_full[b], (sg >> 1) & 1, PJ_SPIN_LIMIT));
                 if (!ok) break;
                 tc_fence_after();
-                if (PARTS == 3 && u < units - 1) {
+                if (PARTS == 3 && MANY && u < units - 1) {
 #pragma unroll
                     for (int j = 0; j < CARRY; ++j) {
                         const int at = 16 * (2 * j + half);
@@ -852,7 +886,7 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
 #pragma unroll
                         for (int e = 0; e < 16; ++e) y[e] = __uint_as_float(x[e]);
                         if constexpr (PARTS == 3) {
-                            if (u > 0) {
+                            if (MANY && u > 0) {
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) {
                                     float before = sum[0][e];
@@ -880,13 +914,13 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
     } else if (warp == PJ_LOADERS / 32 + PJ_EPI_WARPS) {
         // ---------------- products ----------------
         const bool lead = tc_elect();
-        const uint64_t d0 = tc_smem_desc(smem_u32(ring));
+        const uint64_t d0 = tc_smem_desc(__shfl_sync(FULL, smem_u32(ring), 0));
         int s = 0, sg = 0, worked = 0;
         uint32_t ph = 0;
         bool ok = true;
         for (Tile tile = first_tile(); tile.lt < my_tiles && ok; tile = after(tile)) {
             const int count = __shfl_sync(FULL, tile.count, 0), nt = __shfl_sync(FULL, tile_n(tile), 0), steps = chunks + rank_steps(count);
-            const uint32_t idesc = pj_idesc(TYPE, nt), idesc_t = pj_idesc(RIPPLE_TYPE_BF16, nt), small = tmem + (uint32_t)(2 * BN + (worked & 1) * BN);
+            const uint32_t idesc = pj_idesc(TYPE, nt), idesc_t = pj_idesc(RIPPLE_TYPE_BF16, nt), small = __shfl_sync(FULL, tmem + (uint32_t)(2 * BN + (worked & 1) * BN), 0);
             uint32_t acc = 0;
             int left = p.k, left_t = count * r_pad, b = 0;
             for (int st = 0; st < steps; ++st) {
@@ -899,13 +933,14 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
                     if (before > 0) ok = __all_sync(FULL, mbar_wait_bounded(&acc_empty[b], (before - 1) & 1, PJ_SPIN_LIMIT));
                     if (!ok) break;
                     tc_fence_after();
-                    acc = tmem + (uint32_t)(b * BN);
+                    acc = __shfl_sync(FULL, tmem + (uint32_t)(b * BN), 0);
                 }
                 ok = __all_sync(FULL, (SHRINK || mbar_wait_bounded(&full_w[s], ph, PJ_SPIN_LIMIT)) && mbar_wait_bounded(&full_x[s], ph, PJ_SPIN_LIMIT));
                 if (!ok) break;
                 fence_async_smem();      // the loaders' stores, for the tensor core (on the reader's side: loads in flight are not waited for)
                 tc_fence_after();
-                const uint64_t x = d0 + (uint64_t)((uint32_t)s * (S::STAGE >> 4)), w = x + (S::X_STAGE >> 4);
+                // (broadcast: operands that the compiler cannot see to be the warp's take ten times as long to issue)
+                const uint64_t x = d0 + (uint64_t)((uint32_t)__shfl_sync(FULL, s, 0) * (S::STAGE >> 4)), w = x + (S::X_STAGE >> 4);
                 const bool last = st == steps - 1 || (PARTS == 3 && st < chunks - 1 && st % PJ_UNIT == PJ_UNIT - 1);
                 constexpr uint64_t XP = S::X_PART >> 4, WP = S::W_PART >> 4;
                 if (lead) {
@@ -961,14 +996,19 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
         bool ok = true;
         for (Tile tile = first_tile(); tile.lt < my_tiles && ok; tile = after(tile)) {
             const int steps = chunks + rank_steps(tile.count), c0 = tile.part * BN, bytes = tile_n(tile) * 128;
+            // (tiles of 256 columns: two groups of the layout, one behind the other in shared memory)
             const uint8_t* from = p.layout + (int64_t)(c0 / PJ_COLS) * chunks * PARTS * PJ_CHUNK + c0 % PJ_COLS * 128;
+            const int bytes1 = min(bytes, PJ_CHUNK), bytes2 = bytes - bytes1;
             for (int st = 0; st < steps; ++st, ++g, from += PARTS * PJ_CHUNK) {
                 ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
                 if (!ok) break;
                 if (st < chunks) {
                     mbar_expect(&full_w[s], PARTS * bytes);
-                    for (int part = 0; part < PARTS; ++part)
-                        tc_copy_bulk(ring + s * S::STAGE + S::X_STAGE + part * S::W_PART, from + part * PJ_CHUNK, bytes, &full_w[s]);
+                    for (int part = 0; part < PARTS; ++part) {
+                        uint8_t* const to = ring + s * S::STAGE + S::X_STAGE + part * S::W_PART;
+                        tc_copy_bulk(to, from + part * PJ_CHUNK, bytes1, &full_w[s]);
+                        if (BN > PJ_COLS && bytes2 > 0) tc_copy_bulk(to + PJ_CHUNK, from + ((int64_t)chunks * PARTS + part) * PJ_CHUNK, bytes2, &full_w[s]);
+                    }
                 } else {
                     mbar_arrive(&full_w[s]);       // (the loaders bring what a step over ranks reads)
                 }
@@ -990,13 +1030,20 @@ __global__ void __launch_bounds__(PJ_THREADS, 1) k_project_rows(const __grid_con
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM) : "memory");
 }
 
-template <int TYPE, int BN, bool SHRINK>
+template <int TYPE, int BN, bool SHRINK, bool MANY>
 static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
-    constexpr size_t bytes = PjShape<TYPE, BN>::BYTES;
-    const cudaError_t e = cudaFuncSetAttribute(k_project_rows<TYPE, BN, SHRINK>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    using S = PjShape<TYPE, BN, MANY>;
+    const cudaError_t e = cudaFuncSetAttribute(k_project_rows<TYPE, BN, SHRINK, MANY>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::BYTES);
     if (e != cudaSuccess) return e;
     const int64_t across = SHRINK ? p.batches : (p.n + BN - 1) / BN, tiles = across * ((p.rows + PJ_ROWS - 1) / PJ_ROWS);
-    return launch(k_project_rows<TYPE, BN, SHRINK>, dim3((unsigned)std::min<int64_t>(tiles, sm_count())), PJ_THREADS, bytes, stream, p);
+    return launch(k_project_rows<TYPE, BN, SHRINK, MANY>, dim3((unsigned)std::min<int64_t>(tiles, sm_count())), S::THREADS, S::BYTES, stream, p);
+}
+template <int TYPE, int BN, bool SHRINK>
+static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
+    if constexpr (TYPE == RIPPLE_TYPE_F32) {
+        if (p.chunks > PJ_UNIT) return project_tiles<TYPE, BN, SHRINK, true>(p, stream);
+    }
+    return project_tiles<TYPE, BN, SHRINK, false>(p, stream);
 }
 
 template <int TYPE>
@@ -1021,8 +1068,11 @@ static cudaError_t project(ProjectParams p, void* stream) {
         if (e != cudaSuccess) return e;
     }
     if (few) return launch(k_project_few<TYPE>, dim3((p.rows + PF_ROWS - 1) / PF_ROWS, (p.n + PF_COLS - 1) / PF_COLS), 256, 0, stream, p);
-    // Tiles of 32 columns where those of 128 would leave most SMs without one.
+    // Tiles of 32 columns where those of 128 would leave most SMs without one; of 256 (16-bit rows) where those leave none.
     const int64_t wide = (int64_t)((p.n + 127) / 128) * row_tiles;
+    if constexpr (TYPE != RIPPLE_TYPE_F32) {
+        if (p.n > 128 && (int64_t)((p.n + 255) / 256) * row_tiles >= sm_count()) return project_tiles<TYPE, 256, false>(p, stream);
+    }
     return wide >= sm_count() / 2 ? project_tiles<TYPE, 128, false>(p, stream) : project_tiles<TYPE, 32, false>(p, stream);
 }
 
@@ -1148,6 +1198,7 @@ extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) 
     }
     if (extents_meet(y, work)) REFUSE("project_rows: y overlaps the workspace");
 
+    if (a->x_rows == 0) return RIPPLE_OK;     // every row is a padding row
     OnDevice on(a->device);
     if (on.err != cudaSuccess) return launch_failed("cudaSetDevice", on.err);
     ProjectParams p = {};
