@@ -488,7 +488,7 @@ template <typename T> __device__ __forceinline__ uint4 word_of(const Piece<T, 8>
 //   epilogue   takes a finished accumulator while the next is being filled: bias, activation, and out
 // fp32: six products of parts (all but those below 2^-23); the large one of the first parts is handed over every 256 entries
 // and summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
-// Barriers, all waits bounded: full_x[s] (one arrival per loader warp), full_w[s] (bytes), empty[s] (the products that read
+// Barriers, all waits bounded: full_x[s] (one arrival per loader warp, 16-bit rows: per thread), full_w[s] (bytes), empty[s] (the products that read
 // stage s), acc_full[b], acc_empty[b] (one arrival per epilogue warp).
 template <int TYPE, int BN, bool SHRINK, bool MANY>
 __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project_rows(const __grid_constant__ ProjectParams p) {
@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
     auto rank_steps = [&](int count) { return SHRINK ? 0 : (count * r_pad + RANKS - 1) / RANKS; };
 
     if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&full_x[s], PJ_LOADERS / 32); mbar_init(&full_w[s], 1); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full_x[s], PARTS == 3 ? PJ_LOADERS / 32 : PJ_LOADERS); mbar_init(&full_w[s], 1); mbar_init(&empty[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], PJ_EPI_WARPS); }
         mbar_init(&drained, 1);
         s_fail = 0;
@@ -550,7 +550,6 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
     if (warp < PJ_LOADERS / 32) {
         // ---------------- rows, and what comes out of the bank ----------------
         constexpr int RSTEP = PJ_LOADERS / 8, ITS = PJ_ROWS / RSTEP, W_ITS = (BN + RSTEP - 1) / RSTEP;
-        constexpr int LAG = PARTS == 3 ? 0 : STAGES / 2;        // steps whose copies are in flight when one is told to be there
         const int c = tid & 7, rb = tid >> 3;       // thread: piece c (8 entries) of the rows rb + RSTEP it
         const uint32_t mine = smem_u32(ring) + tc_swz(rb, c);
         const bool vec = (reinterpret_cast<uintptr_t>(p.x) & 15) == 0 && p.ld_x % (16 / (int)sizeof(T)) == 0;
@@ -659,7 +658,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
         };
         bool ok = true, fetched = false;
-        int s = 0, g = 0, told = 0;
+        int s = 0;
         uint32_t ph = 1;                            // (a fresh barrier counts as completed)
         Tile tile = first_tile();
         aim(tile);
@@ -670,7 +669,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
             const Tile following = after(tile);
             const int steps = chunks + rank_steps(tile.count);
             aim(following);
-            for (int st = 0; st < steps; ++st, ++g) {
+            for (int st = 0; st < steps; ++st) {
                 ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
                 if (!ok) break;
                 const uint32_t x_to = mine + (uint32_t)(s * S::STAGE), w_to = x_to + S::X_STAGE;
@@ -726,12 +725,17 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                         }
                     }
                 }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                if (g >= LAG) {
-                    asm volatile("cp.async.wait_group %0;" ::"n"(LAG) : "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&full_x[told]);
-                    if (++told == STAGES) told = 0;
+                // 16-bit rows: the barrier counts threads, and the copies of a thread arrive for it when they have landed
+                if (PARTS == 1 && vec) {
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full_x[s])) : "memory");
+                } else {
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    if (PARTS == 1) {
+                        mbar_arrive(&full_x[s]);
+                    } else {
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&full_x[s]);
+                    }
                 }
                 if (regs) {                         // what the next step keeps is requested now: of this tile, or of the one after it
                     if (st + 1 < chunks) fetch(st + 2 == chunks);
@@ -742,13 +746,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
             }
             tile = following;
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        __syncwarp();
-        if (lane == 0 && ok)
-            for (int d = 0; d < min(g, LAG); ++d) {
-                mbar_arrive(&full_x[told]);
-                if (++told == STAGES) told = 0;
-            }
+        asm volatile("cp.async.wait_all;" ::: "memory");
         if (!ok) s_fail = 1;
     } else if (warp < PJ_LOADERS / 32 + PJ_EPI_WARPS) {
         // ---------------- epilogue ----------------
