@@ -239,24 +239,44 @@ template <typename T> __device__ __forceinline__ void load8(float (&v)[8], const
 }
 
 // Few rows: t_i by a block per ROWS rows, a warp per four ranks, eight entries of K per lane; rows of one adapter share its loads.
-// The blocks in front plan the tiles (of the tensor-core form).
+// The rows lie in shared memory as fp32, SF_K entries at a time.  The blocks in front plan the tiles (of the tensor-core form).
+constexpr int SF_K = 1024;
 template <int TYPE, int ROWS>
 __global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ ProjectParams p, int planned) {
     using T = typename Elem<TYPE>::T;
     constexpr int PA = TYPE == RIPPLE_TYPE_F32 ? 3 : 1, RANKS = 4;
     pdl_enter();
     if ((int)blockIdx.x < planned) return plan_tile(p, blockIdx.x);
+    __shared__ __align__(16) float xs[ROWS][SF_K];
     const int i0 = (blockIdx.x - planned) * ROWS, lane = lane_id();
     const T* x[ROWS];
     int slot[ROWS];
-    bool vec = true;
+    bool any = false;
 #pragma unroll
     for (int q = 0; q < ROWS; ++q) {
         const int64_t from = i0 + q < p.rows ? row_of(p, i0 + q) : -1;
         slot[q] = from >= 0 ? slot_of(p, i0 + q) : -1;
         x[q] = static_cast<const T*>(p.x) + max(from, (int64_t)0) * p.ld_x;
-        vec = vec && (reinterpret_cast<uintptr_t>(x[q]) & 15) == 0;
+        any = any || slot[q] >= 0;
     }
+    if (!any) return;
+    auto stage = [&](int k0) {           // entries k0 .. k0 + SF_K - 1, zeros beyond K
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) {
+            T v[SF_K / 128];
+#pragma unroll
+            for (int e = 0; e < SF_K / 128; ++e) {
+                const int kk = k0 + 128 * e + (int)threadIdx.x;
+                v[e] = kk < p.k ? x[q][kk] : from_f32<T>(0.f);
+            }
+#pragma unroll
+            for (int e = 0; e < SF_K / 128; ++e) xs[q][128 * e + threadIdx.x] = to_f32(v[e]);
+        }
+        __syncthreads();
+    };
+    const bool once = p.k <= SF_K;
+    if (once) stage(0);
     const int64_t plane = (int64_t)p.bank.r_pad * p.bank.k_pad;
     for (;;) {
         int a = -1;                          // the first adapter that is left, and its rows
@@ -270,40 +290,37 @@ __global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ Proj
             if (mine[q]) slot[q] = -1;
         }
         const SlotInfo info = p.bank.info[a];
-        for (int r0 = (threadIdx.x >> 5) * RANKS; r0 < p.bank.r_pad; r0 += 4 * RANKS) {
+        for (int r1 = 0; r1 < p.bank.r_pad; r1 += 4 * RANKS) {
+            const int r0 = r1 + (threadIdx.x >> 5) * RANKS;
             const uint16_t* const w = p.bank.a + (int64_t)a * PA * plane + (int64_t)r0 * p.bank.k_pad;
             float sum[ROWS][RANKS] = {};
-            if (r0 < info.rank) {
-                for (int kk = lane * 8; kk < p.k; kk += 256) {
-                    float xv[ROWS][8];
+            for (int k0 = 0; k0 < p.k; k0 += SF_K) {
+                if (!once) stage(k0);
+                if (r0 >= info.rank) continue;
+                const int end = min(SF_K, p.k - k0);
+                for (int kk = lane * 8; kk < end; kk += 256) {      // (A has zeros up to a multiple of 64 entries)
+                    float wv[RANKS][8];
 #pragma unroll
-                    for (int q = 0; q < ROWS; ++q) {
-                        if (vec && kk + 8 <= p.k) {
-                            load8(xv[q], x[q] + kk);
+                    for (int r = 0; r < RANKS; ++r) {
+                        if constexpr (PA == 3) {
+                            float part[2][8];
+                            const __nv_bfloat16* const from = reinterpret_cast<const __nv_bfloat16*>(w) + r * p.bank.k_pad + k0 + kk;
+                            load8(wv[r], from), load8(part[0], from + plane), load8(part[1], from + 2 * plane);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) wv[r][e] += part[0][e] + part[1][e];
                         } else {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) xv[q][e] = kk + e < p.k ? to_f32(x[q][kk + e]) : 0.f;
+                            load8(wv[r], reinterpret_cast<const T*>(w) + r * p.bank.k_pad + k0 + kk);
                         }
                     }
 #pragma unroll
-                    for (int r = 0; r < RANKS; ++r) {
-                        float wv[8];
-                        if constexpr (PA == 3) {
-                            float part[8];
-                            load8(wv, reinterpret_cast<const __nv_bfloat16*>(w) + 2 * plane + r * p.bank.k_pad + kk);
+                    for (int q = 0; q < ROWS; ++q) {
+                        const float4 x0 = *reinterpret_cast<const float4*>(&xs[q][kk]), x1 = *reinterpret_cast<const float4*>(&xs[q][kk + 4]);
 #pragma unroll
-                            for (int h = 1; h >= 0; --h) {
-                                load8(part, reinterpret_cast<const __nv_bfloat16*>(w) + h * plane + r * p.bank.k_pad + kk);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) wv[e] += part[e];
-                            }
-                        } else {
-                            load8(wv, reinterpret_cast<const T*>(w) + r * p.bank.k_pad + kk);
+                        for (int r = 0; r < RANKS; ++r) {
+                            float& t = sum[q][r];
+                            t = fmaf(x0.x, wv[r][0], t), t = fmaf(x0.y, wv[r][1], t), t = fmaf(x0.z, wv[r][2], t), t = fmaf(x0.w, wv[r][3], t);
+                            t = fmaf(x1.x, wv[r][4], t), t = fmaf(x1.y, wv[r][5], t), t = fmaf(x1.z, wv[r][6], t), t = fmaf(x1.w, wv[r][7], t);
                         }
-#pragma unroll
-                        for (int q = 0; q < ROWS; ++q)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) sum[q][r] = fmaf(xv[q][e], wv[e], sum[q][r]);
                     }
                 }
             }
@@ -488,8 +505,8 @@ template <typename T> __device__ __forceinline__ uint4 word_of(const Piece<T, 8>
 //   epilogue   takes a finished accumulator while the next is being filled: bias, activation, and out
 // fp32: six products of parts (all but those below 2^-23); the large one of the first parts is handed over every 256 entries
 // and summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
-// Barriers, all waits bounded: full_x[s] (one arrival per loader warp, 16-bit rows: per thread), full_w[s] (bytes), empty[s] (the products that read
-// stage s), acc_full[b], acc_empty[b] (one arrival per epilogue warp).
+// Barriers, all waits bounded: full[s] (one arrival per loader warp, 16-bit rows: per thread; one with the bytes of the weights),
+// empty[s] (the products that read stage s), acc_full[b], acc_empty[b] (one arrival per epilogue warp).
 template <int TYPE, int BN, bool SHRINK, bool MANY>
 __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project_rows(const __grid_constant__ ProjectParams p) {
     using T = typename Elem<TYPE>::T;
@@ -498,7 +515,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
     constexpr int PARTS = S::PARTS, STAGES = S::STAGES, NB = BN / 32, RANKS = S::RANKS, B_PLANES = pj_b_planes(TYPE);
     constexpr uint32_t TMEM = S::TMEM;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t full_x[STAGES], full_w[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
+    __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int s_fail;
 
@@ -531,7 +548,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
     auto rank_steps = [&](int count) { return SHRINK ? 0 : (count * r_pad + RANKS - 1) / RANKS; };
 
     if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&full_x[s], PARTS == 3 ? PJ_LOADERS / 32 : PJ_LOADERS); mbar_init(&full_w[s], 1); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], (PARTS == 3 ? PJ_LOADERS / 32 : PJ_LOADERS) + (SHRINK ? 0 : 1)); mbar_init(&empty[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], PJ_EPI_WARPS); }
         mbar_init(&drained, 1);
         s_fail = 0;
@@ -727,14 +744,14 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                 }
                 // 16-bit rows: the barrier counts threads, and the copies of a thread arrive for it when they have landed
                 if (PARTS == 1 && vec) {
-                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full_x[s])) : "memory");
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[s])) : "memory");
                 } else {
                     asm volatile("cp.async.wait_all;" ::: "memory");
                     if (PARTS == 1) {
-                        mbar_arrive(&full_x[s]);
+                        mbar_arrive(&full[s]);
                     } else {
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&full_x[s]);
+                        if (lane == 0) mbar_arrive(&full[s]);
                     }
                 }
                 if (regs) {                         // what the next step keeps is requested now: of this tile, or of the one after it
@@ -933,7 +950,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                     tc_fence_after();
                     acc = __shfl_sync(FULL, tmem + (uint32_t)(b * BN), 0);
                 }
-                ok = __all_sync(FULL, (SHRINK || mbar_wait_bounded(&full_w[s], ph, PJ_SPIN_LIMIT)) && mbar_wait_bounded(&full_x[s], ph, PJ_SPIN_LIMIT));
+                ok = __all_sync(FULL, mbar_wait_bounded(&full[s], ph, PJ_SPIN_LIMIT));
                 if (!ok) break;
                 fence_async_smem();      // the loaders' stores, for the tensor core (on the reader's side: loads in flight are not waited for)
                 tc_fence_after();
@@ -1001,14 +1018,14 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                 ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
                 if (!ok) break;
                 if (st < chunks) {
-                    mbar_expect(&full_w[s], PARTS * bytes);
+                    mbar_expect(&full[s], PARTS * bytes);
                     for (int part = 0; part < PARTS; ++part) {
                         uint8_t* const to = ring + s * S::STAGE + S::X_STAGE + part * S::W_PART;
-                        tc_copy_bulk(to, from + part * PJ_CHUNK, bytes1, &full_w[s]);
-                        if (BN > PJ_COLS && bytes2 > 0) tc_copy_bulk(to + PJ_CHUNK, from + ((int64_t)chunks * PARTS + part) * PJ_CHUNK, bytes2, &full_w[s]);
+                        tc_copy_bulk(to, from + part * PJ_CHUNK, bytes1, &full[s]);
+                        if (BN > PJ_COLS && bytes2 > 0) tc_copy_bulk(to + PJ_CHUNK, from + ((int64_t)chunks * PARTS + part) * PJ_CHUNK, bytes2, &full[s]);
                     }
                 } else {
-                    mbar_arrive(&full_w[s]);       // (the loaders bring what a step over ranks reads)
+                    mbar_arrive(&full[s]);       // (the loaders bring what a step over ranks reads)
                 }
                 if (++s == STAGES) { s = 0; ph ^= 1; }
             }
@@ -1017,7 +1034,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
         // no copy of this CTA may be in flight when it leaves: the latest into each stage (usually long there)
         for (int k = 0; k < min(g, STAGES); ++k) {
             const int latest = g - 1 - k;
-            mbar_wait_bounded(&full_w[latest % STAGES], (uint32_t)(latest / STAGES) & 1, PJ_SPIN_LIMIT);
+            mbar_wait_bounded(&full[latest % STAGES], (uint32_t)(latest / STAGES) & 1, PJ_SPIN_LIMIT);
         }
     }
 
