@@ -253,9 +253,11 @@ __global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ Proj
     int slot[ROWS];
     bool any = false;
 #pragma unroll
-    for (int q = 0; q < ROWS; ++q) {
-        const int64_t from = i0 + q < p.rows ? row_of(p, i0 + q) : -1;
-        slot[q] = from >= 0 ? slot_of(p, i0 + q) : -1;
+    for (int q = 0; q < ROWS; ++q) {         // (an id and a slot at once: every load that waits for another costs half a microsecond)
+        const int i = min(i0 + q, p.rows - 1);
+        const int64_t from = row_of(p, i);
+        slot[q] = p.slots[i];
+        if (from < 0 || slot[q] < 0 || slot[q] >= p.n_slots || i0 + q >= p.rows) slot[q] = -1;
         x[q] = static_cast<const T*>(p.x) + max(from, (int64_t)0) * p.ld_x;
         any = any || slot[q] >= 0;
     }
@@ -341,95 +343,117 @@ __global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ Proj
     }
 }
 
-// Few rows: 16 rows x 32 columns of y per block.  A lane is a column, a warp an eighth of every 512 entries of K; what the warps
+// Few rows: 16 rows x 32 columns of y per block.  A lane is a column, a warp an eighth of every 256 entries of K; what the warps
 // have summed meets in shared memory, where each finishes two rows: t_i B_a, bias, activation.  Sums in fp32 throughout.
-// Latency is all that counts here: one load of W and sixteen products per entry of K and lane, and no pipeline to fill.
-constexpr int PF_ROWS = 16, PF_COLS = 32, PF_K = 512, PF_LD = 20;
+// Latency is all that counts here: 32 entries of W per lane and 16 of the rows per thread are always on their way, those of the next
+// 256 entries while these are multiplied.
+constexpr int PF_ROWS = 16, PF_COLS = 32, PF_K = 256, PF_LD = 20;
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_project_few(const __grid_constant__ ProjectParams p) {
     using T = typename Elem<TYPE>::T;
-    constexpr int B_PLANES = pj_b_planes(TYPE);
-    if (!p.bank.info) pdl_enter();       // with adapters the kernel before computes t: what it waited for is there, t is waited for below
-    __shared__ __align__(16) float xs[PF_K * PF_LD];
-    __shared__ int64_t from[PF_ROWS];
-    const int warp = threadIdx.x >> 5, lane = lane_id(), i0 = blockIdx.x * PF_ROWS, col = blockIdx.y * PF_COLS + lane;
-    if (threadIdx.x < PF_ROWS) from[threadIdx.x] = i0 + (int)threadIdx.x < p.rows ? row_of(p, i0 + threadIdx.x) : -1;
-    __syncthreads();
-    const T* const w = static_cast<const T*>(p.plain) + min(col, p.n - 1);
+    constexpr int B_PLANES = pj_b_planes(TYPE), OWN = PF_K / 8;
+    const bool adapted = p.bank.info != nullptr;
+    if (!adapted) pdl_enter();           // with adapters the kernel before computes t: what it waited for is there, t is waited for below
+    __shared__ __align__(16) float xs[2][PF_K * PF_LD];
+    const int warp = threadIdx.x >> 5, lane = lane_id(), i0 = blockIdx.x * PF_ROWS;
+    const int col = blockIdx.y * PF_COLS + lane, col_in = min(col, p.n - 1);
+    const T* const w = static_cast<const T*>(p.plain) + (int64_t)warp * OWN * p.n + col_in;
+    T wv[OWN];
+    auto fetch_w = [&](int k0) {
+        const int left = p.k - k0 - warp * OWN;
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) wv[j] = j < left ? w[(int64_t)(k0 + j) * p.n] : from_f32<T>(0.f);
+    };
+    fetch_w(0);
+    // thread: a row and every 16th entry of it
+    const int xr = threadIdx.x >> 4, xk = threadIdx.x & 15;
+    const int64_t x_from = i0 + xr < p.rows ? row_of(p, i0 + xr) : -1;
+    const T* const x = static_cast<const T*>(p.x) + max(x_from, (int64_t)0) * p.ld_x + xk;
+    T xv[PF_K / 16];
+    auto fetch_x = [&](int k0) {
+        const int left = x_from >= 0 ? p.k - k0 - xk : 0;
+#pragma unroll
+        for (int e = 0; e < PF_K / 16; ++e) xv[e] = 16 * e < left ? x[k0 + 16 * e] : from_f32<T>(0.f);
+    };
+    auto keep_x = [&](int b) {
+#pragma unroll
+        for (int e = 0; e < PF_K / 16; ++e) xs[b][(xk + 16 * e) * PF_LD + xr] = to_f32(xv[e]);
+    };
+    fetch_x(0);
+    // the two rows that this warp finishes, and their adapters
+    bool live[2];
+    int slot[2] = {-1, -1}, rank[2] = {0, 0};
+    const int rp = p.bank.r_pad;
+    const int64_t plane = (int64_t)p.n * rp;
+    const __nv_bfloat16* b_at[2] = {};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = i0 + 2 * warp + h;
+        live[h] = i < p.rows && row_of(p, i) >= 0;
+        if (adapted && i < p.rows) slot[h] = p.slots[i];
+        if (slot[h] < 0 || slot[h] >= p.n_slots) slot[h] = -1;
+        b_at[h] = reinterpret_cast<const __nv_bfloat16*>(p.bank.b) + (int64_t)max(slot[h], 0) * B_PLANES * plane + (int64_t)col_in * rp;
+        if (slot[h] >= 0) rank[h] = p.bank.info[slot[h]].rank;
+    }
+    const float bias = p.bias ? p.bias[col_in] : 0.f;
     float sum[PF_ROWS] = {};
-    for (int k0 = 0; k0 < p.k; k0 += PF_K) {
-        const int here = min(PF_K, p.k - k0);
-        // thread: a row and every 16th entry; all of its loads before the first is used
-        {
-            const int r = threadIdx.x >> 4, k1 = threadIdx.x & 15;
-            const int64_t at = from[r];
-            const T* const x = static_cast<const T*>(p.x) + max(at, (int64_t)0) * p.ld_x + k0;
+    keep_x(0);
+    __syncthreads();
+    int b = 0;
+    for (int k0 = 0; k0 < p.k; k0 += PF_K, b ^= 1) {
+        const bool more = k0 + PF_K < p.k;
+        float now[OWN];
 #pragma unroll
-            for (int half = 0; half < PF_K; half += PF_K / 2) {
-                T v[PF_K / 32];
+        for (int j = 0; j < OWN; ++j) now[j] = to_f32(wv[j]);
+        if (more) fetch_x(k0 + PF_K), fetch_w(k0 + PF_K);
 #pragma unroll
-                for (int e = 0; e < PF_K / 32; ++e) v[e] = at >= 0 && half + k1 + 16 * e < here ? x[half + k1 + 16 * e] : from_f32<T>(0.f);
-#pragma unroll
-                for (int e = 0; e < PF_K / 32; ++e) if (half + k1 + 16 * e < here) xs[(half + k1 + 16 * e) * PF_LD + r] = to_f32(v[e]);
-            }
-        }
-        __syncthreads();
-        const int per = (here + 7) / 8, end = min((warp + 1) * per, here);
-#pragma unroll 8
-        for (int kk = warp * per; kk < end; ++kk) {
-            const float wv = to_f32(w[(int64_t)(k0 + kk) * p.n]);
+        for (int j = 0; j < OWN; ++j) {
 #pragma unroll
             for (int r = 0; r < PF_ROWS; r += 4) {
-                const float4 x = *reinterpret_cast<const float4*>(xs + kk * PF_LD + r);
-                sum[r] = fmaf(x.x, wv, sum[r]), sum[r + 1] = fmaf(x.y, wv, sum[r + 1]);
-                sum[r + 2] = fmaf(x.z, wv, sum[r + 2]), sum[r + 3] = fmaf(x.w, wv, sum[r + 3]);
+                const float4 v = *reinterpret_cast<const float4*>(&xs[b][(warp * OWN + j) * PF_LD + r]);
+                sum[r] = fmaf(v.x, now[j], sum[r]), sum[r + 1] = fmaf(v.y, now[j], sum[r + 1]);
+                sum[r + 2] = fmaf(v.z, now[j], sum[r + 2]), sum[r + 3] = fmaf(v.w, now[j], sum[r + 3]);
             }
         }
+        if (more) keep_x(b ^ 1);
         __syncthreads();
     }
-    float* const part = xs;              // warp x row x column
+    float* const part = xs[0];           // warp x row x column
 #pragma unroll
     for (int r = 0; r < PF_ROWS; ++r) part[(warp * PF_ROWS + r) * PF_COLS + lane] = sum[r];
-    if (p.bank.info) pdl_enter();
+    if (adapted) pdl_enter();
     __syncthreads();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int r = 2 * warp + h, i = i0 + r;
-        if (i >= p.rows || from[r] < 0) continue;
         float y = 0.f;
 #pragma unroll
         for (int q = 0; q < 8; ++q) y += part[(q * PF_ROWS + r) * PF_COLS + lane];
-        if (p.bias) y += p.bias[min(col, p.n - 1)];
-        const int a = p.bank.info ? slot_of(p, i) : -1;
-        if (a >= 0) {
-            const int rp = p.bank.r_pad, rank = p.bank.info[a].rank;
-            const int64_t plane = (int64_t)p.n * rp;
-            const __nv_bfloat16* const b = reinterpret_cast<const __nv_bfloat16*>(p.bank.b) + (int64_t)a * B_PLANES * plane + (int64_t)min(col, p.n - 1) * rp;
-            float d = 0.f;
-            for (int k = 0; k < rank; k += 8) {
-                float t[8], bv[8], more[8];
-                if constexpr (TYPE == RIPPLE_TYPE_F32) {
-                    load8(t, static_cast<const float*>(p.t) + (int64_t)i * rp + k);
-                } else {
-                    load8(t, static_cast<const __nv_bfloat16*>(p.t) + (int64_t)i * 2 * rp + k);
-                    load8(more, static_cast<const __nv_bfloat16*>(p.t) + (int64_t)i * 2 * rp + rp + k);
+        y += bias;
+        float d = 0.f;
+        for (int k = 0; k < rank[h]; k += 8) {
+            float t[8], bv[8], more[8];
+            if constexpr (TYPE == RIPPLE_TYPE_F32) {
+                load8(t, static_cast<const float*>(p.t) + (int64_t)i * rp + k);
+            } else {
+                load8(t, static_cast<const __nv_bfloat16*>(p.t) + (int64_t)i * 2 * rp + k);
+                load8(more, static_cast<const __nv_bfloat16*>(p.t) + (int64_t)i * 2 * rp + rp + k);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) t[e] += more[e];
-                }
-                load8(bv, b + (B_PLANES - 1) * plane + k);
-#pragma unroll
-                for (int q = B_PLANES - 2; q >= 0; --q) {
-                    load8(more, b + q * plane + k);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) bv[e] += more[e];
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d = fmaf(t[e], bv[e], d);
+                for (int e = 0; e < 8; ++e) t[e] += more[e];
             }
-            y += d;
+            load8(bv, b_at[h] + (B_PLANES - 1) * plane + k);
+#pragma unroll
+            for (int q = B_PLANES - 2; q >= 0; --q) {
+                load8(more, b_at[h] + q * plane + k);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) bv[e] += more[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d = fmaf(t[e], bv[e], d);
         }
+        if (rank[h] > 0) y += d;
         if (p.act == RIPPLE_ACT_RELU && y < 0.f) y = 0.f;
-        if (col < p.n) {
+        if (col < p.n && live[h]) {
             if (p.out_f32) static_cast<float*>(p.y)[(int64_t)i * p.ld_y + col] = y;
             else static_cast<T*>(p.y)[(int64_t)i * p.ld_y + col] = from_f32<T>(y);
         }
