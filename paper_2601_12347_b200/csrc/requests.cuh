@@ -98,6 +98,17 @@ inline int sm_count() {
     return n;
 }
 
+// Lets a kernel have `bytes` of dynamic shared memory; `ready`: the devices where it has been told so
+template <typename K>
+inline cudaError_t allow_shared(K kernel, int bytes, bool (&ready)[64]) {
+    int d = 0;
+    cudaError_t e = cudaGetDevice(&d);
+    if (e != cudaSuccess || (d < 64 && ready[d])) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && d < 64) ready[d] = true;
+    return e;
+}
+
 inline ripple_status launch_failed(const char* what, cudaError_t e) {
     note_error("%s failed: %s", what, cudaGetErrorString(e));
     return e == cudaErrorMemoryAllocation ? RIPPLE_ERR_OOM : RIPPLE_ERR_CUDA;

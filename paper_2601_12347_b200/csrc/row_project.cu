@@ -1072,7 +1072,8 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
 template <int TYPE, int BN, bool SHRINK, bool MANY>
 static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
     using S = PjShape<TYPE, BN, MANY>;
-    const cudaError_t e = cudaFuncSetAttribute(k_project_rows<TYPE, BN, SHRINK, MANY>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::BYTES);
+    static bool ready[64];       // by device
+    const cudaError_t e = allow_shared(k_project_rows<TYPE, BN, SHRINK, MANY>, (int)S::BYTES, ready);
     if (e != cudaSuccess) return e;
     const int64_t across = SHRINK ? p.batches : (p.n + BN - 1) / BN, tiles = across * ((p.rows + PJ_ROWS - 1) / PJ_ROWS);
     return launch(k_project_rows<TYPE, BN, SHRINK, MANY>, dim3((unsigned)std::min<int64_t>(tiles, sm_count())), S::THREADS, S::BYTES, stream, p);

@@ -50,36 +50,48 @@ def _type_of(dtype, name: str) -> int:
     return t
 
 
-def _on_device(t, name: str, device=None):
+# A call of a few rows takes a few microseconds on the device; what is checked here before it is therefore checked with as few
+# calls into PyTorch as it can be, and explained only where it fails.
+def _refuse(t, name: str, index: int):
+    """Why a tensor is not one that the device `index` (-1: any) can read."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: a CUDA tensor expected, got {type(t).__name__}")
     if not t.is_cuda:
         raise ValueError(f"{name}: a CUDA tensor expected, it is on {t.device}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
-    if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{name} requires gradients, which these operators do not form: call them under torch.no_grad()")
-    return t
+    if index >= 0 and t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, the other tensors on cuda:{index}")
+    raise ValueError(f"{name} requires gradients, which these operators do not form: call them under torch.no_grad()")
 
 
-def _matrix(t, name: str, width: Optional[int] = None, dtype=None, device=None) -> Tuple[int, int, int]:
+def _device_of(t, name: str) -> int:
+    index = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if index < 0 or not t.is_cuda:
+        _refuse(t, name, -1)
+    return index
+
+
+def _matrix(t, name: str, width: Optional[int], dtype, index: int) -> Tuple[int, int, int]:
     """Address, leading dimension and rows of a matrix whose columns lie side by side."""
-    _on_device(t, name, device)
-    if t.dim() != 2 or (width is not None and t.shape[1] != width):
-        raise ValueError(f"{name}: [rows, {'columns' if width is None else width}] expected, got {tuple(t.shape)}")
+    if not isinstance(t, torch.Tensor) or t.get_device() != index or (t.requires_grad and torch.is_grad_enabled()):
+        _refuse(t, name, index)
+    shape = t.shape
+    if len(shape) != 2 or (width is not None and shape[1] != width):
+        raise ValueError(f"{name}: [rows, {'columns' if width is None else width}] expected, got {tuple(shape)}")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name}: {dtype} expected, got {t.dtype}")
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name}: the columns of a row must lie side by side, the stride is {t.stride(1)}")
-    return t.data_ptr(), (t.stride(0) if rows > 1 else max(cols, 1)), rows
+    rows, cols = shape
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError(f"{name}: the columns of a row must lie side by side, the stride is {inner}")
+    return t.data_ptr(), (ld if rows > 1 else max(cols, 1)), rows
 
 
-def _vector(t, name: str, size: int, dtype, device) -> int:
-    _on_device(t, name, device)
+def _vector(t, name: str, size: int, dtype, index: int) -> int:
+    if not isinstance(t, torch.Tensor) or t.get_device() != index or (t.requires_grad and torch.is_grad_enabled()):
+        _refuse(t, name, index)
     if t.dtype != dtype:
         raise TypeError(f"{name}: {dtype} expected, got {t.dtype}")
-    if t.dim() != 1 or t.shape[0] != size or (size > 1 and t.stride(0) != 1):
+    if t.shape != (size,) or (size > 1 and t.stride(0) != 1):
         raise ValueError(f"{name}: [{size}], contiguous, expected, got {tuple(t.shape)} of stride {t.stride()}")
     return t.data_ptr()
 
@@ -102,8 +114,12 @@ def _to_device(a, dtype, device, name: str):
     return a.to(device=device, dtype=dtype or a.dtype).contiguous()
 
 
-def _stream(device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+def _stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# (the same number without an object around it, where PyTorch has it)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream)
 
 
 class Norm:
@@ -117,16 +133,19 @@ class Norm:
         self.kind, self.eps = int(kind), float(eps)
         self.weight = None if weight is None else _to_device(weight, torch.float32, device, "weight")
         self.bias = None if bias is None else _to_device(bias, torch.float32, device, "bias")
+        self.width = self.index = None         # any, without vectors
         for t in (self.weight, self.bias):
             if t is not None:
-                if t.dim() != 1:
-                    raise ValueError(f"norm vectors: one dimension expected, got {tuple(t.shape)}")
+                if t.dim() != 1 or self.width not in (None, t.shape[0]) or self.index not in (None, t.get_device()):
+                    raise ValueError("norm vectors: one dimension, one size and one device expected")
+                self.width, self.index = t.shape[0], t.get_device()
                 torch.cuda.current_stream(t.device).synchronize()    # usable on every stream from here on
+        self._args = (self.kind, self.eps, 0 if self.weight is None else self.weight.data_ptr(), 0 if self.bias is None else self.bias.data_ptr())
 
-    def _packed(self, width: int, device, name: str):
-        return (self.kind, self.eps,
-                0 if self.weight is None else _vector(self.weight, f"{name}.weight", width, torch.float32, device),
-                0 if self.bias is None else _vector(self.bias, f"{name}.bias", width, torch.float32, device))
+    def _packed(self, width: int, index: int, name: str):
+        if self.width is not None and (self.width != width or self.index != index):
+            raise ValueError(f"{name}: vectors of {width} entries on cuda:{index} expected, got {self.width} on cuda:{self.index}")
+        return self._args
 
 
 _NO_NORM = (NORM_NONE, 0.0, 0, 0)
@@ -143,75 +162,74 @@ def norm_rows(y=None, *, post: Optional[Norm] = None, gate=None, gate_act: int =
     or residual if there are no ids, but overlap no input otherwise."""
     if y is None and residual is None:
         raise ValueError("neither y nor residual")
-    first = y if y is not None else residual
-    _on_device(first, "y" if y is not None else "residual")
-    device = first.device
-    if first.dim() != 2:
-        raise ValueError(f"two dimensions expected, got {tuple(first.shape)}")
+    first, name = (y, "y") if y is not None else (residual, "residual")
+    index = _device_of(first, name)
+    ptr, ld, rows = _matrix(first, name, None, None, index)
     width = first.shape[1]
     ids_ptr = gate_ptr = gate_ld = res_ptr = res_ld = res_rows = y_ptr = y_ld = vec_ptr = 0
     gate_width = 1
     if y is not None:
-        y_ptr, y_ld, rows = _matrix(y, "y", None, None, device)
-        dtype = y.dtype
-    elif gate is not None or post is not None:
-        raise ValueError("gate or post without y")
-    if residual is not None:
-        res_ptr, res_ld, res_rows = _matrix(residual, "residual", width, None, device)
-        stream_dtype = residual.dtype
+        y_ptr, y_ld, dtype = ptr, ld, y.dtype
+        if normed_dtype is not None and normed_dtype != dtype:
+            raise TypeError(f"normed_dtype: y's type, {dtype}, expected, got {normed_dtype}")
+        if residual is not None:
+            res_ptr, res_ld, res_rows = _matrix(residual, "residual", width, None, index)
+            stream_dtype = residual.dtype
+        else:
+            stream_dtype = dtype
     else:
-        stream_dtype = dtype
-    if y is None:
-        rows = res_rows
+        if gate is not None or post is not None:
+            raise ValueError("gate or post without y")
+        res_ptr, res_ld, res_rows, stream_dtype = ptr, ld, rows, residual.dtype
+        dtype = normed_dtype or stream_dtype
         if ids is not None:
             if getattr(ids, "dim", lambda: 0)() != 1:
                 raise ValueError("ids: one dimension expected")
             rows = ids.shape[0]
-        dtype = normed_dtype or stream_dtype
-    elif normed_dtype is not None and normed_dtype != dtype:
-        raise TypeError(f"normed_dtype: y's type, {dtype}, expected, got {normed_dtype}")
     t, ts = _type_of(dtype, "y" if y is not None else "normed_dtype"), _type_of(stream_dtype, "residual")
     if ts != t and ts != TYPE_F32:
         raise TypeError(f"residual: {dtype} or float32 expected, got {stream_dtype}")
     if ids is not None:
         if residual is None:
             raise ValueError("ids without residual")
-        ids_ptr = _vector(ids, "ids", rows, torch.int32, device)
+        ids_ptr = _vector(ids, "ids", rows, torch.int32, index)
     elif residual is not None and res_rows != rows:
         raise ValueError(f"residual: {rows} rows expected, got {res_rows}")
     if gate is not None:
-        gate_width = gate.shape[1] if isinstance(gate, torch.Tensor) and gate.dim() == 2 else 0
-        if gate_width not in (1, width):
-            raise ValueError(f"gate: [{rows}, {width}] or [{rows}, 1] expected")
-        gate_ptr, gate_ld, gr = _matrix(gate, "gate", None, dtype, device)
-        if gr != rows:
-            raise ValueError(f"gate: {rows} rows expected, got {gr}")
+        gate_ptr, gate_ld, gr = _matrix(gate, "gate", None, dtype, index)
+        gate_width = gate.shape[1]
+        if gate_width not in (1, width) or gr != rows:
+            raise ValueError(f"gate: [{rows}, {width}] or [{rows}, 1] expected, got {tuple(gate.shape)}")
     number = 1.0
     if isinstance(scale, torch.Tensor):
-        vec_ptr = _vector(scale, "scale", width, torch.float32, device)
+        vec_ptr = _vector(scale, "scale", width, torch.float32, index)
     else:
         number = float(scale)
-    if out is None and (y is not None or pre is None):
-        out = torch.empty((rows, width), dtype=stream_dtype, device=device)
     out_ptr = out_ld = n_ptr = n_ld = 0
     if out is not None:
-        out_ptr, out_ld, got = _matrix(out, "out", width, stream_dtype, device)
+        out_ptr, out_ld, got = _matrix(out, "out", width, stream_dtype, index)
         if got != rows:
             raise ValueError(f"out: {rows} rows expected, got {got}")
+    elif y is not None or pre is None:
+        out = torch.empty((rows, width), dtype=stream_dtype, device=first.device)
+        out_ptr, out_ld = out.data_ptr(), width
     if pre is not None:
         if normed_out is None:
-            normed_out = torch.empty((rows, width), dtype=dtype, device=device)
-        n_ptr, n_ld, got = _matrix(normed_out, "normed_out", width, dtype, device)
-        if got != rows:
-            raise ValueError(f"normed_out: {rows} rows expected, got {got}")
+            normed_out = torch.empty((rows, width), dtype=dtype, device=first.device)
+            n_ptr, n_ld = normed_out.data_ptr(), width
+        else:
+            n_ptr, n_ld, got = _matrix(normed_out, "normed_out", width, dtype, index)
+            if got != rows:
+                raise ValueError(f"normed_out: {rows} rows expected, got {got}")
     elif normed_out is not None:
         raise ValueError("normed_out without pre")
-    args = (_NO_NORM if post is None else post._packed(width, device, "post")) + (_NO_NORM if pre is None else pre._packed(width, device, "pre"))
+    post_args = _NO_NORM if post is None else post._packed(width, index, "post")
+    pre_args = _NO_NORM if pre is None else pre._packed(width, index, "pre")
     if rows == 0:
         return out, normed_out
     _check(_ripple.load_library().ripple_norm_rows(_NORM_ARGS.pack(
         rows, width, t, ts, int(gate_act), y_ptr, y_ld, gate_ptr, gate_ld, res_ptr, res_ld, res_rows, ids_ptr, vec_ptr,
-        out_ptr, out_ld, n_ptr, n_ld, *args, number, gate_width, device.index, 0, _stream(device))))
+        out_ptr, out_ld, n_ptr, n_ld, *post_args, *pre_args, number, gate_width, index, 0, _stream(index))))
     return out, normed_out
 
 
@@ -225,7 +243,7 @@ class Projection:
         if W.dim() != 2:
             raise ValueError(f"W: [K, N] expected, got {tuple(W.shape)}")
         self.lib = _ripple.load_library()
-        self.dtype, self.device = W.dtype, W.device
+        self.dtype, self.device, self.index = W.dtype, W.device, W.get_device()
         self.type = _type_of(W.dtype, "W")
         self.K, self.N = W.shape
         if act not in (ACT_IDENTITY, ACT_RELU):
@@ -239,8 +257,9 @@ class Projection:
             raise ValueError(f"bias: [{self.N}] expected, got {tuple(self.bias.shape)}")
         self.layout = torch.empty(size, dtype=torch.uint8, device=self.device)
         _check(self.lib.ripple_project_layout(self.type, self.K, self.N, W.data_ptr(), self.N, self.layout.data_ptr(),
-                                              self.device.index, _stream(self.device)))
+                                              self.index, _stream(self.index)))
         torch.cuda.current_stream(self.device).synchronize()     # usable on every stream from here on
+        self._tail = (self.layout.data_ptr(), 0 if self.bias is None else self.bias.data_ptr())
 
 
 class AdapterBank:
@@ -252,13 +271,14 @@ class AdapterBank:
         if not 1 <= self.slots <= MAX_SLOTS or not 1 <= self.max_rank <= MAX_RANK:
             raise ValueError(f"1 to {MAX_SLOTS} slots of rank 1 to {MAX_RANK} expected, got {slots} of {max_rank}")
         self.buffer = torch.empty(p.lib.ripple_adapter_bytes(p.type, p.K, p.N, self.slots, self.max_rank), dtype=torch.uint8, device=p.device)
+        self._scratch = (-1, 0)          # rows of the last call, and the scratch that it takes
         self._set(0, self.slots, 0, None, None, None)
 
     def _set(self, first, count, rank, A, B, scale):
         p = self.projection
         _check(p.lib.ripple_adapter_set(self.buffer.data_ptr(), p.type, p.K, p.N, self.slots, self.max_rank, first, count, rank,
                                         None if A is None else A.data_ptr(), None if B is None else B.data_ptr(), scale,
-                                        p.device.index, _stream(p.device)))
+                                        p.index, _stream(p.index)))
 
     def set(self, slot: int, A, B, scale: Union[float, Sequence[float]] = 1.0) -> None:
         """A [K, r], B [r, N] into `slot`; or A [m, K, r], B [m, r, N], scale: m numbers (or one for all) into `slot` and those
@@ -293,41 +313,47 @@ def project_rows(x, projection: Projection, bank: Optional[AdapterBank] = None, 
     range or empty: no adapter).  x [any, K] of the projection's type, ids int32 or None; the result has that type, or fp32 if
     out_dtype (or out) says so.  `out` shares no memory with an input."""
     p = projection
-    x_ptr, x_ld, x_rows = _matrix(x, "x", p.K, p.dtype, p.device)
+    index = p.index
+    x_ptr, x_ld, x_rows = _matrix(x, "x", p.K, p.dtype, index)
     rows, ids_ptr, bank_ptr, slots_ptr, n_slots, max_rank = x_rows, 0, 0, 0, 0, 0
     if ids is not None:
         if getattr(ids, "dim", lambda: 0)() != 1:
             raise ValueError("ids: one dimension expected")
         rows = ids.shape[0]
-        ids_ptr = _vector(ids, "ids", rows, torch.int32, p.device)
+        ids_ptr = _vector(ids, "ids", rows, torch.int32, index)
     if (bank is None) != (slots is None):
         raise ValueError("bank and slots go together")
     if bank is not None:
         if bank.projection is not p:
             raise ValueError("the bank belongs to another projection")
         bank_ptr, n_slots, max_rank = bank.buffer.data_ptr(), bank.slots, bank.max_rank
-        slots_ptr = _vector(slots, "slots", rows, torch.int32, p.device)
+        slots_ptr = _vector(slots, "slots", rows, torch.int32, index)
     if out is None:
         out = torch.empty((rows, p.N), dtype=out_dtype or p.dtype, device=p.device)
-    elif out_dtype is not None and out.dtype != out_dtype:
-        raise TypeError(f"out: {out_dtype} expected, got {out.dtype}")
-    y_ptr, y_ld, got = _matrix(out, "out", p.N, None, p.device)
-    if got != rows:
-        raise ValueError(f"out: {rows} rows expected, got {got}")
-    out_type = _type_of(out.dtype, "out")
+        y_ptr, y_ld = out.data_ptr(), p.N
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError(f"out: {out_dtype} expected, got {out.dtype}")
+        y_ptr, y_ld, got = _matrix(out, "out", p.N, None, index)
+        if got != rows:
+            raise ValueError(f"out: {rows} rows expected, got {got}")
+    out_type = p.type if out.dtype == p.dtype else _type_of(out.dtype, "out")
     if out_type not in (p.type, TYPE_F32):
         raise TypeError(f"out: {p.dtype} or float32 expected, got {out.dtype}")
     if rows == 0:
         return out
-    head = (rows, p.type, out_type, p.K, p.N, p.act, n_slots, max_rank, p.device.index, x_ptr, x_ld, x_rows, ids_ptr,
-            p.layout.data_ptr(), 0 if p.bias is None else p.bias.data_ptr(), bank_ptr, slots_ptr, y_ptr, y_ld)
-    need, work, work_ptr = 0, None, 0
+    head = (rows, p.type, out_type, p.K, p.N, p.act, n_slots, max_rank, index, x_ptr, x_ld, x_rows, ids_ptr, *p._tail, bank_ptr,
+            slots_ptr, y_ptr, y_ld)
+    need = work_ptr = 0
     if bank_ptr:
-        need = p.lib.ripple_project_workspace_bytes(_PROJECT_ARGS.pack(*head, 0, 0, 0))
+        known, need = bank._scratch
+        if known != rows:
+            need = p.lib.ripple_project_workspace_bytes(_PROJECT_ARGS.pack(*head, 0, 0, 0))
+            bank._scratch = (rows, need)
         if need > 0:
-            work = torch.empty(need, dtype=torch.uint8, device=p.device)
+            work = torch.empty(need, dtype=torch.uint8, device=p.device)     # of this call: the allocator keeps it until the stream has passed it
             work_ptr = work.data_ptr()
-    _check(p.lib.ripple_project_rows(_PROJECT_ARGS.pack(*head, work_ptr, need, _stream(p.device))))
+    _check(p.lib.ripple_project_rows(_PROJECT_ARGS.pack(*head, work_ptr, need, _stream(index))))
     return out
 
 
