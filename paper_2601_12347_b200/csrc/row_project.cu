@@ -14,7 +14,7 @@ namespace rp {
 constexpr int PJ_COLS = 128, PJ_KC = 64;
 constexpr int PJ_CHUNK = PJ_COLS * 128;
 // Bank: scale and rank of every slot; A transposed (rank x K, zeros beyond both; fp32 as three planes of bf16 parts); B transposed
-// (n x rank, zeros beyond the rank) in planes of bf16: one for bf16, two for fp16 (its 11 bits), three for fp32.
+// (n x rank, zeros beyond the rank) in planes of bf16: one for bf16, two for fp16 (its 11 bits), three for fp32; and the same in fp32.
 struct SlotInfo { float scale; int32_t rank; };
 
 __host__ __device__ inline int pj_parts(int type) { return type == RIPPLE_TYPE_F32 ? 3 : 1; }
@@ -30,16 +30,21 @@ struct BankView {
     const SlotInfo* info;
     const uint16_t* a;   // slot x plane x r_pad x k_pad
     const uint16_t* b;   // slot x plane x n x r_pad
+    const float* b32;    // slot x n x r_pad
     int r_pad, k_pad;
 };
 __host__ __device__ inline int64_t bank_a_at(int slots) { return up128((int64_t)slots * (int64_t)sizeof(SlotInfo) + 128); }
 __host__ __device__ inline int64_t bank_b_at(int type, int k, int slots, int max_rank) {
     return bank_a_at(slots) + up128((int64_t)slots * pj_up(max_rank, 16) * pj_up(k, PJ_KC) * pj_parts(type) * 2);
 }
-__host__ __device__ inline BankView bank_view(const void* bank, int type, int k, int slots, int max_rank) {
+__host__ __device__ inline int64_t bank_b32_at(int type, int k, int n, int slots, int max_rank) {
+    return bank_b_at(type, k, slots, max_rank) + up128((int64_t)slots * n * pj_up(max_rank, 16) * pj_b_planes(type) * 2);
+}
+__host__ __device__ inline BankView bank_view(const void* bank, int type, int k, int n, int slots, int max_rank) {
     const uint8_t* p = static_cast<const uint8_t*>(bank);
     return {reinterpret_cast<const SlotInfo*>(p), reinterpret_cast<const uint16_t*>(p + bank_a_at(slots)),
-            reinterpret_cast<const uint16_t*>(p + bank_b_at(type, k, slots, max_rank)), pj_up(max_rank, 16), pj_up(k, PJ_KC)};
+            reinterpret_cast<const uint16_t*>(p + bank_b_at(type, k, slots, max_rank)),
+            reinterpret_cast<const float*>(p + bank_b32_at(type, k, n, slots, max_rank)), pj_up(max_rank, 16), pj_up(k, PJ_KC)};
 }
 
 // An fp32 value as three bf16 parts, 8 bits each: the first cut (rounded, values next to the largest would become
@@ -51,13 +56,17 @@ __device__ __forceinline__ void pj_parts_of(float x, __nv_bfloat16 (&h)[3]) {
     h[2] = __float2bfloat16_rn(left - __bfloat162float(h[1]));
 }
 
-// two values; the remainders of an infinite one are NaN (the epilogue drops the small products where the large one is not finite)
+// Two values, every part cut: 8 + 8 + 8 bits, nothing left.  (The remainders of an infinite value are NaN: the epilogue drops the
+// small products where the large one is not finite.)
 __device__ __forceinline__ void pj_parts_of2(float x0, float x1, uint32_t& a, uint32_t& b, uint32_t& c) {
-    asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(a) : "f"(x1), "f"(x0));
-    x0 -= __uint_as_float(a << 16), x1 -= __uint_as_float(a & 0xffff0000u);
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b) : "f"(x1), "f"(x0));
-    x0 -= __uint_as_float(b << 16), x1 -= __uint_as_float(b & 0xffff0000u);
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(c) : "f"(x1), "f"(x0));
+    auto cut = [](float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); };
+    auto upper = [](float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); };
+    const float h0 = cut(x0), h1 = cut(x1);
+    a = upper(x0, x1);
+    x0 -= h0, x1 -= h1;
+    const float m0 = cut(x0), m1 = cut(x1);
+    b = upper(x0, x1);
+    c = upper(x0 - m0, x1 - m1);
 }
 
 // one thread per 16-byte piece of a 16-bit chunk: eight entries of K of one output column
@@ -99,7 +108,7 @@ __global__ void k_layout_weights(const T* W, int64_t ld, int k, int n, uint8_t* 
 
 // count adapters into the slots from `first`; bad: set where an entry is not finite
 template <int TYPE>
-__global__ void k_set_adapters(uint16_t* a_out, uint16_t* b_out, const typename Elem<TYPE>::T* A, const typename Elem<TYPE>::T* B, int first,
+__global__ void k_set_adapters(uint16_t* a_out, uint16_t* b_out, float* b32_out, const typename Elem<TYPE>::T* A, const typename Elem<TYPE>::T* B, int first,
                                int count, int rank, int k, int n, int r_pad, int k_pad, int* bad) {
     pdl_enter();
     using T = typename Elem<TYPE>::T;
@@ -127,6 +136,7 @@ __global__ void k_set_adapters(uint16_t* a_out, uint16_t* b_out, const typename 
             if (r < rank) v = B[(s * rank + r) * n + j];
             uint16_t* const to = b_out + (first + s) * PB * per_b + e;
             float left = to_f32(v);
+            b32_out[(first + s) * per_b + e] = left;
             for (int q = 0; q < PB; ++q) {
                 const __nv_bfloat16 h = q == 0 && PB == 3 ? __float2bfloat16_rz(left) : __float2bfloat16_rn(left);
                 to[q * per_b] = __bfloat16_as_ushort(h);
@@ -159,6 +169,7 @@ struct ProjectParams {
     int n_slots;
     const int32_t* slots;
     TilePlan* plan;        // one per 128 rows
+    float* base;           // JOINED: x_i W, rows x n up to a multiple of 16
     void* t;               // t_i = scale_a x_i A_a: fp32, rows x r_pad; 16-bit rows: two bf16 parts, rows x 2 x r_pad
     int batches;           // tensor-core form of t: batches of adapters that are multiplied side by side
     void* y;
@@ -208,9 +219,9 @@ __global__ void k_plan_tiles(const __grid_constant__ ProjectParams p) {
 }
 
 template <int TYPE>
-__device__ __forceinline__ void store_t(const ProjectParams& p, int64_t i, int r, float t) {
+__device__ __forceinline__ void store_t(const ProjectParams& p, int64_t i, int r, float t, bool parts) {
     const int rp = p.bank.r_pad;
-    if constexpr (TYPE == RIPPLE_TYPE_F32) {
+    if (TYPE == RIPPLE_TYPE_F32 || !parts) {
         static_cast<float*>(p.t)[i * rp + r] = t;
     } else {
         __nv_bfloat16* const to = static_cast<__nv_bfloat16*>(p.t) + i * 2 * rp + r;
@@ -239,7 +250,8 @@ template <typename T> __device__ __forceinline__ void load8(float (&v)[8], const
 }
 
 // Few rows: t_i by a block per ROWS rows, a warp per four ranks, eight entries of K per lane; rows of one adapter share its loads.
-// The rows lie in shared memory as fp32, SF_K entries at a time.  The blocks in front plan the tiles (of the tensor-core form).
+// The rows lie in shared memory as fp32, SF_K entries at a time.  The blocks in front plan the tiles (of the tensor-core form; for
+// k_project_few there are none, and t is fp32).
 constexpr int SF_K = 1024;
 template <int TYPE, int ROWS>
 __global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ ProjectParams p, int planned) {
@@ -336,7 +348,7 @@ __global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ Proj
                     float t = sum[q][0];
 #pragma unroll
                     for (int r = 1; r < RANKS; ++r) t = lane == r ? sum[q][r] : t;
-                    store_t<TYPE>(p, i0 + q, r0 + lane, r0 + lane < info.rank ? t * info.scale : 0.f);
+                    store_t<TYPE>(p, i0 + q, r0 + lane, r0 + lane < info.rank ? t * info.scale : 0.f, planned > 0);
                 }
             }
         }
@@ -351,7 +363,7 @@ constexpr int PF_ROWS = 16, PF_COLS = 32, PF_K = 256, PF_LD = 20;
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_project_few(const __grid_constant__ ProjectParams p) {
     using T = typename Elem<TYPE>::T;
-    constexpr int B_PLANES = pj_b_planes(TYPE), OWN = PF_K / 8;
+    constexpr int OWN = PF_K / 8;
     const bool adapted = p.bank.info != nullptr;
     if (!adapted) pdl_enter();           // with adapters the kernel before computes t: what it waited for is there, t is waited for below
     __shared__ __align__(16) float xs[2][PF_K * PF_LD];
@@ -384,15 +396,14 @@ __global__ void __launch_bounds__(256) k_project_few(const __grid_constant__ Pro
     bool live[2];
     int slot[2] = {-1, -1}, rank[2] = {0, 0};
     const int rp = p.bank.r_pad;
-    const int64_t plane = (int64_t)p.n * rp;
-    const __nv_bfloat16* b_at[2] = {};
+    const float* b_at[2] = {};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int i = i0 + 2 * warp + h;
         live[h] = i < p.rows && row_of(p, i) >= 0;
         if (adapted && i < p.rows) slot[h] = p.slots[i];
         if (slot[h] < 0 || slot[h] >= p.n_slots) slot[h] = -1;
-        b_at[h] = reinterpret_cast<const __nv_bfloat16*>(p.bank.b) + (int64_t)max(slot[h], 0) * B_PLANES * plane + (int64_t)col_in * rp;
+        b_at[h] = p.bank.b32 + ((int64_t)max(slot[h], 0) * p.n + col_in) * rp;
         if (slot[h] >= 0) rank[h] = p.bank.info[slot[h]].rank;
     }
     const float bias = p.bias ? p.bias[col_in] : 0.f;
@@ -432,22 +443,9 @@ __global__ void __launch_bounds__(256) k_project_few(const __grid_constant__ Pro
         y += bias;
         float d = 0.f;
         for (int k = 0; k < rank[h]; k += 8) {
-            float t[8], bv[8], more[8];
-            if constexpr (TYPE == RIPPLE_TYPE_F32) {
-                load8(t, static_cast<const float*>(p.t) + (int64_t)i * rp + k);
-            } else {
-                load8(t, static_cast<const __nv_bfloat16*>(p.t) + (int64_t)i * 2 * rp + k);
-                load8(more, static_cast<const __nv_bfloat16*>(p.t) + (int64_t)i * 2 * rp + rp + k);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) t[e] += more[e];
-            }
-            load8(bv, b_at[h] + (B_PLANES - 1) * plane + k);
-#pragma unroll
-            for (int q = B_PLANES - 2; q >= 0; --q) {
-                load8(more, b_at[h] + q * plane + k);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) bv[e] += more[e];
-            }
+            float t[8], bv[8];
+            load8(t, static_cast<const float*>(p.t) + (int64_t)i * rp + k);
+            load8(bv, b_at[h] + k);
 #pragma unroll
             for (int e = 0; e < 8; ++e) d = fmaf(t[e], bv[e], d);
         }
@@ -468,7 +466,7 @@ constexpr int PJ_ROWS = 128;             // rows per tile: the lanes of the accu
 constexpr int PJ_EPI_WARPS = 8;          // two per quarter of the lanes
 constexpr int PJ_FEW = 1024;             // rows up to which t is computed a block per row
 constexpr int64_t PJ_FEW_PRODUCTS = 64 << 20;   // rows x K x n up to which y is summed without tensor cores
-constexpr int PJ_SHRINK_COLS = 64;       // ranks of adapters side by side, where t is computed on the tensor cores
+constexpr int PJ_T_COLS = 64;            // ranks of adapters side by side, where t is computed on the tensor cores
 constexpr int PJ_UNIT = 4;               // fp32: chunks (256 entries of K) whose large products share an accumulator
 constexpr uint32_t PJ_SPIN_LIMIT = 1u << 22;
 constexpr int PJ_STAGING = PJ_EPI_WARPS * (32 * 17 + 128) * 4;    // the epilogue's turned blocks, and its bias
@@ -520,7 +518,8 @@ template <typename T> __device__ __forceinline__ uint4 word_of(const Piece<T, 8>
 
 // A persistent CTA takes tiles of 128 rows x BN columns: lanes of the accumulator are rows, its columns output columns.
 // SHRINK: the columns are the ranks of adapters that the tile's rows use, side by side, and each row keeps those of its own: t.
-// Else: columns of y; behind the steps over K come steps over ranks, the adapters of the tile one behind the other, where a
+// JOINED: columns of W, and behind them such ranks: one pass over the rows for both; k_finish_rows makes y of them.
+// RANKS: columns of y; behind the steps over K come steps over ranks, the adapters of the tile one behind the other, where a
 // row's operand is its t at its adapter's ranks and zero at all others.
 //   loaders    fetch the rows by id, chunk by chunk of 64 entries, into the swizzled layout that the tensor core reads: 16-bit
 //              rows as asynchronous copies, fp32 rows (and rows that are not 16-byte aligned) through registers,
@@ -531,11 +530,15 @@ template <typename T> __device__ __forceinline__ uint4 word_of(const Piece<T, 8>
 // and summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
 // Barriers, all waits bounded: full[s] (one arrival per loader warp, 16-bit rows: per thread; one with the bytes of the weights),
 // empty[s] (the products that read stage s), acc_full[b], acc_empty[b] (one arrival per epilogue warp).
-template <int TYPE, int BN, bool SHRINK, bool MANY>
+// What a launch of k_project_rows computes: t; y, with steps over ranks; or x W with t beside it.
+enum { PJ_SHRINK, PJ_RANKS, PJ_JOINED };
+
+template <int TYPE, int BN, int MODE, bool MANY>
 __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project_rows(const __grid_constant__ ProjectParams p) {
     using T = typename Elem<TYPE>::T;
     using S = PjShape<TYPE, BN, MANY>;
-    constexpr int PJ_LOADERS = S::LOADERS;
+    constexpr bool SHRINK = MODE == PJ_SHRINK, JOINED = MODE == PJ_JOINED, BATCHED = SHRINK || JOINED;
+    constexpr int PJ_LOADERS = S::LOADERS, A_COLS = SHRINK ? BN : PJ_T_COLS, W_COLS = JOINED ? BN - PJ_T_COLS : BN;
     constexpr int PARTS = S::PARTS, STAGES = S::STAGES, NB = BN / 32, RANKS = S::RANKS, B_PLANES = pj_b_planes(TYPE);
     constexpr uint32_t TMEM = S::TMEM;
     extern __shared__ uint8_t smem_raw[];
@@ -544,32 +547,33 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
     __shared__ volatile int s_fail;
 
     const int tid = threadIdx.x, warp = __shfl_sync(FULL, tid >> 5, 0), lane = tid & 31;
-    const int across = SHRINK ? p.batches : (p.n + BN - 1) / BN, row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
+    const int across = SHRINK ? p.batches : (p.n + W_COLS - 1) / W_COLS, row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
     const int64_t tiles = (int64_t)across * row_tiles;
     const int my_tiles = (int)((tiles - blockIdx.x + gridDim.x - 1) / gridDim.x), chunks = p.chunks;
-    const int r_pad = p.bank.r_pad, at_once = SHRINK ? BN / r_pad : 0;
+    const int r_pad = p.bank.r_pad, at_once = BATCHED && r_pad ? A_COLS / r_pad : 0;
     uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    // A tile: 128 rows, and a tile of columns or a batch of adapters (SHRINK: every `across`-th batch of the row tile's, as many as
-    // its adapters fill).  The next row tile's count of adapters is asked for early.
-    struct Tile { int lt, rows, part, count, count_next; };
+    // A tile: 128 rows, a tile of columns, and (SHRINK, JOINED) a batch of adapters: SHRINK takes every `across`-th batch that the
+    // adapters of the rows fill, JOINED all of them (one where there are none).  The next row tile's count of adapters is asked for early.
+    struct Tile { int lt, rows, part, batch, count, count_next; };
     auto row_tile = [&](int lt) { return (int)((blockIdx.x + (int64_t)lt * gridDim.x) / across); };
     auto part_of = [&](int lt) { return (int)((blockIdx.x + (int64_t)lt * gridDim.x) % across); };
     auto adapters = [&](int lt) { return p.plan && lt < my_tiles ? p.plan[row_tile(lt)].count : 0; };
     auto after = [&](const Tile& t) {
         Tile n = t;
-        if constexpr (SHRINK) n.part += across;
-        while (!SHRINK || n.part * at_once >= n.count) {
+        if constexpr (BATCHED) n.batch += SHRINK ? across : 1;
+        while (!BATCHED || n.batch * at_once >= n.count) {
             if (++n.lt >= my_tiles) break;
-            n.rows = row_tile(n.lt), n.part = part_of(n.lt), n.count = n.count_next;
+            n.rows = row_tile(n.lt), n.part = part_of(n.lt), n.batch = SHRINK ? n.part : 0, n.count = n.count_next;
             n.count_next = adapters(n.lt + 1);
             if (!SHRINK) break;
         }
         return n;
     };
-    auto first_tile = [&]() { return after(Tile{-1, 0, 0, 0, adapters(0)}); };
-    // columns that are multiplied
-    auto tile_n = [&](const Tile& t) { return SHRINK ? min(at_once, t.count - t.part * at_once) * r_pad : min(BN, (p.n - t.part * BN + 15) & ~15); };
-    auto rank_steps = [&](int count) { return SHRINK ? 0 : (count * r_pad + RANKS - 1) / RANKS; };
+    auto first_tile = [&]() { return after(Tile{-1, 0, 0, 0, 0, adapters(0)}); };
+    // columns that are multiplied: of W, and ranks of the batch behind them
+    auto tile_w = [&](const Tile& t) { return SHRINK ? 0 : min(W_COLS, (p.n - t.part * W_COLS + 15) & ~15); };
+    auto tile_n = [&](const Tile& t) { return tile_w(t) + (BATCHED ? min(at_once, t.count - t.batch * at_once) * r_pad : 0); };
+    auto rank_steps = [&](int count) { return BATCHED ? 0 : (count * r_pad + RANKS - 1) / RANKS; };
 
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], (PARTS == 3 ? PJ_LOADERS / 32 : PJ_LOADERS) + (SHRINK ? 0 : 1)); mbar_init(&empty[s], 1); }
@@ -590,7 +594,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
 
     if (warp < PJ_LOADERS / 32) {
         // ---------------- rows, and what comes out of the bank ----------------
-        constexpr int RSTEP = PJ_LOADERS / 8, ITS = PJ_ROWS / RSTEP, W_ITS = (BN + RSTEP - 1) / RSTEP;
+        constexpr int RSTEP = PJ_LOADERS / 8, ITS = PJ_ROWS / RSTEP, W_ITS = ((BATCHED ? A_COLS : BN) + RSTEP - 1) / RSTEP;
         const int c = tid & 7, rb = tid >> 3;       // thread: piece c (8 entries) of the rows rb + RSTEP it
         const uint32_t mine = smem_u32(ring) + tc_swz(rb, c);
         const bool vec = (reinterpret_cast<uintptr_t>(p.x) & 15) == 0 && p.ld_x % (16 / (int)sizeof(T)) == 0;
@@ -602,8 +606,8 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
         // their results are dropped); of the rows of A; the rows' places among the adapters, a byte each; and all of it for the next tile.
         const T* const x0 = static_cast<const T*>(p.x) + c * 8;
         const T* at[ITS];
-        const uint16_t* a_at[SHRINK ? W_ITS : 1];
-        int next[ITS], slot_next[SHRINK ? W_ITS : 1], slot0 = -1;
+        const uint16_t* a_at[BATCHED ? W_ITS : 1];
+        int next[ITS], slot_next[BATCHED ? W_ITS : 1], slot0 = -1;
         uint32_t which = 0, which_next = 0;
         auto aim = [&](const Tile& t) {
             if (t.lt >= my_tiles) return;
@@ -615,10 +619,10 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
             }
             if (!p.plan) return;
             const TilePlan& plan = p.plan[t.rows];
-            if constexpr (SHRINK) {                 // slots of the rows of A that this thread fetches
+            if constexpr (BATCHED) {                // slots of the rows of A that this thread fetches
 #pragma unroll
                 for (int it = 0; it < W_ITS; ++it) {
-                    const int n = rb + RSTEP * it, j = t.part * at_once + n / r_pad;
+                    const int n = rb + RSTEP * it, j = t.batch * at_once + n / r_pad;
                     slot_next[it] = n < at_once * r_pad && j < t.count ? plan.slot[j] : -1;
                 }
             } else if (t.count) {
@@ -633,11 +637,11 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
 #pragma unroll
             for (int it = 0; it < ITS; ++it) at[it] = x0 + next[it] * p.ld_x;
             which = which_next;
-            if constexpr (SHRINK) {
+            if constexpr (BATCHED) {
                 const int64_t plane = (int64_t)r_pad * p.bank.k_pad;
 #pragma unroll
                 for (int it = 0; it < W_ITS; ++it)
-                    a_at[it] = slot_next[it] < 0 ? nullptr : p.bank.a + (int64_t)slot_next[it] * PARTS * plane + (int64_t)((rb + RSTEP * it) % r_pad) * p.bank.k_pad + c * 8;
+                    a_at[it] = !p.plan || slot_next[it] < 0 ? nullptr : p.bank.a + (int64_t)slot_next[it] * PARTS * plane + (int64_t)((rb + RSTEP * it) % r_pad) * p.bank.k_pad + c * 8;
             } else {
                 slot0 = slot_next[0];
             }
@@ -713,9 +717,9 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
             for (int st = 0; st < steps; ++st) {
                 ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
                 if (!ok) break;
-                const uint32_t x_to = mine + (uint32_t)(s * S::STAGE), w_to = x_to + S::X_STAGE;
+                const uint32_t x_to = mine + (uint32_t)(s * S::STAGE), w_to = x_to + S::X_STAGE + (JOINED ? 128 * tile_w(tile) : 0);
                 if (st < chunks) {
-                    if constexpr (SHRINK) {
+                    if constexpr (BATCHED) {
                         const int64_t plane = (int64_t)r_pad * p.bank.k_pad;
 #pragma unroll
                         for (int it = 0; it < W_ITS; ++it) {
@@ -737,7 +741,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
 #pragma unroll
                         for (int it = 0; it < ITS; ++it) copy_some(x_to + it * (RSTEP * 128), tail > 0 ? at[it] : at[it] - c * 8, tail > 0 ? 2 * tail : 0);
                     }
-                } else if constexpr (!SHRINK) {
+                } else if constexpr (!BATCHED) {
                     const int step = st - chunks, q = step * RANKS + c_rank, j = q / r_pad, r = q % r_pad;
                     const int slot = step == 0 ? slot0 : j < tile.count ? p.plan[tile.rows].slot[j] : -1;
                     const int64_t plane = (int64_t)p.n * r_pad;
@@ -802,24 +806,24 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
         int sg = 0, worked = 0;                 // accumulators and tiles taken so far
         for (Tile tile = first_tile(); tile.lt < my_tiles && ok; tile = after(tile)) {
             // thread: a row, and the 16-column blocks half, half + 2, ... of the tile
-            const int nt = tile_n(tile);
-            const int i = tile.rows * PJ_ROWS + 32 * q + lane, c0 = SHRINK ? 0 : tile.part * BN;
-            int own = -1, rank = 0;            // SHRINK: the row's adapter within the batch
+            const int nt = tile_n(tile), nw = tile_w(tile);
+            const int i = tile.rows * PJ_ROWS + 32 * q + lane, c0 = SHRINK ? 0 : tile.part * W_COLS;
+            int own = -1, rank = 0;            // SHRINK, JOINED: the row's adapter within the batch
             float scale = 0.f;
             bool live = i < p.rows;
-            if constexpr (SHRINK) {
+            if (!SHRINK) live = live && row_of(p, i) >= 0;
+            if (BATCHED && p.plan) {
                 const TilePlan& plan = p.plan[tile.rows];
                 const int at = plan.row[32 * q + lane];
                 if (at != PJ_NONE) {
                     const SlotInfo info = p.bank.info[plan.slot[at]];
                     rank = info.rank, scale = info.scale;
-                    own = at - tile.part * at_once;
+                    own = at - tile.batch * at_once;
                 }
-            } else {
-                live = live && row_of(p, i) >= 0;
+                live = live && tile.batch == 0;       // (JOINED: W's columns are multiplied with every batch, and kept with the first)
             }
             const uint32_t rows_live = __ballot_sync(FULL, live);
-            if constexpr (!SHRINK) {                // the bias of this warp's columns, while the products are still on their way
+            if constexpr (!BATCHED) {               // the bias of this warp's columns, while the products are still on their way
                 __syncwarp();
                 for (int e = lane; e < 16 * NB; e += 32) {
                     const int col = c0 + 16 * (2 * (e >> 4) + half) + (e & 15);
@@ -829,7 +833,18 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
             }
             // 16 finished sums of this row, from column `at` of the tile
             auto finish = [&](float (&y)[16], int at) {
-                if constexpr (SHRINK) {
+                if (JOINED && at < nw) {
+                    if (live) {
+                        float* const to = p.base + (int64_t)i * pj_up(p.n, 16) + c0 + at;
+                        uint32_t v[8], w[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = __float_as_uint(y[e]), w[e] = __float_as_uint(y[8 + e]);
+                        pj_store8(to, v), pj_store8(to + 8, w);
+                    }
+                    return;
+                }
+                if constexpr (BATCHED) {
+                    at -= nw;
                     if (own < 0 || own != at / r_pad) return;
                     const int r = at % r_pad;
                     uint32_t v[8], w[8];
@@ -1034,10 +1049,10 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
         uint32_t ph = 1;
         bool ok = true;
         for (Tile tile = first_tile(); tile.lt < my_tiles && ok; tile = after(tile)) {
-            const int steps = chunks + rank_steps(tile.count), c0 = tile.part * BN, bytes = tile_n(tile) * 128;
-            // (tiles of 256 columns: two groups of the layout, one behind the other in shared memory)
-            const uint8_t* from = p.layout + (int64_t)(c0 / PJ_COLS) * chunks * PARTS * PJ_CHUNK + c0 % PJ_COLS * 128;
-            const int bytes1 = min(bytes, PJ_CHUNK), bytes2 = bytes - bytes1;
+            const int steps = chunks + rank_steps(tile.count), c0 = tile.part * W_COLS, bytes = tile_w(tile) * 128;
+            // (a tile's columns may lie in two groups of the layout, and one behind the other in shared memory)
+            const int skip = c0 % PJ_COLS * 128, bytes1 = min(bytes, PJ_CHUNK - skip), bytes2 = bytes - bytes1;
+            const uint8_t* from = p.layout + (int64_t)(c0 / PJ_COLS) * chunks * PARTS * PJ_CHUNK;
             for (int st = 0; st < steps; ++st, ++g, from += PARTS * PJ_CHUNK) {
                 ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
                 if (!ok) break;
@@ -1045,8 +1060,8 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                     mbar_expect(&full[s], PARTS * bytes);
                     for (int part = 0; part < PARTS; ++part) {
                         uint8_t* const to = ring + s * S::STAGE + S::X_STAGE + part * S::W_PART;
-                        tc_copy_bulk(to, from + part * PJ_CHUNK, bytes1, &full[s]);
-                        if (BN > PJ_COLS && bytes2 > 0) tc_copy_bulk(to + PJ_CHUNK, from + ((int64_t)chunks * PARTS + part) * PJ_CHUNK, bytes2, &full[s]);
+                        tc_copy_bulk(to, from + part * PJ_CHUNK + skip, bytes1, &full[s]);
+                        if (bytes2 > 0) tc_copy_bulk(to + bytes1, from + ((int64_t)chunks * PARTS + part) * PJ_CHUNK, bytes2, &full[s]);
                     }
                 } else {
                     mbar_arrive(&full[s]);       // (the loaders bring what a step over ranks reads)
@@ -1069,51 +1084,129 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM) : "memory");
 }
 
-template <int TYPE, int BN, bool SHRINK, bool MANY>
+// y = act(x W + bias + t B), x W and t from memory: a lane is a column and keeps its row of B (RB x 16 ranks) in registers while the
+// rows are those of one adapter; FR_ROWS rows one after the other, four requested at once.
+// Bound by the bytes of x W, t and y.
+constexpr int FR_COLS = 64, FR_ROWS = 16;
+template <typename T, int RB>
+__global__ void __launch_bounds__(256) k_finish_rows(const __grid_constant__ ProjectParams p) {
+    pdl_enter();
+    const int col = threadIdx.x % FR_COLS, i0 = (blockIdx.x * (256 / FR_COLS) + threadIdx.x / FR_COLS) * FR_ROWS, rp = p.bank.r_pad, ld = pj_up(p.n, 16);
+    if (col >= p.n) return;
+    const float bias = p.bias ? p.bias[col] : 0.f;
+    float4 b[RB][4];
+    int have = -1, rank = 0;
+    for (int i = i0; i < min(i0 + FR_ROWS, p.rows); i += 4) {
+        int slot[4];
+        bool live[4];
+        float x[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int at = min(i + q, p.rows - 1);
+            live[q] = i + q < p.rows && row_of(p, at) >= 0;
+            slot[q] = p.slots[at];
+            x[q] = p.base[(int64_t)at * ld + col];
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (!live[q]) continue;
+            const int a = slot[q] >= 0 && slot[q] < p.n_slots ? slot[q] : -1;
+            if (a >= 0 && a != have) {
+                have = a;
+                rank = p.bank.info[a].rank;
+                const float4* const from = reinterpret_cast<const float4*>(p.bank.b32 + ((int64_t)a * p.n + col) * rp);
+                if (rank > 0) {
+#pragma unroll
+                    for (int k = 0; k < RB; ++k)
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) b[k][h] = __ldg(from + 4 * k + h);
+                }
+            }
+            float y = x[q] + bias;
+            if (a >= 0 && rank > 0) {
+                const float4* const t = reinterpret_cast<const float4*>(static_cast<const float*>(p.t) + (int64_t)(i + q) * rp);
+                float d = 0.f;
+#pragma unroll
+                for (int k = 0; k < RB; ++k)
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const float4 v = __ldg(t + 4 * k + h);
+                        d = fmaf(v.x, b[k][h].x, d), d = fmaf(v.y, b[k][h].y, d), d = fmaf(v.z, b[k][h].z, d), d = fmaf(v.w, b[k][h].w, d);
+                    }
+                y += d;
+            }
+            if (p.act == RIPPLE_ACT_RELU && y < 0.f) y = 0.f;
+            static_cast<T*>(p.y)[(int64_t)(i + q) * p.ld_y + col] = from_f32<T>(y);
+        }
+    }
+}
+
+static cudaError_t finish_rows(const ProjectParams& p, void* stream) {
+    const int per = 256 / FR_COLS * FR_ROWS;
+    const dim3 grid((p.rows + per - 1) / per);
+    switch (p.bank.r_pad / 16) {
+        case 1: return launch(k_finish_rows<float, 1>, grid, 256, 0, stream, p);
+        case 2: return launch(k_finish_rows<float, 2>, grid, 256, 0, stream, p);
+        case 3: return launch(k_finish_rows<float, 3>, grid, 256, 0, stream, p);
+        default: return launch(k_finish_rows<float, 4>, grid, 256, 0, stream, p);
+    }
+}
+
+template <int TYPE, int BN, int MODE, bool MANY>
 static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
     using S = PjShape<TYPE, BN, MANY>;
     static bool ready[64];       // by device
-    const cudaError_t e = allow_shared(k_project_rows<TYPE, BN, SHRINK, MANY>, (int)S::BYTES, ready);
+    const cudaError_t e = allow_shared(k_project_rows<TYPE, BN, MODE, MANY>, (int)S::BYTES, ready);
     if (e != cudaSuccess) return e;
-    const int64_t across = SHRINK ? p.batches : (p.n + BN - 1) / BN, tiles = across * ((p.rows + PJ_ROWS - 1) / PJ_ROWS);
-    return launch(k_project_rows<TYPE, BN, SHRINK, MANY>, dim3((unsigned)std::min<int64_t>(tiles, sm_count())), S::THREADS, S::BYTES, stream, p);
+    const int columns = MODE == PJ_JOINED ? BN - PJ_T_COLS : BN;
+    const int64_t across = MODE == PJ_SHRINK ? p.batches : (p.n + columns - 1) / columns, tiles = across * ((p.rows + PJ_ROWS - 1) / PJ_ROWS);
+    return launch(k_project_rows<TYPE, BN, MODE, MANY>, dim3((unsigned)std::min<int64_t>(tiles, sm_count())), S::THREADS, S::BYTES, stream, p);
 }
-template <int TYPE, int BN, bool SHRINK>
+template <int TYPE, int BN, int MODE>
 static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
     if constexpr (TYPE == RIPPLE_TYPE_F32) {
-        if (p.chunks > PJ_UNIT) return project_tiles<TYPE, BN, SHRINK, true>(p, stream);
+        if (p.chunks > PJ_UNIT) return project_tiles<TYPE, BN, MODE, true>(p, stream);
     }
-    return project_tiles<TYPE, BN, SHRINK, false>(p, stream);
+    return project_tiles<TYPE, BN, MODE, false>(p, stream);
 }
 
 template <int TYPE>
 static cudaError_t project(ProjectParams p, void* stream) {
+    constexpr bool F32 = TYPE == RIPPLE_TYPE_F32;
     const int row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
     const bool few = (int64_t)p.rows * p.k * p.n <= PJ_FEW_PRODUCTS && p.rows <= PJ_FEW;
+    cudaError_t e = cudaSuccess;
     if (p.bank.info) {
-        cudaError_t e;
+        // fp32, narrow: x W and t in one pass over the rows, whose parts are what takes the time
+        if constexpr (F32) {
+            if (p.base) {
+                e = launch(k_plan_tiles, dim3(row_tiles), 128, 0, stream, p);
+                if (e == cudaSuccess) e = project_tiles<TYPE, 128, PJ_JOINED>(p, stream);
+                return e == cudaSuccess ? finish_rows(p, stream) : e;
+            }
+        }
         if (p.rows <= PJ_FEW) {
             const int planned = few ? 0 : row_tiles;
             // (four rows per block once there are several blocks for every SM)
             if (p.rows <= 4 * sm_count()) e = launch(k_shrink_few<TYPE, 1>, dim3(planned + p.rows), 128, 0, stream, p, planned);
             else e = launch(k_shrink_few<TYPE, 4>, dim3(planned + (p.rows + 3) / 4), 128, 0, stream, p, planned);
         } else {
-            const int at_once = PJ_SHRINK_COLS / p.bank.r_pad;
+            const int at_once = PJ_T_COLS / p.bank.r_pad;
             // batches of adapters side by side while there are SMs for them, one behind the other beyond
             const int batches = (std::min(p.n_slots, PJ_ROWS) + at_once - 1) / at_once;
             p.batches = std::max(1, std::min(batches, sm_count() / row_tiles));
             e = launch(k_plan_tiles, dim3(row_tiles), 128, 0, stream, p);
-            if (e == cudaSuccess) e = project_tiles<TYPE, PJ_SHRINK_COLS, true>(p, stream);
+            if (e == cudaSuccess) e = project_tiles<TYPE, PJ_T_COLS, PJ_SHRINK>(p, stream);
         }
         if (e != cudaSuccess) return e;
     }
     if (few) return launch(k_project_few<TYPE>, dim3((p.rows + PF_ROWS - 1) / PF_ROWS, (p.n + PF_COLS - 1) / PF_COLS), 256, 0, stream, p);
     // Tiles of 32 columns where those of 128 would leave most SMs without one; of 256 (16-bit rows) where those leave none.
     const int64_t wide = (int64_t)((p.n + 127) / 128) * row_tiles;
-    if constexpr (TYPE != RIPPLE_TYPE_F32) {
-        if (p.n > 128 && (int64_t)((p.n + 255) / 256) * row_tiles >= sm_count()) return project_tiles<TYPE, 256, false>(p, stream);
+    if constexpr (!F32) {
+        if (p.n > 128 && (int64_t)((p.n + 255) / 256) * row_tiles >= sm_count()) return project_tiles<TYPE, 256, PJ_RANKS>(p, stream);
     }
-    return wide >= sm_count() / 2 ? project_tiles<TYPE, 128, false>(p, stream) : project_tiles<TYPE, 32, false>(p, stream);
+    return wide >= sm_count() / 2 ? project_tiles<TYPE, 128, PJ_RANKS>(p, stream) : project_tiles<TYPE, 32, PJ_RANKS>(p, stream);
 }
 
 }  // namespace rp
@@ -1141,7 +1234,7 @@ extern "C" int64_t ripple_project_layout_bytes(int32_t type, int32_t k, int32_t 
 
 extern "C" int64_t ripple_adapter_bytes(int32_t type, int32_t k, int32_t n, int32_t slots, int32_t max_rank) {
     if (!shape_ok(type, k, n) || !bank_ok(slots, max_rank)) return -1;
-    return bank_b_at(type, k, slots, max_rank) + up128((int64_t)slots * n * pj_up(max_rank, 16) * pj_b_planes(type) * 2);
+    return bank_b32_at(type, k, n, slots, max_rank) + up128((int64_t)slots * n * pj_up(max_rank, 16) * 4);
 }
 
 extern "C" ripple_status ripple_project_layout(int32_t type, int32_t k, int32_t n, const void* W, int64_t ld_w, void* layout,
@@ -1177,7 +1270,7 @@ extern "C" ripple_status ripple_adapter_set(void* bank, int32_t type, int32_t k,
     OnDevice on(device);
     if (on.err != cudaSuccess) return launch_failed("cudaSetDevice", on.err);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const BankView v = bank_view(bank, type, k, slots, max_rank);
+    const BankView v = bank_view(bank, type, k, n, slots, max_rank);
     SlotInfo* info = const_cast<SlotInfo*>(v.info);
     // (the 128 bytes behind the slots' table: the flag)
     int* bad = reinterpret_cast<int*>(static_cast<uint8_t*>(bank) + bank_a_at(slots) - 128);
@@ -1187,9 +1280,10 @@ extern "C" ripple_status ripple_adapter_set(void* bank, int32_t type, int32_t k,
     if (e == cudaSuccess && rank > 0) {
         const dim3 grid(592);
         uint16_t *a = const_cast<uint16_t*>(v.a), *b = const_cast<uint16_t*>(v.b);
-        if (type == RIPPLE_TYPE_F32) e = launch(k_set_adapters<RIPPLE_TYPE_F32>, grid, 256, 0, cuda_stream, a, b, (const float*)A, (const float*)B, first, count, rank, k, n, v.r_pad, v.k_pad, bad);
-        else if (type == RIPPLE_TYPE_BF16) e = launch(k_set_adapters<RIPPLE_TYPE_BF16>, grid, 256, 0, cuda_stream, a, b, (const __nv_bfloat16*)A, (const __nv_bfloat16*)B, first, count, rank, k, n, v.r_pad, v.k_pad, bad);
-        else e = launch(k_set_adapters<RIPPLE_TYPE_F16>, grid, 256, 0, cuda_stream, a, b, (const __half*)A, (const __half*)B, first, count, rank, k, n, v.r_pad, v.k_pad, bad);
+        float* const b32 = const_cast<float*>(v.b32);
+        if (type == RIPPLE_TYPE_F32) e = launch(k_set_adapters<RIPPLE_TYPE_F32>, grid, 256, 0, cuda_stream, a, b, b32, (const float*)A, (const float*)B, first, count, rank, k, n, v.r_pad, v.k_pad, bad);
+        else if (type == RIPPLE_TYPE_BF16) e = launch(k_set_adapters<RIPPLE_TYPE_BF16>, grid, 256, 0, cuda_stream, a, b, b32, (const __nv_bfloat16*)A, (const __nv_bfloat16*)B, first, count, rank, k, n, v.r_pad, v.k_pad, bad);
+        else e = launch(k_set_adapters<RIPPLE_TYPE_F16>, grid, 256, 0, cuda_stream, a, b, b32, (const __half*)A, (const __half*)B, first, count, rank, k, n, v.r_pad, v.k_pad, bad);
         if (e == cudaSuccess) e = cudaMemcpyAsync(&host_bad, bad, sizeof(int), cudaMemcpyDeviceToHost, st);
         if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     }
@@ -1204,11 +1298,16 @@ extern "C" ripple_status ripple_adapter_set(void* bank, int32_t type, int32_t k,
     return RIPPLE_OK;
 }
 
+static bool pj_joined(const ripple_project_rows_args* a) {
+    return a->bank && a->type == RIPPLE_TYPE_F32 && a->rows > PJ_FEW && a->n <= 128 - PJ_T_COLS;
+}
+
 extern "C" int64_t ripple_project_workspace_bytes(const ripple_project_rows_args* a) {
     if (!a || a->rows < 0 || !shape_ok(a->type, a->k, a->n)) return -1;
     if (!a->bank) return 0;
     if (!bank_ok(a->n_slots, a->max_rank)) return -1;
-    return (a->rows + 127) / 128 * (int64_t)sizeof(TilePlan) + up128(a->rows * pj_up(a->max_rank, 16) * 4);
+    return (a->rows + 127) / 128 * (int64_t)sizeof(TilePlan) + up128(a->rows * pj_up(a->max_rank, 16) * 4)
+           + (pj_joined(a) ? up128(a->rows * pj_up(a->n, 16) * 4) : 0);
 }
 
 extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) {
@@ -1246,10 +1345,11 @@ extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) 
     p.x = a->x, p.ld_x = a->ld_x, p.x_rows = a->x_rows, p.ids = a->ids;
     p.layout = static_cast<const uint8_t*>(a->layout), p.bias = a->bias;
     p.plain = p.layout + layout_plain_at(a->type, a->k, a->n);
-    if (a->bank) p.bank = bank_view(a->bank, a->type, a->k, a->n_slots, a->max_rank);
+    if (a->bank) p.bank = bank_view(a->bank, a->type, a->k, a->n, a->n_slots, a->max_rank);
     p.n_slots = a->n_slots, p.slots = a->slots, p.plan = static_cast<TilePlan*>(a->workspace);
     if (a->bank) p.t = static_cast<uint8_t*>(a->workspace) + (a->rows + 127) / 128 * (int64_t)sizeof(TilePlan);
     else p.plan = nullptr;
+    if (pj_joined(a)) p.base = reinterpret_cast<float*>(static_cast<uint8_t*>(p.t) + up128(a->rows * pj_up(a->max_rank, 16) * 4));
     p.y = a->y, p.ld_y = a->ld_y, p.out_f32 = a->out_type == RIPPLE_TYPE_F32;
     cudaError_t e;
     if (a->type == RIPPLE_TYPE_F32) e = project<RIPPLE_TYPE_F32>(p, a->cuda_stream);
