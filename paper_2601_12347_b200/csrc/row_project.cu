@@ -476,7 +476,9 @@ template <int TYPE, int BN, bool MANY> struct PjShape {
     static constexpr int PARTS = TYPE == RIPPLE_TYPE_F32 ? 3 : 1;
     static constexpr int LOADERS = PARTS == 3 && !MANY ? 512 : 256;            // threads that fetch rows
     static constexpr int THREADS = LOADERS + 32 * PJ_EPI_WARPS + 64;          // and the warps that issue and that fetch weights
-    static constexpr uint32_t TMEM = (PARTS == 3 ? 4 : 2) * BN;               // two accumulators and, fp32, two for the small products
+    // columns of tensor memory: two accumulators and, fp32, two for the small products, or room for three of them each
+    static constexpr int BUFFER = PARTS == 1 ? BN : BN == 128 ? 256 : BN == 64 ? 256 : 128;
+    static constexpr uint32_t TMEM = PARTS == 3 && MANY ? 4 * BN : 2 * BUFFER;
     static constexpr int X_PART = PJ_ROWS * 128, X_STAGE = PARTS * X_PART;
     static constexpr int W_PART = BN * 128, W_STAGE = PARTS * W_PART;
     static constexpr int STAGE = X_STAGE + W_STAGE;
@@ -539,6 +541,11 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
     using S = PjShape<TYPE, BN, MANY>;
     constexpr bool SHRINK = MODE == PJ_SHRINK, JOINED = MODE == PJ_JOINED, BATCHED = SHRINK || JOINED;
     constexpr int PJ_LOADERS = S::LOADERS, A_COLS = SHRINK ? BN : PJ_T_COLS, W_COLS = JOINED ? BN - PJ_T_COLS : BN;
+    // fp32, narrow tiles: the parts of W lie one behind the other and are multiplied at once, x1 [w1 w2 w3], x2 [w1 w2], x3 w1: half the
+    // instructions, and two thirds of what they read of shared memory.  Accumulators: large, small, small.
+    // (Whether a tile is narrow is a matter of the projection alone, not of the adapters that its rows happen to use: a row's result does not
+    // depend on its neighbours.)
+    constexpr int SIDE = S::PARTS == 3 && !MANY ? (BN < S::BUFFER / 3 ? BN : S::BUFFER / 3 / 16 * 16) : 0;      // up to so many columns
     constexpr int PARTS = S::PARTS, STAGES = S::STAGES, NB = BN / 32, RANKS = S::RANKS, B_PLANES = pj_b_planes(TYPE);
     constexpr uint32_t TMEM = S::TMEM;
     extern __shared__ uint8_t smem_raw[];
@@ -550,7 +557,9 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
     const int across = SHRINK ? p.batches : (p.n + W_COLS - 1) / W_COLS, row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
     const int64_t tiles = (int64_t)across * row_tiles;
     const int my_tiles = (int)((tiles - blockIdx.x + gridDim.x - 1) / gridDim.x), chunks = p.chunks;
-    const int r_pad = p.bank.r_pad, at_once = BATCHED && r_pad ? A_COLS / r_pad : 0;
+    const int r_pad = p.bank.r_pad, joined_w = (p.n + 15) & ~15;
+    const bool joined_side = JOINED && SIDE > 0 && joined_w + r_pad <= SIDE;
+    const int at_once = BATCHED && r_pad ? (joined_side ? min(A_COLS, SIDE - joined_w) : A_COLS) / r_pad : 0;
     uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     // A tile: 128 rows, a tile of columns, and (SHRINK, JOINED) a batch of adapters: SHRINK takes every `across`-th batch that the
     // adapters of the rows fill, JOINED all of them (one where there are none).  The next row tile's count of adapters is asked for early.
@@ -573,6 +582,13 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
     // columns that are multiplied: of W, and ranks of the batch behind them
     auto tile_w = [&](const Tile& t) { return SHRINK ? 0 : min(W_COLS, (p.n - t.part * W_COLS + 15) & ~15); };
     auto tile_n = [&](const Tile& t) { return tile_w(t) + (BATCHED ? min(at_once, t.count - t.batch * at_once) * r_pad : 0); };
+    auto side_by_side = [&](const Tile& t) { return SIDE > 0 && (SHRINK || (JOINED ? joined_side : tile_w(t) <= SIDE)); };
+    // bytes between the parts of a tile's W (and A) in a stage
+    auto w_part = [&](const Tile& t) { return side_by_side(t) ? tile_n(t) * 128 : S::W_PART; };
+    // Tensor memory: fp32 tiles of one unit have their large and small accumulators in one of two buffers; with MANY two of the former
+    // for units, two of the latter for tiles.
+    auto large_at = [&](int b) { return (uint32_t)(PARTS == 3 && !MANY ? S::BUFFER * b : BN * b); };
+    auto small_at = [&](int b, int worked, bool side, int nt) { return side ? large_at(b) + (uint32_t)nt : !MANY ? large_at(b) + BN : (uint32_t)(2 * BN + (worked & 1) * BN); };
     auto rank_steps = [&](int count) { return BATCHED ? 0 : (count * r_pad + RANKS - 1) / RANKS; };
 
     if (tid == 0) {
@@ -718,6 +734,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                 ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
                 if (!ok) break;
                 const uint32_t x_to = mine + (uint32_t)(s * S::STAGE), w_to = x_to + S::X_STAGE + (JOINED ? 128 * tile_w(tile) : 0);
+                const int between = PARTS == 3 ? w_part(tile) : 0;
                 if (st < chunks) {
                     if constexpr (BATCHED) {
                         const int64_t plane = (int64_t)r_pad * p.bank.k_pad;
@@ -725,7 +742,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                         for (int it = 0; it < W_ITS; ++it) {
                             if (!a_at[it]) continue;
 #pragma unroll
-                            for (int q = 0; q < PARTS; ++q) copy(w_to + q * S::W_PART + it * (RSTEP * 128), a_at[it] + q * plane);
+                            for (int q = 0; q < PARTS; ++q) copy(w_to + q * between + it * (RSTEP * 128), a_at[it] + q * plane);
                             a_at[it] += PJ_KC;
                         }
                     }
@@ -748,12 +765,12 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
 #pragma unroll
                     for (int it = 0; it < W_ITS; ++it) {
                         const int in_tile = rb + RSTEP * it, col = tile.part * BN + in_tile;
-                        if (BN < RSTEP && in_tile >= BN) continue;
+                        if (in_tile >= (PARTS == 3 ? tile_n(tile) : BN)) continue;      // (behind them lies the next part)
                         const bool real = slot >= 0 && col < p.n;
                         const uint16_t* const from = p.bank.b + (real ? (int64_t)slot * B_PLANES * plane + (int64_t)col * r_pad + r : 0);
                         if constexpr (PARTS == 3) {
 #pragma unroll
-                            for (int k = 0; k < B_PLANES; ++k) copy_some(w_to + k * S::W_PART + it * (RSTEP * 128), from + (real ? k * plane : 0), real ? 16 : 0);
+                            for (int k = 0; k < B_PLANES; ++k) copy_some(w_to + k * between + it * (RSTEP * 128), from + (real ? k * plane : 0), real ? 16 : 0);
                         } else if (c_plane < B_PLANES) {
                             copy_some(w_to + it * (RSTEP * 128), from + (real ? c_plane * plane : 0), real ? 16 : 0);
                         }
@@ -913,7 +930,8 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
             float sum[CARRY][16];              // fp32: of the units before the last
             for (int u = 0; u < units && ok; ++u, ++sg) {
                 const int b = sg & 1;
-                const uint32_t large = lanes + (uint32_t)(b * BN), small = lanes + (uint32_t)(2 * BN + (worked & 1) * BN);
+                const bool side = side_by_side(tile);
+                const uint32_t large = lanes + large_at(b), small = lanes + small_at(b, worked, side, nt);
                 ok = __all_sync(FULL, mbar_wait_bounded(&acc_full[b], (sg >> 1) & 1, PJ_SPIN_LIMIT));
                 if (!ok) break;
                 tc_fence_after();
@@ -954,6 +972,12 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                             // (an infinite entry has no parts: its small products may be NaN)
 #pragma unroll
                             for (int e = 0; e < 16; ++e) if (fabsf(y[e]) < INFINITY) y[e] += __uint_as_float(x[e]);
+                            if (SIDE > 0 && side) {
+                                tc_load16(x, small + (uint32_t)(nt + at));
+                                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) if (fabsf(y[e]) < INFINITY) y[e] += __uint_as_float(x[e]);
+                            }
                         }
                         finish(y, at);
                     }
@@ -974,8 +998,10 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
         bool ok = true;
         for (Tile tile = first_tile(); tile.lt < my_tiles && ok; tile = after(tile)) {
             const int count = __shfl_sync(FULL, tile.count, 0), nt = __shfl_sync(FULL, tile_n(tile), 0), steps = chunks + rank_steps(count);
-            const uint32_t idesc = pj_idesc(TYPE, nt), idesc_t = pj_idesc(RIPPLE_TYPE_BF16, nt), small = __shfl_sync(FULL, tmem + (uint32_t)(2 * BN + (worked & 1) * BN), 0);
-            uint32_t acc = 0;
+            const bool side = __shfl_sync(FULL, side_by_side(tile), 0);
+            const uint32_t idesc2 = pj_idesc(TYPE, 2 * nt), idesc3 = pj_idesc(TYPE, 3 * nt);
+            const uint32_t idesc = pj_idesc(TYPE, nt), idesc_t = pj_idesc(RIPPLE_TYPE_BF16, nt);
+            uint32_t acc = 0, small = 0;
             int left = p.k, left_t = count * r_pad, b = 0;
             for (int st = 0; st < steps; ++st) {
                 const bool first = PARTS == 3 ? st < chunks && st % PJ_UNIT == 0 : st == 0;
@@ -987,7 +1013,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                     if (before > 0) ok = __all_sync(FULL, mbar_wait_bounded(&acc_empty[b], (before - 1) & 1, PJ_SPIN_LIMIT));
                     if (!ok) break;
                     tc_fence_after();
-                    acc = __shfl_sync(FULL, tmem + (uint32_t)(b * BN), 0);
+                    acc = __shfl_sync(FULL, tmem + large_at(b), 0), small = __shfl_sync(FULL, tmem + small_at(b, worked, side, nt), 0);
                 }
                 ok = __all_sync(FULL, mbar_wait_bounded(&full[s], ph, PJ_SPIN_LIMIT));
                 if (!ok) break;
@@ -1005,6 +1031,12 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                         for (int j = 0; j < PJ_KC / 16; ++j) {        // 16 entries = 32 bytes per instruction
                             if (16 * j < here) {
                                 const uint64_t x1 = x + 2 * j, w1 = w + 2 * j;
+                                if (SIDE > 0 && side) {
+                                    tc_mma_bf16(acc, x1, w1, idesc3, (st | j) != 0);
+                                    tc_mma_bf16(small, x1 + XP, w1, idesc2, 1u);
+                                    tc_mma_bf16(small, x1 + 2 * XP, w1, kind, 1u);
+                                    continue;
+                                }
                                 tc_mma_bf16(acc, x1, w1, kind, !first || j != 0);
                                 if constexpr (PARTS == 3) {
                                     tc_mma_bf16(small, x1, w1 + WP, kind, (st | j) != 0);
@@ -1051,6 +1083,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
         for (Tile tile = first_tile(); tile.lt < my_tiles && ok; tile = after(tile)) {
             const int steps = chunks + rank_steps(tile.count), c0 = tile.part * W_COLS, bytes = tile_w(tile) * 128;
             // (a tile's columns may lie in two groups of the layout, and one behind the other in shared memory)
+            const int between = w_part(tile);
             const int skip = c0 % PJ_COLS * 128, bytes1 = min(bytes, PJ_CHUNK - skip), bytes2 = bytes - bytes1;
             const uint8_t* from = p.layout + (int64_t)(c0 / PJ_COLS) * chunks * PARTS * PJ_CHUNK;
             for (int st = 0; st < steps; ++st, ++g, from += PARTS * PJ_CHUNK) {
@@ -1059,7 +1092,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                 if (st < chunks) {
                     mbar_expect(&full[s], PARTS * bytes);
                     for (int part = 0; part < PARTS; ++part) {
-                        uint8_t* const to = ring + s * S::STAGE + S::X_STAGE + part * S::W_PART;
+                        uint8_t* const to = ring + s * S::STAGE + S::X_STAGE + part * between;
                         tc_copy_bulk(to, from + part * PJ_CHUNK + skip, bytes1, &full[s]);
                         if (bytes2 > 0) tc_copy_bulk(to + bytes1, from + ((int64_t)chunks * PARTS + part) * PJ_CHUNK, bytes2, &full[s]);
                     }
@@ -1085,31 +1118,38 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
 }
 
 // y = act(x W + bias + t B), x W and t from memory: a lane is a column and keeps its row of B (RB x 16 ranks) in registers while the
-// rows are those of one adapter; FR_ROWS rows one after the other, four requested at once.
+// rows are those of one adapter; FR_ROWS rows one after the other, four at once on their way, t whether or not it is wanted.
 // Bound by the bytes of x W, t and y.
 constexpr int FR_COLS = 64, FR_ROWS = 16;
 template <typename T, int RB>
 __global__ void __launch_bounds__(256) k_finish_rows(const __grid_constant__ ProjectParams p) {
     pdl_enter();
+    constexpr int AT_ONCE = RB == 1 ? 4 : RB == 2 ? 2 : 1;
     const int col = threadIdx.x % FR_COLS, i0 = (blockIdx.x * (256 / FR_COLS) + threadIdx.x / FR_COLS) * FR_ROWS, rp = p.bank.r_pad, ld = pj_up(p.n, 16);
-    if (col >= p.n) return;
+    if (col >= p.n || i0 >= p.rows) return;
     const float bias = p.bias ? p.bias[col] : 0.f;
+    const int end = min(i0 + FR_ROWS, p.rows);
     float4 b[RB][4];
     int have = -1, rank = 0;
-    for (int i = i0; i < min(i0 + FR_ROWS, p.rows); i += 4) {
-        int slot[4];
-        bool live[4];
-        float x[4];
+    for (int i = i0; i < end; i += AT_ONCE) {
+        int slot[AT_ONCE], id[AT_ONCE];
+        float x[AT_ONCE];
+        float4 t[AT_ONCE][RB][4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < AT_ONCE; ++q) {
             const int at = min(i + q, p.rows - 1);
-            live[q] = i + q < p.rows && row_of(p, at) >= 0;
+            id[q] = p.ids ? p.ids[at] : 0;
             slot[q] = p.slots[at];
             x[q] = p.base[(int64_t)at * ld + col];
+            const float4* const from = reinterpret_cast<const float4*>(static_cast<const float*>(p.t) + (int64_t)at * rp);
+#pragma unroll
+            for (int k = 0; k < RB; ++k)
+#pragma unroll
+                for (int h = 0; h < 4; ++h) t[q][k][h] = __ldg(from + 4 * k + h);
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (!live[q]) continue;
+        for (int q = 0; q < AT_ONCE; ++q) {
+            if (i + q >= end || (p.ids && (id[q] < 0 || id[q] >= p.x_rows))) continue;
             const int a = slot[q] >= 0 && slot[q] < p.n_slots ? slot[q] : -1;
             if (a >= 0 && a != have) {
                 have = a;
@@ -1124,16 +1164,15 @@ __global__ void __launch_bounds__(256) k_finish_rows(const __grid_constant__ Pro
             }
             float y = x[q] + bias;
             if (a >= 0 && rank > 0) {
-                const float4* const t = reinterpret_cast<const float4*>(static_cast<const float*>(p.t) + (int64_t)(i + q) * rp);
-                float d = 0.f;
+                float d[4] = {};
 #pragma unroll
                 for (int k = 0; k < RB; ++k)
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
-                        const float4 v = __ldg(t + 4 * k + h);
-                        d = fmaf(v.x, b[k][h].x, d), d = fmaf(v.y, b[k][h].y, d), d = fmaf(v.z, b[k][h].z, d), d = fmaf(v.w, b[k][h].w, d);
+                        const float4 v = t[q][k][h], w = b[k][h];
+                        d[0] = fmaf(v.x, w.x, d[0]), d[1] = fmaf(v.y, w.y, d[1]), d[2] = fmaf(v.z, w.z, d[2]), d[3] = fmaf(v.w, w.w, d[3]);
                     }
-                y += d;
+                y += (d[0] + d[1]) + (d[2] + d[3]);
             }
             if (p.act == RIPPLE_ACT_RELU && y < 0.f) y = 0.f;
             static_cast<T*>(p.y)[(int64_t)(i + q) * p.ld_y + col] = from_f32<T>(y);
