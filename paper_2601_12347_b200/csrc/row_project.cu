@@ -1117,72 +1117,65 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM) : "memory");
 }
 
-// y = act(x W + bias + t B), x W and t from memory: a lane is a column and keeps its row of B (RB x 16 ranks) in registers while the
-// rows are those of one adapter; FR_ROWS rows one after the other, four at once on their way, t whether or not it is wanted.
+// y = act(x W + bias + t B), x W and t from memory: a thread is a column and takes 16 rows one after the other, keeping its row of B
+// (RB x 16 ranks) in registers while they are those of one adapter.  A block's t, slots and sums are all requested at once.
 // Bound by the bytes of x W, t and y.
-constexpr int FR_COLS = 64, FR_ROWS = 16;
+constexpr int FR_COLS = 64, FR_ROWS = 16, FR_BLOCK = 256 / FR_COLS * FR_ROWS;
 template <typename T, int RB>
 __global__ void __launch_bounds__(256) k_finish_rows(const __grid_constant__ ProjectParams p) {
     pdl_enter();
-    constexpr int AT_ONCE = RB == 1 ? 4 : RB == 2 ? 2 : 1;
-    const int col = threadIdx.x % FR_COLS, i0 = (blockIdx.x * (256 / FR_COLS) + threadIdx.x / FR_COLS) * FR_ROWS, rp = p.bank.r_pad, ld = pj_up(p.n, 16);
-    if (col >= p.n || i0 >= p.rows) return;
-    const float bias = p.bias ? p.bias[col] : 0.f;
-    const int end = min(i0 + FR_ROWS, p.rows);
+    __shared__ float4 ts[FR_BLOCK][RB * 4];
+    __shared__ int slots[FR_BLOCK];           // -1: no adapter, -2: a padding row
+    const int col = threadIdx.x % FR_COLS, first = blockIdx.x * FR_BLOCK, r0 = threadIdx.x / FR_COLS * FR_ROWS, rp = p.bank.r_pad, ld = pj_up(p.n, 16);
+    float x[FR_ROWS];
+#pragma unroll
+    for (int q = 0; q < FR_ROWS; ++q) x[q] = col < p.n ? p.base[(int64_t)min(first + r0 + q, p.rows - 1) * ld + col] : 0.f;
+#pragma unroll
+    for (int k = 0; k < RB; ++k) {
+        const int e = k * 256 + threadIdx.x, r = e / (RB * 4);
+        ts[r][e % (RB * 4)] = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p.t) + (int64_t)min(first + r, p.rows - 1) * rp) + e % (RB * 4));
+    }
+    if (threadIdx.x < FR_BLOCK) {
+        const int i = first + threadIdx.x, a = i < p.rows ? p.slots[i] : -1;
+        const bool live = i < p.rows && row_of(p, i) >= 0;
+        slots[threadIdx.x] = !live ? -2 : a >= 0 && a < p.n_slots && p.bank.info[a].rank > 0 ? a : -1;
+    }
+    const float bias = p.bias && col < p.n ? p.bias[col] : 0.f;
+    __syncthreads();
+    if (col >= p.n) return;
     float4 b[RB][4];
-    int have = -1, rank = 0;
-    for (int i = i0; i < end; i += AT_ONCE) {
-        int slot[AT_ONCE], id[AT_ONCE];
-        float x[AT_ONCE];
-        float4 t[AT_ONCE][RB][4];
+    int have = -1;
 #pragma unroll
-        for (int q = 0; q < AT_ONCE; ++q) {
-            const int at = min(i + q, p.rows - 1);
-            id[q] = p.ids ? p.ids[at] : 0;
-            slot[q] = p.slots[at];
-            x[q] = p.base[(int64_t)at * ld + col];
-            const float4* const from = reinterpret_cast<const float4*>(static_cast<const float*>(p.t) + (int64_t)at * rp);
-#pragma unroll
-            for (int k = 0; k < RB; ++k)
-#pragma unroll
-                for (int h = 0; h < 4; ++h) t[q][k][h] = __ldg(from + 4 * k + h);
-        }
-#pragma unroll
-        for (int q = 0; q < AT_ONCE; ++q) {
-            if (i + q >= end || (p.ids && (id[q] < 0 || id[q] >= p.x_rows))) continue;
-            const int a = slot[q] >= 0 && slot[q] < p.n_slots ? slot[q] : -1;
-            if (a >= 0 && a != have) {
+    for (int q = 0; q < FR_ROWS; ++q) {
+        const int a = slots[r0 + q];
+        if (a == -2) continue;
+        float y = x[q] + bias;
+        if (a >= 0) {
+            if (a != have) {
                 have = a;
-                rank = p.bank.info[a].rank;
                 const float4* const from = reinterpret_cast<const float4*>(p.bank.b32 + ((int64_t)a * p.n + col) * rp);
-                if (rank > 0) {
-#pragma unroll
-                    for (int k = 0; k < RB; ++k)
-#pragma unroll
-                        for (int h = 0; h < 4; ++h) b[k][h] = __ldg(from + 4 * k + h);
-                }
-            }
-            float y = x[q] + bias;
-            if (a >= 0 && rank > 0) {
-                float d[4] = {};
 #pragma unroll
                 for (int k = 0; k < RB; ++k)
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        const float4 v = t[q][k][h], w = b[k][h];
-                        d[0] = fmaf(v.x, w.x, d[0]), d[1] = fmaf(v.y, w.y, d[1]), d[2] = fmaf(v.z, w.z, d[2]), d[3] = fmaf(v.w, w.w, d[3]);
-                    }
-                y += (d[0] + d[1]) + (d[2] + d[3]);
+                    for (int h = 0; h < 4; ++h) b[k][h] = __ldg(from + 4 * k + h);
             }
-            if (p.act == RIPPLE_ACT_RELU && y < 0.f) y = 0.f;
-            static_cast<T*>(p.y)[(int64_t)(i + q) * p.ld_y + col] = from_f32<T>(y);
+            float d[4] = {};
+#pragma unroll
+            for (int k = 0; k < RB; ++k)
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const float4 v = ts[r0 + q][4 * k + h], w = b[k][h];
+                    d[0] = fmaf(v.x, w.x, d[0]), d[1] = fmaf(v.y, w.y, d[1]), d[2] = fmaf(v.z, w.z, d[2]), d[3] = fmaf(v.w, w.w, d[3]);
+                }
+            y += (d[0] + d[1]) + (d[2] + d[3]);
         }
+        if (p.act == RIPPLE_ACT_RELU && y < 0.f) y = 0.f;
+        static_cast<T*>(p.y)[(int64_t)(first + r0 + q) * p.ld_y + col] = from_f32<T>(y);
     }
 }
 
 static cudaError_t finish_rows(const ProjectParams& p, void* stream) {
-    const int per = 256 / FR_COLS * FR_ROWS;
-    const dim3 grid((p.rows + per - 1) / per);
+    const dim3 grid((p.rows + FR_BLOCK - 1) / FR_BLOCK);
     switch (p.bank.r_pad / 16) {
         case 1: return launch(k_finish_rows<float, 1>, grid, 256, 0, stream, p);
         case 2: return launch(k_finish_rows<float, 2>, grid, 256, 0, stream, p);
