@@ -564,21 +564,33 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
     // A tile: 128 rows, a tile of columns, and (SHRINK, JOINED) a batch of adapters: SHRINK takes every `across`-th batch that the
     // adapters of the rows fill, JOINED all of them (one where there are none).  The next row tile's count of adapters is asked for early.
     struct Tile { int lt, rows, part, batch, count, count_next; };
-    auto row_tile = [&](int lt) { return (int)((blockIdx.x + (int64_t)lt * gridDim.x) / across); };
-    auto part_of = [&](int lt) { return (int)((blockIdx.x + (int64_t)lt * gridDim.x) % across); };
-    auto adapters = [&](int lt) { return p.plan && lt < my_tiles ? p.plan[row_tile(lt)].count : 0; };
+    // (Positions are stepped from tile to tile: two 64-bit divisions per tile and warp were 3000 cycles.)
+    const int rows_on = gridDim.x / across, parts_on = gridDim.x % across;
+    auto on = [&](int& rows, int& part) {
+        rows += rows_on, part += parts_on;
+        if (part >= across) part -= across, ++rows;
+    };
+    auto adapters = [&](int lt, int rows) { return p.plan && lt < my_tiles ? p.plan[rows].count : 0; };
     auto after = [&](const Tile& t) {
         Tile n = t;
         if constexpr (BATCHED) n.batch += SHRINK ? across : 1;
         while (!BATCHED || n.batch * at_once >= n.count) {
             if (++n.lt >= my_tiles) break;
-            n.rows = row_tile(n.lt), n.part = part_of(n.lt), n.batch = SHRINK ? n.part : 0, n.count = n.count_next;
-            n.count_next = adapters(n.lt + 1);
+            on(n.rows, n.part);
+            n.batch = SHRINK ? n.part : 0, n.count = n.count_next;
+            int rows = n.rows, part = n.part;
+            on(rows, part);
+            n.count_next = adapters(n.lt + 1, rows);
             if (!SHRINK) break;
         }
         return n;
     };
-    auto first_tile = [&]() { return after(Tile{-1, 0, 0, 0, 0, adapters(0)}); };
+    auto first_tile = [&]() {
+        const int rows = blockIdx.x / across, part = blockIdx.x % across;
+        Tile before{-1, rows - rows_on, part - parts_on, 0, 0, adapters(0, rows)};
+        if (before.part < 0) before.part += across, --before.rows;
+        return after(before);
+    };
     // columns that are multiplied: of W, and ranks of the batch behind them
     auto tile_w = [&](const Tile& t) { return SHRINK ? 0 : min(W_COLS, (p.n - t.part * W_COLS + 15) & ~15); };
     auto tile_n = [&](const Tile& t) { return tile_w(t) + (BATCHED ? min(at_once, t.count - t.batch * at_once) * r_pad : 0); };
@@ -622,44 +634,53 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
         // their results are dropped); of the rows of A; the rows' places among the adapters, a byte each; and all of it for the next tile.
         const T* const x0 = static_cast<const T*>(p.x) + c * 8;
         const T* at[ITS];
-        const uint16_t* a_at[BATCHED ? W_ITS : 1];
-        int next[ITS], slot_next[BATCHED ? W_ITS : 1], slot0 = -1;
-        uint32_t which = 0, which_next = 0;
+        const uint16_t* a_at[BATCHED ? W_ITS : 1] = {};
+        // (aim() only asks for what the next tile's addresses come from; turn(), a tile later, looks at it: what is looked at right away
+        // is waited for, 4500 cycles at the start of every tile)
+        int id_next[ITS], row_next[BATCHED ? 1 : ITS], slot_next[BATCHED ? W_ITS : 1], slot0 = -1;
+        uint32_t which = 0;
+        int place[BATCHED ? W_ITS : 1], a_row[BATCHED ? W_ITS : 1];      // rows of A that this thread fetches: adapter within the batch, offset
+        if (BATCHED && r_pad) {
+#pragma unroll
+            for (int it = 0; it < W_ITS; ++it) place[it] = (rb + RSTEP * it) / r_pad, a_row[it] = (rb + RSTEP * it) % r_pad * p.bank.k_pad + c * 8;
+        }
+        const int first_place = !BATCHED && r_pad ? c_rank / r_pad : 0;
         auto aim = [&](const Tile& t) {
             if (t.lt >= my_tiles) return;
             const int r0 = t.rows * PJ_ROWS + rb;
 #pragma unroll
             for (int it = 0; it < ITS; ++it) {
-                const int i = r0 + RSTEP * it;
-                next[it] = i < p.rows ? max((int)row_of(p, i), 0) : 0;
+                const int i = min(r0 + RSTEP * it, p.rows - 1);
+                id_next[it] = p.ids ? p.ids[i] : i;
             }
             if (!p.plan) return;
             const TilePlan& plan = p.plan[t.rows];
             if constexpr (BATCHED) {                // slots of the rows of A that this thread fetches
 #pragma unroll
-                for (int it = 0; it < W_ITS; ++it) {
-                    const int n = rb + RSTEP * it, j = t.batch * at_once + n / r_pad;
-                    slot_next[it] = n < at_once * r_pad && j < t.count ? plan.slot[j] : -1;
-                }
-            } else if (t.count) {
-                which_next = 0;
+                for (int it = 0; it < W_ITS; ++it) slot_next[it] = plan.slot[min(t.batch * at_once + place[it], PJ_ROWS - 1)];
+            } else {
 #pragma unroll
-                for (int it = 0; it < ITS; ++it) which_next |= (uint32_t)plan.row[rb + RSTEP * it] << (8 * it);
-                const int j = c_rank / r_pad;
-                slot_next[0] = j < t.count ? plan.slot[j] : -1;
+                for (int it = 0; it < ITS; ++it) row_next[it] = plan.row[rb + RSTEP * it];
+                slot_next[0] = plan.slot[min(first_place, PJ_ROWS - 1)];
             }
         };
-        auto turn = [&]() {                         // to the next tile
+        auto row_next_at = [&](int it) { return x0 + (id_next[it] >= 0 && id_next[it] < p.x_rows ? id_next[it] : 0) * p.ld_x; };
+        auto turn = [&](const Tile& t) {            // to the tile that was aimed at
 #pragma unroll
-            for (int it = 0; it < ITS; ++it) at[it] = x0 + next[it] * p.ld_x;
-            which = which_next;
+            for (int it = 0; it < ITS; ++it) at[it] = row_next_at(it);
+            if (!p.plan) return;
             if constexpr (BATCHED) {
                 const int64_t plane = (int64_t)r_pad * p.bank.k_pad;
 #pragma unroll
-                for (int it = 0; it < W_ITS; ++it)
-                    a_at[it] = !p.plan || slot_next[it] < 0 ? nullptr : p.bank.a + (int64_t)slot_next[it] * PARTS * plane + (int64_t)((rb + RSTEP * it) % r_pad) * p.bank.k_pad + c * 8;
+                for (int it = 0; it < W_ITS; ++it) {
+                    const bool real = place[it] < at_once && t.batch * at_once + place[it] < t.count;
+                    a_at[it] = !real ? nullptr : p.bank.a + (int64_t)slot_next[it] * PARTS * plane + a_row[it];
+                }
             } else {
-                slot0 = slot_next[0];
+                which = 0;
+#pragma unroll
+                for (int it = 0; it < ITS; ++it) which |= (uint32_t)row_next[it] << (8 * it);
+                slot0 = first_place < t.count ? slot_next[0] : -1;
             }
         };
         constexpr int WORDS = sizeof(T) / 2;        // 16-byte words of eight entries
@@ -724,7 +745,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
         Tile tile = first_tile();
         aim(tile);
         while (tile.lt < my_tiles && ok) {
-            if (!fetched || !regs) turn();
+            if (!fetched || !regs) turn(tile);
             if (regs && !fetched) fetch(chunks == 1);
             fetched = true;
             const Tile following = after(tile);
@@ -799,10 +820,19 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                         if (lane == 0) mbar_arrive(&full[s]);
                     }
                 }
+                if (PARTS == 3 && st == min(1, steps - 1) && p.ids && following.lt < my_tiles) {
+                    // the next tile's rows, on their way to L2 a tile ahead: gathered rows come from far (project-cached-rows 136 -> 128 us; rows in
+                    // order, and 16-bit rows, whose copies run further ahead, lose by it)
+#pragma unroll
+                    for (int it = 0; it < ITS; ++it) {
+                        const uint8_t* const line = reinterpret_cast<const uint8_t*>(row_next_at(it) - c * 8);
+                        for (int at = c * 128; at < p.k * (int)sizeof(T); at += 1024) asm volatile("prefetch.global.L2 [%0];" ::"l"(line + at));
+                    }
+                }
                 if (regs) {                         // what the next step keeps is requested now: of this tile, or of the one after it
                     if (st + 1 < chunks) fetch(st + 2 == chunks);
                     else if (st + 1 < steps) fetch_t(tile, st + 1 - chunks);
-                    else if (following.lt < my_tiles) turn(), fetch(chunks == 1);
+                    else if (following.lt < my_tiles) turn(following), fetch(chunks == 1);
                 }
                 if (++s == STAGES) { s = 0; ph ^= 1; }
             }
