@@ -748,9 +748,8 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
             if (!fetched || !regs) turn(tile);
             if (regs && !fetched) fetch(chunks == 1);
             fetched = true;
-            const Tile following = after(tile);
             const int steps = chunks + rank_steps(tile.count);
-            aim(following);
+            Tile following = tile;
             for (int st = 0; st < steps; ++st) {
                 ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
                 if (!ok) break;
@@ -819,6 +818,10 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&full[s]);
                     }
+                }
+                if (st == 0) {                      // (between two steps and not before the first: the stages ahead hide it)
+                    following = after(tile);
+                    aim(following);
                 }
                 if (PARTS == 3 && st == min(1, steps - 1) && p.ids && following.lt < my_tiles) {
                     // the next tile's rows, on their way to L2 a tile ahead: gathered rows come from far (project-cached-rows 136 -> 128 us; rows in
