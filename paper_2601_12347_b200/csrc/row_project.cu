@@ -1256,12 +1256,13 @@ static cudaError_t project(ProjectParams p, void* stream) {
             if (p.rows <= 4 * sm_count()) e = launch(k_shrink_few<TYPE, 1>, dim3(planned + p.rows), 128, 0, stream, p, planned);
             else e = launch(k_shrink_few<TYPE, 4>, dim3(planned + (p.rows + 3) / 4), 128, 0, stream, p, planned);
         } else {
-            const int at_once = PJ_T_COLS / p.bank.r_pad;
+            constexpr int T_COLS = F32 ? PJ_T_COLS : 2 * PJ_T_COLS;
+            const int at_once = T_COLS / p.bank.r_pad;
             // batches of adapters side by side while there are SMs for them, one behind the other beyond
             const int batches = (std::min(p.n_slots, PJ_ROWS) + at_once - 1) / at_once;
             p.batches = std::max(1, std::min(batches, sm_count() / row_tiles));
             e = launch(k_plan_tiles, dim3(row_tiles), 128, 0, stream, p);
-            if (e == cudaSuccess) e = project_tiles<TYPE, PJ_T_COLS, PJ_SHRINK>(p, stream);
+            if (e == cudaSuccess) e = project_tiles<TYPE, T_COLS, PJ_SHRINK>(p, stream);
         }
         if (e != cudaSuccess) return e;
     }
