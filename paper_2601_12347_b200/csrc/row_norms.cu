@@ -373,6 +373,8 @@ template <typename T, typename TR, int V, bool RING>
 static cudaError_t launch_norm(const NormParams& p, void* stream) {
     const int D = p.width;
     if (D <= 256) return launch_norm<T, TR, V, 8, false, RING>(p, 1, stream);
+    if (D <= 512) return launch_norm<T, TR, V, 16, false, RING>(p, 1, stream);
+    if (D <= 768) return launch_norm<T, TR, V, 24, false, RING>(p, 1, stream);
     if (D <= 1024) return launch_norm<T, TR, V, 32, false, RING>(p, 1, stream);
     if (D <= 4096) return launch_norm<T, TR, V, 16, true, RING>(p, (D + 511) / 512, stream);
     return launch_norm<T, TR, V, 32, true, RING>(p, (D + 1023) / 1024, stream);

@@ -464,8 +464,8 @@ __device__ int g_request_timeout;
 
 constexpr int PJ_ROWS = 128;             // rows per tile: the lanes of the accumulator
 constexpr int PJ_EPI_WARPS = 8;          // two per quarter of the lanes
-constexpr int PJ_FEW = 1024;             // rows up to which t is computed a block per row
-constexpr int64_t PJ_FEW_PRODUCTS = 64 << 20;   // rows x K x n up to which y is summed without tensor cores
+constexpr int PJ_FEW = 3000;             // rows up to which t is computed by k_shrink_few
+constexpr int PF_MOST = 160, PF_MOST_F32 = 320;   // blocks up to which y is computed by k_project_few
 constexpr int PJ_T_COLS = 64;            // ranks of adapters side by side, where t is computed on the tensor cores
 constexpr int PJ_UNIT = 4;               // fp32: chunks (256 entries of K) whose large products share an accumulator
 constexpr uint32_t PJ_SPIN_LIMIT = 1u << 22;
@@ -1235,11 +1235,13 @@ static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
     return project_tiles<TYPE, BN, MODE, false>(p, stream);
 }
 
+static int64_t few_blocks(int64_t rows, int n) { return (rows + PF_ROWS - 1) / PF_ROWS * ((n + PF_COLS - 1) / PF_COLS); }
+
 template <int TYPE>
 static cudaError_t project(ProjectParams p, void* stream) {
     constexpr bool F32 = TYPE == RIPPLE_TYPE_F32;
     const int row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
-    const bool few = (int64_t)p.rows * p.k * p.n <= PJ_FEW_PRODUCTS && p.rows <= PJ_FEW;
+    const bool few = few_blocks(p.rows, p.n) <= (F32 ? PF_MOST_F32 : PF_MOST);
     cudaError_t e = cudaSuccess;
     if (p.bank.info) {
         // fp32, narrow: x W and t in one pass over the rows, whose parts are what takes the time
@@ -1250,7 +1252,7 @@ static cudaError_t project(ProjectParams p, void* stream) {
                 return e == cudaSuccess ? finish_rows(p, stream) : e;
             }
         }
-        if (p.rows <= PJ_FEW) {
+        if (few || p.rows <= PJ_FEW) {
             const int planned = few ? 0 : row_tiles;
             // (four rows per block once there are several blocks for every SM)
             if (p.rows <= 4 * sm_count()) e = launch(k_shrink_few<TYPE, 1>, dim3(planned + p.rows), 128, 0, stream, p, planned);
@@ -1365,7 +1367,7 @@ extern "C" ripple_status ripple_adapter_set(void* bank, int32_t type, int32_t k,
 }
 
 static bool pj_joined(const ripple_project_rows_args* a) {
-    return a->bank && a->type == RIPPLE_TYPE_F32 && a->rows > PJ_FEW && a->n <= 128 - PJ_T_COLS;
+    return a->bank && a->type == RIPPLE_TYPE_F32 && a->rows > PJ_FEW && few_blocks(a->rows, a->n) > PF_MOST_F32 && a->n <= 128 - PJ_T_COLS;
 }
 
 extern "C" int64_t ripple_project_workspace_bytes(const ripple_project_rows_args* a) {
