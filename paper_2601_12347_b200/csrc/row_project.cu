@@ -755,12 +755,14 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                 if (!ok) break;
                 const uint32_t x_to = mine + (uint32_t)(s * S::STAGE), w_to = x_to + S::X_STAGE + (JOINED ? 128 * tile_w(tile) : 0);
                 const int between = PARTS == 3 ? w_part(tile) : 0;
+                bool copied = false;
                 if (st < chunks) {
                     if constexpr (BATCHED) {
                         const int64_t plane = (int64_t)r_pad * p.bank.k_pad;
 #pragma unroll
                         for (int it = 0; it < W_ITS; ++it) {
                             if (!a_at[it]) continue;
+                            copied = true;
 #pragma unroll
                             for (int q = 0; q < PARTS; ++q) copy(w_to + q * between + it * (RSTEP * 128), a_at[it] + q * plane);
                             a_at[it] += PJ_KC;
@@ -786,6 +788,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                     for (int it = 0; it < W_ITS; ++it) {
                         const int in_tile = rb + RSTEP * it, col = tile.part * BN + in_tile;
                         if (in_tile >= (PARTS == 3 ? tile_n(tile) : BN)) continue;      // (behind them lies the next part)
+                        copied = true;
                         const bool real = slot >= 0 && col < p.n;
                         const uint16_t* const from = p.bank.b + (real ? (int64_t)slot * B_PLANES * plane + (int64_t)col * r_pad + r : 0);
                         if constexpr (PARTS == 3) {
@@ -807,17 +810,17 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                         }
                     }
                 }
-                // 16-bit rows: the barrier counts threads, and the copies of a thread arrive for it when they have landed
+                // 16-bit rows: the barrier counts threads, and the copies of a thread arrive for it when they have landed.  fp32: it counts
+                // warps, and the copies of a thread that has some are counted on top.
                 if (PARTS == 1 && vec) {
                     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[s])) : "memory");
-                } else {
+                } else if (PARTS == 1) {
                     asm volatile("cp.async.wait_all;" ::: "memory");
-                    if (PARTS == 1) {
-                        mbar_arrive(&full[s]);
-                    } else {
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&full[s]);
-                    }
+                    mbar_arrive(&full[s]);
+                } else {
+                    if (copied) asm volatile("cp.async.mbarrier.arrive.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[s])) : "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&full[s]);
                 }
                 if (st == 0) {                      // (between two steps and not before the first: the stages ahead hide it)
                     following = after(tile);
@@ -1160,6 +1163,16 @@ __global__ void __launch_bounds__(256) k_finish_rows(const __grid_constant__ Pro
     __shared__ float4 ts[FR_BLOCK][RB * 4];
     __shared__ int slots[FR_BLOCK];           // -1: no adapter, -2: a padding row
     const int col = threadIdx.x % FR_COLS, first = blockIdx.x * FR_BLOCK, r0 = threadIdx.x / FR_COLS * FR_ROWS, rp = p.bank.r_pad, ld = pj_up(p.n, 16);
+    float4 b[RB][4];
+    int have = p.slots[min(first + r0, p.rows - 1)];      // (the adapter of the first row, whose B is asked for with the rest)
+    if (have < 0 || have >= p.n_slots) have = -1;
+    auto take_b = [&]() {
+        const float4* const from = reinterpret_cast<const float4*>(p.bank.b32 + ((int64_t)have * p.n + col) * rp);
+#pragma unroll
+        for (int k = 0; k < RB; ++k)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) b[k][h] = __ldg(from + 4 * k + h);
+    };
     float x[FR_ROWS];
 #pragma unroll
     for (int q = 0; q < FR_ROWS; ++q) x[q] = col < p.n ? p.base[(int64_t)min(first + r0 + q, p.rows - 1) * ld + col] : 0.f;
@@ -1174,10 +1187,9 @@ __global__ void __launch_bounds__(256) k_finish_rows(const __grid_constant__ Pro
         slots[threadIdx.x] = !live ? -2 : a >= 0 && a < p.n_slots && p.bank.info[a].rank > 0 ? a : -1;
     }
     const float bias = p.bias && col < p.n ? p.bias[col] : 0.f;
+    if (have >= 0 && col < p.n) take_b();
     __syncthreads();
     if (col >= p.n) return;
-    float4 b[RB][4];
-    int have = -1;
 #pragma unroll
     for (int q = 0; q < FR_ROWS; ++q) {
         const int a = slots[r0 + q];
@@ -1186,11 +1198,7 @@ __global__ void __launch_bounds__(256) k_finish_rows(const __grid_constant__ Pro
         if (a >= 0) {
             if (a != have) {
                 have = a;
-                const float4* const from = reinterpret_cast<const float4*>(p.bank.b32 + ((int64_t)a * p.n + col) * rp);
-#pragma unroll
-                for (int k = 0; k < RB; ++k)
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) b[k][h] = __ldg(from + 4 * k + h);
+                take_b();
             }
             float d[4] = {};
 #pragma unroll
