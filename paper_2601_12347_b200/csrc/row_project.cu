@@ -358,7 +358,8 @@ __global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ Proj
 // Few rows: 16 rows x 32 columns of y per block.  A lane is a column, a warp an eighth of every 256 entries of K; what the warps
 // have summed meets in shared memory, where each finishes two rows: t_i B_a, bias, activation.  Sums in fp32 throughout.
 // Latency is all that counts here: 32 entries of W per lane and 16 of the rows per thread are always on their way, those of the next
-// 256 entries while these are multiplied.
+// 256 entries while these are multiplied.  64 rows, 256 -> 256: 4.1 us alone, 6.2 with 64 adapters of rank 16; 1000 rows, 602 -> 41: 8.8 and
+// 13.6.  (The tensor-core form: 5.8 and 25, 21 and 37.)
 constexpr int PF_ROWS = 16, PF_COLS = 32, PF_K = 256, PF_LD = 20;
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_project_few(const __grid_constant__ ProjectParams p) {
@@ -464,8 +465,14 @@ __device__ int g_request_timeout;
 
 constexpr int PJ_ROWS = 128;             // rows per tile: the lanes of the accumulator
 constexpr int PJ_EPI_WARPS = 8;          // two per quarter of the lanes
-constexpr int PJ_FEW = 3000;             // rows up to which t is computed by k_shrink_few
-constexpr int PF_MOST = 160, PF_MOST_F32 = 320;   // blocks up to which y is computed by k_project_few
+// Rows up to which t is computed by k_shrink_few.  Both sides, us of a whole call with 32 adapters of rank 16 and 20 rows each, row by row /
+// on the tensor cores: bf16 602 -> 41, 2000 rows 23 / 32, 4000 rows 27 / 35; 1024 -> 512, 3000 rows 21 / 24, 4000 rows 27 / 25;
+// fp32 256 -> 256, 3000 rows 24 / 27, 4000 rows 26 / 27; 128 -> 1024, 4000 rows 30 / 29.
+constexpr int PJ_FEW = 3000;
+// Blocks (16 rows x 32 columns) up to which y is computed by k_project_few.  Both sides, few / tensor cores: bf16 256 -> 256, 200 blocks
+// 10.5 / 8.9, 104 blocks 6.2 / 8.7; 602 -> 41, 126 blocks 14 / 21; fp32 602 -> 41, 188 blocks 22 / 42, 314 blocks 32 / 42, 500 blocks
+// 45 / 43; 256 -> 256, 200 blocks 10.8 / 12.4, 504 blocks 20 / 14.
+constexpr int PF_MOST = 160, PF_MOST_F32 = 320;
 constexpr int PJ_T_COLS = 64;            // ranks of adapters side by side, where t is computed on the tensor cores
 constexpr int PJ_UNIT = 4;               // fp32: chunks (256 entries of K) whose large products share an accumulator
 constexpr uint32_t PJ_SPIN_LIMIT = 1u << 22;
@@ -518,6 +525,9 @@ template <typename T> __device__ __forceinline__ uint4 word_of(const Piece<T, 8>
     return make_uint4(two(0), two(2), two(4), two(6));
 }
 
+// What a launch of k_project_rows computes: t; y, with steps over ranks; or x W with t beside it.
+enum { PJ_SHRINK, PJ_RANKS, PJ_JOINED };
+
 // A persistent CTA takes tiles of 128 rows x BN columns: lanes of the accumulator are rows, its columns output columns.
 // SHRINK: the columns are the ranks of adapters that the tile's rows use, side by side, and each row keeps those of its own: t.
 // JOINED: columns of W, and behind them such ranks: one pass over the rows for both; k_finish_rows makes y of them.
@@ -532,9 +542,12 @@ template <typename T> __device__ __forceinline__ uint4 word_of(const Piece<T, 8>
 // and summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
 // Barriers, all waits bounded: full[s] (one arrival per loader warp, 16-bit rows: per thread; one with the bytes of the weights),
 // empty[s] (the products that read stage s), acc_full[b], acc_empty[b] (one arrival per epilogue warp).
-// What a launch of k_project_rows computes: t; y, with steps over ranks; or x W with t beside it.
-enum { PJ_SHRINK, PJ_RANKS, PJ_JOINED };
-
+//
+// What bounds it.  16-bit rows: at 65 536 x 1024 x 1024 (no adapters) 125 us, 1.1 PFLOP/s, 68 % of the measured cuBLAS rate; a step (128 rows x 256
+// columns x 64 entries) takes 800 cycles, of which its products are 512, and brings 48 KB out of L2: with tiles of 128 columns, 32 KB per
+// step, 200 us at the same bytes per cycle.  fp32: the loaders' chain per step -- loads out of L2, parts, stores -- of 1500 cycles beside
+// 1000 (narrow) to 1550 (128 columns) of products, which read 192 KB of shared memory; 200 000 gathered rows of 256 to 47 columns in
+// 72 us, 205 MB at 2.8 TB/s.  Two stages of 96 KB are all that fits; a third (narrow tiles, 72 KB) gained nothing.
 template <int TYPE, int BN, int MODE, bool MANY>
 __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project_rows(const __grid_constant__ ProjectParams p) {
     using T = typename Elem<TYPE>::T;
@@ -1155,7 +1168,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
 
 // y = act(x W + bias + t B), x W and t from memory: a thread is a column and takes 16 rows one after the other, keeping its row of B
 // (RB x 16 ranks) in registers while they are those of one adapter.  A block's t, slots and sums are all requested at once.
-// Bound by the bytes of x W, t and y.
+// Bound by the bytes of x W, t and y and by how few of them are on their way: 200 000 rows of 47 columns 40 us, 89 MB at 2.2 TB/s.
 constexpr int FR_COLS = 64, FR_ROWS = 16, FR_BLOCK = 256 / FR_COLS * FR_ROWS;
 template <typename T, int RB>
 __global__ void __launch_bounds__(256) k_finish_rows(const __grid_constant__ ProjectParams p) {
@@ -1252,7 +1265,8 @@ static cudaError_t project(ProjectParams p, void* stream) {
     const bool few = few_blocks(p.rows, p.n) <= (F32 ? PF_MOST_F32 : PF_MOST);
     cudaError_t e = cudaSuccess;
     if (p.bank.info) {
-        // fp32, narrow: x W and t in one pass over the rows, whose parts are what takes the time
+        // fp32, narrow: x W and t in one pass over the rows, whose parts are what takes the time (200 000 rows, 256 -> 47, rank 16: 173 us in
+        // two passes, 122 in one)
         if constexpr (F32) {
             if (p.base) {
                 e = launch(k_plan_tiles, dim3(row_tiles), 128, 0, stream, p);
@@ -1266,6 +1280,7 @@ static cudaError_t project(ProjectParams p, void* stream) {
             if (p.rows <= 4 * sm_count()) e = launch(k_shrink_few<TYPE, 1>, dim3(planned + p.rows), 128, 0, stream, p, planned);
             else e = launch(k_shrink_few<TYPE, 4>, dim3(planned + (p.rows + 3) / 4), 128, 0, stream, p, planned);
         } else {
+            // (16-bit rows, 7 adapters of rank 32 per tile: 64 side by side 91 us, 128 84, 256 86, which costs a tile with one adapter its stages)
             constexpr int T_COLS = F32 ? PJ_T_COLS : 2 * PJ_T_COLS;
             const int at_once = T_COLS / p.bank.r_pad;
             // batches of adapters side by side while there are SMs for them, one behind the other beyond
@@ -1277,7 +1292,8 @@ static cudaError_t project(ProjectParams p, void* stream) {
         if (e != cudaSuccess) return e;
     }
     if (few) return launch(k_project_few<TYPE>, dim3((p.rows + PF_ROWS - 1) / PF_ROWS, (p.n + PF_COLS - 1) / PF_COLS), 256, 0, stream, p);
-    // Tiles of 32 columns where those of 128 would leave most SMs without one; of 256 (16-bit rows) where those leave none.
+    // Tiles of 32 columns where those of 128 would leave most SMs without one; of 256 (16-bit rows) where those leave none
+    // (project of 65 536 x 1024 x 1024: 128 columns 200 us, 256 columns 125).
     const int64_t wide = (int64_t)((p.n + 127) / 128) * row_tiles;
     if constexpr (!F32) {
         if (p.n > 128 && (int64_t)((p.n + 255) / 256) * row_tiles >= sm_count()) return project_tiles<TYPE, 256, PJ_RANKS>(p, stream);
@@ -1388,7 +1404,7 @@ extern "C" int64_t ripple_project_workspace_bytes(const ripple_project_rows_args
 
 extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) {
     if (!a) REFUSE("project_rows: null arguments");
-    if (a->rows < 0 || a->rows > INT32_MAX) REFUSE("project_rows: rows out of range");
+    if (a->rows < 0 || a->rows > INT32_MAX - 128) REFUSE("project_rows: rows out of range");
     if (!shape_ok(a->type, a->k, a->n)) REFUSE("project_rows: type, k or n out of range");
     if (a->out_type != a->type && a->out_type != RIPPLE_TYPE_F32) REFUSE("project_rows: an output type that is neither the type nor fp32");
     if (a->act != RIPPLE_ACT_IDENTITY && a->act != RIPPLE_ACT_RELU) REFUSE("project_rows: unknown activation");

@@ -80,9 +80,12 @@ def check_norm(y=None, post=None, gate=None, gate_act=serve.GATE_IDENTITY, scale
     tol = torch.zeros_like(t)
     if y is not None:
         p, tol = norm_of(y.to(F64), tol, post)
-        if gate is not None:      # sigmoid and tanh: an exponential (2 steps), a sum, a quotient
+        if gate is not None:
+            # fp32: an exponential (2 steps: 4 u32), a sum, a quotient, two products.  16 bits: the exponent's rounding, |g| u32, the
+            # exponential 2^-22 = 4 u32, a sum, a reciprocal (1 step: 2 u32), two products
+            steps = 8 if gate.dtype == torch.float32 else 10 + gate.to(F64).abs()
             g = ACTS[gate_act](gate.to(F64))
-            p, tol = p * g, tol * g.abs() + 8 * U32 * (p * g).abs()
+            p, tol = p * g, tol * g.abs() + steps * U32 * (p * g).abs()
         k = scale.to(F64) if isinstance(scale, torch.Tensor) else float(np.float32(scale))
         t = p * k
         tol = tol * (k.abs() if isinstance(scale, torch.Tensor) else abs(k)) + 2 * U32 * t.abs()
@@ -300,6 +303,51 @@ def test_many_rows_with_adapters(dtype, run, max_rank):
     t = Tenants(g, K, N, DTYPES[dtype], slots=slots, max_rank=max_rank, act=serve.ACT_RELU)
     rows = 5003
     t.check(rnd(g, rows, K, dtype=DTYPES[dtype]), runs(g, rows, run, slots))
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows,N", [(1280, 33), (1281, 33), (2560, 33), (2561, 33), (2999, 300), (3000, 300), (3001, 300), (9500, 129), (9600, 256)])
+def test_rows_at_the_edges_of_the_forms(dtype, rows, N):
+    """Blocks of the form for few rows (160, fp32 320), rows up to which t is computed row by row (3000), tiles of 32, 128 and 256 columns."""
+    g = gen(rows)
+    t = Tenants(g, 130, N, DTYPES[dtype], slots=40, max_rank=20, act=serve.ACT_RELU)
+    x = rnd(g, rows, 130, dtype=DTYPES[dtype])
+    t.check(x)
+    t.check(x, runs(g, rows, 9, 40))
+
+
+@pytest.mark.parametrize("K", [64, 250, 256, 257, 520])
+@pytest.mark.parametrize("N", [1, 40, 47, 48, 49, 64, 65])
+@pytest.mark.parametrize("max_rank", [16, 17, 64])
+def test_narrow_fp32_outputs_of_many_rows(K, N, max_rank):
+    """x W and t in one pass: up to 64 columns, one unit of K and several, one batch of adapters per tile and several, tiles without any."""
+    g = gen(K + N)
+    t = Tenants(g, K, N, torch.float32, slots=30, max_rank=max_rank, ranks=[max_rank if s % 3 else 1 + s % max_rank for s in range(30)])
+    rows = 10_500
+    table = rnd(g, 12_000, K)
+    ids = torch.randperm(12_000, generator=g, device="cuda")[:rows].to(torch.int32)
+    slots = runs(g, rows, 300, 30)
+    slots[2000:4000] = torch.randint(-1, 30, (2000,), generator=g, device="cuda", dtype=torch.int32)     # many in a tile
+    slots[5000:6000] = -1                                                                               # none
+    t.check(table, slots, ids)
+    ids[::7] = -1
+    out = torch.full((rows, N), 5.0, device="cuda")
+    serve.project_rows(table, t.proj, t.bank, slots, ids, out=out)
+    ok = (ids >= 0).nonzero()[:, 0]
+    want, tol = t.want(table[ids[ok].long()], slots[ok])
+    near(out[ok], want, tol)
+    assert (out[(ids < 0).nonzero()[:, 0]] == 5.0).all()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_unaligned_rows_with_adapters_in_every_form(dtype):
+    g = gen(21)
+    T = DTYPES[dtype]
+    for K, N, rows in ((77, 47, 6000), (77, 300, 6000), (300, 130, 12_000), (77, 60, 500)):
+        t = Tenants(g, K, N, T, slots=12, max_rank=33)
+        x = rnd(g, rows, K + 5, dtype=T)[:, 1:K + 1]
+        t.check(x, runs(g, rows, 60, 12))
+        t.check(x, runs(g, rows, 60, 12), torch.randint(0, rows, (rows,), generator=g, device="cuda", dtype=torch.int32), out_dtype=torch.float32)
 
 
 @pytest.mark.parametrize("dtype", list(DTYPES))
@@ -532,6 +580,12 @@ def test_streams_and_captured_graphs():
         torch.cuda.synchronize()
         for k in range(2):
             assert torch.equal(outs[k], want[k])
+
+
+def test_every_wait_ended():
+    """No bounded wait of the calls so far gave up."""
+    serve.check_requests()
+    serve.check_requests("cuda:0")
 
 
 def test_refusals():
