@@ -544,8 +544,9 @@ enum { PJ_SHRINK, PJ_RANKS, PJ_JOINED };
 // empty[s] (the products that read stage s), acc_full[b], acc_empty[b] (one arrival per epilogue warp).
 //
 // What bounds it.  16-bit rows: at 65 536 x 1024 x 1024 (no adapters) 125 us, 1.1 PFLOP/s, 68 % of the measured cuBLAS rate; a step (128 rows x 256
-// columns x 64 entries) takes 800 cycles, of which its products are 512, and brings 48 KB out of L2: with tiles of 128 columns, 32 KB per
-// step, 200 us at the same bytes per cycle.  fp32: the loaders' chain per step -- loads out of L2, parts, stores -- of 1500 cycles beside
+// columns x 64 entries) takes 800 cycles, of which its products are 512, and brings 48 KB out of L2 (27 % of what L2 can): hand-overs
+// between the roles, and power.  Tiles of 128 columns, half the products per hand-over: 200 us.  Asking ahead for the next step's operands,
+// or for two steps' at once: 185 and 176 with adapters, against 171.  fp32: the loaders' chain per step -- loads out of L2, parts, stores -- of 1500 cycles beside
 // 1000 (narrow) to 1550 (128 columns) of products, which read 192 KB of shared memory; 200 000 gathered rows of 256 to 47 columns in
 // 72 us, 205 MB at 2.8 TB/s.  Two stages of 96 KB are all that fits; a third (narrow tiles, 72 KB) gained nothing.
 template <int TYPE, int BN, int MODE, bool MANY>

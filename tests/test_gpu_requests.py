@@ -121,7 +121,7 @@ def test_norms_of_every_width_and_type(width, dtype, res):
                scale=-0.7, residual=r.to(R), pre=vectors(g, width, serve.NORM_LAYER, True))
 
 
-@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 63, 1000])
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 63, 1000, 20_011])
 @pytest.mark.parametrize("width", [32, 602, 2048])
 def test_norms_with_parts_left_out(rows, width):
     g = gen(rows)
@@ -155,18 +155,19 @@ def test_norms_of_strided_broadcast_and_unaligned_rows():
     assert torch.equal(s, s2) and torch.equal(n, n2) and torch.equal(m[:, :D], y) and torch.equal(m[:, D:2 * D], gate)
 
 
-@pytest.mark.parametrize("width", [100, 2000])
-def test_norms_in_place(width):
+@pytest.mark.parametrize("width", [100, 600, 2000])
+@pytest.mark.parametrize("rows", [50, 30_000])
+def test_norms_in_place(width, rows):
     g = gen(2)
-    y, r, gate = rnd(g, 50, width), rnd(g, 60, width), rnd(g, 50, width)
+    y, r, gate = rnd(g, rows, width), rnd(g, rows + 10, width), rnd(g, rows, width)
     ln = vectors(g, width, serve.NORM_LAYER, True)
-    want = serve.norm_rows(y, post=ln, gate=gate, residual=r[:50], pre=ln)
+    want = serve.norm_rows(y, post=ln, gate=gate, residual=r[:rows], pre=ln)
     y2, r2 = y.clone(), r.clone()
-    got = serve.norm_rows(y2, post=ln, gate=gate, residual=r2[:50], pre=ln, out=r2[:50], normed_out=y2)
+    got = serve.norm_rows(y2, post=ln, gate=gate, residual=r2[:rows], pre=ln, out=r2[:rows], normed_out=y2)
     assert got[0].data_ptr() == r2.data_ptr() and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
-    assert torch.equal(r2[50:], r[50:])
+    assert torch.equal(r2[rows:], r[rows:])
     g2 = gate.clone()
-    got = serve.norm_rows(y, post=ln, gate=g2, residual=r[:50], pre=ln, out=g2)
+    got = serve.norm_rows(y, post=ln, gate=g2, residual=r[:rows], pre=ln, out=g2)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
@@ -182,6 +183,15 @@ def test_padding_rows_are_left_as_they_were():
         s, n = check_norm(y[ok], residual=table, ids=ids[ok].contiguous(), pre=rms)
         assert torch.equal(out[ok], s) and torch.equal(normed[ok], n)
         pad = torch.tensor([1, 3, 5, 6], device="cuda")
+        assert (out[pad] == 7.0).all() and (normed[pad] == 8.0).all()
+        # more rows than are on their way at once, a third of them padding
+        rows = 12_000
+        y, ids = rnd(g, rows, width), torch.randint(-5, 10, (rows,), generator=g, device="cuda", dtype=torch.int32)
+        out, normed, one = torch.full_like(y, 7.0), torch.full_like(y, 8.0), rnd(g, rows, 1)
+        serve.norm_rows(y, gate=one, residual=table, ids=ids, pre=rms, out=out, normed_out=normed)
+        ok, pad = (ids >= 0).nonzero()[:, 0], (ids < 0).nonzero()[:, 0]
+        s, n = check_norm(y[ok], gate=one[ok], residual=table, ids=ids[ok].contiguous(), pre=rms)
+        assert torch.equal(out[ok], s) and torch.equal(normed[ok], n)
         assert (out[pad] == 7.0).all() and (normed[pad] == 8.0).all()
 
 
