@@ -350,6 +350,38 @@ def test_narrow_fp32_outputs_of_many_rows(K, N, max_rank):
 
 
 @pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("K,N,rows", [(8192, 130, 200), (8192, 40, 3500), (16, 65536, 40), (16, 65536, 400)])
+def test_the_largest_widths(dtype, K, N, rows):
+    g = gen(K + N)
+    t = Tenants(g, K, N, DTYPES[dtype], slots=3, max_rank=64)
+    t.check(rnd(g, rows, K, dtype=DTYPES[dtype]), runs(g, rows, 30, 3))
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("N", [16, 200])
+def test_as_many_slots_as_a_bank_can_have(dtype, N):
+    """Every row another adapter of 4096: a full tile uses 128."""
+    g = gen(22)
+    K, T = 40, DTYPES[dtype]
+    p = serve.Projection(torch.zeros(K, N, dtype=T, device="cuda"))
+    bank = serve.AdapterBank(p, 4096, 2)
+    A, B = rnd(g, 4096, K, 2, dtype=T, scale=K ** -0.5), rnd(g, 4096, 2, N, dtype=T)
+    bank.set(0, A, B, 1.0)
+    for rows in (300, 9000):
+        x = rnd(g, rows, K, dtype=T)
+        slots = torch.randperm(9000, generator=g, device="cuda")[:rows].remainder(4096).to(torch.int32)
+        got = serve.project_rows(x, p, bank, slots)
+        a, b, x64 = A[slots.long()].to(F64), B[slots.long()].to(F64), x.to(F64)
+        t = torch.bmm(x64[:, None], a)
+        want = torch.bmm(t, b)[:, 0]
+        c = (K / 16 + 32) * 2.0 ** -23
+        tol = torch.bmm(c * torch.bmm(x64.abs()[:, None], a.abs()) + (2.0 ** -16 + 40 * 2.0 ** -23) * t.abs(), b.abs())[:, 0]
+        near(got, want, tol)
+    with pytest.raises(ValueError):
+        bank.set(4095, A[:2], B[:2])
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
 def test_unaligned_rows_with_adapters_in_every_form(dtype):
     g = gen(21)
     T = DTYPES[dtype]
