@@ -417,6 +417,8 @@ ripple_status ripple_norm_rows(const ripple_norm_rows_args* args);
  *   y_i = act(x_i W + bias + scale_a (x_i A_a) B_a),  x_i = x[ids_i] (ids NULL: x[i]),  a = slots_i.
  * W (k x n) is laid out once by ripple_project_layout into a buffer of ripple_project_layout_bytes; the adapters of one
  * projection, A_a (k x r) and B_a (r x n) with r <= max_rank, live in a bank of `slots` places that ripple_adapter_set fills.
+ * Rows of one adapter are best side by side: above a few thousand rows, 128 neighbouring rows are multiplied with every adapter that one
+ * of them uses (146 433 fp32 rows of 295, n = 47, 63 adapters: 795 us in runs of two rows, 193 in runs of 20, 121 in runs of 2000).
  * Layout and bank are the caller's device memory, 128-byte aligned.  Sums are fp32; x, W, A and B share one type (fp32 products
  * are formed on the tensor cores from three bf16 parts per operand, all 24 bits), y has that type or F32. */
 #define RIPPLE_MAX_RANK 64

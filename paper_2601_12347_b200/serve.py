@@ -311,7 +311,8 @@ class AdapterBank:
 def project_rows(x, projection: Projection, bank: Optional[AdapterBank] = None, slots=None, ids=None, out=None, out_dtype=None):
     """act(x[ids] W + bias + scale_a (x[ids] A_a) B_a) for every row, a = slots[i] (int32; a slot that is negative, out of
     range or empty: no adapter).  x [any, K] of the projection's type, ids int32 or None; the result has that type, or fp32 if
-    out_dtype (or out) says so.  `out` shares no memory with an input."""
+    out_dtype (or out) says so.  `out` shares no memory with an input.  Any order of slots is right; above a few thousand rows, rows of
+    one slot side by side are fastest."""
     p = projection
     index = p.index
     x_ptr, x_ld, x_rows = _matrix(x, "x", p.K, p.dtype, index)
