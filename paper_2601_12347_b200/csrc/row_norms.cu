@@ -370,10 +370,10 @@ static cudaError_t launch_norm(NormParams p, int warps, void* stream) {
         p.stages = blocks <= sm_count() ? 1 : RN_STAGES * one <= 48 * 1024 ? RN_STAGES : 2 * one <= 200 * 1024 ? 2 : 1;
         bytes = p.stages * one;
     }
-    if (bytes > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e != cudaSuccess) return e;
-    }
+    // (the most that any call takes, once: a limit set call by call would be another thread's between its setting and its launch)
+    static bool ready[64];       // by device
+    const cudaError_t e = allow_shared(kernel, 200 * 1024, ready);
+    if (e != cudaSuccess) return e;
     if (blocks > sm_count() && (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, block, bytes) != cudaSuccess || per_sm < 1)) per_sm = 1;
     return launch(kernel, dim3((unsigned)std::min<int64_t>(blocks, (int64_t)per_sm * sm_count())), block, bytes, stream, p);
 }

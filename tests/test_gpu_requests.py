@@ -624,6 +624,41 @@ def test_streams_and_captured_graphs():
             assert torch.equal(outs[k], want[k])
 
 
+def test_threads_with_calls_of_different_sizes():
+    """Four host threads on streams of their own: what a call sets up is not another's."""
+    import threading
+    g = gen(23)
+    work = []
+    for width in (256, 2048, 8192, 16384):
+        y, r, gate = (rnd(g, 700, width) for _ in range(3))
+        ln = vectors(g, width, serve.NORM_LAYER, True)
+        t = Tenants(g, 128, width // 8, torch.bfloat16)
+        x, slots = rnd(g, 4000, 128, dtype=torch.bfloat16), runs(g, 4000, 40, 5)
+        call = lambda y=y, r=r, gate=gate, ln=ln, t=t, x=x, slots=slots: (*serve.norm_rows(y, post=ln, gate=gate, residual=r, pre=ln),
+                                                                           serve.project_rows(x, t.proj, t.bank, slots))
+        work.append((call, call()))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(call, want):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(60):
+                    got = call()
+                torch.cuda.current_stream().synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(got, want)):
+                    wrong.append("values")
+        except Exception as e:
+            wrong.append(repr(e))
+
+    threads = [threading.Thread(target=run, args=w) for w in work]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
 def test_every_wait_ended():
     """No bounded wait of the calls so far gave up."""
     serve.check_requests()
