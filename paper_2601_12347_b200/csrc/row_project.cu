@@ -765,7 +765,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
             const int steps = chunks + rank_steps(tile.count);
             Tile following = tile;
             for (int st = 0; st < steps; ++st) {
-                ok = mbar_wait_bounded(&empty[s], ph, PJ_SPIN_LIMIT);
+                ok = mbar_wait_warp(&empty[s], ph, PJ_SPIN_LIMIT);
                 if (!ok) break;
                 const uint32_t x_to = mine + (uint32_t)(s * S::STAGE), w_to = x_to + S::X_STAGE + (JOINED ? 128 * tile_w(tile) : 0);
                 const int between = PARTS == 3 ? w_part(tile) : 0;
@@ -982,7 +982,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                 const int b = sg & 1;
                 const bool side = side_by_side(tile);
                 const uint32_t large = lanes + large_at(b), small = lanes + small_at(b, worked, side, nt);
-                ok = __all_sync(FULL, mbar_wait_bounded(&acc_full[b], (sg >> 1) & 1, PJ_SPIN_LIMIT));
+                ok = mbar_wait_warp(&acc_full[b], (sg >> 1) & 1, PJ_SPIN_LIMIT);
                 if (!ok) break;
                 tc_fence_after();
                 if (PARTS == 3 && MANY && u < units - 1) {
@@ -1060,12 +1060,12 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                     const int before = sg >> 1;
                     ++sg;
                     // the epilogue must have read this accumulator (and with it the small products of the tile before the last)
-                    if (before > 0) ok = __all_sync(FULL, mbar_wait_bounded(&acc_empty[b], (before - 1) & 1, PJ_SPIN_LIMIT));
+                    if (before > 0) ok = mbar_wait_warp(&acc_empty[b], (before - 1) & 1, PJ_SPIN_LIMIT);
                     if (!ok) break;
                     tc_fence_after();
                     acc = __shfl_sync(FULL, tmem + large_at(b), 0), small = __shfl_sync(FULL, tmem + small_at(b, worked, side, nt), 0);
                 }
-                ok = __all_sync(FULL, mbar_wait_bounded(&full[s], ph, PJ_SPIN_LIMIT));
+                ok = mbar_wait_warp(&full[s], ph, PJ_SPIN_LIMIT);
                 if (!ok) break;
                 fence_async_smem();      // the loaders' stores, for the tensor core (on the reader's side: loads in flight are not waited for)
                 tc_fence_after();

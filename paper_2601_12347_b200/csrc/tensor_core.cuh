@@ -12,7 +12,7 @@ __device__ __forceinline__ void mbar_init(uint64_t* bar, int count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
 }
 
-// true once the phase with the given parity has completed; gives up after `limit` polls
+// true once the phase with the given parity has completed; gives up after `limit` polls.  For roles of one thread: see mbar_wait_warp
 __device__ __forceinline__ bool mbar_wait_bounded(uint64_t* bar, uint32_t parity, uint32_t limit) {
     const uint32_t addr = smem_u32(bar);
     for (uint32_t it = 0; it < limit; ++it) {
@@ -25,6 +25,13 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint64_t* bar, uint32_t parity
         if (ok) return true;
     }
     return false;
+}
+
+// The same by all lanes of a (converged) warp, with one verdict for all of them.  Lanes that poll for themselves may disagree where the
+// barrier completes around the last poll: those that gave up would then wait for the others at one barrier, and the others for
+// them at another, without end.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, uint32_t limit) {
+    return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, limit)) != 0;
 }
 
 // true in one lane of the (converged) warp
