@@ -338,7 +338,7 @@ k_update_rows_tc(Ctl* ctl, const __grid_constant__ UpdPair pair) {
             __syncwarp();
             if (lane == 0) mbar_arrive(&full_x[s]);
             // the stage that the step before used takes the chunk NH - 1 steps ahead
-            ok = mbar_wait_bounded(&empty[s_prev], ph_prev, spin_limit);
+            ok = mbar_wait_warp(&empty[s_prev], ph_prev, spin_limit);
             keep(s_prev);
             request(g + NH - 1 < total_steps);
             if (g > 0 && s_prev == NH - 1) ph_prev ^= 1;
@@ -542,7 +542,7 @@ k_update_rows_tc(Ctl* ctl, const __grid_constant__ UpdPair pair) {
             float sum[PIECES ? BLOCKS : 1][BLK];
             for (int part = 0; part < parts; ++part, ++sg) {
                 const int b = sg & 1;
-                ok = mbar_wait_bounded(&acc_full[b], (sg >> 1) & 1, spin_limit);
+                ok = mbar_wait_warp(&acc_full[b], (sg >> 1) & 1, spin_limit);
                 if (!ok) { s_fail = 1; break; }
                 tc_fence_after();
                 if (warp_busy) {
@@ -607,7 +607,7 @@ k_update_rows_tc(Ctl* ctl, const __grid_constant__ UpdPair pair) {
                     b = sg & 1;
                     const int ub = sg >> 1;
                     ++sg;
-                    if (ub > 0) ok = __all_sync(FULL, mbar_wait_bounded(&acc_empty[b], (ub - 1) & 1, spin_limit));
+                    if (ub > 0) ok = mbar_wait_warp(&acc_empty[b], (ub - 1) & 1, spin_limit);
                     if (!ok) return;
                     tc_fence_after();
                     d_addr = tmem_base + (uint32_t)(b * BUF);
@@ -617,10 +617,8 @@ k_update_rows_tc(Ctl* ctl, const __grid_constant__ UpdPair pair) {
                 if (PIECES || kc == 0) begin();
                 if (!ok) break;
                 if (RESIDENT) sw = kc;
-                bool there = true;
-                if (!RESIDENT || lt == 0) there = mbar_wait_bounded(&full_w[sw], phw, spin_limit);
-                there = there && mbar_wait_bounded(&full_x[s], ph, spin_limit);
-                ok = __all_sync(FULL, there);
+                if (!RESIDENT || lt == 0) ok = mbar_wait_warp(&full_w[sw], phw, spin_limit);
+                ok = ok && mbar_wait_warp(&full_x[s], ph, spin_limit);
                 if (!ok) break;
                 // The loaders' stores become visible to the tensor core's async proxy here, on the reader's side of the
                 // barrier: in the loaders the fence would wait for their row gathers in flight as well.

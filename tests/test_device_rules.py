@@ -30,7 +30,7 @@ def heads_around(text, at):
     return heads
 
 
-@pytest.mark.parametrize("name", ["row_project.cu"])
+@pytest.mark.parametrize("name", ["row_project.cu", "layer_update_tc.cu"])
 def test_lanes_of_a_warp_give_up_together(name):
     """A wait that runs out for some lanes of a warp only leaves them at another barrier than the rest, for good: what polls
     for itself is the role of one thread, and a warp that waits has one verdict."""
