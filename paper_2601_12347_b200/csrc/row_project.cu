@@ -231,11 +231,15 @@ __device__ __forceinline__ void store_t(const ProjectParams& p, int64_t i, int r
     }
 }
 
-// eight neighbouring entries as fp32
-__device__ __forceinline__ void load8(float (&v)[8], const float* from) {
+// Memory that no kernel in flight writes may be read past the rules of coherence, and is: the bank alone, which is complete before a call that
+// reads it is made.  Everything else may be the output of the kernel just before (t and the plan always are; rows, ids, slots, W and
+// bias where the caller made them on the same stream), which this kernel's blocks may have been resident beside.
+__device__ __forceinline__ float4 bank_word(const float4* from) { return __ldg(from); }
+// eight neighbouring entries of the bank as fp32
+__device__ __forceinline__ void bank8(float (&v)[8], const float* from) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const float4 e = __ldg(reinterpret_cast<const float4*>(from) + i);
+        const float4 e = bank_word(reinterpret_cast<const float4*>(from) + i);
         v[4 * i] = e.x, v[4 * i + 1] = e.y, v[4 * i + 2] = e.z, v[4 * i + 3] = e.w;
     }
 }
@@ -243,8 +247,9 @@ __device__ __forceinline__ float2 two_of(uint32_t x, __nv_bfloat16) { return mak
 __device__ __forceinline__ float2 two_of(uint32_t x, __half) {
     return make_float2(__half2float(__ushort_as_half((unsigned short)(x & 0xffff))), __half2float(__ushort_as_half((unsigned short)(x >> 16))));
 }
-template <typename T> __device__ __forceinline__ void load8(float (&v)[8], const T* from) {
-    const uint4 e = __ldg(reinterpret_cast<const uint4*>(from));
+template <typename T> __device__ __forceinline__ void bank8(float (&v)[8], const T* from) {
+    const float4 w = bank_word(reinterpret_cast<const float4*>(from));
+    const uint4 e = make_uint4(__float_as_uint(w.x), __float_as_uint(w.y), __float_as_uint(w.z), __float_as_uint(w.w));
     const float2 a = two_of(e.x, T()), b = two_of(e.y, T()), c = two_of(e.z, T()), d = two_of(e.w, T());
     v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
 }
@@ -319,11 +324,11 @@ __global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ Proj
                         if constexpr (PA == 3) {
                             float part[2][8];
                             const __nv_bfloat16* const from = reinterpret_cast<const __nv_bfloat16*>(w) + r * p.bank.k_pad + k0 + kk;
-                            load8(wv[r], from), load8(part[0], from + plane), load8(part[1], from + 2 * plane);
+                            bank8(wv[r], from), bank8(part[0], from + plane), bank8(part[1], from + 2 * plane);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) wv[r][e] += part[0][e] + part[1][e];
                         } else {
-                            load8(wv[r], reinterpret_cast<const T*>(w) + r * p.bank.k_pad + k0 + kk);
+                            bank8(wv[r], reinterpret_cast<const T*>(w) + r * p.bank.k_pad + k0 + kk);
                         }
                     }
 #pragma unroll
@@ -366,7 +371,9 @@ __global__ void __launch_bounds__(256) k_project_few(const __grid_constant__ Pro
     using T = typename Elem<TYPE>::T;
     constexpr int OWN = PF_K / 8;
     const bool adapted = p.bank.info != nullptr;
-    if (!adapted) pdl_enter();           // with adapters the kernel before computes t: what it waited for is there, t is waited for below
+    // With adapters the kernel before computes t, which is waited for below.  It began once all before it was over, so what those kernels
+    // wrote is there; up to the wait it is read out of L2, where it is, and not out of an L1 that nothing has brought up to date.
+    if (!adapted) pdl_enter();
     __shared__ __align__(16) float xs[2][PF_K * PF_LD];
     const int warp = threadIdx.x >> 5, lane = lane_id(), i0 = blockIdx.x * PF_ROWS;
     const int col = blockIdx.y * PF_COLS + lane, col_in = min(col, p.n - 1);
@@ -375,39 +382,43 @@ __global__ void __launch_bounds__(256) k_project_few(const __grid_constant__ Pro
     auto fetch_w = [&](int k0) {
         const int left = p.k - k0 - warp * OWN;
 #pragma unroll
-        for (int j = 0; j < OWN; ++j) wv[j] = j < left ? w[(int64_t)(k0 + j) * p.n] : from_f32<T>(0.f);
+        for (int j = 0; j < OWN; ++j) wv[j] = j < left ? __ldcg(w + (int64_t)(k0 + j) * p.n) : from_f32<T>(0.f);
     };
     fetch_w(0);
     // thread: a row and every 16th entry of it
     const int xr = threadIdx.x >> 4, xk = threadIdx.x & 15;
-    const int64_t x_from = i0 + xr < p.rows ? row_of(p, i0 + xr) : -1;
+    // the row that this thread fetches and the two that its warp finishes; all is asked for before any of it is looked at, since a load that
+    // waits for another costs half a microsecond
+    const int row[3] = {i0 + xr, i0 + 2 * warp, i0 + 2 * warp + 1};
+    int id[3], slot[2] = {-1, -1}, rank[2] = {0, 0};
+#pragma unroll
+    for (int h = 0; h < 3; ++h) id[h] = p.ids ? __ldcg(p.ids + min(row[h], p.rows - 1)) : row[h];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) if (adapted) slot[h] = __ldcg(p.slots + min(row[1 + h], p.rows - 1));
+#pragma unroll
+    for (int h = 0; h < 3; ++h) if (row[h] >= p.rows || id[h] >= p.x_rows) id[h] = -1;
+    const int64_t x_from = id[0];
     const T* const x = static_cast<const T*>(p.x) + max(x_from, (int64_t)0) * p.ld_x + xk;
     T xv[PF_K / 16];
     auto fetch_x = [&](int k0) {
         const int left = x_from >= 0 ? p.k - k0 - xk : 0;
 #pragma unroll
-        for (int e = 0; e < PF_K / 16; ++e) xv[e] = 16 * e < left ? x[k0 + 16 * e] : from_f32<T>(0.f);
+        for (int e = 0; e < PF_K / 16; ++e) xv[e] = 16 * e < left ? __ldcg(x + k0 + 16 * e) : from_f32<T>(0.f);
     };
     auto keep_x = [&](int b) {
 #pragma unroll
         for (int e = 0; e < PF_K / 16; ++e) xs[b][(xk + 16 * e) * PF_LD + xr] = to_f32(xv[e]);
     };
     fetch_x(0);
-    // the two rows that this warp finishes, and their adapters
-    bool live[2];
-    int slot[2] = {-1, -1}, rank[2] = {0, 0};
     const int rp = p.bank.r_pad;
     const float* b_at[2] = {};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int i = i0 + 2 * warp + h;
-        live[h] = i < p.rows && row_of(p, i) >= 0;
-        if (adapted && i < p.rows) slot[h] = p.slots[i];
-        if (slot[h] < 0 || slot[h] >= p.n_slots) slot[h] = -1;
+        if (id[1 + h] < 0 || slot[h] < 0 || slot[h] >= p.n_slots) slot[h] = -1;
         b_at[h] = p.bank.b32 + ((int64_t)max(slot[h], 0) * p.n + col_in) * rp;
         if (slot[h] >= 0) rank[h] = p.bank.info[slot[h]].rank;
     }
-    const float bias = p.bias ? p.bias[col_in] : 0.f;
+    const float bias = p.bias ? __ldcg(p.bias + col_in) : 0.f;
     float sum[PF_ROWS] = {};
     keep_x(0);
     __syncthreads();
@@ -445,14 +456,19 @@ __global__ void __launch_bounds__(256) k_project_few(const __grid_constant__ Pro
         float d = 0.f;
         for (int k = 0; k < rank[h]; k += 8) {
             float t[8], bv[8];
-            load8(t, static_cast<const float*>(p.t) + (int64_t)i * rp + k);
-            load8(bv, b_at[h] + k);
+            const float4* const t_at = reinterpret_cast<const float4*>(static_cast<const float*>(p.t) + (int64_t)i * rp + k);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float4 f = __ldcg(t_at + e);
+                t[4 * e] = f.x, t[4 * e + 1] = f.y, t[4 * e + 2] = f.z, t[4 * e + 3] = f.w;
+            }
+            bank8(bv, b_at[h] + k);
 #pragma unroll
             for (int e = 0; e < 8; ++e) d = fmaf(t[e], bv[e], d);
         }
         if (rank[h] > 0) y += d;
         if (p.act == RIPPLE_ACT_RELU && y < 0.f) y = 0.f;
-        if (col < p.n && live[h]) {
+        if (col < p.n && id[1 + h] >= 0) {
             if (p.out_f32) static_cast<float*>(p.y)[(int64_t)i * p.ld_y + col] = y;
             else static_cast<T*>(p.y)[(int64_t)i * p.ld_y + col] = from_f32<T>(y);
         }
@@ -705,7 +721,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
             for (int it = 0; it < ITS; ++it) {
                 if (vec && left >= 8) {
 #pragma unroll
-                    for (int h = 0; h < WORDS; ++h) raw[it][h] = __ldg(reinterpret_cast<const uint4*>(at[it]) + h);
+                    for (int h = 0; h < WORDS; ++h) raw[it][h] = reinterpret_cast<const uint4*>(at[it])[h];
                 } else {
                     Piece<T, 8> v;
 #pragma unroll
@@ -726,7 +742,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                     const bool own = (int)(which >> (8 * it) & 255) == j;
                     const uint4* const from = reinterpret_cast<const uint4*>(static_cast<const float*>(p.t) + (i0 + RSTEP * it) * r_pad + r);
 #pragma unroll
-                    for (int h = 0; h < WORDS; ++h) raw[it][h] = own ? __ldg(from + h) : make_uint4(0, 0, 0, 0);
+                    for (int h = 0; h < WORDS; ++h) raw[it][h] = own ? __ldcg(from + h) : make_uint4(0, 0, 0, 0);
                 }
             }
         };
@@ -894,7 +910,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                 __syncwarp();
                 for (int e = lane; e < 16 * NB; e += 32) {
                     const int col = c0 + 16 * (2 * (e >> 4) + half) + (e & 15);
-                    bias[e] = p.bias && col < p.n ? __ldg(p.bias + col) : 0.f;
+                    bias[e] = p.bias && col < p.n ? p.bias[col] : 0.f;
                 }
                 __syncwarp();
             }
@@ -1185,7 +1201,7 @@ __global__ void __launch_bounds__(256) k_finish_rows(const __grid_constant__ Pro
 #pragma unroll
         for (int k = 0; k < RB; ++k)
 #pragma unroll
-            for (int h = 0; h < 4; ++h) b[k][h] = __ldg(from + 4 * k + h);
+            for (int h = 0; h < 4; ++h) b[k][h] = bank_word(from + 4 * k + h);
     };
     float x[FR_ROWS];
 #pragma unroll
@@ -1193,7 +1209,7 @@ __global__ void __launch_bounds__(256) k_finish_rows(const __grid_constant__ Pro
 #pragma unroll
     for (int k = 0; k < RB; ++k) {
         const int e = k * 256 + threadIdx.x, r = e / (RB * 4);
-        ts[r][e % (RB * 4)] = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p.t) + (int64_t)min(first + r, p.rows - 1) * rp) + e % (RB * 4));
+        ts[r][e % (RB * 4)] = __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(p.t) + (int64_t)min(first + r, p.rows - 1) * rp) + e % (RB * 4));
     }
     if (threadIdx.x < FR_BLOCK) {
         const int i = first + threadIdx.x, a = i < p.rows ? p.slots[i] : -1;

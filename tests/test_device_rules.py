@@ -39,3 +39,15 @@ def test_lanes_of_a_warp_give_up_together(name):
     assert alone and re.search(r"\bmbar_wait_warp\s*\(", text)
     for at in alone:
         assert any(re.search(r"\blead\b|\blane == 0\b", h) for h in heads_around(text, at)), text[max(0, at - 200):at + 60]
+
+
+@pytest.mark.parametrize("name", ["row_project.cu", "row_norms.cu", "requests.cuh"])
+def test_only_the_bank_is_read_past_coherence(name):
+    """Kernels start while the one before still runs: what that one may write (rows, t, a plan) is read by ordinary loads, or out of L2;
+    never as memory that stays as it is."""
+    text = source(name)
+    assert not re.search(r"__restrict__|ld\.global\.nc", open(os.path.join(CSRC, name)).read())
+    for m in re.finditer(r"\b__ldg\s*\(", text):
+        assert any(re.search(r"\bbank_word\b", h) for h in heads_around(text, m.start())), text[m.start() - 100:m.end() + 60]
+    for m in re.finditer(r"\bbank(?:_word|8)\s*\(([^;]*);", text):
+        assert not re.search(r"\bp\.(t|x|y|base|plan|plain|bias|ids|slots)\b|\bat\[", m.group(1)), m.group(0)
