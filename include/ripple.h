@@ -473,7 +473,9 @@ int64_t ripple_project_workspace_bytes(const ripple_project_rows_args* args);
 ripple_status ripple_project_rows(const ripple_project_rows_args* args);
 
 /* Waits for the device and tells whether a bounded device-side wait of a call of requests gave up since the last query
- * (TIMEOUT: the results of those calls are not to be used).  The calls themselves return before their kernels have run. */
+ * (TIMEOUT, once: the results of those calls are not to be used).  The calls themselves return before their kernels have run, so
+ * nothing else tells.  (Diagnostic: with RIPPLE_DEBUG_TC_WITHHOLD=1 in the environment, read by every call, waits run out after a
+ * second or so.) */
 ripple_status ripple_request_status(int32_t device);
 
 /* Library version string. */

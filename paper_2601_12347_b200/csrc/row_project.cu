@@ -4,6 +4,7 @@
 #include "tensor_core.cuh"
 
 #include <algorithm>
+#include <cstdlib>
 
 namespace rp {
 
@@ -175,6 +176,7 @@ struct ProjectParams {
     void* y;
     int64_t ld_y;
     int out_f32;
+    int withhold;          // diagnostic: no CTA's first accumulator counts as filled
 };
 
 __device__ __forceinline__ int64_t row_of(const ProjectParams& p, int i) {
@@ -491,7 +493,8 @@ constexpr int PJ_FEW = 3000;
 constexpr int PF_MOST = 160, PF_MOST_F32 = 320;
 constexpr int PJ_T_COLS = 64;            // ranks of adapters side by side, where t is computed on the tensor cores
 constexpr int PJ_UNIT = 4;               // fp32: chunks (256 entries of K) whose large products share an accumulator
-constexpr uint32_t PJ_SPIN_LIMIT = 1u << 22;
+// Polls after which a wait gives up: about a second.  (A limit out of the arguments, shorter for the diagnostic: project-short-runs 83 -> 86 us.)
+constexpr uint32_t PJ_SPIN_LIMIT = 1u << 18;
 constexpr int PJ_STAGING = PJ_EPI_WARPS * (32 * 17 + 128) * 4;    // the epilogue's turned blocks, and its bias
 
 // MANY: fp32 rows of more than one unit, whose sums the epilogue carries in registers that twice the loader warps would need
@@ -635,7 +638,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
 
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], (PARTS == 3 ? PJ_LOADERS / 32 : PJ_LOADERS) + (SHRINK ? 0 : 1)); mbar_init(&empty[s], 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], PJ_EPI_WARPS); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], p.withhold ? 2 : 1 /* one arrives */); mbar_init(&acc_empty[b], PJ_EPI_WARPS); }
         mbar_init(&drained, 1);
         s_fail = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -1460,6 +1463,8 @@ extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) 
     else p.plan = nullptr;
     if (pj_joined(a)) p.base = reinterpret_cast<float*>(static_cast<uint8_t*>(p.t) + up128(a->rows * pj_up(a->max_rank, 16) * 4));
     p.y = a->y, p.ld_y = a->ld_y, p.out_f32 = a->out_type == RIPPLE_TYPE_F32;
+    const char* const withhold = getenv("RIPPLE_DEBUG_TC_WITHHOLD");
+    p.withhold = withhold && withhold[0] == '1';
     cudaError_t e;
     if (a->type == RIPPLE_TYPE_F32) e = project<RIPPLE_TYPE_F32>(p, a->cuda_stream);
     else if (a->type == RIPPLE_TYPE_BF16) e = project<RIPPLE_TYPE_BF16>(p, a->cuda_stream);

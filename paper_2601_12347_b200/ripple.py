@@ -443,7 +443,9 @@ class Ripple:
         """Request-based inference: what `head` (serve.RequestHead) makes of the rows `ids` (CUDA int32) of H^layer (default:
         the last), each with the adapters of its slot.  Runs on the current stream of the context's device and does not wait for it; the
         context's next call waits on the device until the rows have been read.  An id out of range leaves its row of the
-        result undefined.  While a graph is captured nothing is ordered: replay it between the context's calls."""
+        result undefined.  While a graph is captured nothing is ordered: replay it between the context's calls.
+        Like all calls of requests it returns before its kernels have run: `serve.check_requests` waits for them and raises if one of
+        their bounded waits gave up."""
         got = head(self.embeddings(self.L if layer is None else layer), ids, slots)
         if not self._torch.cuda.is_current_stream_capturing():
             self._stream.wait_stream(self._torch.cuda.current_stream(self._device))

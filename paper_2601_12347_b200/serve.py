@@ -9,7 +9,8 @@ request's tenant beside each:
     RequestHead    a stack of such blocks over the rows of one layer; `Ripple.answer` runs it
 
 Everything runs on the current CUDA stream of the tensors' device (not necessarily the current device) and returns once
-it is launched; calls can be captured into CUDA graphs.  Outputs and scratch come from PyTorch's allocator, so every call
+it is launched; calls can be captured into CUDA graphs.  Device-side waits are bounded; a call whose wait gave up has returned long
+before, and its results are not to be used: `check_requests`, where a program waits for its results anyway, tells of it.  Outputs and scratch come from PyTorch's allocator, so every call
 and every captured graph has its own.  Rows whose id lies outside the table (a negative id marks padding) are not
 written: they keep what `out` holds.  Rows are fp32, bf16 or fp16; sums and statistics are fp32.  The library infers: inputs that
 require gradients are refused while gradients are recorded.
@@ -359,7 +360,8 @@ def project_rows(x, projection: Projection, bank: Optional[AdapterBank] = None, 
 
 
 def check_requests(device=None) -> None:
-    """Waits for the device; raises RippleError (ERR_TIMEOUT) if a bounded device-side wait gave up since the last check."""
+    """Waits for the device; raises RippleError (ERR_TIMEOUT) if a bounded device-side wait of a call (project_rows, a RequestHead,
+    Ripple.answer) gave up since the last check: the results since then are not to be used.  No other call tells."""
     index = torch.cuda.current_device() if device is None else torch.device(device).index
     _check(_ripple.load_library().ripple_request_status(-1 if index is None else index))
 
