@@ -155,18 +155,21 @@ template <typename T, int V> __device__ __forceinline__ void store(void* to, con
     }
 }
 
-// 16-bit rows take the hardware's exponential and reciprocal: with the rounding of the exponent off by at most (10 + |g|) 2^-24, where the
-// output rounds at 2^-12 or more
-template <bool FAST>
+// How exact a sigmoid is.  Rows of 16 bits: the hardware's exponential and reciprocal, with the rounding of the exponent off by at most
+// (10 + |g|) 2^-24, where the outputs round at 2^-12 or more.  Beside an fp32 stream, which would show that: expf, off by 4 2^-24 however large
+// |g|, and the hardware's reciprocal, 2 2^-24.  (150 003 rows of 256 with full gates, 537 MB: 92 us the former, 96 the latter, 108 with a division.)
+enum { GATE_16, GATE_16_BESIDE_32, GATE_32 };
+template <int EXACT>
 __device__ __forceinline__ float sigmoid_of(float g) {
-    if constexpr (!FAST) return 1.0f / (1.0f + expf(-g));
+    if constexpr (EXACT == GATE_32) return 1.0f / (1.0f + expf(-g));
     float e, s;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
+    if constexpr (EXACT == GATE_16) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
+    else e = expf(-g);
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.0f + e));
     return s;
 }
 // (one decision per access and not per element)
-template <bool FAST, int V>
+template <int EXACT, int V>
 __device__ __forceinline__ void gates_of(Vec<V>& g, int act) {
     if (act == RIPPLE_GATE_IDENTITY) return;
     Vec<V> s = g;
@@ -182,7 +185,7 @@ __device__ __forceinline__ void gates_of(Vec<V>& g, int act) {
         }
     };
     if (act == RIPPLE_GATE_TANH) each([](float x) { return tanhf(x); });
-    else each([](float x) { return sigmoid_of<FAST>(x); });
+    else each([](float x) { return sigmoid_of<EXACT>(x); });
     if (act == RIPPLE_GATE_SILU) times<V>(g, s);
     else g = s;
 }
@@ -223,7 +226,7 @@ constexpr int RN_STAGES = 3;     // rows on their way at most
 template <typename T, typename TR, int V, int NP, bool MULTI, bool RING>
 __global__ void __launch_bounds__(MULTI ? (NP * V > 16 ? 512 : 256) : 128) k_norm_rows(const __grid_constant__ NormParams p) {
     pdl_enter();
-    constexpr bool FAST = sizeof(T) == 2;
+    constexpr int EXACT = sizeof(T) == 4 ? GATE_32 : sizeof(TR) == 4 ? GATE_16_BESIDE_32 : GATE_16;
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float scratch[MULTI ? 32 : 1];
     const int W = MULTI ? p.warps_per_row : 1, threads = 32 * W, t = MULTI ? threadIdx.x : lane_id();
@@ -333,12 +336,12 @@ __global__ void __launch_bounds__(MULTI ? (NP * V > 16 ? 512 : 256) : 128) k_nor
             if (wide_gate) {
                 each([&](int j, int c) {
                     Vec<V> k = RING ? load<T, V>(in + at_g + c * (int)sizeof(T)) : load<T, V>(&g_reg[RING ? 0 : j]);
-                    gates_of<FAST, V>(k, p.gate_act);
+                    gates_of<EXACT, V>(k, p.gate_act);
                     times<V>(s[j], k);
                 });
             }
             Vec<1> row_gate = {g_now};
-            if (p.gate && !wide_gate) gates_of<FAST, 1>(row_gate, p.gate_act);
+            if (p.gate && !wide_gate) gates_of<EXACT, 1>(row_gate, p.gate_act);
             const Vec<V> k = all_of<V>(row_gate.x * (p.scale_vector ? 1.0f : p.scale));
 #pragma unroll
             for (int j = 0; j < NP; ++j) times<V>(s[j], k);

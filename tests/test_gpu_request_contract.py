@@ -49,3 +49,22 @@ def test_a_wait_that_gives_up_is_reported(monkeypatch, dtype, K, N, rows, run):
     monkeypatch.delenv("RIPPLE_DEBUG_TC_WITHHOLD")
     t.check(x, of)
     serve.check_requests()
+
+
+# ---- gates over an fp32 stream
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("act", [serve.GATE_SIGMOID, serve.GATE_SILU])
+@pytest.mark.parametrize("wide", [True, False])
+@pytest.mark.parametrize("width", [5, 256, 2050])
+def test_gates_of_an_fp32_stream_are_as_exact_as_fp32(dtype, act, wide, width):
+    """s = act(gate) y in fp32: an exponential (2 steps: 4 u32), a sum, a reciprocal (1 step: 2 u32), two products (SiLU's, y's):
+    9 u32, whatever the type of the gate and however far it lies from zero."""
+    g = gen(31)
+    T = R.DTYPES[dtype]
+    y = rnd(g, 300, width, dtype=T) + 1
+    gate = torch.linspace(-40, 40, 300 * (width if wide else 1), device="cuda").view(300, -1).to(T)
+    s, _ = serve.norm_rows(y, gate=gate, gate_act=act, residual=torch.zeros(300, width, device="cuda"))
+    want = R.ACTS[act](gate.to(F64)) * y.to(F64)
+    assert s.dtype == torch.float32
+    worst = ((s.to(F64) - want).abs() / want.abs().clamp(min=2.0 ** -100)).max()
+    assert float(worst) <= 9 * U32, f"{float(worst) / U32} u32"
