@@ -1376,9 +1376,8 @@ extern "C" ripple_status ripple_adapter_set(void* bank, int32_t type, int32_t k,
     const int size = type_size(type);
     if (rank > 0 && (!A || !B || !scale || !aligned(A, size) || !aligned(B, size))) REFUSE("adapter_set: null or misaligned pointer");
     if (count == 0) return RIPPLE_OK;
-    if (rank > 0)
-        for (int i = 0; i < count; ++i)
-            if (!(scale[i] - scale[i] == 0.f)) REFUSE("adapter_set: a scale is not finite");
+    bool bad_scale = false;
+    for (int i = 0; rank > 0 && i < count; ++i) bad_scale = bad_scale || !(scale[i] - scale[i] == 0.f);
     OnDevice on(device);
     if (on.err != cudaSuccess) return launch_failed("cudaSetDevice", on.err);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -1388,8 +1387,9 @@ extern "C" ripple_status ripple_adapter_set(void* bank, int32_t type, int32_t k,
     int* bad = reinterpret_cast<int*>(static_cast<uint8_t*>(bank) + bank_a_at(slots) - 128);
     int host_bad = 0;
     SlotInfo host_info[256];
+    const bool holds = rank > 0 && !bad_scale;
     cudaError_t e = cudaMemsetAsync(bad, 0, sizeof(int), st);
-    if (e == cudaSuccess && rank > 0) {
+    if (e == cudaSuccess && holds) {
         const dim3 grid(592);
         uint16_t *a = const_cast<uint16_t*>(v.a), *b = const_cast<uint16_t*>(v.b);
         float* const b32 = const_cast<float*>(v.b32);
@@ -1401,10 +1401,12 @@ extern "C" ripple_status ripple_adapter_set(void* bank, int32_t type, int32_t k,
     }
     for (int at = 0; at < count && e == cudaSuccess; at += 256) {
         const int m = std::min(256, count - at);
-        for (int i = 0; i < m; ++i) host_info[i] = rank > 0 && !host_bad ? SlotInfo{scale[at + i], rank} : SlotInfo{0.f, 0};
+        for (int i = 0; i < m; ++i) host_info[i] = holds && !host_bad ? SlotInfo{scale[at + i], rank} : SlotInfo{0.f, 0};
         e = cudaMemcpyAsync(info + first + at, host_info, m * sizeof(SlotInfo), cudaMemcpyHostToDevice, st);
         if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     }
+    // (wrong whether or not there was a device to empty the slots on)
+    if (bad_scale) REFUSE("adapter_set: a scale is not finite%s%s", e == cudaSuccess ? "" : ", and the slots could not be emptied: ", e == cudaSuccess ? "" : cudaGetErrorString(e));
     if (e != cudaSuccess) return launch_failed("adapter_set", e);
     if (host_bad) REFUSE("adapter_set: an entry is not finite");
     return RIPPLE_OK;

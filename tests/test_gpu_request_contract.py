@@ -68,3 +68,20 @@ def test_gates_of_an_fp32_stream_are_as_exact_as_fp32(dtype, act, wide, width):
     assert s.dtype == torch.float32
     worst = ((s.to(F64) - want).abs() / want.abs().clamp(min=2.0 ** -100)).max()
     assert float(worst) <= 9 * U32, f"{float(worst) / U32} u32"
+
+
+# ---- adapters that are refused
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("rows", [7, 4000])
+def test_a_refused_scale_empties_its_slots(scale, rows):
+    g = gen(32)
+    t = R.Tenants(g, 60, 30, torch.float32, slots=4, max_rank=8)
+    x = rnd(g, rows, 60)
+    of = (torch.arange(rows, device="cuda") % 4).to(torch.int32)
+    with pytest.raises(serve.RippleError, match="not finite"):
+        t.bank.set(1, torch.stack([t.A[0][:, :3]] * 2), torch.stack([t.B[0][:3]] * 2), [0.5, scale])
+    del t.A[1], t.A[2]                  # both slots of the call hold no adapter any more, the others what they held
+    t.check(x, of)
+    t.A[2], t.B[2], t.scale[2] = t.A[0][:, :3].contiguous(), t.B[0][:3].contiguous(), 2.0
+    t.bank.set(2, t.A[2], t.B[2], 2.0)
+    t.check(x, of)
