@@ -420,7 +420,8 @@ ripple_status ripple_norm_rows(const ripple_norm_rows_args* args);
  * Rows of one adapter are best side by side: above a few thousand rows, 128 neighbouring rows are multiplied with every adapter that one
  * of them uses (146 433 fp32 rows of 295, n = 47, 63 adapters: 795 us in runs of two rows, 193 in runs of 20, 121 in runs of 2000).
  * Layout and bank are the caller's device memory, 128-byte aligned.  Sums are fp32; x, W, A and B share one type (fp32 products
- * are formed on the tensor cores from three bf16 parts per operand, all 24 bits), y has that type or F32. */
+ * are formed on the tensor cores from three bf16 parts per operand, all 24 bits), y has that type or F32.  x A goes into the second product
+ * with all its bits; with 16 where y has 16 bits. */
 #define RIPPLE_MAX_RANK 64
 #define RIPPLE_MAX_SLOTS 4096
 #define RIPPLE_MAX_PROJECT_K 8192

@@ -171,7 +171,8 @@ struct ProjectParams {
     const int32_t* slots;
     TilePlan* plan;        // one per 128 rows
     float* base;           // JOINED: x_i W, rows x n up to a multiple of 16
-    void* t;               // t_i = scale_a x_i A_a: fp32, rows x r_pad; 16-bit rows: two bf16 parts, rows x 2 x r_pad
+    void* t;               // t_i = scale_a x_i A_a: fp32, rows x r_pad; 16-bit rows: bf16 parts, rows x t_parts x r_pad
+    int t_parts;           // 16-bit results: two, 16 bits of t beside outputs of at most 11; fp32 results: three, all 24
     int batches;           // tensor-core form of t: batches of adapters that are multiplied side by side
     void* y;
     int64_t ld_y;
@@ -221,15 +222,17 @@ __global__ void k_plan_tiles(const __grid_constant__ ProjectParams p) {
 }
 
 template <int TYPE>
-__device__ __forceinline__ void store_t(const ProjectParams& p, int64_t i, int r, float t, bool parts) {
+__device__ __forceinline__ void store_t(const ProjectParams& p, int64_t i, int r, float t, int parts) {
     const int rp = p.bank.r_pad;
     if (TYPE == RIPPLE_TYPE_F32 || !parts) {
         static_cast<float*>(p.t)[i * rp + r] = t;
     } else {
-        __nv_bfloat16* const to = static_cast<__nv_bfloat16*>(p.t) + i * 2 * rp + r;
-        const __nv_bfloat16 h = __float2bfloat16_rn(t);
-        to[0] = h;
-        to[rp] = __float2bfloat16_rn(__hisinf(h) ? 0.f : t - __bfloat162float(h));
+        __nv_bfloat16* const to = static_cast<__nv_bfloat16*>(p.t) + i * parts * rp + r;
+        for (int q = 0; q < parts; ++q) {
+            const __nv_bfloat16 h = __float2bfloat16_rn(t);
+            to[q * rp] = h;
+            t = __hisinf(h) ? 0.f : t - __bfloat162float(h);
+        }
     }
 }
 
@@ -355,7 +358,7 @@ __global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ Proj
                     float t = sum[q][0];
 #pragma unroll
                     for (int r = 1; r < RANKS; ++r) t = lane == r ? sum[q][r] : t;
-                    store_t<TYPE>(p, i0 + q, r0 + lane, r0 + lane < info.rank ? t * info.scale : 0.f, planned > 0);
+                    store_t<TYPE>(p, i0 + q, r0 + lane, r0 + lane < info.rank ? t * info.scale : 0.f, planned > 0 ? p.t_parts : 0);
                 }
             }
         }
@@ -510,7 +513,6 @@ template <int TYPE, int BN, bool MANY> struct PjShape {
     static constexpr int STAGE = X_STAGE + W_STAGE;
     static constexpr int STAGES = 200 * 1024 / STAGE < 8 ? 200 * 1024 / STAGE : 8;
     static constexpr size_t BYTES = (size_t)STAGES * STAGE + PJ_STAGING + 1024;
-    static constexpr int RANKS = PARTS == 3 ? 64 : 32;      // ranks that a step of t_i B_a takes
 };
 
 // instruction descriptor: fp32 accumulators, both operands K-major, 128 rows, n columns
@@ -545,7 +547,9 @@ template <typename T> __device__ __forceinline__ uint4 word_of(const Piece<T, 8>
 }
 
 // What a launch of k_project_rows computes: t; y, with steps over ranks; or x W with t beside it.
-enum { PJ_SHRINK, PJ_RANKS, PJ_JOINED };
+// _3: t of 16-bit rows in three parts, for fp32 results, half as many ranks per step (30 011 rows, fp16, 512 -> 768, 7 adapters of rank 32 per
+// tile: 139 us, in two parts 92; 65 536 bf16 rows of 1024, one adapter of rank 16 per tile: 207 and 205).
+enum { PJ_SHRINK, PJ_RANKS, PJ_JOINED, PJ_SHRINK_3, PJ_RANKS_3 };
 
 // A persistent CTA takes tiles of 128 rows x BN columns: lanes of the accumulator are rows, its columns output columns.
 // SHRINK: the columns are the ranks of adapters that the tile's rows use, side by side, and each row keeps those of its own: t.
@@ -572,14 +576,16 @@ template <int TYPE, int BN, int MODE, bool MANY>
 __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project_rows(const __grid_constant__ ProjectParams p) {
     using T = typename Elem<TYPE>::T;
     using S = PjShape<TYPE, BN, MANY>;
-    constexpr bool SHRINK = MODE == PJ_SHRINK, JOINED = MODE == PJ_JOINED, BATCHED = SHRINK || JOINED;
+    constexpr bool SHRINK = MODE == PJ_SHRINK || MODE == PJ_SHRINK_3, JOINED = MODE == PJ_JOINED, BATCHED = SHRINK || JOINED;
     constexpr int PJ_LOADERS = S::LOADERS, A_COLS = SHRINK ? BN : PJ_T_COLS, W_COLS = JOINED ? BN - PJ_T_COLS : BN;
     // fp32, narrow tiles: the parts of W lie one behind the other and are multiplied at once, x1 [w1 w2 w3], x2 [w1 w2], x3 w1: half the
     // instructions, and two thirds of what they read of shared memory.  Accumulators: large, small, small.
     // (Whether a tile is narrow is a matter of the projection alone, not of the adapters that its rows happen to use: a row's result does not
     // depend on its neighbours.)
     constexpr int SIDE = S::PARTS == 3 && !MANY ? (BN < S::BUFFER / 3 ? BN : S::BUFFER / 3 / 16 * 16) : 0;      // up to so many columns
-    constexpr int PARTS = S::PARTS, STAGES = S::STAGES, NB = BN / 32, RANKS = S::RANKS, B_PLANES = pj_b_planes(TYPE);
+    constexpr int PARTS = S::PARTS, STAGES = S::STAGES, NB = BN / 32, B_PLANES = pj_b_planes(TYPE);
+    constexpr int T_PARTS = MODE == PJ_SHRINK_3 || MODE == PJ_RANKS_3 ? 3 : 2;
+    constexpr int RANKS = PARTS == 3 ? 64 : T_PARTS == 3 ? 16 : 32;            // ranks that a step of t_i B_a takes
     constexpr uint32_t TMEM = S::TMEM;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
@@ -662,7 +668,7 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
         const bool regs = PARTS == 3 || !vec;
         const int tail = p.k - (chunks - 1) * PJ_KC - c * 8;      // entries of this thread's piece of the last chunk
         // rank steps: this thread's piece of a step is a plane's ranks from c_rank
-        const int c_plane = PARTS == 3 ? 0 : c >> 2, c_rank = PARTS == 3 ? c * 8 : (c & 3) * 8;
+        const int c_plane = c / (RANKS / 8), c_rank = c % (RANKS / 8) * 8;
         // This thread's pieces of the rows of the tile being fetched, at its next chunk (rows that do not exist read row 0 of x, and
         // their results are dropped); of the rows of A; the rows' places among the adapters, a byte each; and all of it for the next tile.
         const T* const x0 = static_cast<const T*>(p.x) + c * 8;
@@ -839,7 +845,8 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                         for (int it = 0; it < ITS; ++it) {
                             const bool own = (int)(which >> (8 * it) & 255) == j;
                             const __nv_bfloat16* const t = static_cast<const __nv_bfloat16*>(p.t);
-                            copy_some(x_to + it * (RSTEP * 128), own ? t + ((i0 + RSTEP * it) * 2 + c_plane) * r_pad + r : t, own ? 16 : 0);
+                            if (c_plane >= T_PARTS) continue;                            // (a fourth place that no product reads)
+                            copy_some(x_to + it * (RSTEP * 128), own ? t + ((i0 + RSTEP * it) * T_PARTS + c_plane) * r_pad + r : t, own ? 16 : 0);
                         }
                     }
                 }
@@ -942,14 +949,17 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                         for (int e = 0; e < 8; ++e) v[e] = __float_as_uint(y[e]), w[e] = __float_as_uint(y[8 + e]);
                         pj_store8(to, v), pj_store8(to + 8, w);
                     } else {
-                        __nv_bfloat16* const to = static_cast<__nv_bfloat16*>(p.t) + (int64_t)i * 2 * r_pad + r;
+                        __nv_bfloat16* const to = static_cast<__nv_bfloat16*>(p.t) + (int64_t)i * T_PARTS * r_pad + r;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            v[e] = pj_pair<__nv_bfloat16>(y[2 * e], y[2 * e + 1]);
-                            const float h0 = __uint_as_float(v[e] << 16), h1 = __uint_as_float(v[e] & 0xffff0000u);
-                            w[e] = pj_pair<__nv_bfloat16>(fabsf(h0) < INFINITY ? y[2 * e] - h0 : 0.f, fabsf(h1) < INFINITY ? y[2 * e + 1] - h1 : 0.f);
+                        for (int q = 0; q < T_PARTS; ++q) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                v[e] = pj_pair<__nv_bfloat16>(y[2 * e], y[2 * e + 1]);
+                                const float h0 = __uint_as_float(v[e] << 16), h1 = __uint_as_float(v[e] & 0xffff0000u);
+                                y[2 * e] = fabsf(h0) < INFINITY ? y[2 * e] - h0 : 0.f, y[2 * e + 1] = fabsf(h1) < INFINITY ? y[2 * e + 1] - h1 : 0.f;
+                            }
+                            pj_store8(to + q * r_pad, v);
                         }
-                        pj_store8(to, v), pj_store8(to + r_pad, w);
                     }
                     return;
                 }
@@ -1117,14 +1127,18 @@ __global__ void __launch_bounds__(PjShape<TYPE, BN, MANY>::THREADS, 1) k_project
                             }
                         }
                     } else {
-                        // t in two parts (64 bytes of a row each), B in one or two
+                        // t in two parts (64 bytes of a row each) or three (32 bytes each), B in one or two.  Left out: with two the product
+                        // of the second parts (2^-18 of t B), with three that of the third and the second (2^-27).
+                        constexpr int NEXT = RANKS / 8;
 #pragma unroll
                         for (int j = 0; j < RANKS / 16; ++j) {
                             if (16 * j < left_t) {
                                 const uint64_t x1 = x + 2 * j, w1 = w + 2 * j;
                                 tc_mma_bf16(acc, x1, w1, idesc_t, 1u);
-                                tc_mma_bf16(acc, x1 + 4, w1, idesc_t, 1u);
-                                if (B_PLANES == 2) tc_mma_bf16(acc, x1, w1 + 4, idesc_t, 1u);
+                                tc_mma_bf16(acc, x1 + NEXT, w1, idesc_t, 1u);
+                                if (B_PLANES == 2) tc_mma_bf16(acc, x1, w1 + NEXT, idesc_t, 1u);
+                                if (T_PARTS == 3) tc_mma_bf16(acc, x1 + 2 * NEXT, w1, idesc_t, 1u);
+                                if (T_PARTS == 3 && B_PLANES == 2) tc_mma_bf16(acc, x1 + NEXT, w1 + NEXT, idesc_t, 1u);
                             }
                         }
                     }
@@ -1265,7 +1279,7 @@ static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
     const cudaError_t e = allow_shared(k_project_rows<TYPE, BN, MODE, MANY>, (int)S::BYTES, ready);
     if (e != cudaSuccess) return e;
     const int columns = MODE == PJ_JOINED ? BN - PJ_T_COLS : BN;
-    const int64_t across = MODE == PJ_SHRINK ? p.batches : (p.n + columns - 1) / columns, tiles = across * ((p.rows + PJ_ROWS - 1) / PJ_ROWS);
+    const int64_t across = MODE == PJ_SHRINK || MODE == PJ_SHRINK_3 ? p.batches : (p.n + columns - 1) / columns, tiles = across * ((p.rows + PJ_ROWS - 1) / PJ_ROWS);
     return launch(k_project_rows<TYPE, BN, MODE, MANY>, dim3((unsigned)std::min<int64_t>(tiles, sm_count())), S::THREADS, S::BYTES, stream, p);
 }
 template <int TYPE, int BN, int MODE>
@@ -1277,6 +1291,18 @@ static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
 }
 
 static int64_t few_blocks(int64_t rows, int n) { return (rows + PF_ROWS - 1) / PF_ROWS * ((n + PF_COLS - 1) / PF_COLS); }
+
+// Tiles of 32 columns where those of 128 would leave most SMs without one; of 256 (16-bit rows) where those leave none
+// (project of 65 536 x 1024 x 1024: 128 columns 200 us, 256 columns 125).
+template <int TYPE, int MODE>
+static cudaError_t project_columns(const ProjectParams& p, void* stream) {
+    const int row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
+    const int64_t wide = (int64_t)((p.n + 127) / 128) * row_tiles;
+    if constexpr (TYPE != RIPPLE_TYPE_F32) {
+        if (p.n > 128 && (int64_t)((p.n + 255) / 256) * row_tiles >= sm_count()) return project_tiles<TYPE, 256, MODE>(p, stream);
+    }
+    return wide >= sm_count() / 2 ? project_tiles<TYPE, 128, MODE>(p, stream) : project_tiles<TYPE, 32, MODE>(p, stream);
+}
 
 template <int TYPE>
 static cudaError_t project(ProjectParams p, void* stream) {
@@ -1307,18 +1333,18 @@ static cudaError_t project(ProjectParams p, void* stream) {
             const int batches = (std::min(p.n_slots, PJ_ROWS) + at_once - 1) / at_once;
             p.batches = std::max(1, std::min(batches, sm_count() / row_tiles));
             e = launch(k_plan_tiles, dim3(row_tiles), 128, 0, stream, p);
-            if (e == cudaSuccess) e = project_tiles<TYPE, T_COLS, PJ_SHRINK>(p, stream);
+            if constexpr (!F32) {
+                if (e == cudaSuccess && p.t_parts == 3) e = project_tiles<TYPE, T_COLS, PJ_SHRINK_3>(p, stream);
+            }
+            if (e == cudaSuccess && p.t_parts == 2) e = project_tiles<TYPE, T_COLS, PJ_SHRINK>(p, stream);
         }
         if (e != cudaSuccess) return e;
     }
     if (few) return launch(k_project_few<TYPE>, dim3((p.rows + PF_ROWS - 1) / PF_ROWS, (p.n + PF_COLS - 1) / PF_COLS), 256, 0, stream, p);
-    // Tiles of 32 columns where those of 128 would leave most SMs without one; of 256 (16-bit rows) where those leave none
-    // (project of 65 536 x 1024 x 1024: 128 columns 200 us, 256 columns 125).
-    const int64_t wide = (int64_t)((p.n + 127) / 128) * row_tiles;
     if constexpr (!F32) {
-        if (p.n > 128 && (int64_t)((p.n + 255) / 256) * row_tiles >= sm_count()) return project_tiles<TYPE, 256, PJ_RANKS>(p, stream);
+        if (p.bank.info && p.t_parts == 3) return project_columns<TYPE, PJ_RANKS_3>(p, stream);
     }
-    return wide >= sm_count() / 2 ? project_tiles<TYPE, 128, PJ_RANKS>(p, stream) : project_tiles<TYPE, 32, PJ_RANKS>(p, stream);
+    return project_columns<TYPE, PJ_RANKS>(p, stream);
 }
 
 }  // namespace rp
@@ -1416,12 +1442,14 @@ static bool pj_joined(const ripple_project_rows_args* a) {
     return a->bank && a->type == RIPPLE_TYPE_F32 && a->rows > PJ_FEW && few_blocks(a->rows, a->n) > PF_MOST_F32 && a->n <= 128 - PJ_T_COLS;
 }
 
+// t: fp32, or up to three bf16 parts (what of it a call needs depends on the result's type, its size does not)
+static int64_t t_bytes(const ripple_project_rows_args* a) { return up128(a->rows * pj_up(a->max_rank, 16) * (a->type == RIPPLE_TYPE_F32 ? 4 : 6)); }
+
 extern "C" int64_t ripple_project_workspace_bytes(const ripple_project_rows_args* a) {
     if (!a || a->rows < 0 || !shape_ok(a->type, a->k, a->n)) return -1;
     if (!a->bank) return 0;
     if (!bank_ok(a->n_slots, a->max_rank)) return -1;
-    return (a->rows + 127) / 128 * (int64_t)sizeof(TilePlan) + up128(a->rows * pj_up(a->max_rank, 16) * 4)
-           + (pj_joined(a) ? up128(a->rows * pj_up(a->n, 16) * 4) : 0);
+    return (a->rows + 127) / 128 * (int64_t)sizeof(TilePlan) + t_bytes(a) + (pj_joined(a) ? up128(a->rows * pj_up(a->n, 16) * 4) : 0);
 }
 
 extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) {
@@ -1463,8 +1491,8 @@ extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) 
     p.n_slots = a->n_slots, p.slots = a->slots, p.plan = static_cast<TilePlan*>(a->workspace);
     if (a->bank) p.t = static_cast<uint8_t*>(a->workspace) + (a->rows + 127) / 128 * (int64_t)sizeof(TilePlan);
     else p.plan = nullptr;
-    if (pj_joined(a)) p.base = reinterpret_cast<float*>(static_cast<uint8_t*>(p.t) + up128(a->rows * pj_up(a->max_rank, 16) * 4));
-    p.y = a->y, p.ld_y = a->ld_y, p.out_f32 = a->out_type == RIPPLE_TYPE_F32;
+    if (pj_joined(a)) p.base = reinterpret_cast<float*>(static_cast<uint8_t*>(p.t) + t_bytes(a));
+    p.y = a->y, p.ld_y = a->ld_y, p.out_f32 = a->out_type == RIPPLE_TYPE_F32, p.t_parts = a->type != RIPPLE_TYPE_F32 && p.out_f32 ? 3 : 2;
     const char* const withhold = getenv("RIPPLE_DEBUG_TC_WITHHOLD");
     p.withhold = withhold && withhold[0] == '1';
     cudaError_t e;

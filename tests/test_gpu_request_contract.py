@@ -85,3 +85,50 @@ def test_a_refused_scale_empties_its_slots(scale, rows):
     t.A[2], t.B[2], t.scale[2] = t.A[0][:, :3].contiguous(), t.B[0][:3].contiguous(), 2.0
     t.bank.set(2, t.A[2], t.B[2], 2.0)
     t.check(x, of)
+
+
+# ---- fp32 results of 16-bit rows
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("K,N,rows,run", [(64, 40, 500, 5), (64, 200, 4000, 9), (64, 200, 4000, 700), (48, 512, 20_000, 300), (200, 33, 3000, 1)])
+@pytest.mark.parametrize("rank", [1, 16, 33, 64])
+def test_fp32_results_keep_the_bits_of_x_a(dtype, K, N, rows, run, rank):
+    """fp32 results of 16-bit rows: x A and its product with B are sums of fp32, in calls of every size.  x W + bias is
+    zero, so that nothing hides them.  Two sums of products of which the tensor core cuts what an addition loses (2^-23, 16 products at
+    a time; fp16's B in two parts, t in three: up to five products for one), t's last part rounds at 2^-25, the product of t's third and
+    B's second part, left out, is below 2^-26."""
+    g = gen(K + rank)
+    T = R.DTYPES[dtype]
+    p = serve.Projection(torch.zeros(K, N, dtype=T, device="cuda"))
+    bank = serve.AdapterBank(p, 20, rank)
+    A, B = rnd(g, 20, K, rank, dtype=T, scale=K ** -0.5), rnd(g, 20, rank, N, dtype=T)
+    bank.set(0, A, B, 1.0)
+    x, of = rnd(g, rows, K, dtype=T), runs(g, rows, run, 20)
+    got = serve.project_rows(x, p, bank, of, out_dtype=torch.float32).to(F64)
+    want, tol = torch.zeros_like(got), torch.zeros_like(got)
+    for s in range(20):
+        mine = (of == s).nonzero()[:, 0]
+        t, b = x[mine].to(F64) @ A[s].to(F64), B[s].to(F64).abs()
+        want[mine] = t @ B[s].to(F64)
+        first = (K / 16 + 8) * 2.0 ** -23 * (x[mine].to(F64).abs() @ A[s].to(F64).abs())
+        # (a tile's adapters stand one behind the other: additions of zeros lose nothing)
+        second = (5 * (rank / 16 + 2) + 4) * 2.0 ** -23
+        tol[mine] = (first + second * t.abs()) @ b + U32 * want[mine].abs()
+    assert float(((got - want).abs() - tol).max()) <= 0, f"{float(((got - want).abs() / tol.clamp(min=1e-300)).max())} of the tolerance"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows", [20, 4000])
+def test_one_product_of_one_rank_is_exact_to_fp32(dtype, rows):
+    """K = 1, rank 1: t is x a, 16 or 22 bits; y = t b scale.  Roundings: t (fp32) and its scale 2 u32, its last part 2^-25, the sum of up to
+    five products of parts, each addition cut at 2^-23."""
+    g = gen(33)
+    T = R.DTYPES[dtype]
+    p = serve.Projection(torch.zeros(1, 40, dtype=T, device="cuda"))
+    bank = serve.AdapterBank(p, 3, 1)
+    A, B = rnd(g, 3, 1, 1, dtype=T), rnd(g, 3, 1, 40, dtype=T)
+    bank.set(0, A, B, [1 / 3, 0.7, -1.1])
+    x, of = rnd(g, rows, 1, dtype=T), torch.randint(0, 3, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    scale = torch.tensor([1 / 3, 0.7, -1.1], device="cuda").to(F64)
+    want = x.to(F64) * (A[:, :, 0].to(F64) * scale[:, None])[of.long()] * B[:, 0].to(F64)[of.long()]
+    got = serve.project_rows(x, p, bank, of, out_dtype=torch.float32)
+    assert float(((got.to(F64) - want).abs() / want.abs().clamp(min=1e-30)).max()) <= 2 * U32 + 2.0 ** -25 + 5 * 2.0 ** -23
