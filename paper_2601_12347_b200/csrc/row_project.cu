@@ -48,10 +48,13 @@ __host__ __device__ inline BankView bank_view(const void* bank, int type, int k,
             reinterpret_cast<const float*>(p + bank_b32_at(type, k, n, slots, max_rank)), pj_up(max_rank, 16), pj_up(k, PJ_KC)};
 }
 
-// An fp32 value as three bf16 parts, 8 bits each: the first cut (rounded, values next to the largest would become
-// infinite), the others what is left, rounded; both remainders are exact.  An infinite value has no remainders.
+// An fp32 weight as three bf16 parts, 8 bits each, rounded; both remainders are exact.  The second part has either sign and
+// at most 2^-8 of the value: with the rows' parts, which are cut (pj_parts_of2: third part below 2^-15), the products that are left out stay below
+// 2^-23 of the whole and have no sign of their own.  (With a first part that is cut as well x3 w2 reached 2^-22, always towards zero.)  Only
+// a value that would round to infinity is cut, and an infinite value has no remainders.
 __device__ __forceinline__ void pj_parts_of(float x, __nv_bfloat16 (&h)[3]) {
-    h[0] = __float2bfloat16_rz(x);
+    h[0] = __float2bfloat16_rn(x);
+    if (__hisinf(h[0]) && isfinite(x)) h[0] = __float2bfloat16_rz(x);
     float left = isfinite(x) ? x - __bfloat162float(h[0]) : 0.f;
     h[1] = __float2bfloat16_rn(left);
     h[2] = __float2bfloat16_rn(left - __bfloat162float(h[1]));
@@ -138,10 +141,16 @@ __global__ void k_set_adapters(uint16_t* a_out, uint16_t* b_out, float* b32_out,
             uint16_t* const to = b_out + (first + s) * PB * per_b + e;
             float left = to_f32(v);
             b32_out[(first + s) * per_b + e] = left;
-            for (int q = 0; q < PB; ++q) {
-                const __nv_bfloat16 h = q == 0 && PB == 3 ? __float2bfloat16_rz(left) : __float2bfloat16_rn(left);
-                to[q * per_b] = __bfloat16_as_ushort(h);
-                left -= __bfloat162float(h);
+            if constexpr (PB == 3) {
+                __nv_bfloat16 h[3];
+                pj_parts_of(left, h);
+                for (int q = 0; q < 3; ++q) to[q * per_b] = __bfloat16_as_ushort(h[q]);
+            } else {
+                for (int q = 0; q < PB; ++q) {
+                    const __nv_bfloat16 h = __float2bfloat16_rn(left);
+                    to[q * per_b] = __bfloat16_as_ushort(h);
+                    left -= __bfloat162float(h);
+                }
             }
         }
         fine = fine && isfinite(to_f32(v));
@@ -561,7 +570,7 @@ enum { PJ_SHRINK, PJ_RANKS, PJ_JOINED, PJ_SHRINK_3, PJ_RANKS_3 };
 //              fp32 entries as three bf16 parts; and what comes out of the bank
 //   one thread copies the weights' chunks, one issues the products
 //   epilogue   takes a finished accumulator while the next is being filled: bias, activation, and out
-// fp32: six products of parts (all but those below 2^-23); the large one of the first parts is handed over every 256 entries
+// fp32: six products of parts (all but those below 2^-23, see pj_parts_of); the large one of the first parts is handed over every 256 entries
 // and summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
 // Barriers, all waits bounded: full[s] (one arrival per loader warp, 16-bit rows: per thread; one with the bytes of the weights),
 // empty[s] (the products that read stage s), acc_full[b], acc_empty[b] (one arrival per epilogue warp).

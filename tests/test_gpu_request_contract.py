@@ -132,3 +132,41 @@ def test_one_product_of_one_rank_is_exact_to_fp32(dtype, rows):
     want = x.to(F64) * (A[:, :, 0].to(F64) * scale[:, None])[of.long()] * B[:, 0].to(F64)[of.long()]
     got = serve.project_rows(x, p, bank, of, out_dtype=torch.float32)
     assert float(((got.to(F64) - want).abs() / want.abs().clamp(min=1e-30)).max()) <= 2 * U32 + 2.0 ** -25 + 5 * 2.0 ** -23
+
+
+# ---- parts of fp32 operands
+def test_products_that_are_left_out_of_fp32_ones_are_small_and_have_no_sign():
+    """K = 1: y = x w from six products of parts.  For x = w = 1 + k 2^-7 - 2^-23 the second part of w is 2^-23 and what is left out
+    below 2^-37; x1 w1 has 16 bits and is exact, the other five are added up with cuts of at most 2^-23 of their sum of at most
+    2^-6, five times 2^-29, and rounded once with the first: 2^-24 + 5 2^-29.  Over x and w from 1 to 2 the roundings have no
+    sign and the cuts at most 5 2^-29 = 2^-26.7 (left out x3 w2 with the sign of x w: 2^-25)."""
+    g = gen(34)
+    rows, N = 9000, 200
+    x, w = 1 + torch.rand(rows, 1, generator=g, device="cuda"), 1 + torch.rand(1, N, generator=g, device="cuda")
+    k = torch.arange(100, device="cuda")
+    x[:100, 0] = w[0, :100] = 1 + k * 2.0 ** -7 - 2.0 ** -23 * (k > 0)
+    for n in (N, 40):
+        for sign in (1, -1):
+            W = (sign * w[:, N - n:] if n < N else sign * w).contiguous()
+            want = x.to(F64) @ W.to(F64)
+            off = (serve.project_rows(x, serve.Projection(W)).to(F64) - want) / want
+            assert float(off[100:].mean().abs()) <= 2.0 ** -26.7
+            assert float(off.abs().max()) <= 2.0 ** -23 + 2.0 ** -24 + 2.0 ** -32 + 2.0 ** -24 + 5 * 2.0 ** -29
+            if n == N:
+                assert float(off[k, k].abs().max()) <= 2.0 ** -24 + 5 * 2.0 ** -29
+
+
+def test_fp32_weights_next_to_the_largest():
+    """They have no part that rounds to infinity, in a layout and in a bank."""
+    big = torch.finfo(torch.float32).max
+    W = torch.diag(torch.tensor([big, -big, big * (1 - 2.0 ** -9), 1.0], device="cuda"))
+    x = torch.full((9000, 4), 0.5, device="cuda")
+    want = (x.to(F64) @ W.to(F64)).to(torch.float32)
+    assert torch.equal(serve.project_rows(x, serve.Projection(W.repeat(1, 50)))[:, :4], want)
+    p = serve.Projection(torch.zeros(4, 200, device="cuda"))
+    bank = serve.AdapterBank(p, 2, 4)
+    slots = torch.zeros(9000, dtype=torch.int32, device="cuda")
+    bank.set(0, torch.eye(4, device="cuda"), W.repeat(1, 50))
+    assert torch.equal(serve.project_rows(x, p, bank, slots)[:, :4], want)
+    bank.set(0, W, torch.eye(4, device="cuda").repeat(1, 50))
+    assert torch.equal(serve.project_rows(x, p, bank, slots)[:, :4], want)
