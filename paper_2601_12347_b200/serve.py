@@ -97,8 +97,8 @@ def _vector(t, name: str, size: int, dtype, index: int) -> int:
     return t.data_ptr()
 
 
-def _to_device(a, dtype, device, name: str):
-    """A weight given as an array or a tensor, contiguous on the device."""
+def _to_device(a, dtype, device, name: str, copy: bool = False):
+    """A weight given as an array or a tensor, contiguous on the device; with `copy` never the caller's memory."""
     if isinstance(a, torch.Tensor):
         if device is None and a.is_cuda:
             device = a.device
@@ -112,7 +112,7 @@ def _to_device(a, dtype, device, name: str):
         raise ValueError(f"{name}: a CUDA device expected, got {device}")
     if device.index is None:
         device = torch.device("cuda", torch.cuda.current_device())
-    return a.to(device=device, dtype=dtype or a.dtype).contiguous()
+    return a.to(device=device, dtype=dtype or a.dtype, copy=copy).contiguous()
 
 
 def _stream(index: int) -> int:
@@ -124,7 +124,7 @@ _stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream)
 
 
 class Norm:
-    """Layer or root-mean-square norm with its vectors (arrays or tensors; kept in fp32 on the device)."""
+    """Layer or root-mean-square norm with its vectors (arrays or tensors; an fp32 copy is kept on the device)."""
 
     def __init__(self, kind: int, weight=None, bias=None, eps: float = 1e-5, device=None):
         if kind not in (NORM_LAYER, NORM_RMS):
@@ -132,8 +132,8 @@ class Norm:
         if not eps >= 0:
             raise ValueError(f"eps: {eps}")
         self.kind, self.eps = int(kind), float(eps)
-        self.weight = None if weight is None else _to_device(weight, torch.float32, device, "weight")
-        self.bias = None if bias is None else _to_device(bias, torch.float32, device, "bias")
+        self.weight = None if weight is None else _to_device(weight, torch.float32, device, "weight", copy=True)
+        self.bias = None if bias is None else _to_device(bias, torch.float32, device, "bias", copy=True)
         self.width = self.index = None         # any, without vectors
         for t in (self.weight, self.bias):
             if t is not None:
@@ -237,7 +237,7 @@ def norm_rows(y=None, *, post: Optional[Norm] = None, gate=None, gate_act: int =
 class Projection:
     """y = act(x W + bias), W [K, N] input-major like the layers' matrices, laid out once for the tensor cores.
 
-    W, bias: arrays or tensors; `dtype` (default: W's) is the type of x, W and the adapters; the bias is kept in fp32."""
+    W, bias: arrays or tensors; `dtype` (default: W's) is the type of x, W and the adapters.  Copies are kept, of the bias in fp32."""
 
     def __init__(self, W, bias=None, act: int = ACT_IDENTITY, dtype=None, device=None):
         W = _to_device(W, dtype, device, "W")
@@ -253,7 +253,7 @@ class Projection:
         size = self.lib.ripple_project_layout_bytes(self.type, self.K, self.N)
         if size < 0:
             raise ValueError(f"W: {self.K} x {self.N} is out of range")
-        self.bias = None if bias is None else _to_device(bias, torch.float32, self.device, "bias")
+        self.bias = None if bias is None else _to_device(bias, torch.float32, self.device, "bias", copy=True)
         if self.bias is not None and tuple(self.bias.shape) != (self.N,):
             raise ValueError(f"bias: [{self.N}] expected, got {tuple(self.bias.shape)}")
         self.layout = torch.empty(size, dtype=torch.uint8, device=self.device)

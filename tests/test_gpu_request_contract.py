@@ -170,3 +170,15 @@ def test_fp32_weights_next_to_the_largest():
     assert torch.equal(serve.project_rows(x, p, bank, slots)[:, :4], want)
     bank.set(0, W, torch.eye(4, device="cuda").repeat(1, 50))
     assert torch.equal(serve.project_rows(x, p, bank, slots)[:, :4], want)
+
+
+# ---- weights
+def test_operators_keep_copies_of_their_weights():
+    g = gen(35)
+    w, b, W, bias = 1 + rnd(g, 64), rnd(g, 64), rnd(g, 64, 40), rnd(g, 40)
+    x = rnd(g, 9, 64)
+    n, p = serve.Norm(serve.NORM_LAYER, w, b), serve.Projection(W, bias)
+    want = serve.norm_rows(x, pre=n)[1], serve.project_rows(x, p)
+    for t in (w, b, W, bias):
+        t.zero_()
+    assert torch.equal(serve.norm_rows(x, pre=n)[1], want[0]) and torch.equal(serve.project_rows(x, p), want[1])
