@@ -11,7 +11,9 @@ request's tenant beside each:
 Everything runs on the current CUDA stream of the tensors' device (not necessarily the current device) and returns once
 it is launched; calls can be captured into CUDA graphs.  Device-side waits are bounded; a call whose wait gave up has returned long
 before, and its results are not to be used: `check_requests`, where a program waits for its results anyway, tells of it.  Outputs and scratch come from PyTorch's allocator, so every call
-and every captured graph has its own.  Rows whose id lies outside the table (a negative id marks padding) are not
+and every captured graph has its own.  Operators (Norm, Projection, AdapterBank, RequestHead) may be dropped while calls that read them
+are in flight, on whatever stream; tensors of the caller follow PyTorch's rule (`Tensor.record_stream`), and a captured graph reads
+both as long as it is replayed.  Rows whose id lies outside the table (a negative id marks padding) are not
 written: they keep what `out` holds.  Rows are fp32, bf16 or fp16; sums and statistics are fp32.  The library infers: inputs that
 require gradients are refused while gradients are recorded.
 """
@@ -123,7 +125,27 @@ def _stream(index: int) -> int:
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream)
 
 
-class Norm:
+class _Buffers:
+    """Device memory that an operator keeps.  It belongs to the stream that it was allocated on; PyTorch's allocator is told of every
+    other that a call reads it on, so that an operator may be dropped while such calls are in flight.  (Once per stream: what counts is
+    where the stream stands when the memory is given back.)"""
+
+    def _keep(self, index: Optional[int], *tensors):
+        self._tensors = tensors
+        self._streams = set() if index is None else {_stream(index)}
+
+    def _read_on(self, stream: int):
+        if stream in self._streams:
+            return
+        for t in self._tensors:
+            with torch.cuda.device(t.device):
+                if torch.cuda.is_current_stream_capturing():
+                    return                     # (nothing is in flight; who replays the graph keeps the operator)
+                t.record_stream(torch.cuda.current_stream())
+        self._streams.add(stream)
+
+
+class Norm(_Buffers):
     """Layer or root-mean-square norm with its vectors (arrays or tensors; an fp32 copy is kept on the device)."""
 
     def __init__(self, kind: int, weight=None, bias=None, eps: float = 1e-5, device=None):
@@ -141,11 +163,13 @@ class Norm:
                     raise ValueError("norm vectors: one dimension, one size and one device expected")
                 self.width, self.index = t.shape[0], t.get_device()
                 torch.cuda.current_stream(t.device).synchronize()    # usable on every stream from here on
+        self._keep(self.index, *(t for t in (self.weight, self.bias) if t is not None))
         self._args = (self.kind, self.eps, 0 if self.weight is None else self.weight.data_ptr(), 0 if self.bias is None else self.bias.data_ptr())
 
-    def _packed(self, width: int, index: int, name: str):
+    def _packed(self, width: int, index: int, stream: int, name: str):
         if self.width is not None and (self.width != width or self.index != index):
             raise ValueError(f"{name}: vectors of {width} entries on cuda:{index} expected, got {self.width} on cuda:{self.index}")
+        self._read_on(stream)
         return self._args
 
 
@@ -224,17 +248,18 @@ def norm_rows(y=None, *, post: Optional[Norm] = None, gate=None, gate_act: int =
                 raise ValueError(f"normed_out: {rows} rows expected, got {got}")
     elif normed_out is not None:
         raise ValueError("normed_out without pre")
-    post_args = _NO_NORM if post is None else post._packed(width, index, "post")
-    pre_args = _NO_NORM if pre is None else pre._packed(width, index, "pre")
+    stream = _stream(index)
+    post_args = _NO_NORM if post is None else post._packed(width, index, stream, "post")
+    pre_args = _NO_NORM if pre is None else pre._packed(width, index, stream, "pre")
     if rows == 0:
         return out, normed_out
     _check(_ripple.load_library().ripple_norm_rows(_NORM_ARGS.pack(
         rows, width, t, ts, int(gate_act), y_ptr, y_ld, gate_ptr, gate_ld, res_ptr, res_ld, res_rows, ids_ptr, vec_ptr,
-        out_ptr, out_ld, n_ptr, n_ld, *post_args, *pre_args, number, gate_width, index, 0, _stream(index))))
+        out_ptr, out_ld, n_ptr, n_ld, *post_args, *pre_args, number, gate_width, index, 0, stream)))
     return out, normed_out
 
 
-class Projection:
+class Projection(_Buffers):
     """y = act(x W + bias), W [K, N] input-major like the layers' matrices, laid out once for the tensor cores.
 
     W, bias: arrays or tensors; `dtype` (default: W's) is the type of x, W and the adapters.  Copies are kept, of the bias in fp32."""
@@ -260,10 +285,11 @@ class Projection:
         _check(self.lib.ripple_project_layout(self.type, self.K, self.N, W.data_ptr(), self.N, self.layout.data_ptr(),
                                               self.index, _stream(self.index)))
         torch.cuda.current_stream(self.device).synchronize()     # usable on every stream from here on
+        self._keep(self.index, *(t for t in (self.layout, self.bias) if t is not None))
         self._tail = (self.layout.data_ptr(), 0 if self.bias is None else self.bias.data_ptr())
 
 
-class AdapterBank:
+class AdapterBank(_Buffers):
     """Low-rank adapters of one projection, by slot."""
 
     def __init__(self, projection: Projection, slots: int, max_rank: int):
@@ -272,6 +298,7 @@ class AdapterBank:
         if not 1 <= self.slots <= MAX_SLOTS or not 1 <= self.max_rank <= MAX_RANK:
             raise ValueError(f"1 to {MAX_SLOTS} slots of rank 1 to {MAX_RANK} expected, got {slots} of {max_rank}")
         self.buffer = torch.empty(p.lib.ripple_adapter_bytes(p.type, p.K, p.N, self.slots, self.max_rank), dtype=torch.uint8, device=p.device)
+        self._keep(p.index, self.buffer)
         self._scratch = (-1, 0)          # rows of the last call, and the scratch that it takes
         self._set(0, self.slots, 0, None, None, None)
 
@@ -344,6 +371,10 @@ def project_rows(x, projection: Projection, bank: Optional[AdapterBank] = None, 
         raise TypeError(f"out: {p.dtype} or float32 expected, got {out.dtype}")
     if rows == 0:
         return out
+    stream = _stream(index)
+    p._read_on(stream)
+    if bank is not None:
+        bank._read_on(stream)
     head = (rows, p.type, out_type, p.K, p.N, p.act, n_slots, max_rank, index, x_ptr, x_ld, x_rows, ids_ptr, *p._tail, bank_ptr,
             slots_ptr, y_ptr, y_ld)
     need = work_ptr = 0
@@ -355,7 +386,7 @@ def project_rows(x, projection: Projection, bank: Optional[AdapterBank] = None, 
         if need > 0:
             work = torch.empty(need, dtype=torch.uint8, device=p.device)     # of this call: the allocator keeps it until the stream has passed it
             work_ptr = work.data_ptr()
-    _check(p.lib.ripple_project_rows(_PROJECT_ARGS.pack(*head, work_ptr, need, _stream(index))))
+    _check(p.lib.ripple_project_rows(_PROJECT_ARGS.pack(*head, work_ptr, need, stream)))
     return out
 
 
@@ -378,7 +409,7 @@ class Block:
     scale: Union[float, "torch.Tensor"] = 1.0
 
 
-class RequestHead:
+class RequestHead(_Buffers):
     """A head that requests run on the cached rows of their vertices: residual blocks, a last norm, the logits' projection.
 
     The residual stream starts from the fp32 rows of the cache and stays fp32; the blocks run in the projections' type."""
@@ -389,6 +420,7 @@ class RequestHead:
         for i, b in enumerate(self.blocks):
             if b.up.N != b.down.K or b.down.N != b.up.K or b.up.dtype != b.down.dtype or b.up.dtype != logits.dtype or b.up.K != logits.K:
                 raise ValueError(f"block {i}: the widths or types of its projections do not fit")
+        self._keep(None, *(b.scale for b in self.blocks if isinstance(b.scale, torch.Tensor)))
 
     def __call__(self, table, ids, slots=None, out_dtype=torch.float32):
         """Logits [len(ids), N] of the rows `ids` (int32) of `table`, each with the adapters of its slot (without slots: of the
@@ -396,6 +428,7 @@ class RequestHead:
         def project(x, p, bank, **kw):
             return project_rows(x, p, bank, slots, **kw) if bank is not None and slots is not None else project_rows(x, p, **kw)
 
+        self._read_on(_stream(self.logits.index))
         first = self.blocks[0].pre if self.blocks else self.norm
         _, n = norm_rows(residual=table, ids=ids, pre=first, normed_dtype=self.logits.dtype)
         s, at = table, ids

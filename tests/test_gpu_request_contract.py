@@ -182,3 +182,33 @@ def test_operators_keep_copies_of_their_weights():
     for t in (w, b, W, bias):
         t.zero_()
     assert torch.equal(serve.norm_rows(x, pre=n)[1], want[0]) and torch.equal(serve.project_rows(x, p), want[1])
+
+
+# ---- buffers of operators that are dropped while they are read
+def test_an_operator_may_be_dropped_while_it_is_read():
+    """Its buffers go back to the allocator when the streams that read them have passed the calls, not before."""
+    g = gen(37)
+    x, of = rnd(g, 64, 128), torch.zeros(64, dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    for kind in ("norm", "projection", "bank", "scale of a block"):
+        n = serve.Norm(serve.NORM_LAYER, rnd(g, 128), rnd(g, 128))
+        p = serve.Projection(rnd(g, 128, 1000), rnd(g, 1000))
+        bank = serve.AdapterBank(p, 8, 16)
+        scale = rnd(g, 128)
+        head = serve.RequestHead([serve.Block(n, p, serve.Projection(rnd(g, 1000, 128)), scale=scale)], n, serve.Projection(rnd(g, 128, 9)))
+        call = {"norm": lambda: serve.norm_rows(x, pre=n), "scale of a block": lambda: head(x, of)}.get(kind, lambda: serve.project_rows(x, p, bank, of))
+        call()                                              # (kernels are loaded at their first use)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(200_000_000)                  # a tenth of a second of work before the call
+            call()
+        kept = {"norm": lambda: [n.weight, n.bias], "projection": lambda: [p.layout, p.bias], "bank": lambda: [bank.buffer],
+                "scale of a block": lambda: [scale]}[kind]()
+        places = [(t.data_ptr(), t.numel(), t.dtype) for t in kept]
+        done = torch.cuda.Event()
+        done.record(side)
+        del kept, call, n, p, bank, scale, head
+        again = [torch.empty(size, dtype=dtype, device="cuda").data_ptr() for _, size, dtype in places]     # (nothing is written there)
+        assert not done.query(), "the call was over before it could be looked at"
+        assert not set(again) & {at for at, _, _ in places}
+        torch.cuda.synchronize()
