@@ -15,7 +15,7 @@ and every captured graph has its own.  Operators (Norm, Projection, AdapterBank,
 are in flight, on whatever stream; tensors of the caller follow PyTorch's rule (`Tensor.record_stream`), and a captured graph reads
 both as long as it is replayed.  Rows whose id lies outside the table (a negative id marks padding) are not
 written: they keep what `out` holds.  Rows are fp32, bf16 or fp16; sums and statistics are fp32.  The library infers: inputs that
-require gradients are refused while gradients are recorded.
+require gradients are refused while gradients are recorded, and inputs that carry tangents always.
 """
 from __future__ import annotations
 
@@ -26,6 +26,7 @@ from typing import List, Optional, Sequence, Tuple, Union
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from . import ripple as _ripple
 from .ripple import ACT_IDENTITY, ACT_RELU, OK, RippleError
@@ -64,6 +65,13 @@ def _refuse(t, name: str, index: int):
     if index >= 0 and t.get_device() != index:
         raise ValueError(f"{name} is on {t.device}, the other tensors on cuda:{index}")
     raise ValueError(f"{name} requires gradients, which these operators do not form: call them under torch.no_grad()")
+
+
+def _refuse_tangents(**tensors) -> None:
+    """Within a level of forward-mode differentiation: no input may carry a tangent, which would be dropped."""
+    for name, t in tensors.items():
+        if isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError(f"{name} carries a tangent, which these operators do not form")
 
 
 def _device_of(t, name: str) -> int:
@@ -187,6 +195,8 @@ def norm_rows(y=None, *, post: Optional[Norm] = None, gate=None, gate_act: int =
     or residual if there are no ids, but overlap no input otherwise."""
     if y is None and residual is None:
         raise ValueError("neither y nor residual")
+    if getattr(forward_ad, "_current_level", 0) >= 0:
+        _refuse_tangents(y=y, gate=gate, scale=scale, residual=residual, out=out, normed_out=normed_out)
     first, name = (y, "y") if y is not None else (residual, "residual")
     index = _device_of(first, name)
     ptr, ld, rows = _matrix(first, name, None, None, index)
@@ -343,6 +353,8 @@ def project_rows(x, projection: Projection, bank: Optional[AdapterBank] = None, 
     one slot side by side are fastest."""
     p = projection
     index = p.index
+    if getattr(forward_ad, "_current_level", 0) >= 0:
+        _refuse_tangents(x=x, out=out)
     x_ptr, x_ld, x_rows = _matrix(x, "x", p.K, p.dtype, index)
     rows, ids_ptr, bank_ptr, slots_ptr, n_slots, max_rank = x_rows, 0, 0, 0, 0, 0
     if ids is not None:

@@ -212,3 +212,20 @@ def test_an_operator_may_be_dropped_while_it_is_read():
         assert not done.query(), "the call was over before it could be looked at"
         assert not set(again) & {at for at, _, _ in places}
         torch.cuda.synchronize()
+
+
+# ---- tangents
+def test_tangents_are_refused():
+    import torch.autograd.forward_ad as fw
+    g = gen(36)
+    x, r = rnd(g, 4, 8), rnd(g, 4, 8)
+    p, ids = serve.Projection(rnd(g, 8, 6)), torch.arange(4, device="cuda", dtype=torch.int32)
+    with fw.dual_level():
+        d = fw.make_dual(x, torch.ones_like(x))
+        for call in (lambda: serve.norm_rows(d), lambda: serve.norm_rows(x, residual=d), lambda: serve.norm_rows(x, gate=d),
+                     lambda: serve.norm_rows(x, scale=fw.make_dual(x[0].clone(), x[0].clone())), lambda: serve.norm_rows(residual=d, ids=ids),
+                     lambda: serve.project_rows(d, p), lambda: serve.norm_rows(x, out=d)):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        serve.norm_rows(x, residual=r), serve.project_rows(x, p)       # (others are as they were)
+    serve.norm_rows(d.detach())
