@@ -1469,7 +1469,7 @@ extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) 
     if (a->act != RIPPLE_ACT_IDENTITY && a->act != RIPPLE_ACT_RELU) REFUSE("project_rows: unknown activation");
     const int size = type_size(a->type), out_size = type_size(a->out_type);
     if (a->rows == 0) return RIPPLE_OK;
-    if (!a->x || !a->layout || !a->y) REFUSE("project_rows: null pointer");
+    if ((!a->x && a->x_rows != 0) || !a->layout || !a->y) REFUSE("project_rows: null pointer");
     if (!aligned(a->x, size) || !aligned(a->y, out_size) || !aligned(a->layout, 128) || !aligned(a->bias, 4) || !aligned(a->ids, 4) || !aligned(a->slots, 4) || !aligned(a->bank, 128))
         REFUSE("project_rows: misaligned pointer");
     if (a->ld_x < 0 || a->ld_y < a->n) REFUSE("project_rows: leading dimension out of range");

@@ -261,7 +261,7 @@ def norm_rows(y=None, *, post: Optional[Norm] = None, gate=None, gate_act: int =
     stream = _stream(index)
     post_args = _NO_NORM if post is None else post._packed(width, index, stream, "post")
     pre_args = _NO_NORM if pre is None else pre._packed(width, index, stream, "pre")
-    if rows == 0:
+    if rows == 0 or (ids is not None and res_rows == 0):       # (without rows every id lies outside)
         return out, normed_out
     _check(_ripple.load_library().ripple_norm_rows(_NORM_ARGS.pack(
         rows, width, t, ts, int(gate_act), y_ptr, y_ld, gate_ptr, gate_ld, res_ptr, res_ld, res_rows, ids_ptr, vec_ptr,
@@ -381,7 +381,7 @@ def project_rows(x, projection: Projection, bank: Optional[AdapterBank] = None, 
     out_type = p.type if out.dtype == p.dtype else _type_of(out.dtype, "out")
     if out_type not in (p.type, TYPE_F32):
         raise TypeError(f"out: {p.dtype} or float32 expected, got {out.dtype}")
-    if rows == 0:
+    if rows == 0 or x_rows == 0:
         return out
     stream = _stream(index)
     p._read_on(stream)

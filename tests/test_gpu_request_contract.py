@@ -229,3 +229,24 @@ def test_tangents_are_refused():
                 call()
         serve.norm_rows(x, residual=r), serve.project_rows(x, p)       # (others are as they were)
     serve.norm_rows(d.detach())
+
+
+# ---- tables without rows
+def test_tables_without_rows():
+    """Every id lies outside: nothing is written."""
+    g = gen(39)
+    ids = torch.tensor([-1, 0, 5], dtype=torch.int32, device="cuda")
+    p = serve.Projection(rnd(g, 8, 6))
+    bank = serve.AdapterBank(p, 2, 4)
+    x, y = torch.empty(0, 8, device="cuda"), rnd(g, 3, 8)
+    out = torch.full((3, 6), 7.0, device="cuda")
+    serve.project_rows(x, p, ids=ids, out=out), serve.project_rows(x, p, bank, ids, ids, out=out)
+    assert (out == 7.0).all()
+    s, n = torch.full((3, 8), 7.0, device="cuda"), torch.full((3, 8), 7.0, device="cuda")
+    rms = serve.Norm(serve.NORM_RMS)
+    serve.norm_rows(y, residual=x, ids=ids, out=s, pre=rms, normed_out=n), serve.norm_rows(residual=x, ids=ids, out=s, pre=rms, normed_out=n)
+    assert (s == 7.0).all() and (n == 7.0).all()
+    with pytest.raises(ValueError):
+        serve.norm_rows(y, residual=x)
+    with pytest.raises(ValueError):
+        serve.norm_rows(y, ids=ids)

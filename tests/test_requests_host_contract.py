@@ -1,0 +1,19 @@
+"""What the calls of requests promise that needs no device to be seen."""
+import pytest
+
+from paper_2601_12347_b200 import ripple
+
+import test_requests_host as H
+
+lib = H.lib
+
+
+@H.no_device
+@pytest.mark.parametrize("x", [0, 1 << 24])
+@pytest.mark.parametrize("adapters", [True, False])
+def test_a_table_without_rows_has_no_address(lib, x, adapters):
+    """Every id lies outside: the call is fine and launches nothing, whatever the address of nothing is."""
+    kw = {} if adapters else dict(bank=0, slots=0)
+    assert lib.ripple_project_rows(H._project_args(x=x, x_rows=0, ids=8 << 24, **kw)) == ripple.OK
+    assert lib.ripple_project_rows(H._project_args(x=x, x_rows=0, **kw)) == ripple.ERR_INVALID_ARG      # rows without ids
+    assert lib.ripple_project_rows(H._project_args(x=0, x_rows=4, ids=8 << 24, **kw)) == ripple.ERR_INVALID_ARG
