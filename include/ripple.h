@@ -366,7 +366,7 @@ ripple_status ripple_probe_gather_rate(int32_t device, int64_t n_rows, int32_t r
  * leading dimension in elements (inputs: any >= 0, outputs: >= width).  Text of an error: ripple_last_error(NULL).
  *
  * ids: NULL, or for every row of the call the row of the table that it reads.  An id outside the table (a negative
- * one marks a padding row) leaves that row of every output as it was. */
+ * one marks a padding row) leaves that row of every output as it was, unless the call says otherwise. */
 typedef enum { RIPPLE_TYPE_F32 = 0, RIPPLE_TYPE_BF16 = 1, RIPPLE_TYPE_F16 = 2 } ripple_type;
 typedef enum { RIPPLE_NORM_NONE = 0, RIPPLE_NORM_LAYER = 1, RIPPLE_NORM_RMS = 2 } ripple_norm_kind;
 typedef enum { RIPPLE_GATE_IDENTITY = 0, RIPPLE_GATE_SIGMOID = 1, RIPPLE_GATE_SILU = 2, RIPPLE_GATE_TANH = 3 } ripple_gate_act;
@@ -406,7 +406,10 @@ typedef struct {
     float scale;
     int32_t gate_width;       /* 1 (one gate per row) or `width`                                                 */
     int32_t device;           /* CUDA device ordinal of the pointers, or -1 for the current device               */
-    int32_t reserved;
+    union {
+        int32_t clear_padding;/* 1: padding rows of the outputs become zeros instead of staying as they were     */
+        int32_t reserved;     /* (its former name)                                                               */
+    };
     void* cuda_stream;        /* cudaStream_t                                                                    */
 } ripple_norm_rows_args;
 

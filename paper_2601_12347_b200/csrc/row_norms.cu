@@ -31,7 +31,7 @@ struct NormParams {
     int64_t ld_y, ld_gate, ld_residual, ld_stream, ld_normed, residual_rows;
     ripple_norm post, pre;
     float scale;
-    int gate_act, gate_width;
+    int gate_act, gate_width, clear_padding;
     int warps_per_row;
     int y_bytes, residual_bytes, stage_bytes, stages;   // of a row in the ring; rows in it
 };
@@ -360,6 +360,22 @@ __global__ void __launch_bounds__(MULTI ? (NP * V > 16 ? 512 : 256) : 128) k_nor
     if constexpr (RING) asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
+// Zeros in the padding rows, for calls that ask for them: a warp looks at 32 ids and clears what they leave out.  (A kernel of its own: in
+// k_norm_rows, in or behind its loop, these stores cost all calls 2 to 5 %, by the registers they change.)
+template <typename T, typename TR>
+__global__ void __launch_bounds__(256) k_clear_padding(const __grid_constant__ NormParams p) {
+    pdl_enter();
+    const int64_t first = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * 32;
+    const int64_t from = first + lane_id() < p.rows ? p.ids[first + lane_id()] : 0;
+    for (uint32_t left = __ballot_sync(FULL, first + lane_id() < p.rows && (from < 0 || from >= p.residual_rows)); left; left &= left - 1) {
+        const int64_t row = first + __ffs(left) - 1;
+        for (int c = lane_id(); c < p.width; c += 32) {
+            if (p.clear_padding & 1) static_cast<TR*>(p.stream)[row * p.ld_stream + c] = from_f32<TR>(0.f);
+            if (p.clear_padding & 2) static_cast<T*>(p.normed)[row * p.ld_normed + c] = from_f32<T>(0.f);
+        }
+    }
+}
+
 template <typename T, typename TR, int V, int E, bool MULTI, bool RING>
 static cudaError_t launch_norm(NormParams p, int warps, void* stream) {
     auto* const kernel = k_norm_rows<T, TR, V, E / V, MULTI, RING>;
@@ -396,6 +412,10 @@ static cudaError_t launch_norm(const NormParams& p, void* stream) {
 template <typename T, typename TR>
 static cudaError_t launch_norm(NormParams p, int v, void* stream) {
     constexpr int WIDE = 16 / sizeof(T);
+    if (p.clear_padding && p.ids) {
+        const cudaError_t e = launch(k_clear_padding<T, TR>, dim3((unsigned)((p.rows + 255LL) / 256)), 256, 0, stream, p);
+        if (e != cudaSuccess) return e;
+    }
     auto up16 = [](int64_t x) { return (int)((x + 15) / 16 * 16); };
     p.y_bytes = up16(p.width * (int64_t)sizeof(T)), p.residual_bytes = up16(p.width * (int64_t)sizeof(TR));
     p.stage_bytes = (p.y ? p.y_bytes : 0) + (p.residual ? p.residual_bytes : 0) + (p.gate && p.gate_width != 1 ? p.y_bytes : 0);
@@ -432,6 +452,7 @@ extern "C" ripple_status ripple_norm_rows(const ripple_norm_rows_args* a) {
     if (a->ids && !a->residual) REFUSE("ids without residual");
     if (a->residual && (a->residual_rows < 0 || (!a->ids && a->residual_rows < a->rows))) REFUSE("fewer residual rows than rows");
     if (!a->stream && !a->normed) REFUSE("no output");
+    if (a->clear_padding < 0 || a->clear_padding > 1) REFUSE("clear_padding must be 0 or 1");
     if ((a->normed != nullptr) != (a->pre.kind != RIPPLE_NORM_NONE)) REFUSE("normed and pre go together");
     if (a->ld_y < 0 || a->ld_gate < 0 || a->ld_residual < 0) REFUSE("negative leading dimension");
     if ((a->stream && a->ld_stream < a->width) || (a->normed && a->ld_normed < a->width)) REFUSE("leading dimension of an output below its width");
@@ -477,6 +498,7 @@ extern "C" ripple_status ripple_norm_rows(const ripple_norm_rows_args* a) {
     p.residual_rows = a->residual_rows;
     p.post = a->post, p.pre = a->pre;
     p.scale = a->scale, p.gate_act = a->gate_act, p.gate_width = a->gate_width;
+    p.clear_padding = a->clear_padding ? (a->stream ? 1 : 0) | (a->normed ? 2 : 0) : 0;
     cudaError_t e;
     const bool mixed = a->stream_type != a->type;
     switch (a->type) {

@@ -442,8 +442,8 @@ class Ripple:
     def answer(self, head, ids, slots=None, layer: Optional[int] = None):
         """Request-based inference: what `head` (serve.RequestHead) makes of the rows `ids` (CUDA int32) of H^layer (default:
         the last), each with the adapters of its slot.  Runs on the current stream of the context's device and does not wait for it; the
-        context's next call waits on the device until the rows have been read.  An id out of range leaves its row of the
-        result undefined.  While a graph is captured nothing is ordered: replay it between the context's calls.
+        context's next call waits on the device until the rows have been read.  The row of an id out of range
+        holds what the head makes of zeros.  While a graph is captured nothing is ordered: replay it between the context's calls.
         Like all calls of requests it returns before its kernels have run: `serve.check_requests` waits for them and raises if one of
         their bounded waits gave up."""
         got = head(self.embeddings(self.L if layer is None else layer), ids, slots)

@@ -14,7 +14,7 @@ before, and its results are not to be used: `check_requests`, where a program wa
 and every captured graph has its own.  Operators (Norm, Projection, AdapterBank, RequestHead) may be dropped while calls that read them
 are in flight, on whatever stream; tensors of the caller follow PyTorch's rule (`Tensor.record_stream`), and a captured graph reads
 both as long as it is replayed.  Rows whose id lies outside the table (a negative id marks padding) are not
-written: they keep what `out` holds.  Rows are fp32, bf16 or fp16; sums and statistics are fp32.  The library infers: inputs that
+written: they keep what `out` holds, and without `out` what the memory of the result held (a RequestHead's hold what it makes of zeros).  Rows are fp32, bf16 or fp16; sums and statistics are fp32.  The library infers: inputs that
 require gradients are refused while gradients are recorded, and inputs that carry tangents always.
 """
 from __future__ import annotations
@@ -185,14 +185,14 @@ _NO_NORM = (NORM_NONE, 0.0, 0, 0)
 
 
 def norm_rows(y=None, *, post: Optional[Norm] = None, gate=None, gate_act: int = GATE_IDENTITY, scale=1.0,
-              residual=None, ids=None, pre: Optional[Norm] = None, normed_dtype=None, out=None, normed_out=None):
+              residual=None, ids=None, pre: Optional[Norm] = None, normed_dtype=None, out=None, normed_out=None, clear_padding: bool = False):
     """(s, n):  s = residual[ids] + scale * act(gate) * post(y),  n = pre(s);  n is None without `pre`.
 
     y [rows, D]: a block's output; without it s = residual[ids], which is returned only if `out` or no `pre` is given.
     gate [rows, D] or [rows, 1], of y's type; scale: a number, or an fp32 vector [D].
     residual [any, D]: y's type or fp32; row ids[i] (int32) of it, or row i, goes to row i; without it s = scale * ...
     s has residual's type, n y's (without y: normed_dtype, or residual's).  out / normed_out: where to write s / n; they may be y,
-    or residual if there are no ids, but overlap no input otherwise."""
+    or residual if there are no ids, but overlap no input otherwise.  clear_padding: the rows of ids outside the residual become zeros."""
     if y is None and residual is None:
         raise ValueError("neither y nor residual")
     if getattr(forward_ad, "_current_level", 0) >= 0:
@@ -262,10 +262,13 @@ def norm_rows(y=None, *, post: Optional[Norm] = None, gate=None, gate_act: int =
     post_args = _NO_NORM if post is None else post._packed(width, index, stream, "post")
     pre_args = _NO_NORM if pre is None else pre._packed(width, index, stream, "pre")
     if rows == 0 or (ids is not None and res_rows == 0):       # (without rows every id lies outside)
+        for t in (out, normed_out):
+            if clear_padding and t is not None:
+                t.zero_()
         return out, normed_out
     _check(_ripple.load_library().ripple_norm_rows(_NORM_ARGS.pack(
         rows, width, t, ts, int(gate_act), y_ptr, y_ld, gate_ptr, gate_ld, res_ptr, res_ld, res_rows, ids_ptr, vec_ptr,
-        out_ptr, out_ld, n_ptr, n_ld, *post_args, *pre_args, number, gate_width, index, 0, stream)))
+        out_ptr, out_ld, n_ptr, n_ld, *post_args, *pre_args, number, gate_width, index, bool(clear_padding), stream)))
     return out, normed_out
 
 
@@ -436,17 +439,17 @@ class RequestHead(_Buffers):
 
     def __call__(self, table, ids, slots=None, out_dtype=torch.float32):
         """Logits [len(ids), N] of the rows `ids` (int32) of `table`, each with the adapters of its slot (without slots: of the
-        shared projections alone)."""
+        shared projections alone).  A row whose id lies outside the table enters every norm that gathers as zeros."""
         def project(x, p, bank, **kw):
             return project_rows(x, p, bank, slots, **kw) if bank is not None and slots is not None else project_rows(x, p, **kw)
 
         self._read_on(_stream(self.logits.index))
         first = self.blocks[0].pre if self.blocks else self.norm
-        _, n = norm_rows(residual=table, ids=ids, pre=first, normed_dtype=self.logits.dtype)
+        _, n = norm_rows(residual=table, ids=ids, pre=first, normed_dtype=self.logits.dtype, clear_padding=True)
         s, at = table, ids
         for i, b in enumerate(self.blocks):
             y = project(project(n, b.up, b.up_bank), b.down, b.down_bank)
             following = self.blocks[i + 1].pre if i + 1 < len(self.blocks) else self.norm
-            s, n = norm_rows(y, post=b.post, scale=b.scale, residual=s, ids=at, pre=following)
+            s, n = norm_rows(y, post=b.post, scale=b.scale, residual=s, ids=at, pre=following, clear_padding=True)
             at = None
         return project(n, self.logits, self.logits_bank, out_dtype=out_dtype)

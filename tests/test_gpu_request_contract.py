@@ -250,3 +250,65 @@ def test_tables_without_rows():
         serve.norm_rows(y, residual=x)
     with pytest.raises(ValueError):
         serve.norm_rows(y, ids=ids)
+
+
+# ---- padding rows
+@pytest.mark.parametrize("dtype,res", [("fp32", "fp32"), ("bf16", "fp32"), ("fp16", "fp16")])
+@pytest.mark.parametrize("width", [8, 47, 602, 1500, 5000])
+def test_padding_rows_of_norms_are_cleared_where_that_is_asked_for(dtype, res, width):
+    g = gen(41)
+    T, S = R.DTYPES[dtype], R.DTYPES[res]
+    rms = serve.Norm(serve.NORM_RMS)
+    for rows in (1, 31, 2000):
+        y, table = rnd(g, rows, width, dtype=T), rnd(g, 10, width, dtype=S)
+        ids = torch.randint(-3, 13, (rows,), generator=g, device="cuda", dtype=torch.int32)
+        pad = (ids < 0) | (ids >= 10)
+        for at in (0, 1):                           # outputs of their own, and columns of wider ones (which go another way)
+            got = []
+            for clear in (False, True):
+                out, normed = torch.full((rows, width + 3 * at), 7.0, dtype=S, device="cuda"), torch.full((rows, width + 5 * at), 7.0, dtype=T, device="cuda")
+                s, n = serve.norm_rows(y, residual=table, ids=ids, pre=rms, out=out[:, at:width + at], normed_out=normed[:, 2 * at:width + 2 * at], clear_padding=clear)
+                got.append((s[~pad], n[~pad]))
+                assert (s[pad] == (0.0 if clear else 7.0)).all() and (n[pad] == (0.0 if clear else 7.0)).all()
+                assert (out[:, :at] == 7.0).all() and (out[:, width + at:] == 7.0).all() and (normed[:, :2 * at] == 7.0).all() and (normed[:, width + 2 * at:] == 7.0).all()
+            assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+        _, n = serve.norm_rows(residual=table, ids=ids, pre=rms, normed_dtype=T, clear_padding=True)
+        assert (n[pad] == 0.0).all()
+        s, n = serve.norm_rows(y, residual=table[:0], ids=ids, pre=rms, clear_padding=True)
+        assert (s == 0).all() and (n == 0).all()
+        s, _ = serve.norm_rows(y, pre=rms, clear_padding=True)                    # (no ids: nothing is padding)
+        assert torch.equal(s, y)
+
+
+@pytest.mark.parametrize("blocks", [0, 2])
+@pytest.mark.parametrize("rows", [6, 3000])
+def test_padding_rows_of_an_answer_hold_no_old_memory(blocks, rows):
+    g = gen(38)
+    head, ups, downs, logits = R.make_head(g, 48, 96, 11, torch.bfloat16)
+    head = serve.RequestHead(head.blocks[:blocks], head.norm, head.logits, head.logits_bank)
+    table = rnd(g, 100, 48)
+    ids, of = torch.randint(0, 100, (rows,), generator=g, device="cuda", dtype=torch.int32), runs(gen(1), rows, 3, 6)
+    want = head(table, ids, of)
+    bad = ids.clone()
+    bad[1::5], bad[3::5] = -1, 100
+    bad[0], bad[2] = 2 ** 31 - 1, -2 ** 31
+    pad = bad != ids
+    for x in (float("nan"), 1e3):
+        junk = [torch.full((rows, w), x, device="cuda") for w in (24, 48, 96, 11)]      # what the allocator will hand out again
+        del junk
+        got = head(table, bad, of)
+        assert torch.equal(got[~pad], want[~pad])
+        # zeros behind the norms that gather: the first, and the one that ends the first block
+        s = torch.zeros(rows, 48, dtype=F64, device="cuda")
+        n = s
+        for i in range(1, blocks):
+            b = head.blocks[i]
+            h, _ = ups[i].want(n, of)
+            y, _ = downs[i].want(h, of if b.down_bank is not None else None)
+            s = s + (b.scale.to(F64) if isinstance(b.scale, torch.Tensor) else b.scale) * R.norm_of(y, torch.zeros_like(y), b.post)[0]
+            n = R.norm_of(s, torch.zeros_like(s), head.norm)[0]
+        # (bf16: bounds as for a head's other rows)
+        zero = logits.want(n, of)[0]
+        assert float((got[pad].to(F64) - zero[pad]).norm()) <= 2.0 ** -8 * 4 * float(zero[pad].norm())
+    got = head(table[:0], bad, of)
+    assert float((got.to(F64) - zero).norm()) <= 2.0 ** -8 * 4 * float(zero.norm())

@@ -9,6 +9,13 @@ lib = H.lib
 
 
 @H.no_device
+@pytest.mark.parametrize("clear", [-1, 2, 1 << 20])
+def test_unknown_treatments_of_padding_rows_are_refused(lib, clear):
+    assert lib.ripple_norm_rows(H._norm_args(reserved=clear)) == ripple.ERR_INVALID_ARG
+    assert b"clear_padding" in lib.ripple_last_error(None)
+
+
+@H.no_device
 @pytest.mark.parametrize("x", [0, 1 << 24])
 @pytest.mark.parametrize("adapters", [True, False])
 def test_a_table_without_rows_has_no_address(lib, x, adapters):
