@@ -312,3 +312,28 @@ def test_padding_rows_of_an_answer_hold_no_old_memory(blocks, rows):
         assert float((got[pad].to(F64) - zero[pad]).norm()) <= 2.0 ** -8 * 4 * float(zero[pad].norm())
     got = head(table[:0], bad, of)
     assert float((got.to(F64) - zero).norm()) <= 2.0 ** -8 * 4 * float(zero.norm())
+
+
+# ---- answers beside batches
+def test_a_batch_waits_for_an_answer_on_another_stream(env):
+    ripple, _ = env
+    g = gen(40)
+    model = I.sage_model([20, 64, 48])
+    n = 4000
+    src, dst = I.er_graph(n, 4 * n, 3)
+    rp = ripple.Ripple(n, src, dst, I.features(n, 20, 3), model, I.make_weights(model, 3))
+    head, *_ = R.make_head(g, 48, 96, 11, torch.float32)
+    ids = torch.arange(n, dtype=torch.int32, device="cuda")
+    stream, side = I.UpdateStream(n, src, dst, 20, 3), torch.cuda.Stream()
+    for _ in range(3):
+        want = rp.answer(head, ids)
+        ups, feats = stream.next_batch(300)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)              # the answer's rows are read long after the batch was asked for
+            got = rp.answer(head, ids)
+        rp.apply_batch(ups, feats)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        assert not torch.equal(rp.answer(head, ids), want)
+    rp.close()
