@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ Proj
 
 // Few rows: 16 rows x 32 columns of y per block.  A lane is a column, a warp an eighth of every 256 entries of K; what the warps
 // have summed meets in shared memory, where each finishes two rows: t_i B_a, bias, activation.  Sums in fp32 throughout.
-// Latency is all that counts here: 32 entries of W per lane and 16 of the rows per thread are always on their way, those of the next
+// Latency is all that counts here (which calls take this form: few_form): 32 entries of W per lane and 16 of the rows per thread are always on their way, those of the next
 // 256 entries while these are multiplied.  64 rows, 256 -> 256: 4.1 us alone, 6.2 with 64 adapters of rank 16; 1000 rows, 602 -> 41: 8.8 and
 // 13.6.  (The tensor-core form: 5.8 and 25, 21 and 37.)
 constexpr int PF_ROWS = 16, PF_COLS = 32, PF_K = 256, PF_LD = 20;
@@ -499,9 +499,8 @@ constexpr int PJ_EPI_WARPS = 8;          // two per quarter of the lanes
 // on the tensor cores: bf16 602 -> 41, 2000 rows 23 / 32, 4000 rows 27 / 35; 1024 -> 512, 3000 rows 21 / 24, 4000 rows 27 / 25;
 // fp32 256 -> 256, 3000 rows 24 / 27, 4000 rows 26 / 27; 128 -> 1024, 4000 rows 30 / 29.
 constexpr int PJ_FEW = 3000;
-// Blocks (16 rows x 32 columns) up to which y is computed by k_project_few.  Both sides, few / tensor cores: bf16 256 -> 256, 200 blocks
-// 10.5 / 8.9, 104 blocks 6.2 / 8.7; 602 -> 41, 126 blocks 14 / 21; fp32 602 -> 41, 188 blocks 22 / 42, 314 blocks 32 / 42, 500 blocks
-// 45 / 43; 256 -> 256, 200 blocks 10.8 / 12.4, 504 blocks 20 / 14.
+constexpr int PJ_SMS = 148;              // of a B200 (for rules that are asked where no device is current, too)
+// Blocks (16 rows x 32 columns) up to which y is computed by k_project_few: few_form.
 constexpr int PF_MOST = 160, PF_MOST_F32 = 320;
 constexpr int PJ_T_COLS = 64;            // ranks of adapters side by side, where t is computed on the tensor cores
 constexpr int PJ_UNIT = 4;               // fp32: chunks (256 entries of K) whose large products share an accumulator
@@ -1299,25 +1298,41 @@ static cudaError_t project_tiles(const ProjectParams& p, void* stream) {
     return project_tiles<TYPE, BN, MODE, false>(p, stream);
 }
 
-static int64_t few_blocks(int64_t rows, int n) { return (rows + PF_ROWS - 1) / PF_ROWS * ((n + PF_COLS - 1) / PF_COLS); }
+// Whether y is computed by k_project_few.  A block takes one round over K per 256 entries and blocks come in waves, so what decides is the
+// number of blocks and, beyond three rounds, K.  Both sides, few / tensor cores, us:
+//   16 bits:  256 -> 256 104 blocks 6.2 / 8.7, 200 blocks 10.5 / 8.9;  602 -> 41, 126 blocks 14 / 21;  rows that 16 bytes divide, one wave: K = 768
+//             9.5 / 7.0, with adapters 11.5 / 11.6;  1024 12.5 / 8.0, with 14.5 / 12.2;  8192 87 / 39, with 91 / 52;  rows that they do not: 1001
+//             12.3 / 16.6, with 14.4 / 22.4;  8191 88 / 98, with 93 / 114
+//   fp32:     602 -> 41, 188 blocks 22 / 42, 314 blocks 32 / 42, 500 blocks 45 / 43;  256 -> 256, 200 blocks 10.8 / 12.4, 504 blocks 20 / 14;  one wave:
+//             1024 10.9 / 18.4;  8192 72 / 122;  two waves: 1024 20.5 / 18.6, with adapters 25.8 / 27.4;  8192 140 / 123, with 156 / 162;  1001 20.9 / 25.5;
+//             three waves: 2048 55 / 34, with 64 / 48
+static bool few_form(int type, int64_t rows, int k, int n, bool adapters, bool aligned) {
+    const int64_t blocks = (rows + PF_ROWS - 1) / PF_ROWS * ((n + PF_COLS - 1) / PF_COLS);
+    const bool deep = k > 3 * PF_K;
+    if (type != RIPPLE_TYPE_F32) return blocks <= PF_MOST && !(deep && aligned);
+    return blocks <= (!deep ? PF_MOST_F32 : adapters || !aligned ? 2 * PJ_SMS : PJ_SMS);
+}
 
-// Tiles of 32 columns where those of 128 would leave most SMs without one; of 256 (16-bit rows) where those leave none
-// (project of 65 536 x 1024 x 1024: 128 columns 200 us, 256 columns 125).
+// Tiles of 32 columns where that makes no more than one per SM: less to wait for in each.  A second one costs as much again, and then
+// tiles of 128 do.  Both sides, 32 / 128 columns, us: bf16 1024 -> 512, 128 tiles of 32 8.3 / 9.3, 192 13.1 / 9.4; 8192 -> 130, 120 tiles 41 / 46, 160
+// 76 / 47; 256 -> 256, 128 tiles 4.7 / 5.5, 192 6.2 / 5.6; fp32 1024 -> 512, 128 tiles 20 / 24, 192 36 / 24; with 32 adapters of rank 16 bf16 256 -> 256,
+// 128 tiles 12.1 / 13.0, 192 18.9 / 15.8; fp32 2048 -> 300, 120 tiles 57 / 61, 160 90 / 64.
+// Of 256 (16-bit rows) where those leave no SM without one (65 536 x 1024 x 1024: 128 columns 200 us, 256 columns 125).
 template <int TYPE, int MODE>
 static cudaError_t project_columns(const ProjectParams& p, void* stream) {
     const int row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
-    const int64_t wide = (int64_t)((p.n + 127) / 128) * row_tiles;
     if constexpr (TYPE != RIPPLE_TYPE_F32) {
         if (p.n > 128 && (int64_t)((p.n + 255) / 256) * row_tiles >= sm_count()) return project_tiles<TYPE, 256, MODE>(p, stream);
     }
-    return wide >= sm_count() / 2 ? project_tiles<TYPE, 128, MODE>(p, stream) : project_tiles<TYPE, 32, MODE>(p, stream);
+    return (int64_t)((p.n + 31) / 32) * row_tiles <= PJ_SMS ? project_tiles<TYPE, 32, MODE>(p, stream) : project_tiles<TYPE, 128, MODE>(p, stream);
 }
 
 template <int TYPE>
 static cudaError_t project(ProjectParams p, void* stream) {
     constexpr bool F32 = TYPE == RIPPLE_TYPE_F32;
     const int row_tiles = (p.rows + PJ_ROWS - 1) / PJ_ROWS;
-    const bool few = few_blocks(p.rows, p.n) <= (F32 ? PF_MOST_F32 : PF_MOST);
+    const bool aligned = (reinterpret_cast<uintptr_t>(p.x) & 15) == 0 && p.ld_x * type_size(TYPE) % 16 == 0;
+    const bool few = few_form(TYPE, p.rows, p.k, p.n, p.bank.info != nullptr, aligned);
     cudaError_t e = cudaSuccess;
     if (p.bank.info) {
         // fp32, narrow: x W and t in one pass over the rows, whose parts are what takes the time (200 000 rows, 256 -> 47, rank 16: 173 us in
@@ -1448,7 +1463,7 @@ extern "C" ripple_status ripple_adapter_set(void* bank, int32_t type, int32_t k,
 }
 
 static bool pj_joined(const ripple_project_rows_args* a) {
-    return a->bank && a->type == RIPPLE_TYPE_F32 && a->rows > PJ_FEW && few_blocks(a->rows, a->n) > PF_MOST_F32 && a->n <= 128 - PJ_T_COLS;
+    return a->bank && a->type == RIPPLE_TYPE_F32 && a->rows > PJ_FEW && !few_form(a->type, a->rows, a->k, a->n, true, true) && a->n <= 128 - PJ_T_COLS;
 }
 
 // t: fp32, or up to three bf16 parts (what of it a call needs depends on the result's type, its size does not)

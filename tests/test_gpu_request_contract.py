@@ -337,3 +337,19 @@ def test_a_batch_waits_for_an_answer_on_another_stream(env):
         assert torch.equal(got, want)
         assert not torch.equal(rp.answer(head, ids), want)
     rp.close()
+
+
+# ---- the forms' edges
+@pytest.mark.parametrize("dtype", list(R.DTYPES))
+@pytest.mark.parametrize("K,N,rows", [
+    (768, 20, 700), (769, 20, 700), (776, 33, 1184), (776, 33, 1185), (776, 33, 2368), (776, 33, 2369),    # three rounds over K; one and two waves
+    (776, 20, 4736), (776, 20, 4737), (128, 20, 5120), (128, 20, 5121),                                    # (fp32: or x W and x A in one pass)
+    (64, 512, 1152), (64, 512, 1153), (64, 1184, 512), (64, 1185, 512),                          # one tile of 32 columns per SM, and more
+])
+def test_rows_at_the_edges_of_the_rules(dtype, K, N, rows):
+    g = gen(K + N + rows)
+    t = R.Tenants(g, K, N, R.DTYPES[dtype], slots=12, max_rank=20, act=serve.ACT_RELU)
+    wide = rnd(g, rows, K + 8, dtype=R.DTYPES[dtype])
+    for x in (wide[:, :K].contiguous(), wide[:, 1:K + 1], wide[:, 8:]):        # (aligned or not, by K and the first column)
+        t.check(x)
+        t.check(x, runs(g, rows, 9, 12))
