@@ -142,6 +142,15 @@ class _Buffers:
         self._tensors = tensors
         self._streams = set() if index is None else {_stream(index)}
 
+    # (A deep copy or a pickled one would hold the addresses of this one's memory and not keep it.)
+    def __reduce_ex__(self, protocol):
+        raise TypeError(f"a {type(self).__name__} holds device memory and cannot be copied or pickled: make another from its weights")
+
+    def __copy__(self):
+        other = object.__new__(type(self))
+        other.__dict__.update(self.__dict__)
+        return other
+
     def _read_on(self, stream: int):
         if stream in self._streams:
             return
