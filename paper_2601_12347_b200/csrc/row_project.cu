@@ -376,9 +376,9 @@ __global__ void __launch_bounds__(128) k_shrink_few(const __grid_constant__ Proj
 
 // Few rows: 16 rows x 32 columns of y per block.  A lane is a column, a warp an eighth of every 256 entries of K; what the warps
 // have summed meets in shared memory, where each finishes two rows: t_i B_a, bias, activation.  Sums in fp32 throughout.
-// Latency is all that counts here (which calls take this form: few_form): 32 entries of W per lane and 16 of the rows per thread are always on their way, those of the next
-// 256 entries while these are multiplied.  64 rows, 256 -> 256: 4.1 us alone, 6.2 with 64 adapters of rank 16; 1000 rows, 602 -> 41: 8.8 and
-// 13.6.  (The tensor-core form: 5.8 and 25, 21 and 37.)
+// Latency is all that counts here (which calls take this form: few_form): 32 entries of W per lane and 16 of the rows per thread are always on
+// their way, those of the next 256 entries while these are multiplied.  64 rows, 256 -> 256: 4.3 us alone, 6.4 with 64 adapters of rank 16; 1000
+// rows, 602 -> 41: 8.8 and 13.7.  (The tensor-core form: 5.8 and 25, 21 and 37.)
 constexpr int PF_ROWS = 16, PF_COLS = 32, PF_K = 256, PF_LD = 20;
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_project_few(const __grid_constant__ ProjectParams p) {
