@@ -482,6 +482,138 @@ ripple_status ripple_project_rows(const ripple_project_rows_args* args);
  * second or so.) */
 ripple_status ripple_request_status(int32_t device);
 
+/* ---- Training ------------------------------------------------------------------------------------------
+ * What a head is fitted with that requests then run: learned rows looked up beside the cached ones, the gradient of a norm, the loss
+ * of a linear layer over many classes, and the way back.  Everything said of requests holds: no context, the caller's device memory and
+ * stream, nothing allocated or synchronised, capturable, ids of 32 bits.  Scratch is the caller's: `workspace`, 128-byte aligned, of
+ * this call alone until it has finished on the stream, at least as long as the call's ..._workspace_bytes says (HOST; the same arguments; -1: they
+ * are out of range).  Results do not depend on timing: sums are formed in a fixed order.  Padding rows (ids or labels outside their
+ * range) are written here: zeros, and they add nothing to any gradient, whatever they hold.  Inputs and outputs share no memory, unless said. */
+
+/* out_i = scale * table[ids_i], zeros for ids outside the table.  One rounding. */
+typedef struct {
+    int64_t rows;
+    int32_t width;            /* columns, 1 .. 16384                                                             */
+    int32_t type;             /* ripple_type of the table                                                        */
+    int32_t out_type;         /* ripple_type of out: `type`, or any if the table is F32                           */
+    int32_t device;           /* CUDA device ordinal of the pointers, or -1 for the current device               */
+    const void* table;        /* table_rows x width                                                              */
+    int64_t ld_table, table_rows;
+    const int32_t* ids;       /* `rows` entries                                                                  */
+    void* out;                /* rows x width                                                                    */
+    int64_t ld_out;
+    float scale;
+    int32_t reserved;
+    void* cuda_stream;
+} ripple_lookup_rows_args;
+ripple_status ripple_lookup_rows(const ripple_lookup_rows_args* args);
+
+/* Its gradient: out[r] = scale * sum of dy_i over all i with ids_i = r, in the order of i; zeros where there is none.  accumulate: the sum
+ * is added to the rows of out that ids name (once for each row, rounded once), and no other row is touched. */
+typedef struct {
+    int64_t rows;
+    int32_t width;            /* columns, 1 .. 16384                                                             */
+    int32_t type;             /* ripple_type of dy                                                               */
+    int32_t out_type;         /* ripple_type of out: `type` or F32                                               */
+    int32_t device;
+    const void* dy;           /* rows x width                                                                    */
+    int64_t ld_dy;
+    const int32_t* ids;
+    void* out;                /* out_rows x width                                                                */
+    int64_t ld_out, out_rows;
+    float scale;
+    int32_t accumulate;
+    void* workspace;
+    int64_t workspace_bytes;
+    void* cuda_stream;
+} ripple_lookup_rows_grad_args;
+int64_t ripple_lookup_rows_grad_workspace_bytes(const ripple_lookup_rows_grad_args* args);
+ripple_status ripple_lookup_rows_grad(const ripple_lookup_rows_grad_args* args);
+
+/* The way back through n = norm(x[ids]) of ripple_norm_rows, from dn.  With x^ the normalised row (before weight and bias), d = dn * weight and
+ * means over the columns:
+ *   dx = (d - mean(d) - x^ mean(d x^)) / sqrt(var + eps) + add     (RMS: without mean(d)),   dweight = sum dn x^,  dbias = sum dn.
+ * Statistics are formed anew, in fp32, from x; dx is rounded once.  dx belongs to the call's rows (ripple_lookup_rows_grad adds rows of one id up). */
+typedef struct {
+    int64_t rows;
+    int32_t width;            /* columns, 1 .. 16384                                                             */
+    int32_t type;             /* ripple_type of dn                                                               */
+    int32_t x_type;           /* ripple_type of x, add and dx: `type` or F32                                     */
+    int32_t device;
+    const void* dn;           /* rows x width                                                                    */
+    int64_t ld_dn;
+    const void* x;            /* x_rows x width                                                                  */
+    int64_t ld_x, x_rows;     /* without ids at least `rows` rows                                                */
+    const int32_t* ids;       /* NULL: row i reads row i                                                         */
+    const void* add;          /* rows x width: a gradient that reaches x past the norm; NULL: none               */
+    int64_t ld_add;
+    void* dx;                 /* rows x width; NULL: not wanted.  May take the place of dn or add (or, without ids, x) with the same leading */
+    int64_t ld_dx;            /* dimension and type                                                              */
+    float* dweight;           /* `width` entries; NULL: not wanted                                               */
+    float* dbias;             /* the same                                                                        */
+    ripple_norm norm;         /* LAYER or RMS; its bias is not read                                              */
+    void* workspace;
+    int64_t workspace_bytes;
+    void* cuda_stream;
+} ripple_norm_rows_grad_args;
+int64_t ripple_norm_rows_grad_workspace_bytes(const ripple_norm_rows_grad_args* args);
+ripple_status ripple_norm_rows_grad(const ripple_norm_rows_grad_args* args);
+
+/* Softmax cross entropy of a linear layer over n classes:  z = x W + bias,  lse_i = log sum_c exp z_ic,  loss_i = lse_i - z_i,label (0 for
+ * labels outside [0, n)).  Neither call keeps the logits: they are formed tile by tile.  x, W, dx and dW share one type; products of fp32 are formed
+ * on the tensor cores from three bf16 parts per operand.  A bias of minus infinity takes a class out; a row with no class left has loss 0,
+ * lse minus infinity and no gradient. */
+#define RIPPLE_MAX_LOSS_K 8192
+#define RIPPLE_MAX_CLASSES 16777216
+typedef struct {
+    int64_t rows;
+    int32_t type;             /* ripple_type of x and W                                                          */
+    int32_t k, n;             /* 1 .. RIPPLE_MAX_LOSS_K, 1 .. RIPPLE_MAX_CLASSES                                  */
+    int32_t device;
+    const void* x;            /* rows x k                                                                        */
+    int64_t ld_x;
+    const void* W;            /* k x n, input-major like the layers' matrices                                    */
+    int64_t ld_w;
+    const float* bias;        /* n entries; NULL: zeros                                                          */
+    const int32_t* labels;    /* `rows` entries                                                                  */
+    float* loss;              /* `rows` entries; NULL: not wanted                                                */
+    float* lse;               /* `rows` entries                                                                  */
+    void* workspace;
+    int64_t workspace_bytes;
+    void* cuda_stream;
+} ripple_loss_rows_args;
+int64_t ripple_loss_rows_workspace_bytes(const ripple_loss_rows_args* args);
+ripple_status ripple_loss_rows(const ripple_loss_rows_args* args);
+
+/* Its gradient: g = dloss_i (softmax(z)_ic - [c = label_i]), dx = g W^T, dW = x^T g, dbias = sum_i g.  g is formed in pieces of the classes; as an
+ * operand of the products it has the type's bits (fp16: scaled by a power of two; fp32: three parts), in dbias all of fp32. */
+typedef struct {
+    int64_t rows;
+    int32_t type;
+    int32_t k, n;
+    int32_t device;
+    const void* x;
+    int64_t ld_x;
+    const void* W;
+    int64_t ld_w;
+    const float* bias;
+    const int32_t* labels;
+    const float* lse;         /* what ripple_loss_rows gave                                                      */
+    const float* dloss;       /* `rows` entries; NULL: `scale` for every row                                     */
+    void* dx;                 /* rows x k; NULL: not wanted                                                      */
+    int64_t ld_dx;
+    void* dW;                 /* k x n; NULL: not wanted                                                         */
+    int64_t ld_dw;
+    float* dbias;             /* n entries; NULL: not wanted                                                     */
+    float scale;              /* of dloss                                                                        */
+    int32_t reserved;
+    void* workspace;
+    int64_t workspace_bytes;
+    void* cuda_stream;
+} ripple_loss_rows_grad_args;
+int64_t ripple_loss_rows_grad_workspace_bytes(const ripple_loss_rows_grad_args* args);
+ripple_status ripple_loss_rows_grad(const ripple_loss_rows_grad_args* args);
+
 /* Library version string. */
 const char* ripple_version(void);
 

@@ -10,7 +10,8 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libripple.so")
 SOURCES = ["ripple_api.cu", "graph_store.cu", "frontier.cu", "scatter.cu", "layer_update.cu", "layer_update_tc.cu",
            "monotonic.cu", "attention.cu", "partition.cu", "router.cu",
-           "row_norms.cu", "row_project.cu"]
+           "row_norms.cu", "row_project.cu",
+           "row_lookup.cu", "row_norms_grad.cu", "row_loss.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC,-fopenmp,-O2", "-cudart", "static"]
 

@@ -12,6 +12,7 @@
 namespace rp {
 
 void note_error(const char* fmt, ...);   // text for ripple_last_error(NULL)
+cudaError_t take_loss_timeout(int* gave_up);   // whether a bounded wait of row_loss.cu gave up on the current device; cleared
 
 inline int type_size(int t) { return t == RIPPLE_TYPE_F32 ? 4 : 2; }
 inline bool type_ok(int t) { return t >= RIPPLE_TYPE_F32 && t <= RIPPLE_TYPE_F16; }

@@ -1,0 +1,561 @@
+// Rows looked up by id, and the gradient of the table they came from:
+//   out_i = scale table[ids_i],      dtable[r] = scale * sum of dy_i over the i with ids_i = r, in the order of i.
+// The gradient sorts (id, i) by id and sums runs of one id.  Every 32 places of the sorted list are a warp's, however the ids are
+// distributed: a run that lies within them is finished there; what a run has in them that goes on beyond is a partial sum, and the partial sums
+// are again a sorted list, a sixteenth as long (later a 32nd), for the same kernel.  No atomics on sums, so every call gives the same bits.
+#include "row_vectors.cuh"
+
+#include <algorithm>
+#include <utility>
+
+namespace rp {
+
+// ---- lookup --------------------------------------------------------------------------------------------------------
+struct LookupParams {
+    int rows, width, lanes;      // lanes: threads of a row, a power of two
+    const void* table;
+    int64_t ld_table, table_rows;
+    const int32_t* ids;          // null: zeros everywhere
+    void* out;
+    int64_t ld_out;
+    float scale;
+};
+
+constexpr int LK_BLOCK = 256;
+
+template <typename T, typename TO, int V>
+__global__ void __launch_bounds__(LK_BLOCK) k_lookup_rows(const __grid_constant__ LookupParams p) {
+    pdl_enter();
+    const int t = threadIdx.x & (p.lanes - 1), per_block = LK_BLOCK / p.lanes;
+    const Vec<V> scale = all_of<V>(p.scale);
+    for (int64_t row = (int64_t)blockIdx.x * per_block + threadIdx.x / p.lanes; row < p.rows; row += (int64_t)gridDim.x * per_block) {
+        const int64_t id = p.ids ? p.ids[row] : -1;
+        const bool real = id >= 0 && id < p.table_rows;
+        const T* const from = static_cast<const T*>(p.table) + (real ? id : 0) * p.ld_table;
+        TO* const to = static_cast<TO*>(p.out) + row * p.ld_out;
+#pragma unroll 4
+        for (int c = t * V; c < p.width; c += p.lanes * V) {
+            Vec<V> v = all_of<V>(0.f);
+            if (real) {
+                v = load<T, V>(from + c);
+                times<V>(v, scale);
+            }
+            store<TO, V>(to + c, v);
+        }
+    }
+}
+
+template <typename T, typename TO, int V>
+static cudaError_t launch_lookup(LookupParams p, void* stream) {
+    p.lanes = 1;
+    while (p.lanes < LK_BLOCK && p.lanes * V < p.width) p.lanes *= 2;
+    const int64_t blocks = ((int64_t)p.rows * p.lanes + LK_BLOCK - 1) / LK_BLOCK;
+    return launch(k_lookup_rows<T, TO, V>, dim3((unsigned)std::min<int64_t>(blocks, (int64_t)sm_count() * 32)), LK_BLOCK, 0, stream, p);
+}
+
+template <typename T, typename TO>
+static cudaError_t launch_lookup(const LookupParams& p, int v, void* stream) {
+    constexpr int WIDE = 16 / sizeof(T);
+    if (v >= WIDE) return launch_lookup<T, TO, WIDE>(p, stream);
+    if (v >= 2) return launch_lookup<T, TO, 2>(p, stream);
+    return launch_lookup<T, TO, 1>(p, stream);
+}
+
+// ---- (id, place) in the order of ids -----------------------------------------------------------------------------------
+// From the lowest digit up; a pass counts the digits of every tile, adds the counts up, and moves the entries; entries of one digit
+// stay in order.  Ids outside the table become `table_rows` and come last.
+constexpr int SR_TILE = 4096, SR_WARPS = 8, SR_BITS = 11;
+constexpr int SR_SMALL = 4096, SR_SMALL_BITS = 8;      // entries that one block sorts in shared memory, digits of 8 bits
+
+struct SortParams {
+    int n, tiles;
+    int shift, digits;           // of this pass
+    uint32_t table_rows;
+    const int32_t* ids;          // first pass; else null
+    const uint32_t* keys;
+    const int32_t* places;
+    uint32_t* keys_out;
+    int32_t* places_out;
+    int32_t* counts;             // digits x tiles, then their exclusive sums along the tiles
+    int32_t* totals;             // digits
+};
+
+__device__ __forceinline__ uint32_t key_of(int id, uint32_t table_rows) { return min((uint32_t)id, table_rows); }    // (negative ids are large)
+__device__ __forceinline__ uint32_t sort_key(const SortParams& p, int i) { return p.ids ? key_of(p.ids[i], p.table_rows) : p.keys[i]; }
+
+__global__ void __launch_bounds__(32 * SR_WARPS) k_sort_count(const __grid_constant__ SortParams p) {
+    pdl_enter();
+    __shared__ int32_t count[1 << SR_BITS];
+    for (int d = threadIdx.x; d < p.digits; d += blockDim.x) count[d] = 0;
+    __syncthreads();
+    const int first = blockIdx.x * SR_TILE;
+#pragma unroll 4
+    for (int e = threadIdx.x; e < SR_TILE; e += blockDim.x) {
+        const int i = first + e;
+        const bool in = i < p.n;
+        const int d = in ? (int)(sort_key(p, i) >> p.shift & (uint32_t)(p.digits - 1)) : -1;
+        // (equal digits of a warp at once: popular ids would queue up at one place)
+        const uint32_t same = __match_any_sync(FULL, d);
+        if (in && (same & ((1u << lane_id()) - 1)) == 0) atomicAdd(&count[d], __popc(same));
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < p.digits; d += blockDim.x) p.counts[(int64_t)d * p.tiles + blockIdx.x] = count[d];
+}
+
+// a warp per digit
+__global__ void __launch_bounds__(256) k_sort_scan(const __grid_constant__ SortParams p) {
+    pdl_enter();
+    const int d = blockIdx.x * 8 + (threadIdx.x >> 5), lane = lane_id();
+    if (d >= p.digits) return;
+    int32_t* const row = p.counts + (int64_t)d * p.tiles;
+    int sum = 0;
+    for (int t = 0; t < p.tiles; t += 32) {
+        const int v = t + lane < p.tiles ? row[t + lane] : 0, up_to = warp_inclusive_scan(v);
+        if (t + lane < p.tiles) row[t + lane] = sum + up_to - v;
+        sum += __shfl_sync(FULL, up_to, 31);
+    }
+    if (lane == 0) p.totals[d] = sum;
+}
+
+// Places of a tile's entries, warp by warp in contiguous parts: at[warp][digit] is where the warp's next entry of that digit goes.
+// entry(e): the digit of the tile's entry e, negative beyond its end; move(e, to): its new place.
+template <int WARPS, typename E, typename M, typename B>
+__device__ __forceinline__ void move_tile(int32_t* at, int digits, int entries, E entry, M move, B base) {
+    const int warp = threadIdx.x >> 5, lane = lane_id();
+    const int part = (entries + 32 * WARPS - 1) / (32 * WARPS) * 32, begin = warp * part;
+    for (int d = threadIdx.x; d < digits * WARPS; d += 32 * WARPS) at[d] = 0;
+    __syncthreads();
+    const uint32_t before = (1u << lane) - 1;
+    for (int e = begin; e < begin + part; e += 32) {
+        const int d = entry(e + lane);
+        const uint32_t same = __match_any_sync(FULL, d);
+        if (d >= 0 && (same & before) == 0) at[warp * digits + d] += __popc(same);
+        __syncwarp();
+    }
+    __syncthreads();
+    base();                      // counts of the warps become places: at[w][d] = start of d + entries of the warps before
+    __syncthreads();
+    for (int e = begin; e < begin + part; e += 32) {
+        const int d = entry(e + lane);
+        const uint32_t same = __match_any_sync(FULL, d);
+        const int start = d >= 0 ? at[warp * digits + d] : 0;
+        __syncwarp();
+        if (d >= 0) {
+            move(e + lane, start + __popc(same & before));
+            if ((same & before) == 0) at[warp * digits + d] = start + __popc(same);
+        }
+        __syncwarp();
+    }
+    __syncthreads();
+}
+
+__global__ void __launch_bounds__(32 * SR_WARPS) k_sort_move(const __grid_constant__ SortParams p) {
+    pdl_enter();
+    extern __shared__ int32_t at[];            // warps x digits, and behind them the digits' starts
+    __shared__ int32_t scratch[33];
+    int32_t* const start = at + SR_WARPS * p.digits;
+    // starts of the digits: sums of the totals before them
+    const int per = (p.digits + blockDim.x - 1) / blockDim.x, d0 = threadIdx.x * per;
+    int mine = 0, all;
+    for (int d = d0; d < min(d0 + per, p.digits); ++d) mine += p.totals[d];
+    int sum = block_exclusive_scan(mine, scratch, all);
+    for (int d = d0; d < min(d0 + per, p.digits); ++d) {
+        start[d] = sum + p.counts[(int64_t)d * p.tiles + blockIdx.x];
+        sum += p.totals[d];
+    }
+    const int first = blockIdx.x * SR_TILE;
+    auto entry = [&](int e) { return e < SR_TILE && first + e < p.n ? (int)(sort_key(p, first + e) >> p.shift & (uint32_t)(p.digits - 1)) : -1; };
+    auto move = [&](int e, int to) {
+        const int i = first + e;
+        p.keys_out[to] = sort_key(p, i);
+        p.places_out[to] = p.ids ? i : p.places[i];
+    };
+    auto base = [&]() {
+        for (int d = threadIdx.x; d < p.digits; d += blockDim.x) {
+            int sum = start[d];
+            for (int w = 0; w < SR_WARPS; ++w) {
+                const int c = at[w * p.digits + d];
+                at[w * p.digits + d] = sum;
+                sum += c;
+            }
+        }
+    };
+    move_tile<SR_WARPS>(at, p.digits, SR_TILE, entry, move, base);
+}
+
+// All passes of up to SR_SMALL entries by one block.
+constexpr int SS_WARPS = 16;
+struct SmallSort {
+    uint32_t key[2][SR_SMALL];
+    uint16_t place[2][SR_SMALL];
+    int32_t at[SS_WARPS << SR_SMALL_BITS];
+    int32_t scratch[33];
+};
+__global__ void __launch_bounds__(32 * SS_WARPS) k_sort_small(const __grid_constant__ SortParams p, int bits) {
+    pdl_enter();
+    extern __shared__ __align__(16) uint8_t raw[];
+    SmallSort& s = *reinterpret_cast<SmallSort*>(raw);
+    constexpr int DIGITS = 1 << SR_SMALL_BITS;
+    for (int i = threadIdx.x; i < p.n; i += blockDim.x) s.key[0][i] = key_of(p.ids[i], p.table_rows), s.place[0][i] = (uint16_t)i;
+    __syncthreads();
+    int b = 0;
+    for (int shift = 0; shift < bits; shift += SR_SMALL_BITS, b ^= 1) {
+        auto entry = [&](int e) { return e < p.n ? (int)(s.key[b][e] >> shift & (DIGITS - 1)) : -1; };
+        auto move = [&](int e, int to) { s.key[b ^ 1][to] = s.key[b][e], s.place[b ^ 1][to] = s.place[b][e]; };
+        auto base = [&]() {
+            const int d = threadIdx.x;
+            int mine = 0, all;
+            if (d < DIGITS) for (int w = 0; w < SS_WARPS; ++w) mine += s.at[w * DIGITS + d];
+            int sum = block_exclusive_scan(mine, s.scratch, all);
+            if (d < DIGITS) {
+                for (int w = 0; w < SS_WARPS; ++w) {
+                    const int c = s.at[w * DIGITS + d];
+                    s.at[w * DIGITS + d] = sum;
+                    sum += c;
+                }
+            }
+        };
+        move_tile<SS_WARPS>(s.at, DIGITS, p.n, entry, move, base);
+    }
+    for (int i = threadIdx.x; i < p.n; i += blockDim.x) p.keys_out[i] = s.key[b][i], p.places_out[i] = s.place[b][i];
+}
+static_assert(32 * SS_WARPS >= 1 << SR_SMALL_BITS, "a thread per digit");
+
+// ---- sums of runs --------------------------------------------------------------------------------------------------
+// A list entry of the partial sums: the key, with EMPTY where the run only goes on through this place.
+constexpr uint32_t EMPTY = 0x80000000u, NO_KEY = 0xffffffffu;
+
+struct RunParams {
+    int n, width, chunk, chunks, slices;    // places of a warp, a multiple of 32; parts of the columns, a warp each
+    uint32_t table_rows;
+    const uint32_t* keys;        // n, ascending (without EMPTY), NO_KEY anywhere
+    const int32_t* places;       // row of src of every entry; null: the entry's own
+    const void* src;
+    int64_t ld_src;
+    uint32_t* next_keys;         // 2 x chunks: partial sums of runs that go on beyond a chunk
+    float* next;                 // 2 x chunks x ld_next
+    int ld_next;
+    void* out;
+    int64_t ld_out;
+    float scale;
+    int accumulate;
+};
+
+constexpr int RS_AHEAD = 8;      // rows on their way
+
+template <typename T, typename TO, int V, int NP>
+__global__ void __launch_bounds__(128) k_sum_runs(const __grid_constant__ RunParams p) {
+    pdl_enter();
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int lane = lane_id(), chunk = (int)(at / p.slices), slice = (int)(at % p.slices);
+    if (chunk >= p.chunks) return;
+    const int c0 = slice * (32 * V * NP) + lane * V;
+    const int begin = chunk * p.chunk, end = min(p.n, begin + p.chunk);
+    const Vec<V> scale = all_of<V>(p.scale);
+    auto bare = [](uint32_t k) { return k & ~EMPTY; };
+    const uint32_t none = bare(NO_KEY), before = begin > 0 ? bare(p.keys[begin - 1]) : none, after = end < p.n ? bare(p.keys[end]) : none;
+    Vec<V> sum[NP];
+#pragma unroll
+    for (int j = 0; j < NP; ++j) sum[j] = all_of<V>(0.f);
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int j = 0; j < NP; ++j) if (c0 + j * 32 * V < p.width) f(j, c0 + j * 32 * V);
+    };
+    uint32_t run = bare(p.keys[begin]);
+    bool from_before = run == before;
+    uint32_t left0 = NO_KEY, left1 = NO_KEY;    // keys of this chunk's partial sums: of the run that it begins in, of the one that it ends in
+    auto finish = [&](bool goes_on) {
+        if (run < p.table_rows) {
+            if (from_before || goes_on) {
+                float* const to = p.next + (int64_t)(2 * chunk + (from_before ? 0 : 1)) * p.ld_next;
+                each([&](int j, int c) { store<float, V>(to + c, sum[j]); });
+                if (from_before) left0 = run;
+                if (goes_on) left1 = from_before ? run | EMPTY : run;
+            } else {
+                TO* const to = static_cast<TO*>(p.out) + (int64_t)run * p.ld_out;
+                each([&](int j, int c) {
+                    times<V>(sum[j], scale);
+                    if (p.accumulate) plus<V>(sum[j], load<TO, V>(to + c));
+                    store<TO, V>(to + c, sum[j]);
+                });
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NP; ++j) sum[j] = all_of<V>(0.f);
+    };
+    for (int i0 = begin; i0 < end; i0 += 32) {
+        const int i = min(i0 + lane, end - 1), count = min(32, end - i0);
+        const uint32_t key = p.keys[i];
+        const int place = p.places ? p.places[i] : i;
+        for (int e0 = 0; e0 < count; e0 += RS_AHEAD) {
+            Piece<T, V> v[RS_AHEAD][NP];
+            uint32_t k[RS_AHEAD];
+            // (an entry that holds nothing -- padding, EMPTY, none at all -- is not read)
+#pragma unroll
+            for (int u = 0; u < RS_AHEAD; ++u) {
+                k[u] = __shfl_sync(FULL, key, min(e0 + u, 31));
+                const T* const from = static_cast<const T*>(p.src) + (int64_t)__shfl_sync(FULL, place, min(e0 + u, 31)) * p.ld_src;
+                if (e0 + u >= count) k[u] = NO_KEY;
+                if (k[u] < p.table_rows) each([&](int j, int c) { v[u][j] = *reinterpret_cast<const Piece<T, V>*>(from + c); });
+            }
+#pragma unroll
+            for (int u = 0; u < RS_AHEAD; ++u) {
+                if (e0 + u >= count) break;
+                const uint32_t now = bare(k[u]);
+                if (now != run) {
+                    finish(false);
+                    run = now, from_before = false;
+                }
+                if (k[u] < p.table_rows) each([&](int j, int) { plus<V>(sum[j], load<T, V>(&v[u][j])); });
+            }
+        }
+    }
+    finish(run == after);
+    if (p.next_keys && slice == 0 && lane < 2) p.next_keys[2 * chunk + lane] = lane ? left1 : left0;
+}
+
+// Places of a warp: of the rows themselves, of lists of partial sums.
+constexpr int RS_ROWS = 32, RS_SUMS = 64;
+
+template <typename T, typename TO, int V, int NP>
+static cudaError_t launch_runs(RunParams p, void* stream) {
+    p.slices = (p.width + 32 * V * NP - 1) / (32 * V * NP);
+    const int64_t warps = (int64_t)p.chunks * p.slices;
+    return launch(k_sum_runs<T, TO, V, NP>, dim3((unsigned)((warps + 3) / 4)), 128, 0, stream, p);
+}
+
+// ---- few rows ------------------------------------------------------------------------------------------------------
+// Up to FW_ROWS rows: a block for each.  The block of an id's first row finds the others and sums them; one launch in place of a sort.
+constexpr int FW_ROWS = 256;
+template <typename T, typename TO, int V>
+__global__ void __launch_bounds__(FW_ROWS) k_lookup_grad_few(const __grid_constant__ RunParams p, const int32_t* ids) {
+    pdl_enter();
+    __shared__ int32_t rows[FW_ROWS];
+    __shared__ int32_t before[FW_ROWS / 32 + 1];
+    const int me = blockIdx.x, t = threadIdx.x, id = ids[me];
+    if (id < 0 || (uint32_t)id >= p.table_rows) return;
+    const bool same = t < p.n && ids[t] == id;
+    if (__syncthreads_or(same && t < me)) return;
+    // the rows of this id, in order
+    const uint32_t all = __ballot_sync(FULL, same);
+    if (lane_id() == 0) before[t >> 5] = __popc(all);
+    __syncthreads();
+    int count = 0, at = 0;
+    for (int w = 0; w < FW_ROWS / 32; ++w) {
+        if (w == t >> 5) at = count;
+        count += before[w];
+    }
+    if (same) rows[at + __popc(all & ((1u << lane_id()) - 1))] = t;
+    __syncthreads();
+    const Vec<V> scale = all_of<V>(p.scale);
+    TO* const to = static_cast<TO*>(p.out) + (int64_t)id * p.ld_out;
+    for (int c = t * V; c < p.width; c += FW_ROWS * V) {
+        Vec<V> sum = all_of<V>(0.f);
+#pragma unroll 8
+        for (int i = 0; i < count; ++i) plus<V>(sum, load<T, V>(static_cast<const T*>(p.src) + (int64_t)rows[i] * p.ld_src + c));
+        times<V>(sum, scale);
+        if (p.accumulate) plus<V>(sum, load<TO, V>(to + c));
+        store<TO, V>(to + c, sum);
+    }
+}
+
+// ---- the call ------------------------------------------------------------------------------------------------------
+static int64_t up128(int64_t x) { return (x + 127) / 128 * 128; }
+
+// What a call keeps where in its workspace (bytes).
+struct GradPlan {
+    int n, bits, tiles, passes, digit_bits;
+    int64_t keys[2], places[2], counts, totals;
+    int levels;                  // lists of partial sums
+    int64_t list_keys[12], list[12];
+    int list_n[12], ld;
+    int64_t bytes;
+};
+static GradPlan plan_grad(int64_t rows, int64_t table_rows, int width) {
+    GradPlan g = {};
+    g.n = (int)rows;
+    if (rows <= FW_ROWS || table_rows == 0) return g;
+    while (g.bits < 32 && (uint64_t)table_rows >> g.bits) ++g.bits;
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += up128(bytes);
+        return here;
+    };
+    g.passes = (g.bits + SR_BITS - 1) / SR_BITS;
+    g.digit_bits = (g.bits + g.passes - 1) / g.passes;
+    g.tiles = (int)((rows + SR_TILE - 1) / SR_TILE);
+    const bool small = rows <= SR_SMALL;
+    for (int b = 0; b < (small ? 1 : 2); ++b) g.keys[b] = take(rows * 4), g.places[b] = take(rows * 4);
+    if (!small) g.counts = take(((int64_t)g.tiles << g.digit_bits) * 4), g.totals = take((int64_t)4 << g.digit_bits);
+    g.ld = (width + 7) / 8 * 8;
+    int64_t n = rows;
+    for (int chunk = RS_ROWS; n > chunk; chunk = RS_SUMS) {
+        n = (n + chunk - 1) / chunk * 2;
+        g.list_n[g.levels] = (int)n;
+        g.list_keys[g.levels] = take(n * 4);
+        g.list[g.levels++] = take(n * g.ld * 4);
+    }
+    g.bytes = at;
+    return g;
+}
+
+template <typename T, typename TO, int V>
+static cudaError_t launch_lookup_grad(const ripple_lookup_rows_grad_args& a, void* stream) {
+    const GradPlan g = plan_grad(a.rows, a.out_rows, a.width);
+    cudaError_t e = cudaSuccess;
+    RunParams r = {};
+    r.n = g.n, r.width = a.width, r.table_rows = (uint32_t)a.out_rows, r.scale = a.scale, r.accumulate = a.accumulate;
+    r.src = a.dy, r.ld_src = a.ld_dy, r.out = a.out, r.ld_out = a.ld_out;
+    uint8_t* const work = static_cast<uint8_t*>(a.workspace);
+    if (!a.accumulate) {
+        LookupParams z = {};
+        z.rows = (int)a.out_rows, z.width = a.width, z.out = a.out, z.ld_out = a.ld_out;
+        if ((e = launch_lookup<TO, TO, V>(z, stream)) != cudaSuccess) return e;
+    }
+    if (a.rows == 0) return e;
+    if (a.rows <= FW_ROWS) return launch(k_lookup_grad_few<T, TO, V>, dim3((unsigned)a.rows), FW_ROWS, 0, stream, r, a.ids);
+    SortParams s = {};
+    s.n = g.n, s.tiles = g.tiles, s.table_rows = (uint32_t)a.out_rows, s.ids = a.ids;
+    auto keys = [&](int b) { return reinterpret_cast<uint32_t*>(work + g.keys[b]); };
+    auto places = [&](int b) { return reinterpret_cast<int32_t*>(work + g.places[b]); };
+    int b = 0;                   // where the sorted list is
+    if (a.rows <= SR_SMALL) {
+        static bool ready[64];
+        if ((e = allow_shared(k_sort_small, (int)sizeof(SmallSort), ready)) != cudaSuccess) return e;
+        s.keys_out = keys(0), s.places_out = places(0);
+        e = launch(k_sort_small, dim3(1), 32 * SS_WARPS, sizeof(SmallSort), stream, s, g.bits);
+    } else {
+        static bool ready[64];
+        if ((e = allow_shared(k_sort_move, (SR_WARPS + 1) << (SR_BITS + 2), ready)) != cudaSuccess) return e;
+        s.counts = reinterpret_cast<int32_t*>(work + g.counts), s.totals = reinterpret_cast<int32_t*>(work + g.totals);
+        s.digits = 1 << g.digit_bits;
+        for (int pass = 0; pass < g.passes && e == cudaSuccess; ++pass) {
+            s.shift = pass * g.digit_bits;
+            if (pass > 0) s.ids = nullptr, s.keys = keys(b), s.places = places(b), b ^= 1;
+            s.keys_out = keys(b), s.places_out = places(b);
+            e = launch(k_sort_count, dim3((unsigned)g.tiles), 32 * SR_WARPS, 0, stream, s);
+            if (e == cudaSuccess) e = launch(k_sort_scan, dim3((unsigned)(s.digits + 7) / 8), 256, 0, stream, s);
+            if (e == cudaSuccess) e = launch(k_sort_move, dim3((unsigned)g.tiles), 32 * SR_WARPS, (size_t)(SR_WARPS + 1) * s.digits * 4, stream, s);
+        }
+    }
+    if (e != cudaSuccess) return e;
+    r.keys = keys(b), r.places = places(b), r.ld_next = g.ld;
+    for (int l = 0; l <= g.levels && e == cudaSuccess; ++l) {
+        r.chunk = l == 0 ? RS_ROWS : RS_SUMS;
+        r.chunks = (r.n + r.chunk - 1) / r.chunk;
+        const bool more = l < g.levels;
+        r.next_keys = more ? reinterpret_cast<uint32_t*>(work + g.list_keys[l]) : nullptr;
+        r.next = more ? reinterpret_cast<float*>(work + g.list[l]) : nullptr;
+        if (l == 0) e = launch_runs<T, TO, V, (V * (int)sizeof(T) == 16 ? 1 : 4 / V)>(r, stream);
+        else e = launch_runs<float, TO, V, (V >= 4 ? 1 : 4 / V)>(r, stream);
+        if (more) r.keys = r.next_keys, r.places = nullptr, r.src = r.next, r.ld_src = g.ld, r.n = g.list_n[l];
+    }
+    return e;
+}
+
+template <typename T, typename TO>
+static cudaError_t launch_lookup_grad(const ripple_lookup_rows_grad_args& a, int v) {
+    constexpr int WIDE = 16 / sizeof(T);
+    if (v >= WIDE) return launch_lookup_grad<T, TO, WIDE>(a, a.cuda_stream);
+    if (v >= 2) return launch_lookup_grad<T, TO, 2>(a, a.cuda_stream);
+    return launch_lookup_grad<T, TO, 1>(a, a.cuda_stream);
+}
+
+// The widest access, up to 16 bytes of the first type, that matrices of `width` columns allow.
+struct Access {
+    int v;
+    Access(int width, int size) : v(16 / size) { while (width % v) v >>= 1; }
+    void fits(const void* ptr, int64_t ld, int size) {
+        while (v > 1 && (ld % v || reinterpret_cast<uintptr_t>(ptr) % (v * size < 16 ? v * size : 16))) v >>= 1;
+    }
+};
+
+}  // namespace rp
+
+using namespace rp;
+
+#define REFUSE(...)                      \
+    do {                                 \
+        note_error(WHAT ": " __VA_ARGS__); \
+        return RIPPLE_ERR_INVALID_ARG;   \
+    } while (0)
+
+#define WHAT "lookup_rows"
+extern "C" ripple_status ripple_lookup_rows(const ripple_lookup_rows_args* a) {
+    if (!a) REFUSE("null arguments");
+    if (a->rows < 0 || a->rows > INT32_MAX) REFUSE("rows out of range");
+    if (a->width < 1 || a->width > 16384) REFUSE("width must be 1 to 16384");
+    if (!type_ok(a->type) || !type_ok(a->out_type) || (a->out_type != a->type && a->type != RIPPLE_TYPE_F32))
+        REFUSE("unknown type, or another type of out than a 16-bit table's");
+    if (a->table_rows < 0) REFUSE("negative number of table rows");
+    if (a->rows > 0 && ((!a->table && a->table_rows > 0) || !a->ids || !a->out)) REFUSE("null table, ids or out");
+    if (a->ld_table < 0 || a->ld_out < a->width) REFUSE("leading dimension negative, or of out below its width");
+    const int ts = type_size(a->type), os = type_size(a->out_type);
+    for (auto [ptr, size] : {std::pair<const void*, int>{a->table, ts}, {a->out, os}, {a->ids, 4}})
+        if (reinterpret_cast<uintptr_t>(ptr) % size) REFUSE("misaligned pointer");
+    const Extent table{a->table, a->table_rows, a->ld_table, a->width, ts}, out{a->out, a->rows, a->ld_out, a->width, os}, ids{a->ids, a->rows, 1, 1, 4};
+    if (extents_meet(out, table) || extents_meet(out, ids)) REFUSE("out overlaps an input");
+    if (a->rows == 0) return RIPPLE_OK;
+    Access v(a->width, ts);
+    v.fits(a->table, a->ld_table, ts), v.fits(a->out, a->ld_out, os);
+    OnDevice on(a->device);
+    if (on.err != cudaSuccess) return launch_failed("cudaSetDevice", on.err);
+    LookupParams p = {};
+    p.rows = (int)a->rows, p.width = a->width, p.table = a->table, p.ld_table = a->ld_table, p.table_rows = a->table_rows, p.ids = a->ids;
+    p.out = a->out, p.ld_out = a->ld_out, p.scale = a->scale;
+    cudaError_t e;
+    switch (a->type * 4 + a->out_type) {
+        case RIPPLE_TYPE_F32 * 4 + RIPPLE_TYPE_F32: e = launch_lookup<float, float>(p, v.v, a->cuda_stream); break;
+        case RIPPLE_TYPE_F32 * 4 + RIPPLE_TYPE_BF16: e = launch_lookup<float, __nv_bfloat16>(p, v.v, a->cuda_stream); break;
+        case RIPPLE_TYPE_F32 * 4 + RIPPLE_TYPE_F16: e = launch_lookup<float, __half>(p, v.v, a->cuda_stream); break;
+        case RIPPLE_TYPE_BF16 * 4 + RIPPLE_TYPE_BF16: e = launch_lookup<__nv_bfloat16, __nv_bfloat16>(p, v.v, a->cuda_stream); break;
+        default: e = launch_lookup<__half, __half>(p, v.v, a->cuda_stream); break;
+    }
+    return e == cudaSuccess ? RIPPLE_OK : launch_failed("lookup_rows launch", e);
+}
+#undef WHAT
+
+static bool lookup_grad_sizes_ok(const ripple_lookup_rows_grad_args* a) {
+    return a->rows >= 0 && a->rows <= INT32_MAX && a->width >= 1 && a->width <= 16384 && a->out_rows >= 0 && a->out_rows < INT32_MAX;
+}
+
+extern "C" int64_t ripple_lookup_rows_grad_workspace_bytes(const ripple_lookup_rows_grad_args* a) {
+    return a && lookup_grad_sizes_ok(a) ? plan_grad(a->rows, a->out_rows, a->width).bytes : -1;
+}
+
+#define WHAT "lookup_rows_grad"
+extern "C" ripple_status ripple_lookup_rows_grad(const ripple_lookup_rows_grad_args* a) {
+    if (!a) REFUSE("null arguments");
+    if (!lookup_grad_sizes_ok(a)) REFUSE("rows, width (1 to 16384) or rows of out out of range");
+    if (!type_ok(a->type) || !type_ok(a->out_type) || (a->out_type != a->type && a->out_type != RIPPLE_TYPE_F32))
+        REFUSE("unknown type, or a type of out that is neither dy's nor fp32");
+    if (a->accumulate < 0 || a->accumulate > 1) REFUSE("accumulate must be 0 or 1");
+    if ((a->rows > 0 && (!a->dy || !a->ids)) || (a->out_rows > 0 && !a->out)) REFUSE("null dy, ids or out");
+    if (a->ld_dy < 0 || a->ld_out < a->width) REFUSE("leading dimension negative, or of out below its width");
+    const int ts = type_size(a->type), os = type_size(a->out_type);
+    for (auto [ptr, size] : {std::pair<const void*, int>{a->dy, ts}, {a->out, os}, {a->ids, 4}})
+        if (reinterpret_cast<uintptr_t>(ptr) % size) REFUSE("misaligned pointer");
+    const int64_t need = plan_grad(a->rows, a->out_rows, a->width).bytes;
+    if (a->workspace_bytes < need || (need > 0 && !a->workspace)) REFUSE("workspace too small");
+    if (reinterpret_cast<uintptr_t>(a->workspace) & 127) REFUSE("misaligned workspace");
+    const Extent dy{a->dy, a->rows, a->ld_dy, a->width, ts}, out{a->out, a->out_rows, a->ld_out, a->width, os}, ids{a->ids, a->rows, 1, 1, 4},
+        work{need > 0 ? a->workspace : nullptr, 1, 1, need, 1};
+    for (const Extent* o : {&out, &work})
+        for (const Extent* in : {&dy, &ids})
+            if (extents_meet(*o, *in)) REFUSE("out or the workspace overlaps an input");
+    if (extents_meet(out, work)) REFUSE("out overlaps the workspace");
+    if (a->out_rows == 0) return RIPPLE_OK;
+    Access v(a->width, ts);
+    v.fits(a->dy, a->ld_dy, ts), v.fits(a->out, a->ld_out, os);
+    OnDevice on(a->device);
+    if (on.err != cudaSuccess) return launch_failed("cudaSetDevice", on.err);
+    cudaError_t e;
+    const bool wide = a->out_type != a->type;
+    switch (a->type) {
+        case RIPPLE_TYPE_F32: e = launch_lookup_grad<float, float>(*a, v.v); break;
+        case RIPPLE_TYPE_BF16: e = wide ? launch_lookup_grad<__nv_bfloat16, float>(*a, v.v) : launch_lookup_grad<__nv_bfloat16, __nv_bfloat16>(*a, v.v); break;
+        default: e = wide ? launch_lookup_grad<__half, float>(*a, v.v) : launch_lookup_grad<__half, __half>(*a, v.v); break;
+    }
+    return e == cudaSuccess ? RIPPLE_OK : launch_failed("lookup_rows_grad launch", e);
+}

@@ -1,0 +1,1006 @@
+// Softmax cross entropy of a linear layer over many classes, and its gradient, without the logits ever being in memory:
+//   z = x W + b,  lse_i = log sum_c exp z_ic,  loss_i = lse_i - z_i,label;
+//   g = dloss_i (softmax(z)_ic - [c = label_i]),  dx = g W^T,  dW = x^T g,  db = sum over the rows of g.
+// Four products of one kernel (k_product) with three ends: maxima and sums of exponentials of a tile (the loss); g of a tile, as an operand of
+// the products that follow (the gradient, in pieces of the classes); and plain results.
+#include "requests.cuh"
+#include "tensor_core.cuh"
+
+#include <cuda.h>
+
+#include <algorithm>
+#include <cstdlib>
+#include <utility>
+
+namespace rp {
+
+// Set where a bounded wait gave up; read and cleared by ripple_request_status.
+__device__ int g_loss_timeout;
+
+cudaError_t take_loss_timeout(int* gave_up) {
+    const int zero = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(gave_up, g_loss_timeout, sizeof(int));
+    if (e == cudaSuccess && *gave_up) e = cudaMemcpyToSymbol(g_loss_timeout, &zero, sizeof(int));
+    return e;
+}
+
+// ---- a product on pairs of tensor cores ----------------------------------------------------------------------------
+// C [m, n] = A B over k, operands of 16 bits, fp32 as three planes of bf16 parts.  A pair of CTAs takes 256 rows x LS_COLS columns of C: each
+// brings its 128 rows of A and its half of the tile's columns of B, the pair's tensor cores read both halves, and each has its 128 rows
+// of C.  (One CTA by itself brings 48 KB per 64 entries of k, where an SM gets 64 bytes a cycle out of L2: 768 cycles for 512 of products.)
+// Operands come by TMA in either order, k along the rows of memory or across them; what lies outside a matrix arrives as zeros.
+constexpr int LS_ROWS = 256, LS_KC = 64;
+constexpr int LS_EPI_WARPS = 8, LS_THREADS = 64 + 32 * LS_EPI_WARPS;
+constexpr int LS_PAIRS = 74;             // of a B200 (for plans that are asked where no device is current, too)
+constexpr int LS_UNIT = 4;               // fp32: chunks (256 entries of k) whose large products share an accumulator
+constexpr int LS_GROUP = 8;              // tiles of rows that are worked on side by side, so that B's tiles are read out of L2
+constexpr uint32_t LS_SPIN_LIMIT = 1u << 18;       // polls after which a wait gives up: about a second
+constexpr float LOG2E = 1.4426950408889634f;
+
+template <int TYPE> struct LossShape {
+    static constexpr int PARTS = TYPE == RIPPLE_TYPE_F32 ? 3 : 1;
+    static constexpr int COLS = PARTS == 3 ? 128 : 256;
+    static constexpr int A_PART = 128 * 128, B_PART = COLS / 2 * 128;       // bytes of a CTA's operands of 64 entries of k
+    static constexpr int STAGE = PARTS * (A_PART + B_PART);
+    static constexpr int STAGES = PARTS == 3 ? 3 : 6;
+    static constexpr int BIAS = LS_EPI_WARPS * (COLS / 2) * 4;
+    static constexpr size_t BYTES = (size_t)STAGES * STAGE + BIAS + 1024;
+};
+
+enum { END_LSE, END_GRAD, END_OUT };
+constexpr int LS_CONTROL = 128;          // blocks of k_look_at_rows
+
+// What k_look_at_rows found, block by block.
+struct RowControl {
+    float most[LS_CONTROL];              // largest finite |dloss|
+    int32_t odd[LS_CONTROL];             // a row without a label holds something that is not finite
+};
+
+struct alignas(64) ProductParams {
+    CUtensorMap a, a_clean, b;           // a_clean: read in place of a where rows without labels hold something that is not finite
+    const RowControl* control;           // null: a as it is
+    int m, n, k;
+    int row_tiles, col_tiles, splits, split_chunks;
+    int b_col0, b_k0;                    // where this piece begins in B
+    // logits
+    const float* bias;                   // of the piece
+    const int32_t* labels;
+    int class0, classes;                 // first class of the piece, number of all
+    float2* sums;                        // LSE: 2 x col_tiles x m: largest logit, sum of exp(logit - largest)
+    float* at_label;
+    const float* lse;                    // GRAD
+    const float* dloss;
+    float scale;
+    uint16_t* g;                         // planes x m x ld_g; null: not wanted
+    int64_t ld_g, g_plane;
+    float* g_sums;                       // row groups of 32 x ld_g; null: not wanted
+    // OUT
+    void* out;
+    int64_t ld_out, split_stride;        // fp32: elements between the splits' results
+    int out_f32, add_to_out;
+    int unscale;                         // g was scaled: see grad_scale
+    const int32_t* dead_rows;            // labels, where rows without one are zeros; else null
+    int withhold;                        // diagnostic: no first accumulator counts as filled
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the address of a shared variable in the pair's first CTA
+__device__ __forceinline__ uint32_t in_leader(const void* p) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(p)));
+    return a;
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// a box of a tensor, completing on a barrier of either CTA of the pair
+__device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(tmem_d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// arrives at the barrier of both CTAs once the products issued so far have finished
+__device__ __forceinline__ void pair_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+}
+// Descriptor of an operand whose rows of memory run across k, 128-byte swizzle: 64 entries of its rows or columns side by side, 8 entries of k
+// 1024 bytes apart, the next 64 rows or columns 8192.
+__device__ __forceinline__ uint64_t across_desc(uint32_t saddr) {
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(8192 >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+__device__ __forceinline__ float exp2_of(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void store8(void* to, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+template <typename T> __device__ __forceinline__ uint32_t pair_of(float a, float b) {
+    const T x = from_f32<T>(a), y = from_f32<T>(b);
+    return (uint32_t)*reinterpret_cast<const uint16_t*>(&x) | (uint32_t)*reinterpret_cast<const uint16_t*>(&y) << 16;
+}
+// An fp32 value as three bf16 parts, rounded; both remainders are exact.  An infinite value has no remainders.
+__device__ __forceinline__ void three_parts(float x, __nv_bfloat16 (&h)[3]) {
+    h[0] = __float2bfloat16_rn(x);
+    if (__hisinf(h[0]) && isfinite(x)) h[0] = __float2bfloat16_rz(x);
+    const float left = isfinite(x) ? x - __bfloat162float(h[0]) : 0.f;
+    h[1] = __float2bfloat16_rn(left);
+    h[2] = __float2bfloat16_rn(left - __bfloat162float(h[1]));
+}
+
+// fp16: g is scaled by a power of two that brings the largest |dloss| to 2^14 .. 2^15, where probabilities down to 2^-29 of it keep all
+// bits; the results are scaled back.  (bf16 and its parts have fp32's range.)
+__device__ __forceinline__ float grad_scale(const RowControl* control, float scale) {
+    float most = 0.f;
+    for (int i = lane_id(); i < LS_CONTROL; i += 32) most = fmaxf(most, control->most[i]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(FULL, most, o));
+    most *= fabsf(scale);
+    if (!(most > 0.f) || !isfinite(most)) return 1.f;
+    int e;
+    frexpf(most, &e);            // most <= 2^e
+    return ldexpf(1.f, max(-126, min(126, 15 - e)));
+}
+
+// Sums over the warp's rows of 32 columns: lane c has the sum of v[c].
+__device__ __forceinline__ float column_sums(float (&v)[32]) {
+#pragma unroll
+    for (int half = 16; half > 0; half >>= 1) {
+        const bool upper = lane_id() & half;
+#pragma unroll
+        for (int i = 0; i < half; ++i) {
+            const float mine = upper ? v[i + half] : v[i], other = upper ? v[i] : v[i + half];
+            v[i] = mine + __shfl_xor_sync(FULL, other, half);
+        }
+    }
+    return v[0];
+}
+
+// Warp 0 of each CTA brings operands, warp 1 of the pair's first CTA issues the products, the others take finished accumulators while the next
+// are being filled.  Barriers, all waits bounded: full[s] in the first CTA (its one arrival announces the bytes of both), empty[s] in both
+// (the products that read stage s), acc_full[b] in both, acc_empty[b] in the first CTA (one arrival per epilogue warp of the pair).
+// fp32: six products of parts (all but those below 2^-24); the large one, of the first parts, is handed over every 256 entries of k and
+// summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
+template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_product(const __grid_constant__ ProductParams p) {
+    using S = LossShape<TYPE>;
+    using T = typename Elem<TYPE == RIPPLE_TYPE_F16 ? RIPPLE_TYPE_F16 : RIPPLE_TYPE_BF16>::T;      // of the operands
+    constexpr int PARTS = S::PARTS, STAGES = S::STAGES, COLS = S::COLS, NB = COLS / 64;       // NB: 32-column blocks of an epilogue warp
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int s_fail;
+
+    const int tid = threadIdx.x, warp = __shfl_sync(FULL, tid >> 5, 0), lane = tid & 31;
+    const uint32_t rank = cluster_rank();
+    const int64_t tiles = (int64_t)p.row_tiles * p.col_tiles, all = tiles * p.splits;
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, chunks = (p.k + LS_KC - 1) / LS_KC;
+    uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    // A tile of C, and the chunks of k of its split.  nt: columns that are multiplied, a multiple of 32; each CTA brings half of them.
+    struct Tile { int row, col, split, first, last, nt; };
+    auto tile_at = [&](int64_t i) {
+        Tile t;
+        t.split = (int)(i / tiles);
+        const int64_t in = i - t.split * tiles, per_group = (int64_t)LS_GROUP * p.col_tiles;
+        const int group = (int)(in / per_group), rows = min(LS_GROUP, p.row_tiles - group * LS_GROUP);
+        const int64_t rest = in - group * per_group;
+        t.col = (int)(rest / rows), t.row = group * LS_GROUP + (int)(rest % rows);
+        t.first = t.split * p.split_chunks, t.last = min(chunks, t.first + p.split_chunks);
+        t.nt = min(COLS, (p.n - t.col * COLS + 31) & ~31);
+        return t;
+    };
+
+    if (tid == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], p.withhold ? 2 : 1 /* one arrives */); mbar_init(&acc_empty[b], 2 * LS_EPI_WARPS); }
+        mbar_init(&drained, 1);
+        s_fail = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    pdl_enter();
+    // Tensor memory: two accumulators and, fp32, two for the small products
+    auto large_at = [&](int b) { return (uint32_t)(COLS * b); };
+    auto small_at = [&](int worked) { return (uint32_t)(2 * COLS + COLS * (worked & 1)); };
+
+    if (warp == 0) {
+        // ---------------- operands ----------------
+        bool odd = false;
+        if (p.control) {
+            for (int i = lane; i < LS_CONTROL; i += 32) odd = odd || p.control->odd[i];
+            odd = __any_sync(FULL, odd);
+        }
+        asm volatile("fence.proxy.async;" ::: "memory");      // (what kernels before wrote, for the copies)
+        const bool lead = tc_elect();
+        if (lead) {
+            const CUtensorMap* const a = odd ? &p.a_clean : &p.a;
+            const uint32_t to0 = smem_u32(ring);
+            bool ok = true;
+            int s = 0, issued = 0;
+            uint32_t ph = 1;                    // (a fresh barrier counts as completed)
+            for (int64_t i = pair; i < all && ok; i += pairs) {
+                const Tile t = tile_at(i);
+                const int row0 = t.row * LS_ROWS + (int)rank * 128, col0 = p.b_col0 + t.col * COLS + (int)rank * (t.nt / 2);
+                for (int c = t.first; c < t.last; ++c) {
+                    ok = mbar_wait_bounded(&empty[s], ph, LS_SPIN_LIMIT);
+                    if (!ok) break;
+                    if (rank == 0) mbar_expect(&full[s], 2 * S::STAGE);
+                    const uint32_t bar = in_leader(&full[s]), to = to0 + (uint32_t)(s * S::STAGE), to_b = to + PARTS * S::A_PART;
+#pragma unroll
+                    for (int q = 0; q < PARTS; ++q) {
+                        if constexpr (A_ACROSS) {
+                            for (int h = 0; h < 2; ++h) load_box(to + q * S::A_PART + h * 8192, a, row0 + 64 * h, c * LS_KC, q, bar);
+                        } else {
+                            load_box(to + q * S::A_PART, a, c * LS_KC, row0, q, bar);
+                        }
+                        if constexpr (B_ACROSS) {
+                            for (int h = 0; h < COLS / 128; ++h) load_box(to_b + q * S::B_PART + h * 8192, &p.b, col0 + 64 * h, p.b_k0 + c * LS_KC, q, bar);
+                        } else {
+                            load_box(to_b + q * S::B_PART, &p.b, p.b_k0 + c * LS_KC, col0, q, bar);
+                        }
+                    }
+                    ++issued;
+                    if (++s == STAGES) { s = 0; ph ^= 1; }
+                }
+            }
+            if (!ok) {
+                s_fail = 1;
+                // copies in flight: the last of every stage (they complete in the first CTA, which outlives the second's)
+                if (rank == 0) {
+                    for (int back = min(issued, STAGES); back > 0; --back) {
+                        const int at = issued - back;
+                        mbar_wait_bounded(&full[at % STAGES], (uint32_t)(at / STAGES) & 1, LS_SPIN_LIMIT);
+                    }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---------------- products ----------------
+        if (rank == 0) {
+            const bool lead = tc_elect();
+            const uint32_t base = __shfl_sync(FULL, smem_u32(ring), 0);
+            const uint64_t a0 = A_ACROSS ? across_desc(base) : tc_smem_desc(base);
+            const uint64_t b0 = B_ACROSS ? across_desc(base + PARTS * S::A_PART) : tc_smem_desc(base + PARTS * S::A_PART);
+            constexpr uint64_t A_STEP = A_ACROSS ? 128 : 2, B_STEP = B_ACROSS ? 128 : 2;       // 16 entries of k
+            constexpr uint64_t AP = S::A_PART >> 4, BP = S::B_PART >> 4;
+            constexpr uint32_t KIND = TYPE == RIPPLE_TYPE_F16 ? 0u : 1u;
+            int s = 0, sg = 0, worked = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            for (int64_t i = pair; i < all && ok; i += pairs, ++worked) {
+                const Tile t = tile_at(i);
+                const int nt = __shfl_sync(FULL, t.nt, 0), first = __shfl_sync(FULL, t.first, 0), last = __shfl_sync(FULL, t.last, 0);
+                const uint32_t idesc = (1u << 4) | (KIND << 7) | (KIND << 10) | ((uint32_t)A_ACROSS << 15) | ((uint32_t)B_ACROSS << 16)
+                                     | ((uint32_t)(nt >> 3) << 17) | ((uint32_t)(LS_ROWS >> 4) << 24);
+                uint32_t acc = 0;
+                const uint32_t small = __shfl_sync(FULL, tmem + small_at(worked), 0);
+                int b = 0;
+                for (int c = first; c < last; ++c) {
+                    const int in = c - first;
+                    const bool fresh = PARTS == 3 ? in % LS_UNIT == 0 : in == 0;
+                    if (fresh) {
+                        b = sg & 1;
+                        const int before = sg >> 1;
+                        ++sg;
+                        // the epilogue must have read this accumulator (and with it the small products of the tile before the last)
+                        if (before > 0) ok = mbar_wait_warp(&acc_empty[b], (before - 1) & 1, LS_SPIN_LIMIT);
+                        if (!ok) break;
+                        tc_fence_after();
+                        acc = __shfl_sync(FULL, tmem + large_at(b), 0);
+                    }
+                    ok = mbar_wait_warp(&full[s], ph, LS_SPIN_LIMIT);
+                    if (!ok) break;
+                    tc_fence_after();
+                    // (broadcast: operands that the compiler cannot see to be the warp's take ten times as long to issue)
+                    const uint64_t at = (uint64_t)((uint32_t)__shfl_sync(FULL, s, 0) * (S::STAGE >> 4)), a = a0 + at, w = b0 + at;
+                    const bool done = c == last - 1 || (PARTS == 3 && in % LS_UNIT == LS_UNIT - 1);
+                    if (lead) {
+#pragma unroll
+                        for (int j = 0; j < LS_KC / 16; ++j) {
+                            const uint64_t a1 = a + A_STEP * j, w1 = w + B_STEP * j;
+                            pair_mma(acc, a1, w1, idesc, !fresh || j != 0);
+                            if constexpr (PARTS == 3) {
+                                pair_mma(small, a1, w1 + BP, idesc, (in | j) != 0);
+                                pair_mma(small, a1 + AP, w1, idesc, 1u);
+                                pair_mma(small, a1 + AP, w1 + BP, idesc, 1u);
+                                pair_mma(small, a1, w1 + 2 * BP, idesc, 1u);
+                                pair_mma(small, a1 + 2 * AP, w1, idesc, 1u);
+                            }
+                        }
+                        pair_commit(&empty[s]);
+                        if (done) pair_commit(&acc_full[b]);
+                    }
+                    __syncwarp();
+                    if (++s == STAGES) { s = 0; ph ^= 1; }
+                }
+            }
+            if (!ok) {
+                if (lead) {
+                    s_fail = 1;
+                    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&drained)) : "memory");
+                    mbar_wait_bounded(&drained, 0, LS_SPIN_LIMIT);
+                }
+                __syncwarp();
+            }
+        }
+    } else {
+        // ---------------- epilogue ----------------
+        // thread: a row, and the 32-column blocks half, half + 2, ... of the tile
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16);
+        float* const bias = reinterpret_cast<float*>(ring + STAGES * S::STAGE) + (warp - 2) * 32 * NB;
+        float factor = 1.f;                      // GRAD: of g; OUT: of the result
+        if (TYPE == RIPPLE_TYPE_F16 && p.control) {
+            if (END == END_GRAD) factor = grad_scale(p.control, p.scale);
+            if (END == END_OUT && p.unscale) factor = 1.f / grad_scale(p.control, p.scale);
+        }
+        const uint32_t release = in_leader(&acc_empty[0]);
+        bool ok = true;
+        int sg = 0, worked = 0;
+        for (int64_t i = pair; i < all && ok; i += pairs, ++worked) {
+            const Tile t = tile_at(i);
+            const int row = t.row * LS_ROWS + (int)rank * 128 + 32 * q + lane, col0 = t.col * COLS;
+            const bool in_rows = row < p.m;
+            int label = -1;
+            float lse = 0.f, weight = 0.f, top = -INFINITY, sum = 0.f;
+            bool live = in_rows;
+            if constexpr (END != END_OUT) {
+                __syncwarp();
+                for (int e = lane; e < 32 * NB; e += 32) {
+                    const int col = col0 + 32 * (2 * (e >> 5) + half) + (e & 31);
+                    bias[e] = col >= p.n ? -INFINITY : p.bias ? p.bias[col] : 0.f;
+                }
+                __syncwarp();
+                if (in_rows) label = p.labels[row];
+                if (label >= p.classes) label = -1;
+                live = label >= 0;
+            }
+            if constexpr (END == END_GRAD) {
+                if (live) {
+                    lse = p.lse[row], weight = p.scale * (p.dloss ? p.dloss[row] : 1.f);
+                    live = lse != -INFINITY;
+                }
+            }
+            if constexpr (END != END_OUT) label = live ? label - p.class0 - col0 : -1;       // within the tile
+            if constexpr (END == END_OUT) {
+                if (p.dead_rows && in_rows) {
+                    const int of_row = p.dead_rows[row];
+                    live = of_row >= 0 && of_row < p.classes;
+                }
+            }
+            // 32 finished sums of this row, from column `at` of the tile
+            auto finish = [&](float (&y)[32], int j) {
+                const int at = 32 * (2 * j + half);
+                if constexpr (END == END_LSE) {
+                    const float4* const b4 = reinterpret_cast<const float4*>(bias + 32 * j);
+                    float most = top;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float4 b = b4[e];
+                        y[4 * e] += b.x, y[4 * e + 1] += b.y, y[4 * e + 2] += b.z, y[4 * e + 3] += b.w;
+                    }
+                    if (__any_sync(FULL, (unsigned)(label - at) < 32u)) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) if (label == at + e) p.at_label[row] = y[e];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) most = fmaxf(most, y[e]);
+                    const float base = most == -INFINITY ? 0.f : most * LOG2E;
+                    sum *= exp2_of(top * LOG2E - base);
+                    float more[4] = {};
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) more[e & 3] += exp2_of(fmaf(y[e], LOG2E, -base));
+                    sum += (more[0] + more[1]) + (more[2] + more[3]);
+                    top = most;
+                } else if constexpr (END == END_GRAD) {
+                    const float4* const b4 = reinterpret_cast<const float4*>(bias + 32 * j);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float4 b = b4[e];
+                        y[4 * e] += b.x, y[4 * e + 1] += b.y, y[4 * e + 2] += b.z, y[4 * e + 3] += b.w;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) y[e] = exp2_of((y[e] - lse) * LOG2E);
+                    if (__any_sync(FULL, (unsigned)(label - at) < 32u)) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) if (label == at + e) y[e] -= 1.f;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) y[e] = live ? y[e] * weight : 0.f;
+                    if (p.g && in_rows) {
+                        uint16_t* const to = p.g + (int64_t)row * p.ld_g + col0 + at;
+                        if constexpr (PARTS == 1) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                uint32_t v[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) v[e] = pair_of<T>(y[16 * h + 2 * e] * factor, y[16 * h + 2 * e + 1] * factor);
+                                store8(to + 16 * h, v);
+                            }
+                        } else {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                float left[16];
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) left[e] = y[16 * h + e];
+#pragma unroll
+                                for (int q3 = 0; q3 < 3; ++q3) {
+                                    uint32_t v[8];
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) {
+                                        v[e] = pair_of<__nv_bfloat16>(left[2 * e], left[2 * e + 1]);
+                                        const float h0 = __uint_as_float(v[e] << 16), h1 = __uint_as_float(v[e] & 0xffff0000u);
+                                        left[2 * e] = fabsf(h0) < INFINITY ? left[2 * e] - h0 : 0.f, left[2 * e + 1] = fabsf(h1) < INFINITY ? left[2 * e + 1] - h1 : 0.f;
+                                    }
+                                    store8(to + q3 * p.g_plane + 16 * h, v);
+                                }
+                            }
+                        }
+                    }
+                    if (p.g_sums) {
+                        const float s = column_sums(y);
+                        if (row - lane < p.m) p.g_sums[(int64_t)((row - lane) >> 5) * p.ld_g + col0 + at + lane] = s;
+                    }
+                } else {
+                    if (!in_rows) return;
+                    const int col = col0 + at, out_size = p.out_f32 ? 4 : 2;
+                    uint8_t* const to = static_cast<uint8_t*>(p.out) + ((int64_t)row * p.ld_out + col + t.split * p.split_stride) * out_size;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) y[e] = live ? y[e] * factor : 0.f;
+                    if (p.add_to_out) {
+                        const float* const from = reinterpret_cast<const float*>(to);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) if (col + e < p.n) y[e] += from[e];
+                    }
+                    if (col + 32 <= p.n) {
+                        uint32_t v[8];
+                        if (p.out_f32) {
+#pragma unroll
+                            for (int h = 0; h < 4; ++h) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) v[e] = __float_as_uint(y[8 * h + e]);
+                                store8(to + 32 * h, v);
+                            }
+                        } else {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) v[e] = pair_of<T>(y[16 * h + 2 * e], y[16 * h + 2 * e + 1]);
+                                store8(to + 32 * h, v);
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            if (col + e >= p.n) continue;
+                            if (p.out_f32) reinterpret_cast<float*>(to)[e] = y[e];
+                            else reinterpret_cast<T*>(to)[e] = from_f32<T>(y[e]);
+                        }
+                    }
+                }
+            };
+            const int units = PARTS == 3 ? (t.last - t.first + LS_UNIT - 1) / LS_UNIT : 1;
+            float carry[PARTS == 3 ? NB : 1][32];          // fp32: of the units before the last
+            for (int u = 0; u < units && ok; ++u, ++sg) {
+                const int b = sg & 1;
+                ok = mbar_wait_warp(&acc_full[b], (sg >> 1) & 1, LS_SPIN_LIMIT);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t large = lanes + large_at(b), small = lanes + small_at(worked);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    const int at = 32 * (2 * j + half);
+                    if (at >= t.nt) continue;
+                    uint32_t x[32];
+                    float y[32];
+                    tc_load32(x, large + (uint32_t)at);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) y[e] = __uint_as_float(x[e]);
+                    if constexpr (PARTS == 3) {
+                        if (u > 0) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) y[e] += carry[j][e];
+                        }
+                        if (u < units - 1) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) carry[j][e] = y[e];
+                            continue;
+                        }
+                        tc_load32(x, small + (uint32_t)at);
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                        // (an infinite entry has no parts: its small products may be NaN)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) if (fabsf(y[e]) < INFINITY) y[e] += __uint_as_float(x[e]);
+                    }
+                    finish(y, j);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_at(release + 8 * (uint32_t)b);
+            }
+            if (END == END_LSE && ok && in_rows) p.sums[(int64_t)(2 * t.col + half) * p.m + row] = make_float2(top, sum);
+        }
+        if (!ok) s_fail = 1;
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after();
+    if (s_fail && tid == 0) g_loss_timeout = 1;
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+// ---- what stands around the products -----------------------------------------------------------------------------------
+__device__ __forceinline__ bool has_label(const int32_t* labels, int64_t row, int classes) { return (uint32_t)labels[row] < (uint32_t)classes; }
+
+// A matrix as an operand: planes of 16-bit parts, rows `ld` apart, zeros beyond the columns.  labels: rows without one become zeros, because in x^T g
+// whatever they hold is multiplied by zero.  control: only if such a row holds something that is not finite.
+struct OperandParams {
+    const void* from;
+    int64_t rows, ld_from;
+    int cols, lanes;
+    uint16_t* to;
+    int64_t ld, plane;
+    const int32_t* labels;
+    int classes;
+    const RowControl* control;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) k_operand(const __grid_constant__ OperandParams p) {
+    pdl_enter();
+    if (p.control) {
+        bool odd = false;
+        for (int i = lane_id(); i < LS_CONTROL; i += 32) odd = odd || p.control->odd[i];
+        if (!__any_sync(FULL, odd)) return;
+    }
+    const int t = threadIdx.x & (p.lanes - 1), per_block = 256 / p.lanes;
+    const bool vec = (reinterpret_cast<uintptr_t>(p.from) & 15) == 0 && p.ld_from % (16 / (int)sizeof(T)) == 0;
+    for (int64_t row = (int64_t)blockIdx.x * per_block + threadIdx.x / p.lanes; row < p.rows; row += (int64_t)gridDim.x * per_block) {
+        const T* const from = static_cast<const T*>(p.from) + row * p.ld_from;
+        uint16_t* const to = p.to + row * p.ld;
+        const bool live = !p.labels || has_label(p.labels, row, p.classes);
+        for (int c = t * 8; c < p.ld; c += p.lanes * 8) {
+            Piece<T, 8> v;
+            if (live && vec && c + 8 <= p.cols) {
+                v = *reinterpret_cast<const Piece<T, 8>*>(from + c);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v.v[e] = live && c + e < p.cols ? from[c + e] : from_f32<T>(0.f);
+            }
+            if constexpr (sizeof(T) == 4) {
+                Piece<__nv_bfloat16, 8> part[3];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    __nv_bfloat16 h[3];
+                    three_parts(v.v[e], h);
+                    part[0].v[e] = h[0], part[1].v[e] = h[1], part[2].v[e] = h[2];
+                }
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<Piece<__nv_bfloat16, 8>*>(to + q * p.plane + c) = part[q];
+            } else {
+                *reinterpret_cast<Piece<T, 8>*>(to + c) = v;
+            }
+        }
+    }
+}
+
+// What the gradient has to know of all rows: the largest dloss (fp16), and whether a row without a label holds something that is not finite (x read in place).
+template <typename T>
+__global__ void __launch_bounds__(256) k_look_at_rows(const T* x, int64_t ld_x, int k, const int32_t* labels, const float* dloss, int64_t rows, int classes, RowControl* control) {
+    pdl_enter();
+    __shared__ float scratch[8];
+    float most = 0.f;
+    bool odd = false;
+    for (int64_t r0 = (int64_t)blockIdx.x * 256 + (threadIdx.x & ~31); r0 < rows; r0 += (int64_t)LS_CONTROL * 256) {
+        const int64_t row = r0 + lane_id();
+        const bool live = row < rows && has_label(labels, row, classes);
+        if (live) {
+            const float w = dloss ? fabsf(dloss[row]) : 1.f;
+            if (isfinite(w)) most = fmaxf(most, w);
+        }
+        for (uint32_t left = x ? __ballot_sync(FULL, row < rows && !live) : 0; left; left &= left - 1) {
+            const T* const from = x + (r0 + __ffs(left) - 1) * ld_x;
+            for (int c = lane_id(); c < k; c += 32) odd = odd || !isfinite(to_f32(from[c]));
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(FULL, most, o));
+    if (lane_id() == 0) scratch[threadIdx.x >> 5] = most;
+    const int any = __syncthreads_or(odd);
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 8; ++w) most = fmaxf(most, scratch[w]);
+        control->most[blockIdx.x] = most, control->odd[blockIdx.x] = any;
+    }
+}
+
+// Loss and lse of 32 rows per block from the tiles' sums; the warps take turns over the tiles.
+__global__ void __launch_bounds__(512) k_finish_loss(const float2* sums, int parts, int64_t rows, const float* at_label, const int32_t* labels, int classes, float* loss, float* lse) {
+    pdl_enter();
+    __shared__ float2 mine[16][33];
+    const int warp = threadIdx.x >> 5, lane = lane_id();
+    const int64_t row = (int64_t)blockIdx.x * 32 + lane;
+    float top = -INFINITY, sum = 0.f;
+    auto join = [&](float2 s) {
+        const float most = fmaxf(top, s.x), base = most == -INFINITY ? 0.f : most;
+        sum = sum * exp2_of((top - base) * LOG2E) + s.y * exp2_of((s.x - base) * LOG2E);
+        top = most;
+    };
+    if (row < rows) {
+#pragma unroll 8
+        for (int i = warp; i < parts; i += 16) join(sums[i * rows + row]);
+    }
+    mine[warp][lane] = make_float2(top, sum);
+    __syncthreads();
+    if (warp > 0 || row >= rows) return;
+    top = -INFINITY, sum = 0.f;
+    for (int w = 0; w < 16; ++w) join(mine[w][lane]);
+    const float l = top == -INFINITY && sum == 0.f ? -INFINITY : top + logf(sum);
+    lse[row] = l;
+    if (loss) loss[row] = has_label(labels, row, classes) && l != -INFINITY ? l - at_label[row] : 0.f;
+}
+
+// out = the sum of the splits' results, in order.
+template <typename T>
+__global__ void __launch_bounds__(256) k_join_parts(const float* parts, int splits, int64_t split_stride, int64_t ld, T* out, int64_t ld_out, int64_t rows, int cols) {
+    pdl_enter();
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+#pragma unroll 4
+        for (int c = blockIdx.x * 1024 + threadIdx.x; c < min(cols, (int)(blockIdx.x + 1) * 1024); c += 256) {
+            float sum = 0.f;
+            for (int s = 0; s < splits; ++s) sum += parts[s * split_stride + row * ld + c];
+            out[row * ld_out + c] = from_f32<T>(sum);
+        }
+    }
+}
+
+// dbias from the sums over groups of 32 rows; a block has 32 columns, the warps take turns over the groups.
+__global__ void __launch_bounds__(512) k_join_columns(const float* sums, int64_t groups, int64_t ld, int cols, float* out) {
+    pdl_enter();
+    __shared__ float mine[16][33];
+    const int warp = threadIdx.x >> 5, lane = lane_id(), c = blockIdx.x * 32 + lane;
+    float sum = 0.f;
+    if (c < cols) {
+#pragma unroll 8
+        for (int64_t i = warp; i < groups; i += 16) sum += sums[i * ld + c];
+    }
+    mine[warp][lane] = sum;
+    __syncthreads();
+    if (warp > 0 || c >= cols) return;
+    sum = 0.f;
+    for (int w = 0; w < 16; ++w) sum += mine[w][lane];
+    out[c] = sum;
+}
+
+// ---- plans -----------------------------------------------------------------------------------------------------------
+static int up_to(int64_t x, int to) { return (int)((x + to - 1) / to * to); }
+static int64_t aligned128(int64_t x) { return (x + 127) / 128 * 128; }
+static int parts_of(int type) { return type == RIPPLE_TYPE_F32 ? 3 : 1; }
+static int cols_of(int type) { return type == RIPPLE_TYPE_F32 ? 128 : 256; }
+
+// Whether TMA can read a matrix where it lies.
+static bool readable(int type, const void* p, int64_t ld, int64_t cols) {
+    return type != RIPPLE_TYPE_F32 && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 && ld >= cols && ld < (1ll << 36);
+}
+static bool writable(int size, const void* p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0 && ld * size % 32 == 0; }
+
+struct Slots {
+    int64_t at = 0;
+    int64_t take(int64_t bytes) {
+        const int64_t here = at;
+        at += aligned128(bytes);
+        return here;
+    }
+};
+
+struct Operand { int64_t at = -1, ld = 0, plane = 0; };      // at: in the workspace; -1: read where it is
+static Operand operand(Slots& s, int type, const void* p, int64_t ld, int64_t rows, int64_t cols, bool copy) {
+    Operand o;
+    if (!copy && readable(type, p, ld, cols)) return o;
+    o.ld = up_to(cols, 8), o.plane = aligned128(rows * o.ld * 2) / 2;
+    o.at = s.take(parts_of(type) * o.plane * 2);
+    return o;
+}
+
+struct LossPlan {
+    Operand x, w;
+    int64_t sums, at_label, bytes;
+    int col_tiles;
+};
+static LossPlan plan_loss(const ripple_loss_rows_args& a) {
+    LossPlan l = {};
+    Slots s;
+    l.x = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, false), l.w = operand(s, a.type, a.W, a.ld_w, a.k, a.n, false);
+    l.col_tiles = (a.n + cols_of(a.type) - 1) / cols_of(a.type);
+    l.sums = s.take(2ll * l.col_tiles * a.rows * 8), l.at_label = s.take(a.rows * 4);
+    l.bytes = s.at;
+    return l;
+}
+
+// Entries of g that are in memory at once (whole tiles of columns of all rows, one tile at least).
+constexpr int64_t LS_PIECE = 1ll << 27;
+
+// A product C [m, n] over k: how many parts k is split into so that every pair of SMs has work, each at least eight chunks long.
+static int splits_of(int type, int64_t m, int64_t n, int64_t k) {
+    const int64_t tiles = ((m + LS_ROWS - 1) / LS_ROWS) * ((n + cols_of(type) - 1) / cols_of(type)), chunks = (k + LS_KC - 1) / LS_KC;
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(LS_PAIRS / tiles, chunks / 8));
+    const int64_t each = (chunks + splits - 1) / splits;
+    return (int)((chunks + each - 1) / each);
+}
+
+struct GradPlanLoss {
+    Operand x, x_clean, w;
+    int piece, pieces;
+    int64_t g, ld_g, g_plane, g_sums, control, dx, ld_dx, dw, ld_dw, bytes;     // dx, dw: -1: written where the caller wants them
+    int dx_splits, dw_splits;
+};
+static GradPlanLoss plan_loss_grad(const ripple_loss_rows_grad_args& a) {
+    GradPlanLoss l = {};
+    Slots s;
+    l.control = s.take(sizeof(RowControl));
+    l.x = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, false), l.w = operand(s, a.type, a.W, a.ld_w, a.k, a.n, false);
+    if (a.dW && l.x.at < 0) l.x_clean = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, true);
+    const int cols = cols_of(a.type), parts = parts_of(a.type), all = up_to(a.n, 64);
+    l.piece = (int)std::min<int64_t>(all, std::max<int64_t>(cols, LS_PIECE / std::max<int64_t>(a.rows, 1) / cols * cols));
+    l.pieces = (a.n + l.piece - 1) / l.piece;
+    l.ld_g = l.piece, l.g_plane = aligned128(a.rows * l.ld_g * 2) / 2;
+    if (a.dx || a.dW) l.g = s.take(parts * l.g_plane * 2);
+    if (a.dbias) l.g_sums = s.take((a.rows + 31) / 32 * l.ld_g * 4);
+    const int out_size = type_size(a.type);
+    l.dx = l.dw = -1;
+    if (a.dx) {
+        l.dx_splits = splits_of(a.type, a.rows, a.k, l.piece);
+        l.ld_dx = up_to(a.k, 8);
+        if (l.pieces > 1 || l.dx_splits > 1 || !writable(out_size, a.dx, a.ld_dx)) l.dx = s.take(l.dx_splits * a.rows * l.ld_dx * 4);
+    }
+    if (a.dW) {
+        l.dw_splits = splits_of(a.type, a.k, l.piece, a.rows);
+        l.ld_dw = l.piece;
+        if (l.dw_splits > 1 || !writable(out_size, a.dW, a.ld_dw) || (int64_t)l.piece * out_size % 32) l.dw = s.take(l.dw_splits * (int64_t)a.k * l.ld_dw * 4);
+    }
+    l.bytes = s.at;
+    return l;
+}
+
+// ---- launches ----------------------------------------------------------------------------------------------------------
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiled encode_tiled() {
+    static const EncodeTiled f = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) fn = nullptr;
+        return reinterpret_cast<EncodeTiled>(fn);
+    }();
+    return f;
+}
+
+// A matrix of 16-bit planes in memory, rows `ld` apart.
+struct Matrix {
+    const void* p;
+    int64_t rows, cols, ld, plane;
+    int planes;
+};
+// Boxes of 64 columns x `box` rows.
+static bool tensor_map(CUtensorMap* map, int type, const Matrix& x, int box) {
+    const cuuint64_t dims[3] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows, (cuuint64_t)x.planes};
+    const cuuint64_t strides[2] = {(cuuint64_t)x.ld * 2, (cuuint64_t)(x.planes > 1 ? x.plane * 2 : x.ld * 2 * x.rows)};
+    const cuuint32_t boxes[3] = {64, (cuuint32_t)box, 1}, steps[3] = {1, 1, 1};
+    const EncodeTiled encode = encode_tiled();
+    return encode && encode(map, type == RIPPLE_TYPE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(x.p), dims, strides, boxes, steps,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// a [.., k] (A_ACROSS: [k, ..]), b [.., k] (B_ACROSS: [k, ..])
+template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END>
+static cudaError_t launch_product(ProductParams p, const Matrix& a, const Matrix* a_clean, const Matrix& b, int splits, void* stream) {
+    using S = LossShape<TYPE>;
+    auto* const kernel = k_product<TYPE, A_ACROSS, B_ACROSS, END>;
+    static bool ready[64];
+    cudaError_t e = allow_shared(kernel, (int)S::BYTES, ready);
+    if (e != cudaSuccess) return e;
+    if (!tensor_map(&p.a, TYPE, a, A_ACROSS ? 64 : 128) || !tensor_map(&p.a_clean, TYPE, a_clean ? *a_clean : a, A_ACROSS ? 64 : 128) ||
+        !tensor_map(&p.b, TYPE, b, B_ACROSS ? 64 : S::COLS / 2))
+        return cudaErrorInvalidValue;
+    p.row_tiles = (p.m + LS_ROWS - 1) / LS_ROWS, p.col_tiles = (p.n + S::COLS - 1) / S::COLS;
+    const int chunks = (p.k + LS_KC - 1) / LS_KC;
+    p.split_chunks = (chunks + splits - 1) / splits, p.splits = (chunks + p.split_chunks - 1) / p.split_chunks;      // (none empty)
+    const char* const withhold = std::getenv("RIPPLE_DEBUG_TC_WITHHOLD");
+    p.withhold = withhold && withhold[0] == '1';
+    const int64_t all = (int64_t)p.row_tiles * p.col_tiles * p.splits;
+    return launch(kernel, dim3((unsigned)(2 * std::min<int64_t>(all, std::max(1, sm_count() / 2)))), LS_THREADS, S::BYTES, stream, p);
+}
+
+template <int TYPE>
+static cudaError_t launch_operand(const void* from, int64_t ld_from, int64_t rows, int64_t cols, const Operand& o, uint8_t* work, const int32_t* labels, int classes,
+                                  const RowControl* control, void* stream) {
+    OperandParams p = {from, rows, ld_from, (int)cols, 1, reinterpret_cast<uint16_t*>(work + o.at), o.ld, o.plane, labels, classes, control};
+    while (p.lanes < 256 && p.lanes * 8 < o.ld) p.lanes *= 2;
+    const int64_t blocks = (rows * p.lanes + 255) / 256;
+    return launch(k_operand<typename Elem<TYPE>::T>, dim3((unsigned)std::min<int64_t>(blocks, (int64_t)sm_count() * 16)), 256, 0, stream, p);
+}
+
+static Matrix matrix_of(const Operand& o, int type, const void* p, int64_t ld, int64_t rows, int64_t cols, const uint8_t* work) {
+    if (o.at < 0) return {p, rows, cols, ld, 0, 1};
+    return {work + o.at, rows, cols, o.ld, o.plane, parts_of(type)};
+}
+
+template <int TYPE>
+static cudaError_t run_loss(const ripple_loss_rows_args& a) {
+    const LossPlan l = plan_loss(a);
+    uint8_t* const work = static_cast<uint8_t*>(a.workspace);
+    cudaError_t e = cudaSuccess;
+    if (l.x.at >= 0) e = launch_operand<TYPE>(a.x, a.ld_x, a.rows, a.k, l.x, work, nullptr, 0, nullptr, a.cuda_stream);
+    if (e == cudaSuccess && l.w.at >= 0) e = launch_operand<TYPE>(a.W, a.ld_w, a.k, a.n, l.w, work, nullptr, 0, nullptr, a.cuda_stream);
+    if (e != cudaSuccess) return e;
+    ProductParams p = {};
+    p.m = (int)a.rows, p.n = a.n, p.k = a.k;
+    p.bias = a.bias, p.labels = a.labels, p.classes = a.n;
+    p.sums = reinterpret_cast<float2*>(work + l.sums), p.at_label = reinterpret_cast<float*>(work + l.at_label);
+    e = launch_product<TYPE, false, true, END_LSE>(p, matrix_of(l.x, a.type, a.x, a.ld_x, a.rows, a.k, work), nullptr, matrix_of(l.w, a.type, a.W, a.ld_w, a.k, a.n, work), 1, a.cuda_stream);
+    if (e != cudaSuccess) return e;
+    return launch(k_finish_loss, dim3((unsigned)((a.rows + 31) / 32)), 512, 0, a.cuda_stream, (const float2*)p.sums, 2 * l.col_tiles, a.rows, (const float*)p.at_label, a.labels, a.n, a.loss, a.lse);
+}
+
+template <typename T>
+static cudaError_t join_parts(const float* parts, int splits, int64_t stride, int64_t ld, void* out, int64_t ld_out, int64_t rows, int cols, void* stream) {
+    return launch(k_join_parts<T>, dim3((unsigned)((cols + 1023) / 1024), (unsigned)std::min<int64_t>(rows, 16384)), 256, 0, stream, parts, splits, stride, ld, static_cast<T*>(out), ld_out, rows, cols);
+}
+
+template <int TYPE>
+static cudaError_t run_loss_grad(const ripple_loss_rows_grad_args& a) {
+    using T = typename Elem<TYPE>::T;
+    const GradPlanLoss l = plan_loss_grad(a);
+    uint8_t* const work = static_cast<uint8_t*>(a.workspace);
+    void* const stream = a.cuda_stream;
+    RowControl* const control = reinterpret_cast<RowControl*>(work + l.control);
+    const bool look_in_x = l.x_clean.at >= 0;
+    cudaError_t e = cudaSuccess;
+    if (look_in_x || TYPE == RIPPLE_TYPE_F16)
+        e = launch(k_look_at_rows<T>, dim3(LS_CONTROL), 256, 0, stream, look_in_x ? static_cast<const T*>(a.x) : nullptr, a.ld_x, a.k, a.labels, a.dloss, a.rows, a.n, control);
+    if (e == cudaSuccess && l.x.at >= 0) e = launch_operand<TYPE>(a.x, a.ld_x, a.rows, a.k, l.x, work, a.labels, a.n, nullptr, stream);
+    if (e == cudaSuccess && look_in_x) e = launch_operand<TYPE>(a.x, a.ld_x, a.rows, a.k, l.x_clean, work, a.labels, a.n, control, stream);
+    if (e == cudaSuccess && l.w.at >= 0) e = launch_operand<TYPE>(a.W, a.ld_w, a.k, a.n, l.w, work, nullptr, 0, nullptr, stream);
+    if (e != cudaSuccess) return e;
+    const Matrix x = matrix_of(l.x, a.type, a.x, a.ld_x, a.rows, a.k, work), w = matrix_of(l.w, a.type, a.W, a.ld_w, a.k, a.n, work);
+    const Matrix x_clean = look_in_x ? matrix_of(l.x_clean, a.type, a.x, a.ld_x, a.rows, a.k, work) : x;
+    for (int c0 = 0; c0 < a.n; c0 += l.piece) {
+        const int classes = std::min(l.piece, a.n - c0);
+        ProductParams p = {};
+        p.m = (int)a.rows, p.n = classes, p.k = a.k, p.b_col0 = c0;
+        p.bias = a.bias ? a.bias + c0 : nullptr, p.labels = a.labels, p.class0 = c0, p.classes = a.n;
+        p.lse = a.lse, p.dloss = a.dloss, p.scale = a.scale;
+        p.ld_g = l.ld_g, p.g_plane = l.g_plane;
+        if (a.dx || a.dW) p.g = reinterpret_cast<uint16_t*>(work + l.g);
+        if (a.dbias) p.g_sums = reinterpret_cast<float*>(work + l.g_sums);
+        p.control = TYPE == RIPPLE_TYPE_F16 ? control : nullptr;
+        // (rows without labels are zeros in g whatever their logits: x as it is)
+        const Matrix* const same = TYPE == RIPPLE_TYPE_F16 ? &x : nullptr;
+        e = launch_product<TYPE, false, true, END_GRAD>(p, x, same, w, 1, stream);
+        if (e != cudaSuccess) return e;
+        if (a.dbias && (e = launch(k_join_columns, dim3((unsigned)(classes + 31) / 32), 512, 0, stream, (const float*)p.g_sums, (a.rows + 31) / 32, l.ld_g, classes, a.dbias + c0)) != cudaSuccess) return e;
+        const Matrix g{work + l.g, a.rows, classes, l.ld_g, l.g_plane, parts_of(TYPE)};
+        ProductParams o = {};
+        o.unscale = TYPE == RIPPLE_TYPE_F16, o.scale = a.scale, o.classes = a.n;
+        if (a.dx) {
+            ProductParams d = o;
+            d.m = (int)a.rows, d.n = a.k, d.k = classes, d.b_k0 = c0, d.control = p.control, d.dead_rows = a.labels;
+            if (l.dx < 0) d.out = a.dx, d.ld_out = a.ld_dx, d.out_f32 = TYPE == RIPPLE_TYPE_F32;
+            else d.out = work + l.dx, d.ld_out = l.ld_dx, d.split_stride = a.rows * l.ld_dx, d.out_f32 = 1, d.add_to_out = c0 > 0;
+            // (the last piece may be too short for all parts: the last of them keep what they have)
+            e = launch_product<TYPE, false, false, END_OUT>(d, g, &g, w, l.dx_splits, stream);
+            if (e != cudaSuccess) return e;
+        }
+        if (a.dW) {
+            ProductParams d = o;
+            d.m = a.k, d.n = classes, d.k = (int)a.rows;
+            d.control = look_in_x || TYPE == RIPPLE_TYPE_F16 ? control : nullptr;
+            if (l.dw < 0) d.out = static_cast<T*>(a.dW) + c0, d.ld_out = a.ld_dw, d.out_f32 = TYPE == RIPPLE_TYPE_F32;
+            else d.out = work + l.dw, d.ld_out = l.ld_dw, d.split_stride = a.k * l.ld_dw, d.out_f32 = 1;
+            e = launch_product<TYPE, true, true, END_OUT>(d, x, &x_clean, g, l.dw_splits, stream);
+            if (e == cudaSuccess && l.dw >= 0) e = join_parts<T>(static_cast<const float*>(d.out), l.dw_splits, d.split_stride, d.ld_out, static_cast<T*>(a.dW) + c0, a.ld_dw, a.k, classes, stream);
+            if (e != cudaSuccess) return e;
+        }
+    }
+    if (a.dx && l.dx >= 0) e = join_parts<T>(reinterpret_cast<const float*>(work + l.dx), l.dx_splits, a.rows * l.ld_dx, l.ld_dx, a.dx, a.ld_dx, a.rows, a.k, stream);
+    return e;
+}
+
+}  // namespace rp
+
+using namespace rp;
+
+#define REFUSE(...)                        \
+    do {                                   \
+        note_error(WHAT ": " __VA_ARGS__); \
+        return RIPPLE_ERR_INVALID_ARG;     \
+    } while (0)
+
+template <typename A> static bool loss_sizes_ok(const A* a) {
+    return a->rows >= 0 && a->rows <= INT32_MAX - LS_ROWS && type_ok(a->type) && a->k >= 1 && a->k <= RIPPLE_MAX_LOSS_K && a->n >= 1 && a->n <= RIPPLE_MAX_CLASSES;
+}
+
+extern "C" int64_t ripple_loss_rows_workspace_bytes(const ripple_loss_rows_args* a) { return a && loss_sizes_ok(a) ? plan_loss(*a).bytes : -1; }
+extern "C" int64_t ripple_loss_rows_grad_workspace_bytes(const ripple_loss_rows_grad_args* a) { return a && loss_sizes_ok(a) ? plan_loss_grad(*a).bytes : -1; }
+
+#define WHAT "loss_rows"
+extern "C" ripple_status ripple_loss_rows(const ripple_loss_rows_args* a) {
+    if (!a) REFUSE("null arguments");
+    if (!loss_sizes_ok(a)) REFUSE("rows, type, k or n out of range");
+    if (a->ld_x < 0 || a->ld_w < 0) REFUSE("negative leading dimension");
+    if (a->rows > 0 && (!a->x || !a->W || !a->labels || !a->lse)) REFUSE("null x, W, labels or lse");
+    const int ts = type_size(a->type);
+    for (auto [ptr, size] : {std::pair<const void*, int>{a->x, ts}, {a->W, ts}, {a->bias, 4}, {a->labels, 4}, {a->loss, 4}, {a->lse, 4}})
+        if (reinterpret_cast<uintptr_t>(ptr) % size) REFUSE("misaligned pointer");
+    if (a->rows == 0) return RIPPLE_OK;
+    const int64_t need = plan_loss(*a).bytes;
+    if (a->workspace_bytes < need || !a->workspace) REFUSE("workspace too small");
+    if (reinterpret_cast<uintptr_t>(a->workspace) & 127) REFUSE("misaligned workspace");
+    const Extent x{a->x, a->rows, a->ld_x, a->k, ts}, W{a->W, a->k, a->ld_w, a->n, ts}, bias{a->bias, 1, 1, a->n, 4}, labels{a->labels, a->rows, 1, 1, 4},
+        loss{a->loss, a->rows, 1, 1, 4}, lse{a->lse, a->rows, 1, 1, 4}, work{a->workspace, 1, 1, need, 1};
+    for (const Extent* out : {&loss, &lse, &work})
+        for (const Extent* in : {&x, &W, &bias, &labels})
+            if (extents_meet(*out, *in)) REFUSE("an output or the workspace overlaps an input");
+    if (extents_meet(loss, lse) || extents_meet(loss, work) || extents_meet(lse, work)) REFUSE("outputs or workspace overlap");
+    OnDevice on(a->device);
+    if (on.err != cudaSuccess) return launch_failed("cudaSetDevice", on.err);
+    const cudaError_t e = a->type == RIPPLE_TYPE_F32 ? run_loss<RIPPLE_TYPE_F32>(*a) : a->type == RIPPLE_TYPE_BF16 ? run_loss<RIPPLE_TYPE_BF16>(*a) : run_loss<RIPPLE_TYPE_F16>(*a);
+    return e == cudaSuccess ? RIPPLE_OK : launch_failed("loss_rows launch", e);
+}
+#undef WHAT
+
+#define WHAT "loss_rows_grad"
+extern "C" ripple_status ripple_loss_rows_grad(const ripple_loss_rows_grad_args* a) {
+    if (!a) REFUSE("null arguments");
+    if (!loss_sizes_ok(a)) REFUSE("rows, type, k or n out of range");
+    if (!a->dx && !a->dW && !a->dbias) REFUSE("no output");
+    if (a->ld_x < 0 || a->ld_w < 0 || (a->dx && a->ld_dx < a->k) || (a->dW && a->ld_dw < a->n)) REFUSE("leading dimension negative, or of an output below its width");
+    if (a->rows > 0 && (!a->x || !a->W || !a->labels || !a->lse)) REFUSE("null x, W, labels or lse");
+    const int ts = type_size(a->type);
+    for (auto [ptr, size] : {std::pair<const void*, int>{a->x, ts}, {a->W, ts}, {a->bias, 4}, {a->labels, 4}, {a->lse, 4}, {a->dloss, 4}, {a->dx, ts}, {a->dW, ts}, {a->dbias, 4}})
+        if (reinterpret_cast<uintptr_t>(ptr) % size) REFUSE("misaligned pointer");
+    const int64_t need = a->rows > 0 ? plan_loss_grad(*a).bytes : 0;
+    if (a->workspace_bytes < need || (need > 0 && !a->workspace)) REFUSE("workspace too small");
+    if (reinterpret_cast<uintptr_t>(a->workspace) & 127) REFUSE("misaligned workspace");
+    const Extent x{a->x, a->rows, a->ld_x, a->k, ts}, W{a->W, a->k, a->ld_w, a->n, ts}, bias{a->bias, 1, 1, a->n, 4}, labels{a->labels, a->rows, 1, 1, 4},
+        lse{a->lse, a->rows, 1, 1, 4}, dloss{a->dloss, a->rows, 1, 1, 4}, dx{a->dx, a->rows, a->ld_dx, a->k, ts}, dW{a->dW, a->k, a->ld_dw, a->n, ts},
+        db{a->dbias, 1, 1, a->n, 4}, work{need > 0 ? a->workspace : nullptr, 1, 1, need, 1};
+    for (const Extent* out : {&dx, &dW, &db, &work})
+        for (const Extent* in : {&x, &W, &bias, &labels, &lse, &dloss})
+            if (extents_meet(*out, *in)) REFUSE("an output or the workspace overlaps an input");
+    for (auto [p, q] : {std::pair<const Extent*, const Extent*>{&dx, &dW}, {&dx, &db}, {&dx, &work}, {&dW, &db}, {&dW, &work}, {&db, &work}})
+        if (extents_meet(*p, *q)) REFUSE("outputs or workspace overlap");
+    OnDevice on(a->device);
+    if (on.err != cudaSuccess) return launch_failed("cudaSetDevice", on.err);
+    cudaError_t e = cudaSuccess;
+    if (a->rows == 0) {          // sums of nothing
+        cudaStream_t stream = static_cast<cudaStream_t>(a->cuda_stream);
+        if (a->dW) e = cudaMemset2DAsync(a->dW, (size_t)a->ld_dw * ts, 0, (size_t)a->n * ts, (size_t)a->k, stream);
+        if (e == cudaSuccess && a->dbias) e = cudaMemsetAsync(a->dbias, 0, (size_t)a->n * 4, stream);
+    } else {
+        e = a->type == RIPPLE_TYPE_F32 ? run_loss_grad<RIPPLE_TYPE_F32>(*a) : a->type == RIPPLE_TYPE_BF16 ? run_loss_grad<RIPPLE_TYPE_BF16>(*a) : run_loss_grad<RIPPLE_TYPE_F16>(*a);
+    }
+    return e == cudaSuccess ? RIPPLE_OK : launch_failed("loss_rows_grad launch", e);
+}

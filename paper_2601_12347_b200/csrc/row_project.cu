@@ -1529,13 +1529,15 @@ extern "C" ripple_status ripple_project_rows(const ripple_project_rows_args* a) 
 extern "C" ripple_status ripple_request_status(int32_t device) {
     OnDevice on(device);
     if (on.err != cudaSuccess) return launch_failed("cudaSetDevice", on.err);
-    int gave_up = 0;
+    int gave_up = 0, in_loss = 0;
     const int zero = 0;
     cudaError_t e = cudaDeviceSynchronize();
     if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&gave_up, g_request_timeout, sizeof(int));
     if (e == cudaSuccess && gave_up) e = cudaMemcpyToSymbol(g_request_timeout, &zero, sizeof(int));
+    if (e == cudaSuccess) e = take_loss_timeout(&in_loss);
     if (e != cudaSuccess) return launch_failed("request_status", e);
-    if (!gave_up) return RIPPLE_OK;
-    note_error("project_rows: a bounded device-side wait gave up; the results of calls since the last query are not to be used");
+    if (!gave_up && !in_loss) return RIPPLE_OK;
+    note_error(gave_up ? "project_rows: a bounded device-side wait gave up; the results of calls since the last query are not to be used"
+                       : "loss_rows: a bounded device-side wait gave up; the results of calls since the last query are not to be used");
     return RIPPLE_ERR_TIMEOUT;
 }

@@ -1,0 +1,209 @@
+"""Operators that train a head on the cached rows: include/ripple.h, "Training".
+
+What requests run (serve.py) has weights; these are fitted here, minibatch by minibatch, to labels of some vertices:
+
+    lookup_rows        y_i = scale * table[ids_i]:  learned rows beside the cached ones
+    lookup_rows_grad   dtable[r] = scale * sum of dy_i over the i with ids_i = r
+    norm_rows_grad     dx, dweight, dbias of n = norm(x[ids]) (serve.norm_rows)
+    loss_rows          softmax cross entropy of x W + bias over many classes, without the logits in memory
+    loss_rows_grad     dx, dW, dbias of it
+
+Gradients are calls of their own; nothing is recorded, and inputs that require gradients are refused while PyTorch records them (call
+under torch.no_grad() or with detached tensors).  As with requests everything runs on the current CUDA stream of the tensors' device (not
+necessarily the current device) and returns once it is launched; calls can be captured into CUDA graphs; outputs and scratch come from PyTorch's
+allocator, so every call and every captured graph has its own.  Sums are fp32 and formed in a fixed order: the same call gives the same
+bits.  Rows are fp32, bf16 or fp16.  Padding (ids or labels outside their range, -1 by custom) gives rows of zeros and adds nothing to
+any gradient, whatever its rows hold.
+"""
+from __future__ import annotations
+
+import struct
+
+import torch
+from torch.autograd import forward_ad
+
+from . import ripple as _ripple
+from .serve import TYPE_F32, Norm, _check, _device_of, _matrix, _refuse_tangents, _stream, _type_of, _vector
+
+# ripple_lookup_rows_args, ripple_lookup_rows_grad_args, ripple_norm_rows_grad_args
+_LOOKUP_ARGS = struct.Struct("=q4i QqqQ Qq fi Q")
+_LOOKUP_GRAD_ARGS = struct.Struct("=q4i QqQ Qqq fi Qq Q")
+_NORM_GRAD_ARGS = struct.Struct("=q4i Qq QqqQ Qq Qq QQ ifQQ Qq Q")
+# ripple_loss_rows_args, ripple_loss_rows_grad_args
+_LOSS_ARGS = struct.Struct("=q4i QqQq QQQQ Qq Q")
+_LOSS_GRAD_ARGS = struct.Struct("=q4i QqQq QQQQ QqQqQ fi Qq Q")
+
+
+def _tangents(**tensors) -> None:
+    if getattr(forward_ad, "_current_level", 0) >= 0:
+        _refuse_tangents(**tensors)
+
+
+def _ids(ids, index: int):
+    if getattr(ids, "dim", lambda: 0)() != 1:
+        raise ValueError("ids: one dimension expected")
+    rows = ids.shape[0]
+    return _vector(ids, "ids", rows, torch.int32, index), rows
+
+
+def _workspace(need: int, like):
+    """Scratch of one call, from the allocator: it keeps the memory until the stream has passed the call."""
+    return torch.empty(need, dtype=torch.uint8, device=like.device) if need > 0 else None
+
+
+def _or_null(t) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def lookup_rows(table, ids, scale: float = 1.0, out=None, out_dtype=None):
+    """scale * table[ids], one row per id (int32), zeros for ids outside the table.  The result has the table's type, or the one that
+    out_dtype (or out) says if the table is fp32."""
+    _tangents(table=table, out=out)
+    index = _device_of(table, "table")
+    ptr, ld, table_rows = _matrix(table, "table", None, None, index)
+    width = table.shape[1]
+    ids_ptr, rows = _ids(ids, index)
+    if out is None:
+        out = torch.empty((rows, width), dtype=out_dtype or table.dtype, device=table.device)
+        out_ptr, out_ld = out.data_ptr(), width
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError(f"out: {out_dtype} expected, got {out.dtype}")
+        out_ptr, out_ld, got = _matrix(out, "out", width, None, index)
+        if got != rows:
+            raise ValueError(f"out: {rows} rows expected, got {got}")
+    t, to = _type_of(table.dtype, "table"), _type_of(out.dtype, "out")
+    if to != t and t != TYPE_F32:
+        raise TypeError(f"out: {table.dtype} expected, got {out.dtype}")
+    _check(_ripple.load_library().ripple_lookup_rows(_LOOKUP_ARGS.pack(
+        rows, width, t, to, index, ptr, ld, table_rows, ids_ptr, out_ptr, out_ld, float(scale), 0, _stream(index))))
+    return out
+
+
+def lookup_rows_grad(dy, ids, table_rows: int, scale: float = 1.0, out=None, out_dtype=None, accumulate: bool = False):
+    """The gradient of lookup_rows' table: [table_rows, D], row r = scale * the sum of dy's rows whose id is r; of dy's type, or fp32 if
+    out_dtype (or out) says so.  accumulate: add to the rows of `out` that ids name, once for each, and touch no other."""
+    _tangents(dy=dy, out=out)
+    index = _device_of(dy, "dy")
+    ptr, ld, rows = _matrix(dy, "dy", None, None, index)
+    width = dy.shape[1]
+    ids_ptr, named = _ids(ids, index)
+    if named != rows:
+        raise ValueError(f"ids: {rows} entries expected, got {named}")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate without out")
+        out = torch.empty((int(table_rows), width), dtype=out_dtype or dy.dtype, device=dy.device)
+        out_ptr, out_ld = out.data_ptr(), width
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError(f"out: {out_dtype} expected, got {out.dtype}")
+        out_ptr, out_ld, got = _matrix(out, "out", width, None, index)
+        if got != table_rows:
+            raise ValueError(f"out: {table_rows} rows expected, got {got}")
+    t, to = _type_of(dy.dtype, "dy"), _type_of(out.dtype, "out")
+    if to not in (t, TYPE_F32):
+        raise TypeError(f"out: {dy.dtype} or float32 expected, got {out.dtype}")
+    lib = _ripple.load_library()
+    head = (rows, width, t, to, index, ptr, ld, ids_ptr, out_ptr, out_ld, int(table_rows), float(scale), bool(accumulate))
+    need = lib.ripple_lookup_rows_grad_workspace_bytes(_LOOKUP_GRAD_ARGS.pack(*head, 0, 0, 0))
+    work = _workspace(need, dy)
+    _check(lib.ripple_lookup_rows_grad(_LOOKUP_GRAD_ARGS.pack(*head, _or_null(work), max(need, 0), _stream(index))))
+    return out
+
+
+def norm_rows_grad(dn, x, norm: Norm, ids=None, add=None, out=None, vectors: bool = True):
+    """(dx, dweight, dbias) of n = norm(x[ids]) from dn [rows, D]; dweight and dbias (fp32) are None where the norm has no such
+    vector, or with vectors=False.  x [any, D]: dn's type or fp32; row ids[i] (int32) of it, or row i, was normalised.  dx [rows, D] has x's type; add [rows, D],
+    of the same type: what reaches x past the norm, added before dx is rounded.  out: where to write dx; it may be dn, add, or, without ids, x."""
+    if not isinstance(norm, Norm):
+        raise TypeError(f"norm: a Norm expected, got {type(norm).__name__}")
+    _tangents(dn=dn, x=x, add=add, out=out)
+    index = _device_of(dn, "dn")
+    dn_ptr, dn_ld, rows = _matrix(dn, "dn", None, None, index)
+    width = dn.shape[1]
+    x_ptr, x_ld, x_rows = _matrix(x, "x", width, None, index)
+    t, tx = _type_of(dn.dtype, "dn"), _type_of(x.dtype, "x")
+    if tx not in (t, TYPE_F32):
+        raise TypeError(f"x: {dn.dtype} or float32 expected, got {x.dtype}")
+    ids_ptr = add_ptr = add_ld = 0
+    if ids is not None:
+        ids_ptr, named = _ids(ids, index)
+        if named != rows:
+            raise ValueError(f"ids: {rows} entries expected, got {named}")
+    elif x_rows != rows:
+        raise ValueError(f"x: {rows} rows expected, got {x_rows}")
+    if add is not None:
+        add_ptr, add_ld, got = _matrix(add, "add", width, x.dtype, index)
+        if got != rows:
+            raise ValueError(f"add: {rows} rows expected, got {got}")
+    if out is None:
+        out = torch.empty((rows, width), dtype=x.dtype, device=dn.device)
+        out_ptr, out_ld = out.data_ptr(), width
+    else:
+        out_ptr, out_ld, got = _matrix(out, "out", width, x.dtype, index)
+        if got != rows:
+            raise ValueError(f"out: {rows} rows expected, got {got}")
+    dweight = torch.empty(width, dtype=torch.float32, device=dn.device) if vectors and norm.weight is not None else None
+    dbias = torch.empty(width, dtype=torch.float32, device=dn.device) if vectors and norm.bias is not None else None
+    lib = _ripple.load_library()
+    stream = _stream(index)
+    head = (rows, width, t, tx, index, dn_ptr, dn_ld, x_ptr, x_ld, x_rows, ids_ptr, add_ptr, add_ld, out_ptr, out_ld,
+            _or_null(dweight), _or_null(dbias), *norm._packed(width, index, stream, "norm"))
+    need = lib.ripple_norm_rows_grad_workspace_bytes(_NORM_GRAD_ARGS.pack(*head, 0, 0, 0))
+    work = _workspace(need, dn)
+    _check(lib.ripple_norm_rows_grad(_NORM_GRAD_ARGS.pack(*head, _or_null(work), max(need, 0), stream)))
+    return out, dweight, dbias
+
+
+def _linear(x, W, labels, bias):
+    """What both calls of the loss check of their inputs: sizes, addresses."""
+    index = _device_of(x, "x")
+    x_ptr, x_ld, rows = _matrix(x, "x", None, None, index)
+    K = x.shape[1]
+    w_ptr, w_ld, wk = _matrix(W, "W", None, x.dtype, index)
+    if wk != K:
+        raise ValueError(f"W: {K} rows expected, got {wk}")
+    t = _type_of(x.dtype, "x")
+    labels_ptr = _vector(labels, "labels", rows, torch.int32, index)
+    bias_ptr = 0 if bias is None else _vector(bias, "bias", W.shape[1], torch.float32, index)
+    return index, rows, (rows, t, K, W.shape[1], index, x_ptr, x_ld, w_ptr, w_ld, bias_ptr, labels_ptr)
+
+
+def loss_rows(x, W, labels, bias=None):
+    """(loss, lse), fp32 [rows]: lse_i = log sum_c exp z_ic, loss_i = lse_i - z_i,label with z = x W + bias; 0 for labels (int32) that are no
+    class.  x [rows, K] and W [K, N] of one type, bias fp32; a bias of minus infinity takes a class out."""
+    _tangents(x=x, W=W, bias=bias)
+    index, rows, head = _linear(x, W, labels, bias)
+    loss, lse = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
+    head = (*head, loss.data_ptr(), lse.data_ptr())
+    lib = _ripple.load_library()
+    need = lib.ripple_loss_rows_workspace_bytes(_LOSS_ARGS.pack(*head, 0, 0, 0))
+    work = _workspace(need, x)
+    _check(lib.ripple_loss_rows(_LOSS_ARGS.pack(*head, _or_null(work), max(need, 0), _stream(index))))
+    return loss, lse
+
+
+def loss_rows_grad(x, W, labels, lse, dloss=1.0, bias=None, dx: bool = True, dW: bool = True):
+    """(dx, dW, dbias) of loss_rows, from what it gave as lse and dloss: fp32 [rows], or a number for all rows.  dx [rows, K] and
+    dW [K, N] have the type of x and W (None where they are not wanted), dbias is fp32 (None without bias).  What each row adds is
+    dloss_i (softmax(z)_i - onehot(label_i)): formed anew from x and W, in pieces of the classes."""
+    _tangents(x=x, W=W, bias=bias, lse=lse, dloss=dloss)
+    index, rows, head = _linear(x, W, labels, bias)
+    lse_ptr = _vector(lse, "lse", rows, torch.float32, index)
+    scale, dloss_ptr = 1.0, 0
+    if isinstance(dloss, torch.Tensor):
+        dloss_ptr = _vector(dloss, "dloss", rows, torch.float32, index)
+    else:
+        scale = float(dloss)
+    if not (dx or dW or bias is not None):
+        raise ValueError("no gradient wanted")
+    gx = torch.empty((rows, x.shape[1]), dtype=x.dtype, device=x.device) if dx else None
+    gw = torch.empty(W.shape, dtype=W.dtype, device=x.device) if dW else None
+    gb = torch.empty(W.shape[1], dtype=torch.float32, device=x.device) if bias is not None else None
+    head = (*head, lse_ptr, dloss_ptr, _or_null(gx), x.shape[1], _or_null(gw), W.shape[1], _or_null(gb), scale, 0)
+    lib = _ripple.load_library()
+    need = lib.ripple_loss_rows_grad_workspace_bytes(_LOSS_GRAD_ARGS.pack(*head, 0, 0, 0))
+    work = _workspace(need, x)
+    _check(lib.ripple_loss_rows_grad(_LOSS_GRAD_ARGS.pack(*head, _or_null(work), max(need, 0), _stream(index))))
+    return gx, gw, gb

@@ -1,0 +1,365 @@
+"""The operators that train a head (train.py) against their formulas in 64 bits.
+
+Tolerances.  u32 = 2^-24 is half a step of fp32; half a step of the output's type comes on top (near).  Sums are bounded by the number of
+additions that a term passes through, times u32, times the sum of the terms' magnitudes; what they are is derived at each check."""
+import math
+
+import pytest
+import torch
+
+from paper_2601_12347_b200 import serve, train
+
+import test_gpu_parity as P
+import test_gpu_requests as R
+
+pytestmark = pytest.mark.gpu
+env = P.env     # skips without a device, builds the library
+
+U32, G, F64, DTYPES = R.U32, R.G, R.F64, R.DTYPES
+near, rnd, gen, half_step = R.near, R.rnd, R.gen, R.half_step
+
+
+@pytest.fixture(autouse=True)
+def _device(env):
+    pass
+
+
+# ---- lookup_rows, lookup_rows_grad -----------------------------------------------------------------------------------
+def draw_ids(g, rows, table, skew=1.0, padding=0.05):
+    at = (torch.rand(rows, generator=g, device="cuda").double() ** skew * table).to(torch.int64).clamp(max=table - 1)
+    ids = torch.randperm(table, generator=g, device="cuda")[at].to(torch.int32)
+    bad = torch.tensor([-1, table, -2 ** 31, 2 ** 31 - 1], dtype=torch.int64, device="cuda").to(torch.int32)
+    which = torch.randint(0, 4, (rows,), generator=g, device="cuda")
+    return torch.where(torch.rand(rows, generator=g, device="cuda") < padding, bad[which], ids)
+
+
+def check_lookup(table, ids, scale=1.0, **kw):
+    got = train.lookup_rows(table, ids, scale=scale, **kw)
+    real = (ids >= 0) & (ids < table.shape[0])
+    want = torch.zeros(ids.shape[0], table.shape[1], dtype=F64, device="cuda")
+    want[real] = table[ids[real].long()].to(F64) * R.np.float32(scale).item()
+    near(got, want, U32 * want.abs())           # one product
+    return got
+
+
+def check_lookup_grad(dy, ids, table_rows, scale=1.0, out=None, accumulate=False, **kw):
+    before = out.clone() if accumulate else None
+    got = train.lookup_rows_grad(dy, ids, table_rows, scale=scale, out=out, accumulate=accumulate, **kw)
+    real = ((ids >= 0) & (ids < table_rows)).nonzero()[:, 0]
+    k = R.np.float32(scale).item()
+    want = torch.zeros(table_rows, dy.shape[1], dtype=F64, device="cuda")
+    mag = torch.zeros_like(want)
+    want.index_put_((ids[real].long(),), dy[real].to(F64) * k, accumulate=True)
+    mag.index_put_((ids[real].long(),), (dy[real].to(F64) * k).abs(), accumulate=True)
+    # a term passes through 32 additions at most (256 in calls of up to 256 rows), and 64 in every list of partial sums (five at most here),
+    # a product, an addition to what was there
+    tol = 580 * U32 * mag + 2 * U32 * want.abs()
+    if accumulate:
+        named = torch.zeros(table_rows, dtype=torch.bool, device="cuda")
+        named[ids[real].long()] = True
+        assert torch.equal(got[~named], before[~named])
+        want = want + before.to(F64)
+        tol = tol + U32 * want.abs()
+        want, tol, got = want[named], tol[named], got[named]
+    near(got, want, tol)
+    return got
+
+
+@pytest.mark.parametrize("width", [1, 2, 3, 7, 8, 32, 47, 100, 128, 250, 256, 602, 1024, 1027, 4096, 16384])
+@pytest.mark.parametrize("dtype,other", [("fp32", "fp32"), ("fp32", "bf16"), ("fp32", "fp16"), ("bf16", "bf16"), ("bf16", "fp32"), ("fp16", "fp16"), ("fp16", "fp32")])
+def test_lookups_of_every_width_and_type(width, dtype, other):
+    g = gen(width)
+    T, O = DTYPES[dtype], DTYPES[other]
+    table = rnd(g, 50, width, dtype=T)
+    for rows in (1, 37, 300):
+        ids = draw_ids(g, rows, 50)
+        if other == dtype or dtype == "fp32":
+            check_lookup(table, ids, scale=math.sqrt(width), out_dtype=O)
+        if other == dtype or other == "fp32":
+            check_lookup_grad(rnd(g, rows, width, dtype=T), ids, 50, scale=math.sqrt(width), out_dtype=O)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows", [0, 1, 2, 31, 32, 33, 255, 256, 257, 1000, 4095, 4096, 4097, 12_289, 70_001, 300_000])
+@pytest.mark.parametrize("table,skew", [(1, 1), (2, 1), (300, 3), (5000, 1), (100_000, 2)])
+def test_gradients_of_every_number_of_rows(dtype, rows, table, skew):
+    """Rows from none to many, all of one id and all of their own, hubs beside single rows."""
+    g = gen(rows + table)
+    ids = draw_ids(g, rows, table, skew)
+    check_lookup_grad(rnd(g, rows, 24, dtype=DTYPES[dtype]), ids, table)
+    if rows:
+        check_lookup(rnd(g, table, 24, dtype=DTYPES[dtype]), ids)
+
+
+@pytest.mark.parametrize("rows", [1, 200, 3000, 50_000])
+@pytest.mark.parametrize("dtype,out", [("fp32", "fp32"), ("bf16", "bf16"), ("fp16", "fp32")])
+def test_gradients_that_are_added(rows, dtype, out):
+    g = gen(rows)
+    ids = draw_ids(g, rows, 4000, 2)
+    check_lookup_grad(rnd(g, rows, 40, dtype=DTYPES[dtype]), ids, 4000, scale=0.5, out=rnd(g, 4000, 40, dtype=DTYPES[out]), accumulate=True)
+
+
+@pytest.mark.parametrize("rows", [5, 400, 9000])
+def test_lookups_over_strides_and_columns(rows):
+    """Rows that lie apart, columns of wider matrices, at every alignment."""
+    g = gen(rows)
+    for dtype in DTYPES.values():
+        for off, width in ((0, 64), (1, 64), (2, 30), (3, 47), (4, 100)):
+            wide = rnd(g, 600, 130, dtype=dtype)
+            ids = draw_ids(g, rows, 600, 2)
+            out = torch.full((rows, 128), 7.0, device="cuda", dtype=dtype)
+            check_lookup(wide[:, off:off + width], ids, out=out[:, off:off + width])
+            assert (out[:, :off] == 7).all() and (out[:, off + width:] == 7).all()
+            dy = rnd(g, rows, 130, dtype=dtype)[:, off:off + width]
+            out = torch.full((600, 128), 7.0, device="cuda", dtype=dtype)
+            check_lookup_grad(dy, ids, 600, out=out[:, off:off + width])
+            assert (out[:, :off] == 7).all() and (out[:, off + width:] == 7).all()
+    row = rnd(g, 1, 64)
+    check_lookup(row.expand(600, 64), draw_ids(g, rows, 600))
+    check_lookup_grad(row.expand(rows, 64), draw_ids(g, rows, 600), 600)
+
+
+@pytest.mark.parametrize("rows", [7, 200, 3000, 20_000])
+def test_padding_rows_may_hold_anything(rows):
+    g = gen(rows)
+    ids = draw_ids(g, rows, 50, padding=0.5)
+    dy = rnd(g, rows, 33)
+    dy[(ids < 0) | (ids >= 50)] = float("nan")
+    got = train.lookup_rows_grad(dy, ids, 50)
+    assert torch.isfinite(got).all()
+    assert (train.lookup_rows(rnd(g, 50, 33), torch.full((rows,), -1, dtype=torch.int32, device="cuda")) == 0).all()
+    assert (train.lookup_rows_grad(dy, torch.full((rows,), -5, dtype=torch.int32, device="cuda"), 50) == 0).all()
+    assert train.lookup_rows_grad(dy, ids, 0).shape == (0, 33)
+    assert (train.lookup_rows(torch.zeros(0, 33, device="cuda"), ids) == 0).all()
+
+
+def test_the_same_call_gives_the_same_bits():
+    g = gen(1)
+    ids = draw_ids(g, 200_000, 500, 3)
+    dy = rnd(g, 200_000, 96)
+    first = train.lookup_rows_grad(dy, ids, 500)
+    for _ in range(5):
+        assert torch.equal(first, train.lookup_rows_grad(dy, ids, 500))
+
+
+def test_tables_beyond_32_bits():
+    g = gen(2)
+    table = torch.zeros(600_000, 4096, dtype=torch.bfloat16, device="cuda")
+    ids = draw_ids(g, 5000, 600_000)
+    ids[:2] = torch.tensor([599_999, 0], dtype=torch.int32)
+    real = ids[(ids >= 0) & (ids < 600_000)].long().unique()
+    table[real] = rnd(g, len(real), 4096, dtype=torch.bfloat16)
+    got = train.lookup_rows(table, ids)
+    ok = ((ids >= 0) & (ids < 600_000)).nonzero()[:, 0]
+    assert torch.equal(got[ok], table[ids[ok].long()])
+    dy = rnd(g, 5000, 4096, dtype=torch.bfloat16)
+    train.lookup_rows_grad(dy, ids, 600_000, out=table)
+    want = torch.zeros(len(real), 4096, dtype=F64, device="cuda")
+    want.index_put_((torch.searchsorted(real, ids[ok].long()),), dy[ok].to(F64), accumulate=True)
+    near(table[real], want, 100 * U32 * want.abs().clamp(min=4))
+    table[real] = 0
+    assert not table.view(torch.int16).any()
+
+
+# ---- norm_rows_grad ------------------------------------------------------------------------------------------------
+def check_norm_grad(dn, x, norm, ids=None, add=None, **kw):
+    """With x^ off by t_x (as in norm_rows' test), d = dn w off by u32: means of D terms are off by G of the terms' magnitudes."""
+    dn64, add64 = dn.to(F64), None if add is None else add.to(F64)
+    rows, D = dn.shape
+    x64 = x.to(F64)
+    real = torch.ones(rows, dtype=torch.bool, device="cuda")
+    if ids is not None:
+        real = (ids >= 0) & (ids < x.shape[0])
+        x64 = x64[torch.where(real, ids, 0).long()]
+    got = train.norm_rows_grad(dn, x, norm, ids=ids, add=add, **kw)
+    dn64 = torch.where(real[:, None], dn64, 0.0)
+    w = norm.weight.to(F64) if norm.weight is not None else torch.ones(D, dtype=F64, device="cuda")
+    layer = norm.kind == serve.NORM_LAYER
+    mean = x64.mean(1, keepdim=True) if layer else 0.0
+    c = x64 - mean
+    c_tol = (G * x64.abs().mean(1, keepdim=True) if layer else 0.0) + U32 * c.abs()
+    inv = 1 / (c.square().mean(1, keepdim=True) + norm.eps).sqrt()
+    inv_rel = G + inv * c_tol.square().mean(1, keepdim=True).sqrt()
+    h = c * inv
+    h_tol = inv * c_tol + h.abs() * (1.1 * inv_rel + U32)
+    d = dn64 * w
+    m1 = d.mean(1, keepdim=True) if layer else torch.zeros_like(inv)
+    m1_tol = G * d.abs().mean(1, keepdim=True) if layer else 0.0
+    m2 = (d * h).mean(1, keepdim=True)
+    m2_tol = G * (d * h).abs().mean(1, keepdim=True) + (d.abs() * h_tol).mean(1, keepdim=True)
+    inner = d - m1 - h * m2
+    inner_tol = 3 * U32 * (d.abs() + abs(m1) + (h * m2).abs()) + m1_tol + h.abs() * m2_tol + h_tol * m2.abs()
+    dx, tol = inner * inv, inv * inner_tol + (inner * inv).abs() * (1.1 * inv_rel + U32)
+    if add is not None:
+        dx = dx + add64
+        tol = tol + U32 * dx.abs()
+    dx, tol = torch.where(real[:, None], dx, 0.0), torch.where(real[:, None], tol, 0.0)
+    near(got[0], dx, tol)
+    # rows per warp or block (592 or 148 of them at least, where there are so many rows), warps of a block, blocks in turns, turns
+    depth = min(rows, rows / 148 + 1 + 4 + 74 + 16) + 4
+    if got[1] is not None:
+        near(got[1], (dn64 * h).sum(0), (dn64.abs() * h_tol).sum(0) + depth * U32 * (dn64 * h).abs().sum(0))
+    if got[2] is not None:
+        near(got[2], dn64.sum(0), depth * U32 * dn64.abs().sum(0))
+    return got
+
+
+def norm_of(g, D, kind, weight=True, bias=True, eps=1e-5):
+    return serve.Norm(kind, 1 + 0.2 * rnd(g, D) if weight else None, 0.3 * rnd(g, D) if bias else None, eps=eps)
+
+
+@pytest.mark.parametrize("width", R.WIDTHS)
+@pytest.mark.parametrize("dtype,xt", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "fp32"), ("fp16", "fp16"), ("fp16", "fp32")])
+def test_norm_gradients_of_every_width_and_type(width, dtype, xt):
+    g = gen(width)
+    T, X = DTYPES[dtype], DTYPES[xt]
+    for rows in (1, 7, 700 if width <= 1032 else 200):
+        dn, x = rnd(g, rows, width, dtype=T), (rnd(g, rows, width, scale=2.0) + 1).to(X)
+        check_norm_grad(dn, x, norm_of(g, width, serve.NORM_LAYER))
+        check_norm_grad(dn, x, norm_of(g, width, serve.NORM_RMS), add=rnd(g, rows, width, dtype=X))
+        ids = torch.randint(-2, rows + 2, (rows,), generator=g, device="cuda", dtype=torch.int32)
+        check_norm_grad(dn, x, norm_of(g, width, serve.NORM_RMS, bias=False), ids=ids, add=rnd(g, rows, width, dtype=X))
+        check_norm_grad(dn, x, norm_of(g, width, serve.NORM_LAYER, weight=False, bias=False), ids=ids)
+
+
+@pytest.mark.parametrize("rows", [1, 3, 4, 5, 590, 593, 5000, 30_011])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_norm_gradients_of_many_rows(rows, dtype):
+    g = gen(rows)
+    for width in (40, 256, 602, 1040):
+        dn, x = rnd(g, rows, width, dtype=DTYPES[dtype]), rnd(g, rows, width) * 3 - 2
+        check_norm_grad(dn, x, norm_of(g, width, serve.NORM_LAYER), add=rnd(g, rows, width))
+
+
+def test_norm_gradients_over_strides_and_in_place():
+    g = gen(3)
+    for dtype in DTYPES.values():
+        for off, width in ((0, 64), (1, 64), (2, 30), (8, 1100), (3, 1101)):
+            dn, x, add, out = (rnd(g, 200, width + 16, dtype=dtype)[:, off:off + width] for _ in range(4))
+            norm = norm_of(g, width, serve.NORM_LAYER)
+            check_norm_grad(dn, x, norm, add=add, out=out)
+            for place in (0, 1, 2):          # (the checks look at copies of what was there before the call)
+                args = [t.clone() for t in (dn, x, add)]
+                got = check_norm_grad(args[0], args[1], norm, add=args[2], out=args[place])
+                assert got[0] is args[place]
+
+
+def test_norm_gradients_of_rows_without_spread():
+    """Constant rows and rows of zeros: the variance is zero, eps alone stands below the root."""
+    g = gen(4)
+    x = torch.zeros(6, 100, device="cuda")
+    x[1:3] = 5.0
+    x[4] = 1e-20
+    for kind in (serve.NORM_LAYER, serve.NORM_RMS):
+        check_norm_grad(rnd(g, 6, 100), x, norm_of(g, 100, kind, eps=1e-3))
+
+
+def test_norm_gradients_of_padding_rows():
+    g = gen(5)
+    dn, x = rnd(g, 50, 70), rnd(g, 50, 70)
+    ids = torch.arange(50, dtype=torch.int32, device="cuda")
+    ids[::3] = -1
+    dn[::3], x[::3] = float("nan"), float("inf")
+    norm = norm_of(g, 70, serve.NORM_LAYER)
+    got = train.norm_rows_grad(dn, x, norm, ids=ids, add=torch.full_like(dn, 3.0))
+    assert (got[0][::3] == 0).all() and all(torch.isfinite(t).all() for t in got)
+    keep = [i for i in range(50) if i % 3]
+    want = train.norm_rows_grad(dn[keep], x[keep], norm, add=torch.full((len(keep), 70), 3.0, device="cuda"))
+    assert torch.equal(got[0][keep], want[0])
+    none = train.norm_rows_grad(dn[:0], x, norm, ids=ids[:0])
+    assert none[0].shape == (0, 70) and (none[1] == 0).all() and (none[2] == 0).all()
+    a, b, c = train.norm_rows_grad(dn[1:2], x[1:2], norm, vectors=False)
+    assert b is None and c is None and torch.equal(a, train.norm_rows_grad(dn[1:2], x[1:2], norm)[0])
+
+
+def test_norm_gradient_against_differences():
+    """d/dt sum(dn norm(x + t v)) and the same for the weight, by central differences of the formula in 64 bits."""
+    g = gen(6)
+    for kind in (serve.NORM_LAYER, serve.NORM_RMS):
+        norm = norm_of(g, 60, kind)
+        dn, x, v, vw = rnd(g, 9, 60), rnd(g, 9, 60), rnd(g, 9, 60), rnd(g, 60)
+        dx, dw, _ = train.norm_rows_grad(dn, x, norm)
+
+        def f(x, w):
+            c = x - x.mean(1, keepdim=True) if kind == serve.NORM_LAYER else x
+            return (dn.to(F64) * (c / (c.square().mean(1, keepdim=True) + norm.eps).sqrt() * w + norm.bias.to(F64))).sum()
+
+        h, w = 1e-5, norm.weight.to(F64)
+        by_x = (f(x.to(F64) + h * v.to(F64), w) - f(x.to(F64) - h * v.to(F64), w)) / (2 * h)
+        by_w = (f(x.to(F64), w + h * vw.to(F64)) - f(x.to(F64), w - h * vw.to(F64))) / (2 * h)
+        # (differences: h^2 of a third derivative of order one; sums of 540 terms of order one in fp32)
+        assert abs(float(by_x - (dx.to(F64) * v.to(F64)).sum())) < 1e-3
+        assert abs(float(by_w - (dw.to(F64) * vw.to(F64)).sum())) < 1e-3
+
+
+# ---- loss_rows, loss_rows_grad ---------------------------------------------------------------------------------------
+def check_loss(x, W, labels, bias=None, dloss=1.0, grad=True, **kw):
+    """z: a product of K terms in steps of 16, each off by 2^-23 of the terms' magnitudes at most (tensor core), 32 for parts, carrying and
+    bias.  lse: a weighted mean of z's errors; exponents of base 2 off by their size times u32, exp2 by 4 u32, sums of 128 terms a tile and of the
+    tiles.  g: p (1 + what z and lse are off), a product; then half a step of the operand's type.  dx, dW: like z, over classes or rows."""
+    rows, K = x.shape
+    N = W.shape[1]
+    x64, W64 = x.to(F64), W.to(F64)
+    b64 = torch.zeros(N, dtype=F64, device="cuda") if bias is None else bias.to(F64)
+    z = x64 @ W64 + b64
+    finite = torch.isfinite(b64)
+    z_tol = (K / 16 + 32) * 2.0 ** -23 * (x64.abs() @ W64.abs()) + 4 * U32 * torch.where(torch.isfinite(z), z.abs(), 0.0)
+    z_tol = torch.where(finite, z_tol, 0.0)
+    lse = torch.logsumexp(z, 1)
+    some = torch.isfinite(lse)
+    most = torch.where(torch.isfinite(z), z.abs(), 0.0).amax(1)
+    lse_tol = z_tol.amax(1) + U32 * (8 * most + 24 + 128 + N / 128 + 2 * torch.where(some, lse.abs(), 0.0))
+    live = (labels >= 0) & (labels < N) & some
+    at = torch.where(live, labels, 0).long()[:, None]
+    loss = torch.where(live, lse - z.gather(1, at)[:, 0], 0.0)
+    got_loss, got_lse = train.loss_rows(x, W, labels, bias=bias)
+    near(got_lse, lse, lse_tol)
+    near(got_loss, loss, torch.where(live, lse_tol + z_tol.gather(1, at)[:, 0], 0.0))
+    if not grad:
+        return
+    dx, dW, db = train.loss_rows_grad(x, W, labels, got_lse, dloss, bias=bias, **kw)
+    k = dloss.to(F64) if isinstance(dloss, torch.Tensor) else torch.full((rows,), R.np.float32(dloss).item(), dtype=F64, device="cuda")
+    k = torch.where(live, k, 0.0)
+    p = torch.where(live[:, None], torch.exp(z - torch.where(some, lse, 0.0)[:, None]), 0.0)
+    rel = z_tol + lse_tol[:, None] + U32 * (4 * torch.where(torch.isfinite(z), (z - torch.where(some, lse, 0.0)[:, None]).abs(), 0.0) + 12)
+    g = p.scatter_add(1, at, -live.to(F64)[:, None]) * k[:, None]
+    g_tol = (p * rel + 3 * U32 * (g.abs() if False else p)) * k.abs()[:, None] + 3 * U32 * g.abs()
+    if db is not None:
+        # 5 additions in a warp, groups of 32 rows in 16 turns, the turns
+        near(db, g.sum(0), g_tol.sum(0) + (5 + rows / 512 + 1 + 16) * U32 * g.abs().sum(0))
+    op = torch.bfloat16 if x.dtype == torch.bfloat16 else torch.float16
+    if x.dtype == torch.float32:
+        g_tol = g_tol + U32 * g.abs()
+    else:
+        g_tol = g_tol + torch.finfo(op).eps / 2 * (g.abs() + g_tol)
+        if op == torch.float16:                 # scaled to 2^14 at least, where multiples of 2^-24 are exact
+            g_tol = g_tol + 2.0 ** -39 * k.abs().max()
+    if dx is not None:
+        near(dx, g @ W64.T, g_tol @ W64.abs().T + (N / 16 + 48) * 2.0 ** -23 * (g.abs() @ W64.abs().T))
+        dead = ~((labels >= 0) & (labels < N))
+        assert (dx[dead] == 0).all()
+    if dW is not None:
+        x0 = torch.where(live[:, None], x64, 0.0)
+        near(dW, x0.T @ g, x0.abs().T @ g_tol + (rows / 16 + 48) * 2.0 ** -23 * (x0.abs().T @ g.abs()))
+
+
+def problem(g, rows, K, N, dtype, bias=True, padding=0.1):
+    x, W = rnd(g, rows, K, dtype=dtype), rnd(g, K, N, dtype=dtype, scale=2 / math.sqrt(K))
+    labels = torch.randint(0, N, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    labels = torch.where(torch.rand(rows, generator=g, device="cuda") < padding, torch.randint(N, N + 3, (rows,), generator=g, device="cuda", dtype=torch.int32) * (1 - 2 * (labels % 2)), labels)
+    return dict(x=x, W=W, labels=labels, bias=rnd(g, N) if bias else None)
+
+
+def rows_of(g, rows):
+    return 0.5 + torch.rand(rows, generator=g, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows,K,N", [(128, 64, 64), (256, 64, 256), (1, 16, 2), (1, 128, 40), (3, 5, 1), (100, 602, 41), (257, 256, 47), (300, 40, 300), (64, 200, 1000),
+                                      (511, 100, 129), (513, 320, 513), (1000, 602, 41), (33, 1024, 2049), (5, 8192, 17)])
+def test_losses_of_every_size_and_type(dtype, rows, K, N):
+    g = gen(rows + K + N)
+    q = problem(g, rows, K, N, DTYPES[dtype])
+    check_loss(**q, dloss=rows_of(g, rows))
+    check_loss(**{**q, "bias": None}, dloss=0.25)
+    serve.check_requests()
