@@ -1,8 +1,9 @@
 // Rows looked up by id, and the gradient of the table they came from:
 //   out_i = scale table[ids_i],      dtable[r] = scale * sum of dy_i over the i with ids_i = r, in the order of i.
 // The gradient sorts (id, i) by id and sums runs of one id.  Every 32 places of the sorted list are a warp's, however the ids are
-// distributed: a run that lies within them is finished there; what a run has in them that goes on beyond is a partial sum, and the partial sums
-// are again a sorted list, a sixteenth as long (later a 32nd), for the same kernel.  No atomics on sums, so every call gives the same bits.
+// distributed: a run that lies within them is finished there; what a run has in them that goes on beyond is a partial sum.  The partial sums of a
+// block's eight warps are such a list again, for one of its warps, and those of all blocks, a 128th as many as entries, for the same kernel.
+// No atomics on sums, so every call gives the same bits.
 #include "row_vectors.cuh"
 
 #include <algorithm>
@@ -15,7 +16,7 @@ struct LookupParams {
     int rows, width, lanes;      // lanes: threads of a row, a power of two
     const void* table;
     int64_t ld_table, table_rows;
-    const int32_t* ids;          // null: zeros everywhere
+    const int32_t* ids;
     void* out;
     int64_t ld_out;
     float scale;
@@ -23,24 +24,29 @@ struct LookupParams {
 
 constexpr int LK_BLOCK = 256;
 
+constexpr int LK_ROWS = 4;       // rows of a thread that are on their way together
+
 template <typename T, typename TO, int V>
 __global__ void __launch_bounds__(LK_BLOCK) k_lookup_rows(const __grid_constant__ LookupParams p) {
     pdl_enter();
     const int t = threadIdx.x & (p.lanes - 1), per_block = LK_BLOCK / p.lanes;
     const Vec<V> scale = all_of<V>(p.scale);
-    for (int64_t row = (int64_t)blockIdx.x * per_block + threadIdx.x / p.lanes; row < p.rows; row += (int64_t)gridDim.x * per_block) {
-        const int64_t id = p.ids ? p.ids[row] : -1;
-        const bool real = id >= 0 && id < p.table_rows;
-        const T* const from = static_cast<const T*>(p.table) + (real ? id : 0) * p.ld_table;
-        TO* const to = static_cast<TO*>(p.out) + row * p.ld_out;
-#pragma unroll 4
+    for (int64_t row0 = (int64_t)blockIdx.x * per_block * LK_ROWS + threadIdx.x / p.lanes; row0 < p.rows; row0 += (int64_t)gridDim.x * per_block * LK_ROWS) {
+        int64_t id[LK_ROWS];
+#pragma unroll
+        for (int u = 0; u < LK_ROWS; ++u) id[u] = row0 + u * per_block < p.rows ? p.ids[row0 + u * per_block] : -1;
         for (int c = t * V; c < p.width; c += p.lanes * V) {
-            Vec<V> v = all_of<V>(0.f);
-            if (real) {
-                v = load<T, V>(from + c);
-                times<V>(v, scale);
+            Vec<V> v[LK_ROWS];
+#pragma unroll
+            for (int u = 0; u < LK_ROWS; ++u) {
+                v[u] = all_of<V>(0.f);
+                if (id[u] >= 0 && id[u] < p.table_rows) v[u] = load<T, V>(static_cast<const T*>(p.table) + id[u] * p.ld_table + c);
             }
-            store<TO, V>(to + c, v);
+#pragma unroll
+            for (int u = 0; u < LK_ROWS; ++u) {
+                if (id[u] >= 0 && id[u] < p.table_rows) times<V>(v[u], scale);      // (zeros stay zeros whatever the scale)
+                if (row0 + u * per_block < p.rows) store<TO, V>(static_cast<TO*>(p.out) + (row0 + u * per_block) * p.ld_out + c, v[u]);
+            }
         }
     }
 }
@@ -49,7 +55,7 @@ template <typename T, typename TO, int V>
 static cudaError_t launch_lookup(LookupParams p, void* stream) {
     p.lanes = 1;
     while (p.lanes < LK_BLOCK && p.lanes * V < p.width) p.lanes *= 2;
-    const int64_t blocks = ((int64_t)p.rows * p.lanes + LK_BLOCK - 1) / LK_BLOCK;
+    const int64_t blocks = ((int64_t)p.rows * p.lanes + LK_BLOCK * LK_ROWS - 1) / (LK_BLOCK * LK_ROWS);
     return launch(k_lookup_rows<T, TO, V>, dim3((unsigned)std::min<int64_t>(blocks, (int64_t)sm_count() * 32)), LK_BLOCK, 0, stream, p);
 }
 
@@ -61,14 +67,60 @@ static cudaError_t launch_lookup(const LookupParams& p, int v, void* stream) {
     return launch_lookup<T, TO, 1>(p, stream);
 }
 
+// ---- zeros ---------------------------------------------------------------------------------------------------------
+// The gradient's table is mostly zeros where ids are few; they are written by blocks behind those of the kernels that sort, which by themselves
+// would leave the memory idle (20 011 ids of a table of 232 965 rows, 602 fp32 columns: ZERO_TIMES).
+struct ZeroParams {
+    uint8_t* at;
+    int64_t units, row_bytes, pitch;       // rows; a table without gaps counts as rows of ZERO_PIECE bytes, the last one shorter
+    int64_t last_bytes;
+};
+constexpr int64_t ZERO_PIECE = 32 * 1024;
+
+static ZeroParams zeros_of(void* p, int64_t rows, int64_t width, int64_t ld, int size) {
+    if (rows == 0) return {};
+    if (ld > width) return {static_cast<uint8_t*>(p), rows, width * size, ld * size, width * size};
+    const int64_t bytes = rows * width * size, units = (bytes + ZERO_PIECE - 1) / ZERO_PIECE;
+    return {static_cast<uint8_t*>(p), units, ZERO_PIECE, ZERO_PIECE, bytes - (units - 1) * ZERO_PIECE};
+}
+// share `part` of `parts`
+static ZeroParams share_of(const ZeroParams& z, int part, int parts) {
+    const int64_t first = z.units * part / parts, end = z.units * (part + 1) / parts;
+    return {z.at + first * z.pitch, end - first, z.row_bytes, z.pitch, end == z.units ? z.last_bytes : z.row_bytes};
+}
+__device__ __forceinline__ void write_zeros(const ZeroParams& z, int block, int blocks) {
+    for (int64_t u = block; u < z.units; u += blocks) {
+        uint8_t* const begin = z.at + u * z.pitch;
+        uint8_t* const end = begin + (u == z.units - 1 ? z.last_bytes : z.row_bytes);
+        uint8_t* const from = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(begin) + 15) & ~(uintptr_t)15);
+        uint8_t* const to = reinterpret_cast<uint8_t*>(reinterpret_cast<uintptr_t>(end) & ~(uintptr_t)15);
+        if (from >= to) {                  // (elements have 2 bytes at least, and lie at multiples of 2)
+            for (uint8_t* p = begin + 2 * threadIdx.x; p < end; p += 2 * blockDim.x) *reinterpret_cast<uint16_t*>(p) = 0;
+            continue;
+        }
+        if (begin + 2 * threadIdx.x < from) *reinterpret_cast<uint16_t*>(begin + 2 * threadIdx.x) = 0;
+        if (to + 2 * threadIdx.x < end) *reinterpret_cast<uint16_t*>(to + 2 * threadIdx.x) = 0;
+#pragma unroll 4
+        for (uint8_t* p = from + 16 * threadIdx.x; p < to; p += 16 * blockDim.x) *reinterpret_cast<uint4*>(p) = make_uint4(0, 0, 0, 0);
+    }
+}
+__global__ void __launch_bounds__(256) k_zeros(const __grid_constant__ ZeroParams z) {
+    pdl_enter();
+    write_zeros(z, blockIdx.x, gridDim.x);
+}
+constexpr int ZERO_BLOCKS = 8;             // per SM
+
 // ---- (id, place) in the order of ids -----------------------------------------------------------------------------------
 // From the lowest digit up; a pass counts the digits of every tile, adds the counts up, and moves the entries; entries of one digit
 // stay in order.  Ids outside the table become `table_rows` and come last.
-constexpr int SR_TILE = 4096, SR_WARPS = 8, SR_BITS = 11;
+constexpr int SR_WARPS = 8, SR_BITS = 11;
+// Entries of a tile: few where that gives every SM a tile or two at most, for a tile takes as long as its warps have rounds.
+constexpr int SR_TILE_FINE = 1024, SR_TILE = 4096, SR_FINE = 1 << 19;
 constexpr int SR_SMALL = 4096, SR_SMALL_BITS = 8;      // entries that one block sorts in shared memory, digits of 8 bits
 
 struct SortParams {
-    int n, tiles;
+    int n, tile, tiles;          // entries of a tile
+    ZeroParams zeros;            // for the blocks behind those that sort
     int shift, digits;           // of this pass
     uint32_t table_rows;
     const int32_t* ids;          // first pass; else null
@@ -85,12 +137,13 @@ __device__ __forceinline__ uint32_t sort_key(const SortParams& p, int i) { retur
 
 __global__ void __launch_bounds__(32 * SR_WARPS) k_sort_count(const __grid_constant__ SortParams p) {
     pdl_enter();
+    if ((int)blockIdx.x >= p.tiles) return write_zeros(p.zeros, blockIdx.x - p.tiles, gridDim.x - p.tiles);
     __shared__ int32_t count[1 << SR_BITS];
     for (int d = threadIdx.x; d < p.digits; d += blockDim.x) count[d] = 0;
     __syncthreads();
-    const int first = blockIdx.x * SR_TILE;
+    const int first = blockIdx.x * p.tile;
 #pragma unroll 4
-    for (int e = threadIdx.x; e < SR_TILE; e += blockDim.x) {
+    for (int e = threadIdx.x; e < p.tile; e += blockDim.x) {
         const int i = first + e;
         const bool in = i < p.n;
         const int d = in ? (int)(sort_key(p, i) >> p.shift & (uint32_t)(p.digits - 1)) : -1;
@@ -105,6 +158,8 @@ __global__ void __launch_bounds__(32 * SR_WARPS) k_sort_count(const __grid_const
 // a warp per digit
 __global__ void __launch_bounds__(256) k_sort_scan(const __grid_constant__ SortParams p) {
     pdl_enter();
+    const int blocks = (p.digits + 7) / 8;
+    if ((int)blockIdx.x >= blocks) return write_zeros(p.zeros, blockIdx.x - blocks, gridDim.x - blocks);
     const int d = blockIdx.x * 8 + (threadIdx.x >> 5), lane = lane_id();
     if (d >= p.digits) return;
     int32_t* const row = p.counts + (int64_t)d * p.tiles;
@@ -151,6 +206,7 @@ __device__ __forceinline__ void move_tile(int32_t* at, int digits, int entries, 
 
 __global__ void __launch_bounds__(32 * SR_WARPS) k_sort_move(const __grid_constant__ SortParams p) {
     pdl_enter();
+    if ((int)blockIdx.x >= p.tiles) return write_zeros(p.zeros, blockIdx.x - p.tiles, gridDim.x - p.tiles);
     extern __shared__ int32_t at[];            // warps x digits, and behind them the digits' starts
     __shared__ int32_t scratch[33];
     int32_t* const start = at + SR_WARPS * p.digits;
@@ -163,8 +219,8 @@ __global__ void __launch_bounds__(32 * SR_WARPS) k_sort_move(const __grid_consta
         start[d] = sum + p.counts[(int64_t)d * p.tiles + blockIdx.x];
         sum += p.totals[d];
     }
-    const int first = blockIdx.x * SR_TILE;
-    auto entry = [&](int e) { return e < SR_TILE && first + e < p.n ? (int)(sort_key(p, first + e) >> p.shift & (uint32_t)(p.digits - 1)) : -1; };
+    const int first = blockIdx.x * p.tile;
+    auto entry = [&](int e) { return e < p.tile && first + e < p.n ? (int)(sort_key(p, first + e) >> p.shift & (uint32_t)(p.digits - 1)) : -1; };
     auto move = [&](int e, int to) {
         const int i = first + e;
         p.keys_out[to] = sort_key(p, i);
@@ -180,7 +236,7 @@ __global__ void __launch_bounds__(32 * SR_WARPS) k_sort_move(const __grid_consta
             }
         }
     };
-    move_tile<SR_WARPS>(at, p.digits, SR_TILE, entry, move, base);
+    move_tile<SR_WARPS>(at, p.digits, p.tile, entry, move, base);
 }
 
 // All passes of up to SR_SMALL entries by one block.
@@ -193,6 +249,7 @@ struct SmallSort {
 };
 __global__ void __launch_bounds__(32 * SS_WARPS) k_sort_small(const __grid_constant__ SortParams p, int bits) {
     pdl_enter();
+    if (blockIdx.x > 0) return write_zeros(p.zeros, blockIdx.x - 1, gridDim.x - 1);
     extern __shared__ __align__(16) uint8_t raw[];
     SmallSort& s = *reinterpret_cast<SmallSort*>(raw);
     constexpr int DIGITS = 1 << SR_SMALL_BITS;
@@ -222,18 +279,18 @@ __global__ void __launch_bounds__(32 * SS_WARPS) k_sort_small(const __grid_const
 static_assert(32 * SS_WARPS >= 1 << SR_SMALL_BITS, "a thread per digit");
 
 // ---- sums of runs --------------------------------------------------------------------------------------------------
-// A list entry of the partial sums: the key, with EMPTY where the run only goes on through this place.
+// An entry of a list of partial sums: the key, with EMPTY where the run only goes on through this place.
 constexpr uint32_t EMPTY = 0x80000000u, NO_KEY = 0xffffffffu;
 
 struct RunParams {
-    int n, width, chunk, chunks, slices;    // places of a warp, a multiple of 32; parts of the columns, a warp each
+    int n, width, slices;        // entries; parts of the columns, a block each
     uint32_t table_rows;
     const uint32_t* keys;        // n, ascending (without EMPTY), NO_KEY anywhere
     const int32_t* places;       // row of src of every entry; null: the entry's own
     const void* src;
     int64_t ld_src;
-    uint32_t* next_keys;         // 2 x chunks: partial sums of runs that go on beyond a chunk
-    float* next;                 // 2 x chunks x ld_next
+    uint32_t* next_keys;         // two for every block's entries: partial sums of runs that go on beyond them
+    float* next;
     int ld_next;
     void* out;
     int64_t ld_out;
@@ -241,87 +298,119 @@ struct RunParams {
     int accumulate;
 };
 
-constexpr int RS_AHEAD = 8;      // rows on their way
+constexpr int RS_WARPS = 8, RS_CHUNK = 32 * RS_WARPS;      // entries of a block, 32 of a warp
 
-template <typename T, typename TO, int V, int NP>
-__global__ void __launch_bounds__(128) k_sum_runs(const __grid_constant__ RunParams p) {
-    pdl_enter();
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int lane = lane_id(), chunk = (int)(at / p.slices), slice = (int)(at % p.slices);
-    if (chunk >= p.chunks) return;
-    const int c0 = slice * (32 * V * NP) + lane * V;
-    const int begin = chunk * p.chunk, end = min(p.n, begin + p.chunk);
-    const Vec<V> scale = all_of<V>(p.scale);
-    auto bare = [](uint32_t k) { return k & ~EMPTY; };
-    const uint32_t none = bare(NO_KEY), before = begin > 0 ? bare(p.keys[begin - 1]) : none, after = end < p.n ? bare(p.keys[end]) : none;
+__device__ __forceinline__ uint32_t bare(uint32_t key) { return key & ~EMPTY; }
+
+// Runs of the same key among entries in order.  add(k, piece): an entry; end: the last run.  A run that lies within the entries is `complete`, the
+// one that comes from before them and the one that goes on behind them are partial sums.
+template <typename TO, int V, int NP>
+struct Runs {
+    const RunParams& p;
+    const int c0;                // this lane's columns: c0 + 32 V j
+    float* head;                 // where this lane's part of the partial sums goes
+    float* tail;
+    uint32_t run, head_key = NO_KEY, tail_key = NO_KEY;
+    bool from_before;
     Vec<V> sum[NP];
+    __device__ __forceinline__ Runs(const RunParams& p_, int c, uint32_t first, uint32_t before, float* h, float* t) : p(p_), c0(c), head(h), tail(t), run(bare(first)), from_before(bare(first) == before) { clear(); }
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int j = 0; j < NP; ++j) sum[j] = all_of<V>(0.f);
-    auto each = [&](auto f) {
+        for (int j = 0; j < NP; ++j) sum[j] = all_of<V>(0.f);
+    }
+    template <typename F> __device__ __forceinline__ void each(F f) {
 #pragma unroll
-        for (int j = 0; j < NP; ++j) if (c0 + j * 32 * V < p.width) f(j, c0 + j * 32 * V);
-    };
-    uint32_t run = bare(p.keys[begin]);
-    bool from_before = run == before;
-    uint32_t left0 = NO_KEY, left1 = NO_KEY;    // keys of this chunk's partial sums: of the run that it begins in, of the one that it ends in
-    auto finish = [&](bool goes_on) {
+        for (int j = 0; j < NP; ++j) if (c0 + j * 32 * V < p.width) f(j, j * 32 * V);
+    }
+    __device__ __forceinline__ void finish(bool goes_on) {
         if (run < p.table_rows) {
             if (from_before || goes_on) {
-                float* const to = p.next + (int64_t)(2 * chunk + (from_before ? 0 : 1)) * p.ld_next;
+                float* const to = from_before ? head : tail;
                 each([&](int j, int c) { store<float, V>(to + c, sum[j]); });
-                if (from_before) left0 = run;
-                if (goes_on) left1 = from_before ? run | EMPTY : run;
+                if (from_before) head_key = run;
+                if (goes_on) tail_key = from_before ? run | EMPTY : run;
             } else {
-                TO* const to = static_cast<TO*>(p.out) + (int64_t)run * p.ld_out;
+                TO* const to = static_cast<TO*>(p.out) + (int64_t)run * p.ld_out + c0;
+                const Vec<V> scale = all_of<V>(p.scale);
                 each([&](int j, int c) {
                     times<V>(sum[j], scale);
                     if (p.accumulate) plus<V>(sum[j], load<TO, V>(to + c));
                     store<TO, V>(to + c, sum[j]);
                 });
             }
-        }
-#pragma unroll
-        for (int j = 0; j < NP; ++j) sum[j] = all_of<V>(0.f);
-    };
-    for (int i0 = begin; i0 < end; i0 += 32) {
-        const int i = min(i0 + lane, end - 1), count = min(32, end - i0);
-        const uint32_t key = p.keys[i];
-        const int place = p.places ? p.places[i] : i;
-        for (int e0 = 0; e0 < count; e0 += RS_AHEAD) {
-            Piece<T, V> v[RS_AHEAD][NP];
-            uint32_t k[RS_AHEAD];
-            // (an entry that holds nothing -- padding, EMPTY, none at all -- is not read)
-#pragma unroll
-            for (int u = 0; u < RS_AHEAD; ++u) {
-                k[u] = __shfl_sync(FULL, key, min(e0 + u, 31));
-                const T* const from = static_cast<const T*>(p.src) + (int64_t)__shfl_sync(FULL, place, min(e0 + u, 31)) * p.ld_src;
-                if (e0 + u >= count) k[u] = NO_KEY;
-                if (k[u] < p.table_rows) each([&](int j, int c) { v[u][j] = *reinterpret_cast<const Piece<T, V>*>(from + c); });
-            }
-#pragma unroll
-            for (int u = 0; u < RS_AHEAD; ++u) {
-                if (e0 + u >= count) break;
-                const uint32_t now = bare(k[u]);
-                if (now != run) {
-                    finish(false);
-                    run = now, from_before = false;
-                }
-                if (k[u] < p.table_rows) each([&](int j, int) { plus<V>(sum[j], load<T, V>(&v[u][j])); });
-            }
+            clear();
         }
     }
-    finish(run == after);
-    if (p.next_keys && slice == 0 && lane < 2) p.next_keys[2 * chunk + lane] = lane ? left1 : left0;
-}
+    template <typename F> __device__ __forceinline__ void add(uint32_t key, F piece) {
+        if (bare(key) != run) {
+            finish(false);
+            run = bare(key), from_before = false;
+        }
+        if (key < p.table_rows) each([&](int j, int) { plus<V>(sum[j], piece(j)); });
+    }
+};
 
-// Places of a warp: of the rows themselves, of lists of partial sums.
-constexpr int RS_ROWS = 32, RS_SUMS = 64;
+template <typename T, typename TO, int V, int NP>
+__global__ void __launch_bounds__(32 * RS_WARPS, 4) k_sum_runs(const __grid_constant__ RunParams p) {
+    pdl_enter();
+    constexpr int COLS = 32 * V * NP;
+    __shared__ __align__(16) float part[2 * RS_WARPS][COLS];
+    __shared__ uint32_t part_key[2 * RS_WARPS];
+    const int warp = threadIdx.x >> 5, lane = lane_id(), block = blockIdx.x / p.slices, slice = blockIdx.x - block * p.slices;
+    const int c0 = slice * COLS + lane * V, first = block * RS_CHUNK, last = min(p.n, first + RS_CHUNK);
+    auto key_at = [&](int i) { return i >= 0 && i < p.n ? bare(p.keys[i]) : bare(NO_KEY); };
+    uint32_t head_key = NO_KEY, tail_key = NO_KEY;
+    const int begin = first + 32 * warp, count = min(32, last - begin);
+    if (count > 0) {
+        const uint32_t before = key_at(begin - 1), after = key_at(begin + count);
+        const int i = begin + min(lane, count - 1);
+        const uint32_t key = p.keys[i];
+        const int place = p.places ? p.places[i] : i;
+        Runs<TO, V, NP> runs(p, c0, __shfl_sync(FULL, key, 0), before, &part[2 * warp][lane * V], &part[2 * warp + 1][lane * V]);
+        // (an entry that holds nothing -- padding, EMPTY, none at all -- is not read)
+        constexpr int AHEAD = sizeof(T) * V * NP > 16 ? 4 : 8;       // rows of a warp that are on their way (32 warps of an SM: 64 KB)
+        using Batch = Piece<T, V>[AHEAD][NP];
+        auto request = [&](Batch& v, int e0) {
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const uint32_t k = __shfl_sync(FULL, key, e0 + u);
+                const T* const from = static_cast<const T*>(p.src) + (int64_t)__shfl_sync(FULL, place, e0 + u) * p.ld_src + c0;
+                if (e0 + u < count && k < p.table_rows) runs.each([&](int j, int c) { v[u][j] = *reinterpret_cast<const Piece<T, V>*>(from + c); });
+            }
+        };
+        auto take = [&](const Batch& v, int e0) {
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const uint32_t k = __shfl_sync(FULL, key, e0 + u);
+                if (e0 + u < count) runs.add(k, [&](int j) { return load<T, V>(&v[u][j]); });
+            }
+        };
+        Batch v;
+#pragma unroll 1
+        for (int e0 = 0; e0 < count; e0 += AHEAD) request(v, e0), take(v, e0);
+        runs.finish(runs.run == after);
+        head_key = runs.head_key, tail_key = runs.tail_key;
+    }
+    if (lane < 2) part_key[2 * warp + lane] = lane ? tail_key : head_key;
+    const bool any = __syncthreads_or(head_key != NO_KEY || tail_key != NO_KEY);
+    if (warp > 0) return;
+    // the warps' partial sums, in the same way
+    head_key = tail_key = NO_KEY;
+    if (any) {
+        const int64_t at = 2ll * block * p.ld_next + c0;
+        Runs<TO, V, NP> runs(p, c0, part_key[0], key_at(first - 1), p.next + at, p.next + at + p.ld_next);
+        for (int e = 0; e < 2 * RS_WARPS; ++e) runs.add(part_key[e], [&](int j) { return load<float, V>(&part[e][lane * V + j * 32 * V]); });
+        runs.finish(runs.run == key_at(last));
+        head_key = runs.head_key, tail_key = runs.tail_key;
+    }
+    if (p.next_keys && slice == 0 && lane < 2) p.next_keys[2 * block + lane] = lane ? tail_key : head_key;
+}
 
 template <typename T, typename TO, int V, int NP>
 static cudaError_t launch_runs(RunParams p, void* stream) {
     p.slices = (p.width + 32 * V * NP - 1) / (32 * V * NP);
-    const int64_t warps = (int64_t)p.chunks * p.slices;
-    return launch(k_sum_runs<T, TO, V, NP>, dim3((unsigned)((warps + 3) / 4)), 128, 0, stream, p);
+    const int64_t blocks = (int64_t)((p.n + RS_CHUNK - 1) / RS_CHUNK) * p.slices;
+    return launch(k_sum_runs<T, TO, V, NP>, dim3((unsigned)blocks), 32 * RS_WARPS, 0, stream, p);
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------
@@ -359,12 +448,51 @@ __global__ void __launch_bounds__(FW_ROWS) k_lookup_grad_few(const __grid_consta
     }
 }
 
+// The same for a table that is small as well: a block for each row of it writes it, zeros included, and no other launch.
+constexpr int64_t FW_TABLE = 4 << 20;      // bytes
+template <typename T, typename TO, int V>
+__global__ void __launch_bounds__(128) k_lookup_grad_table(const __grid_constant__ RunParams p, const int32_t* ids) {
+    pdl_enter();
+    __shared__ int32_t rows[FW_ROWS];
+    __shared__ int32_t before[FW_ROWS / 32];
+    const int t = threadIdx.x;
+    uint32_t all[FW_ROWS / 128];
+    bool same[FW_ROWS / 128];
+#pragma unroll
+    for (int h = 0; h < FW_ROWS / 128; ++h) {
+        same[h] = t + 128 * h < p.n && ids[t + 128 * h] == (int)blockIdx.x;
+        all[h] = __ballot_sync(FULL, same[h]);
+        if (lane_id() == 0) before[(t + 128 * h) >> 5] = __popc(all[h]);
+    }
+    __syncthreads();
+    int count = 0;
+#pragma unroll
+    for (int w = 0; w < FW_ROWS / 32; ++w) {
+#pragma unroll
+        for (int h = 0; h < FW_ROWS / 128; ++h)
+            if (w == (t + 128 * h) >> 5 && same[h]) rows[count + __popc(all[h] & ((1u << lane_id()) - 1))] = t + 128 * h;
+        count += before[w];
+    }
+    __syncthreads();
+    if (count == 0 && p.accumulate) return;
+    const Vec<V> scale = all_of<V>(p.scale);
+    TO* const to = static_cast<TO*>(p.out) + blockIdx.x * p.ld_out;
+    for (int c = t * V; c < p.width; c += 128 * V) {
+        Vec<V> sum = all_of<V>(0.f);
+#pragma unroll 8
+        for (int i = 0; i < count; ++i) plus<V>(sum, load<T, V>(static_cast<const T*>(p.src) + (int64_t)rows[i] * p.ld_src + c));
+        if (count > 0) times<V>(sum, scale);
+        if (p.accumulate) plus<V>(sum, load<TO, V>(to + c));
+        store<TO, V>(to + c, sum);
+    }
+}
+
 // ---- the call ------------------------------------------------------------------------------------------------------
 static int64_t up128(int64_t x) { return (x + 127) / 128 * 128; }
 
 // What a call keeps where in its workspace (bytes).
 struct GradPlan {
-    int n, bits, tiles, passes, digit_bits;
+    int n, bits, tile, tiles, passes, digit_bits;
     int64_t keys[2], places[2], counts, totals;
     int levels;                  // lists of partial sums
     int64_t list_keys[12], list[12];
@@ -384,14 +512,15 @@ static GradPlan plan_grad(int64_t rows, int64_t table_rows, int width) {
     };
     g.passes = (g.bits + SR_BITS - 1) / SR_BITS;
     g.digit_bits = (g.bits + g.passes - 1) / g.passes;
-    g.tiles = (int)((rows + SR_TILE - 1) / SR_TILE);
+    g.tile = rows <= SR_FINE ? SR_TILE_FINE : SR_TILE;
+    g.tiles = (int)((rows + g.tile - 1) / g.tile);
     const bool small = rows <= SR_SMALL;
     for (int b = 0; b < (small ? 1 : 2); ++b) g.keys[b] = take(rows * 4), g.places[b] = take(rows * 4);
     if (!small) g.counts = take(((int64_t)g.tiles << g.digit_bits) * 4), g.totals = take((int64_t)4 << g.digit_bits);
     g.ld = (width + 7) / 8 * 8;
     int64_t n = rows;
-    for (int chunk = RS_ROWS; n > chunk; chunk = RS_SUMS) {
-        n = (n + chunk - 1) / chunk * 2;
+    while (n > RS_CHUNK) {
+        n = (n + RS_CHUNK - 1) / RS_CHUNK * 2;
         g.list_n[g.levels] = (int)n;
         g.list_keys[g.levels] = take(n * 4);
         g.list[g.levels++] = take(n * g.ld * 4);
@@ -408,42 +537,47 @@ static cudaError_t launch_lookup_grad(const ripple_lookup_rows_grad_args& a, voi
     r.n = g.n, r.width = a.width, r.table_rows = (uint32_t)a.out_rows, r.scale = a.scale, r.accumulate = a.accumulate;
     r.src = a.dy, r.ld_src = a.ld_dy, r.out = a.out, r.ld_out = a.ld_out;
     uint8_t* const work = static_cast<uint8_t*>(a.workspace);
-    if (!a.accumulate) {
-        LookupParams z = {};
-        z.rows = (int)a.out_rows, z.width = a.width, z.out = a.out, z.ld_out = a.ld_out;
-        if ((e = launch_lookup<TO, TO, V>(z, stream)) != cudaSuccess) return e;
+    const ZeroParams zeros = a.accumulate ? ZeroParams{} : zeros_of(a.out, a.out_rows, a.width, a.ld_out, sizeof(TO));
+    const unsigned zero_blocks = (unsigned)std::min<int64_t>(zeros.units, (int64_t)ZERO_BLOCKS * sm_count());
+    if (a.rows <= FW_ROWS) {
+        if (a.out_rows * a.width * (int64_t)sizeof(TO) <= FW_TABLE)
+            return launch(k_lookup_grad_table<T, TO, V>, dim3((unsigned)a.out_rows), 128, 0, stream, r, a.ids);
+        if (zeros.units > 0) e = launch(k_zeros, dim3(zero_blocks), 256, 0, stream, zeros);
+        if (e != cudaSuccess || a.rows == 0) return e;
+        return launch(k_lookup_grad_few<T, TO, V>, dim3((unsigned)a.rows), FW_ROWS, 0, stream, r, a.ids);
     }
-    if (a.rows == 0) return e;
-    if (a.rows <= FW_ROWS) return launch(k_lookup_grad_few<T, TO, V>, dim3((unsigned)a.rows), FW_ROWS, 0, stream, r, a.ids);
     SortParams s = {};
-    s.n = g.n, s.tiles = g.tiles, s.table_rows = (uint32_t)a.out_rows, s.ids = a.ids;
+    s.n = g.n, s.tile = g.tile, s.tiles = g.tiles, s.table_rows = (uint32_t)a.out_rows, s.ids = a.ids;
     auto keys = [&](int b) { return reinterpret_cast<uint32_t*>(work + g.keys[b]); };
     auto places = [&](int b) { return reinterpret_cast<int32_t*>(work + g.places[b]); };
     int b = 0;                   // where the sorted list is
     if (a.rows <= SR_SMALL) {
         static bool ready[64];
         if ((e = allow_shared(k_sort_small, (int)sizeof(SmallSort), ready)) != cudaSuccess) return e;
-        s.keys_out = keys(0), s.places_out = places(0);
-        e = launch(k_sort_small, dim3(1), 32 * SS_WARPS, sizeof(SmallSort), stream, s, g.bits);
+        s.keys_out = keys(0), s.places_out = places(0), s.zeros = zeros;
+        e = launch(k_sort_small, dim3(1 + zero_blocks), 32 * SS_WARPS, sizeof(SmallSort), stream, s, g.bits);
     } else {
         static bool ready[64];
         if ((e = allow_shared(k_sort_move, (SR_WARPS + 1) << (SR_BITS + 2), ready)) != cudaSuccess) return e;
         s.counts = reinterpret_cast<int32_t*>(work + g.counts), s.totals = reinterpret_cast<int32_t*>(work + g.totals);
         s.digits = 1 << g.digit_bits;
+        int share = 0;
+        auto next_share = [&]() { s.zeros = share_of(zeros, share, 3 * g.passes), ++share; };
         for (int pass = 0; pass < g.passes && e == cudaSuccess; ++pass) {
             s.shift = pass * g.digit_bits;
             if (pass > 0) s.ids = nullptr, s.keys = keys(b), s.places = places(b), b ^= 1;
             s.keys_out = keys(b), s.places_out = places(b);
-            e = launch(k_sort_count, dim3((unsigned)g.tiles), 32 * SR_WARPS, 0, stream, s);
-            if (e == cudaSuccess) e = launch(k_sort_scan, dim3((unsigned)(s.digits + 7) / 8), 256, 0, stream, s);
-            if (e == cudaSuccess) e = launch(k_sort_move, dim3((unsigned)g.tiles), 32 * SR_WARPS, (size_t)(SR_WARPS + 1) * s.digits * 4, stream, s);
+            next_share();
+            e = launch(k_sort_count, dim3((unsigned)g.tiles + zero_blocks), 32 * SR_WARPS, 0, stream, s);
+            next_share();
+            if (e == cudaSuccess) e = launch(k_sort_scan, dim3((unsigned)(s.digits + 7) / 8 + zero_blocks), 256, 0, stream, s);
+            next_share();
+            if (e == cudaSuccess) e = launch(k_sort_move, dim3((unsigned)g.tiles + zero_blocks), 32 * SR_WARPS, (size_t)(SR_WARPS + 1) * s.digits * 4, stream, s);
         }
     }
     if (e != cudaSuccess) return e;
     r.keys = keys(b), r.places = places(b), r.ld_next = g.ld;
     for (int l = 0; l <= g.levels && e == cudaSuccess; ++l) {
-        r.chunk = l == 0 ? RS_ROWS : RS_SUMS;
-        r.chunks = (r.n + r.chunk - 1) / r.chunk;
         const bool more = l < g.levels;
         r.next_keys = more ? reinterpret_cast<uint32_t*>(work + g.list_keys[l]) : nullptr;
         r.next = more ? reinterpret_cast<float*>(work + g.list[l]) : nullptr;

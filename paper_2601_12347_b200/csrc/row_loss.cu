@@ -706,6 +706,227 @@ static bool readable(int type, const void* p, int64_t ld, int64_t cols) {
 }
 static bool writable(int size, const void* p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0 && ld * size % 32 == 0; }
 
+// ---- few rows, small heads ---------------------------------------------------------------------------------------------
+// W lies in shared memory as fp32, eight rows of x beside it; a lane is a class, warps share the classes and k.  Plain fp32 sums, one launch
+// for the loss, two for its gradient (the second: dW and dbias from g, which is of a few rows).
+constexpr int FL_ROWS = 8, FL_THREADS = 1024, FL_WARPS = FL_THREADS / 32;
+constexpr int FL_BYTES = 220 * 1024;
+constexpr int FL_K = 8;                  // rows of dW per block
+
+struct FewParams {
+    int rows, k, n;
+    const void* x;
+    const void* W;
+    int64_t ld_x, ld_w;
+    const float* bias;
+    const int32_t* labels;
+    float* loss;
+    float* lse;                          // the gradient reads it
+    const float* dloss;
+    float scale;
+    float* g;                            // rows x n; null: not wanted
+    void* dx;
+    int64_t ld_dx;
+    void* dW;
+    int64_t ld_dw;
+    float* dbias;
+};
+__host__ __device__ inline bool few_at_once(int rows, int k, int n);
+__host__ __device__ inline int few_pitch(int n) { return n | 1; }          // of W in shared memory: lanes that are rows of W meet no bank twice
+static int64_t few_bytes(int k, int n) { return ((int64_t)k * few_pitch(n) + FL_ROWS * ((int64_t)k + up_to(n, 32)) + 8 + FL_WARPS * FL_ROWS * 32) * 4; }
+
+template <typename T, bool GRAD>
+__global__ void __launch_bounds__(FL_THREADS, 1) k_loss_few(const __grid_constant__ FewParams p) {
+    pdl_enter();
+    extern __shared__ __align__(16) float few[];
+    const int pitch = few_pitch(p.n), warp = threadIdx.x >> 5, lane = lane_id();
+    const int cols = (p.n + 31) / 32, shares = FL_WARPS / cols, each = (p.k + shares - 1) / shares;      // 32-class blocks; parts of k
+    float* const xs = few;                                // k x FL_ROWS
+    float* const gs = xs + FL_ROWS * p.k;                 // classes x FL_ROWS: logits, then g
+    float* const sums = gs + FL_ROWS * 32 * cols;         // part of k x class block x FL_ROWS x 32
+    float* const ws = sums + FL_WARPS * FL_ROWS * 32;     // k x pitch
+    const T* const x = static_cast<const T*>(p.x);
+    {
+        const T* const W = static_cast<const T*>(p.W);
+        constexpr int U = 8;             // rows that are on their way
+        const int c = warp % cols * 32 + lane;
+        if (c < p.n) {
+            for (int k0 = warp / cols; k0 < p.k && warp / cols < shares; k0 += shares * U) {
+                T v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) if (k0 + u * shares < p.k) v[u] = W[(int64_t)(k0 + u * shares) * p.ld_w + c];
+#pragma unroll
+                for (int u = 0; u < U; ++u) if (k0 + u * shares < p.k) ws[(k0 + u * shares) * pitch + c] = to_f32(v[u]);
+            }
+        }
+    }
+    for (int row0 = blockIdx.x * FL_ROWS; row0 < p.rows; row0 += gridDim.x * FL_ROWS) {
+        for (int k = threadIdx.x; k < p.k; k += FL_THREADS) {
+            T v[FL_ROWS];
+#pragma unroll
+            for (int r = 0; r < FL_ROWS; ++r) v[r] = row0 + r < p.rows ? x[(int64_t)(row0 + r) * p.ld_x + k] : from_f32<T>(0.f);
+#pragma unroll
+            for (int r = 0; r < FL_ROWS; ++r) xs[k * FL_ROWS + r] = to_f32(v[r]);
+        }
+        __syncthreads();
+        const int block = warp % cols, share = warp / cols;
+        if (share < shares) {
+            const int c = min(block * 32 + lane, p.n - 1), end = min(p.k, (share + 1) * each);
+            float z[FL_ROWS] = {};
+#pragma unroll 4
+            for (int k = share * each; k < end; ++k) {
+                const float w = ws[k * pitch + c];
+                const float4 a = *reinterpret_cast<const float4*>(xs + k * FL_ROWS), b = *reinterpret_cast<const float4*>(xs + k * FL_ROWS + 4);
+                z[0] = fmaf(a.x, w, z[0]), z[1] = fmaf(a.y, w, z[1]), z[2] = fmaf(a.z, w, z[2]), z[3] = fmaf(a.w, w, z[3]);
+                z[4] = fmaf(b.x, w, z[4]), z[5] = fmaf(b.y, w, z[5]), z[6] = fmaf(b.z, w, z[6]), z[7] = fmaf(b.w, w, z[7]);
+            }
+#pragma unroll
+            for (int r = 0; r < FL_ROWS; ++r) sums[(warp * FL_ROWS + r) * 32 + lane] = z[r];
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < FL_ROWS * 32 * cols; e += FL_THREADS) {
+            const int r = e / (32 * cols), c = e - r * 32 * cols, row = row0 + r;
+            float z = 0.f;
+            for (int s = 0; s < shares; ++s) z += sums[((s * cols + (c >> 5)) * FL_ROWS + r) * 32 + (c & 31)];
+            if (c < p.n && p.bias) z += p.bias[c];
+            if constexpr (GRAD) {
+                float g = 0.f;
+                if (c < p.n && row < p.rows && has_label(p.labels, row, p.n)) {
+                    const float lse = p.lse[row];
+                    if (lse != -INFINITY) g = (exp2_of((z - lse) * LOG2E) - (p.labels[row] == c ? 1.f : 0.f)) * (p.scale * (p.dloss ? p.dloss[row] : 1.f));
+                }
+                if (p.g && c < p.n && row < p.rows) p.g[(int64_t)row * p.n + c] = g;
+                z = g;
+            }
+            gs[c * FL_ROWS + r] = c < p.n || GRAD ? z : -INFINITY;
+        }
+        __syncthreads();
+        if constexpr (!GRAD) {
+            const int row = row0 + warp;
+            if (warp < FL_ROWS && row < p.rows) {
+                float top = -INFINITY, sum = 0.f;
+                for (int c = lane; c < 32 * cols; c += 32) top = fmaxf(top, gs[c * FL_ROWS + warp]);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+                const float base = top == -INFINITY ? 0.f : top;
+                for (int c = lane; c < 32 * cols; c += 32) sum += exp2_of((gs[c * FL_ROWS + warp] - base) * LOG2E);
+                sum = warp_sum(sum);
+                if (lane == 0) {
+                    const float lse = sum == 0.f && top == -INFINITY ? -INFINITY : top + logf(sum);
+                    p.lse[row] = lse;
+                    if (p.loss) p.loss[row] = has_label(p.labels, row, p.n) && lse != -INFINITY ? lse - gs[p.labels[row] * FL_ROWS + warp] : 0.f;
+                }
+            }
+        } else {
+            for (int k = threadIdx.x; k < p.k && p.dx; k += FL_THREADS) {
+                float d[FL_ROWS] = {};
+#pragma unroll 4
+                for (int c = 0; c < p.n; ++c) {
+                    const float w = ws[k * pitch + c];
+                    const float4 a = *reinterpret_cast<const float4*>(gs + c * FL_ROWS), b = *reinterpret_cast<const float4*>(gs + c * FL_ROWS + 4);
+                    d[0] = fmaf(a.x, w, d[0]), d[1] = fmaf(a.y, w, d[1]), d[2] = fmaf(a.z, w, d[2]), d[3] = fmaf(a.w, w, d[3]);
+                    d[4] = fmaf(b.x, w, d[4]), d[5] = fmaf(b.y, w, d[5]), d[6] = fmaf(b.z, w, d[6]), d[7] = fmaf(b.w, w, d[7]);
+                }
+#pragma unroll
+                for (int r = 0; r < FL_ROWS; ++r) {
+                    const int row = row0 + r;
+                    if (row < p.rows) static_cast<T*>(p.dx)[(int64_t)row * p.ld_dx + k] = from_f32<T>(has_label(p.labels, row, p.n) ? d[r] : 0.f);
+                }
+            }
+            if (few_at_once(p.rows, p.k, p.n)) {         // dW and dbias as well
+                bool live[FL_ROWS];
+#pragma unroll
+                for (int r = 0; r < FL_ROWS; ++r) live[r] = r < p.rows && has_label(p.labels, r, p.n);
+                const int c = warp % cols * 32 + lane;
+                if (c < p.n && warp / cols < shares) {
+                    float g[FL_ROWS], sum = 0.f;
+#pragma unroll
+                    for (int r = 0; r < FL_ROWS; ++r) g[r] = gs[c * FL_ROWS + r], sum += g[r];
+                    if (p.dbias && warp < cols) p.dbias[c] = sum;
+                    for (int k = warp / cols; k < p.k && p.dW; k += shares) {
+                        float d = 0.f;
+#pragma unroll
+                        for (int r = 0; r < FL_ROWS; ++r) if (live[r]) d = fmaf(xs[k * FL_ROWS + r], g[r], d);
+                        static_cast<T*>(p.dW)[(int64_t)k * p.ld_dw + c] = from_f32<T>(d);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// dW = x^T g and dbias: a block has FL_K rows of dW and 32 columns, its warps take turns over the rows of x; those without a label are passed over.
+template <typename T>
+__global__ void __launch_bounds__(FL_THREADS) k_loss_few_weights(const __grid_constant__ FewParams p) {
+    pdl_enter();
+    constexpr int U = 16;                  // rows of a warp that are on their way
+    __shared__ __align__(16) float sums[FL_WARPS][FL_K + 1][32];       // (and before the end, rows of x)
+    static_assert(U <= 32 && U * FL_K <= (FL_K + 1) * 32 && 32 % FL_K == 0, "a warp's rows of x lie in its sums");
+    const int warp = threadIdx.x >> 5, lane = lane_id(), k0 = blockIdx.x * FL_K, c = blockIdx.y * 32 + lane;
+    const int k = min(k0 + (lane & (FL_K - 1)), p.k - 1), c_in = min(c, p.n - 1);
+    const T* const x = static_cast<const T*>(p.x) + k;
+    float* const xs = &sums[warp][0][0];
+    float d[FL_K] = {}, of_bias = 0.f;
+    for (int row0 = warp; row0 < p.rows; row0 += FL_WARPS * U) {
+        // x: a lane has one of the columns of every fourth row
+        constexpr int PER = 32 / FL_K, XU = U / PER;
+        float v[XU], g[U];
+#pragma unroll
+        for (int u = 0; u < XU; ++u) v[u] = to_f32(x[(int64_t)min(row0 + (u * PER + lane / FL_K) * FL_WARPS, p.rows - 1) * p.ld_x]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) g[u] = p.g[(int64_t)min(row0 + u * FL_WARPS, p.rows - 1) * p.n + c_in];
+        const int mine = row0 + (lane % U) * FL_WARPS;
+        const uint32_t live = __ballot_sync(FULL, mine < p.rows && has_label(p.labels, min(mine, p.rows - 1), p.n));
+#pragma unroll
+        for (int u = 0; u < XU; ++u) xs[(u * PER + lane / FL_K) * FL_K + lane % FL_K] = live >> (u * PER + lane / FL_K) & 1 ? v[u] : 0.f;
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float gu = live >> u & 1 ? g[u] : 0.f;
+            of_bias += gu;
+#pragma unroll
+            for (int j = 0; j < FL_K; j += 4) {
+                const float4 a = *reinterpret_cast<const float4*>(xs + u * FL_K + j);
+                d[j] = fmaf(a.x, gu, d[j]), d[j + 1] = fmaf(a.y, gu, d[j + 1]), d[j + 2] = fmaf(a.z, gu, d[j + 2]), d[j + 3] = fmaf(a.w, gu, d[j + 3]);
+            }
+        }
+        __syncwarp();
+    }
+#pragma unroll
+    for (int j = 0; j < FL_K; ++j) sums[warp][j][lane] = d[j];
+    sums[warp][FL_K][lane] = of_bias;
+    __syncthreads();
+    if (warp > FL_K || c >= p.n) return;
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < FL_WARPS; ++w) total += sums[w][warp][lane];
+    if (warp == FL_K) {
+        if (p.dbias && k0 == 0) p.dbias[c] = total;
+    } else if (p.dW && k0 + warp < p.k) {
+        static_cast<T*>(p.dW)[(int64_t)(k0 + warp) * p.ld_dw + c] = from_f32<T>(total);
+    }
+}
+
+// Rows up to which calls of small heads take this form: a round of eight rows on every SM, fp32 of up to 64 classes two.  Both sides, us on the device for
+// the loss and its gradient, this form / tensor cores: fp32 602 -> 41, 1000 rows 12 + 25 / 18 + 50, 2000 rows 18 + 42 / 19 + 53, 4000 rows 29 + 75 / 21 + 65;
+// 256 -> 150, 1000 rows 13 + 28 / 16 + 44, 2000 rows 20 + 49 / 16 + 45; bf16 602 -> 41, 1000 rows 12 + 26 / 12 + 32, 2000 rows 18 + 42 / 13 + 34.
+constexpr int FL_ROUND = FL_ROWS * 2 * LS_PAIRS;
+static bool few_form(int type, int64_t rows, int k, int n) {
+    return rows <= (type == RIPPLE_TYPE_F32 && n <= 64 ? 2 * FL_ROUND : FL_ROUND) && n <= 32 * FL_WARPS && few_bytes(k, n) <= FL_BYTES;
+}
+// Whether one block forms dW too (1 row, 128 -> 40: 8.6 us for the gradient, 9.5 with a launch more; 256 -> 47: 13.4 and 11.7).
+__host__ __device__ inline bool few_at_once(int rows, int k, int n) { return rows <= FL_ROWS && k * n <= 8192; }
+
+template <int TYPE, bool GRAD>
+static cudaError_t launch_few(const FewParams& p, void* stream) {
+    auto* const kernel = k_loss_few<typename Elem<TYPE>::T, GRAD>;
+    static bool ready[64];
+    const cudaError_t e = allow_shared(kernel, FL_BYTES, ready);
+    if (e != cudaSuccess) return e;
+    return launch(kernel, dim3((unsigned)std::min((p.rows + FL_ROWS - 1) / FL_ROWS, sm_count())), FL_THREADS, (size_t)few_bytes(p.k, p.n), stream, p);
+}
+
 struct Slots {
     int64_t at = 0;
     int64_t take(int64_t bytes) {
@@ -731,6 +952,7 @@ struct LossPlan {
 };
 static LossPlan plan_loss(const ripple_loss_rows_args& a) {
     LossPlan l = {};
+    if (few_form(a.type, a.rows, a.k, a.n)) return l;
     Slots s;
     l.x = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, false), l.w = operand(s, a.type, a.W, a.ld_w, a.k, a.n, false);
     l.col_tiles = (a.n + cols_of(a.type) - 1) / cols_of(a.type);
@@ -759,6 +981,11 @@ struct GradPlanLoss {
 static GradPlanLoss plan_loss_grad(const ripple_loss_rows_grad_args& a) {
     GradPlanLoss l = {};
     Slots s;
+    if (few_form(a.type, a.rows, a.k, a.n)) {
+        if ((a.dW || a.dbias) && !few_at_once((int)a.rows, a.k, a.n)) s.take(a.rows * a.n * 4);        // g
+        l.bytes = s.at;
+        return l;
+    }
     l.control = s.take(sizeof(RowControl));
     l.x = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, false), l.w = operand(s, a.type, a.W, a.ld_w, a.k, a.n, false);
     if (a.dW && l.x.at < 0) l.x_clean = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, true);
@@ -849,6 +1076,11 @@ static Matrix matrix_of(const Operand& o, int type, const void* p, int64_t ld, i
 
 template <int TYPE>
 static cudaError_t run_loss(const ripple_loss_rows_args& a) {
+    if (few_form(a.type, a.rows, a.k, a.n)) {
+        FewParams f = {};
+        f.rows = (int)a.rows, f.k = a.k, f.n = a.n, f.x = a.x, f.W = a.W, f.ld_x = a.ld_x, f.ld_w = a.ld_w, f.bias = a.bias, f.labels = a.labels, f.loss = a.loss, f.lse = a.lse;
+        return launch_few<TYPE, false>(f, a.cuda_stream);
+    }
     const LossPlan l = plan_loss(a);
     uint8_t* const work = static_cast<uint8_t*>(a.workspace);
     cudaError_t e = cudaSuccess;
@@ -872,6 +1104,15 @@ static cudaError_t join_parts(const float* parts, int splits, int64_t stride, in
 template <int TYPE>
 static cudaError_t run_loss_grad(const ripple_loss_rows_grad_args& a) {
     using T = typename Elem<TYPE>::T;
+    if (few_form(a.type, a.rows, a.k, a.n)) {
+        FewParams f = {};
+        f.rows = (int)a.rows, f.k = a.k, f.n = a.n, f.x = a.x, f.W = a.W, f.ld_x = a.ld_x, f.ld_w = a.ld_w, f.bias = a.bias, f.labels = a.labels;
+        f.lse = const_cast<float*>(a.lse), f.dloss = a.dloss, f.scale = a.scale, f.dx = a.dx, f.ld_dx = a.ld_dx, f.dW = a.dW, f.ld_dw = a.ld_dw, f.dbias = a.dbias;
+        if ((a.dW || a.dbias) && !few_at_once(f.rows, a.k, a.n)) f.g = static_cast<float*>(a.workspace);
+        const cudaError_t e = launch_few<TYPE, true>(f, a.cuda_stream);
+        if (e != cudaSuccess || !f.g) return e;
+        return launch(k_loss_few_weights<T>, dim3((unsigned)(a.dW ? (a.k + FL_K - 1) / FL_K : 1), (unsigned)(a.n + 31) / 32), FL_THREADS, 0, a.cuda_stream, f);
+    }
     const GradPlanLoss l = plan_loss_grad(a);
     uint8_t* const work = static_cast<uint8_t*>(a.workspace);
     void* const stream = a.cuda_stream;
@@ -956,10 +1197,10 @@ extern "C" ripple_status ripple_loss_rows(const ripple_loss_rows_args* a) {
         if (reinterpret_cast<uintptr_t>(ptr) % size) REFUSE("misaligned pointer");
     if (a->rows == 0) return RIPPLE_OK;
     const int64_t need = plan_loss(*a).bytes;
-    if (a->workspace_bytes < need || !a->workspace) REFUSE("workspace too small");
+    if (a->workspace_bytes < need || (need > 0 && !a->workspace)) REFUSE("workspace too small");
     if (reinterpret_cast<uintptr_t>(a->workspace) & 127) REFUSE("misaligned workspace");
     const Extent x{a->x, a->rows, a->ld_x, a->k, ts}, W{a->W, a->k, a->ld_w, a->n, ts}, bias{a->bias, 1, 1, a->n, 4}, labels{a->labels, a->rows, 1, 1, 4},
-        loss{a->loss, a->rows, 1, 1, 4}, lse{a->lse, a->rows, 1, 1, 4}, work{a->workspace, 1, 1, need, 1};
+        loss{a->loss, a->rows, 1, 1, 4}, lse{a->lse, a->rows, 1, 1, 4}, work{need > 0 ? a->workspace : nullptr, 1, 1, need, 1};
     for (const Extent* out : {&loss, &lse, &work})
         for (const Extent* in : {&x, &W, &bias, &labels})
             if (extents_meet(*out, *in)) REFUSE("an output or the workspace overlaps an input");

@@ -321,7 +321,10 @@ using namespace rp;
         return RIPPLE_ERR_INVALID_ARG;          \
     } while (0)
 
-static int64_t grad_workspace(int64_t rows, int width) { return (int64_t)grad_blocks_most(rows, width) * 2 * width * 4; }
+static int64_t grad_workspace(int64_t rows, int width) {
+    const int64_t blocks = grad_blocks_most(rows, width);
+    return blocks > 1 ? blocks * 2 * width * 4 : 0;       // (one block writes the results)
+}
 
 extern "C" int64_t ripple_norm_rows_grad_workspace_bytes(const ripple_norm_rows_grad_args* a) {
     if (!a || a->rows < 0 || a->rows > INT32_MAX || a->width < 1 || a->width > 16384) return -1;

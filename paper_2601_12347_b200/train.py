@@ -175,7 +175,7 @@ def loss_rows(x, W, labels, bias=None):
     class.  x [rows, K] and W [K, N] of one type, bias fp32; a bias of minus infinity takes a class out."""
     _tangents(x=x, W=W, bias=bias)
     index, rows, head = _linear(x, W, labels, bias)
-    loss, lse = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
+    loss, lse = (torch.empty(rows, dtype=torch.float32, device=x.device) for _ in range(2))
     head = (*head, loss.data_ptr(), lse.data_ptr())
     lib = _ripple.load_library()
     need = lib.ripple_loss_rows_workspace_bytes(_LOSS_ARGS.pack(*head, 0, 0, 0))

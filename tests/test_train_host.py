@@ -72,20 +72,20 @@ def lookup_grad_args(**kw):
 
 
 def norm_grad_args(**kw):
-    M, D = kw.get("rows", 4), kw.get("width", 8)
+    M, D = kw.get("rows", 40), kw.get("width", 8)
     return _pack(train._NORM_GRAD_ARGS, NORM_GRAD, dict(
         rows=M, width=D, type=0, x_type=0, device=-1, dn=A, ld_dn=D, x=2 * A, ld_x=D, x_rows=M, ids=0, add=0, ld_add=0, dx=3 * A, ld_dx=D,
         dweight=4 * A, dbias=5 * A, norm=(1, 1e-5, 6 * A, 0), workspace=7 * A, workspace_bytes=1 << 22, cuda_stream=0), kw)
 
 
 def loss_args(**kw):
-    M, K, N = kw.get("rows", 4), kw.get("k", 16), kw.get("n", 8)
+    M, K, N = kw.get("rows", 4000), kw.get("k", 16), kw.get("n", 8)
     return _pack(train._LOSS_ARGS, LOSS, dict(rows=M, type=0, k=K, n=N, device=-1, x=A, ld_x=K, W=2 * A, ld_w=N, bias=3 * A, labels=4 * A, loss=5 * A,
                                               lse=6 * A, workspace=7 * A, workspace_bytes=1 << 23, cuda_stream=0), kw)
 
 
 def loss_grad_args(**kw):
-    M, K, N = kw.get("rows", 4), kw.get("k", 16), kw.get("n", 8)
+    M, K, N = kw.get("rows", 4000), kw.get("k", 16), kw.get("n", 8)
     return _pack(train._LOSS_GRAD_ARGS, LOSS_GRAD, dict(
         rows=M, type=0, k=K, n=N, device=-1, x=A, ld_x=K, W=2 * A, ld_w=N, bias=3 * A, labels=4 * A, lse=5 * A, dloss=6 * A, dx=7 * A, ld_dx=K,
         dW=8 * A, ld_dw=N, dbias=9 * A, scale=1.0, reserved=0, workspace=10 * A, workspace_bytes=1 << 23, cuda_stream=0), kw)
