@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <cstdlib>
+#include <type_traits>
 #include <utility>
 
 namespace rp {
@@ -30,20 +31,24 @@ cudaError_t take_loss_timeout(int* gave_up) {
 // of C.  (One CTA by itself brings 48 KB per 64 entries of k, where an SM gets 64 bytes a cycle out of L2: 768 cycles for 512 of products.)
 // Operands come by TMA in either order, k along the rows of memory or across them; what lies outside a matrix arrives as zeros.
 constexpr int LS_ROWS = 256, LS_KC = 64;
-constexpr int LS_EPI_WARPS = 8, LS_THREADS = 64 + 32 * LS_EPI_WARPS;
 constexpr int LS_PAIRS = 74;             // of a B200 (for plans that are asked where no device is current, too)
 constexpr int LS_UNIT = 4;               // fp32: chunks (256 entries of k) whose large products share an accumulator
 constexpr int LS_GROUP = 8;              // tiles of rows that are worked on side by side, so that B's tiles are read out of L2
 constexpr uint32_t LS_SPIN_LIMIT = 1u << 18;       // polls after which a wait gives up: about a second
 constexpr float LOG2E = 1.4426950408889634f;
 
-template <int TYPE> struct LossShape {
+// MANY: fp32 over more than one unit of k, whose sums the epilogue carries in registers
+template <int TYPE, bool MANY> struct LossShape {
     static constexpr int PARTS = TYPE == RIPPLE_TYPE_F32 ? 3 : 1;
     static constexpr int COLS = PARTS == 3 ? 128 : 256;
     static constexpr int A_PART = 128 * 128, B_PART = COLS / 2 * 128;       // bytes of a CTA's operands of 64 entries of k
     static constexpr int STAGE = PARTS * (A_PART + B_PART);
     static constexpr int STAGES = PARTS == 3 ? 3 : 6;
-    static constexpr int BIAS = LS_EPI_WARPS * (COLS / 2) * 4;
+    // Warps that take accumulators: sixteen, four to a scheduler, so that one's exponentials are on their way while others add (loss-wide, g
+    // of a piece: 281 us with eight, 215 with sixteen); eight where the sums carried need the registers.
+    static constexpr int EPI_WARPS = MANY ? 8 : 16, GROUPS = EPI_WARPS / 4;
+    static constexpr int THREADS = 64 + 32 * EPI_WARPS;
+    static constexpr int BIAS = EPI_WARPS * (COLS / GROUPS) * 4;
     static constexpr size_t BYTES = (size_t)STAGES * STAGE + BIAS + 1024;
 };
 
@@ -66,7 +71,7 @@ struct alignas(64) ProductParams {
     const float* bias;                   // of the piece
     const int32_t* labels;
     int class0, classes;                 // first class of the piece, number of all
-    float2* sums;                        // LSE: 2 x col_tiles x m: largest logit, sum of exp(logit - largest)
+    float2* sums;                        // LSE: GROUPS x col_tiles x m: largest logit, sum of exp(logit - largest)
     float* at_label;
     const float* lse;                    // GRAD
     const float* dloss;
@@ -97,8 +102,9 @@ __device__ __forceinline__ uint32_t in_leader(const void* p) {
     asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(p)));
     return a;
 }
+// (relaxed: what is handed over is tensor memory, ordered by the fences of tcgen05; a release would wait for the warp's stores to global memory)
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 // a box of a tensor, completing on a barrier of either CTA of the pair
 __device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
@@ -129,8 +135,10 @@ __device__ __forceinline__ void store8(void* to, const uint32_t (&v)[8]) {
                  ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 template <typename T> __device__ __forceinline__ uint32_t pair_of(float a, float b) {
-    const T x = from_f32<T>(a), y = from_f32<T>(b);
-    return (uint32_t)*reinterpret_cast<const uint16_t*>(&x) | (uint32_t)*reinterpret_cast<const uint16_t*>(&y) << 16;
+    uint32_t d;
+    if constexpr (sizeof(T) == 2 && std::is_same<T, __half>::value) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(b), "f"(a));
+    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(b), "f"(a));
+    return d;
 }
 // An fp32 value as three bf16 parts, rounded; both remainders are exact.  An infinite value has no remainders.
 __device__ __forceinline__ void three_parts(float x, __nv_bfloat16 (&h)[3]) {
@@ -174,11 +182,11 @@ __device__ __forceinline__ float column_sums(float (&v)[32]) {
 // (the products that read stage s), acc_full[b] in both, acc_empty[b] in the first CTA (one arrival per epilogue warp of the pair).
 // fp32: six products of parts (all but those below 2^-24); the large one, of the first parts, is handed over every 256 entries of k and
 // summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
-template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_product(const __grid_constant__ ProductParams p) {
-    using S = LossShape<TYPE>;
+template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END, bool MANY>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY>::THREADS, 1) k_product(const __grid_constant__ ProductParams p) {
+    using S = LossShape<TYPE, MANY>;
     using T = typename Elem<TYPE == RIPPLE_TYPE_F16 ? RIPPLE_TYPE_F16 : RIPPLE_TYPE_BF16>::T;      // of the operands
-    constexpr int PARTS = S::PARTS, STAGES = S::STAGES, COLS = S::COLS, NB = COLS / 64;       // NB: 32-column blocks of an epilogue warp
+    constexpr int PARTS = S::PARTS, STAGES = S::STAGES, COLS = S::COLS, GROUPS = S::GROUPS, NB = COLS / (32 * GROUPS);      // NB: 32-column blocks of an epilogue warp
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
     __shared__ uint32_t tmem_slot;
@@ -193,11 +201,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_pro
     struct Tile { int row, col, split, first, last, nt; };
     auto tile_at = [&](int64_t i) {
         Tile t;
-        t.split = (int)(i / tiles);
-        const int64_t in = i - t.split * tiles, per_group = (int64_t)LS_GROUP * p.col_tiles;
-        const int group = (int)(in / per_group), rows = min(LS_GROUP, p.row_tiles - group * LS_GROUP);
-        const int64_t rest = in - group * per_group;
-        t.col = (int)(rest / rows), t.row = group * LS_GROUP + (int)(rest % rows);
+        auto place = [&](auto in, auto in_split) {       // (64-bit divisions take hundreds of cycles: only where there are so many tiles)
+            t.split = (int)(in / in_split), in -= (decltype(in))t.split * in_split;
+            const decltype(in) per_group = (decltype(in))LS_GROUP * p.col_tiles;
+            const int group = (int)(in / per_group), rows = min(LS_GROUP, p.row_tiles - group * LS_GROUP);
+            const uint32_t rest = (uint32_t)(in - group * per_group);
+            t.col = (int)(rest / (uint32_t)rows), t.row = group * LS_GROUP + (int)(rest - (uint32_t)t.col * (uint32_t)rows);
+        };
+        if (all < (1ll << 31)) place((uint32_t)i, (uint32_t)tiles);
+        else place((uint64_t)i, (uint64_t)tiles);
         t.first = t.split * p.split_chunks, t.last = min(chunks, t.first + p.split_chunks);
         t.nt = min(COLS, (p.n - t.col * COLS + 31) & ~31);
         return t;
@@ -205,7 +217,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_pro
 
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], p.withhold ? 2 : 1 /* one arrives */); mbar_init(&acc_empty[b], 2 * LS_EPI_WARPS); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], p.withhold ? 2 : 1 /* one arrives */); mbar_init(&acc_empty[b], 2 * S::EPI_WARPS); }
         mbar_init(&drained, 1);
         s_fail = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -299,7 +311,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_pro
                 int b = 0;
                 for (int c = first; c < last; ++c) {
                     const int in = c - first;
-                    const bool fresh = PARTS == 3 ? in % LS_UNIT == 0 : in == 0;
+                    const bool fresh = MANY ? in % LS_UNIT == 0 : in == 0;
                     if (fresh) {
                         b = sg & 1;
                         const int before = sg >> 1;
@@ -315,7 +327,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_pro
                     tc_fence_after();
                     // (broadcast: operands that the compiler cannot see to be the warp's take ten times as long to issue)
                     const uint64_t at = (uint64_t)((uint32_t)__shfl_sync(FULL, s, 0) * (S::STAGE >> 4)), a = a0 + at, w = b0 + at;
-                    const bool done = c == last - 1 || (PARTS == 3 && in % LS_UNIT == LS_UNIT - 1);
+                    const bool done = c == last - 1 || (MANY && in % LS_UNIT == LS_UNIT - 1);
                     if (lead) {
 #pragma unroll
                         for (int j = 0; j < LS_KC / 16; ++j) {
@@ -347,8 +359,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_pro
         }
     } else {
         // ---------------- epilogue ----------------
-        // thread: a row, and the 32-column blocks half, half + 2, ... of the tile
-        const int q = warp & 3, half = (warp - 2) >> 2;
+        // thread: a row, and the 32-column blocks part, part + GROUPS, ... of the tile
+        const int q = warp & 3, part = (warp - 2) >> 2;
         const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16);
         float* const bias = reinterpret_cast<float*>(ring + STAGES * S::STAGE) + (warp - 2) * 32 * NB;
         float factor = 1.f;                      // GRAD: of g; OUT: of the result
@@ -359,43 +371,51 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_pro
         const uint32_t release = in_leader(&acc_empty[0]);
         bool ok = true;
         int sg = 0, worked = 0;
+        // What a tile's rows and columns have to do with: asked for a tile ahead.
+        struct Ahead { int label; float lse, dloss, bias[NB]; };
+        auto row_of_tile = [&](const Tile& t) { return t.row * LS_ROWS + (int)rank * 128 + 32 * q + lane; };
+        auto ask = [&](const Tile& t) {
+            Ahead a = {-1, 0.f, 1.f};
+            const int row = row_of_tile(t);
+            const int32_t* const labels = END == END_OUT ? p.dead_rows : p.labels;
+            if (row < p.m && labels) a.label = labels[row];
+            if constexpr (END == END_GRAD) {
+                if (row < p.m) a.lse = p.lse[row];
+                if (row < p.m && p.dloss) a.dloss = p.dloss[row];
+            }
+            if constexpr (END != END_OUT) {
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    const int col = t.col * COLS + 32 * (GROUPS * j + part) + lane;
+                    a.bias[j] = col >= p.n ? -INFINITY : p.bias ? p.bias[col] : 0.f;
+                }
+            }
+            return a;
+        };
+        Tile following = tile_at(pair);
+        Ahead asked = ask(following);
         for (int64_t i = pair; i < all && ok; i += pairs, ++worked) {
-            const Tile t = tile_at(i);
-            const int row = t.row * LS_ROWS + (int)rank * 128 + 32 * q + lane, col0 = t.col * COLS;
-            const bool in_rows = row < p.m;
-            int label = -1;
-            float lse = 0.f, weight = 0.f, top = -INFINITY, sum = 0.f;
-            bool live = in_rows;
+            const Tile t = following;
+            const int row = row_of_tile(t), col0 = t.col * COLS;
+            const bool in_rows = row < p.m, labelled = asked.label >= 0 && asked.label < p.classes;
+            bool live = END == END_OUT ? in_rows && (!p.dead_rows || labelled) : labelled;
+            const float lse = asked.lse, weight = p.scale * asked.dloss;
+            float top = -INFINITY, sum = 0.f;
+            if (END == END_GRAD) live = live && lse != -INFINITY;
+            const int label = live ? asked.label - p.class0 - col0 : -1;       // within the tile
             if constexpr (END != END_OUT) {
                 __syncwarp();
-                for (int e = lane; e < 32 * NB; e += 32) {
-                    const int col = col0 + 32 * (2 * (e >> 5) + half) + (e & 31);
-                    bias[e] = col >= p.n ? -INFINITY : p.bias ? p.bias[col] : 0.f;
-                }
+#pragma unroll
+                for (int j = 0; j < NB; ++j) bias[32 * j + lane] = asked.bias[j];
                 __syncwarp();
-                if (in_rows) label = p.labels[row];
-                if (label >= p.classes) label = -1;
-                live = label >= 0;
             }
-            if constexpr (END == END_GRAD) {
-                if (live) {
-                    lse = p.lse[row], weight = p.scale * (p.dloss ? p.dloss[row] : 1.f);
-                    live = lse != -INFINITY;
-                }
-            }
-            if constexpr (END != END_OUT) label = live ? label - p.class0 - col0 : -1;       // within the tile
-            if constexpr (END == END_OUT) {
-                if (p.dead_rows && in_rows) {
-                    const int of_row = p.dead_rows[row];
-                    live = of_row >= 0 && of_row < p.classes;
-                }
-            }
+            if (i + pairs < all) following = tile_at(i + pairs), asked = ask(following);
             // 32 finished sums of this row, from column `at` of the tile
             auto finish = [&](float (&y)[32], int j) {
-                const int at = 32 * (2 * j + half);
+                const int at = 32 * (GROUPS * j + part);
                 if constexpr (END == END_LSE) {
                     const float4* const b4 = reinterpret_cast<const float4*>(bias + 32 * j);
-                    float most = top;
+                    float high[4] = {top, top, top, top};
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float4 b = b4[e];
@@ -406,7 +426,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_pro
                         for (int e = 0; e < 32; ++e) if (label == at + e) p.at_label[row] = y[e];
                     }
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) most = fmaxf(most, y[e]);
+                    for (int e = 0; e < 32; ++e) high[e & 3] = fmaxf(high[e & 3], y[e]);
+                    const float most = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3]));
                     const float base = most == -INFINITY ? 0.f : most * LOG2E;
                     sum *= exp2_of(top * LOG2E - base);
                     float more[4] = {};
@@ -428,7 +449,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_pro
                         for (int e = 0; e < 32; ++e) if (label == at + e) y[e] -= 1.f;
                     }
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) y[e] = live ? y[e] * weight : 0.f;
+                    for (int e = 0; e < 32; ++e) y[e] *= weight;
+                    if (!__all_sync(FULL, live)) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) y[e] = live ? y[e] : 0.f;
+                    }
                     if (p.g && in_rows) {
                         uint16_t* const to = p.g + (int64_t)row * p.ld_g + col0 + at;
                         if constexpr (PARTS == 1) {
@@ -436,7 +461,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_pro
                             for (int h = 0; h < 2; ++h) {
                                 uint32_t v[8];
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) v[e] = pair_of<T>(y[16 * h + 2 * e] * factor, y[16 * h + 2 * e + 1] * factor);
+                                for (int e = 0; e < 8; ++e) {
+                                    if constexpr (TYPE == RIPPLE_TYPE_F16) v[e] = pair_of<T>(y[16 * h + 2 * e] * factor, y[16 * h + 2 * e + 1] * factor);
+                                    else v[e] = pair_of<T>(y[16 * h + 2 * e], y[16 * h + 2 * e + 1]);
+                                }
                                 store8(to + 16 * h, v);
                             }
                         } else {
@@ -501,25 +529,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_pro
                     }
                 }
             };
-            const int units = PARTS == 3 ? (t.last - t.first + LS_UNIT - 1) / LS_UNIT : 1;
-            float carry[PARTS == 3 ? NB : 1][32];          // fp32: of the units before the last
+            const int units = MANY ? (t.last - t.first + LS_UNIT - 1) / LS_UNIT : 1;
+            float carry[MANY ? NB : 1][32];          // fp32: of the units before the last
             for (int u = 0; u < units && ok; ++u, ++sg) {
                 const int b = sg & 1;
                 ok = mbar_wait_warp(&acc_full[b], (sg >> 1) & 1, LS_SPIN_LIMIT);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t large = lanes + large_at(b), small = lanes + small_at(worked);
+                // the accumulator is handed back once this warp's last block has been read
+                const int blocks = t.nt > 32 * part ? min(NB, (t.nt - 32 * part + 32 * GROUPS - 1) / (32 * GROUPS)) : 0;
+                auto hand_back = [&]() {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_at(release + 8 * (uint32_t)b);
+                };
+                if (blocks == 0) hand_back();
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
-                    const int at = 32 * (2 * j + half);
-                    if (at >= t.nt) continue;
+                    const int at = 32 * (GROUPS * j + part);
+                    if (j >= blocks) continue;
                     uint32_t x[32];
                     float y[32];
                     tc_load32(x, large + (uint32_t)at);
                     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
                     for (int e = 0; e < 32; ++e) y[e] = __uint_as_float(x[e]);
-                    if constexpr (PARTS == 3) {
+                    if constexpr (MANY) {
                         if (u > 0) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e) y[e] += carry[j][e];
@@ -527,21 +563,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LS_THREADS, 1) k_pro
                         if (u < units - 1) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e) carry[j][e] = y[e];
+                            if (j == blocks - 1) hand_back();
                             continue;
                         }
-                        tc_load32(x, small + (uint32_t)at);
-                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    }
+                    if constexpr (PARTS == 3) {
                         // (an infinite entry has no parts: its small products may be NaN)
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) if (fabsf(y[e]) < INFINITY) y[e] += __uint_as_float(x[e]);
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t w[16];
+                            tc_load16(w, small + (uint32_t)(at + 16 * h));
+                            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) if (fabsf(y[16 * h + e]) < INFINITY) y[16 * h + e] += __uint_as_float(w[e]);
+                        }
                     }
+                    if (j == blocks - 1) hand_back();
                     finish(y, j);
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) arrive_at(release + 8 * (uint32_t)b);
             }
-            if (END == END_LSE && ok && in_rows) p.sums[(int64_t)(2 * t.col + half) * p.m + row] = make_float2(top, sum);
+            if (END == END_LSE && ok && in_rows) p.sums[(int64_t)(GROUPS * t.col + part) * p.m + row] = make_float2(top, sum);
         }
         if (!ok) s_fail = 1;
     }
@@ -623,7 +664,8 @@ __global__ void __launch_bounds__(256) k_look_at_rows(const T* x, int64_t ld_x, 
         }
         for (uint32_t left = x ? __ballot_sync(FULL, row < rows && !live) : 0; left; left &= left - 1) {
             const T* const from = x + (r0 + __ffs(left) - 1) * ld_x;
-            for (int c = lane_id(); c < k; c += 32) odd = odd || !isfinite(to_f32(from[c]));
+#pragma unroll 8
+            for (int c = lane_id(); c < k; c += 32) odd = odd | !isfinite(to_f32(from[c]));
         }
     }
 #pragma unroll
@@ -636,12 +678,13 @@ __global__ void __launch_bounds__(256) k_look_at_rows(const T* x, int64_t ld_x, 
     }
 }
 
-// Loss and lse of 32 rows per block from the tiles' sums; the warps take turns over the tiles.
+// Loss and lse from the tiles' sums; a block has 32 rows for every TURNS of its 16 warps, which take turns over the tiles.
+template <int TURNS>
 __global__ void __launch_bounds__(512) k_finish_loss(const float2* sums, int parts, int64_t rows, const float* at_label, const int32_t* labels, int classes, float* loss, float* lse) {
     pdl_enter();
     __shared__ float2 mine[16][33];
-    const int warp = threadIdx.x >> 5, lane = lane_id();
-    const int64_t row = (int64_t)blockIdx.x * 32 + lane;
+    const int warp = threadIdx.x >> 5, lane = lane_id(), turn = warp % TURNS;
+    const int64_t row = ((int64_t)blockIdx.x * (16 / TURNS) + warp / TURNS) * 32 + lane;
     float top = -INFINITY, sum = 0.f;
     auto join = [&](float2 s) {
         const float most = fmaxf(top, s.x), base = most == -INFINITY ? 0.f : most;
@@ -650,13 +693,17 @@ __global__ void __launch_bounds__(512) k_finish_loss(const float2* sums, int par
     };
     if (row < rows) {
 #pragma unroll 8
-        for (int i = warp; i < parts; i += 16) join(sums[i * rows + row]);
+        for (int i = turn; i < parts; i += TURNS) join(sums[i * rows + row]);
     }
-    mine[warp][lane] = make_float2(top, sum);
-    __syncthreads();
-    if (warp > 0 || row >= rows) return;
-    top = -INFINITY, sum = 0.f;
-    for (int w = 0; w < 16; ++w) join(mine[w][lane]);
+    if constexpr (TURNS > 1) {
+        mine[warp][lane] = make_float2(top, sum);
+        __syncthreads();
+        if (turn == 0) {
+            top = -INFINITY, sum = 0.f;
+            for (int w = 0; w < TURNS; ++w) join(mine[warp + w][lane]);
+        }
+    }
+    if (turn > 0 || row >= rows) return;
     const float l = top == -INFINITY && sum == 0.f ? -INFINITY : top + logf(sum);
     lse[row] = l;
     if (loss) loss[row] = has_label(labels, row, classes) && l != -INFINITY ? l - at_label[row] : 0.f;
@@ -666,31 +713,36 @@ __global__ void __launch_bounds__(512) k_finish_loss(const float2* sums, int par
 template <typename T>
 __global__ void __launch_bounds__(256) k_join_parts(const float* parts, int splits, int64_t split_stride, int64_t ld, T* out, int64_t ld_out, int64_t rows, int cols) {
     pdl_enter();
+    constexpr int U = 4;
+    const int c0 = blockIdx.x * (256 * U) + threadIdx.x;
     for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
-#pragma unroll 4
-        for (int c = blockIdx.x * 1024 + threadIdx.x; c < min(cols, (int)(blockIdx.x + 1) * 1024); c += 256) {
-            float sum = 0.f;
-            for (int s = 0; s < splits; ++s) sum += parts[s * split_stride + row * ld + c];
-            out[row * ld_out + c] = from_f32<T>(sum);
+        float sum[U] = {};
+#pragma unroll 8
+        for (int s = 0; s < splits; ++s) {
+            const float* const from = parts + s * split_stride + row * ld;
+#pragma unroll
+            for (int u = 0; u < U; ++u) if (c0 + 256 * u < cols) sum[u] += from[c0 + 256 * u];
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u) if (c0 + 256 * u < cols) out[row * ld_out + c0 + 256 * u] = from_f32<T>(sum[u]);
     }
 }
 
 // dbias from the sums over groups of 32 rows; a block has 32 columns, the warps take turns over the groups.
-__global__ void __launch_bounds__(512) k_join_columns(const float* sums, int64_t groups, int64_t ld, int cols, float* out) {
+__global__ void __launch_bounds__(1024) k_join_columns(const float* sums, int64_t groups, int64_t ld, int cols, float* out) {
     pdl_enter();
-    __shared__ float mine[16][33];
+    __shared__ float mine[32][33];
     const int warp = threadIdx.x >> 5, lane = lane_id(), c = blockIdx.x * 32 + lane;
     float sum = 0.f;
     if (c < cols) {
-#pragma unroll 8
-        for (int64_t i = warp; i < groups; i += 16) sum += sums[i * ld + c];
+#pragma unroll 16
+        for (int64_t i = warp; i < groups; i += 32) sum += sums[i * ld + c];
     }
     mine[warp][lane] = sum;
     __syncthreads();
     if (warp > 0 || c >= cols) return;
     sum = 0.f;
-    for (int w = 0; w < 16; ++w) sum += mine[w][lane];
+    for (int w = 0; w < 32; ++w) sum += mine[w][lane];
     out[c] = sum;
 }
 
@@ -698,6 +750,10 @@ __global__ void __launch_bounds__(512) k_join_columns(const float* sums, int64_t
 static int up_to(int64_t x, int to) { return (int)((x + to - 1) / to * to); }
 static int64_t aligned128(int64_t x) { return (x + 127) / 128 * 128; }
 static int parts_of(int type) { return type == RIPPLE_TYPE_F32 ? 3 : 1; }
+// column groups of a tile whose sums the loss keeps apart
+static int groups_of(int type, int k) {
+    return type == RIPPLE_TYPE_F32 && k > LS_UNIT * LS_KC ? LossShape<RIPPLE_TYPE_F32, true>::GROUPS : LossShape<RIPPLE_TYPE_F32, false>::GROUPS;
+}
 static int cols_of(int type) { return type == RIPPLE_TYPE_F32 ? 128 : 256; }
 
 // Whether TMA can read a matrix where it lies.
@@ -956,20 +1012,29 @@ static LossPlan plan_loss(const ripple_loss_rows_args& a) {
     Slots s;
     l.x = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, false), l.w = operand(s, a.type, a.W, a.ld_w, a.k, a.n, false);
     l.col_tiles = (a.n + cols_of(a.type) - 1) / cols_of(a.type);
-    l.sums = s.take(2ll * l.col_tiles * a.rows * 8), l.at_label = s.take(a.rows * 4);
+    l.sums = s.take((int64_t)groups_of(a.type, a.k) * l.col_tiles * a.rows * 8), l.at_label = s.take(a.rows * 4);
     l.bytes = s.at;
     return l;
 }
 
-// Entries of g that are in memory at once (whole tiles of columns of all rows, one tile at least).
-constexpr int64_t LS_PIECE = 1ll << 27;
+// 16-bit entries of g, of all its planes, that are in memory at once (whole tiles of columns of all rows, one tile at least): 512 MB.  Fewer cost loss-wide
+// the rounds of dx in fp32 and tiles of dW too few for all SMs.
+constexpr int64_t LS_PIECE = 1ll << 28;
 
-// A product C [m, n] over k: how many parts k is split into so that every pair of SMs has work, each at least eight chunks long.
+// A product C [m, n] over k: how many parts k is split into where there are fewer tiles than pairs of SMs, so that as many as can be are busy; each part is
+// at least eight chunks long, and their results are written in fp32 and added up.  (Also where there are more tiles, but the last round of
+// them leaves pairs idle: 256 tiles of loss-wide's dx, 212 us a piece in one part, 258 in two.)
 static int splits_of(int type, int64_t m, int64_t n, int64_t k) {
     const int64_t tiles = ((m + LS_ROWS - 1) / LS_ROWS) * ((n + cols_of(type) - 1) / cols_of(type)), chunks = (k + LS_KC - 1) / LS_KC;
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(LS_PAIRS / tiles, chunks / 8));
-    const int64_t each = (chunks + splits - 1) / splits;
-    return (int)((chunks + each - 1) / each);
+    int best = 1;
+    double least = 1e30;
+    for (int s = 1; tiles < LS_PAIRS && s <= std::max<int64_t>(1, std::min<int64_t>(LS_PAIRS, chunks / 8)); ++s) {
+        const int64_t each = (chunks + s - 1) / s;
+        if ((chunks + each - 1) / each != s) continue;
+        const double time = (double)((tiles * s + LS_PAIRS - 1) / LS_PAIRS) * each * (1 + s / 64.0);
+        if (time < least) least = time, best = s;
+    }
+    return best;
 }
 
 struct GradPlanLoss {
@@ -990,7 +1055,7 @@ static GradPlanLoss plan_loss_grad(const ripple_loss_rows_grad_args& a) {
     l.x = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, false), l.w = operand(s, a.type, a.W, a.ld_w, a.k, a.n, false);
     if (a.dW && l.x.at < 0) l.x_clean = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, true);
     const int cols = cols_of(a.type), parts = parts_of(a.type), all = up_to(a.n, 64);
-    l.piece = (int)std::min<int64_t>(all, std::max<int64_t>(cols, LS_PIECE / std::max<int64_t>(a.rows, 1) / cols * cols));
+    l.piece = (int)std::min<int64_t>(all, std::max<int64_t>(cols, LS_PIECE / parts / std::max<int64_t>(a.rows, 1) / cols * cols));
     l.pieces = (a.n + l.piece - 1) / l.piece;
     l.ld_g = l.piece, l.g_plane = aligned128(a.rows * l.ld_g * 2) / 2;
     if (a.dx || a.dW) l.g = s.take(parts * l.g_plane * 2);
@@ -1041,10 +1106,10 @@ static bool tensor_map(CUtensorMap* map, int type, const Matrix& x, int box) {
 }
 
 // a [.., k] (A_ACROSS: [k, ..]), b [.., k] (B_ACROSS: [k, ..])
-template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END>
-static cudaError_t launch_product(ProductParams p, const Matrix& a, const Matrix* a_clean, const Matrix& b, int splits, void* stream) {
-    using S = LossShape<TYPE>;
-    auto* const kernel = k_product<TYPE, A_ACROSS, B_ACROSS, END>;
+template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END, bool MANY>
+static cudaError_t launch_product(ProductParams p, const Matrix& a, const Matrix* a_clean, const Matrix& b, void* stream) {
+    using S = LossShape<TYPE, MANY>;
+    auto* const kernel = k_product<TYPE, A_ACROSS, B_ACROSS, END, MANY>;
     static bool ready[64];
     cudaError_t e = allow_shared(kernel, (int)S::BYTES, ready);
     if (e != cudaSuccess) return e;
@@ -1052,12 +1117,19 @@ static cudaError_t launch_product(ProductParams p, const Matrix& a, const Matrix
         !tensor_map(&p.b, TYPE, b, B_ACROSS ? 64 : S::COLS / 2))
         return cudaErrorInvalidValue;
     p.row_tiles = (p.m + LS_ROWS - 1) / LS_ROWS, p.col_tiles = (p.n + S::COLS - 1) / S::COLS;
-    const int chunks = (p.k + LS_KC - 1) / LS_KC;
-    p.split_chunks = (chunks + splits - 1) / splits, p.splits = (chunks + p.split_chunks - 1) / p.split_chunks;      // (none empty)
     const char* const withhold = std::getenv("RIPPLE_DEBUG_TC_WITHHOLD");
     p.withhold = withhold && withhold[0] == '1';
     const int64_t all = (int64_t)p.row_tiles * p.col_tiles * p.splits;
-    return launch(kernel, dim3((unsigned)(2 * std::min<int64_t>(all, std::max(1, sm_count() / 2)))), LS_THREADS, S::BYTES, stream, p);
+    return launch(kernel, dim3((unsigned)(2 * std::min<int64_t>(all, std::max(1, sm_count() / 2)))), S::THREADS, S::BYTES, stream, p);
+}
+template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END>
+static cudaError_t launch_product(ProductParams p, const Matrix& a, const Matrix* a_clean, const Matrix& b, int splits, void* stream) {
+    const int chunks = (p.k + LS_KC - 1) / LS_KC;
+    p.split_chunks = (chunks + splits - 1) / splits, p.splits = (chunks + p.split_chunks - 1) / p.split_chunks;      // (none empty)
+    if constexpr (TYPE == RIPPLE_TYPE_F32) {
+        if (p.split_chunks > LS_UNIT) return launch_product<TYPE, A_ACROSS, B_ACROSS, END, true>(p, a, a_clean, b, stream);
+    }
+    return launch_product<TYPE, A_ACROSS, B_ACROSS, END, false>(p, a, a_clean, b, stream);
 }
 
 template <int TYPE>
@@ -1093,7 +1165,11 @@ static cudaError_t run_loss(const ripple_loss_rows_args& a) {
     p.sums = reinterpret_cast<float2*>(work + l.sums), p.at_label = reinterpret_cast<float*>(work + l.at_label);
     e = launch_product<TYPE, false, true, END_LSE>(p, matrix_of(l.x, a.type, a.x, a.ld_x, a.rows, a.k, work), nullptr, matrix_of(l.w, a.type, a.W, a.ld_w, a.k, a.n, work), 1, a.cuda_stream);
     if (e != cudaSuccess) return e;
-    return launch(k_finish_loss, dim3((unsigned)((a.rows + 31) / 32)), 512, 0, a.cuda_stream, (const float2*)p.sums, 2 * l.col_tiles, a.rows, (const float*)p.at_label, a.labels, a.n, a.loss, a.lse);
+    const int parts = groups_of(a.type, a.k) * l.col_tiles;
+    auto finish = [&](auto* kernel, int rows) {
+        return launch(kernel, dim3((unsigned)((a.rows + rows - 1) / rows)), 512, 0, a.cuda_stream, (const float2*)p.sums, parts, a.rows, (const float*)p.at_label, a.labels, a.n, a.loss, a.lse);
+    };
+    return parts <= 8 ? finish(k_finish_loss<1>, 512) : finish(k_finish_loss<16>, 32);
 }
 
 template <typename T>
@@ -1141,7 +1217,7 @@ static cudaError_t run_loss_grad(const ripple_loss_rows_grad_args& a) {
         const Matrix* const same = TYPE == RIPPLE_TYPE_F16 ? &x : nullptr;
         e = launch_product<TYPE, false, true, END_GRAD>(p, x, same, w, 1, stream);
         if (e != cudaSuccess) return e;
-        if (a.dbias && (e = launch(k_join_columns, dim3((unsigned)(classes + 31) / 32), 512, 0, stream, (const float*)p.g_sums, (a.rows + 31) / 32, l.ld_g, classes, a.dbias + c0)) != cudaSuccess) return e;
+        if (a.dbias && (e = launch(k_join_columns, dim3((unsigned)(classes + 31) / 32), 1024, 0, stream, (const float*)p.g_sums, (a.rows + 31) / 32, l.ld_g, classes, a.dbias + c0)) != cudaSuccess) return e;
         const Matrix g{work + l.g, a.rows, classes, l.ld_g, l.g_plane, parts_of(TYPE)};
         ProductParams o = {};
         o.unscale = TYPE == RIPPLE_TYPE_F16, o.scale = a.scale, o.classes = a.n;

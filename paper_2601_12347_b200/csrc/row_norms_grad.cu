@@ -60,11 +60,12 @@ constexpr int NG_STAGES = 3;     // rows on their way at most
 // Columns from which the vectors' gradients gather in shared memory: a thread's 32 columns would need 64 registers more.
 constexpr int NG_WIDE = 8192;
 
-// V: neighbouring elements per access, NP: accesses per thread.  A row takes a warp, or (MULTI) the whole block.
+// V: neighbouring elements per access, NP: accesses per thread.  A row takes a warp, or (MULTI) the whole block, of up to THREADS.
 // RING: a thread's part of the rows ahead travels as asynchronous copies into places of shared memory that it alone reads, so no
 // barrier belongs to it.  Else a row is read when its turn comes.  SHARED: dweight and dbias gather in shared memory.
-template <typename T, typename TR, int V, int NP, bool MULTI, bool RING, bool SHARED>
-__global__ void __launch_bounds__(MULTI ? 512 : 128) k_norm_rows_grad(const __grid_constant__ NormGradParams p) {
+// KEEP: the weights of a thread's columns stay in registers (else they are read twice for every row: two fifths of what the kernel asks of L1).
+template <typename T, typename TR, int V, int NP, bool MULTI, bool RING, bool SHARED, bool KEEP, int THREADS>
+__global__ void __launch_bounds__(THREADS) k_norm_rows_grad(const __grid_constant__ NormGradParams p) {
     pdl_enter();
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float scratch[MULTI ? 96 : 1];
@@ -122,6 +123,10 @@ __global__ void __launch_bounds__(MULTI ? 512 : 128) k_norm_rows_grad(const __gr
     for (int j = 0; j < (SHARED ? 1 : NP); ++j) dw[j] = db[j] = all_of<V>(0.f);
     if constexpr (SHARED) each([&](int, int c) { store<float, V>(gather + c, all_of<V>(0.f)), store<float, V>(gather + D + c, all_of<V>(0.f)); });
 
+    Vec<V> weights[KEEP ? NP : 1];
+#pragma unroll
+    for (int j = 0; j < (KEEP ? NP : 1); ++j) weights[j] = all_of<V>(1.f);
+    if constexpr (KEEP) if (p.weight) each([&](int j, int c) { weights[j] = load<float, V>(p.weight + c0 + c); });
     // where this row and the next two come from
     int64_t from = source(first), from1 = source(first + step), from2 = source(first + 2 * step);
     if (ahead > 0) request(0, first, from);
@@ -165,7 +170,8 @@ __global__ void __launch_bounds__(MULTI ? 512 : 128) k_norm_rows_grad(const __gr
         }
         auto weighted = [&](int j, int c) {
             Vec<V> u = d[j];
-            if (p.weight) times<V>(u, load<float, V>(p.weight + c0 + c));
+            if constexpr (KEEP) times<V>(u, weights[j]);
+            else if (p.weight) times<V>(u, load<float, V>(p.weight + c0 + c));
             return u;
         };
         Vec<V> squares = all_of<V>(0.f), of_d = squares, of_dx = squares;
@@ -175,10 +181,17 @@ __global__ void __launch_bounds__(MULTI ? 512 : 128) k_norm_rows_grad(const __gr
             plus<V>(of_d, u);
             add_product<V>(of_dx, u, x[j]);
         });
-        float sums[3] = {folded<V>(squares), folded<V>(of_d), folded<V>(of_dx)};
-        row_sums<MULTI, 3>(sums, scratch, W, turn);
+        float sums[3] = {folded<V>(squares), folded<V>(of_dx), 0.f};
+        if (p.layer) {
+            sums[2] = folded<V>(of_d);
+            row_sums<MULTI, 3>(sums, scratch, W, turn);
+        } else {
+            float two[2] = {sums[0], sums[1]};
+            row_sums<MULTI, 2>(two, scratch, W, turn);
+            sums[0] = two[0], sums[1] = two[1];
+        }
         const float inv = rsqrtf(sums[0] * inv_d + p.eps);
-        const Vec<V> inv_v = all_of<V>(inv), off = all_of<V>(p.layer ? -sums[1] * inv_d : 0.f), along = all_of<V>(-sums[2] * inv * inv_d);
+        const Vec<V> inv_v = all_of<V>(inv), off = all_of<V>(-sums[2] * inv_d), along = all_of<V>(-sums[1] * inv * inv_d);
         each([&](int j, int) { times<V>(x[j], inv_v); });
         if (vectors) {
             if constexpr (SHARED) {
@@ -262,13 +275,13 @@ __global__ void __launch_bounds__(512) k_join_vectors(const float* gathered, int
 
 // Blocks that a call may launch, so that what they gather has a place: more than fit at once at no width, and no more than have rows.
 static int grad_blocks_most(int64_t rows, int width) {
-    const int64_t per_block = width <= 1024 ? 4 : 1;
+    const int64_t per_block = width <= 512 ? 4 : 1;
     return (int)std::min<int64_t>((rows + per_block - 1) / per_block, 148 * 8);
 }
 
-template <typename T, typename TR, int V, int E, bool MULTI, bool RING, bool SHARED>
+template <typename T, typename TR, int V, int E, bool MULTI, bool RING, bool SHARED, bool KEEP, int THREADS>
 static cudaError_t launch_grad(NormGradParams p, int warps, void* stream) {
-    auto* const kernel = k_norm_rows_grad<T, TR, V, E / V, MULTI, RING, SHARED>;
+    auto* const kernel = k_norm_rows_grad<T, TR, V, E / V, MULTI, RING, SHARED, KEEP, THREADS>;
     p.warps_per_row = warps;
     const int block = MULTI ? 32 * warps : 128, rows_per_block = MULTI ? 1 : 4;
     const int64_t blocks = ((int64_t)p.rows + rows_per_block - 1) / rows_per_block;
@@ -292,12 +305,12 @@ static cudaError_t launch_grad(NormGradParams p, int warps, void* stream) {
 template <typename T, typename TR, int V, bool RING>
 static cudaError_t launch_grad(const NormGradParams& p, void* stream) {
     const int D = p.width;
-    if (D <= 256) return launch_grad<T, TR, V, 8, false, RING, false>(p, 1, stream);
-    if (D <= 512) return launch_grad<T, TR, V, 16, false, RING, false>(p, 1, stream);
-    if (D <= 768) return launch_grad<T, TR, V, 24, false, RING, false>(p, 1, stream);
-    if (D <= 1024) return launch_grad<T, TR, V, 32, false, RING, false>(p, 1, stream);
-    if (D <= NG_WIDE) return launch_grad<T, TR, V, 16, true, RING, false>(p, (D + 511) / 512, stream);
-    return launch_grad<T, TR, V, 32, true, false, true>(p, (D + 1023) / 1024, stream);
+    if (D <= 256) return launch_grad<T, TR, V, 8, false, RING, false, true, 128>(p, 1, stream);
+    if (D <= 512) return launch_grad<T, TR, V, 16, false, RING, false, true, 128>(p, 1, stream);
+    if (D <= 1024) return launch_grad<T, TR, V, 16, true, RING, false, true, 64>(p, 2, stream);
+    if (D <= 4096) return launch_grad<T, TR, V, 16, true, RING, false, true, 256>(p, (D + 511) / 512, stream);
+    if (D <= NG_WIDE) return launch_grad<T, TR, V, 16, true, RING, false, false, 512>(p, (D + 511) / 512, stream);
+    return launch_grad<T, TR, V, 32, true, false, true, false, 512>(p, (D + 1023) / 1024, stream);
 }
 
 template <typename T, typename TR>
