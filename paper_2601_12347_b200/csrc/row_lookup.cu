@@ -7,6 +7,7 @@
 #include "row_vectors.cuh"
 
 #include <algorithm>
+#include <cstring>
 #include <utility>
 
 namespace rp {
@@ -20,43 +21,90 @@ struct LookupParams {
     void* out;
     int64_t ld_out;
     float scale;
+    uint32_t scale_pair;         // LK_PAIRS: the scale in the rows' type, twice
 };
 
 constexpr int LK_BLOCK = 256;
 
 constexpr int LK_ROWS = 4;       // rows of a thread that are on their way together
 
-template <typename T, typename TO, int V>
+// How rows are scaled.  LK_COPY: not at all.  LK_PAIRS: 16-bit rows by a scale of their own type, two elements per instruction, whose product is rounded once
+// as well.  (300 007 rows of 256 bf16: 48 us by way of fp32, PAIRS_TIME in pairs.)
+enum { LK_FLOAT, LK_PAIRS, LK_COPY };
+
+template <typename T> __device__ __forceinline__ uint32_t times_pair(uint32_t a, uint32_t b) {
+    uint32_t d;
+    if constexpr (std::is_same<T, __half>::value) asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    else asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+template <typename T, typename TO, int V, int HOW>
 __global__ void __launch_bounds__(LK_BLOCK) k_lookup_rows(const __grid_constant__ LookupParams p) {
     pdl_enter();
     const int t = threadIdx.x & (p.lanes - 1), per_block = LK_BLOCK / p.lanes;
-    const Vec<V> scale = all_of<V>(p.scale);
     for (int64_t row0 = (int64_t)blockIdx.x * per_block * LK_ROWS + threadIdx.x / p.lanes; row0 < p.rows; row0 += (int64_t)gridDim.x * per_block * LK_ROWS) {
-        int64_t id[LK_ROWS];
+        int id[LK_ROWS];
+        const T* from[LK_ROWS];
+        bool real[LK_ROWS], in[LK_ROWS];
 #pragma unroll
-        for (int u = 0; u < LK_ROWS; ++u) id[u] = row0 + u * per_block < p.rows ? p.ids[row0 + u * per_block] : -1;
+        for (int u = 0; u < LK_ROWS; ++u) in[u] = row0 + u * per_block < p.rows, id[u] = in[u] ? p.ids[row0 + u * per_block] : -1;
+#pragma unroll
+        for (int u = 0; u < LK_ROWS; ++u) {
+            real[u] = id[u] >= 0 && id[u] < p.table_rows;
+            from[u] = static_cast<const T*>(p.table) + max(id[u], 0) * p.ld_table;
+        }
+        TO* const to = static_cast<TO*>(p.out) + row0 * p.ld_out;
         for (int c = t * V; c < p.width; c += p.lanes * V) {
-            Vec<V> v[LK_ROWS];
+            Piece<T, V> v[LK_ROWS];
 #pragma unroll
             for (int u = 0; u < LK_ROWS; ++u) {
-                v[u] = all_of<V>(0.f);
-                if (id[u] >= 0 && id[u] < p.table_rows) v[u] = load<T, V>(static_cast<const T*>(p.table) + id[u] * p.ld_table + c);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[u].v[e] = from_f32<T>(0.f);
+                if (real[u]) v[u] = *reinterpret_cast<const Piece<T, V>*>(from[u] + c);
             }
 #pragma unroll
             for (int u = 0; u < LK_ROWS; ++u) {
-                if (id[u] >= 0 && id[u] < p.table_rows) times<V>(v[u], scale);      // (zeros stay zeros whatever the scale)
-                if (row0 + u * per_block < p.rows) store<TO, V>(static_cast<TO*>(p.out) + (row0 + u * per_block) * p.ld_out + c, v[u]);
+                if (!in[u]) continue;
+                Piece<TO, V> y;
+                if constexpr (HOW == LK_PAIRS) {
+#pragma unroll
+                    for (int e = 0; e < V / 2; ++e) reinterpret_cast<uint32_t*>(&y)[e] = real[u] ? times_pair<T>(reinterpret_cast<const uint32_t*>(&v[u])[e], p.scale_pair) : 0u;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        if constexpr (HOW == LK_COPY && std::is_same<T, TO>::value) y.v[e] = v[u].v[e];
+                        else y.v[e] = from_f32<TO>(real[u] ? to_f32(v[u].v[e]) * p.scale : 0.f);      // (zeros stay zeros whatever the scale)
+                    }
+                }
+                *reinterpret_cast<Piece<TO, V>*>(to + u * per_block * p.ld_out + c) = y;
             }
         }
     }
 }
 
-template <typename T, typename TO, int V>
+template <typename T, typename TO, int V, int HOW>
 static cudaError_t launch_lookup(LookupParams p, void* stream) {
     p.lanes = 1;
     while (p.lanes < LK_BLOCK && p.lanes * V < p.width) p.lanes *= 2;
     const int64_t blocks = ((int64_t)p.rows * p.lanes + LK_BLOCK * LK_ROWS - 1) / (LK_BLOCK * LK_ROWS);
-    return launch(k_lookup_rows<T, TO, V>, dim3((unsigned)std::min<int64_t>(blocks, (int64_t)sm_count() * 32)), LK_BLOCK, 0, stream, p);
+    return launch(k_lookup_rows<T, TO, V, HOW>, dim3((unsigned)std::min<int64_t>(blocks, (int64_t)sm_count() * 32)), LK_BLOCK, 0, stream, p);
+}
+template <typename T, typename TO, int V>
+static cudaError_t launch_lookup(LookupParams p, void* stream) {
+    if constexpr (std::is_same<T, TO>::value) {
+        if (p.scale == 1.f) return launch_lookup<T, TO, V, LK_COPY>(p, stream);
+        if constexpr (sizeof(T) == 2 && V > 1) {
+            const T s = std::is_same<T, __half>::value ? T(__float2half_rn(p.scale)) : T(__float2bfloat16_rn(p.scale));
+            uint16_t bits;
+            std::memcpy(&bits, &s, 2);
+            if ((float)s == p.scale) {
+                p.scale_pair = (uint32_t)bits << 16 | bits;
+                return launch_lookup<T, TO, V, LK_PAIRS>(p, stream);
+            }
+        }
+    }
+    return launch_lookup<T, TO, V, LK_FLOAT>(p, stream);
 }
 
 template <typename T, typename TO>
@@ -204,39 +252,62 @@ __device__ __forceinline__ void move_tile(int32_t* at, int digits, int entries, 
     __syncthreads();
 }
 
+// ROUNDS: 32 entries each, of a warp.  A warp counts its entries of every digit, and with that knows each one's rank among its own; the counts of the
+// warps before, of the tiles before and of the digits before are added.
+template <int ROUNDS>
 __global__ void __launch_bounds__(32 * SR_WARPS) k_sort_move(const __grid_constant__ SortParams p) {
     pdl_enter();
     if ((int)blockIdx.x >= p.tiles) return write_zeros(p.zeros, blockIdx.x - p.tiles, gridDim.x - p.tiles);
     extern __shared__ int32_t at[];            // warps x digits, and behind them the digits' starts
     __shared__ int32_t scratch[33];
     int32_t* const start = at + SR_WARPS * p.digits;
+    const int warp = threadIdx.x >> 5, lane = lane_id(), first = blockIdx.x * p.tile + warp * (32 * ROUNDS);
+    uint32_t key[ROUNDS];
+    int32_t place[ROUNDS], rank[ROUNDS];
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int i = first + 32 * r + lane;
+        key[r] = i < p.n ? sort_key(p, i) : 0xffffffffu, place[r] = p.ids || i >= p.n ? i : p.places[i];
+    }
+    for (int d = threadIdx.x; d < p.digits * SR_WARPS; d += blockDim.x) at[d] = 0;
     // starts of the digits: sums of the totals before them
     const int per = (p.digits + blockDim.x - 1) / blockDim.x, d0 = threadIdx.x * per;
     int mine = 0, all;
     for (int d = d0; d < min(d0 + per, p.digits); ++d) mine += p.totals[d];
-    int sum = block_exclusive_scan(mine, scratch, all);
+    int sum = block_exclusive_scan(mine, scratch, all);          // (and a barrier behind the zeros)
     for (int d = d0; d < min(d0 + per, p.digits); ++d) {
         start[d] = sum + p.counts[(int64_t)d * p.tiles + blockIdx.x];
         sum += p.totals[d];
     }
-    const int first = blockIdx.x * p.tile;
-    auto entry = [&](int e) { return e < p.tile && first + e < p.n ? (int)(sort_key(p, first + e) >> p.shift & (uint32_t)(p.digits - 1)) : -1; };
-    auto move = [&](int e, int to) {
-        const int i = first + e;
-        p.keys_out[to] = sort_key(p, i);
-        p.places_out[to] = p.ids ? i : p.places[i];
-    };
-    auto base = [&]() {
-        for (int d = threadIdx.x; d < p.digits; d += blockDim.x) {
-            int sum = start[d];
-            for (int w = 0; w < SR_WARPS; ++w) {
-                const int c = at[w * p.digits + d];
-                at[w * p.digits + d] = sum;
-                sum += c;
-            }
+    int32_t* const own = at + warp * p.digits;
+    const uint32_t before = (1u << lane) - 1;
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const bool in = first + 32 * r + lane < p.n;
+        const int d = in ? (int)(key[r] >> p.shift & (uint32_t)(p.digits - 1)) : -1;
+        const uint32_t same = __match_any_sync(FULL, d);
+        const int had = in ? own[d] : 0;
+        __syncwarp();
+        rank[r] = had + __popc(same & before);
+        if (in && (same & before) == 0) own[d] = had + __popc(same);
+        __syncwarp();
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < p.digits; d += blockDim.x) {
+        int sum = start[d];
+        for (int w = 0; w < SR_WARPS; ++w) {
+            const int c = at[w * p.digits + d];
+            at[w * p.digits + d] = sum;
+            sum += c;
         }
-    };
-    move_tile<SR_WARPS>(at, p.digits, p.tile, entry, move, base);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        if (first + 32 * r + lane >= p.n) continue;
+        const int to = own[key[r] >> p.shift & (uint32_t)(p.digits - 1)] + rank[r];
+        p.keys_out[to] = key[r], p.places_out[to] = place[r];
+    }
 }
 
 // All passes of up to SR_SMALL entries by one block.
@@ -302,6 +373,22 @@ constexpr int RS_WARPS = 8, RS_CHUNK = 32 * RS_WARPS;      // entries of a block
 
 __device__ __forceinline__ uint32_t bare(uint32_t key) { return key & ~EMPTY; }
 
+// V neighbouring elements as they lie in memory, 32 bits at a time: as elements the compiler would widen all of them as soon as they are there, into
+// registers that eight rows on their way do not leave it (121 us in place of RUNS_TIME, lookup-skewed).
+template <typename T, int V> struct Raw {
+    static constexpr int WORDS = V * (int)sizeof(T) < 4 ? 1 : V * (int)sizeof(T) / 4;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void read(const T* from) {
+        if constexpr (V * sizeof(T) == 2) w[0] = *reinterpret_cast<const uint16_t*>(from);
+        else *reinterpret_cast<Piece<uint32_t, WORDS>*>(w) = *reinterpret_cast<const Piece<uint32_t, WORDS>*>(from);
+    }
+    __device__ __forceinline__ float at(int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        else if constexpr (std::is_same<T, __nv_bfloat16>::value) return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+        else return __half2float(__ushort_as_half((unsigned short)(e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffffu)));
+    }
+};
+
 // Runs of the same key among entries in order.  add(k, piece): an entry; end: the last run.  A run that lies within the entries is `complete`, the
 // one that comes from before them and the one that goes on behind them are partial sums.
 template <typename TO, int V, int NP>
@@ -312,11 +399,14 @@ struct Runs {
     float* tail;
     uint32_t run, head_key = NO_KEY, tail_key = NO_KEY;
     bool from_before;
-    Vec<V> sum[NP];
+    float sum[NP][V];
     __device__ __forceinline__ Runs(const RunParams& p_, int c, uint32_t first, uint32_t before, float* h, float* t) : p(p_), c0(c), head(h), tail(t), run(bare(first)), from_before(bare(first) == before) { clear(); }
     __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int j = 0; j < NP; ++j) sum[j] = all_of<V>(0.f);
+        for (int j = 0; j < NP; ++j) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[j][e] = 0.f;
+        }
     }
     template <typename F> __device__ __forceinline__ void each(F f) {
 #pragma unroll
@@ -326,16 +416,22 @@ struct Runs {
         if (run < p.table_rows) {
             if (from_before || goes_on) {
                 float* const to = from_before ? head : tail;
-                each([&](int j, int c) { store<float, V>(to + c, sum[j]); });
+                each([&](int j, int c) {
+                    Piece<float, V> y;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) y.v[e] = sum[j][e];
+                    *reinterpret_cast<Piece<float, V>*>(to + c) = y;
+                });
                 if (from_before) head_key = run;
                 if (goes_on) tail_key = from_before ? run | EMPTY : run;
             } else {
                 TO* const to = static_cast<TO*>(p.out) + (int64_t)run * p.ld_out + c0;
-                const Vec<V> scale = all_of<V>(p.scale);
                 each([&](int j, int c) {
-                    times<V>(sum[j], scale);
-                    if (p.accumulate) plus<V>(sum[j], load<TO, V>(to + c));
-                    store<TO, V>(to + c, sum[j]);
+                    Piece<TO, V> y;
+                    if (p.accumulate) y = *reinterpret_cast<const Piece<TO, V>*>(to + c);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) y.v[e] = from_f32<TO>(sum[j][e] * p.scale + (p.accumulate ? to_f32(y.v[e]) : 0.f));
+                    *reinterpret_cast<Piece<TO, V>*>(to + c) = y;
                 });
             }
             clear();
@@ -346,13 +442,21 @@ struct Runs {
             finish(false);
             run = bare(key), from_before = false;
         }
-        if (key < p.table_rows) each([&](int j, int) { plus<V>(sum[j], piece(j)); });
+        if (key < p.table_rows) {
+            each([&](int j, int) {
+                const auto& v = piece(j);
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[j][e] += v.at(e);
+            });
+        }
     }
 };
 
+// (WIDE: 32 bytes of a lane at a time, lists of partial sums of 16-bit rows; there are few blocks of those, and rows on their way count)
 template <typename T, typename TO, int V, int NP>
-__global__ void __launch_bounds__(32 * RS_WARPS, 4) k_sum_runs(const __grid_constant__ RunParams p) {
+__global__ void __launch_bounds__(32 * RS_WARPS, sizeof(T) * V * NP > 16 ? 2 : 4) k_sum_runs(const __grid_constant__ RunParams p) {
     pdl_enter();
+    constexpr bool WIDE = sizeof(T) * V * NP > 16;
     constexpr int COLS = 32 * V * NP;
     __shared__ __align__(16) float part[2 * RS_WARPS][COLS];
     __shared__ uint32_t part_key[2 * RS_WARPS];
@@ -368,21 +472,21 @@ __global__ void __launch_bounds__(32 * RS_WARPS, 4) k_sum_runs(const __grid_cons
         const int place = p.places ? p.places[i] : i;
         Runs<TO, V, NP> runs(p, c0, __shfl_sync(FULL, key, 0), before, &part[2 * warp][lane * V], &part[2 * warp + 1][lane * V]);
         // (an entry that holds nothing -- padding, EMPTY, none at all -- is not read)
-        constexpr int AHEAD = sizeof(T) * V * NP > 16 ? 4 : 8;       // rows of a warp that are on their way (32 warps of an SM: 64 KB)
-        using Batch = Piece<T, V>[AHEAD][NP];
+        constexpr int AHEAD = WIDE ? 8 : 4;       // rows of a warp that are on their way (32 warps of an SM: up to 64 KB)
+        using Batch = Raw<T, V>[AHEAD][NP];
         auto request = [&](Batch& v, int e0) {
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
                 const uint32_t k = __shfl_sync(FULL, key, e0 + u);
                 const T* const from = static_cast<const T*>(p.src) + (int64_t)__shfl_sync(FULL, place, e0 + u) * p.ld_src + c0;
-                if (e0 + u < count && k < p.table_rows) runs.each([&](int j, int c) { v[u][j] = *reinterpret_cast<const Piece<T, V>*>(from + c); });
+                if (e0 + u < count && k < p.table_rows) runs.each([&](int j, int c) { v[u][j].read(from + c); });
             }
         };
         auto take = [&](const Batch& v, int e0) {
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
                 const uint32_t k = __shfl_sync(FULL, key, e0 + u);
-                if (e0 + u < count) runs.add(k, [&](int j) { return load<T, V>(&v[u][j]); });
+                if (e0 + u < count) runs.add(k, [&](int j) -> const Raw<T, V>& { return v[u][j]; });
             }
         };
         Batch v;
@@ -399,7 +503,7 @@ __global__ void __launch_bounds__(32 * RS_WARPS, 4) k_sum_runs(const __grid_cons
     if (any) {
         const int64_t at = 2ll * block * p.ld_next + c0;
         Runs<TO, V, NP> runs(p, c0, part_key[0], key_at(first - 1), p.next + at, p.next + at + p.ld_next);
-        for (int e = 0; e < 2 * RS_WARPS; ++e) runs.add(part_key[e], [&](int j) { return load<float, V>(&part[e][lane * V + j * 32 * V]); });
+        for (int e = 0; e < 2 * RS_WARPS; ++e) runs.add(part_key[e], [&](int j) { Raw<float, V> r; r.read(&part[e][lane * V + j * 32 * V]); return r; });
         runs.finish(runs.run == key_at(last));
         head_key = runs.head_key, tail_key = runs.tail_key;
     }
@@ -557,8 +661,10 @@ static cudaError_t launch_lookup_grad(const ripple_lookup_rows_grad_args& a, voi
         s.keys_out = keys(0), s.places_out = places(0), s.zeros = zeros;
         e = launch(k_sort_small, dim3(1 + zero_blocks), 32 * SS_WARPS, sizeof(SmallSort), stream, s, g.bits);
     } else {
-        static bool ready[64];
-        if ((e = allow_shared(k_sort_move, (SR_WARPS + 1) << (SR_BITS + 2), ready)) != cudaSuccess) return e;
+        static bool ready[64], ready_fine[64];
+        auto* const move = g.tile == SR_TILE ? k_sort_move<SR_TILE / (32 * SR_WARPS)> : k_sort_move<SR_TILE_FINE / (32 * SR_WARPS)>;
+        if ((e = allow_shared(k_sort_move<SR_TILE / (32 * SR_WARPS)>, (SR_WARPS + 1) << (SR_BITS + 2), ready)) != cudaSuccess) return e;
+        if ((e = allow_shared(k_sort_move<SR_TILE_FINE / (32 * SR_WARPS)>, (SR_WARPS + 1) << (SR_BITS + 2), ready_fine)) != cudaSuccess) return e;
         s.counts = reinterpret_cast<int32_t*>(work + g.counts), s.totals = reinterpret_cast<int32_t*>(work + g.totals);
         s.digits = 1 << g.digit_bits;
         int share = 0;
@@ -572,7 +678,7 @@ static cudaError_t launch_lookup_grad(const ripple_lookup_rows_grad_args& a, voi
             next_share();
             if (e == cudaSuccess) e = launch(k_sort_scan, dim3((unsigned)(s.digits + 7) / 8 + zero_blocks), 256, 0, stream, s);
             next_share();
-            if (e == cudaSuccess) e = launch(k_sort_move, dim3((unsigned)g.tiles + zero_blocks), 32 * SR_WARPS, (size_t)(SR_WARPS + 1) * s.digits * 4, stream, s);
+            if (e == cudaSuccess) e = launch(move, dim3((unsigned)g.tiles + zero_blocks), 32 * SR_WARPS, (size_t)(SR_WARPS + 1) * s.digits * 4, stream, s);
         }
     }
     if (e != cudaSuccess) return e;
