@@ -461,6 +461,15 @@ class Ripple:
             self._stream.wait_stream(self._torch.cuda.current_stream(self._device))
         return got
 
+    def train_step(self, head, ids, labels, kinds=None, dloss=1.0, layer: Optional[int] = None):
+        """A step of `head` (train.ClassHead) on the rows `ids` (CUDA int32) of H^layer (default: the last) with their labels: (loss,
+        gradients), see `ClassHead.step`.  Runs on the current stream of the context's device and does not wait for it; the context's next call
+        waits on the device until the rows have been read, as with `answer`."""
+        got = head.step(self.embeddings(self.L if layer is None else layer), ids, labels, kinds, dloss)
+        if not self._torch.cuda.is_current_stream_capturing():
+            self._stream.wait_stream(self._torch.cuda.current_stream(self._device))
+        return got
+
     def degrees(self):
         def make(which):
             po, pi = ctypes.c_void_p(), ctypes.c_void_p()

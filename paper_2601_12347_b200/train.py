@@ -7,6 +7,8 @@ What requests run (serve.py) has weights; these are fitted here, minibatch by mi
     norm_rows_grad     dx, dweight, dbias of n = norm(x[ids]) (serve.norm_rows)
     loss_rows          softmax cross entropy of x W + bias over many classes, without the logits in memory
     loss_rows_grad     dx, dW, dbias of it
+    ClassHead          a norm and a linear layer over the classes of vertices, with learned rows beside the cached ones: a step is a
+                       run of these calls; `Ripple.train_step` takes it on the rows of a context
 
 Gradients are calls of their own; nothing is recorded, and inputs that require gradients are refused while PyTorch records them (call
 under torch.no_grad() or with detached tensors).  As with requests everything runs on the current CUDA stream of the tensors' device (not
@@ -18,12 +20,14 @@ any gradient, whatever its rows hold.
 from __future__ import annotations
 
 import struct
+from typing import Dict
 
 import torch
 from torch.autograd import forward_ad
 
 from . import ripple as _ripple
-from .serve import TYPE_F32, Norm, _check, _device_of, _matrix, _refuse_tangents, _stream, _type_of, _vector
+from .serve import (NORM_LAYER, NORM_RMS, TYPE_F32, Norm, Projection, RequestHead, _check, _device_of, _matrix, _refuse_tangents, _stream,
+                    _type_of, _vector, norm_rows)
 
 # ripple_lookup_rows_args, ripple_lookup_rows_grad_args, ripple_norm_rows_grad_args
 _LOOKUP_ARGS = struct.Struct("=q4i QqqQ Qq fi Q")
@@ -112,9 +116,9 @@ def lookup_rows_grad(dy, ids, table_rows: int, scale: float = 1.0, out=None, out
     return out
 
 
-def norm_rows_grad(dn, x, norm: Norm, ids=None, add=None, out=None, vectors: bool = True):
+def norm_rows_grad(dn, x, norm: Norm, ids=None, add=None, out=None, dx: bool = True, vectors: bool = True):
     """(dx, dweight, dbias) of n = norm(x[ids]) from dn [rows, D]; dweight and dbias (fp32) are None where the norm has no such
-    vector, or with vectors=False.  x [any, D]: dn's type or fp32; row ids[i] (int32) of it, or row i, was normalised.  dx [rows, D] has x's type; add [rows, D],
+    vector, or with vectors=False; dx=False: no dx.  x [any, D]: dn's type or fp32; row ids[i] (int32) of it, or row i, was normalised.  dx [rows, D] has x's type; add [rows, D],
     of the same type: what reaches x past the norm, added before dx is rounded.  out: where to write dx; it may be dn, add, or, without ids, x."""
     if not isinstance(norm, Norm):
         raise TypeError(f"norm: a Norm expected, got {type(norm).__name__}")
@@ -137,15 +141,20 @@ def norm_rows_grad(dn, x, norm: Norm, ids=None, add=None, out=None, vectors: boo
         add_ptr, add_ld, got = _matrix(add, "add", width, x.dtype, index)
         if got != rows:
             raise ValueError(f"add: {rows} rows expected, got {got}")
-    if out is None:
-        out = torch.empty((rows, width), dtype=x.dtype, device=dn.device)
-        out_ptr, out_ld = out.data_ptr(), width
-    else:
+    out_ptr, out_ld = 0, width
+    if out is not None:
+        if not dx:
+            raise ValueError("out without dx")
         out_ptr, out_ld, got = _matrix(out, "out", width, x.dtype, index)
         if got != rows:
             raise ValueError(f"out: {rows} rows expected, got {got}")
+    elif dx:
+        out = torch.empty((rows, width), dtype=x.dtype, device=dn.device)
+        out_ptr = out.data_ptr()
     dweight = torch.empty(width, dtype=torch.float32, device=dn.device) if vectors and norm.weight is not None else None
     dbias = torch.empty(width, dtype=torch.float32, device=dn.device) if vectors and norm.bias is not None else None
+    if not dx and dweight is None and dbias is None:
+        raise ValueError("no gradient wanted")
     lib = _ripple.load_library()
     stream = _stream(index)
     head = (rows, width, t, tx, index, dn_ptr, dn_ld, x_ptr, x_ld, x_rows, ids_ptr, add_ptr, add_ld, out_ptr, out_ld,
@@ -207,3 +216,83 @@ def loss_rows_grad(x, W, labels, lse, dloss=1.0, bias=None, dx: bool = True, dW:
     work = _workspace(need, x)
     _check(lib.ripple_loss_rows_grad(_LOSS_GRAD_ARGS.pack(*head, _or_null(work), max(need, 0), _stream(index))))
     return gx, gw, gb
+
+
+class LiveNorm(Norm):
+    """A norm whose vectors are the caller's own tensors (fp32, CUDA): what is written into them is seen by the next call."""
+
+    def __init__(self, kind: int, weight, bias=None, eps: float = 1e-5):
+        if kind not in (NORM_LAYER, NORM_RMS):
+            raise ValueError(f"kind: NORM_LAYER or NORM_RMS expected, got {kind}")
+        if not eps >= 0:
+            raise ValueError(f"eps: {eps}")
+        index = _device_of(weight, "weight")
+        if weight.dim() != 1:
+            raise ValueError(f"weight: one dimension expected, got {tuple(weight.shape)}")
+        self.kind, self.eps, self.weight, self.bias = int(kind), float(eps), weight, bias
+        self.width, self.index = weight.shape[0], index
+        w = _vector(weight, "weight", self.width, torch.float32, index)
+        b = 0 if bias is None else _vector(bias, "bias", self.width, torch.float32, index)
+        self._keep(index, *(t for t in (weight, bias) if t is not None))
+        self._args = (self.kind, self.eps, w, b)
+
+
+class ClassHead:
+    """Classes of vertices from their cached rows:  logits = norm(table[ids] + scale * E[kinds]) W + bias.
+
+    Parameters, CUDA tensors that an optimiser updates in place: `norm_weight`, `norm_bias` (fp32 [D]; no bias for NORM_RMS), `W` [D, N] of
+    `dtype`, `bias` (fp32 [N]), and, with `kinds` > 0, `E` [kinds, D] of `dtype`: learned rows of what a vertex is, beside what the graph's layers
+    made of it.  W is drawn from N(0, 1 / D), E starts at zero."""
+
+    def __init__(self, D: int, N: int, kinds: int = 0, kind: int = NORM_LAYER, eps: float = 1e-5, scale: float = 1.0, dtype=torch.float32,
+                 device=None, seed: int = 0):
+        _type_of(dtype, "dtype")
+        device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        g = torch.Generator(device=device).manual_seed(seed)
+        self.W = (torch.randn(D, N, generator=g, device=device) * D ** -0.5).to(dtype)
+        self.bias = torch.zeros(N, device=device)
+        self.norm_weight = torch.ones(D, device=device)
+        self.norm_bias = torch.zeros(D, device=device) if kind == NORM_LAYER else None
+        self.E = torch.zeros(kinds, D, dtype=dtype, device=device) if kinds > 0 else None
+        self.scale = float(scale)
+        self.norm = LiveNorm(kind, self.norm_weight, self.norm_bias, eps)
+
+    def parameters(self) -> Dict[str, torch.Tensor]:
+        """The parameters by name, as the gradients are."""
+        return {k: t for k, t in (("norm_weight", self.norm_weight), ("norm_bias", self.norm_bias), ("W", self.W), ("bias", self.bias), ("E", self.E))
+                if t is not None}
+
+    def _normed(self, table, ids, kinds):
+        """The rows before the norm (None: the table's own) and behind it."""
+        if (kinds is None) != (self.E is None):
+            raise ValueError("kinds go with the learned rows: the head has " + ("none" if self.E is None else "some"))
+        if self.E is None:
+            return None, norm_rows(residual=table, ids=ids, pre=self.norm, normed_dtype=self.W.dtype, clear_padding=True)[1]
+        return norm_rows(lookup_rows(self.E, kinds, self.scale), residual=table, ids=ids, pre=self.norm, clear_padding=True)
+
+    def loss(self, table, ids, labels, kinds=None):
+        """The losses of the rows `ids` (int32) of `table` (fp32, or the head's type), fp32 [len(ids)]; 0 where the label (int32) is none."""
+        return loss_rows(self._normed(table, ids, kinds)[1], self.W, labels, self.bias)[0]
+
+    def step(self, table, ids, labels, kinds=None, dloss=1.0):
+        """(loss, gradients): the losses as `loss` gives them, and by parameter the gradient of their sum weighted by dloss (a number, or
+        fp32 [len(ids)]).  A padding row has a negative id and a negative label.  The gradient of E has the table's type, the others their parameter's."""
+        s, n = self._normed(table, ids, kinds)
+        loss, lse = loss_rows(n, self.W, labels, self.bias)
+        dn, dW, dbias = loss_rows_grad(n, self.W, labels, lse, dloss, self.bias)
+        if s is None:
+            ds, dweight, dnorm_bias = norm_rows_grad(dn, table, self.norm, ids=ids, dx=False)
+        else:
+            ds, dweight, dnorm_bias = norm_rows_grad(dn, s, self.norm)
+        got = {"norm_weight": dweight, "W": dW, "bias": dbias}
+        if dnorm_bias is not None:
+            got["norm_bias"] = dnorm_bias
+        if self.E is not None:
+            got["E"] = lookup_rows_grad(ds, kinds, self.E.shape[0], self.scale)
+        return loss, got
+
+    def request_head(self) -> RequestHead:
+        """What requests run: the head's norm and linear layer as they are now (copies).  Heads with learned rows have no such form."""
+        if self.E is not None:
+            raise ValueError("a head with learned rows has no form for requests")
+        return RequestHead([], Norm(self.norm.kind, self.norm_weight, self.norm_bias, self.norm.eps), Projection(self.W, self.bias))

@@ -186,3 +186,17 @@ def test_what_is_no_cuda_tensor_is_refused():
         train.norm_rows_grad(x, x, None)
     with pytest.raises(TypeError):
         train.lookup_rows(None, ids)
+
+
+def test_rules_of_the_device_code():
+    """As for the kernels of requests: lanes of a warp give up together, and what the kernel before may write is read by ordinary loads."""
+    import re
+
+    import test_device_rules as D
+    D.test_lanes_of_a_warp_give_up_together("row_loss.cu")
+    for name in ("row_loss.cu", "row_lookup.cu", "row_norms_grad.cu", "row_vectors.cuh"):
+        text = open(os.path.join(D.CSRC, name)).read()
+        assert not re.search(r"__restrict__|ld\.global\.nc|__ldg", text), name
+        # every kernel waits for the one before it
+        for m in re.finditer(r"\b__global__\b[^;{]*\{(.{0,4000}?)\n\}", text, flags=re.S):
+            assert "pdl_enter();" in m.group(1) or len(m.group(1)) >= 3990, text[m.start():m.start() + 200]
