@@ -37,8 +37,8 @@ constexpr int LS_GROUP = 8;              // tiles of rows that are worked on sid
 constexpr uint32_t LS_SPIN_LIMIT = 1u << 18;       // polls after which a wait gives up: about a second
 constexpr float LOG2E = 1.4426950408889634f;
 
-// MANY: fp32 over more than one unit of k, whose sums the epilogue carries in registers
-template <int TYPE, bool MANY> struct LossShape {
+// MANY: fp32 over more than one unit of k, whose sums the epilogue carries in registers.  RAW: A is fp32 as the caller has it; warps fetch it and make its parts.
+template <int TYPE, bool MANY, bool RAW = false> struct LossShape {
     static constexpr int PARTS = TYPE == RIPPLE_TYPE_F32 ? 3 : 1;
     static constexpr int COLS = PARTS == 3 ? 128 : 256;
     static constexpr int A_PART = 128 * 128, B_PART = COLS / 2 * 128;       // bytes of a CTA's operands of 64 entries of k
@@ -46,8 +46,10 @@ template <int TYPE, bool MANY> struct LossShape {
     static constexpr int STAGES = PARTS == 3 ? 3 : 6;
     // Warps that take accumulators: sixteen, four to a scheduler, so that one's exponentials are on their way while others add (loss-wide, g
     // of a piece: 281 us with eight, 215 with sixteen); eight where the sums carried need the registers.
-    static constexpr int EPI_WARPS = MANY ? 8 : 16, GROUPS = EPI_WARPS / 4;
-    static constexpr int THREADS = 64 + 32 * EPI_WARPS;
+    static constexpr int EPI_WARPS = MANY || RAW ? 8 : 16, GROUPS = EPI_WARPS / 4;
+    static constexpr int FIRST = RAW ? 4 : 2;            // of them; RAW: whole warpgroups, which share out registers
+    static constexpr int LOADERS = RAW ? 8 : 0;
+    static constexpr int THREADS = 32 * (FIRST + EPI_WARPS + LOADERS);
     static constexpr int BIAS = EPI_WARPS * (COLS / GROUPS) * 4;
     static constexpr size_t BYTES = (size_t)STAGES * STAGE + BIAS + 1024;
 };
@@ -64,6 +66,10 @@ struct RowControl {
 struct alignas(64) ProductParams {
     CUtensorMap a, a_clean, b;           // a_clean: read in place of a where rows without labels hold something that is not finite
     const RowControl* control;           // null: a as it is
+    const float* raw;                    // RAW: A, raw_rows x raw_cols
+    int64_t ld_raw;
+    int raw_rows, raw_cols;
+    const int32_t* raw_labels;           // rows of it without a label are zeros; or null
     int m, n, k;
     int row_tiles, col_tiles, splits, split_chunks;
     int b_col0, b_k0;                    // where this piece begins in B
@@ -180,11 +186,16 @@ __device__ __forceinline__ float column_sums(float (&v)[32]) {
 // Warp 0 of each CTA brings operands, warp 1 of the pair's first CTA issues the products, the others take finished accumulators while the next
 // are being filled.  Barriers, all waits bounded: full[s] in the first CTA (its one arrival announces the bytes of both), empty[s] in both
 // (the products that read stage s), acc_full[b] in both, acc_empty[b] in the first CTA (one arrival per epilogue warp of the pair).
+// RAW: eight more warps bring A, fetched through registers and split into parts on its way (a pass that writes the parts and one that reads them move 16
+// bytes an entry in place of 4: loss-cached-rows, 78 us for the former alone); full[s] then counts the warps of both CTAs as well.
 // fp32: six products of parts (all but those below 2^-24); the large one, of the first parts, is handed over every 256 entries of k and
 // summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
-template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END, bool MANY>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY>::THREADS, 1) k_product(const __grid_constant__ ProductParams p) {
-    using S = LossShape<TYPE, MANY>;
+template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END, bool MANY, bool RAW>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY, RAW>::THREADS, 1) k_product(const __grid_constant__ ProductParams p) {
+    using S = LossShape<TYPE, MANY, RAW>;
+    // What a thread of each role holds in registers, out of what the block is launched with: 640 threads of 96.
+    constexpr bool SHARE = MANY && RAW;
+    static_assert(!SHARE || (S::THREADS == 640 && 128 * 48 + 256 * 152 + 256 * 64 == 640 * 96), "registers are shared out to the last");
     using T = typename Elem<TYPE == RIPPLE_TYPE_F16 ? RIPPLE_TYPE_F16 : RIPPLE_TYPE_BF16>::T;      // of the operands
     constexpr int PARTS = S::PARTS, STAGES = S::STAGES, COLS = S::COLS, GROUPS = S::GROUPS, NB = COLS / (32 * GROUPS);      // NB: 32-column blocks of an epilogue warp
     extern __shared__ uint8_t smem_raw[];
@@ -216,7 +227,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
     };
 
     if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1 + 2 * S::LOADERS); mbar_init(&empty[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], p.withhold ? 2 : 1 /* one arrives */); mbar_init(&acc_empty[b], 2 * S::EPI_WARPS); }
         mbar_init(&drained, 1);
         s_fail = 0;
@@ -236,6 +247,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
     auto large_at = [&](int b) { return (uint32_t)(COLS * b); };
     auto small_at = [&](int worked) { return (uint32_t)(2 * COLS + COLS * (worked & 1)); };
 
+    if (warp < S::FIRST) {
+        if constexpr (SHARE) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (warp == 0) {
         // ---------------- operands ----------------
         bool odd = false;
@@ -257,11 +270,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
                 for (int c = t.first; c < t.last; ++c) {
                     ok = mbar_wait_bounded(&empty[s], ph, LS_SPIN_LIMIT);
                     if (!ok) break;
-                    if (rank == 0) mbar_expect(&full[s], 2 * S::STAGE);
+                    if (rank == 0) mbar_expect(&full[s], 2 * PARTS * (RAW ? S::B_PART : S::A_PART + S::B_PART));
                     const uint32_t bar = in_leader(&full[s]), to = to0 + (uint32_t)(s * S::STAGE), to_b = to + PARTS * S::A_PART;
 #pragma unroll
                     for (int q = 0; q < PARTS; ++q) {
-                        if constexpr (A_ACROSS) {
+                        if constexpr (RAW) {
+                        } else if constexpr (A_ACROSS) {
                             for (int h = 0; h < 2; ++h) load_box(to + q * S::A_PART + h * 8192, a, row0 + 64 * h, c * LS_KC, q, bar);
                         } else {
                             load_box(to + q * S::A_PART, a, c * LS_KC, row0, q, bar);
@@ -357,12 +371,96 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
                 __syncwarp();
             }
         }
+    }
+    } else if (RAW && warp >= S::FIRST + S::EPI_WARPS) {
+        if constexpr (SHARE) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        // ---------------- A, from fp32 ----------------
+        // thread: a piece of eight entries of four rows of memory, `apart` rows from one another
+        const int lt = tid - 32 * (S::FIRST + S::EPI_WARPS), across = A_ACROSS ? 16 : 8, apart = 256 / across;
+        const int piece = lt % across, row_in = lt / across;
+        uint32_t to[4];
+#pragma unroll
+        for (int it = 0; it < 4; ++it) to[it] = smem_u32(ring) + (piece >> 3) * 8192 + tc_swz(row_in + apart * it, piece & 7);
+        const uintptr_t base = reinterpret_cast<uintptr_t>(p.raw);
+        const int wide = base % 16 == 0 && p.ld_raw % 4 == 0 ? 4 : base % 8 == 0 && p.ld_raw % 2 == 0 ? 2 : 1;
+        const uint32_t full0 = in_leader(&full[0]);
+        float v[4][8];
+        auto fetch = [&](const Tile& t, int c) {
+            const int row0 = (A_ACROSS ? c * LS_KC : t.row * LS_ROWS + (int)rank * 128) + row_in;
+            const int col = (A_ACROSS ? t.row * LS_ROWS + (int)rank * 128 : c * LS_KC) + piece * 8, left = p.raw_cols - col;
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                const int row = row0 + apart * it;
+                bool there = row < p.raw_rows && left > 0;
+                if (A_ACROSS && there && p.raw_labels) there = (uint32_t)p.raw_labels[row] < (uint32_t)p.classes;
+                const float* const from = p.raw + (int64_t)row * p.ld_raw + col;
+                if (there && left >= 8 && wide == 4) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float4 f = reinterpret_cast<const float4*>(from)[h];
+                        v[it][4 * h] = f.x, v[it][4 * h + 1] = f.y, v[it][4 * h + 2] = f.z, v[it][4 * h + 3] = f.w;
+                    }
+                } else if (there && left >= 8 && wide == 2) {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const float2 f = reinterpret_cast<const float2*>(from)[h];
+                        v[it][2 * h] = f.x, v[it][2 * h + 1] = f.y;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[it][e] = there && e < left ? from[e] : 0.f;
+                }
+            }
+        };
+        bool ok = true;
+        int s = 0;
+        uint32_t ph = 1;
+        int64_t i = pair;
+        if (i < all) {
+            Tile t = tile_at(i);
+            int c = t.first;
+            fetch(t, c);
+            while (true) {
+                ok = mbar_wait_warp(&empty[s], ph, LS_SPIN_LIMIT);
+                if (!ok) break;
+#pragma unroll
+                for (int it = 0; it < 4; ++it) {
+                    // parts that are cut, 8 bits each, nothing left (of an infinite entry they are NaN: see the epilogue)
+                    uint32_t a[4], b[4], d[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float x0 = v[it][2 * e], x1 = v[it][2 * e + 1];
+                        const float m0 = x0 - __uint_as_float(__float_as_uint(x0) & 0xffff0000u), m1 = x1 - __uint_as_float(__float_as_uint(x1) & 0xffff0000u);
+                        const float l0 = m0 - __uint_as_float(__float_as_uint(m0) & 0xffff0000u), l1 = m1 - __uint_as_float(__float_as_uint(m1) & 0xffff0000u);
+                        a[e] = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
+                        b[e] = __byte_perm(__float_as_uint(m0), __float_as_uint(m1), 0x7632);
+                        d[e] = __byte_perm(__float_as_uint(l0), __float_as_uint(l1), 0x7632);
+                    }
+                    const uint32_t at = to[it] + (uint32_t)(s * S::STAGE);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + S::A_PART), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + 2 * S::A_PART), "r"(d[0]), "r"(d[1]), "r"(d[2]), "r"(d[3]) : "memory");
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(full0 + 8 * (uint32_t)s) : "memory");
+                if (++s == STAGES) { s = 0; ph ^= 1; }
+                if (++c >= t.last) {
+                    i += pairs;
+                    if (i >= all) break;
+                    t = tile_at(i), c = t.first;
+                }
+                fetch(t, c);
+            }
+        }
+        if (!ok) s_fail = 1;
     } else {
+        if constexpr (SHARE) asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
         // ---------------- epilogue ----------------
         // thread: a row, and the 32-column blocks part, part + GROUPS, ... of the tile
-        const int q = warp & 3, part = (warp - 2) >> 2;
+        const int q = warp & 3, part = (warp - S::FIRST) >> 2;
         const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16);
-        float* const bias = reinterpret_cast<float*>(ring + STAGES * S::STAGE) + (warp - 2) * 32 * NB;
+        float* const bias = reinterpret_cast<float*>(ring + STAGES * S::STAGE) + (warp - S::FIRST) * 32 * NB;
         float factor = 1.f;                      // GRAD: of g; OUT: of the result
         if (TYPE == RIPPLE_TYPE_F16 && p.control) {
             if (END == END_GRAD) factor = grad_scale(p.control, p.scale);
@@ -679,8 +777,10 @@ __global__ void __launch_bounds__(256) k_look_at_rows(const T* x, int64_t ld_x, 
 }
 
 // Loss and lse from the tiles' sums; a block has 32 rows for every TURNS of its 16 warps, which take turns over the tiles.
+// running: what the pieces of the classes before gave, and this one adds to; null: it is the only one.
 template <int TURNS>
-__global__ void __launch_bounds__(512) k_finish_loss(const float2* sums, int parts, int64_t rows, const float* at_label, const int32_t* labels, int classes, float* loss, float* lse) {
+__global__ void __launch_bounds__(512) k_finish_loss(const float2* sums, int parts, int64_t rows, const float* at_label, const int32_t* labels, int classes, float* loss, float* lse,
+                                                     float2* running, int first, int last) {
     pdl_enter();
     __shared__ float2 mine[16][33];
     const int warp = threadIdx.x >> 5, lane = lane_id(), turn = warp % TURNS;
@@ -704,6 +804,11 @@ __global__ void __launch_bounds__(512) k_finish_loss(const float2* sums, int par
         }
     }
     if (turn > 0 || row >= rows) return;
+    if (!first) join(running[row]);
+    if (!last) {
+        running[row] = make_float2(top, sum);
+        return;
+    }
     const float l = top == -INFINITY && sum == 0.f ? -INFINITY : top + logf(sum);
     lse[row] = l;
     if (loss) loss[row] = has_label(labels, row, classes) && l != -INFINITY ? l - at_label[row] : 0.f;
@@ -751,9 +856,7 @@ static int up_to(int64_t x, int to) { return (int)((x + to - 1) / to * to); }
 static int64_t aligned128(int64_t x) { return (x + 127) / 128 * 128; }
 static int parts_of(int type) { return type == RIPPLE_TYPE_F32 ? 3 : 1; }
 // column groups of a tile whose sums the loss keeps apart
-static int groups_of(int type, int k) {
-    return type == RIPPLE_TYPE_F32 && k > LS_UNIT * LS_KC ? LossShape<RIPPLE_TYPE_F32, true>::GROUPS : LossShape<RIPPLE_TYPE_F32, false>::GROUPS;
-}
+static int groups_of(int type) { return type == RIPPLE_TYPE_F32 ? LossShape<RIPPLE_TYPE_F32, true, true>::GROUPS : LossShape<RIPPLE_TYPE_BF16, false>::GROUPS; }
 static int cols_of(int type) { return type == RIPPLE_TYPE_F32 ? 128 : 256; }
 
 // Whether TMA can read a matrix where it lies.
@@ -993,26 +1096,33 @@ struct Slots {
 };
 
 struct Operand { int64_t at = -1, ld = 0, plane = 0; };      // at: in the workspace; -1: read where it is
-static Operand operand(Slots& s, int type, const void* p, int64_t ld, int64_t rows, int64_t cols, bool copy) {
+// raw: read as it is in fp32, parts and all (x)
+static Operand operand(Slots& s, int type, const void* p, int64_t ld, int64_t rows, int64_t cols, bool copy, bool raw) {
     Operand o;
-    if (!copy && readable(type, p, ld, cols)) return o;
+    if (!copy && ((raw && type == RIPPLE_TYPE_F32) || readable(type, p, ld, cols))) return o;
     o.ld = up_to(cols, 8), o.plane = aligned128(rows * o.ld * 2) / 2;
     o.at = s.take(parts_of(type) * o.plane * 2);
     return o;
 }
 
+// Bytes of the tiles' sums that are in memory at once (one tile of columns of all rows at least).
+constexpr int64_t LS_SUMS = 1ll << 27;
+
 struct LossPlan {
     Operand x, w;
-    int64_t sums, at_label, bytes;
-    int col_tiles;
+    int64_t sums, at_label, running, bytes;
+    int piece, pieces;           // classes
 };
 static LossPlan plan_loss(const ripple_loss_rows_args& a) {
     LossPlan l = {};
     if (few_form(a.type, a.rows, a.k, a.n)) return l;
     Slots s;
-    l.x = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, false), l.w = operand(s, a.type, a.W, a.ld_w, a.k, a.n, false);
-    l.col_tiles = (a.n + cols_of(a.type) - 1) / cols_of(a.type);
-    l.sums = s.take((int64_t)groups_of(a.type, a.k) * l.col_tiles * a.rows * 8), l.at_label = s.take(a.rows * 4);
+    l.x = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, false, true), l.w = operand(s, a.type, a.W, a.ld_w, a.k, a.n, false, false);
+    const int cols = cols_of(a.type), tiles = (a.n + cols - 1) / cols;
+    const int64_t of_tile = groups_of(a.type) * std::max<int64_t>(a.rows, 1) * 8, at_once = std::min<int64_t>(tiles, std::max<int64_t>(1, LS_SUMS / of_tile));
+    l.piece = (int)at_once * cols, l.pieces = (tiles + (int)at_once - 1) / (int)at_once;
+    l.sums = s.take(at_once * of_tile), l.at_label = s.take(a.rows * 4);
+    if (l.pieces > 1) l.running = s.take(a.rows * 8);
     l.bytes = s.at;
     return l;
 }
@@ -1052,8 +1162,8 @@ static GradPlanLoss plan_loss_grad(const ripple_loss_rows_grad_args& a) {
         return l;
     }
     l.control = s.take(sizeof(RowControl));
-    l.x = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, false), l.w = operand(s, a.type, a.W, a.ld_w, a.k, a.n, false);
-    if (a.dW && l.x.at < 0) l.x_clean = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, true);
+    l.x = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, false, true), l.w = operand(s, a.type, a.W, a.ld_w, a.k, a.n, false, false);
+    if (a.dW && l.x.at < 0 && a.type != RIPPLE_TYPE_F32) l.x_clean = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, true, false);
     const int cols = cols_of(a.type), parts = parts_of(a.type), all = up_to(a.n, 64);
     l.piece = (int)std::min<int64_t>(all, std::max<int64_t>(cols, LS_PIECE / parts / std::max<int64_t>(a.rows, 1) / cols * cols));
     l.pieces = (a.n + l.piece - 1) / l.piece;
@@ -1106,30 +1216,35 @@ static bool tensor_map(CUtensorMap* map, int type, const Matrix& x, int box) {
 }
 
 // a [.., k] (A_ACROSS: [k, ..]), b [.., k] (B_ACROSS: [k, ..])
-template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END, bool MANY>
+template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END, bool MANY, bool RAW>
 static cudaError_t launch_product(ProductParams p, const Matrix& a, const Matrix* a_clean, const Matrix& b, void* stream) {
-    using S = LossShape<TYPE, MANY>;
-    auto* const kernel = k_product<TYPE, A_ACROSS, B_ACROSS, END, MANY>;
+    using S = LossShape<TYPE, MANY, RAW>;
+    auto* const kernel = k_product<TYPE, A_ACROSS, B_ACROSS, END, MANY, RAW>;
     static bool ready[64];
     cudaError_t e = allow_shared(kernel, (int)S::BYTES, ready);
     if (e != cudaSuccess) return e;
-    if (!tensor_map(&p.a, TYPE, a, A_ACROSS ? 64 : 128) || !tensor_map(&p.a_clean, TYPE, a_clean ? *a_clean : a, A_ACROSS ? 64 : 128) ||
-        !tensor_map(&p.b, TYPE, b, B_ACROSS ? 64 : S::COLS / 2))
-        return cudaErrorInvalidValue;
+    if (!tensor_map(&p.b, TYPE, b, B_ACROSS ? 64 : S::COLS / 2)) return cudaErrorInvalidValue;
+    if constexpr (RAW) {
+        p.raw = static_cast<const float*>(a.p), p.ld_raw = a.ld, p.raw_rows = (int)a.rows, p.raw_cols = (int)a.cols;
+    } else {
+        if (!tensor_map(&p.a, TYPE, a, A_ACROSS ? 64 : 128) || !tensor_map(&p.a_clean, TYPE, a_clean ? *a_clean : a, A_ACROSS ? 64 : 128)) return cudaErrorInvalidValue;
+    }
     p.row_tiles = (p.m + LS_ROWS - 1) / LS_ROWS, p.col_tiles = (p.n + S::COLS - 1) / S::COLS;
     const char* const withhold = std::getenv("RIPPLE_DEBUG_TC_WITHHOLD");
     p.withhold = withhold && withhold[0] == '1';
     const int64_t all = (int64_t)p.row_tiles * p.col_tiles * p.splits;
     return launch(kernel, dim3((unsigned)(2 * std::min<int64_t>(all, std::max(1, sm_count() / 2)))), S::THREADS, S::BYTES, stream, p);
 }
-template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END>
+// X: the product reads x as A, which in fp32 is taken as it is
+template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END, bool X>
 static cudaError_t launch_product(ProductParams p, const Matrix& a, const Matrix* a_clean, const Matrix& b, int splits, void* stream) {
     const int chunks = (p.k + LS_KC - 1) / LS_KC;
+    constexpr bool RAW = X && TYPE == RIPPLE_TYPE_F32;
     p.split_chunks = (chunks + splits - 1) / splits, p.splits = (chunks + p.split_chunks - 1) / p.split_chunks;      // (none empty)
     if constexpr (TYPE == RIPPLE_TYPE_F32) {
-        if (p.split_chunks > LS_UNIT) return launch_product<TYPE, A_ACROSS, B_ACROSS, END, true>(p, a, a_clean, b, stream);
+        if (p.split_chunks > LS_UNIT) return launch_product<TYPE, A_ACROSS, B_ACROSS, END, true, RAW>(p, a, a_clean, b, stream);
     }
-    return launch_product<TYPE, A_ACROSS, B_ACROSS, END, false>(p, a, a_clean, b, stream);
+    return launch_product<TYPE, A_ACROSS, B_ACROSS, END, false, RAW>(p, a, a_clean, b, stream);
 }
 
 template <int TYPE>
@@ -1159,17 +1274,23 @@ static cudaError_t run_loss(const ripple_loss_rows_args& a) {
     if (l.x.at >= 0) e = launch_operand<TYPE>(a.x, a.ld_x, a.rows, a.k, l.x, work, nullptr, 0, nullptr, a.cuda_stream);
     if (e == cudaSuccess && l.w.at >= 0) e = launch_operand<TYPE>(a.W, a.ld_w, a.k, a.n, l.w, work, nullptr, 0, nullptr, a.cuda_stream);
     if (e != cudaSuccess) return e;
+    const Matrix x = matrix_of(l.x, a.type, a.x, a.ld_x, a.rows, a.k, work), w = matrix_of(l.w, a.type, a.W, a.ld_w, a.k, a.n, work);
     ProductParams p = {};
-    p.m = (int)a.rows, p.n = a.n, p.k = a.k;
-    p.bias = a.bias, p.labels = a.labels, p.classes = a.n;
+    p.m = (int)a.rows, p.k = a.k, p.labels = a.labels, p.classes = a.n;
     p.sums = reinterpret_cast<float2*>(work + l.sums), p.at_label = reinterpret_cast<float*>(work + l.at_label);
-    e = launch_product<TYPE, false, true, END_LSE>(p, matrix_of(l.x, a.type, a.x, a.ld_x, a.rows, a.k, work), nullptr, matrix_of(l.w, a.type, a.W, a.ld_w, a.k, a.n, work), 1, a.cuda_stream);
-    if (e != cudaSuccess) return e;
-    const int parts = groups_of(a.type, a.k) * l.col_tiles;
-    auto finish = [&](auto* kernel, int rows) {
-        return launch(kernel, dim3((unsigned)((a.rows + rows - 1) / rows)), 512, 0, a.cuda_stream, (const float2*)p.sums, parts, a.rows, (const float*)p.at_label, a.labels, a.n, a.loss, a.lse);
-    };
-    return parts <= 8 ? finish(k_finish_loss<1>, 512) : finish(k_finish_loss<16>, 32);
+    for (int piece = 0; piece < l.pieces && e == cudaSuccess; ++piece) {
+        const int c0 = piece * l.piece;
+        p.n = std::min(l.piece, a.n - c0), p.b_col0 = p.class0 = c0, p.bias = a.bias ? a.bias + c0 : nullptr;
+        e = launch_product<TYPE, false, true, END_LSE, true>(p, x, nullptr, w, 1, a.cuda_stream);
+        if (e != cudaSuccess) break;
+        const int parts = groups_of(a.type) * ((p.n + cols_of(a.type) - 1) / cols_of(a.type));
+        auto finish = [&](auto* kernel, int rows) {
+            return launch(kernel, dim3((unsigned)((a.rows + rows - 1) / rows)), 512, 0, a.cuda_stream, (const float2*)p.sums, parts, a.rows, (const float*)p.at_label, a.labels, a.n, a.loss,
+                          a.lse, l.pieces > 1 ? reinterpret_cast<float2*>(work + l.running) : nullptr, piece == 0 ? 1 : 0, piece == l.pieces - 1 ? 1 : 0);
+        };
+        e = parts <= 8 ? finish(k_finish_loss<1>, 512) : finish(k_finish_loss<16>, 32);
+    }
+    return e;
 }
 
 template <typename T>
@@ -1215,7 +1336,7 @@ static cudaError_t run_loss_grad(const ripple_loss_rows_grad_args& a) {
         p.control = TYPE == RIPPLE_TYPE_F16 ? control : nullptr;
         // (rows without labels are zeros in g whatever their logits: x as it is)
         const Matrix* const same = TYPE == RIPPLE_TYPE_F16 ? &x : nullptr;
-        e = launch_product<TYPE, false, true, END_GRAD>(p, x, same, w, 1, stream);
+        e = launch_product<TYPE, false, true, END_GRAD, true>(p, x, same, w, 1, stream);
         if (e != cudaSuccess) return e;
         if (a.dbias && (e = launch(k_join_columns, dim3((unsigned)(classes + 31) / 32), 1024, 0, stream, (const float*)p.g_sums, (a.rows + 31) / 32, l.ld_g, classes, a.dbias + c0)) != cudaSuccess) return e;
         const Matrix g{work + l.g, a.rows, classes, l.ld_g, l.g_plane, parts_of(TYPE)};
@@ -1227,16 +1348,16 @@ static cudaError_t run_loss_grad(const ripple_loss_rows_grad_args& a) {
             if (l.dx < 0) d.out = a.dx, d.ld_out = a.ld_dx, d.out_f32 = TYPE == RIPPLE_TYPE_F32;
             else d.out = work + l.dx, d.ld_out = l.ld_dx, d.split_stride = a.rows * l.ld_dx, d.out_f32 = 1, d.add_to_out = c0 > 0;
             // (the last piece may be too short for all parts: the last of them keep what they have)
-            e = launch_product<TYPE, false, false, END_OUT>(d, g, &g, w, l.dx_splits, stream);
+            e = launch_product<TYPE, false, false, END_OUT, false>(d, g, &g, w, l.dx_splits, stream);
             if (e != cudaSuccess) return e;
         }
         if (a.dW) {
             ProductParams d = o;
-            d.m = a.k, d.n = classes, d.k = (int)a.rows;
+            d.m = a.k, d.n = classes, d.k = (int)a.rows, d.raw_labels = a.labels;
             d.control = look_in_x || TYPE == RIPPLE_TYPE_F16 ? control : nullptr;
             if (l.dw < 0) d.out = static_cast<T*>(a.dW) + c0, d.ld_out = a.ld_dw, d.out_f32 = TYPE == RIPPLE_TYPE_F32;
             else d.out = work + l.dw, d.ld_out = l.ld_dw, d.split_stride = a.k * l.ld_dw, d.out_f32 = 1;
-            e = launch_product<TYPE, true, true, END_OUT>(d, x, &x_clean, g, l.dw_splits, stream);
+            e = launch_product<TYPE, true, true, END_OUT, true>(d, x, &x_clean, g, l.dw_splits, stream);
             if (e == cudaSuccess && l.dw >= 0) e = join_parts<T>(static_cast<const float*>(d.out), l.dw_splits, d.split_stride, d.ld_out, static_cast<T*>(a.dW) + c0, a.ld_dw, a.k, classes, stream);
             if (e != cudaSuccess) return e;
         }

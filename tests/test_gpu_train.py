@@ -806,3 +806,10 @@ def test_a_batch_waits_for_a_step_on_another_stream(env):
     torch.cuda.synchronize()
     assert torch.equal(got[0], want[0]) and all(torch.equal(got[1][k], want[1][k]) for k in want[1])
     rp.close()
+
+
+@pytest.mark.parametrize("dtype,N", [("bf16", 1100), ("fp32", 600)])
+def test_losses_whose_tile_sums_come_in_pieces(dtype, N):
+    """A million rows: four tiles of columns leave 128 MB of sums, the fifth comes in a piece of its own."""
+    g = gen(18)
+    check_loss(**problem(g, 1_000_000, 16, N, DTYPES[dtype]), grad=False)
