@@ -187,7 +187,7 @@ __device__ __forceinline__ float column_sums(float (&v)[32]) {
 // are being filled.  Barriers, all waits bounded: full[s] in the first CTA (its one arrival announces the bytes of both), empty[s] in both
 // (the products that read stage s), acc_full[b] in both, acc_empty[b] in the first CTA (one arrival per epilogue warp of the pair).
 // RAW: eight more warps bring A, fetched through registers and split into parts on its way (a pass that writes the parts and one that reads them move 16
-// bytes an entry in place of 4: loss-cached-rows, 78 us for the former alone); full[s] then counts the warps of both CTAs as well.
+// bytes an entry in place of 4: loss-cached-rows, 78 us for the former alone); a warp in each CTA passes on to full[s] that a stage is made.
 // fp32: six products of parts (all but those below 2^-24); the large one, of the first parts, is handed over every 256 entries of k and
 // summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
 template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END, bool MANY, bool RAW>
@@ -199,7 +199,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
     using T = typename Elem<TYPE == RIPPLE_TYPE_F16 ? RIPPLE_TYPE_F16 : RIPPLE_TYPE_BF16>::T;      // of the operands
     constexpr int PARTS = S::PARTS, STAGES = S::STAGES, COLS = S::COLS, GROUPS = S::GROUPS, NB = COLS / (32 * GROUPS);      // NB: 32-column blocks of an epilogue warp
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
+    __shared__ uint64_t full[STAGES], empty[STAGES], made[RAW ? STAGES : 1], acc_full[2], acc_empty[2], drained;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int s_fail;
 
@@ -227,7 +227,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
     };
 
     if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1 + 2 * S::LOADERS); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], RAW ? 3 : 1); mbar_init(&empty[s], 1); if (RAW) mbar_init(&made[s], S::LOADERS); }
         for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], p.withhold ? 2 : 1 /* one arrives */); mbar_init(&acc_empty[b], 2 * S::EPI_WARPS); }
         mbar_init(&drained, 1);
         s_fail = 0;
@@ -371,6 +371,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
                 __syncwarp();
             }
         }
+    } else if (RAW && warp == 2) {
+        // ---------------- passes on that a stage of A is made ----------------
+        // (what makes it visible to the other CTA waits for all that a thread has on its way: the loaders' next rows, if they did it themselves)
+        const uint32_t full0 = in_leader(&full[0]);
+        bool ok = true;
+        int s = 0;
+        uint32_t ph = 0;
+        for (int64_t i = pair; i < all && ok; i += pairs) {
+            const Tile t = tile_at(i);
+            for (int c = t.first; c < t.last; ++c) {
+                ok = mbar_wait_warp(&made[s], ph, LS_SPIN_LIMIT);
+                if (!ok) break;
+                if (lane == 0) {
+                    asm volatile("fence.proxy.async;" ::: "memory");
+                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(full0 + 8 * (uint32_t)s) : "memory");
+                }
+                __syncwarp();
+                if (++s == STAGES) { s = 0; ph ^= 1; }
+            }
+        }
+        if (!ok) s_fail = 1;
     }
     } else if (RAW && warp >= S::FIRST + S::EPI_WARPS) {
         if constexpr (SHARE) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
@@ -378,23 +399,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
         // thread: a piece of eight entries of four rows of memory, `apart` rows from one another
         const int lt = tid - 32 * (S::FIRST + S::EPI_WARPS), across = A_ACROSS ? 16 : 8, apart = 256 / across;
         const int piece = lt % across, row_in = lt / across;
-        uint32_t to[4];
-#pragma unroll
-        for (int it = 0; it < 4; ++it) to[it] = smem_u32(ring) + (piece >> 3) * 8192 + tc_swz(row_in + apart * it, piece & 7);
+        const uint32_t to = smem_u32(ring) + (piece >> 3) * 8192 + tc_swz(row_in, piece & 7);       // (`apart` rows on: the same place, so many 1024 bytes on)
         const uintptr_t base = reinterpret_cast<uintptr_t>(p.raw);
-        const int wide = base % 16 == 0 && p.ld_raw % 4 == 0 ? 4 : base % 8 == 0 && p.ld_raw % 2 == 0 ? 2 : 1;
-        const uint32_t full0 = in_leader(&full[0]);
-        float v[4][8];
-        auto fetch = [&](const Tile& t, int c) {
+        const int wide = base % 32 == 0 && p.ld_raw % 8 == 0 ? 8 : base % 16 == 0 && p.ld_raw % 4 == 0 ? 4 : base % 8 == 0 && p.ld_raw % 2 == 0 ? 2 : 1;
+        int of_row[4];               // labels of the rows fetched (looked at when they are there: the rows do not wait for them)
+        auto fetch = [&](float (&v)[4][8], const Tile& t, int c) {
             const int row0 = (A_ACROSS ? c * LS_KC : t.row * LS_ROWS + (int)rank * 128) + row_in;
             const int col = (A_ACROSS ? t.row * LS_ROWS + (int)rank * 128 : c * LS_KC) + piece * 8, left = p.raw_cols - col;
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
                 const int row = row0 + apart * it;
-                bool there = row < p.raw_rows && left > 0;
-                if (A_ACROSS && there && p.raw_labels) there = (uint32_t)p.raw_labels[row] < (uint32_t)p.classes;
+                const bool there = row < p.raw_rows && left > 0;
                 const float* const from = p.raw + (int64_t)row * p.ld_raw + col;
-                if (there && left >= 8 && wide == 4) {
+                if (A_ACROSS) of_row[it] = there && p.raw_labels ? p.raw_labels[row] : 0;
+                // rows further on, on their way to L2: AHEAD chunks, one access in 128 bytes
+                constexpr int AHEAD = 2;
+                if (A_ACROSS && (piece & 3) == 0 && left > 0 && row + AHEAD * LS_KC < p.raw_rows) asm volatile("prefetch.global.L2 [%0];" ::"l"(from + AHEAD * LS_KC * p.ld_raw));
+                if (!A_ACROSS && (piece & 3) == 0 && row < p.raw_rows && left > AHEAD * LS_KC) asm volatile("prefetch.global.L2 [%0];" ::"l"(from + AHEAD * LS_KC));
+                if (there && left >= 8 && wide == 8) {
+                    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                                 : "=f"(v[it][0]), "=f"(v[it][1]), "=f"(v[it][2]), "=f"(v[it][3]), "=f"(v[it][4]), "=f"(v[it][5]), "=f"(v[it][6]), "=f"(v[it][7]) : "l"(from));
+                } else if (there && left >= 8 && wide == 4) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const float4 f = reinterpret_cast<const float4*>(from)[h];
@@ -415,42 +440,58 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
         bool ok = true;
         int s = 0;
         uint32_t ph = 1;
+        auto hand = [&](float (&v)[4][8]) {
+            ok = mbar_wait_warp(&empty[s], ph, LS_SPIN_LIMIT);
+            if (!ok) return;
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                if (A_ACROSS && (uint32_t)of_row[it] >= (uint32_t)p.classes) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[it][e] = 0.f;
+                }
+                // parts that are cut, 8 bits each, nothing left (of an infinite entry they are NaN: see the epilogue)
+                uint32_t a[4], b[4], d[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x0 = v[it][2 * e], x1 = v[it][2 * e + 1];
+                    const float m0 = x0 - __uint_as_float(__float_as_uint(x0) & 0xffff0000u), m1 = x1 - __uint_as_float(__float_as_uint(x1) & 0xffff0000u);
+                    const float l0 = m0 - __uint_as_float(__float_as_uint(m0) & 0xffff0000u), l1 = m1 - __uint_as_float(__float_as_uint(m1) & 0xffff0000u);
+                    a[e] = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
+                    b[e] = __byte_perm(__float_as_uint(m0), __float_as_uint(m1), 0x7632);
+                    d[e] = __byte_perm(__float_as_uint(l0), __float_as_uint(l1), 0x7632);
+                }
+                const uint32_t at = to + (uint32_t)(s * S::STAGE + it * (apart / 8) * 1024);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]) : "memory");
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + S::A_PART), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + 2 * S::A_PART), "r"(d[0]), "r"(d[1]), "r"(d[2]), "r"(d[3]) : "memory");
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&made[s]);
+            if (++s == STAGES) { s = 0; ph ^= 1; }
+        };
+        // (the next rows are asked for as soon as these are in shared memory.  Two chunks on their way do not fit the registers: with spills 93 us for
+        // the loss of 200 000 rows of 256, one chunk RAW_TIME)
+        float v[4][8];
         int64_t i = pair;
-        if (i < all) {
-            Tile t = tile_at(i);
-            int c = t.first;
-            fetch(t, c);
-            while (true) {
-                ok = mbar_wait_warp(&empty[s], ph, LS_SPIN_LIMIT);
-                if (!ok) break;
-#pragma unroll
-                for (int it = 0; it < 4; ++it) {
-                    // parts that are cut, 8 bits each, nothing left (of an infinite entry they are NaN: see the epilogue)
-                    uint32_t a[4], b[4], d[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float x0 = v[it][2 * e], x1 = v[it][2 * e + 1];
-                        const float m0 = x0 - __uint_as_float(__float_as_uint(x0) & 0xffff0000u), m1 = x1 - __uint_as_float(__float_as_uint(x1) & 0xffff0000u);
-                        const float l0 = m0 - __uint_as_float(__float_as_uint(m0) & 0xffff0000u), l1 = m1 - __uint_as_float(__float_as_uint(m1) & 0xffff0000u);
-                        a[e] = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
-                        b[e] = __byte_perm(__float_as_uint(m0), __float_as_uint(m1), 0x7632);
-                        d[e] = __byte_perm(__float_as_uint(l0), __float_as_uint(l1), 0x7632);
-                    }
-                    const uint32_t at = to[it] + (uint32_t)(s * S::STAGE);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + S::A_PART), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + 2 * S::A_PART), "r"(d[0]), "r"(d[1]), "r"(d[2]), "r"(d[3]) : "memory");
-                }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(full0 + 8 * (uint32_t)s) : "memory");
-                if (++s == STAGES) { s = 0; ph ^= 1; }
-                if (++c >= t.last) {
-                    i += pairs;
-                    if (i >= all) break;
-                    t = tile_at(i), c = t.first;
-                }
-                fetch(t, c);
+        Tile t = {};
+        int c = 0;
+        if (i < all) t = tile_at(i), c = t.first, fetch(v, t, c);
+        while (i < all) {
+            hand(v);
+            if (!ok) break;
+            if (++c >= t.last) {
+                i += pairs;
+                if (i >= all) break;
+                t = tile_at(i), c = t.first;
+            }
+            fetch(v, t, c);
+            if (!A_ACROSS && c == t.first && i + pairs < all) {
+                // and the first chunks of the tile after this one
+                const Tile n = tile_at(i + pairs);
+                const int row = n.row * LS_ROWS + (int)rank * 128 + (lt & 127), col = n.first * LS_KC + (lt >> 7) * 64;
+                const float* const from = p.raw + (int64_t)row * p.ld_raw + col;
+                if (row < p.raw_rows && col < p.raw_cols) asm volatile("prefetch.global.L2 [%0];" ::"l"(from));
+                if (row < p.raw_rows && col + 32 < p.raw_cols) asm volatile("prefetch.global.L2 [%0];" ::"l"(from + 32));
             }
         }
         if (!ok) s_fail = 1;
