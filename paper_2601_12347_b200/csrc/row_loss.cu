@@ -874,19 +874,45 @@ __global__ void __launch_bounds__(256) k_join_parts(const float* parts, int spli
     }
 }
 
-// dbias from the sums over groups of 32 rows; a block has 32 columns, the warps take turns over the groups.
+// The same for few columns and many parts: a block has 32 columns of a row, its eight warps take turns over the parts.
+template <typename T>
+__global__ void __launch_bounds__(256) k_join_many_parts(const float* parts, int splits, int64_t split_stride, int64_t ld, T* out, int64_t ld_out, int64_t rows, int cols) {
+    pdl_enter();
+    __shared__ float mine[8][32];
+    const int warp = threadIdx.x >> 5, lane = lane_id(), c = blockIdx.x * 32 + lane;
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+        float sum = 0.f;
+        if (c < cols) {
+#pragma unroll 10
+            for (int s = warp; s < splits; s += 8) sum += parts[s * split_stride + row * ld + c];
+        }
+        mine[warp][lane] = sum;
+        __syncthreads();
+        if (warp == 0 && c < cols) {
+            sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) sum += mine[w][lane];
+            out[row * ld_out + c] = from_f32<T>(sum);
+        }
+        __syncthreads();
+    }
+}
+
+// dbias from the sums over groups of 32 rows; a block has 8 columns, its warps and the four parts of a warp take turns over the groups.
 __global__ void __launch_bounds__(1024) k_join_columns(const float* sums, int64_t groups, int64_t ld, int cols, float* out) {
     pdl_enter();
-    __shared__ float mine[32][33];
-    const int warp = threadIdx.x >> 5, lane = lane_id(), c = blockIdx.x * 32 + lane;
+    __shared__ float mine[32][8];
+    const int warp = threadIdx.x >> 5, lane = lane_id(), c = blockIdx.x * 8 + (lane & 7);
     float sum = 0.f;
     if (c < cols) {
 #pragma unroll 16
-        for (int64_t i = warp; i < groups; i += 32) sum += sums[i * ld + c];
+        for (int64_t i = warp * 4 + (lane >> 3); i < groups; i += 128) sum += sums[i * ld + c];
     }
-    mine[warp][lane] = sum;
+    sum += __shfl_xor_sync(FULL, sum, 8);
+    sum += __shfl_xor_sync(FULL, sum, 16);
+    if (lane < 8) mine[warp][lane] = sum;
     __syncthreads();
-    if (warp > 0 || c >= cols) return;
+    if (warp > 0 || lane >= 8 || c >= cols) return;
     sum = 0.f;
     for (int w = 0; w < 32; ++w) sum += mine[w][lane];
     out[c] = sum;
@@ -946,17 +972,25 @@ __global__ void __launch_bounds__(FL_THREADS, 1) k_loss_few(const __grid_constan
     float* const sums = gs + FL_ROWS * 32 * cols;         // part of k x class block x FL_ROWS x 32
     float* const ws = sums + FL_WARPS * FL_ROWS * 32;     // k x pitch
     const T* const x = static_cast<const T*>(p.x);
+    auto copy = [](float* to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(to)), "l"(from) : "memory"); };
     {
         const T* const W = static_cast<const T*>(p.W);
-        constexpr int U = 8;             // rows that are on their way
+        constexpr int U = 16;            // rows that are on their way (fp32: all)
         const int c = warp % cols * 32 + lane;
         if (c < p.n) {
             for (int k0 = warp / cols; k0 < p.k && warp / cols < shares; k0 += shares * U) {
                 T v[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) if (k0 + u * shares < p.k) v[u] = W[(int64_t)(k0 + u * shares) * p.ld_w + c];
+                for (int u = 0; u < U; ++u) {
+                    const int k = k0 + u * shares;
+                    if (k >= p.k) continue;
+                    if constexpr (sizeof(T) == 4) copy(ws + k * pitch + c, W + (int64_t)k * p.ld_w + c);
+                    else v[u] = W[(int64_t)k * p.ld_w + c];
+                }
+                if constexpr (sizeof(T) == 2) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) if (k0 + u * shares < p.k) ws[(k0 + u * shares) * pitch + c] = to_f32(v[u]);
+                    for (int u = 0; u < U; ++u) if (k0 + u * shares < p.k) ws[(k0 + u * shares) * pitch + c] = to_f32(v[u]);
+                }
             }
         }
     }
@@ -964,10 +998,20 @@ __global__ void __launch_bounds__(FL_THREADS, 1) k_loss_few(const __grid_constan
         for (int k = threadIdx.x; k < p.k; k += FL_THREADS) {
             T v[FL_ROWS];
 #pragma unroll
-            for (int r = 0; r < FL_ROWS; ++r) v[r] = row0 + r < p.rows ? x[(int64_t)(row0 + r) * p.ld_x + k] : from_f32<T>(0.f);
+            for (int r = 0; r < FL_ROWS; ++r) {
+                if constexpr (sizeof(T) == 4) {
+                    if (row0 + r < p.rows) copy(xs + k * FL_ROWS + r, x + (int64_t)(row0 + r) * p.ld_x + k);
+                    else xs[k * FL_ROWS + r] = 0.f;
+                } else {
+                    v[r] = row0 + r < p.rows ? x[(int64_t)(row0 + r) * p.ld_x + k] : from_f32<T>(0.f);
+                }
+            }
+            if constexpr (sizeof(T) == 2) {
 #pragma unroll
-            for (int r = 0; r < FL_ROWS; ++r) xs[k * FL_ROWS + r] = to_f32(v[r]);
+                for (int r = 0; r < FL_ROWS; ++r) xs[k * FL_ROWS + r] = to_f32(v[r]);
+            }
         }
+        if constexpr (sizeof(T) == 4) asm volatile("cp.async.wait_all;" ::: "memory");
         __syncthreads();
         const int block = warp % cols, share = warp / cols;
         if (share < shares) {
@@ -1336,6 +1380,8 @@ static cudaError_t run_loss(const ripple_loss_rows_args& a) {
 
 template <typename T>
 static cudaError_t join_parts(const float* parts, int splits, int64_t stride, int64_t ld, void* out, int64_t ld_out, int64_t rows, int cols, void* stream) {
+    if (splits >= 16 && cols <= 1024)
+        return launch(k_join_many_parts<T>, dim3((unsigned)((cols + 31) / 32), (unsigned)std::min<int64_t>(rows, 16384)), 256, 0, stream, parts, splits, stride, ld, static_cast<T*>(out), ld_out, rows, cols);
     return launch(k_join_parts<T>, dim3((unsigned)((cols + 1023) / 1024), (unsigned)std::min<int64_t>(rows, 16384)), 256, 0, stream, parts, splits, stride, ld, static_cast<T*>(out), ld_out, rows, cols);
 }
 
@@ -1379,7 +1425,7 @@ static cudaError_t run_loss_grad(const ripple_loss_rows_grad_args& a) {
         const Matrix* const same = TYPE == RIPPLE_TYPE_F16 ? &x : nullptr;
         e = launch_product<TYPE, false, true, END_GRAD, true>(p, x, same, w, 1, stream);
         if (e != cudaSuccess) return e;
-        if (a.dbias && (e = launch(k_join_columns, dim3((unsigned)(classes + 31) / 32), 1024, 0, stream, (const float*)p.g_sums, (a.rows + 31) / 32, l.ld_g, classes, a.dbias + c0)) != cudaSuccess) return e;
+        if (a.dbias && (e = launch(k_join_columns, dim3((unsigned)(classes + 7) / 8), 1024, 0, stream, (const float*)p.g_sums, (a.rows + 31) / 32, l.ld_g, classes, a.dbias + c0)) != cudaSuccess) return e;
         const Matrix g{work + l.g, a.rows, classes, l.ld_g, l.g_plane, parts_of(TYPE)};
         ProductParams o = {};
         o.unscale = TYPE == RIPPLE_TYPE_F16, o.scale = a.scale, o.classes = a.n;
