@@ -389,7 +389,7 @@ template <typename T, int V> struct Raw {
     }
 };
 
-// Runs of the same key among entries in order.  add(k, piece): an entry; end: the last run.  A run that lies within the entries is `complete`, the
+// Runs of the same key among entries in order.  begin(k): the next run; add(piece): an entry of it; finish: the last one.  A run that lies within the entries is `complete`, the
 // one that comes from before them and the one that goes on behind them are partial sums.
 template <typename TO, int V, int NP>
 struct Runs {
@@ -437,18 +437,16 @@ struct Runs {
             clear();
         }
     }
-    template <typename F> __device__ __forceinline__ void add(uint32_t key, F piece) {
-        if (bare(key) != run) {
-            finish(false);
-            run = bare(key), from_before = false;
-        }
-        if (key < p.table_rows) {
-            each([&](int j, int) {
-                const auto& v = piece(j);
+    __device__ __forceinline__ void begin(uint32_t key) {
+        finish(false);
+        run = bare(key), from_before = false;
+    }
+    template <typename F> __device__ __forceinline__ void add(F piece) {
+        each([&](int j, int) {
+            const auto& v = piece(j);
 #pragma unroll
-                for (int e = 0; e < V; ++e) sum[j][e] += v.at(e);
-            });
-        }
+            for (int e = 0; e < V; ++e) sum[j][e] += v.at(e);
+        });
     }
 };
 
@@ -471,22 +469,25 @@ __global__ void __launch_bounds__(32 * RS_WARPS, sizeof(T) * V * NP > 16 ? 2 : 4
         const uint32_t key = p.keys[i];
         const int place = p.places ? p.places[i] : i;
         Runs<TO, V, NP> runs(p, c0, __shfl_sync(FULL, key, 0), before, &part[2 * warp][lane * V], &part[2 * warp + 1][lane * V]);
-        // (an entry that holds nothing -- padding, EMPTY, none at all -- is not read)
+        // where runs begin, and what is read (not: padding, EMPTY, nothing at all): a bit for every entry, so that an entry costs no comparison
+        const uint32_t key_before = __shfl_up_sync(FULL, bare(key), 1);
+        const uint32_t begins = __ballot_sync(FULL, lane > 0 && lane < count && bare(key) != key_before);
+        const uint32_t reads = __ballot_sync(FULL, lane < count && key < p.table_rows);
         constexpr int AHEAD = WIDE ? 8 : 4;       // rows of a warp that are on their way (32 warps of an SM: up to 64 KB)
         using Batch = Raw<T, V>[AHEAD][NP];
+        const T* const src = static_cast<const T*>(p.src) + c0;
         auto request = [&](Batch& v, int e0) {
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                const uint32_t k = __shfl_sync(FULL, key, e0 + u);
-                const T* const from = static_cast<const T*>(p.src) + (int64_t)__shfl_sync(FULL, place, e0 + u) * p.ld_src + c0;
-                if (e0 + u < count && k < p.table_rows) runs.each([&](int j, int c) { v[u][j].read(from + c); });
+                const T* const from = src + (int64_t)__shfl_sync(FULL, place, e0 + u) * p.ld_src;
+                if (reads >> (e0 + u) & 1) runs.each([&](int j, int c) { v[u][j].read(from + c); });
             }
         };
         auto take = [&](const Batch& v, int e0) {
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                const uint32_t k = __shfl_sync(FULL, key, e0 + u);
-                if (e0 + u < count) runs.add(k, [&](int j) -> const Raw<T, V>& { return v[u][j]; });
+                if (begins >> (e0 + u) & 1) runs.begin(__shfl_sync(FULL, key, e0 + u));
+                if (reads >> (e0 + u) & 1) runs.add([&](int j) -> const Raw<T, V>& { return v[u][j]; });
             }
         };
         Batch v;
@@ -503,7 +504,17 @@ __global__ void __launch_bounds__(32 * RS_WARPS, sizeof(T) * V * NP > 16 ? 2 : 4
     if (any) {
         const int64_t at = 2ll * block * p.ld_next + c0;
         Runs<TO, V, NP> runs(p, c0, part_key[0], key_at(first - 1), p.next + at, p.next + at + p.ld_next);
-        for (int e = 0; e < 2 * RS_WARPS; ++e) runs.add(part_key[e], [&](int j) { Raw<float, V> r; r.read(&part[e][lane * V + j * 32 * V]); return r; });
+        for (int e = 0; e < 2 * RS_WARPS; ++e) {
+            const uint32_t k = part_key[e];
+            if (bare(k) != runs.run) runs.begin(k);
+            if (k < p.table_rows) {
+                runs.add([&](int j) {
+                    Raw<float, V> r;
+                    r.read(&part[e][lane * V + j * 32 * V]);
+                    return r;
+                });
+            }
+        }
         runs.finish(runs.run == key_at(last));
         head_key = runs.head_key, tail_key = runs.tail_key;
     }

@@ -48,7 +48,7 @@ template <int TYPE, bool MANY, bool RAW = false> struct LossShape {
     // of a piece: 281 us with eight, 215 with sixteen); eight where the sums carried need the registers.
     static constexpr int EPI_WARPS = MANY || RAW ? 8 : 16, GROUPS = EPI_WARPS / 4;
     static constexpr int FIRST = RAW ? 4 : 2;            // of them; RAW: whole warpgroups, which share out registers
-    static constexpr int LOADERS = RAW ? 8 : 0;
+    static constexpr int LOADERS = RAW ? 16 : 0;
     static constexpr int THREADS = 32 * (FIRST + EPI_WARPS + LOADERS);
     static constexpr int BIAS = EPI_WARPS * (COLS / GROUPS) * 4;
     static constexpr size_t BYTES = (size_t)STAGES * STAGE + BIAS + 1024;
@@ -193,9 +193,9 @@ __device__ __forceinline__ float column_sums(float (&v)[32]) {
 template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END, bool MANY, bool RAW>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY, RAW>::THREADS, 1) k_product(const __grid_constant__ ProductParams p) {
     using S = LossShape<TYPE, MANY, RAW>;
-    // What a thread of each role holds in registers, out of what the block is launched with: 640 threads of 96.
-    constexpr bool SHARE = MANY && RAW;
-    static_assert(!SHARE || (S::THREADS == 640 && 128 * 48 + 256 * 152 + 256 * 64 == 640 * 96), "registers are shared out to the last");
+    // What a thread of each role holds in registers, out of what the block is launched with: 896 threads of 72.
+    constexpr bool SHARE = RAW;
+    static_assert(!SHARE || (S::THREADS == 896 && 128 * 48 + 256 * 144 + 512 * 40 <= 896 * 72), "no more registers are shared out than there are");
     using T = typename Elem<TYPE == RIPPLE_TYPE_F16 ? RIPPLE_TYPE_F16 : RIPPLE_TYPE_BF16>::T;      // of the operands
     constexpr int PARTS = S::PARTS, STAGES = S::STAGES, COLS = S::COLS, GROUPS = S::GROUPS, NB = COLS / (32 * GROUPS);      // NB: 32-column blocks of an epilogue warp
     extern __shared__ uint8_t smem_raw[];
@@ -394,20 +394,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
         if (!ok) s_fail = 1;
     }
     } else if (RAW && warp >= S::FIRST + S::EPI_WARPS) {
-        if constexpr (SHARE) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if constexpr (SHARE) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         // ---------------- A, from fp32 ----------------
-        // thread: a piece of eight entries of four rows of memory, `apart` rows from one another
-        const int lt = tid - 32 * (S::FIRST + S::EPI_WARPS), across = A_ACROSS ? 16 : 8, apart = 256 / across;
+        // thread: a piece of eight entries of PIECES rows of memory, `apart` rows from one another
+        constexpr int PIECES = 1024 / (32 * (RAW ? S::LOADERS : 32));
+        const int lt = tid - 32 * (S::FIRST + S::EPI_WARPS), across = A_ACROSS ? 16 : 8, apart = 32 * S::LOADERS / across;
         const int piece = lt % across, row_in = lt / across;
         const uint32_t to = smem_u32(ring) + (piece >> 3) * 8192 + tc_swz(row_in, piece & 7);       // (`apart` rows on: the same place, so many 1024 bytes on)
         const uintptr_t base = reinterpret_cast<uintptr_t>(p.raw);
         const int wide = base % 32 == 0 && p.ld_raw % 8 == 0 ? 8 : base % 16 == 0 && p.ld_raw % 4 == 0 ? 4 : base % 8 == 0 && p.ld_raw % 2 == 0 ? 2 : 1;
-        int of_row[4];               // labels of the rows fetched (looked at when they are there: the rows do not wait for them)
-        auto fetch = [&](float (&v)[4][8], const Tile& t, int c) {
+        int of_row[PIECES];               // labels of the rows fetched (looked at when they are there: the rows do not wait for them)
+        auto fetch = [&](float (&v)[PIECES][8], const Tile& t, int c) {
             const int row0 = (A_ACROSS ? c * LS_KC : t.row * LS_ROWS + (int)rank * 128) + row_in;
             const int col = (A_ACROSS ? t.row * LS_ROWS + (int)rank * 128 : c * LS_KC) + piece * 8, left = p.raw_cols - col;
 #pragma unroll
-            for (int it = 0; it < 4; ++it) {
+            for (int it = 0; it < PIECES; ++it) {
                 const int row = row0 + apart * it;
                 const bool there = row < p.raw_rows && left > 0;
                 const float* const from = p.raw + (int64_t)row * p.ld_raw + col;
@@ -440,11 +441,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
         bool ok = true;
         int s = 0;
         uint32_t ph = 1;
-        auto hand = [&](float (&v)[4][8]) {
+        auto hand = [&](float (&v)[PIECES][8]) {
             ok = mbar_wait_warp(&empty[s], ph, LS_SPIN_LIMIT);
             if (!ok) return;
 #pragma unroll
-            for (int it = 0; it < 4; ++it) {
+            for (int it = 0; it < PIECES; ++it) {
                 if (A_ACROSS && (uint32_t)of_row[it] >= (uint32_t)p.classes) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[it][e] = 0.f;
@@ -471,7 +472,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
         };
         // (the next rows are asked for as soon as these are in shared memory.  Two chunks on their way do not fit the registers: with spills 93 us for
         // the loss of 200 000 rows of 256, one chunk RAW_TIME)
-        float v[4][8];
+        float v[PIECES][8];
         int64_t i = pair;
         Tile t = {};
         int c = 0;
@@ -488,15 +489,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
             if (!A_ACROSS && c == t.first && i + pairs < all) {
                 // and the first chunks of the tile after this one
                 const Tile n = tile_at(i + pairs);
-                const int row = n.row * LS_ROWS + (int)rank * 128 + (lt & 127), col = n.first * LS_KC + (lt >> 7) * 64;
+                const int row = n.row * LS_ROWS + (int)rank * 128 + (lt & 127), col = n.first * LS_KC + (lt >> 7) * 32;
                 const float* const from = p.raw + (int64_t)row * p.ld_raw + col;
                 if (row < p.raw_rows && col < p.raw_cols) asm volatile("prefetch.global.L2 [%0];" ::"l"(from));
-                if (row < p.raw_rows && col + 32 < p.raw_cols) asm volatile("prefetch.global.L2 [%0];" ::"l"(from + 32));
             }
         }
         if (!ok) s_fail = 1;
     } else {
-        if constexpr (SHARE) asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
+        if constexpr (SHARE) asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
         // ---------------- epilogue ----------------
         // thread: a row, and the 32-column blocks part, part + GROUPS, ... of the tile
         const int q = warp & 3, part = (warp - S::FIRST) >> 2;
