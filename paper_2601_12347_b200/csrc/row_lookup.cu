@@ -564,7 +564,7 @@ __global__ void __launch_bounds__(FW_ROWS) k_lookup_grad_few(const __grid_consta
 }
 
 // The same for a table that is small as well: a block for each row of it writes it, zeros included, and no other launch.
-constexpr int64_t FW_TABLE = 4 << 20;      // bytes
+constexpr int64_t FW_TABLE = 4 << 20, FW_TABLE_ROWS = 8192;      // bytes; rows: four rounds of blocks, which for narrow rows are what it takes
 template <typename T, typename TO, int V>
 __global__ void __launch_bounds__(128) k_lookup_grad_table(const __grid_constant__ RunParams p, const int32_t* ids) {
     pdl_enter();
@@ -655,7 +655,7 @@ static cudaError_t launch_lookup_grad(const ripple_lookup_rows_grad_args& a, voi
     const ZeroParams zeros = a.accumulate ? ZeroParams{} : zeros_of(a.out, a.out_rows, a.width, a.ld_out, sizeof(TO));
     const unsigned zero_blocks = (unsigned)std::min<int64_t>(zeros.units, (int64_t)ZERO_BLOCKS * sm_count());
     if (a.rows <= FW_ROWS) {
-        if (a.out_rows * a.width * (int64_t)sizeof(TO) <= FW_TABLE)
+        if (a.out_rows <= FW_TABLE_ROWS && a.out_rows * a.width * (int64_t)sizeof(TO) <= FW_TABLE)
             return launch(k_lookup_grad_table<T, TO, V>, dim3((unsigned)a.out_rows), 128, 0, stream, r, a.ids);
         if (zeros.units > 0) e = launch(k_zeros, dim3(zero_blocks), 256, 0, stream, zeros);
         if (e != cudaSuccess || a.rows == 0) return e;

@@ -169,18 +169,38 @@ __device__ __forceinline__ float grad_scale(const RowControl* control, float sca
     return ldexpf(1.f, max(-126, min(126, 15 - e)));
 }
 
+// Two fp32 operations in one instruction: (a, b) += (c, d), (a, b) *= (c, d), (a, b) = (a, b) (c, c) + (d, d).  (A warp's block of 32 columns of g took 564 instructions,
+// a tile 4500 cycles of issue slots beside 4096 of products at k = 512.)
+__device__ __forceinline__ void add2(float& a, float& b, float c, float d) {
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+__device__ __forceinline__ void mul2(float& a, float& b, float c, float d) {
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+__device__ __forceinline__ void fma2(float& a, float& b, float c, float d) {
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+
 // Sums over the warp's rows of 32 columns: lane c has the sum of v[c].
 __device__ __forceinline__ float column_sums(float (&v)[32]) {
 #pragma unroll
     for (int half = 16; half > 0; half >>= 1) {
         const bool upper = lane_id() & half;
+        if (half == 1) return (upper ? v[1] : v[0]) + __shfl_xor_sync(FULL, upper ? v[0] : v[1], 1);
 #pragma unroll
-        for (int i = 0; i < half; ++i) {
-            const float mine = upper ? v[i + half] : v[i], other = upper ? v[i] : v[i + half];
-            v[i] = mine + __shfl_xor_sync(FULL, other, half);
+        for (int i = 0; i < half; i += 2) {
+            float mine[2], other[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                mine[e] = upper ? v[i + e + half] : v[i + e];
+                other[e] = __shfl_xor_sync(FULL, upper ? v[i + e] : v[i + e + half], half);
+            }
+            add2(mine[0], mine[1], other[0], other[1]);
+            v[i] = mine[0], v[i + 1] = mine[1];
         }
     }
-    return v[0];
+    return 0.f;
 }
 
 // Warp 0 of each CTA brings operands, warp 1 of the pair's first CTA issues the products, the others take finished accumulators while the next
@@ -502,9 +522,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
         const int q = warp & 3, part = (warp - S::FIRST) >> 2;
         const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16);
         float* const bias = reinterpret_cast<float*>(ring + STAGES * S::STAGE) + (warp - S::FIRST) * 32 * NB;
-        float factor = 1.f;                      // GRAD: of g; OUT: of the result
+        float factor = 1.f, unfactor = 1.f;      // GRAD: of g, and of its sums; OUT: of the result
         if (TYPE == RIPPLE_TYPE_F16 && p.control) {
-            if (END == END_GRAD) factor = grad_scale(p.control, p.scale);
+            if (END == END_GRAD) factor = grad_scale(p.control, p.scale), unfactor = 1.f / factor;
             if (END == END_OUT && p.unscale) factor = 1.f / grad_scale(p.control, p.scale);
         }
         const uint32_t release = in_leader(&acc_empty[0]);
@@ -538,7 +558,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
             const int row = row_of_tile(t), col0 = t.col * COLS;
             const bool in_rows = row < p.m, labelled = asked.label >= 0 && asked.label < p.classes;
             bool live = END == END_OUT ? in_rows && (!p.dead_rows || labelled) : labelled;
-            const float lse = asked.lse, weight = p.scale * asked.dloss;
+            const float lse = asked.lse, weight = p.scale * asked.dloss * (END == END_GRAD ? factor : 1.f);
             float top = -INFINITY, sum = 0.f;
             if (END == END_GRAD) live = live && lse != -INFINITY;
             const int label = live ? asked.label - p.class0 - col0 : -1;       // within the tile
@@ -558,7 +578,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float4 b = b4[e];
-                        y[4 * e] += b.x, y[4 * e + 1] += b.y, y[4 * e + 2] += b.z, y[4 * e + 3] += b.w;
+                        add2(y[4 * e], y[4 * e + 1], b.x, b.y), add2(y[4 * e + 2], y[4 * e + 3], b.z, b.w);
                     }
                     if (__any_sync(FULL, (unsigned)(label - at) < 32u)) {
 #pragma unroll
@@ -571,7 +591,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
                     sum *= exp2_of(top * LOG2E - base);
                     float more[4] = {};
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) more[e & 3] += exp2_of(fmaf(y[e], LOG2E, -base));
+                    for (int e = 0; e < 32; e += 2) {
+                        fma2(y[e], y[e + 1], LOG2E, -base);
+                        add2(more[e & 2], more[(e & 2) + 1], exp2_of(y[e]), exp2_of(y[e + 1]));
+                    }
                     sum += (more[0] + more[1]) + (more[2] + more[3]);
                     top = most;
                 } else if constexpr (END == END_GRAD) {
@@ -579,16 +602,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float4 b = b4[e];
-                        y[4 * e] += b.x, y[4 * e + 1] += b.y, y[4 * e + 2] += b.z, y[4 * e + 3] += b.w;
+                        add2(y[4 * e], y[4 * e + 1], b.x, b.y), add2(y[4 * e + 2], y[4 * e + 3], b.z, b.w);
                     }
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) y[e] = exp2_of((y[e] - lse) * LOG2E);
+                    for (int e = 0; e < 32; e += 2) {
+                        add2(y[e], y[e + 1], -lse, -lse);
+                        mul2(y[e], y[e + 1], LOG2E, LOG2E);
+                        y[e] = exp2_of(y[e]), y[e + 1] = exp2_of(y[e + 1]);
+                    }
                     if (__any_sync(FULL, (unsigned)(label - at) < 32u)) {
 #pragma unroll
                         for (int e = 0; e < 32; ++e) if (label == at + e) y[e] -= 1.f;
                     }
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) y[e] *= weight;
+                    for (int e = 0; e < 32; e += 2) mul2(y[e], y[e + 1], weight, weight);
                     if (!__all_sync(FULL, live)) {
 #pragma unroll
                         for (int e = 0; e < 32; ++e) y[e] = live ? y[e] : 0.f;
@@ -600,10 +627,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
                             for (int h = 0; h < 2; ++h) {
                                 uint32_t v[8];
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    if constexpr (TYPE == RIPPLE_TYPE_F16) v[e] = pair_of<T>(y[16 * h + 2 * e] * factor, y[16 * h + 2 * e + 1] * factor);
-                                    else v[e] = pair_of<T>(y[16 * h + 2 * e], y[16 * h + 2 * e + 1]);
-                                }
+                                for (int e = 0; e < 8; ++e) v[e] = pair_of<T>(y[16 * h + 2 * e], y[16 * h + 2 * e + 1]);
                                 store8(to + 16 * h, v);
                             }
                         } else {
@@ -628,7 +652,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
                     }
                     if (p.g_sums) {
                         const float s = column_sums(y);
-                        if (row - lane < p.m) p.g_sums[(int64_t)((row - lane) >> 5) * p.ld_g + col0 + at + lane] = s;
+                        if (row - lane < p.m) p.g_sums[(int64_t)((row - lane) >> 5) * p.ld_g + col0 + at + lane] = s * unfactor;
                     }
                 } else {
                     if (!in_rows) return;

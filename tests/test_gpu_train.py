@@ -99,6 +99,16 @@ def test_gradients_that_are_added(rows, dtype, out):
     check_lookup_grad(rnd(g, rows, 40, dtype=DTYPES[dtype]), ids, 4000, scale=0.5, out=rnd(g, 4000, 40, dtype=DTYPES[out]), accumulate=True)
 
 
+@pytest.mark.parametrize("width", [1, 2, 3])
+@pytest.mark.parametrize("rows", [0, 1, 100, 256, 257])
+@pytest.mark.parametrize("table", [8192, 8193, 2_000_000])
+def test_narrow_gradients_of_long_tables(width, rows, table):
+    g = gen(rows + table)
+    for accumulate in (False, True):
+        out = rnd(g, table, width)
+        check_lookup_grad(rnd(g, rows, width), draw_ids(g, rows, table, 2), table, out=out, accumulate=accumulate)
+
+
 @pytest.mark.parametrize("rows", [5, 400, 9000])
 def test_lookups_over_strides_and_columns(rows):
     """Rows that lie apart, columns of wider matrices, at every alignment."""
