@@ -26,10 +26,9 @@ cudaError_t take_loss_timeout(int* gave_up) {
 }
 
 // ---- a product on pairs of tensor cores ----------------------------------------------------------------------------
-// C [m, n] = A B over k, operands of 16 bits, fp32 as three planes of bf16 parts.  A pair of CTAs takes 256 rows x LS_COLS columns of C: each
+// C [m, n] = A B over k, operands of 16 bits, fp32 as three planes of bf16 parts.  A pair of CTAs takes 256 rows x COLS columns of C: each
 // brings its 128 rows of A and its half of the tile's columns of B, the pair's tensor cores read both halves, and each has its 128 rows
-// of C.  (One CTA by itself brings 48 KB per 64 entries of k, where an SM gets 64 bytes a cycle out of L2: 768 cycles for 512 of products.)
-// Operands come by TMA in either order, k along the rows of memory or across them; what lies outside a matrix arrives as zeros.
+// of C: 32 KB per 64 entries of k and CTA, where a CTA by itself would bring 48 for the same products.  Operands come by TMA in either order, k along the rows of memory or across them; what lies outside a matrix arrives as zeros.
 constexpr int LS_ROWS = 256, LS_KC = 64;
 constexpr int LS_PAIRS = 74;             // of a B200 (for plans that are asked where no device is current, too)
 constexpr int LS_UNIT = 4;               // fp32: chunks (256 entries of k) whose large products share an accumulator
@@ -206,8 +205,14 @@ __device__ __forceinline__ float column_sums(float (&v)[32]) {
 // Warp 0 of each CTA brings operands, warp 1 of the pair's first CTA issues the products, the others take finished accumulators while the next
 // are being filled.  Barriers, all waits bounded: full[s] in the first CTA (its one arrival announces the bytes of both), empty[s] in both
 // (the products that read stage s), acc_full[b] in both, acc_empty[b] in the first CTA (one arrival per epilogue warp of the pair).
-// RAW: eight more warps bring A, fetched through registers and split into parts on its way (a pass that writes the parts and one that reads them move 16
+// RAW: sixteen more warps bring A, fetched through registers and split into parts on its way (a pass that writes the parts and one that reads them move 16
 // bytes an entry in place of 4: loss-cached-rows, 78 us for the former alone); a warp in each CTA passes on to full[s] that a stage is made.
+//
+// What bounds it.  16-bit operands: the tensor cores, 82 to 89 % of the time active with plain results and maxima (16 384 x 1024 x 65 536: 1.40 ms, 1.57
+// PFLOP/s; dx and dW of it 1.4 to 1.5), over seconds the 1000 W of the card; g of a tile takes its warps longer than products over less than a thousand entries of k
+// (6001 x 512 x 32 003: 222 us, 0.89 PFLOP/s; exponentials, column sums by shuffles).  fp32 x: hand-overs between the roles, 3500 cycles for 64 entries of k whose products are
+// 1000 and whose operands take 1600 cycles of shared memory (200 000 rows of 256 to 47 classes: 78 us, 2.6 TB/s).  Tried there: 8 warps (79 us), two chunks on their way in
+// registers (93, spills), asynchronous copies into shared memory and two stages (104).
 // fp32: six products of parts (all but those below 2^-24); the large one, of the first parts, is handed over every 256 entries of k and
 // summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
 template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END, bool MANY, bool RAW>
@@ -490,8 +495,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
             if (lane == 0) mbar_arrive(&made[s]);
             if (++s == STAGES) { s = 0; ph ^= 1; }
         };
-        // (the next rows are asked for as soon as these are in shared memory.  Two chunks on their way do not fit the registers: with spills 93 us for
-        // the loss of 200 000 rows of 256, one chunk RAW_TIME)
+        // (the next rows are asked for as soon as these are in shared memory)
         float v[PIECES][8];
         int64_t i = pair;
         Tile t = {};
@@ -922,21 +926,24 @@ __global__ void __launch_bounds__(256) k_join_many_parts(const float* parts, int
     }
 }
 
-// dbias from the sums over groups of 32 rows; a block has 8 columns, its warps and the four parts of a warp take turns over the groups.
+// dbias from the sums over groups of 32 rows; a block has COLS columns, its warps and the parts of a warp take turns over the groups.  Eight where that is
+// what makes a block for every SM, else 32 (16 384 columns: 28 us and 11).
+template <int COLS>
 __global__ void __launch_bounds__(1024) k_join_columns(const float* sums, int64_t groups, int64_t ld, int cols, float* out) {
     pdl_enter();
-    __shared__ float mine[32][8];
-    const int warp = threadIdx.x >> 5, lane = lane_id(), c = blockIdx.x * 8 + (lane & 7);
+    __shared__ float mine[32][COLS];
+    constexpr int TURNS = 32 / COLS;
+    const int warp = threadIdx.x >> 5, lane = lane_id(), c = blockIdx.x * COLS + lane % COLS;
     float sum = 0.f;
     if (c < cols) {
 #pragma unroll 16
-        for (int64_t i = warp * 4 + (lane >> 3); i < groups; i += 128) sum += sums[i * ld + c];
+        for (int64_t i = warp * TURNS + lane / COLS; i < groups; i += 32 * TURNS) sum += sums[i * ld + c];
     }
-    sum += __shfl_xor_sync(FULL, sum, 8);
-    sum += __shfl_xor_sync(FULL, sum, 16);
-    if (lane < 8) mine[warp][lane] = sum;
+#pragma unroll
+    for (int o = COLS; o < 32; o *= 2) sum += __shfl_xor_sync(FULL, sum, o);
+    if (lane < COLS) mine[warp][lane] = sum;
     __syncthreads();
-    if (warp > 0 || lane >= 8 || c >= cols) return;
+    if (warp > 0 || lane >= COLS || c >= cols) return;
     sum = 0.f;
     for (int w = 0; w < 32; ++w) sum += mine[w][lane];
     out[c] = sum;
@@ -1449,7 +1456,12 @@ static cudaError_t run_loss_grad(const ripple_loss_rows_grad_args& a) {
         const Matrix* const same = TYPE == RIPPLE_TYPE_F16 ? &x : nullptr;
         e = launch_product<TYPE, false, true, END_GRAD, true>(p, x, same, w, 1, stream);
         if (e != cudaSuccess) return e;
-        if (a.dbias && (e = launch(k_join_columns, dim3((unsigned)(classes + 7) / 8), 1024, 0, stream, (const float*)p.g_sums, (a.rows + 31) / 32, l.ld_g, classes, a.dbias + c0)) != cudaSuccess) return e;
+        if (a.dbias) {
+            const int wide = classes > 8 * 2 * LS_PAIRS ? 32 : 8;
+            auto* const join = wide == 32 ? k_join_columns<32> : k_join_columns<8>;
+            e = launch(join, dim3((unsigned)((classes + wide - 1) / wide)), 1024, 0, stream, (const float*)p.g_sums, (a.rows + 31) / 32, l.ld_g, classes, a.dbias + c0);
+            if (e != cudaSuccess) return e;
+        }
         const Matrix g{work + l.g, a.rows, classes, l.ld_g, l.g_plane, parts_of(TYPE)};
         ProductParams o = {};
         o.unscale = TYPE == RIPPLE_TYPE_F16, o.scale = a.scale, o.classes = a.n;
