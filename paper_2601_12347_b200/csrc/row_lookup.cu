@@ -374,7 +374,7 @@ constexpr int RS_WARPS = 8, RS_CHUNK = 32 * RS_WARPS;      // entries of a block
 __device__ __forceinline__ uint32_t bare(uint32_t key) { return key & ~EMPTY; }
 
 // V neighbouring elements as they lie in memory, 32 bits at a time: as elements the compiler would widen all of them as soon as they are there, into
-// registers that eight rows on their way do not leave it (300 007 rows of 256 bf16: 121 us in place of 58).
+// registers that there are not (300 007 rows of 256 bf16: 121 us in place of 58).
 template <typename T, int V> struct Raw {
     static constexpr int WORDS = V * (int)sizeof(T) < 4 ? 1 : V * (int)sizeof(T) / 4;
     uint32_t w[WORDS];
@@ -450,12 +450,16 @@ struct Runs {
     }
 };
 
-// (WIDE: 32 bytes of a lane at a time, lists of partial sums of 16-bit rows; there are few blocks of those, and rows on their way count)
+constexpr int RS_GROUPS = 2;       // of four rows of a warp, on their way at once
+// Rows travel as asynchronous copies into places of shared memory that a lane alone reads: what is on its way takes no registers (300 007 rows of 256 bf16:
+// four rows of a warp in registers 58 us, eight as copies 44; sixteen, which leave room for two blocks of an SM, 53).
+template <typename T, int V> constexpr int rs_ring_bytes(int np) { return V * (int)sizeof(T) >= 16 ? RS_WARPS * 4 * RS_GROUPS * 32 * V * np * (int)sizeof(T) : 0; }
 template <typename T, typename TO, int V, int NP>
-__global__ void __launch_bounds__(32 * RS_WARPS, sizeof(T) * V * NP > 16 ? 2 : 4) k_sum_runs(const __grid_constant__ RunParams p) {
+__global__ void __launch_bounds__(32 * RS_WARPS) k_sum_runs(const __grid_constant__ RunParams p) {
     pdl_enter();
-    constexpr bool WIDE = sizeof(T) * V * NP > 16;
+    constexpr bool RING = V * sizeof(T) >= 16;
     constexpr int COLS = 32 * V * NP;
+    extern __shared__ __align__(16) uint8_t ring[];
     __shared__ __align__(16) float part[2 * RS_WARPS][COLS];
     __shared__ uint32_t part_key[2 * RS_WARPS];
     const int warp = threadIdx.x >> 5, lane = lane_id(), block = blockIdx.x / p.slices, slice = blockIdx.x - block * p.slices;
@@ -473,26 +477,58 @@ __global__ void __launch_bounds__(32 * RS_WARPS, sizeof(T) * V * NP > 16 ? 2 : 4
         const uint32_t key_before = __shfl_up_sync(FULL, bare(key), 1);
         const uint32_t begins = __ballot_sync(FULL, lane > 0 && lane < count && bare(key) != key_before);
         const uint32_t reads = __ballot_sync(FULL, lane < count && key < p.table_rows);
-        constexpr int AHEAD = WIDE ? 8 : 4;       // rows of a warp that are on their way (32 warps of an SM: up to 64 KB)
-        using Batch = Raw<T, V>[AHEAD][NP];
         const T* const src = static_cast<const T*>(p.src) + c0;
-        auto request = [&](Batch& v, int e0) {
+        if constexpr (RING) {
+            // four rows to a group of copies, RS_GROUPS groups on their way
+            constexpr int ROW = COLS * (int)sizeof(T);
+            uint8_t* const mine = ring + warp * (4 * RS_GROUPS * ROW) + lane * V * (int)sizeof(T);
+            auto request = [&](int e0) {
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const T* const from = src + (int64_t)__shfl_sync(FULL, place, e0 + u) * p.ld_src;
-                if (reads >> (e0 + u) & 1) runs.each([&](int j, int c) { v[u][j].read(from + c); });
-            }
-        };
-        auto take = [&](const Batch& v, int e0) {
+                for (int u = 0; u < 4; ++u) {
+                    const T* const from = src + (int64_t)__shfl_sync(FULL, place, (e0 + u) & 31) * p.ld_src;
+                    const uint32_t to = (uint32_t)__cvta_generic_to_shared(mine + ((e0 + u) & (4 * RS_GROUPS - 1)) * ROW);
+                    if (e0 < 32 && (reads >> ((e0 + u) & 31) & 1)) runs.each([&](int, int c) { copy_async<V * (int)sizeof(T)>(to + c * (int)sizeof(T), from + c); });
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                if (begins >> (e0 + u) & 1) runs.begin(__shfl_sync(FULL, key, e0 + u));
-                if (reads >> (e0 + u) & 1) runs.add([&](int j) -> const Raw<T, V>& { return v[u][j]; });
-            }
-        };
-        Batch v;
+            for (int g = 0; g < RS_GROUPS; ++g) request(4 * g);
 #pragma unroll 1
-        for (int e0 = 0; e0 < count; e0 += AHEAD) request(v, e0), take(v, e0);
+            for (int e0 = 0; e0 < count; e0 += 4) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(RS_GROUPS - 1) : "memory");
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (begins >> (e0 + u) & 1) runs.begin(__shfl_sync(FULL, key, e0 + u));
+                    const T* const from = reinterpret_cast<const T*>(mine + ((e0 + u) & (4 * RS_GROUPS - 1)) * ROW);
+                    if (reads >> (e0 + u) & 1) {
+                        runs.add([&](int j) {
+                            Raw<T, V> r;
+                            r.read(from + j * 32 * V);
+                            return r;
+                        });
+                    }
+                }
+                request(e0 + 4 * RS_GROUPS);
+            }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        } else {
+            // (narrower accesses through registers: 20 011 rows of 602 fp32, 24 us, as copies of 8 bytes 29)
+            constexpr int AHEAD = 4;
+            Raw<T, V> v[AHEAD][NP];
+#pragma unroll 1
+            for (int e0 = 0; e0 < count; e0 += AHEAD) {
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const T* const from = src + (int64_t)__shfl_sync(FULL, place, e0 + u) * p.ld_src;
+                    if (reads >> (e0 + u) & 1) runs.each([&](int j, int c) { v[u][j].read(from + c); });
+                }
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    if (begins >> (e0 + u) & 1) runs.begin(__shfl_sync(FULL, key, e0 + u));
+                    if (reads >> (e0 + u) & 1) runs.add([&](int j) -> const Raw<T, V>& { return v[u][j]; });
+                }
+            }
+        }
         runs.finish(runs.run == after);
         head_key = runs.head_key, tail_key = runs.tail_key;
     }
@@ -525,7 +561,11 @@ template <typename T, typename TO, int V, int NP>
 static cudaError_t launch_runs(RunParams p, void* stream) {
     p.slices = (p.width + 32 * V * NP - 1) / (32 * V * NP);
     const int64_t blocks = (int64_t)((p.n + RS_CHUNK - 1) / RS_CHUNK) * p.slices;
-    return launch(k_sum_runs<T, TO, V, NP>, dim3((unsigned)blocks), 32 * RS_WARPS, 0, stream, p);
+    constexpr int bytes = rs_ring_bytes<T, V>(NP);
+    static bool ready[64];
+    const cudaError_t e = allow_shared(k_sum_runs<T, TO, V, NP>, bytes, ready);
+    if (e != cudaSuccess) return e;
+    return launch(k_sum_runs<T, TO, V, NP>, dim3((unsigned)blocks), 32 * RS_WARPS, bytes, stream, p);
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------
