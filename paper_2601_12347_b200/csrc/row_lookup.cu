@@ -812,7 +812,7 @@ extern "C" ripple_status ripple_lookup_rows(const ripple_lookup_rows_args* a) {
 #undef WHAT
 
 static bool lookup_grad_sizes_ok(const ripple_lookup_rows_grad_args* a) {
-    return a->rows >= 0 && a->rows <= INT32_MAX && a->width >= 1 && a->width <= 16384 && a->out_rows >= 0 && a->out_rows < INT32_MAX;
+    return a->rows >= 0 && a->rows <= INT32_MAX - SR_TILE && a->width >= 1 && a->width <= 16384 && a->out_rows >= 0 && a->out_rows < INT32_MAX;
 }
 
 extern "C" int64_t ripple_lookup_rows_grad_workspace_bytes(const ripple_lookup_rows_grad_args* a) {

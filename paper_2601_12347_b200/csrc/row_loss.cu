@@ -54,7 +54,7 @@ template <int TYPE, bool MANY, bool RAW = false> struct LossShape {
 };
 
 enum { END_LSE, END_GRAD, END_OUT };
-constexpr int LS_CONTROL = 128;          // blocks of k_look_at_rows
+constexpr int LS_CONTROL = 512;          // blocks of k_look_at_rows (where few rows have labels, it reads most of x)
 
 // What k_look_at_rows found, block by block.
 struct RowControl {
@@ -822,7 +822,7 @@ __global__ void __launch_bounds__(256) k_look_at_rows(const T* x, int64_t ld_x, 
     __shared__ float scratch[8];
     float most = 0.f;
     bool odd = false;
-    for (int64_t r0 = (int64_t)blockIdx.x * 256 + (threadIdx.x & ~31); r0 < rows; r0 += (int64_t)LS_CONTROL * 256) {
+    for (int64_t r0 = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * 32; r0 < rows; r0 += (int64_t)LS_CONTROL * 256) {
         const int64_t row = r0 + lane_id();
         const bool live = row < rows && has_label(labels, row, classes);
         if (live) {

@@ -276,6 +276,8 @@ def test_norm_gradients_of_padding_rows():
     keep = [i for i in range(50) if i % 3]
     want = train.norm_rows_grad(dn[keep], x[keep], norm, add=torch.full((len(keep), 70), 3.0, device="cuda"))
     assert torch.equal(got[0][keep], want[0])
+    for t in train.norm_rows_grad(dn, x[:0], norm, ids=ids):          # a table without rows
+        assert (t == 0).all()
     none = train.norm_rows_grad(dn[:0], x, norm, ids=ids[:0])
     assert none[0].shape == (0, 70) and (none[1] == 0).all() and (none[2] == 0).all()
     a, b, c = train.norm_rows_grad(dn[1:2], x[1:2], norm, vectors=False)
@@ -450,6 +452,22 @@ def test_rows_without_a_label_may_hold_anything(rows, K, dtype):
     for a, b in zip(got, want):
         assert torch.isfinite(a).all() and torch.equal(a, b)
     assert (got[0][dead] == 0).all()
+
+
+@pytest.mark.parametrize("rows", [1, 60, 1500, 70_000])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_few_labels_or_none(rows, dtype):
+    """Most vertices of a batch have no label: one in a thousand, the last one alone, none."""
+    g = gen(rows)
+    for padding in (0.999, 1.0):
+        q = problem(g, rows, 64, 48, DTYPES[dtype], padding=padding)
+        if padding < 1:
+            q["labels"][-1] = 7
+        check_loss(**q, dloss=rows_of(g, rows))
+    loss, lse = train.loss_rows(**q)
+    assert (loss == 0).all() and torch.isfinite(lse).all()
+    q["x"][:] = float("nan")
+    assert all((t == 0).all() for t in train.loss_rows_grad(lse=train.loss_rows(**q)[1], **q))
 
 
 @pytest.mark.parametrize("rows", [60, 1500])

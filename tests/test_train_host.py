@@ -109,7 +109,7 @@ def test_lookup_rows_refuses(lib, wrong):
 @no_device
 @pytest.mark.parametrize("wrong", [
     dict(rows=-1), dict(rows=1 << 31), dict(width=0), dict(width=16385), dict(type=3), dict(out_type=1), dict(type=1, out_type=2), dict(out_rows=-1),
-    dict(out_rows=(1 << 31) - 1), dict(accumulate=2), dict(accumulate=-1), dict(dy=0), dict(ids=0), dict(out=0), dict(ld_dy=-1), dict(ld_out=7),
+    dict(rows=(1 << 31) - 1), dict(out_rows=(1 << 31) - 1), dict(accumulate=2), dict(accumulate=-1), dict(dy=0), dict(ids=0), dict(out=0), dict(ld_dy=-1), dict(ld_out=7),
     dict(dy=A + 1), dict(ids=2 * A + 2), dict(out=3 * A + 2), dict(workspace=0), dict(workspace_bytes=64), dict(workspace=4 * A + 64), dict(out=A),
     dict(out=2 * A + 4), dict(out=4 * A), dict(workspace=A), dict(workspace=2 * A - 128),
 ], ids=str)
