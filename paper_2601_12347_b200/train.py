@@ -20,6 +20,7 @@ any gradient, whatever its rows hold.
 from __future__ import annotations
 
 import struct
+from functools import lru_cache
 from typing import Dict
 
 import torch
@@ -38,11 +39,6 @@ _LOSS_ARGS = struct.Struct("=q4i QqQq QQQQ Qq Q")
 _LOSS_GRAD_ARGS = struct.Struct("=q4i QqQq QQQQ QqQqQ fi Qq Q")
 
 
-def _tangents(**tensors) -> None:
-    if getattr(forward_ad, "_current_level", 0) >= 0:
-        _refuse_tangents(**tensors)
-
-
 def _ids(ids, index: int):
     if getattr(ids, "dim", lambda: 0)() != 1:
         raise ValueError("ids: one dimension expected")
@@ -55,6 +51,35 @@ def _workspace(need: int, like):
     return torch.empty(need, dtype=torch.uint8, device=like.device) if need > 0 else None
 
 
+# Bytes of scratch, by sizes (and how matrices are aligned): asked of the library once for each.
+@lru_cache(maxsize=4096)
+def _lookup_grad_need(rows, width, t, to, table_rows):
+    return _ripple.load_library().ripple_lookup_rows_grad_workspace_bytes(
+        _LOOKUP_GRAD_ARGS.pack(rows, width, t, to, 0, 0, width, 0, 0, width, table_rows, 1.0, 0, 0, 0, 0))
+
+
+@lru_cache(maxsize=4096)
+def _norm_grad_need(rows, width, t, tx, vectors):
+    return _ripple.load_library().ripple_norm_rows_grad_workspace_bytes(
+        _NORM_GRAD_ARGS.pack(rows, width, t, tx, 0, 0, width, 0, width, rows, 0, 0, 0, 0, width, 64 if vectors else 0, 0, 1, 0.0, 0, 0, 0, 0, 0))
+
+
+@lru_cache(maxsize=4096)
+def _loss_need(rows, t, K, N, x_at, x_ld, w_at, w_ld):
+    return _ripple.load_library().ripple_loss_rows_workspace_bytes(_LOSS_ARGS.pack(rows, t, K, N, 0, x_at, x_ld, w_at, w_ld, 0, 0, 0, 0, 0, 0, 0))
+
+
+@lru_cache(maxsize=4096)
+def _loss_grad_need(rows, t, K, N, x_at, x_ld, w_at, w_ld, dx_at, dw_at, bias):
+    return _ripple.load_library().ripple_loss_rows_grad_workspace_bytes(_LOSS_GRAD_ARGS.pack(
+        rows, t, K, N, 0, x_at, x_ld, w_at, w_ld, 0, 0, 0, 0, dx_at, K, dw_at, N, 64 if bias else 0, 1.0, 0, 0, 0, 0))
+
+
+def _aligned_as(ptr: int) -> int:
+    """An address that is not null and as aligned as this one."""
+    return 1024 + (ptr & 255)
+
+
 def _or_null(t) -> int:
     return 0 if t is None else t.data_ptr()
 
@@ -62,7 +87,8 @@ def _or_null(t) -> int:
 def lookup_rows(table, ids, scale: float = 1.0, out=None, out_dtype=None):
     """scale * table[ids], one row per id (int32), zeros for ids outside the table.  The result has the table's type, or the one that
     out_dtype (or out) says if the table is fp32."""
-    _tangents(table=table, out=out)
+    if getattr(forward_ad, "_current_level", 0) >= 0:
+        _refuse_tangents(table=table, out=out)
     index = _device_of(table, "table")
     ptr, ld, table_rows = _matrix(table, "table", None, None, index)
     width = table.shape[1]
@@ -87,7 +113,8 @@ def lookup_rows(table, ids, scale: float = 1.0, out=None, out_dtype=None):
 def lookup_rows_grad(dy, ids, table_rows: int, scale: float = 1.0, out=None, out_dtype=None, accumulate: bool = False):
     """The gradient of lookup_rows' table: [table_rows, D], row r = scale * the sum of dy's rows whose id is r; of dy's type, or fp32 if
     out_dtype (or out) says so.  accumulate: add to the rows of `out` that ids name, once for each, and touch no other."""
-    _tangents(dy=dy, out=out)
+    if getattr(forward_ad, "_current_level", 0) >= 0:
+        _refuse_tangents(dy=dy, out=out)
     index = _device_of(dy, "dy")
     ptr, ld, rows = _matrix(dy, "dy", None, None, index)
     width = dy.shape[1]
@@ -110,7 +137,7 @@ def lookup_rows_grad(dy, ids, table_rows: int, scale: float = 1.0, out=None, out
         raise TypeError(f"out: {dy.dtype} or float32 expected, got {out.dtype}")
     lib = _ripple.load_library()
     head = (rows, width, t, to, index, ptr, ld, ids_ptr, out_ptr, out_ld, int(table_rows), float(scale), bool(accumulate))
-    need = lib.ripple_lookup_rows_grad_workspace_bytes(_LOOKUP_GRAD_ARGS.pack(*head, 0, 0, 0))
+    need = _lookup_grad_need(rows, width, t, to, int(table_rows))
     work = _workspace(need, dy)
     _check(lib.ripple_lookup_rows_grad(_LOOKUP_GRAD_ARGS.pack(*head, _or_null(work), max(need, 0), _stream(index))))
     return out
@@ -122,7 +149,8 @@ def norm_rows_grad(dn, x, norm: Norm, ids=None, add=None, out=None, dx: bool = T
     of the same type: what reaches x past the norm, added before dx is rounded.  out: where to write dx; it may be dn, add, or, without ids, x."""
     if not isinstance(norm, Norm):
         raise TypeError(f"norm: a Norm expected, got {type(norm).__name__}")
-    _tangents(dn=dn, x=x, add=add, out=out)
+    if getattr(forward_ad, "_current_level", 0) >= 0:
+        _refuse_tangents(dn=dn, x=x, add=add, out=out)
     index = _device_of(dn, "dn")
     dn_ptr, dn_ld, rows = _matrix(dn, "dn", None, None, index)
     width = dn.shape[1]
@@ -159,7 +187,7 @@ def norm_rows_grad(dn, x, norm: Norm, ids=None, add=None, out=None, dx: bool = T
     stream = _stream(index)
     head = (rows, width, t, tx, index, dn_ptr, dn_ld, x_ptr, x_ld, x_rows, ids_ptr, add_ptr, add_ld, out_ptr, out_ld,
             _or_null(dweight), _or_null(dbias), *norm._packed(width, index, stream, "norm"))
-    need = lib.ripple_norm_rows_grad_workspace_bytes(_NORM_GRAD_ARGS.pack(*head, 0, 0, 0))
+    need = _norm_grad_need(rows, width, t, tx, dweight is not None or dbias is not None)
     work = _workspace(need, dn)
     _check(lib.ripple_norm_rows_grad(_NORM_GRAD_ARGS.pack(*head, _or_null(work), max(need, 0), stream)))
     return out, dweight, dbias
@@ -176,18 +204,22 @@ def _linear(x, W, labels, bias):
     t = _type_of(x.dtype, "x")
     labels_ptr = _vector(labels, "labels", rows, torch.int32, index)
     bias_ptr = 0 if bias is None else _vector(bias, "bias", W.shape[1], torch.float32, index)
-    return index, rows, (rows, t, K, W.shape[1], index, x_ptr, x_ld, w_ptr, w_ld, bias_ptr, labels_ptr)
+    N = W.shape[1]
+    return index, rows, (rows, t, K, N, index, x_ptr, x_ld, w_ptr, w_ld, bias_ptr, labels_ptr), (rows, t, K, N, _aligned_as(x_ptr), x_ld, _aligned_as(w_ptr), w_ld)
 
 
 def loss_rows(x, W, labels, bias=None):
     """(loss, lse), fp32 [rows]: lse_i = log sum_c exp z_ic, loss_i = lse_i - z_i,label with z = x W + bias; 0 for labels (int32) that are no
     class.  x [rows, K] and W [K, N] of one type, bias fp32; a bias of minus infinity takes a class out."""
-    _tangents(x=x, W=W, bias=bias)
-    index, rows, head = _linear(x, W, labels, bias)
-    loss, lse = (torch.empty(rows, dtype=torch.float32, device=x.device) for _ in range(2))
+    if getattr(forward_ad, "_current_level", 0) >= 0:
+        _refuse_tangents(x=x, W=W, bias=bias)
+    index, rows, head, sizes = _linear(x, W, labels, bias)
+    device = x.device
+    loss = torch.empty(rows, dtype=torch.float32, device=device)
+    lse = torch.empty(rows, dtype=torch.float32, device=device)
     head = (*head, loss.data_ptr(), lse.data_ptr())
     lib = _ripple.load_library()
-    need = lib.ripple_loss_rows_workspace_bytes(_LOSS_ARGS.pack(*head, 0, 0, 0))
+    need = _loss_need(*sizes)
     work = _workspace(need, x)
     _check(lib.ripple_loss_rows(_LOSS_ARGS.pack(*head, _or_null(work), max(need, 0), _stream(index))))
     return loss, lse
@@ -197,8 +229,9 @@ def loss_rows_grad(x, W, labels, lse, dloss=1.0, bias=None, dx: bool = True, dW:
     """(dx, dW, dbias) of loss_rows, from what it gave as lse and dloss: fp32 [rows], or a number for all rows.  dx [rows, K] and
     dW [K, N] have the type of x and W (None where they are not wanted), dbias is fp32 (None without bias).  What each row adds is
     dloss_i (softmax(z)_i - onehot(label_i)): formed anew from x and W, in pieces of the classes."""
-    _tangents(x=x, W=W, bias=bias, lse=lse, dloss=dloss)
-    index, rows, head = _linear(x, W, labels, bias)
+    if getattr(forward_ad, "_current_level", 0) >= 0:
+        _refuse_tangents(x=x, W=W, bias=bias, lse=lse, dloss=dloss)
+    index, rows, head, sizes = _linear(x, W, labels, bias)
     lse_ptr = _vector(lse, "lse", rows, torch.float32, index)
     scale, dloss_ptr = 1.0, 0
     if isinstance(dloss, torch.Tensor):
@@ -212,7 +245,7 @@ def loss_rows_grad(x, W, labels, lse, dloss=1.0, bias=None, dx: bool = True, dW:
     gb = torch.empty(W.shape[1], dtype=torch.float32, device=x.device) if bias is not None else None
     head = (*head, lse_ptr, dloss_ptr, _or_null(gx), x.shape[1], _or_null(gw), W.shape[1], _or_null(gb), scale, 0)
     lib = _ripple.load_library()
-    need = lib.ripple_loss_rows_grad_workspace_bytes(_LOSS_GRAD_ARGS.pack(*head, 0, 0, 0))
+    need = _loss_grad_need(*sizes, _aligned_as(gx.data_ptr()) if dx else 0, _aligned_as(gw.data_ptr()) if dW else 0, bias is not None)
     work = _workspace(need, x)
     _check(lib.ripple_loss_rows_grad(_LOSS_GRAD_ARGS.pack(*head, _or_null(work), max(need, 0), _stream(index))))
     return gx, gw, gb
