@@ -996,7 +996,7 @@ template <typename T, bool GRAD>
 __global__ void __launch_bounds__(FL_THREADS, 1) k_loss_few(const __grid_constant__ FewParams p) {
     pdl_enter();
     extern __shared__ __align__(16) float few[];
-    const int pitch = few_pitch(p.n), warp = threadIdx.x >> 5, lane = lane_id();
+    const int pitch = GRAD ? few_pitch(p.n) : p.n, warp = threadIdx.x >> 5, lane = lane_id();       // (the loss has classes as lanes alone)
     const int cols = (p.n + 31) / 32, shares = FL_WARPS / cols, each = (p.k + shares - 1) / shares;      // 32-class blocks; parts of k
     float* const xs = few;                                // k x FL_ROWS
     float* const gs = xs + FL_ROWS * p.k;                 // classes x FL_ROWS: logits, then g
@@ -1004,8 +1004,24 @@ __global__ void __launch_bounds__(FL_THREADS, 1) k_loss_few(const __grid_constan
     float* const ws = sums + FL_WARPS * FL_ROWS * 32;     // k x pitch
     const T* const x = static_cast<const T*>(p.x);
     auto copy = [](float* to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(to)), "l"(from) : "memory"); };
-    {
-        const T* const W = static_cast<const T*>(p.W);
+    const T* const W = static_cast<const T*>(p.W);
+    if (pitch == p.n && p.ld_w == p.n && (reinterpret_cast<uintptr_t>(W) & 15) == 0) {
+        // W lies in memory as it will here: 16 bytes at a time (1000 fp32 rows, 602 -> 41, loss and gradient: 40 us by single entries, 37 so)
+        constexpr int E = 16 / sizeof(T);
+        const int all = p.k * p.n;
+#pragma unroll 8
+        for (int i = threadIdx.x * E; i + E <= all; i += FL_THREADS * E) {
+            if constexpr (sizeof(T) == 4) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(ws + i)), "l"(W + i) : "memory");
+            } else {
+                const Piece<T, 8> v = *reinterpret_cast<const Piece<T, 8>*>(W + i);
+#pragma unroll
+                for (int h = 0; h < 8; h += 4)
+                    *reinterpret_cast<float4*>(ws + i + h) = make_float4(to_f32(v.v[h]), to_f32(v.v[h + 1]), to_f32(v.v[h + 2]), to_f32(v.v[h + 3]));
+            }
+        }
+        for (int i = all / E * E + threadIdx.x; i < all; i += FL_THREADS) ws[i] = to_f32(W[i]);
+    } else {
         constexpr int U = 16;            // rows that are on their way (fp32: all)
         const int c = warp % cols * 32 + lane;
         if (c < p.n) {
@@ -1183,12 +1199,14 @@ __global__ void __launch_bounds__(FL_THREADS) k_loss_few_weights(const __grid_co
     }
 }
 
-// Rows up to which calls of small heads take this form: a round of eight rows on every SM, fp32 of up to 64 classes two.  Both sides, us on the device for
-// the loss and its gradient, this form / tensor cores: fp32 602 -> 41, 1000 rows 12 + 25 / 18 + 50, 2000 rows 18 + 42 / 19 + 53, 4000 rows 29 + 75 / 21 + 65;
-// 256 -> 150, 1000 rows 13 + 28 / 16 + 44, 2000 rows 20 + 49 / 16 + 45; bf16 602 -> 41, 1000 rows 12 + 26 / 12 + 32, 2000 rows 18 + 42 / 13 + 34.
+// Rounds of eight rows on every SM up to which calls of small heads take this form.  Both sides, us on the device for the loss and its gradient, this form / tensor
+// cores.  fp32 602 -> 41: 1184 rows (a round) 9 + 26 / 23 + 58, 3552 rows 21 + 60 / 23 + 61; 256 -> 47: 3552 rows 14 + 34 / 13 + 42; 256 -> 150: 1184 rows
+// 9 + 34 / 14 + 49, 2368 rows 16 + 54 / 15 + 49.  bf16 256 -> 47: 2368 rows 10 + 24 / 9 + 34, 3552 rows 13 + 33 / 9 + 35; 602 -> 41: 1184 rows 9 + 26 / 13 + 30, 2368 rows
+// 14 + 42 / 13 + 33; 64 -> 500: 1184 rows 10 + 29 / 10 + 36, 2368 rows 18 + 48 / 10 + 37.
 constexpr int FL_ROUND = FL_ROWS * 2 * LS_PAIRS;
 static bool few_form(int type, int64_t rows, int k, int n) {
-    return rows <= (type == RIPPLE_TYPE_F32 && n <= 64 ? 2 * FL_ROUND : FL_ROUND) && n <= 32 * FL_WARPS && few_bytes(k, n) <= FL_BYTES;
+    const int rounds = n > 64 ? 1 : type == RIPPLE_TYPE_F32 ? 3 : k <= 256 ? 2 : 1;
+    return rows <= rounds * FL_ROUND && n <= 32 * FL_WARPS && few_bytes(k, n) <= FL_BYTES;
 }
 // Whether one block forms dW too (1 row, 128 -> 40: 8.6 us for the gradient, 9.5 with a launch more; 256 -> 47: 13.4 and 11.7).
 __host__ __device__ inline bool few_at_once(int rows, int k, int n) { return rows <= FL_ROWS && k * n <= 8192; }
