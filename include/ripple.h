@@ -332,7 +332,7 @@ ripple_status ripple_get_stats(ripple_ctx* ctx, ripple_stats* out);
 ripple_status ripple_set_timing(ripple_ctx* ctx, int32_t on);
 
 /* Text of the last error on ctx (if ctx is NULL, of this thread's last failed call without a context: ripple_create and
- * the calls of requests). */
+ * the calls of requests and of training). */
 const char* ripple_last_error(ripple_ctx* ctx);
 
 void ripple_destroy(ripple_ctx* ctx);
@@ -476,7 +476,7 @@ int64_t ripple_project_workspace_bytes(const ripple_project_rows_args* args);
 /* rows = 0 is valid.  args: HOST. */
 ripple_status ripple_project_rows(const ripple_project_rows_args* args);
 
-/* Waits for the device and tells whether a bounded device-side wait of a call of requests gave up since the last query
+/* Waits for the device and tells whether a bounded device-side wait of a call of requests or of training gave up since the last query
  * (TIMEOUT, once: the results of those calls are not to be used).  The calls themselves return before their kernels have run, so
  * nothing else tells.  (Diagnostic: with RIPPLE_DEBUG_TC_WITHHOLD=1 in the environment, read by every call, waits run out after a
  * second or so.) */

@@ -416,7 +416,7 @@ def project_rows(x, projection: Projection, bank: Optional[AdapterBank] = None, 
 
 def check_requests(device=None) -> None:
     """Waits for the device; raises RippleError (ERR_TIMEOUT) if a bounded device-side wait of a call (project_rows, a RequestHead,
-    Ripple.answer) gave up since the last check: the results since then are not to be used.  No other call tells."""
+    Ripple.answer; of train.py the losses) gave up since the last check: the results since then are not to be used.  No other call tells."""
     index = torch.cuda.current_device() if device is None else torch.device(device).index
     _check(_ripple.load_library().ripple_request_status(-1 if index is None else index))
 

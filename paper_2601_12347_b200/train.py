@@ -15,7 +15,7 @@ under torch.no_grad() or with detached tensors).  As with requests everything ru
 necessarily the current device) and returns once it is launched; calls can be captured into CUDA graphs; outputs and scratch come from PyTorch's
 allocator, so every call and every captured graph has its own.  Sums are fp32 and formed in a fixed order: the same call gives the same
 bits.  Rows are fp32, bf16 or fp16.  Padding (ids or labels outside their range, -1 by custom) gives rows of zeros and adds nothing to
-any gradient, whatever its rows hold.
+any gradient, whatever its rows hold.  Device-side waits of the losses are bounded; `serve.check_requests` tells whether one gave up.
 """
 from __future__ import annotations
 
