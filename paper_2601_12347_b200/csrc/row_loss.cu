@@ -168,17 +168,13 @@ __device__ __forceinline__ float grad_scale(const RowControl* control, float sca
     return ldexpf(1.f, max(-126, min(126, 15 - e)));
 }
 
-// Two fp32 operations in one instruction: (a, b) += (c, d), (a, b) *= (c, d), (a, b) = (a, b) (c, c) + (d, d).  (A warp's block of 32 columns of g took 564 instructions,
+// Two fp32 operations in one instruction: (a, b) += (c, d), (a, b) *= (c, d).  (A warp's block of 32 columns of g took 564 instructions,
 // a tile 4500 cycles of issue slots beside 4096 of products at k = 512.)
 __device__ __forceinline__ void add2(float& a, float& b, float c, float d) {
     asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(c), "f"(d));
 }
 __device__ __forceinline__ void mul2(float& a, float& b, float c, float d) {
     asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(c), "f"(d));
-}
-__device__ __forceinline__ void fma2(float& a, float& b, float c, float d) {
-    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
-        : "+f"(a), "+f"(b) : "f"(c), "f"(d));
 }
 
 // Sums over the warp's rows of 32 columns: lane c has the sum of v[c].
@@ -591,12 +587,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
 #pragma unroll
                     for (int e = 0; e < 32; ++e) high[e & 3] = fmaxf(high[e & 3], y[e]);
                     const float most = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3]));
-                    const float base = most == -INFINITY ? 0.f : most * LOG2E;
-                    sum *= exp2_of(top * LOG2E - base);
+                    // (subtracted first: the largest logit adds exactly one, so that lse is no smaller than any logit and no loss negative)
+                    const float base = most == -INFINITY ? 0.f : most;
+                    sum *= exp2_of((top - base) * LOG2E);
                     float more[4] = {};
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
-                        fma2(y[e], y[e + 1], LOG2E, -base);
+                        add2(y[e], y[e + 1], -base, -base);
+                        mul2(y[e], y[e + 1], LOG2E, LOG2E);
                         add2(more[e & 2], more[(e & 2) + 1], exp2_of(y[e]), exp2_of(y[e + 1]));
                     }
                     sum += (more[0] + more[1]) + (more[2] + more[3]);

@@ -1,0 +1,50 @@
+"""The operators that train a head (train.py) where they can go wrong beside what test_gpu_train.py asks of them."""
+import pytest
+import torch
+
+from paper_2601_12347_b200 import train
+
+import test_gpu_train as T
+
+pytestmark = pytest.mark.gpu
+env = T.env     # skips without a device, builds the library
+
+U32, F64, DTYPES = T.U32, T.F64, T.DTYPES
+gen, rnd, near = T.gen, T.rnd, T.near
+
+
+@pytest.fixture(autouse=True)
+def _device(env):
+    pass
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows,N", [(60, 40), (5000, 40), (5000, 700)])
+def test_no_loss_is_negative(dtype, rows, N):
+    """The label's logit stands 10 to 100 above the rest, all of which are zero (all exact): the sum of exponentials is 1 and at most 0.04 more, passes through
+    32 additions at most (blocks of columns of a thread, groups, tiles), and its logarithm goes to the largest logit in one addition."""
+    g = gen(rows + N)
+    x, W = torch.zeros(rows, 32, dtype=DTYPES[dtype], device="cuda"), torch.zeros(32, N, dtype=DTYPES[dtype], device="cuda")
+    x[:, 0] = (10 + 90 * torch.rand(rows, generator=g, device="cuda")).to(DTYPES[dtype])
+    W[0, 3] = 1
+    labels = torch.full((rows,), 3, dtype=torch.int32, device="cuda")
+    loss, lse = train.loss_rows(x, W, labels)
+    assert (loss >= 0).all()
+    z = x[:, 0].to(F64)
+    want = torch.log1p((N - 1) * torch.exp(-z))
+    assert float(want.max()) < 0.04
+    unit = 2.0 ** (torch.floor(torch.log2(z + want)) - 23)        # of fp32 at lse
+    assert ((lse.to(F64) - z - want).abs() <= unit / 2 + 32 * U32).all()
+    assert ((loss.to(F64) - want).abs() <= unit / 2 + 32 * U32).all()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows", [300, 6000])
+def test_no_class_of_a_row_has_a_negative_loss(dtype, rows):
+    """lse is no smaller than any logit, as the call itself forms them: rows with logits of a few and of hundreds, every tenth class as the label."""
+    g = gen(rows)
+    q = T.problem(g, rows, 40, 300, DTYPES[dtype], padding=0)
+    q["x"] = q["x"] * (1 + 20 * torch.rand(rows, 1, generator=g, device="cuda")).to(q["x"].dtype)
+    for c in range(0, 300, 10):
+        q["labels"][:] = c
+        assert (train.loss_rows(**q)[0] >= 0).all()
