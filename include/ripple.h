@@ -559,12 +559,29 @@ typedef struct {
 int64_t ripple_norm_rows_grad_workspace_bytes(const ripple_norm_rows_grad_args* args);
 ripple_status ripple_norm_rows_grad(const ripple_norm_rows_grad_args* args);
 
+#define RIPPLE_MAX_LOSS_K 8192
+#define RIPPLE_MAX_CLASSES 16777216
+/* Which rows take part in a step: row i does if ids_i names a row of the table and labels_i a class.  live_ids_i = ids_i, live_rows_i = i and
+ * live_labels_i = labels_i then, else -1 in all three, so that every call of the step takes the same rows for padding (ripple_norm_rows_grad reads live_ids if it
+ * gathers rows of the table, live_rows if it reads what was gathered). */
+typedef struct {
+    int64_t rows;
+    int32_t classes;          /* 1 .. RIPPLE_MAX_CLASSES                                                         */
+    int32_t device;
+    const int32_t* ids;       /* `rows` entries                                                                  */
+    int64_t table_rows;
+    const int32_t* labels;    /* `rows` entries                                                                  */
+    int32_t* live_ids;        /* `rows` entries; NULL: not wanted                                                */
+    int32_t* live_rows;       /* the same                                                                        */
+    int32_t* live_labels;     /* the same                                                                        */
+    void* cuda_stream;
+} ripple_live_rows_args;
+ripple_status ripple_live_rows(const ripple_live_rows_args* args);
+
 /* Softmax cross entropy of a linear layer over n classes:  z = x W + bias,  lse_i = log sum_c exp z_ic,  loss_i = lse_i - z_i,label (0 for
  * labels outside [0, n)).  Neither call keeps the logits: they are formed tile by tile.  x, W, dx and dW share one type; products of fp32 are formed
  * on the tensor cores from three bf16 parts per operand.  A bias of minus infinity takes a class out; a row with no class left has loss 0,
  * lse minus infinity and no gradient. */
-#define RIPPLE_MAX_LOSS_K 8192
-#define RIPPLE_MAX_CLASSES 16777216
 typedef struct {
     int64_t rows;
     int32_t type;             /* ripple_type of x and W                                                          */

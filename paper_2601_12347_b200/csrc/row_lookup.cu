@@ -119,6 +119,18 @@ static cudaError_t launch_lookup(const LookupParams& p, int v, void* stream) {
     return launch_lookup<T, TO, 1>(p, stream);
 }
 
+// ---- rows of a step ----------------------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(LK_BLOCK) k_live_rows(const __grid_constant__ ripple_live_rows_args p) {
+    pdl_enter();
+    for (int64_t i = (int64_t)blockIdx.x * LK_BLOCK + threadIdx.x; i < p.rows; i += (int64_t)gridDim.x * LK_BLOCK) {
+        const int id = p.ids[i], label = p.labels[i];
+        const bool live = id >= 0 && id < p.table_rows && label >= 0 && label < p.classes;
+        if (p.live_ids) p.live_ids[i] = live ? id : -1;
+        if (p.live_rows) p.live_rows[i] = live ? (int)i : -1;
+        if (p.live_labels) p.live_labels[i] = live ? label : -1;
+    }
+}
+
 // ---- zeros ---------------------------------------------------------------------------------------------------------
 // The gradient's table is mostly zeros where ids are few; they are written by blocks behind those of the kernels that sort, which by themselves
 // would leave the memory idle (20 011 ids of a table of 232 965 rows, 602 fp32 columns: 272 us for lookup and gradient with the zeros first, 152 so).
@@ -808,6 +820,28 @@ extern "C" ripple_status ripple_lookup_rows(const ripple_lookup_rows_args* a) {
         default: e = launch_lookup<__half, __half>(p, v.v, a->cuda_stream); break;
     }
     return e == cudaSuccess ? RIPPLE_OK : launch_failed("lookup_rows launch", e);
+}
+#undef WHAT
+
+#define WHAT "live_rows"
+extern "C" ripple_status ripple_live_rows(const ripple_live_rows_args* a) {
+    if (!a) REFUSE("null arguments");
+    if (a->rows < 0 || a->rows > INT32_MAX || a->table_rows < 0) REFUSE("rows or rows of the table out of range");
+    if (a->classes < 1 || a->classes > RIPPLE_MAX_CLASSES) REFUSE("classes out of range");
+    if (!a->live_ids && !a->live_rows && !a->live_labels) REFUSE("no output");
+    if (a->rows > 0 && (!a->ids || !a->labels)) REFUSE("null ids or labels");
+    const int32_t* const all[] = {a->ids, a->labels, a->live_ids, a->live_rows, a->live_labels};
+    for (const int32_t* ptr : all)
+        if (reinterpret_cast<uintptr_t>(ptr) % 4) REFUSE("misaligned pointer");
+    for (int o = 2; o < 5; ++o)
+        for (int i = 0; i < o; ++i)
+            if (extents_meet({all[o], a->rows, 1, 1, 4}, {all[i], a->rows, 1, 1, 4})) REFUSE("an output overlaps another argument");
+    if (a->rows == 0) return RIPPLE_OK;
+    OnDevice on(a->device);
+    if (on.err != cudaSuccess) return launch_failed("cudaSetDevice", on.err);
+    const int64_t blocks = std::min<int64_t>((a->rows + LK_BLOCK - 1) / LK_BLOCK, (int64_t)sm_count() * 8);
+    const cudaError_t e = launch(k_live_rows, dim3((unsigned)blocks), LK_BLOCK, 0, a->cuda_stream, *a);
+    return e == cudaSuccess ? RIPPLE_OK : launch_failed("live_rows launch", e);
 }
 #undef WHAT
 

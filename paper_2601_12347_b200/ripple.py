@@ -39,7 +39,7 @@ EXPORTED = [
     "ripple_adapter_set", "ripple_project_workspace_bytes", "ripple_project_rows", "ripple_request_status",
     # training (train.py)
     "ripple_lookup_rows", "ripple_lookup_rows_grad", "ripple_lookup_rows_grad_workspace_bytes",
-    "ripple_norm_rows_grad", "ripple_norm_rows_grad_workspace_bytes",
+    "ripple_norm_rows_grad", "ripple_norm_rows_grad_workspace_bytes", "ripple_live_rows",
     "ripple_loss_rows", "ripple_loss_rows_workspace_bytes", "ripple_loss_rows_grad", "ripple_loss_rows_grad_workspace_bytes",
 ]
 # partitioned execution (include/ripple_part.h); the first 18 return a status
@@ -171,7 +171,7 @@ def load_library(path: Optional[str] = None):
     for name in ("ripple_project_layout_bytes", "ripple_adapter_bytes", "ripple_project_workspace_bytes"):
         getattr(lib, name).restype = i64
     # training: likewise by train.py
-    for name in ("ripple_lookup_rows", "ripple_lookup_rows_grad", "ripple_norm_rows_grad", "ripple_loss_rows", "ripple_loss_rows_grad"):
+    for name in ("ripple_lookup_rows", "ripple_lookup_rows_grad", "ripple_norm_rows_grad", "ripple_live_rows", "ripple_loss_rows", "ripple_loss_rows_grad"):
         getattr(lib, name).argtypes, getattr(lib, name).restype = [vp], i32
     for name in ("ripple_lookup_rows_grad_workspace_bytes", "ripple_norm_rows_grad_workspace_bytes", "ripple_loss_rows_workspace_bytes",
                  "ripple_loss_rows_grad_workspace_bytes"):

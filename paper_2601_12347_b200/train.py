@@ -34,7 +34,8 @@ from .serve import (NORM_LAYER, NORM_RMS, TYPE_F32, Norm, Projection, RequestHea
 _LOOKUP_ARGS = struct.Struct("=q4i QqqQ Qq fi Q")
 _LOOKUP_GRAD_ARGS = struct.Struct("=q4i QqQ Qqq fi Qq Q")
 _NORM_GRAD_ARGS = struct.Struct("=q4i Qq QqqQ Qq Qq QQ ifQQ Qq Q")
-# ripple_loss_rows_args, ripple_loss_rows_grad_args
+# ripple_live_rows_args, ripple_loss_rows_args, ripple_loss_rows_grad_args
+_LIVE_ARGS = struct.Struct("=q2i Qq QQQQ Q")
 _LOSS_ARGS = struct.Struct("=q4i QqQq QQQQ Qq Q")
 _LOSS_GRAD_ARGS = struct.Struct("=q4i QqQq QQQQ QqQqQ fi Qq Q")
 
@@ -295,6 +296,18 @@ class ClassHead:
         return {k: t for k, t in (("norm_weight", self.norm_weight), ("norm_bias", self.norm_bias), ("W", self.W), ("bias", self.bias), ("E", self.E))
                 if t is not None}
 
+    def _live(self, table, ids, labels):
+        """ids, rows and labels of the rows that take part; -1 in all three for the others."""
+        index = _device_of(table, "table")
+        table_rows = _matrix(table, "table", None, None, index)[2]
+        ids_ptr, rows = _ids(ids, index)
+        labels_ptr = _vector(labels, "labels", rows, torch.int32, index)
+        live = torch.empty((3, rows), dtype=torch.int32, device=table.device)
+        at = live.data_ptr()
+        _check(_ripple.load_library().ripple_live_rows(_LIVE_ARGS.pack(
+            rows, self.W.shape[1], index, ids_ptr, table_rows, labels_ptr, at, at + 4 * rows, at + 8 * rows, _stream(index))))
+        return live.unbind(0)
+
     def _normed(self, table, ids, kinds):
         """The rows before the norm (None: the table's own) and behind it."""
         if (kinds is None) != (self.E is None):
@@ -304,19 +317,23 @@ class ClassHead:
         return norm_rows(lookup_rows(self.E, kinds, self.scale), residual=table, ids=ids, pre=self.norm, clear_padding=True)
 
     def loss(self, table, ids, labels, kinds=None):
-        """The losses of the rows `ids` (int32) of `table` (fp32, or the head's type), fp32 [len(ids)]; 0 where the label (int32) is none."""
+        """The losses of the rows `ids` (int32) of `table` (fp32, or the head's type), fp32 [len(ids)]; 0 where the id names no row or the
+        label (int32) no class."""
+        ids, _, labels = self._live(table, ids, labels)
         return loss_rows(self._normed(table, ids, kinds)[1], self.W, labels, self.bias)[0]
 
     def step(self, table, ids, labels, kinds=None, dloss=1.0):
         """(loss, gradients): the losses as `loss` gives them, and by parameter the gradient of their sum weighted by dloss (a number, or
-        fp32 [len(ids)]).  A padding row has a negative id and a negative label.  The gradient of E has the table's type, the others their parameter's."""
+        fp32 [len(ids)]).  Rows whose id names no row of the table or whose label no class (-1 by custom) have loss 0 and add nothing to any gradient, whatever the
+        table and dloss hold there; kinds out of range are vertices without a learned row.  The gradient of E has the table's type, the others their parameter's."""
+        ids, rows, labels = self._live(table, ids, labels)
         s, n = self._normed(table, ids, kinds)
         loss, lse = loss_rows(n, self.W, labels, self.bias)
         dn, dW, dbias = loss_rows_grad(n, self.W, labels, lse, dloss, self.bias)
         if s is None:
             ds, dweight, dnorm_bias = norm_rows_grad(dn, table, self.norm, ids=ids, dx=False)
         else:
-            ds, dweight, dnorm_bias = norm_rows_grad(dn, s, self.norm)
+            ds, dweight, dnorm_bias = norm_rows_grad(dn, s, self.norm, ids=rows)
         got = {"norm_weight": dweight, "W": dW, "bias": dbias}
         if dnorm_bias is not None:
             got["norm_bias"] = dnorm_bias

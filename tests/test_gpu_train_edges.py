@@ -48,3 +48,38 @@ def test_no_class_of_a_row_has_a_negative_loss(dtype, rows):
     for c in range(0, 300, 10):
         q["labels"][:] = c
         assert (train.loss_rows(**q)[0] >= 0).all()
+
+
+@pytest.mark.parametrize("dtype,bound", [("fp32", 1e-5), ("bf16", 0.03)])
+@pytest.mark.parametrize("kinds", [0, 7])
+@pytest.mark.parametrize("norm,eps", [(T.serve.NORM_LAYER, 1e-5), (T.serve.NORM_RMS, 0.0)])
+@pytest.mark.parametrize("rows", [60, 5000])
+def test_rows_of_a_step_that_take_no_part(dtype, bound, kinds, norm, eps, rows):
+    """An id outside the table beside a label, a row that is not finite beside no label, both: nothing of them reaches a gradient.  Against the other rows alone in
+    64 bits; bounds as for whole steps (test_a_step_of_a_head)."""
+    g = gen(rows + kinds)
+    head = train.ClassHead(72, 33, kinds=kinds, kind=norm, eps=eps, scale=1.5, dtype=DTYPES[dtype], seed=3)
+    head.bias += 0.1 * rnd(g, 33)
+    table = rnd(g, 900, 72) + 0.3
+    table[100] = float("nan")
+    table[101, 5] = float("inf")
+    ids = torch.randint(102, 900, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    labels = torch.randint(0, 33, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    of, w = None, T.rows_of(g, rows)
+    if kinds:
+        head.E += rnd(g, kinds, 72, dtype=DTYPES[dtype], scale=0.3)
+        of = torch.randint(-1, kinds, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    ids[0::7], ids[1::7] = -1, 900
+    ids[2::7], labels[2::7] = 100, -1
+    ids[3::7], labels[3::7] = 101, 33
+    ids[4::7], labels[4::7] = -2 ** 31, 2 ** 31 - 1
+    live = torch.arange(rows, device="cuda") % 7 > 4
+    w[~live] = float("nan")
+    loss, grads = head.step(table, ids, labels, of, dloss=w)
+    assert torch.equal(loss, head.loss(table, ids, labels, of)) and (loss[~live] == 0).all()
+    want_loss, want = T.step_in_64_bits(head, table, ids[live], labels[live], of[live] if kinds else None, w[live].to(F64))
+    assert float((loss[live].to(F64) - want_loss).norm() / want_loss.norm()) < bound
+    for k in want:
+        assert float((grads[k].to(F64) - want[k]).norm() / want[k].norm()) < bound, k
+    for t in head.step(table, torch.full_like(ids, -1), labels, of)[1].values():
+        assert (t == 0).all()
