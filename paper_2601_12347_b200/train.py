@@ -253,7 +253,8 @@ def loss_rows_grad(x, W, labels, lse, dloss=1.0, bias=None, dx: bool = True, dW:
 
 
 class LiveNorm(Norm):
-    """A norm whose vectors are the caller's own tensors (fp32, CUDA): what is written into them is seen by the next call."""
+    """A norm whose vectors are the caller's own tensors (fp32, CUDA), `weight` and `bias`: what is written into them, and what is put in their
+    place, is seen by the next call."""
 
     def __init__(self, kind: int, weight, bias=None, eps: float = 1e-5):
         if kind not in (NORM_LAYER, NORM_RMS):
@@ -264,17 +265,31 @@ class LiveNorm(Norm):
         if weight.dim() != 1:
             raise ValueError(f"weight: one dimension expected, got {tuple(weight.shape)}")
         self.kind, self.eps, self.weight, self.bias = int(kind), float(eps), weight, bias
-        self.width, self.index = weight.shape[0], index
-        w = _vector(weight, "weight", self.width, torch.float32, index)
-        b = 0 if bias is None else _vector(bias, "bias", self.width, torch.float32, index)
-        self._keep(index, *(t for t in (weight, bias) if t is not None))
-        self._args = (self.kind, self.eps, w, b)
+        self._at = None
+        self._packed(weight.shape[0], index, _stream(index), "norm")
+
+    @property
+    def width(self):
+        return self.weight.shape[0]
+
+    @property
+    def index(self):
+        return self.weight.get_device()
+
+    def _packed(self, width: int, index: int, stream: int, name: str):
+        weight, bias = self.weight, self.bias
+        at = _vector(weight, name + ": weight", width, torch.float32, index), 0 if bias is None else _vector(bias, name + ": bias", width, torch.float32, index)
+        if at != self._at:           # (other memory than at the call before: no stream is known to read it yet)
+            self._keep(None, *(t for t in (weight, bias) if t is not None))
+            self._at = at
+        self._read_on(stream)
+        return self.kind, self.eps, *at
 
 
 class ClassHead:
     """Classes of vertices from their cached rows:  logits = norm(table[ids] + scale * E[kinds]) W + bias.
 
-    Parameters, CUDA tensors that an optimiser updates in place: `norm_weight`, `norm_bias` (fp32 [D]; no bias for NORM_RMS), `W` [D, N] of
+    Parameters, CUDA tensors that an optimiser updates in place or others of their shape and type take the place of: `norm_weight`, `norm_bias` (fp32 [D]; no bias for NORM_RMS), `W` [D, N] of
     `dtype`, `bias` (fp32 [N]), and, with `kinds` > 0, `E` [kinds, D] of `dtype`: learned rows of what a vertex is, beside what the graph's layers
     made of it.  W is drawn from N(0, 1 / D), E starts at zero."""
 
@@ -285,11 +300,12 @@ class ClassHead:
         g = torch.Generator(device=device).manual_seed(seed)
         self.W = (torch.randn(D, N, generator=g, device=device) * D ** -0.5).to(dtype)
         self.bias = torch.zeros(N, device=device)
-        self.norm_weight = torch.ones(D, device=device)
-        self.norm_bias = torch.zeros(D, device=device) if kind == NORM_LAYER else None
         self.E = torch.zeros(kinds, D, dtype=dtype, device=device) if kinds > 0 else None
         self.scale = float(scale)
-        self.norm = LiveNorm(kind, self.norm_weight, self.norm_bias, eps)
+        self.norm = LiveNorm(kind, torch.ones(D, device=device), torch.zeros(D, device=device) if kind == NORM_LAYER else None, eps)
+
+    norm_weight = property(lambda self: self.norm.weight, lambda self, t: setattr(self.norm, "weight", t))
+    norm_bias = property(lambda self: self.norm.bias, lambda self, t: setattr(self.norm, "bias", t))
 
     def parameters(self) -> Dict[str, torch.Tensor]:
         """The parameters by name, as the gradients are."""

@@ -83,3 +83,31 @@ def test_rows_of_a_step_that_take_no_part(dtype, bound, kinds, norm, eps, rows):
         assert float((grads[k].to(F64) - want[k]).norm() / want[k].norm()) < bound, k
     for t in head.step(table, torch.full_like(ids, -1), labels, of)[1].values():
         assert (t == 0).all()
+
+
+@pytest.mark.parametrize("how", ["data", "attribute", "norm"])
+def test_vectors_of_a_norm_that_are_put_in_place_of_others(how):
+    """The memory of a head's norm moves (an optimiser that flattens parameters, `head.norm_weight = ...`): the next step reads what is there now."""
+    g = gen(1)
+    table, ids, labels = rnd(g, 50, 40), torch.arange(50, dtype=torch.int32, device="cuda"), torch.arange(50, dtype=torch.int32, device="cuda") % 5
+    head, other = train.ClassHead(40, 5, seed=2), train.ClassHead(40, 5, seed=2)
+    head.step(table, ids, labels)
+    weight, bias = 1 + 0.3 * rnd(g, 40), 0.3 * rnd(g, 40)
+    other.norm_weight.copy_(weight), other.norm_bias.copy_(bias)
+    if how == "data":
+        head.norm_weight.data, head.norm_bias.data = weight, bias
+    elif how == "attribute":
+        head.norm_weight, head.norm_bias = weight, bias
+    else:
+        head.norm.weight, head.norm.bias = weight, bias
+    assert head.parameters()["norm_weight"].data_ptr() == weight.data_ptr()
+    (loss, grads), (want_loss, want) = head.step(table, ids, labels), other.step(table, ids, labels)
+    assert torch.equal(loss, want_loss) and all(torch.equal(grads[k], want[k]) for k in want)
+    for bad in (weight[:39], weight.double(), weight.cpu(), torch.cat([weight, weight])[::2]):
+        head.norm_weight = bad
+        with pytest.raises((TypeError, ValueError), match="weight"):
+            head.step(table, ids, labels)
+    head.norm_weight, head.norm_bias = weight, None
+    other.norm_bias = None
+    assert "norm_bias" not in head.step(table, ids, labels)[1]
+    assert torch.equal(head.loss(table, ids, labels), other.loss(table, ids, labels))
