@@ -31,12 +31,16 @@ cudaError_t take_loss_timeout(int* gave_up) {
 // of C: 32 KB per 64 entries of k and CTA, where a CTA by itself would bring 48 for the same products.  Operands come by TMA in either order, k along the rows of memory or across them; what lies outside a matrix arrives as zeros.
 constexpr int LS_ROWS = 256, LS_KC = 64;
 constexpr int LS_PAIRS = 74;             // of a B200 (for plans that are asked where no device is current, too)
-constexpr int LS_UNIT = 4;               // fp32: chunks (256 entries of k) whose large products share an accumulator
+enum { END_LSE, END_GRAD, END_OUT };
+// Chunks of k whose products share an accumulator, which then is handed over and summed in registers: the tensor core cuts what its additions lose, so sums of
+// terms of one sign come out too small, in proportion to their length (fp16, 100 000 entries: 6.5e-4, more than half a step of the result; here 2.7e-5 of
+// it at most).  fp32: of the large products.  Results in 16 bits: a 16th of half a step of theirs.
+__host__ __device__ constexpr int unit_of(int type, int end) { return type == RIPPLE_TYPE_F32 ? 4 : end != END_OUT ? 32 : type == RIPPLE_TYPE_F16 ? 64 : 512; }
 constexpr int LS_GROUP = 8;              // tiles of rows that are worked on side by side, so that B's tiles are read out of L2
 constexpr uint32_t LS_SPIN_LIMIT = 1u << 18;       // polls after which a wait gives up: about a second
 constexpr float LOG2E = 1.4426950408889634f;
 
-// MANY: fp32 over more than one unit of k, whose sums the epilogue carries in registers.  RAW: A is fp32 as the caller has it; warps fetch it and make its parts.
+// MANY: more than one unit of k, whose sums the epilogue carries in registers.  RAW: A is fp32 as the caller has it; warps fetch it and make its parts.
 template <int TYPE, bool MANY, bool RAW = false> struct LossShape {
     static constexpr int PARTS = TYPE == RIPPLE_TYPE_F32 ? 3 : 1;
     static constexpr int COLS = PARTS == 3 ? 128 : 256;
@@ -53,7 +57,6 @@ template <int TYPE, bool MANY, bool RAW = false> struct LossShape {
     static constexpr size_t BYTES = (size_t)STAGES * STAGE + BIAS + 1024;
 };
 
-enum { END_LSE, END_GRAD, END_OUT };
 constexpr int LS_CONTROL = 512;          // blocks of k_look_at_rows (where few rows have labels, it reads most of x)
 
 // What k_look_at_rows found, block by block.
@@ -218,7 +221,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
     constexpr bool SHARE = RAW;
     static_assert(!SHARE || (S::THREADS == 896 && 128 * 48 + 256 * 144 + 512 * 40 <= 896 * 72), "no more registers are shared out than there are");
     using T = typename Elem<TYPE == RIPPLE_TYPE_F16 ? RIPPLE_TYPE_F16 : RIPPLE_TYPE_BF16>::T;      // of the operands
-    constexpr int PARTS = S::PARTS, STAGES = S::STAGES, COLS = S::COLS, GROUPS = S::GROUPS, NB = COLS / (32 * GROUPS);      // NB: 32-column blocks of an epilogue warp
+    constexpr int PARTS = S::PARTS, STAGES = S::STAGES, COLS = S::COLS, GROUPS = S::GROUPS, NB = COLS / (32 * GROUPS), UNIT = unit_of(TYPE, END);      // NB: 32-column blocks of an epilogue warp
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[STAGES], empty[STAGES], made[RAW ? STAGES : 1], acc_full[2], acc_empty[2], drained;
     __shared__ uint32_t tmem_slot;
@@ -346,7 +349,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
                 int b = 0;
                 for (int c = first; c < last; ++c) {
                     const int in = c - first;
-                    const bool fresh = MANY ? in % LS_UNIT == 0 : in == 0;
+                    const bool fresh = MANY ? in % UNIT == 0 : in == 0;
                     if (fresh) {
                         b = sg & 1;
                         const int before = sg >> 1;
@@ -362,7 +365,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
                     tc_fence_after();
                     // (broadcast: operands that the compiler cannot see to be the warp's take ten times as long to issue)
                     const uint64_t at = (uint64_t)((uint32_t)__shfl_sync(FULL, s, 0) * (S::STAGE >> 4)), a = a0 + at, w = b0 + at;
-                    const bool done = c == last - 1 || (MANY && in % LS_UNIT == LS_UNIT - 1);
+                    const bool done = c == last - 1 || (MANY && in % UNIT == UNIT - 1);
                     if (lead) {
 #pragma unroll
                         for (int j = 0; j < LS_KC / 16; ++j) {
@@ -694,8 +697,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
                     }
                 }
             };
-            const int units = MANY ? (t.last - t.first + LS_UNIT - 1) / LS_UNIT : 1;
-            float carry[MANY ? NB : 1][32];          // fp32: of the units before the last
+            const int units = MANY ? (t.last - t.first + UNIT - 1) / UNIT : 1;
+            float carry[MANY ? NB : 1][32];          // of the units before the last
             for (int u = 0; u < units && ok; ++u, ++sg) {
                 const int b = sg & 1;
                 ok = mbar_wait_warp(&acc_full[b], (sg >> 1) & 1, LS_SPIN_LIMIT);
@@ -952,7 +955,10 @@ static int up_to(int64_t x, int to) { return (int)((x + to - 1) / to * to); }
 static int64_t aligned128(int64_t x) { return (x + 127) / 128 * 128; }
 static int parts_of(int type) { return type == RIPPLE_TYPE_F32 ? 3 : 1; }
 // column groups of a tile whose sums the loss keeps apart
-static int groups_of(int type) { return type == RIPPLE_TYPE_F32 ? LossShape<RIPPLE_TYPE_F32, true, true>::GROUPS : LossShape<RIPPLE_TYPE_BF16, false>::GROUPS; }
+static int groups_of(int type, int k) {
+    const bool many = (k + LS_KC - 1) / LS_KC > unit_of(type, END_LSE);
+    return type == RIPPLE_TYPE_F32 ? LossShape<RIPPLE_TYPE_F32, true, true>::GROUPS : many ? LossShape<RIPPLE_TYPE_BF16, true>::GROUPS : LossShape<RIPPLE_TYPE_BF16, false>::GROUPS;
+}
 static int cols_of(int type) { return type == RIPPLE_TYPE_F32 ? 128 : 256; }
 
 // Whether TMA can read a matrix where it lies.
@@ -1251,7 +1257,7 @@ static LossPlan plan_loss(const ripple_loss_rows_args& a) {
     Slots s;
     l.x = operand(s, a.type, a.x, a.ld_x, a.rows, a.k, false, true), l.w = operand(s, a.type, a.W, a.ld_w, a.k, a.n, false, false);
     const int cols = cols_of(a.type), tiles = (a.n + cols - 1) / cols;
-    const int64_t of_tile = groups_of(a.type) * std::max<int64_t>(a.rows, 1) * 8, at_once = std::min<int64_t>(tiles, std::max<int64_t>(1, LS_SUMS / of_tile));
+    const int64_t of_tile = groups_of(a.type, a.k) * std::max<int64_t>(a.rows, 1) * 8, at_once = std::min<int64_t>(tiles, std::max<int64_t>(1, LS_SUMS / of_tile));
     l.piece = (int)at_once * cols, l.pieces = (tiles + (int)at_once - 1) / (int)at_once;
     l.sums = s.take(at_once * of_tile), l.at_label = s.take(a.rows * 4);
     if (l.pieces > 1) l.running = s.take(a.rows * 8);
@@ -1373,9 +1379,7 @@ static cudaError_t launch_product(ProductParams p, const Matrix& a, const Matrix
     const int chunks = (p.k + LS_KC - 1) / LS_KC;
     constexpr bool RAW = X && TYPE == RIPPLE_TYPE_F32;
     p.split_chunks = (chunks + splits - 1) / splits, p.splits = (chunks + p.split_chunks - 1) / p.split_chunks;      // (none empty)
-    if constexpr (TYPE == RIPPLE_TYPE_F32) {
-        if (p.split_chunks > LS_UNIT) return launch_product<TYPE, A_ACROSS, B_ACROSS, END, true, RAW>(p, a, a_clean, b, stream);
-    }
+    if (p.split_chunks > unit_of(TYPE, END)) return launch_product<TYPE, A_ACROSS, B_ACROSS, END, true, RAW>(p, a, a_clean, b, stream);
     return launch_product<TYPE, A_ACROSS, B_ACROSS, END, false, RAW>(p, a, a_clean, b, stream);
 }
 
@@ -1415,7 +1419,7 @@ static cudaError_t run_loss(const ripple_loss_rows_args& a) {
         p.n = std::min(l.piece, a.n - c0), p.b_col0 = p.class0 = c0, p.bias = a.bias ? a.bias + c0 : nullptr;
         e = launch_product<TYPE, false, true, END_LSE, true>(p, x, nullptr, w, 1, a.cuda_stream);
         if (e != cudaSuccess) break;
-        const int parts = groups_of(a.type) * ((p.n + cols_of(a.type) - 1) / cols_of(a.type));
+        const int parts = groups_of(a.type, a.k) * ((p.n + cols_of(a.type) - 1) / cols_of(a.type));
         auto finish = [&](auto* kernel, int rows) {
             return launch(kernel, dim3((unsigned)((a.rows + rows - 1) / rows)), 512, 0, a.cuda_stream, (const float2*)p.sums, parts, a.rows, (const float*)p.at_label, a.labels, a.n, a.loss,
                           a.lse, l.pieces > 1 ? reinterpret_cast<float2*>(work + l.running) : nullptr, piece == 0 ? 1 : 0, piece == l.pieces - 1 ? 1 : 0);

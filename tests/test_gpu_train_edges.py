@@ -111,3 +111,44 @@ def test_vectors_of_a_norm_that_are_put_in_place_of_others(how):
     other.norm_bias = None
     assert "norm_bias" not in head.step(table, ids, labels)[1]
     assert torch.equal(head.loss(table, ids, labels), other.loss(table, ids, labels))
+
+
+# A step of a 16-bit product (16 entries of k) loses at most 2^-22 of the running sum; an accumulator takes 2048 entries of z, 4096 (fp16) or 32 768 (bf16) of dx and dW.
+LOST = {"fp16": 256 * 2.0 ** -22, "bf16": 2048 * 2.0 ** -22}
+
+
+@pytest.mark.parametrize("dtype", list(LOST))
+def test_long_sums_of_one_sign(dtype):
+    """Gradients summed over 100 000 rows and 65 536 classes, in as many tiles as pairs of SMs or more (no split over k), all terms of one sign and exact in their
+    type: what is lost does not grow with the length."""
+    g = gen(2)
+    t = DTYPES[dtype]
+    # W = 0: every class has p = 1 / 2048
+    x, W = (0.5 + torch.rand(100_000, 2560, generator=g, device="cuda")).to(t), torch.zeros(2560, 2048, dtype=t, device="cuda")
+    labels = torch.zeros(100_000, dtype=torch.int32, device="cuda")
+    dW = train.loss_rows_grad(x, W, labels, train.loss_rows(x, W, labels)[1], dx=False)[1]
+    want = x.sum(0, dtype=F64) / 2048
+    near(dW[:, 1:], want[:, None].expand(-1, 2047), (LOST[dtype] + 64 * U32) * want[:, None])
+    # x = 0: p = 1 / 65 536; the label's column of W is zero
+    x, W = torch.zeros(2560, 2048, dtype=t, device="cuda"), (0.5 + torch.rand(2048, 65_536, generator=g, device="cuda")).to(t)
+    W[:, 0] = 0
+    labels = labels[:2560]
+    dx = train.loss_rows_grad(x, W, labels, train.loss_rows(x, W, labels)[1], dW=False)[0]
+    want = W.sum(1, dtype=F64) / 65_536
+    near(dx, want.expand(2560, -1), (LOST[dtype] + 64 * U32) * want)
+    T.serve.check_requests()
+
+
+@pytest.mark.parametrize("dtype", list(LOST))
+@pytest.mark.parametrize("K", [1024, 2048, 2049, 5000, 8192])
+def test_long_logits_of_one_sign(dtype, K):
+    g = gen(K)
+    x, W = (0.5 + torch.rand(300, K, generator=g, device="cuda")).to(DTYPES[dtype]), ((0.5 + torch.rand(K, 257, generator=g, device="cuda")) * 20 / K).to(DTYPES[dtype])
+    labels = torch.arange(300, dtype=torch.int32, device="cuda") % 257
+    z = x.to(F64) @ W.to(F64)
+    loss, lse = train.loss_rows(x, W, labels)
+    tol = (min(K, 2048) / 16 * 2.0 ** -22 + 32 * U32) * z.amax(1)      # (20 to 30: a further 32 u32 for exponents and sums)
+    near(lse, torch.logsumexp(z, 1), tol)
+    near(loss, torch.logsumexp(z, 1) - z.gather(1, labels.long()[:, None])[:, 0], 2 * tol)
+    T.check_loss(x, W, labels, dloss=T.rows_of(g, 300))
+    T.serve.check_requests()
