@@ -61,7 +61,7 @@ constexpr int LS_CONTROL = 512;          // blocks of k_look_at_rows (where few 
 
 // What k_look_at_rows found, block by block.
 struct RowControl {
-    float most[LS_CONTROL];              // largest finite |dloss|
+    float most[LS_CONTROL], least[LS_CONTROL];      // largest and smallest |dloss| that is finite and not zero (0, infinity: none)
     int32_t odd[LS_CONTROL];             // a row without a label holds something that is not finite
 };
 
@@ -92,6 +92,7 @@ struct alignas(64) ProductParams {
     int64_t ld_out, split_stride;        // fp32: elements between the splits' results
     int out_f32, add_to_out;
     int unscale;                         // g was scaled: see grad_scale
+    int by_row;                          // fp16, GRAD: runs only where weights_differ, and scales every row by itself; OUT: g was formed so, there
     const int32_t* dead_rows;            // labels, where rows without one are zeros; else null
     int withhold;                        // diagnostic: no first accumulator counts as filled
 };
@@ -157,18 +158,31 @@ __device__ __forceinline__ void three_parts(float x, __nv_bfloat16 (&h)[3]) {
     h[2] = __float2bfloat16_rn(left - __bfloat162float(h[1]));
 }
 
-// fp16: g is scaled by a power of two that brings the largest |dloss| to 2^14 .. 2^15, where probabilities down to 2^-29 of it keep all
-// bits; the results are scaled back.  (bf16 and its parts have fp32's range.)
+// The power of two that brings a weight to 2^14 .. 2^15.
+__device__ __forceinline__ float scale_of(float weight) {
+    weight = fabsf(weight);
+    if (!(weight > 0.f) || !isfinite(weight)) return 1.f;
+    int e;
+    frexpf(weight, &e);          // weight <= 2^e
+    return ldexpf(1.f, max(-126, min(126, 15 - e)));
+}
+// fp16: g is scaled by the power of two of the largest |dloss|, so that probabilities down to 2^-29 of it keep all bits, and the results are scaled back.  (bf16
+// and its parts have fp32's range.)
 __device__ __forceinline__ float grad_scale(const RowControl* control, float scale) {
     float most = 0.f;
     for (int i = lane_id(); i < LS_CONTROL; i += 32) most = fmaxf(most, control->most[i]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(FULL, most, o));
-    most *= fabsf(scale);
-    if (!(most > 0.f) || !isfinite(most)) return 1.f;
-    int e;
-    frexpf(most, &e);            // most <= 2^e
-    return ldexpf(1.f, max(-126, min(126, 15 - e)));
+    return scale_of(most * scale);
+}
+// Rows whose weight is far below the largest would have few bits left of their small probabilities (2^-24 of it: none of 2^-16), which dW does not notice and their own rows
+// of dx do.  Where weights lie more than 2^8 apart, g is formed a second time for dx, every row scaled by itself.
+__device__ __forceinline__ bool weights_differ(const RowControl* control) {
+    float most = 0.f, least = INFINITY;
+    for (int i = lane_id(); i < LS_CONTROL; i += 32) most = fmaxf(most, control->most[i]), least = fminf(least, control->least[i]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(FULL, most, o)), least = fminf(least, __shfl_xor_sync(FULL, least, o));
+    return least < most * (1.f / 256);
 }
 
 // Two fp32 operations in one instruction: (a, b) += (c, d), (a, b) *= (c, d).  (A warp's block of 32 columns of g took 564 instructions,
@@ -222,6 +236,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
     static_assert(!SHARE || (S::THREADS == 896 && 128 * 48 + 256 * 144 + 512 * 40 <= 896 * 72), "no more registers are shared out than there are");
     using T = typename Elem<TYPE == RIPPLE_TYPE_F16 ? RIPPLE_TYPE_F16 : RIPPLE_TYPE_BF16>::T;      // of the operands
     constexpr int PARTS = S::PARTS, STAGES = S::STAGES, COLS = S::COLS, GROUPS = S::GROUPS, NB = COLS / (32 * GROUPS), UNIT = unit_of(TYPE, END);      // NB: 32-column blocks of an epilogue warp
+    if constexpr (TYPE == RIPPLE_TYPE_F16 && END == END_GRAD) {
+        if (p.by_row) {
+            pdl_enter();
+            if (!weights_differ(p.control)) return;
+        }
+    }
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[STAGES], empty[STAGES], made[RAW ? STAGES : 1], acc_full[2], acc_empty[2], drained;
     __shared__ uint32_t tmem_slot;
@@ -526,9 +546,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
         const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16);
         float* const bias = reinterpret_cast<float*>(ring + STAGES * S::STAGE) + (warp - S::FIRST) * 32 * NB;
         float factor = 1.f, unfactor = 1.f;      // GRAD: of g, and of its sums; OUT: of the result
+        bool by_row = false;
         if (TYPE == RIPPLE_TYPE_F16 && p.control) {
-            if (END == END_GRAD) factor = grad_scale(p.control, p.scale), unfactor = 1.f / factor;
-            if (END == END_OUT && p.unscale) factor = 1.f / grad_scale(p.control, p.scale);
+            if (END == END_GRAD) factor = grad_scale(p.control, p.scale), unfactor = 1.f / factor, by_row = p.by_row;
+            if (END == END_OUT && p.unscale) factor = 1.f / grad_scale(p.control, p.scale), by_row = p.by_row && weights_differ(p.control);
         }
         const uint32_t release = in_leader(&acc_empty[0]);
         bool ok = true;
@@ -543,8 +564,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
             if (row < p.m && labels) a.label = labels[row];
             if constexpr (END == END_GRAD) {
                 if (row < p.m) a.lse = p.lse[row];
-                if (row < p.m && p.dloss) a.dloss = p.dloss[row];
             }
+            if (END == END_GRAD || (END == END_OUT && by_row)) if (row < p.m && p.dloss) a.dloss = p.dloss[row];
             if constexpr (END != END_OUT) {
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
@@ -561,6 +582,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
             const int row = row_of_tile(t), col0 = t.col * COLS;
             const bool in_rows = row < p.m, labelled = asked.label >= 0 && asked.label < p.classes;
             bool live = END == END_OUT ? in_rows && (!p.dead_rows || labelled) : labelled;
+            if (TYPE == RIPPLE_TYPE_F16 && by_row) {
+                factor = scale_of(p.scale * asked.dloss);
+                if (END == END_OUT) factor = 1.f / factor;
+            }
             const float lse = asked.lse, weight = p.scale * asked.dloss * (END == END_GRAD ? factor : 1.f);
             float top = -INFINITY, sum = 0.f;
             if (END == END_GRAD) live = live && lse != -INFINITY;
@@ -816,12 +841,12 @@ __global__ void __launch_bounds__(256) k_operand(const __grid_constant__ Operand
     }
 }
 
-// What the gradient has to know of all rows: the largest dloss (fp16), and whether a row without a label holds something that is not finite (x read in place).
+// What the gradient has to know of all rows: the largest and the smallest dloss (fp16), and whether a row without a label holds something that is not finite (x read in place).
 template <typename T>
 __global__ void __launch_bounds__(256) k_look_at_rows(const T* x, int64_t ld_x, int k, const int32_t* labels, const float* dloss, int64_t rows, int classes, RowControl* control) {
     pdl_enter();
-    __shared__ float scratch[8];
-    float most = 0.f;
+    __shared__ float2 scratch[8];
+    float most = 0.f, least = INFINITY;
     bool odd = false;
     for (int64_t r0 = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * 32; r0 < rows; r0 += (int64_t)LS_CONTROL * 256) {
         const int64_t row = r0 + lane_id();
@@ -829,6 +854,7 @@ __global__ void __launch_bounds__(256) k_look_at_rows(const T* x, int64_t ld_x, 
         if (live) {
             const float w = dloss ? fabsf(dloss[row]) : 1.f;
             if (isfinite(w)) most = fmaxf(most, w);
+            if (w > 0.f) least = fminf(least, w);
         }
         for (uint32_t left = x ? __ballot_sync(FULL, row < rows && !live) : 0; left; left &= left - 1) {
             const T* const from = x + (r0 + __ffs(left) - 1) * ld_x;
@@ -837,12 +863,12 @@ __global__ void __launch_bounds__(256) k_look_at_rows(const T* x, int64_t ld_x, 
         }
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(FULL, most, o));
-    if (lane_id() == 0) scratch[threadIdx.x >> 5] = most;
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(FULL, most, o)), least = fminf(least, __shfl_xor_sync(FULL, least, o));
+    if (lane_id() == 0) scratch[threadIdx.x >> 5] = make_float2(most, least);
     const int any = __syncthreads_or(odd);
     if (threadIdx.x == 0) {
-        for (int w = 1; w < 8; ++w) most = fmaxf(most, scratch[w]);
-        control->most[blockIdx.x] = most, control->odd[blockIdx.x] = any;
+        for (int w = 1; w < 8; ++w) most = fmaxf(most, scratch[w].x), least = fminf(least, scratch[w].y);
+        control->most[blockIdx.x] = most, control->least[blockIdx.x] = least, control->odd[blockIdx.x] = any;
     }
 }
 
@@ -1485,15 +1511,6 @@ static cudaError_t run_loss_grad(const ripple_loss_rows_grad_args& a) {
         const Matrix g{work + l.g, a.rows, classes, l.ld_g, l.g_plane, parts_of(TYPE)};
         ProductParams o = {};
         o.unscale = TYPE == RIPPLE_TYPE_F16, o.scale = a.scale, o.classes = a.n;
-        if (a.dx) {
-            ProductParams d = o;
-            d.m = (int)a.rows, d.n = a.k, d.k = classes, d.b_k0 = c0, d.control = p.control, d.dead_rows = a.labels;
-            if (l.dx < 0) d.out = a.dx, d.ld_out = a.ld_dx, d.out_f32 = TYPE == RIPPLE_TYPE_F32;
-            else d.out = work + l.dx, d.ld_out = l.ld_dx, d.split_stride = a.rows * l.ld_dx, d.out_f32 = 1, d.add_to_out = c0 > 0;
-            // (the last piece may be too short for all parts: the last of them keep what they have)
-            e = launch_product<TYPE, false, false, END_OUT, false>(d, g, &g, w, l.dx_splits, stream);
-            if (e != cudaSuccess) return e;
-        }
         if (a.dW) {
             ProductParams d = o;
             d.m = a.k, d.n = classes, d.k = (int)a.rows, d.raw_labels = a.labels;
@@ -1502,6 +1519,21 @@ static cudaError_t run_loss_grad(const ripple_loss_rows_grad_args& a) {
             else d.out = work + l.dw, d.ld_out = l.ld_dw, d.split_stride = a.k * l.ld_dw, d.out_f32 = 1;
             e = launch_product<TYPE, true, true, END_OUT, true>(d, x, &x_clean, g, l.dw_splits, stream);
             if (e == cudaSuccess && l.dw >= 0) e = join_parts<T>(static_cast<const float*>(d.out), l.dw_splits, d.split_stride, d.ld_out, static_cast<T*>(a.dW) + c0, a.ld_dw, a.k, classes, stream);
+            if (e != cudaSuccess) return e;
+        }
+        if (a.dx) {
+            const bool by_row = TYPE == RIPPLE_TYPE_F16 && a.dloss;
+            if (by_row) {
+                p.by_row = 1, p.g_sums = nullptr;
+                e = launch_product<TYPE, false, true, END_GRAD, true>(p, x, same, w, 1, stream);
+                if (e != cudaSuccess) return e;
+            }
+            ProductParams d = o;
+            d.m = (int)a.rows, d.n = a.k, d.k = classes, d.b_k0 = c0, d.control = p.control, d.dead_rows = a.labels, d.dloss = a.dloss, d.by_row = by_row;
+            if (l.dx < 0) d.out = a.dx, d.ld_out = a.ld_dx, d.out_f32 = TYPE == RIPPLE_TYPE_F32;
+            else d.out = work + l.dx, d.ld_out = l.ld_dx, d.split_stride = a.rows * l.ld_dx, d.out_f32 = 1, d.add_to_out = c0 > 0;
+            // (the last piece may be too short for all parts: the last of them keep what they have)
+            e = launch_product<TYPE, false, false, END_OUT, false>(d, g, &g, w, l.dx_splits, stream);
             if (e != cudaSuccess) return e;
         }
     }

@@ -152,3 +152,29 @@ def test_long_logits_of_one_sign(dtype, K):
     near(loss, torch.logsumexp(z, 1) - z.gather(1, labels.long()[:, None])[:, 0], 2 * tol)
     T.check_loss(x, W, labels, dloss=T.rows_of(g, 300))
     T.serve.check_requests()
+
+
+@pytest.mark.parametrize("apart", [1, 200, 300, 2 ** 12, 2 ** 24])
+@pytest.mark.parametrize("rows,K,N", [(300, 64, 40_000), (2000, 24, 150_000)])
+def test_fp16_rows_of_small_weight_keep_their_gradients(rows, K, N, apart):
+    """Weights that lie `apart` in one call (from 2^14 down, all results in fp16's range), probabilities of about 1 / N: each row of dx is as good as one of a call
+    of its own.  g is off by half a step (a row's largest to 2^14 at least, or 2^8 less: multiples of 2^-24 are exact) and what z and lse are off."""
+    g = gen(N)
+    x, W = rnd(g, rows, K, scale=0.05, dtype=torch.float16), (0.5 + torch.rand(K, N, generator=g, device="cuda")).half()
+    labels = torch.randint(-1, N, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    w = 2.0 ** 14 * torch.where(torch.arange(rows, device="cuda") % 3 == 0, 1.0, 1.0 / apart) * (0.5 + 0.4 * torch.rand(rows, generator=g, device="cuda"))
+    w[5], w[6] = 0, -w[6]
+    loss, lse = train.loss_rows(x, W, labels)
+    dx, dW, _ = train.loss_rows_grad(x, W, labels, lse, w)
+    for only in (train.loss_rows_grad(x, W, labels, lse, w, dW=False)[0], train.loss_rows_grad(x, W, labels, lse, w / 2, dW=False)[0] * 2):
+        near(only, dx.to(F64), 2.0 ** -24)                  # (powers of two; a half of what lies below 2^-14 loses a bit)
+    live = (labels >= 0).to(F64)[:, None]
+    W64 = W.to(F64)
+    p = torch.softmax(x.to(F64) @ W64, 1)
+    rel = 48 * 2.0 ** -23 * (x.to(F64).abs() @ W64.abs()).amax(1, keepdim=True) + (N / 128 + 256) * U32 + 2.0 ** -11
+    e = p.scatter_add(1, labels.clamp(min=0).long()[:, None], -torch.ones_like(live)) * live
+    g_tol = (p * rel + e.abs() * 2.0 ** -11 + 2.0 ** -31) * live
+    k = w.to(F64)[:, None]
+    near(dx, e @ W64.T * k, (g_tol @ W64.T + (N / 16 + 48) * 2.0 ** -23 * (e.abs() @ W64.T)) * k.abs())
+    assert float(((dW.to(F64) - x.to(F64).T @ (e * k)).norm() / dW.to(F64).norm())) < 1e-3
+    T.serve.check_requests()
