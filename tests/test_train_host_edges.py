@@ -41,3 +41,37 @@ def test_live_rows_refuses(lib, wrong):
 def test_no_rows_are_fine(lib):
     assert lib.ripple_live_rows(live_args(rows=0, ids=0, labels=0)) == ripple.OK
     assert lib.ripple_live_rows(None) == ripple.ERR_INVALID_ARG
+
+
+def kernels_of(text):
+    """(name, body) of every kernel of a source, whatever its length."""
+    import re
+    for m in re.finditer(r"\b__global__\b", text):
+        name = re.compile(r"\b(k_\w+)\s*\(").search(text, m.end())
+        at = text.index("{", text.index(")", name.end()))
+        depth, end = 1, at + 1
+        while depth:
+            depth += {"{": 1, "}": -1}.get(text[end], 0)
+            end += 1
+        yield name.group(1), text[at + 1:end - 1]
+
+
+@pytest.mark.parametrize("name", ["row_lookup.cu", "row_norms_grad.cu", "row_loss.cu", "row_norms.cu"])
+def test_every_kernel_waits_for_the_one_before(name):
+    """Launches may overlap with the kernel before: nothing is read before pdl_enter, the first statement.  Products of the losses set up barriers and tensor memory
+    first, and read nothing of the caller's until then."""
+    import re
+
+    import test_device_rules as D
+    text = D.source(name)
+    found = dict(kernels_of(text))
+    assert len(found) == len(re.findall(r"\b__global__\b", text)) > 0
+    for kernel, body in found.items():
+        if kernel != "k_product":
+            assert re.match(r"\s*pdl_enter\(\);", body), kernel
+            continue
+        outer = [m.start() for m in re.finditer(r"\bpdl_enter\(\);", body) if body[:m.start()].count("{") == body[:m.start()].count("}")]
+        assert len(outer) == 1
+        inner = re.search(r"if \(p\.by_row\) \{\s*pdl_enter\(\);\s*if \(!weights_differ\(p\.control\)\) return;\s*\}", body)
+        before = body[:inner.start()] + body[inner.end():outer[0]]
+        assert not re.search(r"\bp\.(control|raw|raw_labels|bias|labels|sums|at_label|lse|dloss|g|g_sums|out|dead_rows|a|a_clean|b)\b", before)
