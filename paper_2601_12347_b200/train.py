@@ -341,7 +341,7 @@ class ClassHead:
     def step(self, table, ids, labels, kinds=None, dloss=1.0):
         """(loss, gradients): the losses as `loss` gives them, and by parameter the gradient of their sum weighted by dloss (a number, or
         fp32 [len(ids)]).  Rows whose id names no row of the table or whose label no class (-1 by custom) have loss 0 and add nothing to any gradient, whatever the
-        table and dloss hold there; kinds out of range are vertices without a learned row.  The gradient of E has the table's type, the others their parameter's."""
+        table and dloss hold there; kinds out of range are vertices without a learned row.  Gradients have the shape and type of their parameter (E's is summed in fp32)."""
         ids, rows, labels = self._live(table, ids, labels)
         s, n = self._normed(table, ids, kinds)
         loss, lse = loss_rows(n, self.W, labels, self.bias)
@@ -354,7 +354,7 @@ class ClassHead:
         if dnorm_bias is not None:
             got["norm_bias"] = dnorm_bias
         if self.E is not None:
-            got["E"] = lookup_rows_grad(ds, kinds, self.E.shape[0], self.scale)
+            got["E"] = lookup_rows_grad(ds, kinds, self.E.shape[0], self.scale).to(self.E.dtype)
         return loss, got
 
     def request_head(self) -> RequestHead:

@@ -178,3 +178,15 @@ def test_fp16_rows_of_small_weight_keep_their_gradients(rows, K, N, apart):
     near(dx, e @ W64.T * k, (g_tol @ W64.T + (N / 16 + 48) * 2.0 ** -23 * (e.abs() @ W64.T)) * k.abs())
     assert float(((dW.to(F64) - x.to(F64).T @ (e * k)).norm() / dW.to(F64).norm())) < 1e-3
     T.serve.check_requests()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_gradients_have_their_parameters_type(dtype):
+    """What an optimiser of PyTorch asks of them, for a 16-bit head with learned rows on the fp32 cache too."""
+    g = gen(3)
+    head = train.ClassHead(40, 5, kinds=3, dtype=DTYPES[dtype], seed=2)
+    ids = torch.arange(50, dtype=torch.int32, device="cuda")
+    _, grads = head.step(rnd(g, 50, 40), ids, ids % 5, ids % 3)
+    assert set(grads) == set(head.parameters())
+    for k, p in head.parameters().items():
+        p.grad = grads[k]               # (refused where type or shape differ)
