@@ -33,9 +33,10 @@ constexpr int LS_ROWS = 256, LS_KC = 64;
 constexpr int LS_PAIRS = 74;             // of a B200 (for plans that are asked where no device is current, too)
 enum { END_LSE, END_GRAD, END_OUT };
 // Chunks of k whose products share an accumulator, which then is handed over and summed in registers: the tensor core cuts what its additions lose, so sums of
-// terms of one sign come out too small, in proportion to their length (fp16, 100 000 entries: 6.5e-4, more than half a step of the result; here 2.7e-5 of
-// it at most).  fp32: of the large products.  Results in 16 bits: a 16th of half a step of theirs.
-__host__ __device__ constexpr int unit_of(int type, int end) { return type == RIPPLE_TYPE_F32 ? 4 : end != END_OUT ? 32 : type == RIPPLE_TYPE_F16 ? 64 : 512; }
+// terms of one sign come out too small, in proportion to their length (fp16, 100 000 entries: 6.5e-4 of it, more than half a step of the result, bf16 2e-3).  fp32: of the
+// large products.  Results in 16 bits: an eighth of half a step of theirs.  (The epilogue has half the warps then, for the registers: 6001 x 512 x 32 003 in fp16, dx and dW 144 us
+// and 151 in one accumulator, 155 and 161 in pieces of 4096.)
+__host__ __device__ constexpr int unit_of(int type, int end) { return type == RIPPLE_TYPE_F32 ? 4 : end != END_OUT ? 32 : type == RIPPLE_TYPE_F16 ? 128 : 512; }
 constexpr int LS_GROUP = 8;              // tiles of rows that are worked on side by side, so that B's tiles are read out of L2
 constexpr uint32_t LS_SPIN_LIMIT = 1u << 18;       // polls after which a wait gives up: about a second
 constexpr float LOG2E = 1.4426950408889634f;
@@ -63,6 +64,7 @@ constexpr int LS_CONTROL = 512;          // blocks of k_look_at_rows (where few 
 struct RowControl {
     float most[LS_CONTROL], least[LS_CONTROL];      // largest and smallest |dloss| that is finite and not zero (0, infinity: none)
     int32_t odd[LS_CONTROL];             // a row without a label holds something that is not finite
+    int32_t differ;                      // fp16: weights_differ (written by the first product that forms g)
 };
 
 struct alignas(64) ProductParams {
@@ -92,7 +94,8 @@ struct alignas(64) ProductParams {
     int64_t ld_out, split_stride;        // fp32: elements between the splits' results
     int out_f32, add_to_out;
     int unscale;                         // g was scaled: see grad_scale
-    int by_row;                          // fp16, GRAD: runs only where weights_differ, and scales every row by itself; OUT: g was formed so, there
+    int by_row;                          // fp16, GRAD: runs only where weights differ, and scales every row by itself; OUT: g was formed so, there
+    int32_t* differ;                     // fp16, GRAD: where to write whether they do; else null
     const int32_t* dead_rows;            // labels, where rows without one are zeros; else null
     int withhold;                        // diagnostic: no first accumulator counts as filled
 };
@@ -226,8 +229,9 @@ __device__ __forceinline__ float column_sums(float (&v)[32]) {
 // (6001 x 512 x 32 003: 222 us, 0.89 PFLOP/s; exponentials, column sums by shuffles).  fp32 x: hand-overs between the roles, 3500 cycles for 64 entries of k whose products are
 // 1000 and whose operands take 1600 cycles of shared memory (200 000 rows of 256 to 47 classes: 78 us, 2.6 TB/s).  Tried there: 8 warps (79 us), two chunks on their way in
 // registers (93, spills), asynchronous copies into shared memory and two stages (104).
-// fp32: six products of parts (all but those below 2^-24); the large one, of the first parts, is handed over every 256 entries of k and
-// summed in registers, because the tensor core cuts what its additions lose; the small ones gather over the whole tile.
+// fp32: six products of parts.  What they leave out is below 1.5 2^-23 of a term where A's parts are cut on their way (RAW: the third of x by the second of W 2^-23, the second
+// by the third 2^-24; cut parts have x's sign, so that it does not average out), 2^-24 where both have rounded parts.  The large product, of the first parts, is handed over every 256 entries of k and
+// summed in registers, because the tensor core cuts what its additions lose (see unit_of); the small ones gather over the whole tile.
 template <int TYPE, bool A_ACROSS, bool B_ACROSS, int END, bool MANY, bool RAW>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY, RAW>::THREADS, 1) k_product(const __grid_constant__ ProductParams p) {
     using S = LossShape<TYPE, MANY, RAW>;
@@ -239,7 +243,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
     if constexpr (TYPE == RIPPLE_TYPE_F16 && END == END_GRAD) {
         if (p.by_row) {
             pdl_enter();
-            if (!weights_differ(p.control)) return;
+            if (!p.control->differ) return;
         }
     }
     extern __shared__ uint8_t smem_raw[];
@@ -549,7 +553,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
         bool by_row = false;
         if (TYPE == RIPPLE_TYPE_F16 && p.control) {
             if (END == END_GRAD) factor = grad_scale(p.control, p.scale), unfactor = 1.f / factor, by_row = p.by_row;
-            if (END == END_OUT && p.unscale) factor = 1.f / grad_scale(p.control, p.scale), by_row = p.by_row && weights_differ(p.control);
+            if (END == END_GRAD && p.differ && blockIdx.x == 0 && warp == S::FIRST) {
+                const bool differ = weights_differ(p.control);
+                if (lane == 0) *p.differ = differ;
+            }
+            if (END == END_OUT && p.unscale) factor = 1.f / grad_scale(p.control, p.scale), by_row = p.by_row && p.control->differ;
         }
         const uint32_t release = in_leader(&acc_empty[0]);
         bool ok = true;
@@ -650,6 +658,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LossShape<TYPE, MANY
 #pragma unroll
                         for (int e = 0; e < 32; ++e) y[e] = live ? y[e] : 0.f;
                     }
+                    // (16 bits: g is rounded to its operand's type, half a step beside the half step of dx and dW; in parts the products would take three times as long)
                     if (p.g && in_rows) {
                         uint16_t* const to = p.g + (int64_t)row * p.ld_g + col0 + at;
                         if constexpr (PARTS == 1) {
@@ -1232,7 +1241,9 @@ __global__ void __launch_bounds__(FL_THREADS) k_loss_few_weights(const __grid_co
 // Rounds of eight rows on every SM up to which calls of small heads take this form.  Both sides, us on the device for the loss and its gradient, this form / tensor
 // cores.  fp32 602 -> 41: 1184 rows (a round) 9 + 26 / 23 + 58, 3552 rows 21 + 60 / 23 + 61; 256 -> 47: 3552 rows 14 + 34 / 13 + 42; 256 -> 150: 1184 rows
 // 9 + 34 / 14 + 49, 2368 rows 16 + 54 / 15 + 49.  bf16 256 -> 47: 2368 rows 10 + 24 / 9 + 34, 3552 rows 13 + 33 / 9 + 35; 602 -> 41: 1184 rows 9 + 26 / 13 + 30, 2368 rows
-// 14 + 42 / 13 + 33; 64 -> 500: 1184 rows 10 + 29 / 10 + 36, 2368 rows 18 + 48 / 10 + 37.
+// 14 + 42 / 13 + 33; 64 -> 500: 1184 rows 10 + 29 / 10 + 36, 2368 rows 18 + 48 / 10 + 37.  Above 512 classes, one share of k: 64 -> 600, 300 and 1184 rows, fp32 11 + 29 / 10 + 39 and
+// 11 + 40 / 10 + 48, bf16 12 + 31 / 8 + 32 and 12 + 42 / 8 + 34, fp16 12 + 31 / 8 + 39 and 12 + 42 / 8 + 43; 32 -> 1000, fp32 12 + 33 / 10 + 39 and 12 + 38 / 11 + 48, bf16 13 + 34 / 8 + 33 and
+// 13 + 38 / 8 + 37, fp16 13 + 34 / 8 + 41 and 13 + 39 / 8 + 45: bf16 would be 5 to 11 us faster on the tensor cores there.
 constexpr int FL_ROUND = FL_ROWS * 2 * LS_PAIRS;
 static bool few_form(int type, int64_t rows, int k, int n) {
     const int rounds = n > 64 ? 1 : type == RIPPLE_TYPE_F32 ? 3 : k <= 256 ? 2 : 1;
@@ -1497,7 +1508,7 @@ static cudaError_t run_loss_grad(const ripple_loss_rows_grad_args& a) {
         p.ld_g = l.ld_g, p.g_plane = l.g_plane;
         if (a.dx || a.dW) p.g = reinterpret_cast<uint16_t*>(work + l.g);
         if (a.dbias) p.g_sums = reinterpret_cast<float*>(work + l.g_sums);
-        p.control = TYPE == RIPPLE_TYPE_F16 ? control : nullptr;
+        p.control = TYPE == RIPPLE_TYPE_F16 ? control : nullptr, p.differ = TYPE == RIPPLE_TYPE_F16 && c0 == 0 ? &control->differ : nullptr;
         // (rows without labels are zeros in g whatever their logits: x as it is)
         const Matrix* const same = TYPE == RIPPLE_TYPE_F16 ? &x : nullptr;
         e = launch_product<TYPE, false, true, END_GRAD, true>(p, x, same, w, 1, stream);
@@ -1511,6 +1522,16 @@ static cudaError_t run_loss_grad(const ripple_loss_rows_grad_args& a) {
         const Matrix g{work + l.g, a.rows, classes, l.ld_g, l.g_plane, parts_of(TYPE)};
         ProductParams o = {};
         o.unscale = TYPE == RIPPLE_TYPE_F16, o.scale = a.scale, o.classes = a.n;
+        const bool by_row = TYPE == RIPPLE_TYPE_F16 && a.dx && a.dloss;        // dx behind dW then: its g may be another
+        auto form_dx = [&]() {
+            ProductParams d = o;
+            d.m = (int)a.rows, d.n = a.k, d.k = classes, d.b_k0 = c0, d.control = p.control, d.dead_rows = a.labels, d.dloss = a.dloss, d.by_row = by_row;
+            if (l.dx < 0) d.out = a.dx, d.ld_out = a.ld_dx, d.out_f32 = TYPE == RIPPLE_TYPE_F32;
+            else d.out = work + l.dx, d.ld_out = l.ld_dx, d.split_stride = a.rows * l.ld_dx, d.out_f32 = 1, d.add_to_out = c0 > 0;
+            // (the last piece may be too short for all parts: the last of them keep what they have)
+            return launch_product<TYPE, false, false, END_OUT, false>(d, g, &g, w, l.dx_splits, stream);
+        };
+        if (a.dx && !by_row && (e = form_dx()) != cudaSuccess) return e;
         if (a.dW) {
             ProductParams d = o;
             d.m = a.k, d.n = classes, d.k = (int)a.rows, d.raw_labels = a.labels;
@@ -1521,19 +1542,10 @@ static cudaError_t run_loss_grad(const ripple_loss_rows_grad_args& a) {
             if (e == cudaSuccess && l.dw >= 0) e = join_parts<T>(static_cast<const float*>(d.out), l.dw_splits, d.split_stride, d.ld_out, static_cast<T*>(a.dW) + c0, a.ld_dw, a.k, classes, stream);
             if (e != cudaSuccess) return e;
         }
-        if (a.dx) {
-            const bool by_row = TYPE == RIPPLE_TYPE_F16 && a.dloss;
-            if (by_row) {
-                p.by_row = 1, p.g_sums = nullptr;
-                e = launch_product<TYPE, false, true, END_GRAD, true>(p, x, same, w, 1, stream);
-                if (e != cudaSuccess) return e;
-            }
-            ProductParams d = o;
-            d.m = (int)a.rows, d.n = a.k, d.k = classes, d.b_k0 = c0, d.control = p.control, d.dead_rows = a.labels, d.dloss = a.dloss, d.by_row = by_row;
-            if (l.dx < 0) d.out = a.dx, d.ld_out = a.ld_dx, d.out_f32 = TYPE == RIPPLE_TYPE_F32;
-            else d.out = work + l.dx, d.ld_out = l.ld_dx, d.split_stride = a.rows * l.ld_dx, d.out_f32 = 1, d.add_to_out = c0 > 0;
-            // (the last piece may be too short for all parts: the last of them keep what they have)
-            e = launch_product<TYPE, false, false, END_OUT, false>(d, g, &g, w, l.dx_splits, stream);
+        if (by_row) {
+            p.by_row = 1, p.g_sums = nullptr, p.differ = nullptr;
+            e = launch_product<TYPE, false, true, END_GRAD, true>(p, x, same, w, 1, stream);
+            if (e == cudaSuccess) e = form_dx();
             if (e != cudaSuccess) return e;
         }
     }

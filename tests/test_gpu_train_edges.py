@@ -113,8 +113,8 @@ def test_vectors_of_a_norm_that_are_put_in_place_of_others(how):
     assert torch.equal(head.loss(table, ids, labels), other.loss(table, ids, labels))
 
 
-# A step of a 16-bit product (16 entries of k) loses at most 2^-22 of the running sum; an accumulator takes 2048 entries of z, 4096 (fp16) or 32 768 (bf16) of dx and dW.
-LOST = {"fp16": 256 * 2.0 ** -22, "bf16": 2048 * 2.0 ** -22}
+# A step of a 16-bit product (16 entries of k) loses at most 2^-22 of the running sum; an accumulator takes 2048 entries of z, 8192 (fp16) or 32 768 (bf16) of dx and dW.
+LOST = {"fp16": 512 * 2.0 ** -22, "bf16": 2048 * 2.0 ** -22}
 
 
 @pytest.mark.parametrize("dtype", list(LOST))

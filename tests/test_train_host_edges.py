@@ -72,6 +72,6 @@ def test_every_kernel_waits_for_the_one_before(name):
             continue
         outer = [m.start() for m in re.finditer(r"\bpdl_enter\(\);", body) if body[:m.start()].count("{") == body[:m.start()].count("}")]
         assert len(outer) == 1
-        inner = re.search(r"if \(p\.by_row\) \{\s*pdl_enter\(\);\s*if \(!weights_differ\(p\.control\)\) return;\s*\}", body)
+        inner = re.search(r"if \(p\.by_row\) \{\s*pdl_enter\(\);\s*if \(!p\.control->differ\) return;\s*\}", body)
         before = body[:inner.start()] + body[inner.end():outer[0]]
         assert not re.search(r"\bp\.(control|raw|raw_labels|bias|labels|sums|at_label|lse|dloss|g|g_sums|out|dead_rows|a|a_clean|b)\b", before)
