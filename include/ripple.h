@@ -490,7 +490,7 @@ ripple_status ripple_request_status(int32_t device);
  * are out of range).  Results do not depend on timing: sums are formed in a fixed order.  Padding rows (ids or labels outside their
  * range) are written here: zeros, and they add nothing to any gradient, whatever they hold.  Inputs and outputs share no memory, unless said. */
 
-/* out_i = scale * table[ids_i], zeros for ids outside the table.  One rounding. */
+/* out_i = scale * table[ids_i], zeros for ids outside the table.  The product is formed in fp32, then rounded to out's type. */
 typedef struct {
     int64_t rows;
     int32_t width;            /* columns, 1 .. 16384                                                             */
@@ -509,7 +509,7 @@ typedef struct {
 ripple_status ripple_lookup_rows(const ripple_lookup_rows_args* args);
 
 /* Its gradient: out[r] = scale * sum of dy_i over all i with ids_i = r, in the order of i; zeros where there is none.  accumulate: the sum
- * is added to the rows of out that ids name (once for each row, rounded once), and no other row is touched. */
+ * is added to the rows of out that ids name (once for each row, in fp32, then rounded to out's type), and no other row is touched. */
 typedef struct {
     int64_t rows;
     int32_t width;            /* columns, 1 .. 16384                                                             */
@@ -603,7 +603,8 @@ int64_t ripple_loss_rows_workspace_bytes(const ripple_loss_rows_args* args);
 ripple_status ripple_loss_rows(const ripple_loss_rows_args* args);
 
 /* Its gradient: g = dloss_i (softmax(z)_ic - [c = label_i]), dx = g W^T, dW = x^T g, dbias = sum_i g.  g is formed in pieces of the classes; as an
- * operand of the products it has the type's bits (fp16: scaled by a power of two; fp32: three parts), in dbias all of fp32. */
+ * operand of the products it has the type's bits (fp16: scaled by a power of two, of the call or, for dx where weights lie far apart, of the row; fp32: three parts), in
+ * dbias all of fp32.  The workspace holds, of 16-bit x that is read in place, room for a second x: rows without a label that are not finite are cleared in a copy. */
 typedef struct {
     int64_t rows;
     int32_t type;

@@ -32,8 +32,8 @@ constexpr int LK_BLOCK = 256;
 
 constexpr int LK_ROWS = 4;       // rows of a thread that are on their way together
 
-// How rows are scaled.  LK_COPY: not at all.  LK_PAIRS: 16-bit rows by a scale of their own type, two elements per instruction, whose product is rounded once
-// as well.  (300 007 rows of 256 bf16: 48 us by way of fp32, 34 in pairs.)
+// How rows are scaled.  LK_COPY: not at all.  LK_PAIRS: 16-bit rows by a scale of their own type, two elements per instruction, whose product is rounded
+// once.  LK_FLOAT: by way of fp32, rounded there and to the result's type.  (300 007 rows of 256 bf16: 48 us by way of fp32, 34 in pairs.)
 enum { LK_FLOAT, LK_PAIRS, LK_COPY };
 
 template <typename T> __device__ __forceinline__ uint32_t times_pair(uint32_t a, uint32_t b) {

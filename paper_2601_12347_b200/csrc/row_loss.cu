@@ -224,7 +224,7 @@ __device__ __forceinline__ float column_sums(float (&v)[32]) {
 // RAW: sixteen more warps bring A, fetched through registers and split into parts on its way (a pass that writes the parts and one that reads them move 16
 // bytes an entry in place of 4: loss-cached-rows, 78 us for the former alone); a warp in each CTA passes on to full[s] that a stage is made.
 //
-// What bounds it.  16-bit operands: the tensor cores, 82 to 89 % of the time active with plain results and maxima (16 384 x 1024 x 65 536: 1.40 ms, 1.57
+// What bounds it.  16-bit operands: the tensor cores, 85 to 89 % of the time active with plain results and maxima, 77 where sums are handed over (16 384 x 1024 x 65 536: 1.40 ms, 1.57
 // PFLOP/s; dx and dW of it 1.4 to 1.5), over seconds the 1000 W of the card; g of a tile takes its warps longer than products over less than a thousand entries of k
 // (6001 x 512 x 32 003: 222 us, 0.89 PFLOP/s; exponentials, column sums by shuffles).  fp32 x: hand-overs between the roles, 3500 cycles for 64 entries of k whose products are
 // 1000 and whose operands take 1600 cycles of shared memory (200 000 rows of 256 to 47 classes: 78 us, 2.6 TB/s).  Tried there: 8 warps (79 us), two chunks on their way in

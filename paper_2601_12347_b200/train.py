@@ -86,7 +86,7 @@ def _or_null(t) -> int:
 
 
 def lookup_rows(table, ids, scale: float = 1.0, out=None, out_dtype=None):
-    """scale * table[ids], one row per id (int32), zeros for ids outside the table.  The result has the table's type, or the one that
+    """scale * table[ids], one row per id (int32), zeros for ids outside the table; formed in fp32.  The result has the table's type, or the one that
     out_dtype (or out) says if the table is fp32."""
     if getattr(forward_ad, "_current_level", 0) >= 0:
         _refuse_tangents(table=table, out=out)
