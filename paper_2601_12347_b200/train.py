@@ -297,12 +297,12 @@ class ClassHead:
                  device=None, seed: int = 0):
         _type_of(dtype, "dtype")
         device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-        g = torch.Generator(device=device).manual_seed(seed)
-        self.W = (torch.randn(D, N, generator=g, device=device) * D ** -0.5).to(dtype)
-        self.bias = torch.zeros(N, device=device)
+        f32 = dict(dtype=torch.float32, device=device)            # (whatever PyTorch's default type is)
+        self.W = (torch.randn(D, N, generator=torch.Generator(device=device).manual_seed(seed), **f32) * D ** -0.5).to(dtype)
+        self.bias = torch.zeros(N, **f32)
         self.E = torch.zeros(kinds, D, dtype=dtype, device=device) if kinds > 0 else None
         self.scale = float(scale)
-        self.norm = LiveNorm(kind, torch.ones(D, device=device), torch.zeros(D, device=device) if kind == NORM_LAYER else None, eps)
+        self.norm = LiveNorm(kind, torch.ones(D, **f32), torch.zeros(D, **f32) if kind == NORM_LAYER else None, eps)
 
     norm_weight = property(lambda self: self.norm.weight, lambda self, t: setattr(self.norm, "weight", t))
     norm_bias = property(lambda self: self.norm.bias, lambda self, t: setattr(self.norm, "bias", t))

@@ -190,3 +190,16 @@ def test_gradients_have_their_parameters_type(dtype):
     assert set(grads) == set(head.parameters())
     for k, p in head.parameters().items():
         p.grad = grads[k]               # (refused where type or shape differ)
+
+
+def test_a_head_made_under_another_default_type():
+    """A program whose default type is bf16: the head's fp32 parameters are fp32, and drawn like any other's."""
+    want = train.ClassHead(40, 5, seed=2)
+    torch.set_default_dtype(torch.bfloat16)
+    try:
+        head = train.ClassHead(40, 5, seed=2)
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert all(torch.equal(p, want.parameters()[k]) and p.dtype == torch.float32 for k, p in head.parameters().items())
+    ids = torch.arange(50, dtype=torch.int32, device="cuda")
+    head.step(rnd(gen(1), 50, 40), ids, ids % 5)
